@@ -452,6 +452,85 @@ int32_t e2egrec_gate_fusion_backward(const e2egrec_mat *dFused, const e2egrec_ma
                                      const e2egrec_mat *gate, const e2egrec_mat *Wg, const e2egrec_mat *dF, float *dWg,
                                      float *dbg, void *ws, size_t *ws_bytes, void *stream);
 
+/* Attention-based fusion of the ranking model's tokens with the encoder's states (Sec. 4.3.2: softmax attention over stacked
+ * features; Sec. 4.1: the items of a user's input sequence are the source nodes whose embeddings e2egrec_sage_forward and
+ * e2egrec_lightgcn_sampled_forward produce).  Three groups of calls, used one after the other: rotary positions, norms of queries
+ * and keys with the rotation in the same pass, attention of ragged sequences of tokens to ragged sequences of states; each
+ * with its gradient.
+ *
+ * Heads: a matrix of rows x (n_heads * head_dim) holds the heads of a row side by side.  A head starts on a 16-byte boundary
+ * (head_dim * element size a multiple of 16); the matrix may be a column range of a wider one (ld).  head_dim <= 256.
+ * Matrices of one call share one dtype; sums, norms, angles and softmax statistics are fp32 or wider, results are rounded once.
+ *
+ * e2egrec_rotary_frequencies: table of the rotary calls, freqs: device double[rot_dim / 2], radians per position:
+ *   f_i = base^(-2 i / rot_dim) * (k_i + (1 - k_i) / factor),  k_i = clamp((trained_len f_i / 2 pi - low) / (high - low), 0, 1):
+ *   for contexts `factor` times as long as the trained one, pairs that turn less than `low` times over the trained length are
+ *   slowed down, those that turn more than `high` times are not (interpolation by parts); factor = 1: the plain frequencies.
+ *   Any other table of finite doubles may be passed to the calls below.  low < high, factor >= 1, base > 0.
+ * e2egrec_rotary: Y = rows of X with the first rot_dim elements of every head rotated in pairs, (i, i + rot_dim / 2) or with
+ *   E2EGREC_ROTARY_INTERLEAVED (2 i, 2 i + 1), by the angle t = pos[row] f_i:
+ *       y_a = scale (x_a cos t - x_b sin t),  y_b = scale (x_b cos t + x_a sin t);   the rest of the head is copied.
+ *   pos: device int32[rows] (any value; the angle is reduced in 64 bits) or NULL: the row's number.  scale > 0 (the magnitude
+ *   that goes with scaled frequencies; 1 without).  E2EGREC_ROTARY_INVERSE rotates the other way: with it the call maps dY to
+ *   dX (the same scale).  rot_dim even, 0 <= rot_dim <= head_dim; freqs may be NULL where rot_dim is 0.  Y may be X.
+ * e2egrec_qk_norm_rotary_forward: for every head of Q and K (one launch for both)  g_i = w_i x_i / sqrt(mean(x^2) + eps)  and then
+ *   the rotation of e2egrec_rotary.  wq, wk: device float[head_dim], NULL for ones.  K, Kn may be NULL (Q alone).  Qn may be Q, Kn K.
+ * e2egrec_qk_norm_rotary_backward: gradients with respect to Q, K and the gains, from the gradients of Qn, Kn and the forward
+ *   call's inputs (nothing else is kept):  u = inverse rotation of dQn;  dwq = sum over rows and heads of u x / rms (device
+ *   float[head_dim], overwritten; NULL to skip);  dQ = (u w - n mean(u w n)) / rms,  n = x / rms.  dQ may be dQn.  Sums run in a
+ *   fixed order.  ws: scratch, 256-byte aligned (size query with ws == NULL; the same for all sizes). */
+#define E2EGREC_ROTARY_INTERLEAVED 1u
+#define E2EGREC_ROTARY_INVERSE     2u
+int32_t e2egrec_rotary_frequencies(int32_t rot_dim, double base, double factor, double trained_len, double low, double high,
+                                   double *freqs, void *stream);
+int32_t e2egrec_rotary(const e2egrec_mat *X, int32_t n_heads, const double *freqs, int32_t rot_dim, const int32_t *pos, float scale,
+                       uint32_t flags, const e2egrec_mat *Y, void *stream);
+int32_t e2egrec_qk_norm_rotary_forward(const e2egrec_mat *Q, const e2egrec_mat *K, int32_t n_heads, int32_t n_kv_heads, const float *wq,
+                                       const float *wk, float eps, const double *freqs, int32_t rot_dim, const int32_t *pos_q,
+                                       const int32_t *pos_k, float scale, uint32_t flags, const e2egrec_mat *Qn, const e2egrec_mat *Kn,
+                                       void *stream);
+int32_t e2egrec_qk_norm_rotary_backward(const e2egrec_mat *dQn, const e2egrec_mat *dKn, const e2egrec_mat *Q, const e2egrec_mat *K,
+                                        int32_t n_heads, int32_t n_kv_heads, const float *wq, const float *wk, float eps,
+                                        const double *freqs, int32_t rot_dim, const int32_t *pos_q, const int32_t *pos_k, float scale,
+                                        uint32_t flags, const e2egrec_mat *dQ, const e2egrec_mat *dK, float *dwq, float *dwk, void *ws,
+                                        size_t *ws_bytes, void *stream);
+
+/* Packed ragged sequences: sequence s owns rows q_ptr[s] .. q_ptr[s+1]-1 of the queries and k_ptr[s] .. k_ptr[s+1]-1 of the
+ * keys and values.  q_ptr, k_ptr: device int64[n_seq+1], not decreasing, within the matrices' rows; lengths may be 0.
+ * max_q, max_k: the longest of each, as far as the caller knows them (0: unknown); they size the launches, longer sequences are
+ * still right, only slower.  k_mask: NULL or device uint8[rows of K], 0 = hidden from every query (padding, filtered entries). */
+typedef struct e2egrec_sequences {
+    int64_t        n_seq;
+    const int64_t *q_ptr, *k_ptr;
+    int64_t        max_q, max_k;
+    const uint8_t *k_mask;
+} e2egrec_sequences;
+
+/* Attention of every sequence's queries to its keys and values, of another length:  for query row i of sequence s and head h,
+ *     out_ih = sum_j p_ij v_jg,   p_ij = exp(scale q_ih . k_jg - lse_ih),   lse_ih = log sum_j exp(scale q_ih . k_jg)
+ * over the visible keys j of s;  g = h / (n_heads / n_kv_heads) (n_heads a multiple of n_kv_heads: neighbouring query heads share
+ * a key head).  A query that sees no key gets out = 0 and lse = -inf, and passes on no gradient.  What hidden keys and rows outside
+ * the sequences hold (infinities, NaN) has no influence; rows of out, lse and of the gradients outside every sequence are left as
+ * they were.  Q, out: [rows x n_heads head_dim]; K, V: [rows x n_kv_heads head_dim] of one number of rows; scale > 0.
+ *   lse     device float[Q rows x n_heads], row-major; may be NULL (serving: nothing is kept for a backward pass)
+ *   status  optional device int32, receives E2EGREC_DEV_RANGE (or-ed) if offsets decrease or leave the matrices (the rows at fault
+ *           are skipped) and E2EGREC_DEV_TIMEOUT if a wait inside a kernel ran out
+ *   ws      scratch, 256-byte aligned (size query with ws == NULL; goes by the shapes, n_seq, max_q and max_k).  Nothing in it
+ *           has to start at zero and nothing is kept in it; calls that may run at the same time need one each.
+ * e2egrec_cross_attention_backward: gradients dQ, dK, dV for dOut, from the forward call's inputs, out and lse:
+ *     dV_jg = sum_ih p_ij dOut_ih,  dS_ij = p_ij (dOut_ih . v_jg - dOut_ih . out_ih),  dQ_ih = scale sum_j dS_ij k_jg,
+ *     dK_jg = scale sum_ih dS_ij q_ih   (i over the queries of s, h over the query heads of g).
+ * Rows of hidden keys get zeros.  dOut, dQ have Q's shape, dK, dV that of K; none may overlap an input.  No floating-point atomics:
+ * results are the same bits from run to run.  With bf16, p and dS are rounded to bf16 where the products run on the tensor cores.
+ * Every matrix of both calls: heads as above. */
+int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V, const e2egrec_sequences *seqs,
+                                        int32_t n_heads, int32_t n_kv_heads, float scale, const e2egrec_mat *out, float *lse,
+                                        int32_t *status, void *ws, size_t *ws_bytes, void *stream);
+int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V,
+                                         const e2egrec_mat *out, const float *lse, const e2egrec_sequences *seqs, int32_t n_heads,
+                                         int32_t n_kv_heads, float scale, const e2egrec_mat *dQ, const e2egrec_mat *dK,
+                                         const e2egrec_mat *dV, int32_t *status, void *ws, size_t *ws_bytes, void *stream);
+
 /* e2egrec_aggregate_forward without a workspace argument (the paper has no counterpart; this is a
  * packaging variant of the call above: it enqueues the same kernels with the same launch shapes, so its
  * output equals that call's bit for bit).
