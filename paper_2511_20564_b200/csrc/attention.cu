@@ -16,19 +16,6 @@ __device__ inline float warp_sum(float v)
     return v;
 }
 
-// The sequence that owns row `row` of a list of offsets (the last s with ptr[s] <= row), or -1
-__device__ inline int64_t owner(const int64_t *ptr, int64_t n_seq, int64_t row)
-{
-    if (n_seq < 1 || row < ptr[0]) return -1;
-    int64_t lo = 0, hi = n_seq;                      // ptr[lo] <= row < ptr[hi], if the list does not decrease
-    while (hi - lo > 1) {
-        const int64_t m = (lo + hi) >> 1;
-        if (ptr[m] <= row) lo = m;
-        else hi = m;
-    }
-    return row < ptr[lo + 1] ? lo : -1;
-}
-
 // One warp per (query row, head).
 template <typename T, int N>
 __global__ void __launch_bounds__(kRowThreads) attn_row_kernel(const __grid_constant__ AttnArgs a)
@@ -187,6 +174,34 @@ __global__ void __launch_bounds__(kRowThreads) attn_row_dkv_kernel(const __grid_
 
 unsigned row_grid(int64_t rows, int heads) { return (unsigned)ceil_div(rows * heads, kRowThreads / 32); }
 
+// Results of stretches of the keys -> out, lse: one warp per (row, head), stretches in order
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads)
+attn_join_kernel(const __grid_constant__ AttnArgs a, int splits, const float *__restrict__ part_o, const float2 *__restrict__ part_ml)
+{
+    const int lane = threadIdx.x & 31, heads = a.kv_heads * a.group;
+    const int64_t unit = ((int64_t)blockIdx.x * kRowThreads + threadIdx.x) >> 5, stride = a.q_rows * heads;
+    const int64_t row = unit / heads;
+    const int h = (int)(unit % heads);
+    if (row >= a.q_rows || owner(a.q_ptr, a.n_seq, row) < 0) return;
+    float m = -INFINITY, l = 0.f;
+    for (int z = 0; z < splits; ++z) m = fmaxf(m, part_ml[z * stride + unit].x);
+    const float base = m == -INFINITY ? 0.f : m;
+    for (int z = 0; z < splits; ++z) {
+        const float2 p = part_ml[z * stride + unit];
+        l += p.y == 0.f ? 0.f : p.y * exp2f(p.x - base);
+    }
+    for (int e = lane; e < a.head_dim; e += 32) {
+        float o = 0.f;
+        for (int z = 0; z < splits; ++z) {
+            const float2 p = part_ml[z * stride + unit];
+            if (p.y != 0.f) o += p.y * exp2f(p.x - base) * part_o[(z * stride + unit) * a.head_dim + e];
+        }
+        static_cast<T *>(a.out)[row * a.ldo + (int64_t)h * a.head_dim + e] = from_float<T>(l == 0.f ? 0.f : o / l);
+    }
+    if (a.lse && lane == 0) a.lse[unit] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
 template <typename T> void row_forward(const AttnArgs &a, cudaStream_t st)
 {
     note_launch();
@@ -223,6 +238,33 @@ int32_t check_heads(const e2egrec_mat *m, int32_t heads, int32_t head_dim, int32
 
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
 
+// How a forward call is carried out
+struct FwdPlan {
+    bool tc;
+    int64_t tiles;                        // blocks of rows per sequence and key head
+    int splits;                           // stretches of the keys
+    size_t o_bytes, ml_bytes;             // their results
+};
+
+FwdPlan plan_forward(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype)
+{
+    FwdPlan p{};
+    p.splits = 1;
+    p.tc = dtype == E2EGREC_BF16 && a.head_dim <= 128;
+    const int64_t max_q = s.max_q ? std::min(s.max_q, a.q_rows) : a.q_rows, max_k = s.max_k ? std::min(s.max_k, a.k_rows) : a.k_rows;
+    if (p.tc) {
+        const int64_t units = std::max<int64_t>(a.n_seq * a.kv_heads, 1);
+        p.tiles = std::max<int64_t>(1, std::min(ceil_div(max_q * a.group, tc_fwd_rows()), (kMaxRows - 1) / units));
+        const int64_t blocks = units * p.tiles;
+        if (blocks < 148) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({148 / blocks, max_k / 512, 64}));
+    }
+    if (p.splits > 1) {
+        p.ml_bytes = align_up((size_t)p.splits * a.q_rows * a.kv_heads * a.group * sizeof(float2), 256);
+        p.o_bytes = align_up((size_t)p.splits * a.q_rows * a.kv_heads * a.group * a.head_dim * sizeof(float), 256);
+    }
+    return p;
+}
+
 // Arguments that a size query has too; fills the sizes of `a`.
 int32_t check_shape(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_sequences *seqs, int32_t n_heads, int32_t n_kv_heads,
                     float scale, AttnArgs &a)
@@ -231,7 +273,7 @@ int32_t check_shape(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_se
     if (Q->dtype != E2EGREC_F32 && Q->dtype != E2EGREC_BF16) return E2EGREC_ERR_DTYPE;
     if (n_kv_heads < 1 || n_heads < n_kv_heads || n_heads % n_kv_heads || Q->dim < 1 || Q->dim % n_heads) return E2EGREC_ERR_ARG;
     if (Q->rows < 0 || K->rows < 0 || Q->rows >= kMaxRows || K->rows >= kMaxRows) return E2EGREC_ERR_ARG;
-    if (seqs->n_seq < 0 || seqs->n_seq >= kMaxRows || seqs->max_q < 0 || seqs->max_k < 0) return E2EGREC_ERR_ARG;
+    if (seqs->n_seq < 0 || seqs->n_seq > (kMaxRows - 1) / n_kv_heads || seqs->max_q < 0 || seqs->max_k < 0) return E2EGREC_ERR_ARG;
     if (!(scale > 0.f) || !(scale <= 3.0e38f)) return E2EGREC_ERR_ARG;
     if (Q->dim / n_heads > kMaxAttnDim) return E2EGREC_ERR_UNSUPPORTED;
     a.n_seq = seqs->n_seq;
@@ -261,7 +303,8 @@ extern "C" int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e
     AttnArgs a{};
     int32_t rc = check_shape(Q, K, seqs, n_heads, n_kv_heads, scale, a);
     if (rc != E2EGREC_OK) return rc;
-    const size_t need = 256;
+    const FwdPlan plan = plan_forward(a, *seqs, Q->dtype);
+    const size_t need = 256 + plan.o_bytes + plan.ml_bytes;
     if (!ws) { *ws_bytes = need; return E2EGREC_OK; }
     if (*ws_bytes < need) { *ws_bytes = need; return E2EGREC_ERR_WORKSPACE; }
     if (reinterpret_cast<uintptr_t>(ws) % 256) return E2EGREC_ERR_ALIGN;
@@ -279,7 +322,15 @@ extern "C" int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e
     a.lse = lse;
     a.status = status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (Q->dtype == E2EGREC_F32) row_forward<float>(a, st);
+    float2 *part_ml = static_cast<float2 *>(ws);
+    float *part_o = reinterpret_cast<float *>(static_cast<char *>(ws) + plan.ml_bytes);
+    if (plan.tc) {
+        if (!tc_attention_forward(a, plan.tiles, plan.splits, part_o, part_ml, st)) return check_launch("cross_attention_forward");
+        if (plan.splits > 1) {
+            note_launch();
+            attn_join_kernel<__nv_bfloat16><<<row_grid(a.q_rows, n_heads), kRowThreads, 0, st>>>(a, plan.splits, part_o, part_ml);
+        }
+    } else if (Q->dtype == E2EGREC_F32) row_forward<float>(a, st);
     else row_forward<__nv_bfloat16>(a, st);
     return check_launch("cross_attention_forward");
 }

@@ -42,4 +42,23 @@ __device__ inline SeqRange seq_range(const AttnArgs &a, int64_t s, bool report)
     return r;
 }
 
+// The sequence that owns row `row` of a list of offsets (the last s with ptr[s] <= row), or -1
+__device__ inline int64_t owner(const int64_t *ptr, int64_t n_seq, int64_t row)
+{
+    if (n_seq < 1 || row < ptr[0]) return -1;
+    int64_t lo = 0, hi = n_seq;                      // ptr[lo] <= row < ptr[hi], if the list does not decrease
+    while (hi - lo > 1) {
+        const int64_t m = (lo + hi) >> 1;
+        if (ptr[m] <= row) lo = m;
+        else hi = m;
+    }
+    return row < ptr[lo + 1] ? lo : -1;
+}
+
+// attention_tc.cu: bf16, head_dim <= 128.  tiles: blocks of tc_fwd_rows() rows per sequence and key head (longer sequences go
+// round again); splits: stretches of the keys, whose results (out in fp32 and (maximum in powers of two, sum)) go to
+// part_o [splits x q_rows x heads x head_dim] and part_ml [splits x q_rows x heads] where splits > 1.
+int tc_fwd_rows();
+bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, float *part_o, float2 *part_ml, cudaStream_t st);
+
 }  // namespace e2egrec

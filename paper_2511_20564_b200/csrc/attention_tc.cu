@@ -1,0 +1,432 @@
+// Attention of ragged sequences on the 5th-generation tensor cores (tcgen05): bf16, head_dim <= 128.
+//
+// The rows of a product are the (query, head of the group) pairs of one key head of one sequence; tiles are 128 x 128.  Every
+// operand tile lies in shared memory as blocks of 64 columns, 128 lines of 128 bytes each, 128-byte swizzled: the same bytes serve
+// as an operand whose K index is contiguous (Q, K, V, dO against head_dim) and as one whose N index is (V, K, Q, dO against rows).
+// Tiles are copied by cp.async, 16 bytes per lane, each warp a quarter of the rows: rows behind a sequence's end and hidden keys are
+// filled with zeros without being read, which a box of a tensor map cannot do, and any offset, stride and head width
+// goes.  Scores and gradients of scores go back to the tensor cores through tensor memory (A operand), never through shared memory.
+// Every wait is bounded; when one runs out the block reports E2EGREC_DEV_TIMEOUT, lets its copies land, frees its tensor memory
+// and returns.
+#include <algorithm>
+
+#include "attention.cuh"
+#include "tcgen05.cuh"
+
+namespace e2egrec {
+namespace {
+
+using bf16 = __nv_bfloat16;
+
+constexpr int kTile = 128;
+constexpr int kBlockBytes = kTile * 128;             // 64 columns of 128 rows
+constexpr int kWordRing = 8;                         // tiles whose visibility words are kept
+
+__device__ inline float exp2_approx(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+__device__ inline uint32_t pack_bf16(float lo, float hi)
+{
+    __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<uint32_t *>(&h);
+}
+
+// 32 columns of the warp's lanes without waiting for them (tmem_load_wait)
+__device__ inline void tmem_load32_async(uint32_t taddr, uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr));
+}
+
+// The 32 rows of one loading warp -> shared memory.  src: the lane's own row (its first element of the head), null for zeros;
+// chunks: 16-byte chunks per row that the products read, of which `real` exist; any: an address that may be named where nothing is read.
+__device__ inline void load_rows(uint32_t tile, int warp_row, const bf16 *src, const void *any, int chunks, int real, int lane)
+{
+    int row = lane / chunks, ch = lane - row * chunks;
+    const int dr = 32 / chunks, dc = 32 - dr * chunks;
+    const uint64_t mine = reinterpret_cast<uint64_t>(src);
+    for (int i = 0; i < chunks; ++i) {
+        const uint64_t p = __shfl_sync(0xFFFFFFFFu, mine, row);
+        const int r = warp_row + row;
+        const uint32_t dst = tile + (uint32_t)(ch >> 3) * kBlockBytes + (uint32_t)r * 128u + (uint32_t)(((ch & 7) ^ (r & 7)) << 4);
+        const bool on = p != 0 && ch < real;
+        cp_async16(dst, on ? reinterpret_cast<const bf16 *>(p) + ch * 8 : any, on);
+        row += dr;
+        ch += dc;
+        if (ch >= chunks) { ch -= chunks; ++row; }
+    }
+}
+
+// Copies that a loading warp has started and not yet announced: the barrier of a tile is arrived at once the warp's copies for
+// it have landed and are visible to the tensor cores; up to three tiles stay under way.
+struct Pending {
+    uint64_t *bar[3] = {nullptr, nullptr, nullptr};
+    __device__ void announce(uint64_t *b, int lane)
+    {
+        if (!b) return;
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) mbar_arrive(b);
+    }
+    __device__ void push(uint64_t *b, int lane)
+    {
+        cp_async_commit();
+        if (bar[2]) {
+            cp_async_wait<3>();
+            announce(bar[2], lane);
+        }
+        bar[2] = bar[1];
+        bar[1] = bar[0];
+        bar[0] = b;
+    }
+    __device__ void flush(int lane)
+    {
+        cp_async_wait<0>();
+        for (int i = 2; i >= 0; --i) {
+            announce(bar[i], lane);
+            bar[i] = nullptr;
+        }
+    }
+};
+
+__device__ inline bool mbar_test(uint64_t *bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
+                 : "=r"(done)
+                 : "r"(smem_u32(bar)), "r"(parity)
+                 : "memory");
+    return done != 0;
+}
+
+// A slot of a ring that the tensor cores may still read: what is under way is announced before the warp waits for it
+__device__ inline bool wait_slot(uint64_t *bar, uint32_t parity, Pending &pend, int lane, volatile int *abort_flag)
+{
+    if (__all_sync(0xFFFFFFFFu, mbar_test(bar, parity))) return true;
+    pend.flush(lane);
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag));
+}
+
+// ------------------------------------------------------------------------------------------------- forward
+constexpr int kFwdThreads = 13 * 32;                 // two warpgroups of softmax, four loading warps, the products' warp
+constexpr int kFwdRows = 2 * kTile;                  // rows of a block: one tile per softmax warpgroup
+
+template <int NB> constexpr int fwd_stages() { return NB == 2 ? 5 : 8; }
+template <int NB> constexpr size_t fwd_smem() { return 1024 + (size_t)(2 + fwd_stages<NB>()) * NB * kBlockBytes; }
+
+template <int NB>
+__global__ void __launch_bounds__(kFwdThreads, 1)
+attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, float *__restrict__ part_o, float2 *__restrict__ part_ml)
+{
+    constexpr int kStages = NB == 2 ? 5 : 8, kTileBytes = NB * kBlockBytes;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], q_full, q_empty, s_full[2], p_full[2], o_full[2], o_empty[2];
+    __shared__ uint32_t words[kWordRing][4];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int64_t u = blockIdx.x;
+    const int z = (int)(u % splits);
+    u /= splits;
+    const int t0 = (int)(u % tiles);
+    u /= tiles;
+    const int h = (int)(u % a.kv_heads);
+    const SeqRange rg = seq_range(a, u / a.kv_heads, z == 0 && t0 == 0 && h == 0 && threadIdx.x == 0);
+    const int64_t rows = (rg.q1 - rg.q0) * a.group;
+    if ((int64_t)t0 * kFwdRows >= rows) return;
+    const int64_t klen = rg.k1 - rg.k0;
+    const int64_t per = ceil_div(ceil_div(klen, splits), kTile) * kTile;
+    const int64_t kb = min(rg.k0 + z * per, rg.k1), ke = min(kb + per, rg.k1);
+    const int n = (int)ceil_div(ke - kb, kTile);
+
+    uint8_t *tiles_smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const uint32_t q_smem = smem_u32(tiles_smem), kv_smem = q_smem + 2 * kTileBytes;
+    const int ksteps = (a.head_dim + 15) / 16;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&kv_full[s], 4);
+            mbar_init(&kv_empty[s], 1);
+        }
+        mbar_init(&q_full, 4);
+        mbar_init(&q_empty, 1);
+        for (int t = 0; t < 2; ++t) {
+            mbar_init(&s_full[t], 1);
+            mbar_init(&p_full[t], 4);
+            mbar_init(&o_full[t], 1);
+            mbar_init(&o_empty[t], 4);
+        }
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;                  // scores (and p) of tile t: columns 128 t; outputs: 256 + 64 NB t
+
+    if (warp >= 8 && warp < 12) {
+        // ---- copies: queries of a block of rows, then keys and values in turn
+        const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8;
+        Pending pend;
+        uint32_t g = 0, jj = 0, item = 0;
+        bool ok = true;
+        for (int64_t t = t0; t * kFwdRows < rows && n > 0 && ok; t += tiles, ++item) {
+            if (item > 0) ok = wait_slot(&q_empty, (item - 1) & 1u, pend, lane, &abort_flag);
+            if (!ok) break;
+            for (int q = 0; q < 2; ++q) {
+                const int64_t r = t * kFwdRows + q * kTile + w * 32 + lane;
+                const bf16 *src = nullptr;
+                if (r < rows) {
+                    const int64_t i = r / a.group;
+                    src = static_cast<const bf16 *>(a.q) + (rg.q0 + i) * a.ldq + (h * a.group + (int)(r - i * a.group)) * (int64_t)a.head_dim;
+                }
+                load_rows(q_smem + q * kTileBytes, w * 32, src, a.q, chunks, real, lane);
+            }
+            pend.push(&q_full, lane);
+            for (int j = 0; j < n && ok; ++j, ++jj) {
+                const int64_t key = kb + (int64_t)j * kTile + w * 32 + lane;
+                const bool seen = key < ke && (!a.mask || a.mask[key]);
+                const uint32_t word = __ballot_sync(0xFFFFFFFFu, seen);
+                for (int v = 0; v < 2; ++v, ++g) {
+                    const uint32_t s = g % kStages;
+                    if (g >= kStages) ok = wait_slot(&kv_empty[s], (g / kStages - 1) & 1u, pend, lane, &abort_flag);
+                    if (!ok) break;
+                    if (v == 0 && lane == 0) words[jj % kWordRing][w] = word;
+                    const bf16 *src = static_cast<const bf16 *>(v ? a.v : a.k) + key * (v ? a.ldv : a.ldk) + h * (int64_t)a.head_dim;
+                    load_rows(kv_smem + s * kTileBytes, w * 32, seen ? src : nullptr, a.q, chunks, real, lane);
+                    pend.push(&kv_full[s], lane);
+                }
+            }
+        }
+        pend.flush(lane);
+    } else if (warp == 12) {
+        // ---- products
+        if (lane == 0) {
+            const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
+            uint32_t g = 0, item = 0, pc[2] = {0, 0};
+            bool ok = true;
+            for (int64_t t = t0; t * kFwdRows < rows && n > 0 && ok; t += tiles, ++item) {
+                const int nt = rows - t * kFwdRows > kTile ? 2 : 1;
+                ok = mbar_wait(&q_full, item & 1u, &abort_flag);
+                if (item > 0)
+                    for (int q = 0; q < nt && ok; ++q) ok = mbar_wait(&o_empty[q], (item - 1) & 1u, &abort_flag);
+                auto scores = [&](uint32_t gk, int q) {
+                    const uint32_t k_addr = kv_smem + (gk % kStages) * kTileBytes, q_addr = q_smem + q * kTileBytes;
+                    for (int k = 0; k < ksteps; ++k) {
+                        const uint32_t off = (uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32;
+                        umma(tmem + q * kTile, make_smem_desc(q_addr + off), make_smem_desc(k_addr + off), id_s, k > 0);
+                    }
+                    umma_commit(&s_full[q]);
+                };
+                if (ok) ok = mbar_wait(&kv_full[g % kStages], (g / kStages) & 1u, &abort_flag);
+                tc_fence_after();
+                if (ok) {
+                    for (int q = 0; q < nt; ++q) scores(g, q);
+                    umma_commit(&kv_empty[g % kStages]);
+                }
+                for (int j = 0; j < n && ok; ++j, g += 2) {
+                    const uint32_t gv = g + 1, gk = g + 2;
+                    const uint32_t v_addr = kv_smem + (gv % kStages) * kTileBytes;
+                    ok = mbar_wait(&kv_full[gv % kStages], (gv / kStages) & 1u, &abort_flag);
+                    for (int q = 0; q < nt && ok; ++q) {
+                        ok = mbar_wait(&p_full[q], pc[q]++ & 1u, &abort_flag);
+                        if (!ok) break;
+                        tc_fence_after();
+                        for (int k = 0; k < kTile / 16; ++k)
+                            umma_ts(tmem + 256 + q * 64 * NB, tmem + q * kTile + k * 8, make_smem_desc_mn(v_addr + k * 2048, kBlockBytes), id_o,
+                                    (j | k) != 0);
+                        if (j + 1 < n) {
+                            if (q == 0) {
+                                ok = mbar_wait(&kv_full[gk % kStages], (gk / kStages) & 1u, &abort_flag);
+                                if (!ok) break;
+                                tc_fence_after();
+                            }
+                            if (q == nt - 1) umma_commit(&kv_empty[gv % kStages]);
+                            scores(gk, q);
+                            if (q == nt - 1) umma_commit(&kv_empty[gk % kStages]);
+                        } else {
+                            umma_commit(&o_full[q]);
+                            if (q == nt - 1) {
+                                umma_commit(&kv_empty[gv % kStages]);
+                                umma_commit(&q_empty);
+                            }
+                        }
+                    }
+                }
+            }
+        }
+    } else {
+        // ---- softmax of tile `q`, one row per thread
+        const int q = warp >> 2, w = warp & 3;
+        const uint32_t lanes = (uint32_t)(w * 32) << 16;
+        const uint32_t s_addr = tmem + lanes + q * kTile, o_addr = tmem + lanes + 256 + q * 64 * NB;
+        const float c1 = a.scale * kLog2e;
+        const int heads = a.kv_heads * a.group;
+        uint32_t jj = 0, item = 0, sc = 0, oc = 0;
+        bool ok = true;
+        for (int64_t t = t0; t * kFwdRows < rows && ok; t += tiles, ++item) {
+            const int64_t r = t * kFwdRows + q * kTile + w * 32 + lane;
+            const bool active = rows - t * kFwdRows > q * kTile;
+            float m = -INFINITY, l = 0.f;
+            if (!active) jj += n;
+            for (int j = 0; j < n && active; ++j, ++jj) {
+                ok = mbar_wait(&s_full[q], sc++ & 1u, &abort_flag);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                tc_fence_after();
+                uint32_t word[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) word[c] = words[jj % kWordRing][c];
+                float top = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t v[32];
+                    tmem_load32_async(s_addr + c * 32, v);
+                    tmem_load_wait();
+                    if (word[c] != 0xFFFFFFFFu) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!((word[c] >> i) & 1u)) v[i] = 0xFF800000u;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[i]));
+                }
+                // The maximum that p and l refer to moves only where a score exceeds it by 8 in the exponent: p <= 2^8 loses
+                // nothing in floating point, and the sums so far are rescaled seldom.
+                const bool moves = top * c1 > m * c1 + 8.f || m == -INFINITY;
+                if (j > 0 && __any_sync(0xFFFFFFFFu, moves && top != -INFINITY)) {
+                    const float f = moves && top != -INFINITY ? exp2_approx((m - top) * c1) : 1.f;
+                    l *= f;
+                    for (int c = 0; c < NB * 2; ++c) {
+                        uint32_t v[32];
+                        tmem_load32_async(o_addr + c * 32, v);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
+                        tmem_store32(o_addr + c * 32, v);
+                    }
+                }
+                if (moves) m = top;
+                const float base = m == -INFINITY ? 0.f : m * c1;
+                float sum = 0.f;
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t v[32], p[16];
+                    tmem_load32_async(s_addr + c * 32, v);
+                    tmem_load_wait();
+                    if (word[c] != 0xFFFFFFFFu) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!((word[c] >> i) & 1u)) v[i] = 0xFF800000u;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 32; i += 2) {
+                        const float x = exp2_approx(fmaf(__uint_as_float(v[i]), c1, -base)), y = exp2_approx(fmaf(__uint_as_float(v[i + 1]), c1, -base));
+                        sum += x + y;
+                        p[i / 2] = pack_bf16(x, y);
+                    }
+                    tmem_store16(s_addr + c * 16, p);
+                }
+                l += sum;
+                tmem_store_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full[q]);
+            }
+            if (!ok) break;
+            if (active && n > 0) {
+                ok = mbar_wait(&o_full[q], oc++ & 1u, &abort_flag);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                tc_fence_after();
+            }
+            const int64_t i = r / a.group;
+            const int head = h * a.group + (int)(r - i * a.group);
+            const int64_t row = rg.q0 + i;
+            const bool live = r < rows;
+            const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
+            if (active)
+                for (int c = 0; c < NB * 2; ++c) {
+                    uint32_t v[32];
+                    if (n > 0) {
+                        tmem_load32_async(o_addr + c * 32, v);
+                        tmem_load_wait();
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) v[e] = n > 0 && l != 0.f ? __float_as_uint(__uint_as_float(v[e]) * inv) : 0u;
+                    if (live && splits == 1) {
+                        bf16 *out = static_cast<bf16 *>(a.out) + row * a.ldo + (int64_t)head * a.head_dim + c * 32;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (c * 32 + e * 8 < a.head_dim) {
+                                uint32_t p[4];
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) p[k] = pack_bf16(__uint_as_float(v[e * 8 + 2 * k]), __uint_as_float(v[e * 8 + 2 * k + 1]));
+                                *reinterpret_cast<uint4 *>(out + e * 8) = make_uint4(p[0], p[1], p[2], p[3]);
+                            }
+                    } else if (live) {
+                        float *out = part_o + (((int64_t)z * a.q_rows + row) * heads + head) * a.head_dim + c * 32;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            if (c * 32 + e * 4 < a.head_dim) *reinterpret_cast<uint4 *>(out + e * 4) = make_uint4(v[e * 4], v[e * 4 + 1], v[e * 4 + 2], v[e * 4 + 3]);
+                    }
+                }
+            if (live && active) {
+                if (splits > 1) part_ml[((int64_t)z * a.q_rows + row) * heads + head] = make_float2(l == 0.f ? -INFINITY : m * c1, l);
+                else if (a.lse) a.lse[row * heads + head] = l == 0.f ? -INFINITY : (m * c1 + log2f(l)) * kLn2;
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0 && n > 0 && active) mbar_arrive(&o_empty[q]);      // only the last block of rows may lack the second tile
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && abort_flag && a.status) atomicOr(reinterpret_cast<unsigned *>(a.status), E2EGREC_DEV_TIMEOUT);
+    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+constexpr int kMaxDevices = 64;
+template <typename Kernel> bool allow_smem(Kernel kernel, size_t bytes, bool (&done)[kMaxDevices])
+{
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return false;
+    if (done[dev]) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != cudaSuccess) return false;
+    done[dev] = true;
+    return true;
+}
+
+}  // namespace
+
+int tc_fwd_rows() { return kFwdRows; }
+
+bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, float *part_o, float2 *part_ml, cudaStream_t st)
+{
+    static bool done[2][kMaxDevices] = {};
+    const bool one = a.head_dim <= 64;
+    if (!(one ? allow_smem(attn_tc_fwd_kernel<1>, fwd_smem<1>(), done[0]) : allow_smem(attn_tc_fwd_kernel<2>, fwd_smem<2>(), done[1]))) return false;
+    const unsigned grid = (unsigned)(a.n_seq * a.kv_heads * tiles * splits);
+    note_launch();
+    if (one) attn_tc_fwd_kernel<1><<<grid, kFwdThreads, fwd_smem<1>(), st>>>(a, (int)tiles, splits, part_o, part_ml);
+    else attn_tc_fwd_kernel<2><<<grid, kFwdThreads, fwd_smem<2>(), st>>>(a, (int)tiles, splits, part_o, part_ml);
+    return true;
+}
+
+}  // namespace e2egrec

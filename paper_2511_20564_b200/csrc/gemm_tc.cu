@@ -12,6 +12,7 @@
 // No cluster launch, no multicast.  Every mbarrier wait is bounded; on a timeout the CTA raises E2EGREC_DEV_TIMEOUT in
 // the status word, skips its remaining tiles, releases its tensor memory and returns.
 #include "gemm_tc.cuh"
+#include "tcgen05.cuh"
 
 #include <cuda.h>
 
@@ -29,150 +30,6 @@ constexpr int kTnEpilogueWarps = 8;          // tc_gemm_tn_kernel: TMA warp, MMA
 constexpr int kTnThreads = (2 + kTnEpilogueWarps) * 32;
 constexpr int kMaxStages = 4;
 constexpr int kMinSplitBlocks = 8;          // k-blocks of 64 rows per split of the weight-gradient product
-constexpr uint32_t kSpinLimit = 4u * 1000u * 1000u;
-
-// ------------------------------------------------------------------------- PTX wrappers
-__device__ inline uint32_t smem_u32(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-
-__device__ inline void mbar_init(uint64_t *bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(count));
-}
-
-__device__ inline void mbar_expect_tx(uint64_t *bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
-}
-
-// Bounded wait for the phase with the given parity; false when the limit ran out or another
-// thread of the CTA has already given up.
-__device__ inline bool mbar_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
-{
-    const uint32_t addr = smem_u32(bar);
-    for (uint32_t it = 0; it < kSpinLimit; ++it) {
-        uint32_t done;
-        asm volatile(
-            "{\n"
-            ".reg .pred p;\n"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-            "selp.u32 %0, 1, 0, p;\n"
-            "}\n"
-            : "=r"(done)
-            : "r"(addr), "r"(parity)
-            : "memory");
-        if (done) return true;
-        if ((it & 1023u) == 1023u && *abort_flag) return false;
-    }
-    *abort_flag = 1;
-    return false;
-}
-
-__device__ inline void tma_load_2d(void *smem_dst, const CUtensorMap *map, int x, int y, uint64_t *bar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-        ::"r"(smem_u32(smem_dst)), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(smem_u32(bar))
-        : "memory");
-}
-
-// Bulk tensor store shared -> global of one box, and the bookkeeping of such stores (issued and awaited by one thread).
-__device__ inline void tma_store_2d(const CUtensorMap *map, const void *smem_src, int x, int y)
-{
-    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<uint64_t>(map)),
-                 "r"(x), "r"(y), "r"(smem_u32(smem_src))
-                 : "memory");
-}
-__device__ inline void tma_store_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-template <int N> __device__ inline void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
-__device__ inline void named_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
-// barrier over `threads` threads that also tells every one of them whether all arrived with ok set
-__device__ inline bool named_barrier_all(int id, int threads, bool ok)
-{
-    uint32_t r;
-    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\tbar.red.and.pred p, %2, %3, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(r)
-                 : "r"((uint32_t)ok), "r"(id), "r"(threads)
-                 : "memory");
-    return r != 0;
-}
-
-__device__ inline void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ inline void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-// Shared-memory operand descriptor: K-major tile of 128-byte rows, 128-byte swizzle.  Eight rows
-// form one 1024-byte swizzle atom, so the stride between 8-row groups is 1024 bytes; the leading
-// byte offset is not used for this layout.
-__device__ inline uint64_t make_smem_desc(uint32_t smem_addr)
-{
-    uint64_t d = 0;
-    d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);        // start address, 16-byte units
-    d |= (uint64_t)1 << 16;                               // leading byte offset (ignored, canonical 1)
-    d |= (uint64_t)(1024 >> 4) << 32;                     // stride byte offset
-    d |= (uint64_t)1 << 46;                               // descriptor version of sm_100
-    d |= (uint64_t)2 << 61;                               // 128-byte swizzle
-    return d;
-}
-
-// Shared-memory operand descriptor for an operand whose M (or N) index is the contiguous one: the tile is
-// a row of 64-element (128-byte) wide column blocks, each block holding one 128-byte line per K index,
-// 128-byte swizzled in groups of eight lines.  Leading byte offset = distance between column blocks,
-// stride byte offset = distance between groups of eight K lines.
-__device__ inline uint64_t make_smem_desc_mn(uint32_t smem_addr, uint32_t block_bytes)
-{
-    uint64_t d = 0;
-    d |= (uint64_t)((smem_addr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)((block_bytes >> 4) & 0x3FFFu) << 16;
-    d |= (uint64_t)(1024 >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)2 << 61;
-    return d;
-}
-
-// Instruction descriptor of kind::f16: bf16 x bf16 -> fp32; a_mn_major / b_mn_major = that operand has its M / N
-// index contiguous in memory, else it is K-major.
-__device__ inline uint32_t make_idesc(int m, int n, bool a_mn_major = false, bool b_mn_major = false)
-{
-    uint32_t d = 0;
-    if (a_mn_major) d |= 1u << 15;
-    if (b_mn_major) d |= 1u << 16;
-    d |= 1u << 4;                    // accumulator fp32
-    d |= 1u << 7;                    // A bf16
-    d |= 1u << 10;                   // B bf16
-    d |= (uint32_t)(n >> 3) << 17;
-    d |= (uint32_t)(m >> 4) << 24;
-    return d;
-}
-
-__device__ inline void umma(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
-{
-    asm volatile(
-        "{\n"
-        ".reg .pred p;\n"
-        "setp.ne.b32 p, %4, 0;\n"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
-        "}\n" ::"r"(tmem_d), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
-        : "memory");
-}
-
-__device__ inline void umma_commit(uint64_t *bar)
-{
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(bar))
-                 : "memory");
-}
-
-__device__ inline void tmem_load32(uint32_t taddr, uint32_t (&r)[32])
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
 
 struct TcEpilogue {
     __nv_bfloat16 *out;        // [rows x ldo]
@@ -262,11 +119,6 @@ __device__ inline float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0
 // issues the MMAs into one of two accumulator buffers in tensor memory, warps 2-9 run the epilogue of the
 // previous tile from the other buffer meanwhile (two warps per group of 32 accumulator lanes, each taking
 // every other block of 32 columns).
-__device__ inline void mbar_arrive(uint64_t *bar)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-
 // What the plain epilogue knows about its row of the current tile.
 struct EpiRow {
     const TcEpilogue *ep;
