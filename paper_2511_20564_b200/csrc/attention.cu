@@ -265,6 +265,26 @@ FwdPlan plan_forward(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtyp
     return p;
 }
 
+struct BwdPlan {
+    bool tc;
+    int64_t q_tiles, k_tiles;
+    size_t dot_bytes;
+};
+
+BwdPlan plan_backward(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype)
+{
+    BwdPlan p{};
+    p.tc = dtype == E2EGREC_BF16 && a.head_dim <= 128;
+    const int64_t max_q = s.max_q ? std::min(s.max_q, a.q_rows) : a.q_rows, max_k = s.max_k ? std::min(s.max_k, a.k_rows) : a.k_rows;
+    if (p.tc) {
+        const int64_t most = (kMaxRows - 1) / std::max<int64_t>(a.n_seq * a.kv_heads, 1);
+        p.q_tiles = std::max<int64_t>(1, std::min(ceil_div(max_q * a.group, 128), most));
+        p.k_tiles = std::max<int64_t>(1, std::min(ceil_div(max_k, 128), most));
+        p.dot_bytes = align_up((size_t)a.q_rows * a.kv_heads * a.group * sizeof(float), 256);
+    }
+    return p;
+}
+
 // Arguments that a size query has too; fills the sizes of `a`.
 int32_t check_shape(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_sequences *seqs, int32_t n_heads, int32_t n_kv_heads,
                     float scale, AttnArgs &a)
@@ -345,7 +365,8 @@ extern "C" int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, con
     AttnArgs a{};
     int32_t rc = check_shape(Q, K, seqs, n_heads, n_kv_heads, scale, a);
     if (rc != E2EGREC_OK) return rc;
-    const size_t need = 256;
+    const BwdPlan plan = plan_backward(a, *seqs, Q->dtype);
+    const size_t need = 256 + plan.dot_bytes;
     if (!ws) { *ws_bytes = need; return E2EGREC_OK; }
     if (*ws_bytes < need) { *ws_bytes = need; return E2EGREC_ERR_WORKSPACE; }
     if (reinterpret_cast<uintptr_t>(ws) % 256) return E2EGREC_ERR_ALIGN;
@@ -371,7 +392,9 @@ extern "C" int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, con
     a.lse = const_cast<float *>(lse);
     a.status = status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (Q->dtype == E2EGREC_F32) row_backward<float>(a, st);
+    if (plan.tc) {
+        if (!tc_attention_backward(a, plan.q_tiles, plan.k_tiles, static_cast<float *>(ws), st)) return check_launch("cross_attention_backward");
+    } else if (Q->dtype == E2EGREC_F32) row_backward<float>(a, st);
     else row_backward<__nv_bfloat16>(a, st);
     return check_launch("cross_attention_backward");
 }

@@ -60,5 +60,7 @@ __device__ inline int64_t owner(const int64_t *ptr, int64_t n_seq, int64_t row)
 // part_o [splits x q_rows x heads x head_dim] and part_ml [splits x q_rows x heads] where splits > 1.
 int tc_fwd_rows();
 bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, float *part_o, float2 *part_ml, cudaStream_t st);
+// q_tiles, k_tiles: tiles of 128 rows and of 128 keys per sequence and key head; dots: [q_rows x heads] scratch
+bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st);
 
 }  // namespace e2egrec

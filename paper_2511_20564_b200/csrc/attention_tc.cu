@@ -402,6 +402,500 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
     if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
+// ------------------------------------------------------------------------------------------------- backward
+// Two kernels, so that no gradient is added up by atomics: dQ goes over the keys of a tile of rows, dK and dV over the rows of a
+// tile of keys; the scores are formed in both.  Two warpgroups share a tile of 128 x 128: 64 columns each, one row per thread.
+constexpr int kBwdThreads = 13 * 32;
+
+template <int NB> constexpr size_t dq_smem() { return 1024 + (size_t)(2 + fwd_stages<NB>()) * NB * kBlockBytes; }
+template <int NB> constexpr size_t dkv_smem() { return 1024 + (size_t)(2 + 4) * NB * kBlockBytes; }
+
+// 64 columns of p or dS of a thread's row as an operand in tensor memory: 32 packed columns
+__device__ inline void store_operand(uint32_t taddr, const float (&v)[64])
+{
+    uint32_t r[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) r[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+    tmem_store32(taddr, r);
+}
+// its place for the products: K step k of 16 (the second warpgroup's half begins 64 columns behind the first's)
+__device__ inline uint32_t operand_step(uint32_t base, int k) { return base + (uint32_t)(k >> 2) * 64u + (uint32_t)(k & 3) * 8u; }
+
+// One row (up to 64 NB columns) of an accumulator -> out, times f; zeros where !keep
+template <int NB>
+__device__ inline void store_row(uint32_t taddr, bf16 *out, int head_dim, float f, bool have, bool keep, bool write)
+{
+    for (int c = 0; c < NB * 2; ++c) {
+        uint32_t v[32];
+        if (have) {
+            tmem_load32_async(taddr + c * 32, v);
+            tmem_load_wait();
+        }
+        if (!write) continue;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (c * 32 + e * 8 < head_dim) {
+                uint32_t p[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    p[k] = have && keep ? pack_bf16(__uint_as_float(v[e * 8 + 2 * k]) * f, __uint_as_float(v[e * 8 + 2 * k + 1]) * f) : 0u;
+                *reinterpret_cast<uint4 *>(out + c * 32 + e * 8) = make_uint4(p[0], p[1], p[2], p[3]);
+            }
+    }
+}
+
+// dQ, and D = dO . out of every row for the other kernel
+template <int NB>
+__global__ void __launch_bounds__(kBwdThreads, 1)
+attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restrict__ dots)
+{
+    constexpr int kStages = NB == 2 ? 5 : 8, kTileBytes = NB * kBlockBytes;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], q_full, q_empty, s_full[2], dp_full, ds_full, o_full, o_empty;
+    __shared__ uint32_t words[kWordRing][4];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int64_t u = blockIdx.x;
+    const int t0 = (int)(u % tiles);
+    u /= tiles;
+    const int h = (int)(u % a.kv_heads);
+    const SeqRange rg = seq_range(a, u / a.kv_heads, t0 == 0 && h == 0 && threadIdx.x == 0);
+    const int64_t rows = (rg.q1 - rg.q0) * a.group;
+    if ((int64_t)t0 * kTile >= rows) return;
+    const int n = (int)ceil_div(rg.k1 - rg.k0, kTile);
+
+    uint8_t *tiles_smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const uint32_t q_smem = smem_u32(tiles_smem), g_smem = q_smem + kTileBytes, kv_smem = q_smem + 2 * kTileBytes;
+    const int ksteps = (a.head_dim + 15) / 16;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&kv_full[s], 4);
+            mbar_init(&kv_empty[s], 1);
+        }
+        mbar_init(&q_full, 4);
+        mbar_init(&q_empty, 1);
+        mbar_init(&s_full[0], 1);
+        mbar_init(&s_full[1], 1);
+        mbar_init(&dp_full, 1);
+        mbar_init(&ds_full, 8);
+        mbar_init(&o_full, 1);
+        mbar_init(&o_empty, 8);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;                  // scores: columns 0 and 128 in turn; dP and dS: 256; dQ: 384
+
+    if (warp >= 8 && warp < 12) {
+        // ---- copies: Q and dO of a tile of rows, then keys and values in turn
+        const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8;
+        Pending pend;
+        uint32_t g = 0, jj = 0, item = 0;
+        bool ok = true;
+        for (int64_t t = t0; t * kTile < rows && n > 0 && ok; t += tiles, ++item) {
+            if (item > 0) ok = wait_slot(&q_empty, (item - 1) & 1u, pend, lane, &abort_flag);
+            if (!ok) break;
+            const int64_t r = t * kTile + w * 32 + lane, i = r / a.group;
+            const int64_t col = (h * a.group + (int)(r - i * a.group)) * (int64_t)a.head_dim;
+            load_rows(q_smem, w * 32, r < rows ? static_cast<const bf16 *>(a.q) + (rg.q0 + i) * a.ldq + col : nullptr, a.q, chunks, real, lane);
+            load_rows(g_smem, w * 32, r < rows ? static_cast<const bf16 *>(a.dout) + (rg.q0 + i) * a.ldg + col : nullptr, a.q, chunks, real, lane);
+            pend.push(&q_full, lane);
+            for (int j = 0; j < n && ok; ++j, ++jj) {
+                const int64_t key = rg.k0 + (int64_t)j * kTile + w * 32 + lane;
+                const bool seen = key < rg.k1 && (!a.mask || a.mask[key]);
+                const uint32_t word = __ballot_sync(0xFFFFFFFFu, seen);
+                for (int v = 0; v < 2; ++v, ++g) {
+                    const uint32_t s = g % kStages;
+                    if (g >= kStages) ok = wait_slot(&kv_empty[s], (g / kStages - 1) & 1u, pend, lane, &abort_flag);
+                    if (!ok) break;
+                    if (v == 0 && lane == 0) words[jj % kWordRing][w] = word;
+                    const bf16 *src = static_cast<const bf16 *>(v ? a.v : a.k) + key * (v ? a.ldv : a.ldk) + h * (int64_t)a.head_dim;
+                    load_rows(kv_smem + s * kTileBytes, w * 32, seen ? src : nullptr, a.q, chunks, real, lane);
+                    pend.push(&kv_full[s], lane);
+                }
+            }
+        }
+        pend.flush(lane);
+    } else if (warp == 12) {
+        // ---- products.  S of the next tile goes out before dQ waits for dS, dP of the next tile behind dQ (whose operand it
+        // overwrites): the warpgroups form p of the next tile beside dQ and dP.
+        if (lane == 0) {
+            const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
+            uint32_t g = 0, item = 0, jj = 0;
+            bool ok = true;
+            auto product = [&](uint32_t d, uint32_t a_addr, uint32_t slot) {
+                const uint32_t b_addr = kv_smem + (slot % kStages) * kTileBytes;
+                for (int k = 0; k < ksteps; ++k) {
+                    const uint32_t off = (uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32;
+                    umma(d, make_smem_desc(a_addr + off), make_smem_desc(b_addr + off), id_s, k > 0);
+                }
+            };
+            auto full = [&](uint32_t slot) {
+                ok = ok && mbar_wait(&kv_full[slot % kStages], (slot / kStages) & 1u, &abort_flag);
+                tc_fence_after();
+                return ok;
+            };
+            for (int64_t t = t0; t * kTile < rows && n > 0 && ok; t += tiles, ++item) {
+                ok = mbar_wait(&q_full, item & 1u, &abort_flag);
+                if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
+                if (!full(g)) break;
+                product(tmem + (jj & 1u) * kTile, q_smem, g);
+                umma_commit(&s_full[jj & 1u]);
+                if (!full(g + 1)) break;
+                product(tmem + 256, g_smem, g + 1);
+                umma_commit(&dp_full);
+                umma_commit(&kv_empty[(g + 1) % kStages]);
+                for (int j = 0; j < n; ++j, g += 2, ++jj) {
+                    if (j + 1 < n) {
+                        if (!full(g + 2)) break;
+                        product(tmem + ((jj + 1) & 1u) * kTile, q_smem, g + 2);
+                        umma_commit(&s_full[(jj + 1) & 1u]);
+                    }
+                    ok = mbar_wait(&ds_full, jj & 1u, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t k_addr = kv_smem + (g % kStages) * kTileBytes;
+                    for (int k = 0; k < kTile / 16; ++k)
+                        umma_ts(tmem + 384, operand_step(tmem + 256, k), make_smem_desc_mn(k_addr + k * 2048, kBlockBytes), id_o, (j | k) != 0);
+                    umma_commit(&kv_empty[g % kStages]);
+                    if (j + 1 < n) {
+                        if (!full(g + 3)) break;
+                        product(tmem + 256, g_smem, g + 3);
+                        umma_commit(&dp_full);
+                        umma_commit(&kv_empty[(g + 3) % kStages]);
+                    } else {
+                        umma_commit(&o_full);
+                        umma_commit(&q_empty);
+                    }
+                }
+            }
+        }
+    } else {
+        // ---- p and dS: 64 columns of one row per thread
+        const int q = warp >> 2, w = warp & 3;
+        const uint32_t lanes = (uint32_t)(w * 32) << 16;
+        const float c1 = a.scale * kLog2e;
+        const int heads = a.kv_heads * a.group;
+        uint32_t jj = 0, item = 0;
+        bool ok = true;
+        for (int64_t t = t0; t * kTile < rows && ok; t += tiles, ++item) {
+            const int64_t r = t * kTile + w * 32 + lane, i = r / a.group;
+            const int head = h * a.group + (int)(r - i * a.group);
+            const int64_t row = rg.q0 + i, col = (int64_t)head * a.head_dim;
+            const bool live = r < rows;
+            float base = INFINITY, dot = 0.f;          // rows that saw no key: p = 0
+            if (live) {
+                const float l = a.lse[row * heads + head];
+                if (l != -INFINITY) base = l * kLog2e;
+                const bf16 *o = static_cast<const bf16 *>(a.o) + row * a.ldo + col, *gr = static_cast<const bf16 *>(a.dout) + row * a.ldg + col;
+                for (int e = 0; e < a.head_dim; e += 8) {
+                    float x[8], y[8];
+                    Chunk<bf16>::load(o + e, x);
+                    Chunk<bf16>::load(gr + e, y);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) dot += x[k] * y[k];
+                }
+                if (l == -INFINITY) dot = 0.f;
+                if (q == 0) dots[row * heads + head] = dot;
+            }
+            for (int j = 0; j < n; ++j, ++jj) {
+                ok = mbar_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                tc_fence_after();
+                float p[64];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const uint32_t word = words[jj % kWordRing][q * 2 + c];
+                    uint32_t v[32];
+                    tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64 + c * 32, v);
+                    tmem_load_wait();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) p[c * 32 + e] = exp2_approx(fmaf(__uint_as_float(v[e]), c1, -base));
+                    if (word != 0xFFFFFFFFu) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!((word >> e) & 1u)) p[c * 32 + e] = 0.f;
+                    }
+                }
+                ok = mbar_wait(&dp_full, jj & 1u, &abort_flag);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t v[32];
+                    tmem_load32_async(tmem + lanes + 256 + q * 64 + c * 32, v);
+                    tmem_load_wait();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) p[c * 32 + e] *= __uint_as_float(v[e]) - dot;
+                }
+                store_operand(tmem + lanes + 256 + q * 64, p);
+                tmem_store_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ds_full);
+            }
+            if (!ok) break;
+            if (n > 0) {
+                ok = mbar_wait(&o_full, item & 1u, &abort_flag);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                tc_fence_after();
+            }
+            if (q == 0) store_row<NB>(tmem + lanes + 384, static_cast<bf16 *>(a.dq) + row * a.ldq2 + col, a.head_dim, a.scale, n > 0, base != INFINITY, live);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0 && n > 0) mbar_arrive(&o_empty);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && abort_flag && a.status) atomicOr(reinterpret_cast<unsigned *>(a.status), E2EGREC_DEV_TIMEOUT);
+    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
+// dK and dV of a tile of keys: S^T = K Q^T and dP^T = V dO^T over the rows of the sequence
+template <int NB>
+__global__ void __launch_bounds__(kBwdThreads, 1)
+attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *__restrict__ dots)
+{
+    constexpr int kStages = 4, kTileBytes = NB * kBlockBytes, kStatRing = 4;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t qg_full[kStages], qg_empty[kStages], kv_full, kv_empty, s_full, p_full, dp_full, ds_full, o_full, o_empty;
+    __shared__ __align__(16) float stat_lse[kStatRing][kTile], stat_dot[kStatRing][kTile];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int64_t u = blockIdx.x;
+    const int t0 = (int)(u % tiles);
+    u /= tiles;
+    const int h = (int)(u % a.kv_heads);
+    const SeqRange rg = seq_range(a, u / a.kv_heads, t0 == 0 && h == 0 && threadIdx.x == 0);
+    const int64_t rows = (rg.q1 - rg.q0) * a.group, keys = rg.k1 - rg.k0;
+    if ((int64_t)t0 * kTile >= keys) return;
+    const int n = (int)ceil_div(rows, kTile);
+
+    uint8_t *tiles_smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    const uint32_t k_smem = smem_u32(tiles_smem), v_smem = k_smem + kTileBytes, qg_smem = k_smem + 2 * kTileBytes;
+    const int ksteps = (a.head_dim + 15) / 16;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(&qg_full[s], 4);
+            mbar_init(&qg_empty[s], 1);
+        }
+        mbar_init(&kv_full, 4);
+        mbar_init(&kv_empty, 1);
+        mbar_init(&s_full, 1);
+        mbar_init(&p_full, 8);
+        mbar_init(&dp_full, 1);
+        mbar_init(&ds_full, 8);
+        mbar_init(&o_full, 1);
+        mbar_init(&o_empty, 8);
+        abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 12) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;                  // S^T and P^T: columns 0; dP^T and dS^T: 128; dV: 256; dK: 384
+
+    if (warp >= 8 && warp < 12) {
+        // ---- copies: keys and values of a tile, then Q and dO of the rows in turn, with the rows' lse and D
+        const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8, heads = a.kv_heads * a.group;
+        Pending pend;
+        uint32_t g = 0, jj = 0, item = 0;
+        bool ok = true;
+        for (int64_t t = t0; t * kTile < keys && n > 0 && ok; t += tiles, ++item) {
+            if (item > 0) ok = wait_slot(&kv_empty, (item - 1) & 1u, pend, lane, &abort_flag);
+            if (!ok) break;
+            const int64_t key = rg.k0 + t * kTile + w * 32 + lane;
+            const bool seen = key < rg.k1 && (!a.mask || a.mask[key]);
+            load_rows(k_smem, w * 32, seen ? static_cast<const bf16 *>(a.k) + key * a.ldk + h * (int64_t)a.head_dim : nullptr, a.q, chunks, real, lane);
+            load_rows(v_smem, w * 32, seen ? static_cast<const bf16 *>(a.v) + key * a.ldv + h * (int64_t)a.head_dim : nullptr, a.q, chunks, real, lane);
+            pend.push(&kv_full, lane);
+            for (int j = 0; j < n && ok; ++j, ++jj) {
+                const int64_t r = (int64_t)j * kTile + w * 32 + lane, i = r / a.group;
+                const int head = h * a.group + (int)(r - i * a.group);
+                const int64_t row = rg.q0 + i, col = (int64_t)head * a.head_dim;
+                float l = INFINITY, d = 0.f;
+                if (r < rows) {
+                    const float x = a.lse[row * heads + head];
+                    if (x != -INFINITY) {
+                        l = x * kLog2e;
+                        d = dots[row * heads + head];
+                    }
+                }
+                for (int v = 0; v < 2; ++v, ++g) {
+                    const uint32_t s = g % kStages;
+                    if (g >= kStages) ok = wait_slot(&qg_empty[s], (g / kStages - 1) & 1u, pend, lane, &abort_flag);
+                    if (!ok) break;
+                    if (v == 0) {
+                        stat_lse[jj % kStatRing][w * 32 + lane] = l;
+                        stat_dot[jj % kStatRing][w * 32 + lane] = d;
+                    }
+                    const bf16 *src = v ? static_cast<const bf16 *>(a.dout) + row * a.ldg + col : static_cast<const bf16 *>(a.q) + row * a.ldq + col;
+                    load_rows(qg_smem + s * kTileBytes, w * 32, l != INFINITY ? src : nullptr, a.q, chunks, real, lane);
+                    pend.push(&qg_full[s], lane);
+                }
+            }
+        }
+        pend.flush(lane);
+    } else if (warp == 12) {
+        // ---- products.  S^T of the next tile follows dV, whose operand it overwrites, dP^T follows dK: the warpgroups form dS
+        // beside dV and the next S^T, and the next p beside dK and the next dP^T.
+        if (lane == 0) {
+            const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
+            uint32_t g = 0, item = 0, jj = 0;
+            bool ok = true;
+            auto product = [&](uint32_t d, uint32_t a_addr, uint32_t slot) {
+                const uint32_t b_addr = qg_smem + (slot % kStages) * kTileBytes;
+                for (int k = 0; k < ksteps; ++k) {
+                    const uint32_t off = (uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32;
+                    umma(d, make_smem_desc(a_addr + off), make_smem_desc(b_addr + off), id_s, k > 0);
+                }
+            };
+            auto gradient = [&](uint32_t d, uint32_t operand, uint32_t slot, bool add) {
+                const uint32_t b_addr = qg_smem + (slot % kStages) * kTileBytes;
+                for (int k = 0; k < kTile / 16; ++k)
+                    umma_ts(d, operand_step(operand, k), make_smem_desc_mn(b_addr + k * 2048, kBlockBytes), id_o, add || k != 0);
+            };
+            auto full = [&](uint32_t slot) {
+                ok = ok && mbar_wait(&qg_full[slot % kStages], (slot / kStages) & 1u, &abort_flag);
+                tc_fence_after();
+                return ok;
+            };
+            for (int64_t t = t0; t * kTile < keys && n > 0 && ok; t += tiles, ++item) {
+                ok = mbar_wait(&kv_full, item & 1u, &abort_flag);
+                if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
+                if (!full(g)) break;
+                product(tmem, k_smem, g);
+                umma_commit(&s_full);
+                if (!full(g + 1)) break;
+                product(tmem + 128, v_smem, g + 1);
+                umma_commit(&dp_full);
+                for (int j = 0; j < n; ++j, g += 2, ++jj) {
+                    ok = mbar_wait(&p_full, jj & 1u, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    gradient(tmem + 256, tmem, g + 1, j > 0);
+                    umma_commit(&qg_empty[(g + 1) % kStages]);
+                    if (j + 1 < n) {
+                        if (!full(g + 2)) break;
+                        product(tmem, k_smem, g + 2);
+                        umma_commit(&s_full);
+                    }
+                    ok = mbar_wait(&ds_full, jj & 1u, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    gradient(tmem + 384, tmem + 128, g, j > 0);
+                    umma_commit(&qg_empty[g % kStages]);
+                    if (j + 1 < n) {
+                        if (!full(g + 3)) break;
+                        product(tmem + 128, v_smem, g + 3);
+                        umma_commit(&dp_full);
+                    } else {
+                        umma_commit(&o_full);
+                        umma_commit(&kv_empty);
+                    }
+                }
+            }
+        }
+    } else {
+        // ---- p and dS: 64 columns (rows of Q) of one key per thread
+        const int q = warp >> 2, w = warp & 3;
+        const uint32_t lanes = (uint32_t)(w * 32) << 16;
+        const float c1 = a.scale * kLog2e;
+        uint32_t jj = 0, item = 0;
+        bool ok = true;
+        for (int64_t t = t0; t * kTile < keys && ok; t += tiles, ++item) {
+            const int64_t key = rg.k0 + t * kTile + w * 32 + lane;
+            const bool live = key < rg.k1, seen = live && (!a.mask || a.mask[key]);
+            for (int j = 0; j < n; ++j, ++jj) {
+                ok = mbar_wait(&s_full, jj & 1u, &abort_flag);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                tc_fence_after();
+                const float4 *lse4 = reinterpret_cast<const float4 *>(stat_lse[jj % kStatRing] + q * 64);
+                const float4 *dot4 = reinterpret_cast<const float4 *>(stat_dot[jj % kStatRing] + q * 64);
+                float p[64];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t v[32];
+                    tmem_load32_async(tmem + lanes + q * 64 + c * 32, v);
+                    tmem_load_wait();
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float4 l = lse4[c * 8 + e];
+                        p[c * 32 + 4 * e] = exp2_approx(fmaf(__uint_as_float(v[4 * e]), c1, -l.x));
+                        p[c * 32 + 4 * e + 1] = exp2_approx(fmaf(__uint_as_float(v[4 * e + 1]), c1, -l.y));
+                        p[c * 32 + 4 * e + 2] = exp2_approx(fmaf(__uint_as_float(v[4 * e + 2]), c1, -l.z));
+                        p[c * 32 + 4 * e + 3] = exp2_approx(fmaf(__uint_as_float(v[4 * e + 3]), c1, -l.w));
+                    }
+                }
+                store_operand(tmem + lanes + q * 64, p);
+                tmem_store_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&p_full);
+                ok = mbar_wait(&dp_full, jj & 1u, &abort_flag);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    uint32_t v[32];
+                    tmem_load32_async(tmem + lanes + 128 + q * 64 + c * 32, v);
+                    tmem_load_wait();
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float4 d = dot4[c * 8 + e];
+                        p[c * 32 + 4 * e] *= __uint_as_float(v[4 * e]) - d.x;
+                        p[c * 32 + 4 * e + 1] *= __uint_as_float(v[4 * e + 1]) - d.y;
+                        p[c * 32 + 4 * e + 2] *= __uint_as_float(v[4 * e + 2]) - d.z;
+                        p[c * 32 + 4 * e + 3] *= __uint_as_float(v[4 * e + 3]) - d.w;
+                    }
+                }
+                store_operand(tmem + lanes + 128 + q * 64, p);
+                tmem_store_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&ds_full);
+            }
+            if (!ok) break;
+            if (n > 0) {
+                ok = mbar_wait(&o_full, item & 1u, &abort_flag);
+                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+                tc_fence_after();
+            }
+            const int64_t col = h * (int64_t)a.head_dim;
+            if (q == 0) store_row<NB>(tmem + lanes + 256, static_cast<bf16 *>(a.dv) + key * a.ldv2 + col, a.head_dim, 1.f, n > 0, seen, live);
+            else store_row<NB>(tmem + lanes + 384, static_cast<bf16 *>(a.dk) + key * a.ldk2 + col, a.head_dim, a.scale, n > 0, seen, live);
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0 && n > 0) mbar_arrive(&o_empty);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && abort_flag && a.status) atomicOr(reinterpret_cast<unsigned *>(a.status), E2EGREC_DEV_TIMEOUT);
+    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+}
+
 constexpr int kMaxDevices = 64;
 template <typename Kernel> bool allow_smem(Kernel kernel, size_t bytes, bool (&done)[kMaxDevices])
 {
@@ -426,6 +920,27 @@ bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, float *p
     note_launch();
     if (one) attn_tc_fwd_kernel<1><<<grid, kFwdThreads, fwd_smem<1>(), st>>>(a, (int)tiles, splits, part_o, part_ml);
     else attn_tc_fwd_kernel<2><<<grid, kFwdThreads, fwd_smem<2>(), st>>>(a, (int)tiles, splits, part_o, part_ml);
+    return true;
+}
+
+bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st)
+{
+    static bool done[4][kMaxDevices] = {};
+    const bool one = a.head_dim <= 64;
+    if (!(one ? allow_smem(attn_tc_dq_kernel<1>, dq_smem<1>(), done[0]) && allow_smem(attn_tc_dkv_kernel<1>, dkv_smem<1>(), done[1])
+              : allow_smem(attn_tc_dq_kernel<2>, dq_smem<2>(), done[2]) && allow_smem(attn_tc_dkv_kernel<2>, dkv_smem<2>(), done[3])))
+        return false;
+    const int64_t units = a.n_seq * a.kv_heads;
+    if (a.q_rows) {
+        note_launch();
+        if (one) attn_tc_dq_kernel<1><<<(unsigned)(units * q_tiles), kBwdThreads, dq_smem<1>(), st>>>(a, (int)q_tiles, dots);
+        else attn_tc_dq_kernel<2><<<(unsigned)(units * q_tiles), kBwdThreads, dq_smem<2>(), st>>>(a, (int)q_tiles, dots);
+    }
+    if (a.k_rows) {
+        note_launch();
+        if (one) attn_tc_dkv_kernel<1><<<(unsigned)(units * k_tiles), kBwdThreads, dkv_smem<1>(), st>>>(a, (int)k_tiles, dots);
+        else attn_tc_dkv_kernel<2><<<(unsigned)(units * k_tiles), kBwdThreads, dkv_smem<2>(), st>>>(a, (int)k_tiles, dots);
+    }
     return true;
 }
 

@@ -62,10 +62,11 @@ def attention(q, k, v, q_ptr, k_ptr, heads, kv_heads, scale, mask=None, dout=Non
     ds <= (head_dim + 2) e scale |q| . |k|; p = exp(score - lse) therefore by a factor 1 + dp, dp <= 2 max ds + 2^-20 (score, lse, the
     hardware's exponential, its argument's rounding up to 2^7 in size: 2^7 e = 2^-17 is added where scores are that large); with
     rounded_p also by h, as p goes into the products in 16 bits.  A sum of n such terms adds n e of their absolute sum.  The backward
-    pass reads `out` as it was stored (off by its own bound)."""
+    pass reads `out` as it was stored (off by its own bound).  A p below 2^-126 has no normal 32-bit value: it may count as zero, so p is
+    off by tiny = 2^-126 on top, and every result by tiny times the sum of what p multiplies."""
     G, hd = heads // kv_heads, q.shape[1] // heads
     e, h = 2.0 ** -24, HALF[dtype]
-    hp = HALF[torch.bfloat16] if rounded_p else 0.0
+    hp, tiny = HALF[torch.bfloat16] if rounded_p else 0.0, 2.0 ** -126
     z = torch.zeros
     out, out_b = z(q.shape, dtype=torch.float64), z(q.shape, dtype=torch.float64)
     lse, lse_b = torch.full((q.shape[0], heads), -math.inf, dtype=torch.float64), z(q.shape[0], heads, dtype=torch.float64)
@@ -86,7 +87,7 @@ def attention(q, k, v, q_ptr, k_ptr, heads, kv_heads, scale, mask=None, dout=Non
         worst = ds_.amax(-1, keepdim=True) + e * sc.abs().amax(-1, keepdim=True)
         dp_ = 2 * worst + 2.0 ** -20 + n * e
         o = torch.einsum("hgqk,khd->qhgd", p, vs)
-        ob = h * o.abs() + torch.einsum("hgqk,khd->qhgd", p * (dp_ + hp + n * e), vs.abs()) * (1 + h) + 2.0 ** -126
+        ob = h * o.abs() + torch.einsum("hgqk,khd->qhgd", p * (dp_ + hp + n * e) + tiny, vs.abs()) * (1 + h) + tiny
         out[rq], out_b[rq] = o.flatten(1), ob.flatten(1)
         lse[rq] = l[..., 0].permute(2, 0, 1).flatten(1)
         lse_b[rq] = (worst[..., 0] + 2.0 ** -20 + n * e + 2 * e * l[..., 0].abs()).permute(2, 0, 1).flatten(1)
@@ -99,17 +100,17 @@ def attention(q, k, v, q_ptr, k_ptr, heads, kv_heads, scale, mask=None, dout=Non
         dD = torch.einsum("qhgd,qhgd->hgq", g.abs(), ob + (hd + 2) * e * o.abs())[..., None]
         ddp = (hd + 2) * e * torch.einsum("qhgd,khd->hgqk", g.abs(), vs.abs())
         dS = p * (dpv - D)
-        dSb = dS.abs() * (dp_ + hp) + p * (ddp + dD) * (1 + dp_ + hp)
+        dSb = dS.abs() * (dp_ + hp) + p * (ddp + dD) * (1 + dp_ + hp) + tiny * (1 + (dpv - D).abs())
         nq = qs.shape[0] * G
         for name, val, bound, terms, rows in (
-                ("dv", torch.einsum("hgqk,qhgd->khd", p, g), torch.einsum("hgqk,qhgd->khd", p * (dp_ + hp), g.abs()),
+                ("dv", torch.einsum("hgqk,qhgd->khd", p, g), torch.einsum("hgqk,qhgd->khd", p * (dp_ + hp) + tiny, g.abs()),
                  torch.einsum("hgqk,qhgd->khd", p, g.abs()) * nq * e, seen),
                 ("dq", torch.einsum("hgqk,khd->qhgd", dS, ks) * scale, torch.einsum("hgqk,khd->qhgd", dSb, ks.abs()) * scale,
                  torch.einsum("hgqk,khd->qhgd", dS.abs(), ks.abs()) * scale * (n + 2) * e, rq),
                 ("dk", torch.einsum("hgqk,qhgd->khd", dS, qs) * scale, torch.einsum("hgqk,qhgd->khd", dSb, qs.abs()) * scale,
                  torch.einsum("hgqk,qhgd->khd", dS.abs(), qs.abs()) * scale * (nq + 2) * e, seen)):
             grads[name][0][rows] = val.flatten(1)
-            grads[name][1][rows] = (h * val.abs() + (bound + terms) * (1 + h) + 2.0 ** -126).flatten(1)
+            grads[name][1][rows] = (h * val.abs() + (bound + terms) * (1 + h) + tiny).flatten(1)
     res = {"out": (out, out_b), "lse": (lse, lse_b)}
     if dout is not None:
         res.update(grads)
