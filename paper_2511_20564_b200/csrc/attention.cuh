@@ -63,4 +63,17 @@ bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, float *p
 // q_tiles, k_tiles: tiles of 128 rows and of 128 keys per sequence and key head; dots: [q_rows x heads] scratch
 bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st);
 
+// attention_few.cu: streaming kernels, fp32 and bf16, head_dim <= 256
+struct FewPlan {
+    int rows;                             // rows per unit
+    bool both;                            // backward: one kernel for dQ, dK and dV
+    int64_t batches;                      // units of rows per sequence and key head
+    int warps, splits;                    // warps per unit, stretches of the keys
+    int64_t key_batches;                  // units of keys of the dK, dV kernel
+};
+FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool backward);
+void few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_o, float2 *part_ml, cudaStream_t st);
+// part_dq: [splits x q_rows x heads x head_dim] where splits > 1; dots: [q_rows x heads] where !both
+void few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st);
+
 }  // namespace e2egrec

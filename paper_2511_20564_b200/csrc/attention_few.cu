@@ -1,0 +1,661 @@
+// Attention where a sequence has few rows (query, head of the group) per key head: single tokens, a candidate, a stack of a few
+// tokens.  Every key and value is used a handful of times, so these kernels stream them: fp32 FMA, 16 bytes per lane and load.
+//
+// `lanes` neighbouring lanes share a key (16 bytes of the head each) and 32 / lanes keys are in a warp's step, kUnroll steps in flight.
+// Each lane group keeps its own running maximum, sum and outputs over the keys it meets; groups, then the warps of a unit, then the
+// stretches of a long list of keys are joined at the end, in a fixed order.  A unit is up to R rows of one sequence and key head.
+#include <algorithm>
+
+#include "attention.cuh"
+
+namespace e2egrec {
+namespace {
+
+constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
+constexpr int kUnroll = 4;                           // steps of keys in flight per warp
+
+template <typename T, int CPL> struct Piece {        // a lane's part of a head's row
+    static constexpr int E = Chunk<T>::kElems * CPL;
+    uint4 raw[CPL];
+    __device__ inline void zero()
+    {
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) raw[c] = make_uint4(0, 0, 0, 0);
+    }
+    // chunk `at`, and (CPL = 2) the chunk `lanes` behind it
+    __device__ inline void load(const T *row, int at, int lanes, int chunks)
+    {
+#pragma unroll
+        for (int c = 0; c < CPL; ++c)
+            if (at + c * lanes < chunks) raw[c] = __ldg(reinterpret_cast<const uint4 *>(row) + at + c * lanes);
+            else raw[c] = make_uint4(0, 0, 0, 0);
+    }
+    __device__ inline void widen(float (&v)[E]) const
+    {
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+            float x[Chunk<T>::kElems];
+            Chunk<T>::unpack(raw[c], x);
+#pragma unroll
+            for (int i = 0; i < Chunk<T>::kElems; ++i) v[c * Chunk<T>::kElems + i] = x[i];
+        }
+    }
+};
+
+template <typename T, int CPL> __device__ inline void store_piece(T *row, int at, int lanes, int chunks, const float (&v)[Piece<T, CPL>::E], float f)
+{
+#pragma unroll
+    for (int c = 0; c < CPL; ++c)
+        if (at + c * lanes < chunks) {
+            float x[Chunk<T>::kElems];
+#pragma unroll
+            for (int i = 0; i < Chunk<T>::kElems; ++i) x[i] = v[c * Chunk<T>::kElems + i] * f;
+            Chunk<T>::store(row + (int64_t)(at + c * lanes) * Chunk<T>::kElems, x);
+        }
+}
+
+template <int E> __device__ inline float dot(const float (&a)[E], const float (&b)[E])
+{
+    float2 t = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < E; i += 2) t = __ffma2_rn(make_float2(a[i], a[i + 1]), make_float2(b[i], b[i + 1]), t);
+    return t.x + t.y;
+}
+template <int E> __device__ inline void axpy(float (&y)[E], float s, const float (&x)[E])
+{
+#pragma unroll
+    for (int i = 0; i < E; i += 2) {
+        const float2 t = __ffma2_rn(make_float2(s, s), make_float2(x[i], x[i + 1]), make_float2(y[i], y[i + 1]));
+        y[i] = t.x;
+        y[i + 1] = t.y;
+    }
+}
+
+// sums over the lanes of a key, N values at once
+template <int N> __device__ inline void key_sums(float (&v)[N], int lanes)
+{
+    for (int o = lanes >> 1; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
+}
+
+struct FewShape {
+    int lanes, chunks;                               // lanes per key (a power of two), 16-byte chunks of a head
+    int warps;                                       // warps per unit: a power of two, at most kFewWarps
+    int batches;                                     // batches of R rows per sequence and key head
+    int splits;                                      // stretches of the keys
+};
+
+__device__ inline float exp2_fast(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+struct Unit {
+    SeqRange rg;
+    int64_t kb, ke, rows;
+    int z, h, first;
+    bool any;
+};
+__device__ inline Unit few_unit(const AttnArgs &a, const FewShape &f, int R, int64_t u)
+{
+    Unit x;
+    x.any = u < a.n_seq * a.kv_heads * f.batches * f.splits;
+    x.z = (int)(u % f.splits);
+    u /= f.splits;
+    x.first = (int)(u % f.batches);
+    u /= f.batches;
+    x.h = (int)(u % a.kv_heads);
+    if (!x.any) {
+        x.rows = x.kb = x.ke = 0;
+        x.rg = SeqRange{0, 0, 0, 0};
+        return x;
+    }
+    x.rg = seq_range(a, u / a.kv_heads, (threadIdx.x & 31) == 0 && x.h == 0 && x.first == 0 && x.z == 0);
+    x.rows = (x.rg.q1 - x.rg.q0) * a.group;
+    const int64_t per = ceil_div(x.rg.k1 - x.rg.k0, f.splits);
+    x.kb = min(x.rg.k0 + x.z * per, x.rg.k1);
+    x.ke = min(x.kb + per, x.rg.k1);
+    return x;
+}
+
+// kb .. ke in turns of warps * kUnroll * (32 / lanes) keys
+template <typename T, int R, int CPL>
+__global__ void __launch_bounds__(kFewThreads)
+attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
+{
+    constexpr int E = Piece<T, CPL>::E;
+    __shared__ float2 join_ml[kFewWarps][R];
+    __shared__ float join_o[kFewWarps][kMaxAttnDim];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int wu = warp & (f.warps - 1);                                            // the warp's number in its unit
+    const Unit x = few_unit(a, f, R, (int64_t)blockIdx.x * (kFewWarps / f.warps) + warp / f.warps);
+    const int grp = lane / f.lanes, at = lane & (f.lanes - 1), kpw = 32 / f.lanes;
+    const int heads = a.kv_heads * a.group;
+    const int64_t koff = x.h * (int64_t)a.head_dim;
+    const float c1 = a.scale * kLog2e;
+    for (int64_t n = 0;; ++n) {
+        const int64_t r0 = (x.first + n * f.batches) * R;
+        const bool live = x.any && r0 < x.rows;
+        if (f.warps == 1 ? !live : !__syncthreads_or((int)live)) break;      // barriers inside: all warps of the block go on, or none
+        float q[R][E], o[R][E], m[R], l[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            Piece<T, CPL> p;
+            p.zero();
+            if (live && r0 + r < x.rows) {
+                const int64_t i = (r0 + r) / a.group;
+                p.load(static_cast<const T *>(a.q) + (x.rg.q0 + i) * a.ldq + (x.h * a.group + (r0 + r - i * a.group)) * a.head_dim, at, f.lanes, f.chunks);
+            }
+            p.widen(q[r]);
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                q[r][e] *= c1;
+                o[r][e] = 0.f;
+            }
+            m[r] = -INFINITY;
+            l[r] = 0.f;
+        }
+        const int64_t step = (int64_t)f.warps * kUnroll * kpw;
+        for (int64_t j0 = x.kb + (int64_t)wu * kUnroll * kpw; live && j0 < x.ke; j0 += step) {
+            Piece<T, CPL> k[kUnroll], v[kUnroll];
+            bool seen[kUnroll];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int64_t j = j0 + u * kpw + grp;
+                seen[u] = j < x.ke && (!a.mask || a.mask[j]);
+                k[u].zero();
+                v[u].zero();
+                if (seen[u]) {
+                    k[u].load(static_cast<const T *>(a.k) + j * a.ldk + koff, at, f.lanes, f.chunks);
+                    v[u].load(static_cast<const T *>(a.v) + j * a.ldv + koff, at, f.lanes, f.chunks);
+                }
+            }
+            float s[R * kUnroll];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                float w[E];
+                k[u].widen(w);
+#pragma unroll
+                for (int r = 0; r < R; ++r) s[r * kUnroll + u] = dot<E>(q[r], w);
+            }
+            key_sums<R * kUnroll>(s, f.lanes);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float top = m[r];
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    if (!seen[u]) s[r * kUnroll + u] = -INFINITY;
+                    top = fmaxf(top, s[r * kUnroll + u]);
+                }
+                const float base = top == -INFINITY ? 0.f : top, c = exp2_fast(m[r] - base);
+                m[r] = top;
+                l[r] *= c;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[r][e] *= c;
+#pragma unroll
+                for (int u = 0; u < kUnroll; ++u) {
+                    s[r * kUnroll + u] = exp2_fast(s[r * kUnroll + u] - base);
+                    l[r] += s[r * kUnroll + u];
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                float w[E];
+                v[u].widen(w);
+#pragma unroll
+                for (int r = 0; r < R; ++r) axpy<E>(o[r], s[r * kUnroll + u], w);
+            }
+        }
+        // lane groups of the warp
+        for (int d = f.lanes; d < 32; d <<= 1)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float m2 = __shfl_xor_sync(0xFFFFFFFFu, m[r], d), l2 = __shfl_xor_sync(0xFFFFFFFFu, l[r], d), top = fmaxf(m[r], m2);
+                const float base = top == -INFINITY ? 0.f : top, c = exp2_fast(m[r] - base), c2 = exp2_fast(m2 - base);
+                l[r] = l[r] * c + l2 * c2;
+                m[r] = top;
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[r][e] = o[r][e] * c + __shfl_xor_sync(0xFFFFFFFFu, o[r][e], d) * c2;
+            }
+        if (f.warps > 1) {
+            if (lane == 0)
+#pragma unroll
+                for (int r = 0; r < R; ++r) join_ml[warp][r] = make_float2(m[r], l[r]);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                __syncthreads();
+                if (grp == 0)
+#pragma unroll
+                    for (int c = 0; c < CPL; ++c)
+                        if (at + c * f.lanes < f.chunks)
+#pragma unroll
+                            for (int e = 0; e < Chunk<T>::kElems; ++e)
+                                join_o[warp][(at + c * f.lanes) * Chunk<T>::kElems + e] = o[r][c * Chunk<T>::kElems + e];
+                __syncthreads();
+                if (wu == 0 && grp == 0) {
+                    float top = -INFINITY;
+                    for (int w = 0; w < f.warps; ++w) top = fmaxf(top, join_ml[warp + w][r].x);
+                    const float base = top == -INFINITY ? 0.f : top;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) o[r][e] = 0.f;
+                    for (int w = 0; w < f.warps; ++w) {
+                        const float2 ml = join_ml[warp + w][r];
+                        const float c = exp2_fast(ml.x - base);
+                        sum += ml.y * c;
+#pragma unroll
+                        for (int k = 0; k < CPL; ++k)
+                            if (at + k * f.lanes < f.chunks)
+#pragma unroll
+                                for (int e = 0; e < Chunk<T>::kElems; ++e)
+                                    o[r][k * Chunk<T>::kElems + e] += c * join_o[warp + w][(at + k * f.lanes) * Chunk<T>::kElems + e];
+                    }
+                    m[r] = top;
+                    l[r] = sum;
+                }
+            }
+        }
+        if (wu == 0 && grp == 0 && live)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+                if (r0 + r < x.rows) {
+                    const int64_t i = (r0 + r) / a.group, row = x.rg.q0 + i;
+                    const int head = x.h * a.group + (int)(r0 + r - i * a.group);
+                    const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
+                    if (f.splits == 1) {
+                        store_piece<T, CPL>(static_cast<T *>(a.out) + row * a.ldo + (int64_t)head * a.head_dim, at, f.lanes, f.chunks, o[r], inv);
+                        if (a.lse && at == 0) a.lse[row * heads + head] = l[r] == 0.f ? -INFINITY : (m[r] + log2f(l[r])) * kLn2;
+                    } else {
+                        const int64_t p = ((int64_t)x.z * a.q_rows + row) * heads + head;
+#pragma unroll
+                        for (int c = 0; c < CPL; ++c)
+                            if (at + c * f.lanes < f.chunks)
+#pragma unroll
+                                for (int e = 0; e < Chunk<T>::kElems; ++e)
+                                    part_o[p * a.head_dim + (at + c * f.lanes) * Chunk<T>::kElems + e] = o[r][c * Chunk<T>::kElems + e] * inv;
+                        if (at == 0) part_ml[p] = make_float2(l[r] == 0.f ? -INFINITY : m[r], l[r]);
+                    }
+                }
+        if (f.warps > 1) __syncthreads();
+    }
+}
+
+// dK and dV of kKeys keys per lane group (j0 and on), over all rows of the sequence.  dots: D of every row, or null where it is to be
+// formed from the stored outputs.
+constexpr int kKeys = 2;
+template <typename T, int CPL>
+__device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int h, int64_t j0, int64_t end, int grp, int at, const FewShape &f,
+                                      const float *dots)
+{
+    constexpr int E = Piece<T, CPL>::E;
+    const int kpw = 32 / f.lanes, heads = a.kv_heads * a.group;
+    const int64_t koff = h * (int64_t)a.head_dim;
+    const float c1 = a.scale * kLog2e;
+    float k[kKeys][E], v[kKeys][E], dk[kKeys][E], dv[kKeys][E];
+    bool seen[kKeys];
+#pragma unroll
+    for (int n = 0; n < kKeys; ++n) {
+        const int64_t j = j0 + n * kpw + grp;
+        seen[n] = j < end && (!a.mask || a.mask[j]);
+        Piece<T, CPL> p, t;
+        p.zero();
+        t.zero();
+        if (seen[n]) {
+            p.load(static_cast<const T *>(a.k) + j * a.ldk + koff, at, f.lanes, f.chunks);
+            t.load(static_cast<const T *>(a.v) + j * a.ldv + koff, at, f.lanes, f.chunks);
+        }
+        p.widen(k[n]);
+        t.widen(v[n]);
+#pragma unroll
+        for (int e = 0; e < E; ++e) dk[n][e] = dv[n][e] = 0.f;
+    }
+    for (int64_t row = rg.q0; row < rg.q1; ++row)
+        for (int g = 0; g < a.group; ++g) {
+            const int head = h * a.group + g;
+            const float l = __ldg(a.lse + row * heads + head);
+            if (l == -INFINITY) continue;
+            const int64_t col = (int64_t)head * a.head_dim;
+            Piece<T, CPL> p, t;
+            p.load(static_cast<const T *>(a.q) + row * a.ldq + col, at, f.lanes, f.chunks);
+            t.load(static_cast<const T *>(a.dout) + row * a.ldg + col, at, f.lanes, f.chunks);
+            float q[E], go[E], s[2 * kKeys], d[1];
+            p.widen(q);
+            t.widen(go);
+            if (dots) {
+                d[0] = __ldg(dots + row * heads + head);
+            } else {
+                Piece<T, CPL> o;
+                o.load(static_cast<const T *>(a.o) + row * a.ldo + col, at, f.lanes, f.chunks);
+                float y[E];
+                o.widen(y);
+                d[0] = dot<E>(go, y);
+                key_sums<1>(d, f.lanes);
+            }
+#pragma unroll
+            for (int n = 0; n < kKeys; ++n) {
+                s[n] = dot<E>(q, k[n]);
+                s[kKeys + n] = dot<E>(go, v[n]);
+            }
+            key_sums<2 * kKeys>(s, f.lanes);
+#pragma unroll
+            for (int n = 0; n < kKeys; ++n) {
+                const float pr = seen[n] ? exp2_fast(fmaf(s[n], c1, -l * kLog2e)) : 0.f;
+                axpy<E>(dv[n], pr, go);
+                axpy<E>(dk[n], seen[n] ? pr * (s[kKeys + n] - d[0]) : 0.f, q);
+            }
+        }
+#pragma unroll
+    for (int n = 0; n < kKeys; ++n) {
+        const int64_t j = j0 + n * kpw + grp;
+        if (j < end) {
+            store_piece<T, CPL>(static_cast<T *>(a.dk) + j * a.ldk2 + koff, at, f.lanes, f.chunks, dk[n], a.scale);
+            store_piece<T, CPL>(static_cast<T *>(a.dv) + j * a.ldv2 + koff, at, f.lanes, f.chunks, dv[n], 1.f);
+        }
+    }
+}
+
+// Backward pass of up to R rows over a stretch of the keys.  kBoth: the unit holds every row of its sequence and key head, so dK and
+// dV of a key are complete as soon as its own step is done and everything is read once; else only dQ (and D, in dots).  A sequence
+// that is longer than the launch was sized for has its rows done batch by batch and its keys' gradients apart.
+// Where all keys are in one turn of the warp, D = sum_j p_j dP_j is formed from what the registers hold instead of the stored
+// outputs: with a handful of keys dP - D cancels, and the rounding of 16-bit outputs showed (dQ of three keys 3.1e-3 off, 2.0e-3 so).
+template <typename T, int R, int CPL, bool kBoth>
+__global__ void __launch_bounds__(kFewThreads)
+attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_dq, float *__restrict__ dots)
+{
+    constexpr int E = Piece<T, CPL>::E, U = R > 2 ? 2 : kUnroll;
+    __shared__ float join[kFewWarps][kMaxAttnDim];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int wu = warp & (f.warps - 1);
+    const Unit x = few_unit(a, f, R, (int64_t)blockIdx.x * (kFewWarps / f.warps) + warp / f.warps);
+    const int grp = lane / f.lanes, at = lane & (f.lanes - 1), kpw = 32 / f.lanes;
+    const int heads = a.kv_heads * a.group;
+    const int64_t koff = x.h * (int64_t)a.head_dim;
+    const float c1 = a.scale * kLog2e;
+    const bool whole = kBoth && x.rows <= R;
+    for (int64_t n = 0;; ++n) {
+        const int64_t r0 = (x.first + n * f.batches) * R;
+        // with kBoth the keys' gradients are written even where there is no row at all
+        const bool live = x.any && (r0 < x.rows || (kBoth && n == 0));
+        if (f.warps == 1 ? !live : !__syncthreads_or((int)live)) break;
+        float q[R][E], g[R][E], dq[R][E], lse[R], d[R];
+        const int64_t step = (int64_t)f.warps * U * kpw;
+        const bool one_turn = f.warps == 1 && f.splits == 1 && x.ke - x.kb <= U * kpw;
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            Piece<T, CPL> p, t;
+            p.zero();
+            t.zero();
+            lse[r] = INFINITY;
+            d[r] = 0.f;
+            if (live && r0 + r < x.rows) {
+                const int64_t i = (r0 + r) / a.group, row = x.rg.q0 + i;
+                const int head = x.h * a.group + (int)(r0 + r - i * a.group);
+                const int64_t col = (int64_t)head * a.head_dim;
+                const float v = a.lse[row * heads + head];
+                if (v != -INFINITY) {
+                    lse[r] = v * kLog2e;
+                    p.load(static_cast<const T *>(a.q) + row * a.ldq + col, at, f.lanes, f.chunks);
+                    t.load(static_cast<const T *>(a.dout) + row * a.ldg + col, at, f.lanes, f.chunks);
+                    if (!one_turn) {
+                        Piece<T, CPL> s;
+                        s.load(static_cast<const T *>(a.o) + row * a.ldo + col, at, f.lanes, f.chunks);
+                        float y[E];
+                        s.widen(y);
+                        t.widen(g[r]);
+                        d[r] = dot<E>(g[r], y);
+                    }
+                }
+            }
+            p.widen(q[r]);
+            t.widen(g[r]);
+#pragma unroll
+            for (int e = 0; e < E; ++e) dq[r][e] = 0.f;
+        }
+        key_sums<R>(d, f.lanes);
+        for (int64_t j0 = x.kb + (int64_t)wu * U * kpw; live && j0 < x.ke; j0 += step) {
+            Piece<T, CPL> k[U], v[U];
+            bool seen[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int64_t j = j0 + u * kpw + grp;
+                seen[u] = j < x.ke && (!a.mask || a.mask[j]);
+                k[u].zero();
+                v[u].zero();
+                if (seen[u]) {
+                    k[u].load(static_cast<const T *>(a.k) + j * a.ldk + koff, at, f.lanes, f.chunks);
+                    v[u].load(static_cast<const T *>(a.v) + j * a.ldv + koff, at, f.lanes, f.chunks);
+                }
+            }
+            float s[2 * R * U];                                                     // scores, then p; dP, then dS
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float w[E], y[E];
+                k[u].widen(w);
+                v[u].widen(y);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    s[r * U + u] = dot<E>(q[r], w);
+                    s[(R + r) * U + u] = dot<E>(g[r], y);
+                }
+            }
+            key_sums<2 * R * U>(s, f.lanes);
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) s[r * U + u] = seen[u] ? exp2_fast(fmaf(s[r * U + u], c1, -lse[r])) : 0.f;
+                if (one_turn) {
+                    float t = 0.f;
+#pragma unroll
+                    for (int u = 0; u < U; ++u) t += seen[u] ? s[r * U + u] * s[(R + r) * U + u] : 0.f;
+                    for (int o = f.lanes; o < 32; o <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+                    d[r] = t;
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u) s[(R + r) * U + u] = seen[u] ? s[r * U + u] * (s[(R + r) * U + u] - d[r]) : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                float w[E];
+                k[u].widen(w);
+#pragma unroll
+                for (int r = 0; r < R; ++r) axpy<E>(dq[r], s[(R + r) * U + u], w);
+                const int64_t j = j0 + u * kpw + grp;
+                if (kBoth && whole && j < x.ke) {
+                    float dk[E], dv[E];
+#pragma unroll
+                    for (int e = 0; e < E; ++e) dk[e] = dv[e] = 0.f;
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        axpy<E>(dk, s[(R + r) * U + u], q[r]);
+                        axpy<E>(dv, s[r * U + u], g[r]);
+                    }
+                    store_piece<T, CPL>(static_cast<T *>(a.dk) + j * a.ldk2 + koff, at, f.lanes, f.chunks, dk, a.scale);
+                    store_piece<T, CPL>(static_cast<T *>(a.dv) + j * a.ldv2 + koff, at, f.lanes, f.chunks, dv, 1.f);
+                }
+            }
+        }
+        for (int o = f.lanes; o < 32; o <<= 1)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int e = 0; e < E; ++e) dq[r][e] += __shfl_xor_sync(0xFFFFFFFFu, dq[r][e], o);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            if (f.warps > 1) {
+                __syncthreads();
+                if (grp == 0)
+#pragma unroll
+                    for (int c = 0; c < CPL; ++c)
+                        if (at + c * f.lanes < f.chunks)
+#pragma unroll
+                            for (int e = 0; e < Chunk<T>::kElems; ++e) join[warp][(at + c * f.lanes) * Chunk<T>::kElems + e] = dq[r][c * Chunk<T>::kElems + e];
+                __syncthreads();
+                if (wu == 0 && grp == 0)
+                    for (int w = 1; w < f.warps; ++w)
+#pragma unroll
+                        for (int c = 0; c < CPL; ++c)
+                            if (at + c * f.lanes < f.chunks)
+#pragma unroll
+                                for (int e = 0; e < Chunk<T>::kElems; ++e) dq[r][c * Chunk<T>::kElems + e] += join[warp + w][(at + c * f.lanes) * Chunk<T>::kElems + e];
+            }
+            if (wu == 0 && grp == 0 && live && r0 + r < x.rows) {
+                const int64_t i = (r0 + r) / a.group, row = x.rg.q0 + i;
+                const int head = x.h * a.group + (int)(r0 + r - i * a.group);
+                if (!kBoth && x.z == 0 && at == 0) dots[row * heads + head] = d[r];
+                if (f.splits == 1) {
+                    store_piece<T, CPL>(static_cast<T *>(a.dq) + row * a.ldq2 + (int64_t)head * a.head_dim, at, f.lanes, f.chunks, dq[r], a.scale);
+                } else {
+                    const int64_t p = (((int64_t)x.z * a.q_rows + row) * heads + head) * a.head_dim;
+#pragma unroll
+                    for (int c = 0; c < CPL; ++c)
+                        if (at + c * f.lanes < f.chunks)
+#pragma unroll
+                            for (int e = 0; e < Chunk<T>::kElems; ++e) part_dq[p + (at + c * f.lanes) * Chunk<T>::kElems + e] = dq[r][c * Chunk<T>::kElems + e] * a.scale;
+                }
+            }
+        }
+        if (f.warps > 1) __syncthreads();
+    }
+    if (kBoth && x.any && !whole)
+        for (int64_t j0 = x.kb + (int64_t)wu * kKeys * kpw; j0 < x.ke; j0 += (int64_t)f.warps * kKeys * kpw)
+            keys_gradients<T, CPL>(a, x.rg, x.h, j0, x.ke, grp, at, f, nullptr);
+}
+
+// dK and dV where the rows of a sequence do not fit one unit
+template <typename T, int CPL>
+__global__ void __launch_bounds__(kFewThreads)
+attn_few_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, const float *__restrict__ dots)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    int64_t u = (int64_t)blockIdx.x * kFewWarps + warp;
+    if (u >= a.n_seq * a.kv_heads * f.batches) return;
+    const int first = (int)(u % f.batches);
+    u /= f.batches;
+    const int h = (int)(u % a.kv_heads);
+    const SeqRange rg = seq_range(a, u / a.kv_heads, lane == 0 && h == 0 && first == 0);
+    const int64_t step = (int64_t)kKeys * (32 / f.lanes);
+    for (int64_t j0 = rg.k0 + first * step; j0 < rg.k1; j0 += f.batches * step)
+        keys_gradients<T, CPL>(a, rg, h, j0, rg.k1, lane / f.lanes, lane & (f.lanes - 1), f, dots);
+}
+
+// dQ of stretches of the keys -> dQ, in order; one warp per (row, head)
+template <typename T>
+__global__ void __launch_bounds__(kFewThreads)
+attn_join_dq_kernel(const __grid_constant__ AttnArgs a, int splits, const float *__restrict__ part)
+{
+    const int lane = threadIdx.x & 31, heads = a.kv_heads * a.group;
+    const int64_t unit = ((int64_t)blockIdx.x * kFewThreads + threadIdx.x) >> 5, stride = a.q_rows * heads;
+    const int64_t row = unit / heads;
+    const int h = (int)(unit % heads);
+    if (row >= a.q_rows || owner(a.q_ptr, a.n_seq, row) < 0) return;
+    for (int e = lane; e < a.head_dim; e += 32) {
+        float t = 0.f;
+        for (int z = 0; z < splits; ++z) t += part[(z * stride + unit) * a.head_dim + e];
+        static_cast<T *>(a.dq)[row * a.ldq2 + (int64_t)h * a.head_dim + e] = from_float<T>(t);
+    }
+}
+
+FewShape few_shape(const AttnArgs &a, int es)
+{
+    FewShape f{};
+    f.chunks = a.head_dim * es / 16;
+    f.lanes = 1;
+    while (f.lanes < f.chunks && f.lanes < 32) f.lanes <<= 1;
+    f.warps = f.batches = f.splits = 1;
+    return f;
+}
+
+unsigned few_grid(const AttnArgs &a, const FewShape &f) { return (unsigned)ceil_div(a.n_seq * a.kv_heads * f.batches * f.splits, kFewWarps / f.warps); }
+
+template <typename T, int R>
+void launch_fwd(const AttnArgs &a, const FewShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
+{
+    note_launch();
+    if (f.chunks <= 32) attn_few_fwd_kernel<T, R, 1><<<few_grid(a, f), kFewThreads, 0, st>>>(a, f, part_o, part_ml);
+    else if constexpr (sizeof(T) == 4) attn_few_fwd_kernel<T, R, 2><<<few_grid(a, f), kFewThreads, 0, st>>>(a, f, part_o, part_ml);
+}
+
+template <typename T, int R, bool kBoth>
+void launch_bwd(const AttnArgs &a, const FewShape &f, float *part_dq, float *dots, cudaStream_t st)
+{
+    note_launch();
+    if (f.chunks <= 32) attn_few_bwd_kernel<T, R, 1, kBoth><<<few_grid(a, f), kFewThreads, 0, st>>>(a, f, part_dq, dots);
+    else if constexpr (sizeof(T) == 4) attn_few_bwd_kernel<T, R, 2, kBoth><<<few_grid(a, f), kFewThreads, 0, st>>>(a, f, part_dq, dots);
+}
+
+}  // namespace
+
+// Rows per unit, warps per unit and stretches of the keys.  The aim is 24 warps per SM; a warp gets a turn of keys at least.
+FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool backward)
+{
+    FewPlan p{};
+    const FewShape f = few_shape(a, es);
+    const int64_t rows = max_q * a.group, units0 = std::max<int64_t>(a.n_seq * a.kv_heads, 1);
+    p.rows = rows <= 1 ? 1 : (rows <= 2 ? 2 : 4);
+    p.both = backward && rows <= p.rows;
+    p.batches = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, p.rows), (((int64_t)1 << 31) - 1) / units0 / 64));
+    const int64_t turn = (int64_t)(32 / f.lanes) * (backward && p.rows > 2 ? 2 : kUnroll);
+    const int64_t want = std::max<int64_t>(1, std::min(ceil_div(148 * 24, units0 * p.batches), ceil_div(max_k, turn)));
+    p.warps = 1;
+    while (p.warps < kFewWarps && p.warps < want) p.warps *= 2;
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(want / p.warps, 64));
+    const int64_t per = (int64_t)(32 / f.lanes) * kKeys;
+    p.key_batches = std::max<int64_t>(1, std::min(ceil_div(max_k, per), (((int64_t)1 << 31) - 1) / units0));
+    return p;
+}
+
+void few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_o, float2 *part_ml, cudaStream_t st)
+{
+    const bool f32 = dtype == E2EGREC_F32;
+    FewShape f = few_shape(a, f32 ? 4 : 2);
+    f.warps = p.warps;
+    f.batches = (int)p.batches;
+    f.splits = p.splits;
+    if (f32) {
+        if (p.rows == 1) launch_fwd<float, 1>(a, f, part_o, part_ml, st);
+        else if (p.rows == 2) launch_fwd<float, 2>(a, f, part_o, part_ml, st);
+        else launch_fwd<float, 4>(a, f, part_o, part_ml, st);
+    } else {
+        if (p.rows == 1) launch_fwd<__nv_bfloat16, 1>(a, f, part_o, part_ml, st);
+        else if (p.rows == 2) launch_fwd<__nv_bfloat16, 2>(a, f, part_o, part_ml, st);
+        else launch_fwd<__nv_bfloat16, 4>(a, f, part_o, part_ml, st);
+    }
+}
+
+template <typename T> static void few_backward(const AttnArgs &a, const FewPlan &p, FewShape f, float *part_dq, float *dots, cudaStream_t st)
+{
+    if (p.both) {
+        if (p.rows == 1) launch_bwd<T, 1, true>(a, f, part_dq, dots, st);
+        else if (p.rows == 2) launch_bwd<T, 2, true>(a, f, part_dq, dots, st);
+        else launch_bwd<T, 4, true>(a, f, part_dq, dots, st);
+    } else {
+        launch_bwd<T, 4, false>(a, f, part_dq, dots, st);
+    }
+    if (f.splits > 1 && a.q_rows) {
+        note_launch();
+        attn_join_dq_kernel<T><<<(unsigned)ceil_div(a.q_rows * a.kv_heads * a.group, kFewWarps), kFewThreads, 0, st>>>(a, f.splits, part_dq);
+    }
+    if (!p.both && a.k_rows) {
+        note_launch();
+        f.batches = (int)p.key_batches;
+        const unsigned grid = (unsigned)ceil_div(a.n_seq * a.kv_heads * f.batches, kFewWarps);
+        if (f.chunks <= 32) attn_few_dkv_kernel<T, 1><<<grid, kFewThreads, 0, st>>>(a, f, dots);
+        else if constexpr (sizeof(T) == 4) attn_few_dkv_kernel<T, 2><<<grid, kFewThreads, 0, st>>>(a, f, dots);
+    }
+}
+
+void few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st)
+{
+    FewShape f = few_shape(a, dtype == E2EGREC_F32 ? 4 : 2);
+    f.warps = p.warps;
+    f.batches = (int)p.batches;
+    f.splits = p.splits;
+    if (dtype == E2EGREC_F32) few_backward<float>(a, p, f, part_dq, dots, st);
+    else few_backward<__nv_bfloat16>(a, p, f, part_dq, dots, st);
+}
+
+}  // namespace e2egrec
