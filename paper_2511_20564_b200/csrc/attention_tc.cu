@@ -3,7 +3,7 @@
 // The rows of a product are the (query, head of the group) pairs of one key head of one sequence; tiles are 128 x 128.  Every
 // operand tile lies in shared memory as blocks of 64 columns, 128 lines of 128 bytes each, 128-byte swizzled: the same bytes serve
 // as an operand whose K index is contiguous (Q, K, V, dO against head_dim) and as one whose N index is (V, K, Q, dO against rows).
-// Tiles are copied by cp.async, 16 bytes per lane, each warp a quarter of the rows: rows behind a sequence's end and hidden keys are
+// Tiles are copied by cp.async, 16 bytes per lane, each loading warp half of the rows: rows behind a sequence's end and hidden keys are
 // filled with zeros without being read, which a box of a tensor map cannot do, and any offset, stride and head width
 // goes.  Scores and gradients of scores go back to the tensor cores through tensor memory (A operand), never through shared memory.
 // Every wait is bounded; when one runs out the block reports E2EGREC_DEV_TIMEOUT, lets its copies land, frees its tensor memory
@@ -19,6 +19,8 @@ namespace {
 using bf16 = __nv_bfloat16;
 
 constexpr int kTile = 128;
+constexpr int kThreads = 12 * 32;                    // two warpgroups over scores, two loading warps, the products' warp; one idle
+constexpr int kLoaders = 2, kMmaWarp = 8 + kLoaders;
 constexpr int kBlockBytes = kTile * 128;             // 64 columns of 128 rows
 constexpr int kWordRing = 8;                         // tiles whose visibility words are kept
 
@@ -49,22 +51,61 @@ __device__ inline void tmem_load32_async(uint32_t taddr, uint32_t (&r)[32])
         : "r"(taddr));
 }
 
-// The 32 rows of one loading warp -> shared memory.  src: the lane's own row (its first element of the head), null for zeros;
-// chunks: 16-byte chunks per row that the products read, of which `real` exist; any: an address that may be named where nothing is read.
-__device__ inline void load_rows(uint32_t tile, int warp_row, const bf16 *src, const void *any, int chunks, int real, int lane)
+__device__ inline void tmem_load16_async(uint32_t taddr, uint32_t (&r)[16])
 {
-    int row = lane / chunks, ch = lane - row * chunks;
-    const int dr = 32 / chunks, dc = 32 - dr * chunks;
-    const uint64_t mine = reinterpret_cast<uint64_t>(src);
-    for (int i = 0; i < chunks; ++i) {
-        const uint64_t p = __shfl_sync(0xFFFFFFFFu, mine, row);
-        const int r = warp_row + row;
-        const uint32_t dst = tile + (uint32_t)(ch >> 3) * kBlockBytes + (uint32_t)r * 128u + (uint32_t)(((ch & 7) ^ (r & 7)) << 4);
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr));
+}
+
+// Registers are dealt out anew once the block runs: 384 threads x 168 at launch = 128 (copies and products) x 88 + 256 x 208.
+__device__ inline void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
+__device__ inline void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
+
+// 32 rows (a quarter of a tile) -> shared memory.  A lane keeps to one 16-byte chunk of the rows, 8 NB lanes side by side take a row;
+// chunks: those that the products read, of which `real` exist (the others are zeros); any: an address that may be named where
+// nothing is read.  copy_rows: rows `stride` elements apart, those whose bit in `word` is off are zeros.  copy_each: the lane's own row
+// (its first element of the head), null for zeros.
+template <int NB> __device__ inline uint32_t chunk_place(uint32_t tile, int part, int lane)
+{
+    const int ch = lane & (8 * NB - 1), row = lane / (8 * NB);
+    return tile + (uint32_t)(ch >> 3) * kBlockBytes + (uint32_t)(part * 32 + row) * 128u + (uint32_t)(((ch & 7) ^ row) << 4);
+}
+template <int NB>
+__device__ inline void copy_rows(uint32_t tile, int part, const bf16 *first, int64_t stride, uint32_t word, const void *any, int chunks, int real,
+                                 int lane)
+{
+    constexpr int kPer = 4 / NB;                          // rows per step
+    const int ch = lane & (8 * NB - 1), row = lane / (8 * NB);
+    if (ch >= chunks) return;
+    const uint32_t dst = chunk_place<NB>(tile, part, lane);
+    const bf16 *src = first + row * stride + ch * 8;
+    const int64_t step = stride * kPer;
+    word = ch < real ? word >> row : 0u;
+#pragma unroll
+    for (int i = 0; i < 8 * NB; ++i) {
+        const bool on = (word >> (i * kPer)) & 1u;
+        // row * 128, and the swizzle's exclusive or of the row's low bits with the chunk
+        cp_async16((dst ^ (uint32_t)(((i * kPer) & 7) << 4)) + (uint32_t)(i * kPer) * 128u, on ? static_cast<const void *>(src) : any, on);
+        src += step;
+    }
+}
+template <int NB>
+__device__ inline void copy_each(uint32_t tile, int part, const bf16 *mine, const void *any, int chunks, int real, int lane)
+{
+    constexpr int kPer = 4 / NB;
+    const int ch = lane & (8 * NB - 1), row = lane / (8 * NB);
+    const uint32_t dst = chunk_place<NB>(tile, part, lane);
+#pragma unroll
+    for (int i = 0; i < 8 * NB; ++i) {
+        const uint64_t p = __shfl_sync(0xFFFFFFFFu, reinterpret_cast<uint64_t>(mine), row + i * kPer);
         const bool on = p != 0 && ch < real;
-        cp_async16(dst, on ? reinterpret_cast<const bf16 *>(p) + ch * 8 : any, on);
-        row += dr;
-        ch += dc;
-        if (ch >= chunks) { ch -= chunks; ++row; }
+        if (ch < chunks)
+            cp_async16((dst ^ (uint32_t)(((i * kPer) & 7) << 4)) + (uint32_t)(i * kPer) * 128u,
+                       on ? static_cast<const void *>(reinterpret_cast<const bf16 *>(p) + ch * 8) : any, on);
     }
 }
 
@@ -119,14 +160,13 @@ __device__ inline bool wait_slot(uint64_t *bar, uint32_t parity, Pending &pend, 
 }
 
 // ------------------------------------------------------------------------------------------------- forward
-constexpr int kFwdThreads = 13 * 32;                 // two warpgroups of softmax, four loading warps, the products' warp
 constexpr int kFwdRows = 2 * kTile;                  // rows of a block: one tile per softmax warpgroup
 
 template <int NB> constexpr int fwd_stages() { return NB == 2 ? 5 : 8; }
 template <int NB> constexpr size_t fwd_smem() { return 1024 + (size_t)(2 + fwd_stages<NB>()) * NB * kBlockBytes; }
 
 template <int NB>
-__global__ void __launch_bounds__(kFwdThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, float *__restrict__ part_o, float2 *__restrict__ part_ml)
 {
     constexpr int kStages = NB == 2 ? 5 : 8, kTileBytes = NB * kBlockBytes;
@@ -157,10 +197,10 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&kv_full[s], 4);
+            mbar_init(&kv_full[s], kLoaders);
             mbar_init(&kv_empty[s], 1);
         }
-        mbar_init(&q_full, 4);
+        mbar_init(&q_full, kLoaders);
         mbar_init(&q_empty, 1);
         for (int t = 0; t < 2; ++t) {
             mbar_init(&s_full[t], 1);
@@ -172,7 +212,7 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == 12) {
+    if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -181,7 +221,9 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
     tc_fence_after();
     const uint32_t tmem = tmem_slot;                  // scores (and p) of tile t: columns 128 t; outputs: 256 + 64 NB t
 
-    if (warp >= 8 && warp < 12) {
+    if (warp >= 8) {
+    fewer_registers();
+    if (warp < kMmaWarp) {
         // ---- copies: queries of a block of rows, then keys and values in turn
         const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8;
         Pending pend;
@@ -190,33 +232,41 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
         for (int64_t t = t0; t * kFwdRows < rows && n > 0 && ok; t += tiles, ++item) {
             if (item > 0) ok = wait_slot(&q_empty, (item - 1) & 1u, pend, lane, &abort_flag);
             if (!ok) break;
-            for (int q = 0; q < 2; ++q) {
-                const int64_t r = t * kFwdRows + q * kTile + w * 32 + lane;
+            for (int b = w; b < kFwdRows / 32; b += kLoaders) {
+                const int64_t r = t * kFwdRows + b * 32 + lane;
                 const bf16 *src = nullptr;
                 if (r < rows) {
                     const int64_t i = r / a.group;
                     src = static_cast<const bf16 *>(a.q) + (rg.q0 + i) * a.ldq + (h * a.group + (int)(r - i * a.group)) * (int64_t)a.head_dim;
                 }
-                load_rows(q_smem + q * kTileBytes, w * 32, src, a.q, chunks, real, lane);
+                copy_each<NB>(q_smem + (b >> 2) * kTileBytes, b & 3, src, a.q, chunks, real, lane);
             }
             pend.push(&q_full, lane);
             for (int j = 0; j < n && ok; ++j, ++jj) {
-                const int64_t key = kb + (int64_t)j * kTile + w * 32 + lane;
-                const bool seen = key < ke && (!a.mask || a.mask[key]);
-                const uint32_t word = __ballot_sync(0xFFFFFFFFu, seen);
+                uint32_t word[4 / kLoaders];
+#pragma unroll
+                for (int b = 0; b < 4 / kLoaders; ++b) {
+                    const int64_t key = kb + (int64_t)j * kTile + (w + b * kLoaders) * 32 + lane;
+                    word[b] = __ballot_sync(0xFFFFFFFFu, key < ke && (!a.mask || a.mask[key]));
+                }
                 for (int v = 0; v < 2; ++v, ++g) {
                     const uint32_t s = g % kStages;
                     if (g >= kStages) ok = wait_slot(&kv_empty[s], (g / kStages - 1) & 1u, pend, lane, &abort_flag);
                     if (!ok) break;
-                    if (v == 0 && lane == 0) words[jj % kWordRing][w] = word;
-                    const bf16 *src = static_cast<const bf16 *>(v ? a.v : a.k) + key * (v ? a.ldv : a.ldk) + h * (int64_t)a.head_dim;
-                    load_rows(kv_smem + s * kTileBytes, w * 32, seen ? src : nullptr, a.q, chunks, real, lane);
+#pragma unroll
+                    for (int b = 0; b < 4 / kLoaders; ++b) {
+                        const int part = w + b * kLoaders;
+                        const int64_t key = kb + (int64_t)j * kTile + part * 32, ld = v ? a.ldv : a.ldk;
+                        if (v == 0 && lane == 0) words[jj % kWordRing][part] = word[b];
+                        copy_rows<NB>(kv_smem + s * kTileBytes, part, static_cast<const bf16 *>(v ? a.v : a.k) + key * ld + h * (int64_t)a.head_dim, ld,
+                                      word[b], a.q, chunks, real, lane);
+                    }
                     pend.push(&kv_full[s], lane);
                 }
             }
         }
         pend.flush(lane);
-    } else if (warp == 12) {
+    } else if (warp == kMmaWarp) {
         // ---- products
         if (lane == 0) {
             const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
@@ -272,7 +322,9 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
                 }
             }
         }
+    }
     } else {
+        more_registers();
         // ---- softmax of tile `q`, one row per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
@@ -293,56 +345,58 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
                 uint32_t word[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) word[c] = words[jj % kWordRing][c];
-                float top = -INFINITY;
+                // the row's 128 scores stay in registers; four chains for the maximum
+                uint32_t v[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_load32_async(s_addr + c * 32, v[c]);
+                tmem_load_wait();
+                float tops[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    uint32_t v[32];
-                    tmem_load32_async(s_addr + c * 32, v);
-                    tmem_load_wait();
                     if (word[c] != 0xFFFFFFFFu) {
 #pragma unroll
                         for (int i = 0; i < 32; ++i)
-                            if (!((word[c] >> i) & 1u)) v[i] = 0xFF800000u;
+                            if (!((word[c] >> i) & 1u)) v[c][i] = 0xFF800000u;
                     }
+                    tops[c] = __uint_as_float(v[c][0]);
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) top = fmaxf(top, __uint_as_float(v[i]));
+                    for (int i = 1; i < 32; ++i) tops[c] = fmaxf(tops[c], __uint_as_float(v[c][i]));
                 }
+                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                 // The maximum that p and l refer to moves only where a score exceeds it by 8 in the exponent: p <= 2^8 loses
                 // nothing in floating point, and the sums so far are rescaled seldom.
                 const bool moves = top * c1 > m * c1 + 8.f || m == -INFINITY;
                 if (j > 0 && __any_sync(0xFFFFFFFFu, moves && top != -INFINITY)) {
                     const float f = moves && top != -INFINITY ? exp2_approx((m - top) * c1) : 1.f;
                     l *= f;
-                    for (int c = 0; c < NB * 2; ++c) {
-                        uint32_t v[32];
-                        tmem_load32_async(o_addr + c * 32, v);
+                    for (int c = 0; c < NB * 4; ++c) {
+                        uint32_t x[16];
+                        tmem_load16_async(o_addr + c * 16, x);
                         tmem_load_wait();
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * f);
-                        tmem_store32(o_addr + c * 32, v);
+                        for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
+                        tmem_store16(o_addr + c * 16, x);
                     }
                 }
                 if (moves) m = top;
                 const float base = m == -INFINITY ? 0.f : m * c1;
-                float sum = 0.f;
+                const float2 scale2 = make_float2(c1, c1), base2 = make_float2(-base, -base);
+                float2 sums[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    uint32_t v[32], p[16];
-                    tmem_load32_async(s_addr + c * 32, v);
-                    tmem_load_wait();
-                    if (word[c] != 0xFFFFFFFFu) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (!((word[c] >> i) & 1u)) v[i] = 0xFF800000u;
-                    }
+                    uint32_t p[16];
+                    sums[c] = make_float2(0.f, 0.f);
 #pragma unroll
                     for (int i = 0; i < 32; i += 2) {
-                        const float x = exp2_approx(fmaf(__uint_as_float(v[i]), c1, -base)), y = exp2_approx(fmaf(__uint_as_float(v[i + 1]), c1, -base));
-                        sum += x + y;
-                        p[i / 2] = pack_bf16(x, y);
+                        float2 x = __ffma2_rn(make_float2(__uint_as_float(v[c][i]), __uint_as_float(v[c][i + 1])), scale2, base2);
+                        x.x = exp2_approx(x.x);
+                        x.y = exp2_approx(x.y);
+                        sums[c] = __fadd2_rn(sums[c], x);
+                        p[i / 2] = pack_bf16(x.x, x.y);
                     }
                     tmem_store16(s_addr + c * 16, p);
                 }
+                const float sum = (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y) + ((sums[2].x + sums[2].y) + (sums[3].x + sums[3].y));
                 l += sum;
                 tmem_store_wait();
                 tc_fence_before();
@@ -399,14 +453,12 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && abort_flag && a.status) atomicOr(reinterpret_cast<unsigned *>(a.status), E2EGREC_DEV_TIMEOUT);
-    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 // ------------------------------------------------------------------------------------------------- backward
 // Two kernels, so that no gradient is added up by atomics: dQ goes over the keys of a tile of rows, dK and dV over the rows of a
 // tile of keys; the scores are formed in both.  Two warpgroups share a tile of 128 x 128: 64 columns each, one row per thread.
-constexpr int kBwdThreads = 13 * 32;
-
 template <int NB> constexpr size_t dq_smem() { return 1024 + (size_t)(2 + fwd_stages<NB>()) * NB * kBlockBytes; }
 template <int NB> constexpr size_t dkv_smem() { return 1024 + (size_t)(2 + 4) * NB * kBlockBytes; }
 
@@ -446,7 +498,7 @@ __device__ inline void store_row(uint32_t taddr, bf16 *out, int head_dim, float 
 
 // dQ, and D = dO . out of every row for the other kernel
 template <int NB>
-__global__ void __launch_bounds__(kBwdThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restrict__ dots)
 {
     constexpr int kStages = NB == 2 ? 5 : 8, kTileBytes = NB * kBlockBytes;
@@ -472,10 +524,10 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&kv_full[s], 4);
+            mbar_init(&kv_full[s], kLoaders);
             mbar_init(&kv_empty[s], 1);
         }
-        mbar_init(&q_full, 4);
+        mbar_init(&q_full, kLoaders);
         mbar_init(&q_empty, 1);
         mbar_init(&s_full[0], 1);
         mbar_init(&s_full[1], 1);
@@ -487,7 +539,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == 12) {
+    if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -496,7 +548,9 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
     tc_fence_after();
     const uint32_t tmem = tmem_slot;                  // scores: columns 0 and 128 in turn; dP and dS: 256; dQ: 384
 
-    if (warp >= 8 && warp < 12) {
+    if (warp >= 8) {
+    fewer_registers();
+    if (warp < kMmaWarp) {
         // ---- copies: Q and dO of a tile of rows, then keys and values in turn
         const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8;
         Pending pend;
@@ -505,28 +559,38 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
         for (int64_t t = t0; t * kTile < rows && n > 0 && ok; t += tiles, ++item) {
             if (item > 0) ok = wait_slot(&q_empty, (item - 1) & 1u, pend, lane, &abort_flag);
             if (!ok) break;
-            const int64_t r = t * kTile + w * 32 + lane, i = r / a.group;
-            const int64_t col = (h * a.group + (int)(r - i * a.group)) * (int64_t)a.head_dim;
-            load_rows(q_smem, w * 32, r < rows ? static_cast<const bf16 *>(a.q) + (rg.q0 + i) * a.ldq + col : nullptr, a.q, chunks, real, lane);
-            load_rows(g_smem, w * 32, r < rows ? static_cast<const bf16 *>(a.dout) + (rg.q0 + i) * a.ldg + col : nullptr, a.q, chunks, real, lane);
+            for (int b = w; b < 4; b += kLoaders) {
+                const int64_t r = t * kTile + b * 32 + lane, i = r / a.group;
+                const int64_t col = (h * a.group + (int)(r - i * a.group)) * (int64_t)a.head_dim;
+                copy_each<NB>(q_smem, b, r < rows ? static_cast<const bf16 *>(a.q) + (rg.q0 + i) * a.ldq + col : nullptr, a.q, chunks, real, lane);
+                copy_each<NB>(g_smem, b, r < rows ? static_cast<const bf16 *>(a.dout) + (rg.q0 + i) * a.ldg + col : nullptr, a.q, chunks, real, lane);
+            }
             pend.push(&q_full, lane);
             for (int j = 0; j < n && ok; ++j, ++jj) {
-                const int64_t key = rg.k0 + (int64_t)j * kTile + w * 32 + lane;
-                const bool seen = key < rg.k1 && (!a.mask || a.mask[key]);
-                const uint32_t word = __ballot_sync(0xFFFFFFFFu, seen);
+                uint32_t word[4 / kLoaders];
+#pragma unroll
+                for (int b = 0; b < 4 / kLoaders; ++b) {
+                    const int64_t key = rg.k0 + (int64_t)j * kTile + (w + b * kLoaders) * 32 + lane;
+                    word[b] = __ballot_sync(0xFFFFFFFFu, key < rg.k1 && (!a.mask || a.mask[key]));
+                }
                 for (int v = 0; v < 2; ++v, ++g) {
                     const uint32_t s = g % kStages;
                     if (g >= kStages) ok = wait_slot(&kv_empty[s], (g / kStages - 1) & 1u, pend, lane, &abort_flag);
                     if (!ok) break;
-                    if (v == 0 && lane == 0) words[jj % kWordRing][w] = word;
-                    const bf16 *src = static_cast<const bf16 *>(v ? a.v : a.k) + key * (v ? a.ldv : a.ldk) + h * (int64_t)a.head_dim;
-                    load_rows(kv_smem + s * kTileBytes, w * 32, seen ? src : nullptr, a.q, chunks, real, lane);
+#pragma unroll
+                    for (int b = 0; b < 4 / kLoaders; ++b) {
+                        const int part = w + b * kLoaders;
+                        const int64_t key = rg.k0 + (int64_t)j * kTile + part * 32, ld = v ? a.ldv : a.ldk;
+                        if (v == 0 && lane == 0) words[jj % kWordRing][part] = word[b];
+                        copy_rows<NB>(kv_smem + s * kTileBytes, part, static_cast<const bf16 *>(v ? a.v : a.k) + key * ld + h * (int64_t)a.head_dim, ld,
+                                      word[b], a.q, chunks, real, lane);
+                    }
                     pend.push(&kv_full[s], lane);
                 }
             }
         }
         pend.flush(lane);
-    } else if (warp == 12) {
+    } else if (warp == kMmaWarp) {
         // ---- products.  S of the next tile goes out before dQ waits for dS, dP of the next tile behind dQ (whose operand it
         // overwrites): the warpgroups form p of the next tile beside dQ and dP.
         if (lane == 0) {
@@ -580,7 +644,9 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
                 }
             }
         }
+    }
     } else {
+        more_registers();
         // ---- p and dS: 64 columns of one row per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
@@ -613,14 +679,15 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 tc_fence_after();
                 float p[64];
+                uint32_t v0[2][32];
+                tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64, v0[0]);
+                tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64 + 32, v0[1]);
+                tmem_load_wait();
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const uint32_t word = words[jj % kWordRing][q * 2 + c];
-                    uint32_t v[32];
-                    tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64 + c * 32, v);
-                    tmem_load_wait();
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) p[c * 32 + e] = exp2_approx(fmaf(__uint_as_float(v[e]), c1, -base));
+                    for (int e = 0; e < 32; ++e) p[c * 32 + e] = exp2_approx(fmaf(__uint_as_float(v0[c][e]), c1, -base));
                     if (word != 0xFFFFFFFFu) {
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
@@ -630,13 +697,14 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
                 ok = mbar_wait(&dp_full, jj & 1u, &abort_flag);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 tc_fence_after();
+                uint32_t v1[2][32];
+                tmem_load32_async(tmem + lanes + 256 + q * 64, v1[0]);
+                tmem_load32_async(tmem + lanes + 256 + q * 64 + 32, v1[1]);
+                tmem_load_wait();
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    uint32_t v[32];
-                    tmem_load32_async(tmem + lanes + 256 + q * 64 + c * 32, v);
-                    tmem_load_wait();
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) p[c * 32 + e] *= __uint_as_float(v[e]) - dot;
+                    for (int e = 0; e < 32; ++e) p[c * 32 + e] *= __uint_as_float(v1[c][e]) - dot;
                 }
                 store_operand(tmem + lanes + 256 + q * 64, p);
                 tmem_store_wait();
@@ -660,12 +728,12 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && abort_flag && a.status) atomicOr(reinterpret_cast<unsigned *>(a.status), E2EGREC_DEV_TIMEOUT);
-    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 // dK and dV of a tile of keys: S^T = K Q^T and dP^T = V dO^T over the rows of the sequence
 template <int NB>
-__global__ void __launch_bounds__(kBwdThreads, 1)
+__global__ void __launch_bounds__(kThreads, 1)
 attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *__restrict__ dots)
 {
     constexpr int kStages = 4, kTileBytes = NB * kBlockBytes, kStatRing = 4;
@@ -691,10 +759,10 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&qg_full[s], 4);
+            mbar_init(&qg_full[s], kLoaders);
             mbar_init(&qg_empty[s], 1);
         }
-        mbar_init(&kv_full, 4);
+        mbar_init(&kv_full, kLoaders);
         mbar_init(&kv_empty, 1);
         mbar_init(&s_full, 1);
         mbar_init(&p_full, 8);
@@ -706,7 +774,7 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == 12) {
+    if (warp == kMmaWarp) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -715,7 +783,9 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
     tc_fence_after();
     const uint32_t tmem = tmem_slot;                  // S^T and P^T: columns 0; dP^T and dS^T: 128; dV: 256; dK: 384
 
-    if (warp >= 8 && warp < 12) {
+    if (warp >= 8) {
+    fewer_registers();
+    if (warp < kMmaWarp) {
         // ---- copies: keys and values of a tile, then Q and dO of the rows in turn, with the rows' lse and D
         const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8, heads = a.kv_heads * a.group;
         Pending pend;
@@ -724,39 +794,52 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
         for (int64_t t = t0; t * kTile < keys && n > 0 && ok; t += tiles, ++item) {
             if (item > 0) ok = wait_slot(&kv_empty, (item - 1) & 1u, pend, lane, &abort_flag);
             if (!ok) break;
-            const int64_t key = rg.k0 + t * kTile + w * 32 + lane;
-            const bool seen = key < rg.k1 && (!a.mask || a.mask[key]);
-            load_rows(k_smem, w * 32, seen ? static_cast<const bf16 *>(a.k) + key * a.ldk + h * (int64_t)a.head_dim : nullptr, a.q, chunks, real, lane);
-            load_rows(v_smem, w * 32, seen ? static_cast<const bf16 *>(a.v) + key * a.ldv + h * (int64_t)a.head_dim : nullptr, a.q, chunks, real, lane);
+            for (int b = w; b < 4; b += kLoaders) {
+                const int64_t key = rg.k0 + t * kTile + b * 32 + lane;
+                const bool seen = key < rg.k1 && (!a.mask || a.mask[key]);
+                copy_each<NB>(k_smem, b, seen ? static_cast<const bf16 *>(a.k) + key * a.ldk + h * (int64_t)a.head_dim : nullptr, a.q, chunks, real, lane);
+                copy_each<NB>(v_smem, b, seen ? static_cast<const bf16 *>(a.v) + key * a.ldv + h * (int64_t)a.head_dim : nullptr, a.q, chunks, real, lane);
+            }
             pend.push(&kv_full, lane);
             for (int j = 0; j < n && ok; ++j, ++jj) {
-                const int64_t r = (int64_t)j * kTile + w * 32 + lane, i = r / a.group;
-                const int head = h * a.group + (int)(r - i * a.group);
-                const int64_t row = rg.q0 + i, col = (int64_t)head * a.head_dim;
-                float l = INFINITY, d = 0.f;
-                if (r < rows) {
-                    const float x = a.lse[row * heads + head];
-                    if (x != -INFINITY) {
-                        l = x * kLog2e;
-                        d = dots[row * heads + head];
+                int64_t row[4 / kLoaders], col[4 / kLoaders];
+                float l[4 / kLoaders], d[4 / kLoaders];
+#pragma unroll
+                for (int b = 0; b < 4 / kLoaders; ++b) {
+                    const int64_t r = (int64_t)j * kTile + (w + b * kLoaders) * 32 + lane, i = r / a.group;
+                    const int head = h * a.group + (int)(r - i * a.group);
+                    row[b] = rg.q0 + i;
+                    col[b] = (int64_t)head * a.head_dim;
+                    l[b] = INFINITY;
+                    d[b] = 0.f;
+                    if (r < rows) {
+                        const float x = a.lse[row[b] * heads + head];
+                        if (x != -INFINITY) {
+                            l[b] = x * kLog2e;
+                            d[b] = dots[row[b] * heads + head];
+                        }
                     }
                 }
                 for (int v = 0; v < 2; ++v, ++g) {
                     const uint32_t s = g % kStages;
                     if (g >= kStages) ok = wait_slot(&qg_empty[s], (g / kStages - 1) & 1u, pend, lane, &abort_flag);
                     if (!ok) break;
-                    if (v == 0) {
-                        stat_lse[jj % kStatRing][w * 32 + lane] = l;
-                        stat_dot[jj % kStatRing][w * 32 + lane] = d;
+#pragma unroll
+                    for (int b = 0; b < 4 / kLoaders; ++b) {
+                        const int part = w + b * kLoaders;
+                        if (v == 0) {
+                            stat_lse[jj % kStatRing][part * 32 + lane] = l[b];
+                            stat_dot[jj % kStatRing][part * 32 + lane] = d[b];
+                        }
+                        const bf16 *src = v ? static_cast<const bf16 *>(a.dout) + row[b] * a.ldg + col[b] : static_cast<const bf16 *>(a.q) + row[b] * a.ldq + col[b];
+                        copy_each<NB>(qg_smem + s * kTileBytes, part, l[b] != INFINITY ? src : nullptr, a.q, chunks, real, lane);
                     }
-                    const bf16 *src = v ? static_cast<const bf16 *>(a.dout) + row * a.ldg + col : static_cast<const bf16 *>(a.q) + row * a.ldq + col;
-                    load_rows(qg_smem + s * kTileBytes, w * 32, l != INFINITY ? src : nullptr, a.q, chunks, real, lane);
                     pend.push(&qg_full[s], lane);
                 }
             }
         }
         pend.flush(lane);
-    } else if (warp == 12) {
+    } else if (warp == kMmaWarp) {
         // ---- products.  S^T of the next tile follows dV, whose operand it overwrites, dP^T follows dK: the warpgroups form dS
         // beside dV and the next S^T, and the next p beside dK and the next dP^T.
         if (lane == 0) {
@@ -816,7 +899,9 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
                 }
             }
         }
+    }
     } else {
+        more_registers();
         // ---- p and dS: 64 columns (rows of Q) of one key per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
@@ -833,18 +918,19 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
                 const float4 *lse4 = reinterpret_cast<const float4 *>(stat_lse[jj % kStatRing] + q * 64);
                 const float4 *dot4 = reinterpret_cast<const float4 *>(stat_dot[jj % kStatRing] + q * 64);
                 float p[64];
+                uint32_t v0[2][32];
+                tmem_load32_async(tmem + lanes + q * 64, v0[0]);
+                tmem_load32_async(tmem + lanes + q * 64 + 32, v0[1]);
+                tmem_load_wait();
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    uint32_t v[32];
-                    tmem_load32_async(tmem + lanes + q * 64 + c * 32, v);
-                    tmem_load_wait();
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float4 l = lse4[c * 8 + e];
-                        p[c * 32 + 4 * e] = exp2_approx(fmaf(__uint_as_float(v[4 * e]), c1, -l.x));
-                        p[c * 32 + 4 * e + 1] = exp2_approx(fmaf(__uint_as_float(v[4 * e + 1]), c1, -l.y));
-                        p[c * 32 + 4 * e + 2] = exp2_approx(fmaf(__uint_as_float(v[4 * e + 2]), c1, -l.z));
-                        p[c * 32 + 4 * e + 3] = exp2_approx(fmaf(__uint_as_float(v[4 * e + 3]), c1, -l.w));
+                        p[c * 32 + 4 * e] = exp2_approx(fmaf(__uint_as_float(v0[c][4 * e]), c1, -l.x));
+                        p[c * 32 + 4 * e + 1] = exp2_approx(fmaf(__uint_as_float(v0[c][4 * e + 1]), c1, -l.y));
+                        p[c * 32 + 4 * e + 2] = exp2_approx(fmaf(__uint_as_float(v0[c][4 * e + 2]), c1, -l.z));
+                        p[c * 32 + 4 * e + 3] = exp2_approx(fmaf(__uint_as_float(v0[c][4 * e + 3]), c1, -l.w));
                     }
                 }
                 store_operand(tmem + lanes + q * 64, p);
@@ -855,18 +941,19 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
                 ok = mbar_wait(&dp_full, jj & 1u, &abort_flag);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 tc_fence_after();
+                uint32_t v1[2][32];
+                tmem_load32_async(tmem + lanes + 128 + q * 64, v1[0]);
+                tmem_load32_async(tmem + lanes + 128 + q * 64 + 32, v1[1]);
+                tmem_load_wait();
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
-                    uint32_t v[32];
-                    tmem_load32_async(tmem + lanes + 128 + q * 64 + c * 32, v);
-                    tmem_load_wait();
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float4 d = dot4[c * 8 + e];
-                        p[c * 32 + 4 * e] *= __uint_as_float(v[4 * e]) - d.x;
-                        p[c * 32 + 4 * e + 1] *= __uint_as_float(v[4 * e + 1]) - d.y;
-                        p[c * 32 + 4 * e + 2] *= __uint_as_float(v[4 * e + 2]) - d.z;
-                        p[c * 32 + 4 * e + 3] *= __uint_as_float(v[4 * e + 3]) - d.w;
+                        p[c * 32 + 4 * e] *= __uint_as_float(v1[c][4 * e]) - d.x;
+                        p[c * 32 + 4 * e + 1] *= __uint_as_float(v1[c][4 * e + 1]) - d.y;
+                        p[c * 32 + 4 * e + 2] *= __uint_as_float(v1[c][4 * e + 2]) - d.z;
+                        p[c * 32 + 4 * e + 3] *= __uint_as_float(v1[c][4 * e + 3]) - d.w;
                     }
                 }
                 store_operand(tmem + lanes + 128 + q * 64, p);
@@ -893,7 +980,7 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && abort_flag && a.status) atomicOr(reinterpret_cast<unsigned *>(a.status), E2EGREC_DEV_TIMEOUT);
-    if (warp == 12) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 constexpr int kMaxDevices = 64;
@@ -918,8 +1005,8 @@ bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, float *p
     if (!(one ? allow_smem(attn_tc_fwd_kernel<1>, fwd_smem<1>(), done[0]) : allow_smem(attn_tc_fwd_kernel<2>, fwd_smem<2>(), done[1]))) return false;
     const unsigned grid = (unsigned)(a.n_seq * a.kv_heads * tiles * splits);
     note_launch();
-    if (one) attn_tc_fwd_kernel<1><<<grid, kFwdThreads, fwd_smem<1>(), st>>>(a, (int)tiles, splits, part_o, part_ml);
-    else attn_tc_fwd_kernel<2><<<grid, kFwdThreads, fwd_smem<2>(), st>>>(a, (int)tiles, splits, part_o, part_ml);
+    if (one) attn_tc_fwd_kernel<1><<<grid, kThreads, fwd_smem<1>(), st>>>(a, (int)tiles, splits, part_o, part_ml);
+    else attn_tc_fwd_kernel<2><<<grid, kThreads, fwd_smem<2>(), st>>>(a, (int)tiles, splits, part_o, part_ml);
     return true;
 }
 
@@ -933,13 +1020,13 @@ bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, 
     const int64_t units = a.n_seq * a.kv_heads;
     if (a.q_rows) {
         note_launch();
-        if (one) attn_tc_dq_kernel<1><<<(unsigned)(units * q_tiles), kBwdThreads, dq_smem<1>(), st>>>(a, (int)q_tiles, dots);
-        else attn_tc_dq_kernel<2><<<(unsigned)(units * q_tiles), kBwdThreads, dq_smem<2>(), st>>>(a, (int)q_tiles, dots);
+        if (one) attn_tc_dq_kernel<1><<<(unsigned)(units * q_tiles), kThreads, dq_smem<1>(), st>>>(a, (int)q_tiles, dots);
+        else attn_tc_dq_kernel<2><<<(unsigned)(units * q_tiles), kThreads, dq_smem<2>(), st>>>(a, (int)q_tiles, dots);
     }
     if (a.k_rows) {
         note_launch();
-        if (one) attn_tc_dkv_kernel<1><<<(unsigned)(units * k_tiles), kBwdThreads, dkv_smem<1>(), st>>>(a, (int)k_tiles, dots);
-        else attn_tc_dkv_kernel<2><<<(unsigned)(units * k_tiles), kBwdThreads, dkv_smem<2>(), st>>>(a, (int)k_tiles, dots);
+        if (one) attn_tc_dkv_kernel<1><<<(unsigned)(units * k_tiles), kThreads, dkv_smem<1>(), st>>>(a, (int)k_tiles, dots);
+        else attn_tc_dkv_kernel<2><<<(unsigned)(units * k_tiles), kThreads, dkv_smem<2>(), st>>>(a, (int)k_tiles, dots);
     }
     return true;
 }
