@@ -109,54 +109,44 @@ __device__ inline void copy_each(uint32_t tile, int part, const bf16 *mine, cons
     }
 }
 
-// Copies that a loading warp has started and not yet announced: the barrier of a tile is arrived at once the warp's copies for
-// it have landed and are visible to the tensor cores; up to three tiles stay under way.
-struct Pending {
-    uint64_t *bar[3] = {nullptr, nullptr, nullptr};
-    __device__ void announce(uint64_t *b, int lane)
-    {
-        if (!b) return;
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) mbar_arrive(b);
-    }
-    __device__ void push(uint64_t *b, int lane)
-    {
-        cp_async_commit();
-        if (bar[2]) {
-            cp_async_wait<3>();
-            announce(bar[2], lane);
-        }
-        bar[2] = bar[1];
-        bar[1] = bar[0];
-        bar[0] = b;
-    }
-    __device__ void flush(int lane)
-    {
-        cp_async_wait<0>();
-        for (int i = 2; i >= 0; --i) {
-            announce(bar[i], lane);
-            bar[i] = nullptr;
-        }
-    }
-};
-
-__device__ inline bool mbar_test(uint64_t *bar, uint32_t parity)
+// A tile's barrier is arrived at by every lane of the loading warps as soon as the lane's copies have landed, without anybody waiting
+// for them, and once more per warp for what it wrote itself (visibility words, statistics of rows).  The lane that issues the products
+// makes the landed bytes visible to the tensor cores (tile_ready).
+constexpr uint32_t kTileArrivals = kLoaders * 33;
+__device__ inline void announce(uint64_t *bar, int lane)
 {
-    uint32_t done;
-    asm volatile("{\n.reg .pred p;\nmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}\n"
-                 : "=r"(done)
-                 : "r"(smem_u32(bar)), "r"(parity)
-                 : "memory");
-    return done != 0;
+    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
+    __syncwarp();
+    if (lane == 0) mbar_arrive(bar);
+}
+__device__ inline bool tile_ready(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
+{
+    const bool ok = mbar_wait(bar, parity, abort_flag);
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    tc_fence_after();
+    return ok;
+}
+// all lanes of a warp
+__device__ inline bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
+{
+    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag));
 }
 
-// A slot of a ring that the tensor cores may still read: what is under way is announced before the warp waits for it
-__device__ inline bool wait_slot(uint64_t *bar, uint32_t parity, Pending &pend, int lane, volatile int *abort_flag)
+// Products of one tile, K step by K step, with descriptors that move on by constants: the instruction stream of the one issuing lane
+// is what feeds the tensor cores (with descriptors built anew for every step an instruction took 122 cycles, its execution 64).
+// head_steps: d = A B^T over the head (both operands' K index contiguous); row_steps: d (+)= A B over 128 rows, A in tensor memory
+// with its steps 4 to 7 `second` columns behind where they would follow, B's N index contiguous.
+template <int NB> __device__ inline void head_steps(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, int ksteps)
 {
-    if (__all_sync(0xFFFFFFFFu, mbar_test(bar, parity))) return true;
-    pend.flush(lane);
-    return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag));
+#pragma unroll
+    for (int k = 0; k < 4 * NB; ++k)
+        if (k < ksteps) umma(d, desc_at(a, (k >> 2) * kBlockBytes + (k & 3) * 32), desc_at(b, (k >> 2) * kBlockBytes + (k & 3) * 32), idesc, k > 0);
+}
+__device__ inline void row_steps(uint32_t d, uint32_t a, uint32_t second, uint64_t b, uint32_t idesc, bool add)
+{
+#pragma unroll
+    for (int k = 0; k < kTile / 16; ++k)
+        umma_ts(d, a + k * 8 + (k >= 4 ? second : 0), desc_at(b, k * 2048), idesc, k > 0 ? 1u : (uint32_t)add);
 }
 
 // ------------------------------------------------------------------------------------------------- forward
@@ -197,10 +187,10 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&kv_full[s], kLoaders);
+            mbar_init(&kv_full[s], kTileArrivals);
             mbar_init(&kv_empty[s], 1);
         }
-        mbar_init(&q_full, kLoaders);
+        mbar_init(&q_full, kTileArrivals);
         mbar_init(&q_empty, 1);
         for (int t = 0; t < 2; ++t) {
             mbar_init(&s_full[t], 1);
@@ -226,11 +216,10 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
     if (warp < kMmaWarp) {
         // ---- copies: queries of a block of rows, then keys and values in turn
         const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8;
-        Pending pend;
         uint32_t g = 0, jj = 0, item = 0;
         bool ok = true;
         for (int64_t t = t0; t * kFwdRows < rows && n > 0 && ok; t += tiles, ++item) {
-            if (item > 0) ok = wait_slot(&q_empty, (item - 1) & 1u, pend, lane, &abort_flag);
+            if (item > 0) ok = warp_wait(&q_empty, (item - 1) & 1u, &abort_flag);
             if (!ok) break;
             for (int b = w; b < kFwdRows / 32; b += kLoaders) {
                 const int64_t r = t * kFwdRows + b * 32 + lane;
@@ -241,7 +230,7 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
                 }
                 copy_each<NB>(q_smem + (b >> 2) * kTileBytes, b & 3, src, a.q, chunks, real, lane);
             }
-            pend.push(&q_full, lane);
+            announce(&q_full, lane);
             for (int j = 0; j < n && ok; ++j, ++jj) {
                 uint32_t word[4 / kLoaders];
 #pragma unroll
@@ -251,7 +240,7 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
                 }
                 for (int v = 0; v < 2; ++v, ++g) {
                     const uint32_t s = g % kStages;
-                    if (g >= kStages) ok = wait_slot(&kv_empty[s], (g / kStages - 1) & 1u, pend, lane, &abort_flag);
+                    if (g >= kStages) ok = warp_wait(&kv_empty[s], (g / kStages - 1) & 1u, &abort_flag);
                     if (!ok) break;
 #pragma unroll
                     for (int b = 0; b < 4 / kLoaders; ++b) {
@@ -261,52 +250,45 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
                         copy_rows<NB>(kv_smem + s * kTileBytes, part, static_cast<const bf16 *>(v ? a.v : a.k) + key * ld + h * (int64_t)a.head_dim, ld,
                                       word[b], a.q, chunks, real, lane);
                     }
-                    pend.push(&kv_full[s], lane);
+                    announce(&kv_full[s], lane);
                 }
             }
         }
-        pend.flush(lane);
+        cp_async_wait_all();
     } else if (warp == kMmaWarp) {
         // ---- products
-        if (lane == 0) {
+        if (elect_one()) {
             const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
             uint32_t g = 0, item = 0, pc[2] = {0, 0};
             bool ok = true;
             for (int64_t t = t0; t * kFwdRows < rows && n > 0 && ok; t += tiles, ++item) {
                 const int nt = rows - t * kFwdRows > kTile ? 2 : 1;
-                ok = mbar_wait(&q_full, item & 1u, &abort_flag);
+                ok = tile_ready(&q_full, item & 1u, &abort_flag);
                 if (item > 0)
                     for (int q = 0; q < nt && ok; ++q) ok = mbar_wait(&o_empty[q], (item - 1) & 1u, &abort_flag);
                 auto scores = [&](uint32_t gk, int q) {
-                    const uint32_t k_addr = kv_smem + (gk % kStages) * kTileBytes, q_addr = q_smem + q * kTileBytes;
-                    for (int k = 0; k < ksteps; ++k) {
-                        const uint32_t off = (uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32;
-                        umma(tmem + q * kTile, make_smem_desc(q_addr + off), make_smem_desc(k_addr + off), id_s, k > 0);
-                    }
+                    head_steps<NB>(tmem + q * kTile, make_smem_desc(q_smem + q * kTileBytes), make_smem_desc(kv_smem + (gk % kStages) * kTileBytes), id_s,
+                                   ksteps);
                     umma_commit(&s_full[q]);
                 };
-                if (ok) ok = mbar_wait(&kv_full[g % kStages], (g / kStages) & 1u, &abort_flag);
-                tc_fence_after();
+                if (ok) ok = tile_ready(&kv_full[g % kStages], (g / kStages) & 1u, &abort_flag);
                 if (ok) {
                     for (int q = 0; q < nt; ++q) scores(g, q);
                     umma_commit(&kv_empty[g % kStages]);
                 }
                 for (int j = 0; j < n && ok; ++j, g += 2) {
                     const uint32_t gv = g + 1, gk = g + 2;
-                    const uint32_t v_addr = kv_smem + (gv % kStages) * kTileBytes;
-                    ok = mbar_wait(&kv_full[gv % kStages], (gv / kStages) & 1u, &abort_flag);
+                    const uint64_t v_desc = make_smem_desc_mn(kv_smem + (gv % kStages) * kTileBytes, kBlockBytes);
+                    ok = tile_ready(&kv_full[gv % kStages], (gv / kStages) & 1u, &abort_flag);
                     for (int q = 0; q < nt && ok; ++q) {
                         ok = mbar_wait(&p_full[q], pc[q]++ & 1u, &abort_flag);
                         if (!ok) break;
                         tc_fence_after();
-                        for (int k = 0; k < kTile / 16; ++k)
-                            umma_ts(tmem + 256 + q * 64 * NB, tmem + q * kTile + k * 8, make_smem_desc_mn(v_addr + k * 2048, kBlockBytes), id_o,
-                                    (j | k) != 0);
+                        row_steps(tmem + 256 + q * 64 * NB, tmem + q * kTile, 0, v_desc, id_o, j > 0);
                         if (j + 1 < n) {
                             if (q == 0) {
-                                ok = mbar_wait(&kv_full[gk % kStages], (gk / kStages) & 1u, &abort_flag);
+                                ok = tile_ready(&kv_full[gk % kStages], (gk / kStages) & 1u, &abort_flag);
                                 if (!ok) break;
-                                tc_fence_after();
                             }
                             if (q == nt - 1) umma_commit(&kv_empty[gv % kStages]);
                             scores(gk, q);
@@ -470,8 +452,7 @@ __device__ inline void store_operand(uint32_t taddr, const float (&v)[64])
     for (int i = 0; i < 32; ++i) r[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
     tmem_store32(taddr, r);
 }
-// its place for the products: K step k of 16 (the second warpgroup's half begins 64 columns behind the first's)
-__device__ inline uint32_t operand_step(uint32_t base, int k) { return base + (uint32_t)(k >> 2) * 64u + (uint32_t)(k & 3) * 8u; }
+// (the second warpgroup's 32 packed columns lie 64 behind the first's: each half stays within the columns that its warpgroup has read)
 
 // One row (up to 64 NB columns) of an accumulator -> out, times f; zeros where !keep
 template <int NB>
@@ -524,10 +505,10 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&kv_full[s], kLoaders);
+            mbar_init(&kv_full[s], kTileArrivals);
             mbar_init(&kv_empty[s], 1);
         }
-        mbar_init(&q_full, kLoaders);
+        mbar_init(&q_full, kTileArrivals);
         mbar_init(&q_empty, 1);
         mbar_init(&s_full[0], 1);
         mbar_init(&s_full[1], 1);
@@ -553,11 +534,10 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
     if (warp < kMmaWarp) {
         // ---- copies: Q and dO of a tile of rows, then keys and values in turn
         const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8;
-        Pending pend;
         uint32_t g = 0, jj = 0, item = 0;
         bool ok = true;
         for (int64_t t = t0; t * kTile < rows && n > 0 && ok; t += tiles, ++item) {
-            if (item > 0) ok = wait_slot(&q_empty, (item - 1) & 1u, pend, lane, &abort_flag);
+            if (item > 0) ok = warp_wait(&q_empty, (item - 1) & 1u, &abort_flag);
             if (!ok) break;
             for (int b = w; b < 4; b += kLoaders) {
                 const int64_t r = t * kTile + b * 32 + lane, i = r / a.group;
@@ -565,7 +545,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
                 copy_each<NB>(q_smem, b, r < rows ? static_cast<const bf16 *>(a.q) + (rg.q0 + i) * a.ldq + col : nullptr, a.q, chunks, real, lane);
                 copy_each<NB>(g_smem, b, r < rows ? static_cast<const bf16 *>(a.dout) + (rg.q0 + i) * a.ldg + col : nullptr, a.q, chunks, real, lane);
             }
-            pend.push(&q_full, lane);
+            announce(&q_full, lane);
             for (int j = 0; j < n && ok; ++j, ++jj) {
                 uint32_t word[4 / kLoaders];
 #pragma unroll
@@ -575,7 +555,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
                 }
                 for (int v = 0; v < 2; ++v, ++g) {
                     const uint32_t s = g % kStages;
-                    if (g >= kStages) ok = wait_slot(&kv_empty[s], (g / kStages - 1) & 1u, pend, lane, &abort_flag);
+                    if (g >= kStages) ok = warp_wait(&kv_empty[s], (g / kStages - 1) & 1u, &abort_flag);
                     if (!ok) break;
 #pragma unroll
                     for (int b = 0; b < 4 / kLoaders; ++b) {
@@ -585,56 +565,50 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
                         copy_rows<NB>(kv_smem + s * kTileBytes, part, static_cast<const bf16 *>(v ? a.v : a.k) + key * ld + h * (int64_t)a.head_dim, ld,
                                       word[b], a.q, chunks, real, lane);
                     }
-                    pend.push(&kv_full[s], lane);
+                    announce(&kv_full[s], lane);
                 }
             }
         }
-        pend.flush(lane);
+        cp_async_wait_all();
     } else if (warp == kMmaWarp) {
         // ---- products.  S of the next tile goes out before dQ waits for dS, dP of the next tile behind dQ (whose operand it
         // overwrites): the warpgroups form p of the next tile beside dQ and dP.
-        if (lane == 0) {
+        if (elect_one()) {
             const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
             uint32_t g = 0, item = 0, jj = 0;
             bool ok = true;
-            auto product = [&](uint32_t d, uint32_t a_addr, uint32_t slot) {
-                const uint32_t b_addr = kv_smem + (slot % kStages) * kTileBytes;
-                for (int k = 0; k < ksteps; ++k) {
-                    const uint32_t off = (uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32;
-                    umma(d, make_smem_desc(a_addr + off), make_smem_desc(b_addr + off), id_s, k > 0);
-                }
+            auto product = [&](uint32_t d, uint64_t a_desc, uint32_t slot) {
+                head_steps<NB>(d, a_desc, make_smem_desc(kv_smem + (slot % kStages) * kTileBytes), id_s, ksteps);
             };
+            const uint64_t q_desc = make_smem_desc(q_smem), g_desc = make_smem_desc(g_smem);
             auto full = [&](uint32_t slot) {
-                ok = ok && mbar_wait(&kv_full[slot % kStages], (slot / kStages) & 1u, &abort_flag);
-                tc_fence_after();
+                ok = ok && tile_ready(&kv_full[slot % kStages], (slot / kStages) & 1u, &abort_flag);
                 return ok;
             };
             for (int64_t t = t0; t * kTile < rows && n > 0 && ok; t += tiles, ++item) {
-                ok = mbar_wait(&q_full, item & 1u, &abort_flag);
+                ok = tile_ready(&q_full, item & 1u, &abort_flag);
                 if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
                 if (!full(g)) break;
-                product(tmem + (jj & 1u) * kTile, q_smem, g);
+                product(tmem + (jj & 1u) * kTile, q_desc, g);
                 umma_commit(&s_full[jj & 1u]);
                 if (!full(g + 1)) break;
-                product(tmem + 256, g_smem, g + 1);
+                product(tmem + 256, g_desc, g + 1);
                 umma_commit(&dp_full);
                 umma_commit(&kv_empty[(g + 1) % kStages]);
                 for (int j = 0; j < n; ++j, g += 2, ++jj) {
                     if (j + 1 < n) {
                         if (!full(g + 2)) break;
-                        product(tmem + ((jj + 1) & 1u) * kTile, q_smem, g + 2);
+                        product(tmem + ((jj + 1) & 1u) * kTile, q_desc, g + 2);
                         umma_commit(&s_full[(jj + 1) & 1u]);
                     }
                     ok = mbar_wait(&ds_full, jj & 1u, &abort_flag);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t k_addr = kv_smem + (g % kStages) * kTileBytes;
-                    for (int k = 0; k < kTile / 16; ++k)
-                        umma_ts(tmem + 384, operand_step(tmem + 256, k), make_smem_desc_mn(k_addr + k * 2048, kBlockBytes), id_o, (j | k) != 0);
+                    row_steps(tmem + 384, tmem + 256, 32, make_smem_desc_mn(kv_smem + (g % kStages) * kTileBytes, kBlockBytes), id_o, j > 0);
                     umma_commit(&kv_empty[g % kStages]);
                     if (j + 1 < n) {
                         if (!full(g + 3)) break;
-                        product(tmem + 256, g_smem, g + 3);
+                        product(tmem + 256, g_desc, g + 3);
                         umma_commit(&dp_full);
                         umma_commit(&kv_empty[(g + 3) % kStages]);
                     } else {
@@ -759,10 +733,10 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&qg_full[s], kLoaders);
+            mbar_init(&qg_full[s], kTileArrivals);
             mbar_init(&qg_empty[s], 1);
         }
-        mbar_init(&kv_full, kLoaders);
+        mbar_init(&kv_full, kTileArrivals);
         mbar_init(&kv_empty, 1);
         mbar_init(&s_full, 1);
         mbar_init(&p_full, 8);
@@ -788,11 +762,10 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
     if (warp < kMmaWarp) {
         // ---- copies: keys and values of a tile, then Q and dO of the rows in turn, with the rows' lse and D
         const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8, heads = a.kv_heads * a.group;
-        Pending pend;
         uint32_t g = 0, jj = 0, item = 0;
         bool ok = true;
         for (int64_t t = t0; t * kTile < keys && n > 0 && ok; t += tiles, ++item) {
-            if (item > 0) ok = wait_slot(&kv_empty, (item - 1) & 1u, pend, lane, &abort_flag);
+            if (item > 0) ok = warp_wait(&kv_empty, (item - 1) & 1u, &abort_flag);
             if (!ok) break;
             for (int b = w; b < 4; b += kLoaders) {
                 const int64_t key = rg.k0 + t * kTile + b * 32 + lane;
@@ -800,7 +773,7 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
                 copy_each<NB>(k_smem, b, seen ? static_cast<const bf16 *>(a.k) + key * a.ldk + h * (int64_t)a.head_dim : nullptr, a.q, chunks, real, lane);
                 copy_each<NB>(v_smem, b, seen ? static_cast<const bf16 *>(a.v) + key * a.ldv + h * (int64_t)a.head_dim : nullptr, a.q, chunks, real, lane);
             }
-            pend.push(&kv_full, lane);
+            announce(&kv_full, lane);
             for (int j = 0; j < n && ok; ++j, ++jj) {
                 int64_t row[4 / kLoaders], col[4 / kLoaders];
                 float l[4 / kLoaders], d[4 / kLoaders];
@@ -822,7 +795,7 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
                 }
                 for (int v = 0; v < 2; ++v, ++g) {
                     const uint32_t s = g % kStages;
-                    if (g >= kStages) ok = wait_slot(&qg_empty[s], (g / kStages - 1) & 1u, pend, lane, &abort_flag);
+                    if (g >= kStages) ok = warp_wait(&qg_empty[s], (g / kStages - 1) & 1u, &abort_flag);
                     if (!ok) break;
 #pragma unroll
                     for (int b = 0; b < 4 / kLoaders; ++b) {
@@ -834,43 +807,37 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
                         const bf16 *src = v ? static_cast<const bf16 *>(a.dout) + row[b] * a.ldg + col[b] : static_cast<const bf16 *>(a.q) + row[b] * a.ldq + col[b];
                         copy_each<NB>(qg_smem + s * kTileBytes, part, l[b] != INFINITY ? src : nullptr, a.q, chunks, real, lane);
                     }
-                    pend.push(&qg_full[s], lane);
+                    announce(&qg_full[s], lane);
                 }
             }
         }
-        pend.flush(lane);
+        cp_async_wait_all();
     } else if (warp == kMmaWarp) {
         // ---- products.  S^T of the next tile follows dV, whose operand it overwrites, dP^T follows dK: the warpgroups form dS
         // beside dV and the next S^T, and the next p beside dK and the next dP^T.
-        if (lane == 0) {
+        if (elect_one()) {
             const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
             uint32_t g = 0, item = 0, jj = 0;
             bool ok = true;
-            auto product = [&](uint32_t d, uint32_t a_addr, uint32_t slot) {
-                const uint32_t b_addr = qg_smem + (slot % kStages) * kTileBytes;
-                for (int k = 0; k < ksteps; ++k) {
-                    const uint32_t off = (uint32_t)(k >> 2) * kBlockBytes + (uint32_t)(k & 3) * 32;
-                    umma(d, make_smem_desc(a_addr + off), make_smem_desc(b_addr + off), id_s, k > 0);
-                }
+            auto product = [&](uint32_t d, uint64_t a_desc, uint32_t slot) {
+                head_steps<NB>(d, a_desc, make_smem_desc(qg_smem + (slot % kStages) * kTileBytes), id_s, ksteps);
             };
             auto gradient = [&](uint32_t d, uint32_t operand, uint32_t slot, bool add) {
-                const uint32_t b_addr = qg_smem + (slot % kStages) * kTileBytes;
-                for (int k = 0; k < kTile / 16; ++k)
-                    umma_ts(d, operand_step(operand, k), make_smem_desc_mn(b_addr + k * 2048, kBlockBytes), id_o, add || k != 0);
+                row_steps(d, operand, 32, make_smem_desc_mn(qg_smem + (slot % kStages) * kTileBytes, kBlockBytes), id_o, add);
             };
+            const uint64_t k_desc = make_smem_desc(k_smem), v_desc = make_smem_desc(v_smem);
             auto full = [&](uint32_t slot) {
-                ok = ok && mbar_wait(&qg_full[slot % kStages], (slot / kStages) & 1u, &abort_flag);
-                tc_fence_after();
+                ok = ok && tile_ready(&qg_full[slot % kStages], (slot / kStages) & 1u, &abort_flag);
                 return ok;
             };
             for (int64_t t = t0; t * kTile < keys && n > 0 && ok; t += tiles, ++item) {
-                ok = mbar_wait(&kv_full, item & 1u, &abort_flag);
+                ok = tile_ready(&kv_full, item & 1u, &abort_flag);
                 if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
                 if (!full(g)) break;
-                product(tmem, k_smem, g);
+                product(tmem, k_desc, g);
                 umma_commit(&s_full);
                 if (!full(g + 1)) break;
-                product(tmem + 128, v_smem, g + 1);
+                product(tmem + 128, v_desc, g + 1);
                 umma_commit(&dp_full);
                 for (int j = 0; j < n; ++j, g += 2, ++jj) {
                     ok = mbar_wait(&p_full, jj & 1u, &abort_flag);
@@ -880,7 +847,7 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
                     umma_commit(&qg_empty[(g + 1) % kStages]);
                     if (j + 1 < n) {
                         if (!full(g + 2)) break;
-                        product(tmem, k_smem, g + 2);
+                        product(tmem, k_desc, g + 2);
                         umma_commit(&s_full);
                     }
                     ok = mbar_wait(&ds_full, jj & 1u, &abort_flag);
@@ -890,7 +857,7 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
                     umma_commit(&qg_empty[g % kStages]);
                     if (j + 1 < n) {
                         if (!full(g + 3)) break;
-                        product(tmem + 128, v_smem, g + 3);
+                        product(tmem + 128, v_desc, g + 3);
                         umma_commit(&dp_full);
                     } else {
                         umma_commit(&o_full);

@@ -155,6 +155,18 @@ __device__ inline void tmem_load32(uint32_t taddr, uint32_t (&r)[32])
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 }
 
+// One lane of a warp that is converged, the same one for all time; the compiler knows the code behind it as run by one lane, which
+// keeps descriptors and addresses of the products in uniform registers.
+__device__ inline bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xFFFFFFFF;\nselp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+    return r != 0;
+}
+
+// A descriptor for an address `bytes` further on (a multiple of 16; the address field has room for all of shared memory)
+__device__ inline uint64_t desc_at(uint64_t d, uint32_t bytes) { return d + (bytes >> 4); }
+
 // As umma, with the A operand in tensor memory: 128 lanes = rows, one 32-bit column = two neighbouring 16-bit K values.
 __device__ inline void umma_ts(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate)
 {
@@ -198,7 +210,6 @@ __device__ inline void cp_async16(uint32_t dst, const void *src, bool on)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(on ? 16 : 0) : "memory");
 }
-__device__ inline void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ inline void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ inline void cp_async_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
 }  // namespace e2egrec
