@@ -791,46 +791,38 @@ def gate_fusion_backward(dFused: torch.Tensor, F: torch.Tensor, n_rows: int, gat
 # ------------------------------------------------------------------------------------------ attention-based fusion
 
 ROTARY_INTERLEAVED, ROTARY_INVERSE = 1, 2
+_NO_WS = 256            # a workspace of this size is one that the library does not use
+_NO_WS_BUFFER = {}
+# the current stream's handle without a stream object around it (that object costs half as much as a small call)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-class _On:
-    """Makes a tensor's device, and the caller's stream on it, current for the allocations and the call inside."""
-
-    def __init__(self, t, stream):
-        if not t.is_cuda:
-            raise E2EGrecError("a tensor is not on a CUDA device")
-        self.device = t.device
-        self.stream = torch.cuda.current_stream(t.device) if stream is None else stream
-        self.ctx = None
-        if stream is not None or torch.cuda.current_device() != t.device.index:
-            self.ctx = torch.cuda.stream(self.stream)
-        self.ptr = C.c_void_p(self.stream.cuda_stream)
-
-    def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
-        return self
-
-    def __exit__(self, *e):
-        if self.ctx is not None:
-            self.ctx.__exit__(*e)
+def _elsewhere(t, stream):
+    """None where the call goes to the current stream of the current device, else a context that makes the tensor's device, and the
+    caller's stream on it, current (allocations inside belong to that stream)."""
+    if not t.is_cuda:
+        raise E2EGrecError("a tensor is not on a CUDA device")
+    if stream is None and torch.cuda.current_device() == t.get_device():
+        return None
+    return torch.cuda.stream(torch.cuda.current_stream(t.device) if stream is None else stream)
 
 
-def _heads_mat(t, on, name):
+def _heads_mat(t, dev, name):
     """A matrix of heads as the library takes it: two dimensions, elements of a row side by side, on the call's device."""
-    if t.dim() != 2 or t.dtype not in _DTYPES or t.device != on.device or (t.shape[1] > 1 and t.stride(1) != 1):
-        raise E2EGrecError(f"{name}: a [rows x heads * head_dim] float32 or bfloat16 matrix with adjacent columns on {on.device} is wanted, "
-                           f"got {tuple(t.shape)} {t.dtype} strides {t.stride()} on {t.device}")
-    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-    return Mat(t.data_ptr(), t.shape[0], t.shape[1], ld, _DTYPES[t.dtype])
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or t.dtype not in _DTYPES or t.get_device() != dev or (strides[1] != 1 and shape[1] > 1):
+        raise E2EGrecError(f"{name}: a [rows x heads * head_dim] float32 or bfloat16 matrix with adjacent columns on device {dev} is wanted, "
+                           f"got {tuple(shape)} {t.dtype} strides {strides} on {t.device}")
+    rows, dim = shape
+    return Mat(t.data_ptr(), rows, dim, strides[0] if rows > 1 else max(strides[0], dim), _DTYPES[t.dtype])
 
 
-def _vector(t, on, dtype, n, name):
-    """Pointer of a contiguous vector of n elements on the call's device; None stays None."""
+def _vector(t, dev, dtype, n, name):
+    """Address of a contiguous vector of n elements on the call's device; None stays None."""
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n or t.device != on.device or not t.is_contiguous():
-        raise E2EGrecError(f"{name}: {n} contiguous {dtype} values on {on.device} are wanted, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.dtype != dtype or t.numel() != n or t.get_device() != dev or not t.is_contiguous():
+        raise E2EGrecError(f"{name}: {n} contiguous {dtype} values on device {dev} are wanted, got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
@@ -842,73 +834,98 @@ def _packed_like(t):
     return torch.empty(t.shape, dtype=t.dtype, device=t.device)
 
 
+def _scratch(need: int, device):
+    if need > _NO_WS:
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    if device not in _NO_WS_BUFFER:
+        _NO_WS_BUFFER[device] = torch.empty(_NO_WS, dtype=torch.uint8, device=device)
+    return _NO_WS_BUFFER[device]
+
+
 def rotary_frequencies(rot_dim: int, base=10000.0, factor=1.0, trained_len=0.0, low=1.0, high=32.0, device="cuda", stream=None):
     """Frequencies of the rotary calls (double[rot_dim / 2], radians per position); see e2egrec_rotary_frequencies."""
     freqs = torch.empty(max(int(rot_dim) // 2, 1), dtype=torch.float64, device=device)
-    with _On(freqs, stream) as on:
-        _check(lib().e2egrec_rotary_frequencies(int(rot_dim), float(base), float(factor), float(trained_len), float(low), float(high),
-                                                freqs.data_ptr(), on.ptr), "e2egrec_rotary_frequencies")
+    ctx = _elsewhere(freqs, stream)
+    if ctx is not None:
+        with ctx:
+            return rotary_frequencies(rot_dim, base, factor, trained_len, low, high, device)
+    _check(lib().e2egrec_rotary_frequencies(int(rot_dim), float(base), float(factor), float(trained_len), float(low), float(high),
+                                            freqs.data_ptr(), _raw_stream(freqs.get_device())), "e2egrec_rotary_frequencies")
     return freqs
 
 
 def rotary(X: torch.Tensor, n_heads: int, freqs, pos=None, scale=1.0, interleaved=False, inverse=False, out=None, stream=None):
     """Enqueues the rotation of every head of X by its row's position (see e2egrec_rotary) and returns the result; out=X
     rotates in place.  inverse=True maps the gradient of the result to that of X."""
-    with _On(X, stream) as on:
-        if out is None:
-            out = _packed_like(X)
-        x, y = _heads_mat(X, on, "X"), _heads_mat(out, on, "out")
-        rot = 0 if freqs is None else 2 * freqs.numel()
-        flags = (ROTARY_INTERLEAVED if interleaved else 0) | (ROTARY_INVERSE if inverse else 0)
-        _check(lib().e2egrec_rotary(C.byref(x), n_heads, _vector(freqs, on, torch.float64, rot // 2, "freqs"), rot,
-                                    _vector(pos, on, torch.int32, X.shape[0], "pos"), scale, flags, C.byref(y), on.ptr), "e2egrec_rotary")
+    ctx = _elsewhere(X, stream)
+    if ctx is not None:
+        with ctx:
+            return rotary(X, n_heads, freqs, pos, scale, interleaved, inverse, out)
+    dev = X.get_device()
+    if out is None:
+        out = _packed_like(X)
+    rot = 0 if freqs is None else 2 * freqs.numel()
+    _check(lib().e2egrec_rotary(C.byref(_heads_mat(X, dev, "X")), n_heads, _vector(freqs, dev, torch.float64, rot // 2, "freqs"), rot,
+                                _vector(pos, dev, torch.int32, X.shape[0], "pos"), scale,
+                                (ROTARY_INTERLEAVED if interleaved else 0) | (ROTARY_INVERSE if inverse else 0),
+                                C.byref(_heads_mat(out, dev, "out")), _raw_stream(dev)), "e2egrec_rotary")
     return out
+
+
+def _qk_arguments(Q, K, n_heads, n_kv_heads, wq, wk, eps, freqs, pos_q, pos_k, scale, interleaved, dev):
+    """The arguments that both calls of the normed form share, from n_heads on."""
+    rot, hd = 0 if freqs is None else 2 * freqs.numel(), Q.shape[1] // max(n_heads, 1)
+    return (n_heads, n_kv_heads, _vector(wq, dev, torch.float32, hd, "wq"), _vector(wk, dev, torch.float32, hd, "wk"), eps,
+            _vector(freqs, dev, torch.float64, rot // 2, "freqs"), rot, _vector(pos_q, dev, torch.int32, Q.shape[0], "pos_q"),
+            None if K is None else _vector(pos_k, dev, torch.int32, K.shape[0], "pos_k"), scale, ROTARY_INTERLEAVED if interleaved else 0)
 
 
 def qk_norm_rotary_forward(Q, K, n_heads: int, n_kv_heads: int, wq=None, wk=None, freqs=None, pos_q=None, pos_k=None, eps=1e-6, scale=1.0,
                            interleaved=False, Qn=None, Kn=None, stream=None):
     """Enqueues the norm of every head of Q and K with the rotation after it (see e2egrec_qk_norm_rotary_forward); returns
     (Qn, Kn).  K may be None (Kn then is)."""
-    with _On(Q, stream) as on:
-        Qn = _packed_like(Q) if Qn is None else Qn
-        Kn = _packed_like(K) if Kn is None and K is not None else Kn
-        q, k = _heads_mat(Q, on, "Q"), None if K is None else _heads_mat(K, on, "K")
-        qn, kn = _heads_mat(Qn, on, "Qn"), None if K is None else _heads_mat(Kn, on, "Kn")
-        rot, hd = 0 if freqs is None else 2 * freqs.numel(), Q.shape[1] // n_heads
-        _check(lib().e2egrec_qk_norm_rotary_forward(
-            C.byref(q), _ref(k), n_heads, n_kv_heads, _vector(wq, on, torch.float32, hd, "wq"), _vector(wk, on, torch.float32, hd, "wk"), eps,
-            _vector(freqs, on, torch.float64, rot // 2, "freqs"), rot, _vector(pos_q, on, torch.int32, Q.shape[0], "pos_q"),
-            None if K is None else _vector(pos_k, on, torch.int32, K.shape[0], "pos_k"), scale, ROTARY_INTERLEAVED if interleaved else 0,
-            C.byref(qn), _ref(kn), on.ptr), "e2egrec_qk_norm_rotary_forward")
+    ctx = _elsewhere(Q, stream)
+    if ctx is not None:
+        with ctx:
+            return qk_norm_rotary_forward(Q, K, n_heads, n_kv_heads, wq, wk, freqs, pos_q, pos_k, eps, scale, interleaved, Qn, Kn)
+    dev = Q.get_device()
+    Qn = _packed_like(Q) if Qn is None else Qn
+    Kn = _packed_like(K) if Kn is None and K is not None else Kn
+    q, qn = _heads_mat(Q, dev, "Q"), _heads_mat(Qn, dev, "Qn")
+    k, kn = (None, None) if K is None else (_heads_mat(K, dev, "K"), _heads_mat(Kn, dev, "Kn"))
+    _check(lib().e2egrec_qk_norm_rotary_forward(
+        C.byref(q), _ref(k), *_qk_arguments(Q, K, n_heads, n_kv_heads, wq, wk, eps, freqs, pos_q, pos_k, scale, interleaved, dev),
+        C.byref(qn), _ref(kn), _raw_stream(dev)), "e2egrec_qk_norm_rotary_forward")
     return Qn, Kn
 
 
 def qk_norm_rotary_backward(dQn, dKn, Q, K, n_heads: int, n_kv_heads: int, wq=None, wk=None, freqs=None, pos_q=None, pos_k=None, eps=1e-6,
                             scale=1.0, interleaved=False, dQ=None, dK=None, gains=True, ws=None, stream=None):
     """Enqueues the gradient of qk_norm_rotary_forward; returns (dQ, dK, dwq, dwk, ws).  gains=False skips dwq and dwk."""
-    with _On(Q, stream) as on:
-        hd = Q.shape[1] // n_heads
-        dQ = _packed_like(Q) if dQ is None else dQ
-        dK = _packed_like(K) if dK is None and K is not None else dK
-        dwq = torch.empty(hd, dtype=torch.float32, device=Q.device) if gains else None
-        dwk = torch.empty(hd, dtype=torch.float32, device=Q.device) if gains and K is not None else None
-        q, gq, dq = _heads_mat(Q, on, "Q"), _heads_mat(dQn, on, "dQn"), _heads_mat(dQ, on, "dQ")
-        k, gk, dk = (None, None, None) if K is None else (_heads_mat(K, on, "K"), _heads_mat(dKn, on, "dKn"), _heads_mat(dK, on, "dK"))
-        rot = 0 if freqs is None else 2 * freqs.numel()
-        args = (n_heads, n_kv_heads, _vector(wq, on, torch.float32, hd, "wq"), _vector(wk, on, torch.float32, hd, "wk"), eps,
-                _vector(freqs, on, torch.float64, rot // 2, "freqs"), rot, _vector(pos_q, on, torch.int32, Q.shape[0], "pos_q"),
-                None if K is None else _vector(pos_k, on, torch.int32, K.shape[0], "pos_k"), scale, ROTARY_INTERLEAVED if interleaved else 0)
+    ctx = _elsewhere(Q, stream)
+    if ctx is not None:
+        with ctx:
+            return qk_norm_rotary_backward(dQn, dKn, Q, K, n_heads, n_kv_heads, wq, wk, freqs, pos_q, pos_k, eps, scale, interleaved, dQ, dK,
+                                           gains, ws)
+    dev, hd = Q.get_device(), Q.shape[1] // max(n_heads, 1)
+    dQ = _packed_like(Q) if dQ is None else dQ
+    dK = _packed_like(K) if dK is None and K is not None else dK
+    dw = torch.empty(2, hd, dtype=torch.float32, device=Q.device) if gains else None
+    dwq, dwk = (None, None) if dw is None else (dw[0], None if K is None else dw[1])
+    q, gq, dq = _heads_mat(Q, dev, "Q"), _heads_mat(dQn, dev, "dQn"), _heads_mat(dQ, dev, "dQ")
+    k, gk, dk = (None, None, None) if K is None else (_heads_mat(K, dev, "K"), _heads_mat(dKn, dev, "dKn"), _heads_mat(dK, dev, "dK"))
+    args = _qk_arguments(Q, K, n_heads, n_kv_heads, wq, wk, eps, freqs, pos_q, pos_k, scale, interleaved, dev)
 
-        def call(ws_ptr, n):
-            _check(lib().e2egrec_qk_norm_rotary_backward(C.byref(gq), _ref(gk), C.byref(q), _ref(k), *args, C.byref(dq), _ref(dk),
-                                                         None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(),
-                                                         ws_ptr, C.byref(n), on.ptr), "e2egrec_qk_norm_rotary_backward")
+    def call(ws_ptr, n):
+        _check(lib().e2egrec_qk_norm_rotary_backward(C.byref(gq), _ref(gk), C.byref(q), _ref(k), *args, C.byref(dq), _ref(dk),
+                                                     None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(),
+                                                     ws_ptr, C.byref(n), _raw_stream(dev)), "e2egrec_qk_norm_rotary_backward")
 
+    if ws is None:
         n = C.c_size_t(0)
-        if ws is None:
-            call(None, n)
-            ws = _dev_bytes(n.value, Q.device)
-        call(ws.data_ptr(), C.c_size_t(ws.numel()))
+        call(None, n)
+        ws = _scratch(n.value, Q.device)
+    call(ws.data_ptr(), C.c_size_t(ws.numel()))
     return dQ, dK, dwq, dwk, ws
 
 
@@ -917,21 +934,21 @@ class Sequences:
     k_ptr[s] .. k_ptr[s+1]-1 of the keys and values; k_mask (uint8 or bool per key row): 0 = hidden."""
 
     def __init__(self, q_ptr: torch.Tensor, k_ptr: torch.Tensor, max_q=0, max_k=0, k_mask=None):
-        if q_ptr.dtype != torch.int64 or k_ptr.dtype != torch.int64 or q_ptr.numel() != k_ptr.numel() or q_ptr.numel() < 1 or \
-                not q_ptr.is_contiguous() or not k_ptr.is_contiguous():
+        n = q_ptr.numel()
+        if q_ptr.dtype != torch.int64 or k_ptr.dtype != torch.int64 or n != k_ptr.numel() or n < 1 or not q_ptr.is_contiguous() or \
+                not k_ptr.is_contiguous():
             raise E2EGrecError("q_ptr and k_ptr: int64 vectors of n_seq + 1 offsets each are wanted")
         if k_mask is not None and (k_mask.dtype not in (torch.uint8, torch.bool) or not k_mask.is_contiguous()):
             raise E2EGrecError("k_mask: a contiguous uint8 or bool vector is wanted")
         self.q_ptr, self.k_ptr, self.k_mask = q_ptr, k_ptr, k_mask
-        self.c = SequencesStruct(q_ptr.numel() - 1, q_ptr.data_ptr(), k_ptr.data_ptr(), int(max_q), int(max_k),
-                                 None if k_mask is None else k_mask.data_ptr())
+        self.c = SequencesStruct(n - 1, q_ptr.data_ptr(), k_ptr.data_ptr(), int(max_q), int(max_k), None if k_mask is None else k_mask.data_ptr())
 
-    def check(self, on, k_rows):
-        for t in (self.q_ptr, self.k_ptr, self.k_mask):
-            if t is not None and t.device != on.device:
-                raise E2EGrecError(f"offsets and mask belong on {on.device}")
-        if self.k_mask is not None and self.k_mask.numel() != k_rows:
-            raise E2EGrecError(f"k_mask: one value for each of the {k_rows} key rows is wanted")
+    def check(self, dev, k_rows):
+        if self.q_ptr.get_device() != dev or self.k_ptr.get_device() != dev:
+            raise E2EGrecError(f"the offsets belong on device {dev}")
+        if self.k_mask is not None and (self.k_mask.numel() != k_rows or self.k_mask.get_device() != dev):
+            raise E2EGrecError(f"k_mask: one value for each of the {k_rows} key rows on device {dev} is wanted")
+        return C.byref(self.c)
 
 
 def cross_attention_forward(Q, K, V, seqs: Sequences, n_heads: int, n_kv_heads: int, scale: float, out=None, lse=None, keep_lse=True,
@@ -939,23 +956,28 @@ def cross_attention_forward(Q, K, V, seqs: Sequences, n_heads: int, n_kv_heads: 
     """Enqueues attention of every sequence's queries to its keys and values (see e2egrec_cross_attention_forward); returns
     (out, lse, ws).  Rows outside the sequences are not written, in matrices that this call allocates either.  keep_lse=False: lse
     is neither allocated nor written."""
-    with _On(Q, stream) as on:
-        seqs.check(on, K.shape[0])
-        out = _packed_like(Q) if out is None else out
-        if lse is None and keep_lse:
-            lse = torch.empty(Q.shape[0], n_heads, dtype=torch.float32, device=Q.device)
-        q, k, v, o = _heads_mat(Q, on, "Q"), _heads_mat(K, on, "K"), _heads_mat(V, on, "V"), _heads_mat(out, on, "out")
-        lp, sp = _vector(lse, on, torch.float32, Q.shape[0] * n_heads, "lse"), _vector(status, on, torch.int32, 1, "status")
+    ctx = _elsewhere(Q, stream)
+    if ctx is not None:
+        with ctx:
+            return cross_attention_forward(Q, K, V, seqs, n_heads, n_kv_heads, scale, out, lse, keep_lse, status, ws)
+    dev, rows = Q.get_device(), Q.shape[0]
+    s = seqs.check(dev, K.shape[0])
+    q, k, v = _heads_mat(Q, dev, "Q"), _heads_mat(K, dev, "K"), _heads_mat(V, dev, "V")
+    out = _packed_like(Q) if out is None else out
+    if lse is None and keep_lse:
+        lse = torch.empty(rows, n_heads, dtype=torch.float32, device=Q.device)
+    o = _heads_mat(out, dev, "out")
+    lp, sp = _vector(lse, dev, torch.float32, rows * n_heads, "lse"), _vector(status, dev, torch.int32, 1, "status")
 
-        def call(ws_ptr, n):
-            _check(lib().e2egrec_cross_attention_forward(C.byref(q), C.byref(k), C.byref(v), C.byref(seqs.c), n_heads, n_kv_heads, scale,
-                                                         C.byref(o), lp, sp, ws_ptr, C.byref(n), on.ptr), "e2egrec_cross_attention_forward")
+    def call(ws_ptr, n):
+        _check(lib().e2egrec_cross_attention_forward(C.byref(q), C.byref(k), C.byref(v), s, n_heads, n_kv_heads, scale, C.byref(o), lp, sp,
+                                                     ws_ptr, C.byref(n), _raw_stream(dev)), "e2egrec_cross_attention_forward")
 
+    if ws is None:
         n = C.c_size_t(0)
-        if ws is None:
-            call(None, n)
-            ws = _dev_bytes(n.value, Q.device)
-        call(ws.data_ptr(), C.c_size_t(ws.numel()))
+        call(None, n)
+        ws = _scratch(n.value, Q.device)
+    call(ws.data_ptr(), C.c_size_t(ws.numel()))
     return out, lse, ws
 
 
@@ -963,23 +985,27 @@ def cross_attention_backward(dOut, Q, K, V, out, lse, seqs: Sequences, n_heads: 
                              status=None, ws=None, stream=None):
     """Enqueues the gradient of cross_attention_forward (see e2egrec_cross_attention_backward); returns (dQ, dK, dV, ws).
     Rows outside the sequences are not written."""
-    with _On(Q, stream) as on:
-        seqs.check(on, K.shape[0])
-        dQ = _packed_like(Q) if dQ is None else dQ
-        dK = _packed_like(K) if dK is None else dK
-        dV = _packed_like(K) if dV is None else dV
-        g, q, k, v, o = (_heads_mat(t, on, n) for t, n in ((dOut, "dOut"), (Q, "Q"), (K, "K"), (V, "V"), (out, "out")))
-        dq, dk, dv = _heads_mat(dQ, on, "dQ"), _heads_mat(dK, on, "dK"), _heads_mat(dV, on, "dV")
-        lp, sp = _vector(lse, on, torch.float32, Q.shape[0] * n_heads, "lse"), _vector(status, on, torch.int32, 1, "status")
+    ctx = _elsewhere(Q, stream)
+    if ctx is not None:
+        with ctx:
+            return cross_attention_backward(dOut, Q, K, V, out, lse, seqs, n_heads, n_kv_heads, scale, dQ, dK, dV, status, ws)
+    dev = Q.get_device()
+    s = seqs.check(dev, K.shape[0])
+    g, q, k, v, o = (_heads_mat(t, dev, n) for t, n in ((dOut, "dOut"), (Q, "Q"), (K, "K"), (V, "V"), (out, "out")))
+    dQ = _packed_like(Q) if dQ is None else dQ
+    dK = _packed_like(K) if dK is None else dK
+    dV = _packed_like(K) if dV is None else dV
+    dq, dk, dv = _heads_mat(dQ, dev, "dQ"), _heads_mat(dK, dev, "dK"), _heads_mat(dV, dev, "dV")
+    lp, sp = _vector(lse, dev, torch.float32, Q.shape[0] * n_heads, "lse"), _vector(status, dev, torch.int32, 1, "status")
 
-        def call(ws_ptr, n):
-            _check(lib().e2egrec_cross_attention_backward(C.byref(g), C.byref(q), C.byref(k), C.byref(v), C.byref(o), lp, C.byref(seqs.c),
-                                                          n_heads, n_kv_heads, scale, C.byref(dq), C.byref(dk), C.byref(dv), sp, ws_ptr,
-                                                          C.byref(n), on.ptr), "e2egrec_cross_attention_backward")
+    def call(ws_ptr, n):
+        _check(lib().e2egrec_cross_attention_backward(C.byref(g), C.byref(q), C.byref(k), C.byref(v), C.byref(o), lp, s, n_heads, n_kv_heads, scale,
+                                                      C.byref(dq), C.byref(dk), C.byref(dv), sp, ws_ptr, C.byref(n), _raw_stream(dev)),
+               "e2egrec_cross_attention_backward")
 
+    if ws is None:
         n = C.c_size_t(0)
-        if ws is None:
-            call(None, n)
-            ws = _dev_bytes(n.value, Q.device)
-        call(ws.data_ptr(), C.c_size_t(ws.numel()))
+        call(None, n)
+        ws = _scratch(n.value, Q.device)
+    call(ws.data_ptr(), C.c_size_t(ws.numel()))
     return dQ, dK, dV, ws

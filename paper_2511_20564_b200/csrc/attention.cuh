@@ -6,6 +6,7 @@
 namespace e2egrec {
 
 constexpr int kMaxAttnDim = 256;
+constexpr int kMaxSplits = 64;               // stretches of the keys, at most
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // Rows (query i, head g of its group) of one key head count as the rows of one matrix: row i * group + g.
@@ -66,6 +67,7 @@ bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, 
 // attention_few.cu: streaming kernels, fp32 and bf16, head_dim <= 256
 struct FewPlan {
     int rows;                             // rows per unit
+    bool one_step;                        // a warp's step holds all keys of a sequence
     bool both;                            // backward: one kernel for dQ, dK and dV
     int64_t batches;                      // units of rows per sequence and key head
     int warps, splits;                    // warps per unit, stretches of the keys

@@ -12,7 +12,7 @@ namespace e2egrec {
 namespace {
 
 constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
-constexpr int kUnroll = 4;                           // steps of keys in flight per warp
+constexpr int kUnroll = 4;                           // steps of keys in flight per warp (1 where a step holds all keys of a sequence)
 
 template <typename T, int CPL> struct Piece {        // a lane's part of a head's row
     static constexpr int E = Chunk<T>::kElems * CPL;
@@ -84,6 +84,7 @@ struct FewShape {
     int warps;                                       // warps per unit: a power of two, at most kFewWarps
     int batches;                                     // batches of R rows per sequence and key head
     int splits;                                      // stretches of the keys
+    uint32_t units;
 };
 
 __device__ inline float exp2_fast(float x)
@@ -99,31 +100,61 @@ struct Unit {
     int z, h, first;
     bool any;
 };
-__device__ inline Unit few_unit(const AttnArgs &a, const FewShape &f, int R, int64_t u)
+__device__ inline Unit few_unit(const AttnArgs &a, const FewShape &f, uint32_t u)            // fewer than 2^31 units: few_plan
 {
     Unit x;
-    x.any = u < a.n_seq * a.kv_heads * f.batches * f.splits;
-    x.z = (int)(u % f.splits);
-    u /= f.splits;
-    x.first = (int)(u % f.batches);
-    u /= f.batches;
-    x.h = (int)(u % a.kv_heads);
+    x.z = x.first = 0;
+    x.any = u < f.units;
+    if (f.splits > 1) {
+        x.z = (int)(u % (uint32_t)f.splits);
+        u /= (uint32_t)f.splits;
+    }
+    if (f.batches > 1) {
+        x.first = (int)(u % (uint32_t)f.batches);
+        u /= (uint32_t)f.batches;
+    }
+    const uint32_t s = u / (uint32_t)a.kv_heads;
+    x.h = (int)(u - s * (uint32_t)a.kv_heads);
     if (!x.any) {
         x.rows = x.kb = x.ke = 0;
         x.rg = SeqRange{0, 0, 0, 0};
         return x;
     }
-    x.rg = seq_range(a, u / a.kv_heads, (threadIdx.x & 31) == 0 && x.h == 0 && x.first == 0 && x.z == 0);
+    x.rg = seq_range(a, s, (threadIdx.x & 31) == 0 && x.h == 0 && x.first == 0 && x.z == 0);
     x.rows = (x.rg.q1 - x.rg.q0) * a.group;
-    const int64_t per = ceil_div(x.rg.k1 - x.rg.k0, f.splits);
-    x.kb = min(x.rg.k0 + x.z * per, x.rg.k1);
-    x.ke = min(x.kb + per, x.rg.k1);
+    x.kb = x.rg.k0;
+    x.ke = x.rg.k1;
+    if (f.splits > 1) {
+        const int64_t per = (x.rg.k1 - x.rg.k0 + f.splits - 1) / f.splits;
+        x.kb = min(x.rg.k0 + x.z * per, x.rg.k1);
+        x.ke = min(x.kb + per, x.rg.k1);
+    }
     return x;
 }
 
+// Rows of a unit one after the other: query row and head of (query, head of the group) pair r0, r0 + 1, ...
+struct RowWalk {
+    int64_t row;
+    int g;
+    __device__ inline RowWalk(const AttnArgs &a, const Unit &x, int64_t r0)
+    {
+        const int64_t i = a.group == 1 ? r0 : (r0 >> 32 ? r0 / a.group : (int64_t)((uint32_t)r0 / (uint32_t)a.group));
+        row = x.rg.q0 + i;
+        g = (int)(r0 - i * a.group);
+    }
+    __device__ inline int head(const AttnArgs &a, const Unit &x) const { return x.h * a.group + g; }
+    __device__ inline void next(const AttnArgs &a)
+    {
+        if (++g == a.group) {
+            g = 0;
+            ++row;
+        }
+    }
+};
+
 // kb .. ke in turns of warps * kUnroll * (32 / lanes) keys
-template <typename T, int R, int CPL>
-__global__ void __launch_bounds__(kFewThreads)
+template <typename T, int R, int U, int CPL>
+__global__ void __launch_bounds__(kFewThreads, CPL == 2 ? 1 : (R > 2 ? 2 : 3))
 attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
 {
     constexpr int E = Piece<T, CPL>::E;
@@ -131,7 +162,7 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     __shared__ float join_o[kFewWarps][kMaxAttnDim];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wu = warp & (f.warps - 1);                                            // the warp's number in its unit
-    const Unit x = few_unit(a, f, R, (int64_t)blockIdx.x * (kFewWarps / f.warps) + warp / f.warps);
+    const Unit x = few_unit(a, f, blockIdx.x * (uint32_t)(kFewWarps / f.warps) + warp / f.warps);
     const int grp = lane / f.lanes, at = lane & (f.lanes - 1), kpw = 32 / f.lanes;
     const int heads = a.kv_heads * a.group;
     const int64_t koff = x.h * (int64_t)a.head_dim;
@@ -141,14 +172,12 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         const bool live = x.any && r0 < x.rows;
         if (f.warps == 1 ? !live : !__syncthreads_or((int)live)) break;      // barriers inside: all warps of the block go on, or none
         float q[R][E], o[R][E], m[R], l[R];
+        RowWalk in(a, x, r0);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
+        for (int r = 0; r < R; ++r, in.next(a)) {
             Piece<T, CPL> p;
             p.zero();
-            if (live && r0 + r < x.rows) {
-                const int64_t i = (r0 + r) / a.group;
-                p.load(static_cast<const T *>(a.q) + (x.rg.q0 + i) * a.ldq + (x.h * a.group + (r0 + r - i * a.group)) * a.head_dim, at, f.lanes, f.chunks);
-            }
+            if (live && r0 + r < x.rows) p.load(static_cast<const T *>(a.q) + in.row * a.ldq + in.head(a, x) * (int64_t)a.head_dim, at, f.lanes, f.chunks);
             p.widen(q[r]);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -158,12 +187,12 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             m[r] = -INFINITY;
             l[r] = 0.f;
         }
-        const int64_t step = (int64_t)f.warps * kUnroll * kpw;
-        for (int64_t j0 = x.kb + (int64_t)wu * kUnroll * kpw; live && j0 < x.ke; j0 += step) {
-            Piece<T, CPL> k[kUnroll], v[kUnroll];
-            bool seen[kUnroll];
+        const int64_t step = (int64_t)f.warps * U * kpw;
+        for (int64_t j0 = x.kb + (int64_t)wu * U * kpw; live && j0 < x.ke; j0 += step) {
+            Piece<T, CPL> k[U], v[U];
+            bool seen[U];
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
+            for (int u = 0; u < U; ++u) {
                 const int64_t j = j0 + u * kpw + grp;
                 seen[u] = j < x.ke && (!a.mask || a.mask[j]);
                 k[u].zero();
@@ -173,22 +202,22 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     v[u].load(static_cast<const T *>(a.v) + j * a.ldv + koff, at, f.lanes, f.chunks);
                 }
             }
-            float s[R * kUnroll];
+            float s[R * U];
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
+            for (int u = 0; u < U; ++u) {
                 float w[E];
                 k[u].widen(w);
 #pragma unroll
-                for (int r = 0; r < R; ++r) s[r * kUnroll + u] = dot<E>(q[r], w);
+                for (int r = 0; r < R; ++r) s[r * U + u] = dot<E>(q[r], w);
             }
-            key_sums<R * kUnroll>(s, f.lanes);
+            key_sums<R * U>(s, f.lanes);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float top = m[r];
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) {
-                    if (!seen[u]) s[r * kUnroll + u] = -INFINITY;
-                    top = fmaxf(top, s[r * kUnroll + u]);
+                for (int u = 0; u < U; ++u) {
+                    if (!seen[u]) s[r * U + u] = -INFINITY;
+                    top = fmaxf(top, s[r * U + u]);
                 }
                 const float base = top == -INFINITY ? 0.f : top, c = exp2_fast(m[r] - base);
                 m[r] = top;
@@ -196,17 +225,17 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
                 for (int e = 0; e < E; ++e) o[r][e] *= c;
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) {
-                    s[r * kUnroll + u] = exp2_fast(s[r * kUnroll + u] - base);
-                    l[r] += s[r * kUnroll + u];
+                for (int u = 0; u < U; ++u) {
+                    s[r * U + u] = exp2_fast(s[r * U + u] - base);
+                    l[r] += s[r * U + u];
                 }
             }
 #pragma unroll
-            for (int u = 0; u < kUnroll; ++u) {
+            for (int u = 0; u < U; ++u) {
                 float w[E];
                 v[u].widen(w);
 #pragma unroll
-                for (int r = 0; r < R; ++r) axpy<E>(o[r], s[r * kUnroll + u], w);
+                for (int r = 0; r < R; ++r) axpy<E>(o[r], s[r * U + u], w);
             }
         }
         // lane groups of the warp
@@ -258,12 +287,13 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 }
             }
         }
+        RowWalk out(a, x, r0);
         if (wu == 0 && grp == 0 && live)
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+            for (int r = 0; r < R; ++r, out.next(a))
                 if (r0 + r < x.rows) {
-                    const int64_t i = (r0 + r) / a.group, row = x.rg.q0 + i;
-                    const int head = x.h * a.group + (int)(r0 + r - i * a.group);
+                    const int64_t row = out.row;
+                    const int head = out.head(a, x);
                     const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
                     if (f.splits == 1) {
                         store_piece<T, CPL>(static_cast<T *>(a.out) + row * a.ldo + (int64_t)head * a.head_dim, at, f.lanes, f.chunks, o[r], inv);
@@ -362,15 +392,15 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
 // that is longer than the launch was sized for has its rows done batch by batch and its keys' gradients apart.
 // Where all keys are in one turn of the warp, D = sum_j p_j dP_j is formed from what the registers hold instead of the stored
 // outputs: with a handful of keys dP - D cancels, and the rounding of 16-bit outputs showed (dQ of three keys 3.1e-3 off, 2.0e-3 so).
-template <typename T, int R, int CPL, bool kBoth>
+template <typename T, int R, int U, int CPL, bool kBoth>
 __global__ void __launch_bounds__(kFewThreads)
 attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_dq, float *__restrict__ dots)
 {
-    constexpr int E = Piece<T, CPL>::E, U = R > 2 ? 2 : kUnroll;
+    constexpr int E = Piece<T, CPL>::E;
     __shared__ float join[kFewWarps][kMaxAttnDim];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wu = warp & (f.warps - 1);
-    const Unit x = few_unit(a, f, R, (int64_t)blockIdx.x * (kFewWarps / f.warps) + warp / f.warps);
+    const Unit x = few_unit(a, f, blockIdx.x * (uint32_t)(kFewWarps / f.warps) + warp / f.warps);
     const int grp = lane / f.lanes, at = lane & (f.lanes - 1), kpw = 32 / f.lanes;
     const int heads = a.kv_heads * a.group;
     const int64_t koff = x.h * (int64_t)a.head_dim;
@@ -384,16 +414,17 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         float q[R][E], g[R][E], dq[R][E], lse[R], d[R];
         const int64_t step = (int64_t)f.warps * U * kpw;
         const bool one_turn = f.warps == 1 && f.splits == 1 && x.ke - x.kb <= U * kpw;
+        RowWalk in(a, x, r0);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
+        for (int r = 0; r < R; ++r, in.next(a)) {
             Piece<T, CPL> p, t;
             p.zero();
             t.zero();
             lse[r] = INFINITY;
             d[r] = 0.f;
             if (live && r0 + r < x.rows) {
-                const int64_t i = (r0 + r) / a.group, row = x.rg.q0 + i;
-                const int head = x.h * a.group + (int)(r0 + r - i * a.group);
+                const int64_t row = in.row;
+                const int head = in.head(a, x);
                 const int64_t col = (int64_t)head * a.head_dim;
                 const float v = a.lse[row * heads + head];
                 if (v != -INFINITY) {
@@ -483,8 +514,9 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             for (int r = 0; r < R; ++r)
 #pragma unroll
                 for (int e = 0; e < E; ++e) dq[r][e] += __shfl_xor_sync(0xFFFFFFFFu, dq[r][e], o);
+        RowWalk out(a, x, r0);
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
+        for (int r = 0; r < R; ++r, out.next(a)) {
             if (f.warps > 1) {
                 __syncthreads();
                 if (grp == 0)
@@ -503,8 +535,8 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                                 for (int e = 0; e < Chunk<T>::kElems; ++e) dq[r][c * Chunk<T>::kElems + e] += join[warp + w][(at + c * f.lanes) * Chunk<T>::kElems + e];
             }
             if (wu == 0 && grp == 0 && live && r0 + r < x.rows) {
-                const int64_t i = (r0 + r) / a.group, row = x.rg.q0 + i;
-                const int head = x.h * a.group + (int)(r0 + r - i * a.group);
+                const int64_t row = out.row;
+                const int head = out.head(a, x);
                 if (!kBoth && x.z == 0 && at == 0) dots[row * heads + head] = d[r];
                 if (f.splits == 1) {
                     store_piece<T, CPL>(static_cast<T *>(a.dq) + row * a.ldq2 + (int64_t)head * a.head_dim, at, f.lanes, f.chunks, dq[r], a.scale);
@@ -531,12 +563,12 @@ __global__ void __launch_bounds__(kFewThreads)
 attn_few_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, const float *__restrict__ dots)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int64_t u = (int64_t)blockIdx.x * kFewWarps + warp;
-    if (u >= a.n_seq * a.kv_heads * f.batches) return;
-    const int first = (int)(u % f.batches);
-    u /= f.batches;
-    const int h = (int)(u % a.kv_heads);
-    const SeqRange rg = seq_range(a, u / a.kv_heads, lane == 0 && h == 0 && first == 0);
+    uint32_t u = blockIdx.x * (uint32_t)kFewWarps + warp;
+    if (u >= f.units) return;
+    const int first = (int)(u % (uint32_t)f.batches);
+    u /= (uint32_t)f.batches;
+    const int h = (int)(u % (uint32_t)a.kv_heads);
+    const SeqRange rg = seq_range(a, u / (uint32_t)a.kv_heads, lane == 0 && h == 0 && first == 0);
     const int64_t step = (int64_t)kKeys * (32 / f.lanes);
     for (int64_t j0 = rg.k0 + first * step; j0 < rg.k1; j0 += f.batches * step)
         keys_gradients<T, CPL>(a, rg, h, j0, rg.k1, lane / f.lanes, lane & (f.lanes - 1), f, dots);
@@ -569,22 +601,70 @@ FewShape few_shape(const AttnArgs &a, int es)
     return f;
 }
 
-unsigned few_grid(const AttnArgs &a, const FewShape &f) { return (unsigned)ceil_div(a.n_seq * a.kv_heads * f.batches * f.splits, kFewWarps / f.warps); }
+unsigned few_grid(const AttnArgs &a, FewShape &f)
+{
+    f.units = (uint32_t)(a.n_seq * a.kv_heads * f.batches * f.splits);
+    return (unsigned)ceil_div(f.units, kFewWarps / f.warps);
+}
 
-template <typename T, int R>
-void launch_fwd(const AttnArgs &a, const FewShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
+template <typename T, int R, int U>
+void launch_fwd(const AttnArgs &a, FewShape f, float *part_o, float2 *part_ml, cudaStream_t st)
 {
     note_launch();
-    if (f.chunks <= 32) attn_few_fwd_kernel<T, R, 1><<<few_grid(a, f), kFewThreads, 0, st>>>(a, f, part_o, part_ml);
-    else if constexpr (sizeof(T) == 4) attn_few_fwd_kernel<T, R, 2><<<few_grid(a, f), kFewThreads, 0, st>>>(a, f, part_o, part_ml);
+    const unsigned grid = few_grid(a, f);
+    if (f.chunks <= 32) attn_few_fwd_kernel<T, R, U, 1><<<grid, kFewThreads, 0, st>>>(a, f, part_o, part_ml);
+    else if constexpr (sizeof(T) == 4) attn_few_fwd_kernel<T, R, U, 2><<<grid, kFewThreads, 0, st>>>(a, f, part_o, part_ml);
 }
 
 template <typename T, int R, bool kBoth>
-void launch_bwd(const AttnArgs &a, const FewShape &f, float *part_dq, float *dots, cudaStream_t st)
+void launch_bwd(const AttnArgs &a, FewShape f, bool one_step, float *part_dq, float *dots, cudaStream_t st)
 {
+    constexpr int U = R > 2 ? 2 : kUnroll;
     note_launch();
-    if (f.chunks <= 32) attn_few_bwd_kernel<T, R, 1, kBoth><<<few_grid(a, f), kFewThreads, 0, st>>>(a, f, part_dq, dots);
-    else if constexpr (sizeof(T) == 4) attn_few_bwd_kernel<T, R, 2, kBoth><<<few_grid(a, f), kFewThreads, 0, st>>>(a, f, part_dq, dots);
+    const unsigned grid = few_grid(a, f);
+    if (f.chunks <= 32) {
+        if (one_step) attn_few_bwd_kernel<T, R, 1, 1, kBoth><<<grid, kFewThreads, 0, st>>>(a, f, part_dq, dots);
+        else attn_few_bwd_kernel<T, R, U, 1, kBoth><<<grid, kFewThreads, 0, st>>>(a, f, part_dq, dots);
+    } else if constexpr (sizeof(T) == 4) {
+        attn_few_bwd_kernel<T, R, U, 2, kBoth><<<grid, kFewThreads, 0, st>>>(a, f, part_dq, dots);
+    }
+}
+
+template <typename T> void forward_of(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
+{
+    if (p.one_step) {
+        if (p.rows == 1) launch_fwd<T, 1, 1>(a, f, part_o, part_ml, st);
+        else if (p.rows == 2) launch_fwd<T, 2, 1>(a, f, part_o, part_ml, st);
+        else launch_fwd<T, 4, 1>(a, f, part_o, part_ml, st);
+    } else {
+        if (p.rows == 1) launch_fwd<T, 1, kUnroll>(a, f, part_o, part_ml, st);
+        else if (p.rows == 2) launch_fwd<T, 2, kUnroll>(a, f, part_o, part_ml, st);
+        else launch_fwd<T, 4, 2>(a, f, part_o, part_ml, st);
+    }
+}
+
+template <typename T> void backward_of(const AttnArgs &a, const FewPlan &p, FewShape f, float *part_dq, float *dots, cudaStream_t st)
+{
+    if (p.both) {
+        if (p.rows == 1) launch_bwd<T, 1, true>(a, f, p.one_step, part_dq, dots, st);
+        else if (p.rows == 2) launch_bwd<T, 2, true>(a, f, p.one_step, part_dq, dots, st);
+        else launch_bwd<T, 4, true>(a, f, p.one_step, part_dq, dots, st);
+    } else {
+        launch_bwd<T, 4, false>(a, f, p.one_step, part_dq, dots, st);
+    }
+    if (f.splits > 1 && a.q_rows) {
+        note_launch();
+        attn_join_dq_kernel<T><<<(unsigned)ceil_div(a.q_rows * a.kv_heads * a.group, kFewWarps), kFewThreads, 0, st>>>(a, f.splits, part_dq);
+    }
+    if (!p.both && a.k_rows) {
+        note_launch();
+        f.batches = (int)p.key_batches;
+        f.splits = 1;
+        f.warps = 1;
+        const unsigned grid = few_grid(a, f);
+        if (f.chunks <= 32) attn_few_dkv_kernel<T, 1><<<grid, kFewThreads, 0, st>>>(a, f, dots);
+        else if constexpr (sizeof(T) == 4) attn_few_dkv_kernel<T, 2><<<grid, kFewThreads, 0, st>>>(a, f, dots);
+    }
 }
 
 }  // namespace
@@ -594,68 +674,40 @@ FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool b
 {
     FewPlan p{};
     const FewShape f = few_shape(a, es);
-    const int64_t rows = max_q * a.group, units0 = std::max<int64_t>(a.n_seq * a.kv_heads, 1);
+    const int64_t rows = max_q * a.group, units0 = std::max<int64_t>(a.n_seq * a.kv_heads, 1), most = (((int64_t)1 << 31) - 1) / units0;
+    const int64_t step = 32 / f.lanes;
     p.rows = rows <= 1 ? 1 : (rows <= 2 ? 2 : 4);
     p.both = backward && rows <= p.rows;
-    p.batches = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, p.rows), (((int64_t)1 << 31) - 1) / units0 / 64));
-    const int64_t turn = (int64_t)(32 / f.lanes) * (backward && p.rows > 2 ? 2 : kUnroll);
+    p.one_step = max_k <= step && f.chunks <= 32;
+    const int64_t turn = step * (p.one_step ? 1 : (p.rows > 2 ? 2 : kUnroll));
+    p.batches = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, p.rows), most));
     const int64_t want = std::max<int64_t>(1, std::min(ceil_div(148 * 24, units0 * p.batches), ceil_div(max_k, turn)));
     p.warps = 1;
     while (p.warps < kFewWarps && p.warps < want) p.warps *= 2;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(want / p.warps, 64));
-    const int64_t per = (int64_t)(32 / f.lanes) * kKeys;
-    p.key_batches = std::max<int64_t>(1, std::min(ceil_div(max_k, per), (((int64_t)1 << 31) - 1) / units0));
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want / p.warps, kMaxSplits, most / p.batches}));
+    p.key_batches = std::max<int64_t>(1, std::min(ceil_div(max_k, step * kKeys), most));
     return p;
+}
+
+static FewShape planned(const AttnArgs &a, const FewPlan &p, int32_t dtype)
+{
+    FewShape f = few_shape(a, (int)dtype_size(dtype));
+    f.warps = p.warps;
+    f.batches = (int)p.batches;
+    f.splits = p.splits;
+    return f;
 }
 
 void few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    const bool f32 = dtype == E2EGREC_F32;
-    FewShape f = few_shape(a, f32 ? 4 : 2);
-    f.warps = p.warps;
-    f.batches = (int)p.batches;
-    f.splits = p.splits;
-    if (f32) {
-        if (p.rows == 1) launch_fwd<float, 1>(a, f, part_o, part_ml, st);
-        else if (p.rows == 2) launch_fwd<float, 2>(a, f, part_o, part_ml, st);
-        else launch_fwd<float, 4>(a, f, part_o, part_ml, st);
-    } else {
-        if (p.rows == 1) launch_fwd<__nv_bfloat16, 1>(a, f, part_o, part_ml, st);
-        else if (p.rows == 2) launch_fwd<__nv_bfloat16, 2>(a, f, part_o, part_ml, st);
-        else launch_fwd<__nv_bfloat16, 4>(a, f, part_o, part_ml, st);
-    }
-}
-
-template <typename T> static void few_backward(const AttnArgs &a, const FewPlan &p, FewShape f, float *part_dq, float *dots, cudaStream_t st)
-{
-    if (p.both) {
-        if (p.rows == 1) launch_bwd<T, 1, true>(a, f, part_dq, dots, st);
-        else if (p.rows == 2) launch_bwd<T, 2, true>(a, f, part_dq, dots, st);
-        else launch_bwd<T, 4, true>(a, f, part_dq, dots, st);
-    } else {
-        launch_bwd<T, 4, false>(a, f, part_dq, dots, st);
-    }
-    if (f.splits > 1 && a.q_rows) {
-        note_launch();
-        attn_join_dq_kernel<T><<<(unsigned)ceil_div(a.q_rows * a.kv_heads * a.group, kFewWarps), kFewThreads, 0, st>>>(a, f.splits, part_dq);
-    }
-    if (!p.both && a.k_rows) {
-        note_launch();
-        f.batches = (int)p.key_batches;
-        const unsigned grid = (unsigned)ceil_div(a.n_seq * a.kv_heads * f.batches, kFewWarps);
-        if (f.chunks <= 32) attn_few_dkv_kernel<T, 1><<<grid, kFewThreads, 0, st>>>(a, f, dots);
-        else if constexpr (sizeof(T) == 4) attn_few_dkv_kernel<T, 2><<<grid, kFewThreads, 0, st>>>(a, f, dots);
-    }
+    if (dtype == E2EGREC_F32) forward_of<float>(a, p, planned(a, p, dtype), part_o, part_ml, st);
+    else forward_of<__nv_bfloat16>(a, p, planned(a, p, dtype), part_o, part_ml, st);
 }
 
 void few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st)
 {
-    FewShape f = few_shape(a, dtype == E2EGREC_F32 ? 4 : 2);
-    f.warps = p.warps;
-    f.batches = (int)p.batches;
-    f.splits = p.splits;
-    if (dtype == E2EGREC_F32) few_backward<float>(a, p, f, part_dq, dots, st);
-    else few_backward<__nv_bfloat16>(a, p, f, part_dq, dots, st);
+    if (dtype == E2EGREC_F32) backward_of<float>(a, p, planned(a, p, dtype), part_dq, dots, st);
+    else backward_of<__nv_bfloat16>(a, p, planned(a, p, dtype), part_dq, dots, st);
 }
 
 }  // namespace e2egrec
