@@ -831,7 +831,7 @@ def _ref(m):
 
 
 def _packed_like(t):
-    return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    return torch.empty_like(t)
 
 
 def _scratch(need: int, device):
@@ -910,7 +910,7 @@ def qk_norm_rotary_backward(dQn, dKn, Q, K, n_heads: int, n_kv_heads: int, wq=No
     dev, hd = Q.get_device(), Q.shape[1] // max(n_heads, 1)
     dQ = _packed_like(Q) if dQ is None else dQ
     dK = _packed_like(K) if dK is None and K is not None else dK
-    dw = torch.empty(2, hd, dtype=torch.float32, device=Q.device) if gains else None
+    dw = Q.new_empty((2, hd), dtype=torch.float32) if gains else None
     dwq, dwk = (None, None) if dw is None else (dw[0], None if K is None else dw[1])
     q, gq, dq = _heads_mat(Q, dev, "Q"), _heads_mat(dQn, dev, "dQn"), _heads_mat(dQ, dev, "dQ")
     k, gk, dk = (None, None, None) if K is None else (_heads_mat(K, dev, "K"), _heads_mat(dKn, dev, "dKn"), _heads_mat(dK, dev, "dK"))
@@ -965,7 +965,7 @@ def cross_attention_forward(Q, K, V, seqs: Sequences, n_heads: int, n_kv_heads: 
     q, k, v = _heads_mat(Q, dev, "Q"), _heads_mat(K, dev, "K"), _heads_mat(V, dev, "V")
     out = _packed_like(Q) if out is None else out
     if lse is None and keep_lse:
-        lse = torch.empty(rows, n_heads, dtype=torch.float32, device=Q.device)
+        lse = Q.new_empty((rows, n_heads), dtype=torch.float32)
     o = _heads_mat(out, dev, "out")
     lp, sp = _vector(lse, dev, torch.float32, rows * n_heads, "lse"), _vector(status, dev, torch.int32, 1, "status")
 

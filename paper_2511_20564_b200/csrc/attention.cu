@@ -84,6 +84,29 @@ attn_join_kernel(const __grid_constant__ AttnArgs a, int splits, int warps, cons
     if (a.lse && lane == 0) a.lse[unit] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
+// dQ of stretches of the keys -> dQ, in order: one thread per four elements, its loads eight at a time
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads)
+attn_join_dq_kernel(const __grid_constant__ AttnArgs a, int splits, const float *__restrict__ part)
+{
+    const int heads = a.kv_heads * a.group, units = a.head_dim / 4;
+    const int64_t n = (int64_t)blockIdx.x * kRowThreads + threadIdx.x, cell = n / units, stride = a.q_rows * heads * units;
+    const int64_t row = cell / heads;
+    if (row >= a.q_rows || owner(a.q_ptr, a.n_seq, row) < 0) return;
+    const float4 *p = reinterpret_cast<const float4 *>(part) + n;
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int z = 0; z < splits; ++z) {
+        const float4 v = p[z * stride];
+        t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+    }
+    T *out = static_cast<T *>(a.dq) + row * a.ldq2 + (cell - row * heads) * a.head_dim + (n - cell * units) * 4;
+    out[0] = from_float<T>(t.x);
+    out[1] = from_float<T>(t.y);
+    out[2] = from_float<T>(t.z);
+    out[3] = from_float<T>(t.w);
+}
+
 // Shapes, types and alignment of one matrix of heads
 int32_t check_heads(const e2egrec_mat *m, int32_t heads, int32_t head_dim, int32_t dtype, int64_t rows)
 {
@@ -98,13 +121,16 @@ int32_t check_heads(const e2egrec_mat *m, int32_t heads, int32_t head_dim, int32
 
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
 
-// Rows (query, head of the group) per key head up to which a bf16 sequence streams through attention_few.cu
-constexpr int64_t kFewRows = 16;
+// The kernels of a call.  A sequence's keys and rows stream (attention_few.cu) where a key head has up to kFewRows rows, or where a
+// sequence is so small that the set-up of a tile costs more than its products; bf16 heads of up to 128 go to the tensor cores
+// otherwise, fp32 ones to tiles of fp32 FMA, wider heads always stream.
+enum class Path { few, tc, simt };
+constexpr int64_t kFewRows = 4;
 
-// How a call is carried out, and what it needs of the workspace
 struct Plan {
-    bool tc;
+    Path path;
     FewPlan few;
+    SimtPlan simt;
     int64_t q_tiles, k_tiles;             // tensor cores: blocks of rows / tiles of keys per sequence and key head
     int splits;                           // stretches of the keys
     size_t part_bytes, ml_bytes, dot_bytes;
@@ -115,24 +141,36 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     Plan p{};
     p.splits = 1;
     const int64_t max_q = s.max_q ? std::min(s.max_q, a.q_rows) : a.q_rows, max_k = s.max_k ? std::min(s.max_k, a.k_rows) : a.k_rows;
+    const int64_t rows = max_q * a.group, units = std::max<int64_t>(a.n_seq * a.kv_heads, 1);
     const size_t cells = (size_t)a.q_rows * a.kv_heads * a.group;
-    p.tc = dtype == E2EGREC_BF16 && a.head_dim <= 128 && max_q * a.group > kFewRows;
-    if (p.tc) {
-        const int64_t units = std::max<int64_t>(a.n_seq * a.kv_heads, 1), most = (kMaxRows - 1) / units;
-        p.q_tiles = std::max<int64_t>(1, std::min(ceil_div(max_q * a.group, backward ? 128 : tc_fwd_rows()), most));
+    const bool small = rows <= kFewRows || rows * max_k <= (dtype == E2EGREC_F32 ? 256 : (backward ? 800 : 2048));
+    p.path = small || a.head_dim > 128 ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
+    if (p.path == Path::tc) {
+        const int64_t most = (kMaxRows - 1) / units;
+        p.q_tiles = std::max<int64_t>(1, std::min(ceil_div(rows, backward ? 128 : tc_fwd_rows()), most));
         p.k_tiles = std::max<int64_t>(1, std::min(ceil_div(max_k, 128), most));
         if (!backward && units * p.q_tiles < 148) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({148 / (units * p.q_tiles), max_k / 512, kMaxSplits}));
-        if (backward) p.dot_bytes = align_up(cells * sizeof(float), 256);
+    } else if (p.path == Path::simt) {
+        p.simt = simt_plan(a, max_q, max_k);
+        p.splits = p.simt.splits;
     } else {
         p.few = few_plan(a, max_q, max_k, (int)dtype_size(dtype), backward);
         p.splits = p.few.splits;
-        if (backward && !p.few.both) p.dot_bytes = align_up(cells * sizeof(float), 256);
     }
+    if (backward && !(p.path == Path::few && p.few.both)) p.dot_bytes = align_up(cells * sizeof(float), 256);
     if (p.splits > 1) {
         p.part_bytes = align_up(p.splits * cells * a.head_dim * sizeof(float), 256);
         if (!backward) p.ml_bytes = align_up(p.splits * cells * sizeof(float2), 256);
     }
     return p;
+}
+
+// A kernel could not be given its shared memory, or the device is not one of the first 64
+int32_t launch_refused(const char *what)
+{
+    const int32_t rc = check_launch(what);
+    if (rc == E2EGREC_OK) set_last_error(what);
+    return E2EGREC_ERR_CUDA;
 }
 
 // Arguments that a size query has too; fills the sizes of `a`.
@@ -160,6 +198,15 @@ int32_t check_shape(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_se
 }
 
 }  // namespace
+
+void join_dq(const AttnArgs &a, int splits, int32_t dtype, const float *part_dq, cudaStream_t st)
+{
+    note_launch();
+    const unsigned grid = (unsigned)ceil_div(a.q_rows * a.kv_heads * a.group * (a.head_dim / 4), kRowThreads);
+    if (dtype == E2EGREC_F32) attn_join_dq_kernel<float><<<grid, kRowThreads, 0, st>>>(a, splits, part_dq);
+    else attn_join_dq_kernel<__nv_bfloat16><<<grid, kRowThreads, 0, st>>>(a, splits, part_dq);
+}
+
 }  // namespace e2egrec
 
 using namespace e2egrec;
@@ -194,11 +241,11 @@ extern "C" int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     float2 *part_ml = static_cast<float2 *>(ws);
     float *part_o = reinterpret_cast<float *>(static_cast<char *>(ws) + plan.ml_bytes);
-    if (plan.tc) {
-        if (!tc_attention_forward(a, plan.q_tiles, plan.splits, part_o, part_ml, st)) return check_launch("cross_attention_forward");
-    } else {
-        few_attention_forward(a, plan.few, Q->dtype, part_o, part_ml, st);
-    }
+    bool ok = true;
+    if (plan.path == Path::tc) ok = tc_attention_forward(a, plan.q_tiles, plan.splits, part_o, part_ml, st);
+    else if (plan.path == Path::simt) ok = simt_attention_forward(a, plan.simt, part_o, part_ml, st);
+    else few_attention_forward(a, plan.few, Q->dtype, part_o, part_ml, st);
+    if (!ok) return launch_refused("cross_attention_forward");
     if (plan.splits > 1) {
         note_launch();
         const int warps = plan.splits > 8 ? kRowThreads / 32 : 1;
@@ -247,10 +294,15 @@ extern "C" int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, con
     a.status = status;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     float *dots = static_cast<float *>(ws), *part_dq = reinterpret_cast<float *>(static_cast<char *>(ws) + plan.dot_bytes);
-    if (plan.tc) {
-        if (!tc_attention_backward(a, plan.q_tiles, plan.k_tiles, dots, st)) return check_launch("cross_attention_backward");
+    bool ok = true;
+    if (plan.path == Path::tc) {
+        ok = tc_attention_backward(a, plan.q_tiles, plan.k_tiles, dots, st);
+    } else if (plan.path == Path::simt) {
+        ok = simt_attention_backward(a, plan.simt, part_dq, dots, st);
+        if (ok && plan.splits > 1 && a.q_rows) join_dq(a, plan.splits, Q->dtype, part_dq, st);
     } else {
         few_attention_backward(a, plan.few, Q->dtype, part_dq, dots, st);
     }
+    if (!ok) return launch_refused("cross_attention_backward");
     return check_launch("cross_attention_backward");
 }

@@ -78,4 +78,16 @@ void few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, f
 // part_dq: [splits x q_rows x heads x head_dim] where splits > 1; dots: [q_rows x heads] where !both
 void few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st);
 
+// dQ of stretches of the keys -> dQ, in order
+void join_dq(const AttnArgs &a, int splits, int32_t dtype, const float *part_dq, cudaStream_t st);
+
+// attention_simt.cu: fp32, head_dim <= 128, tiles of 64 rows x 64 keys
+struct SimtPlan {
+    int64_t q_tiles, k_tiles;             // blocks of rows / of keys per sequence and key head
+    int splits;                           // stretches of the keys (forward, dQ)
+};
+SimtPlan simt_plan(const AttnArgs &a, int64_t max_q, int64_t max_k);
+bool simt_attention_forward(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st);
+bool simt_attention_backward(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st);
+
 }  // namespace e2egrec

@@ -574,23 +574,6 @@ attn_few_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         keys_gradients<T, CPL>(a, rg, h, j0, rg.k1, lane / f.lanes, lane & (f.lanes - 1), f, dots);
 }
 
-// dQ of stretches of the keys -> dQ, in order; one warp per (row, head)
-template <typename T>
-__global__ void __launch_bounds__(kFewThreads)
-attn_join_dq_kernel(const __grid_constant__ AttnArgs a, int splits, const float *__restrict__ part)
-{
-    const int lane = threadIdx.x & 31, heads = a.kv_heads * a.group;
-    const int64_t unit = ((int64_t)blockIdx.x * kFewThreads + threadIdx.x) >> 5, stride = a.q_rows * heads;
-    const int64_t row = unit / heads;
-    const int h = (int)(unit % heads);
-    if (row >= a.q_rows || owner(a.q_ptr, a.n_seq, row) < 0) return;
-    for (int e = lane; e < a.head_dim; e += 32) {
-        float t = 0.f;
-        for (int z = 0; z < splits; ++z) t += part[(z * stride + unit) * a.head_dim + e];
-        static_cast<T *>(a.dq)[row * a.ldq2 + (int64_t)h * a.head_dim + e] = from_float<T>(t);
-    }
-}
-
 FewShape few_shape(const AttnArgs &a, int es)
 {
     FewShape f{};
@@ -652,10 +635,7 @@ template <typename T> void backward_of(const AttnArgs &a, const FewPlan &p, FewS
     } else {
         launch_bwd<T, 4, false>(a, f, p.one_step, part_dq, dots, st);
     }
-    if (f.splits > 1 && a.q_rows) {
-        note_launch();
-        attn_join_dq_kernel<T><<<(unsigned)ceil_div(a.q_rows * a.kv_heads * a.group, kFewWarps), kFewThreads, 0, st>>>(a, f.splits, part_dq);
-    }
+    if (f.splits > 1 && a.q_rows) join_dq(a, f.splits, sizeof(T) == 4 ? E2EGREC_F32 : E2EGREC_BF16, part_dq, st);
     if (!p.both && a.k_rows) {
         note_launch();
         f.batches = (int)p.key_batches;
