@@ -131,7 +131,8 @@ struct Plan {
     Path path;
     FewPlan few;
     SimtPlan simt;
-    int64_t q_tiles, k_tiles;             // tensor cores: blocks of rows / tiles of keys per sequence and key head
+    bool one_tile;                        // tensor cores: a key head's rows fit one tile
+    int64_t q_tiles, k_tiles;             // blocks of rows / tiles of keys per sequence and key head
     int splits;                           // stretches of the keys
     size_t part_bytes, ml_bytes, dot_bytes;
 };
@@ -147,9 +148,12 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     p.path = small || a.head_dim > 128 ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
     if (p.path == Path::tc) {
         const int64_t most = (kMaxRows - 1) / units;
-        p.q_tiles = std::max<int64_t>(1, std::min(ceil_div(rows, backward ? 128 : tc_fwd_rows()), most));
+        p.one_tile = rows <= 128;
+        p.q_tiles = std::max<int64_t>(1, std::min(ceil_div(rows, backward || p.one_tile ? 128 : 256), most));
         p.k_tiles = std::max<int64_t>(1, std::min(ceil_div(max_k, 128), most));
-        if (!backward && units * p.q_tiles < 148) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({148 / (units * p.q_tiles), max_k / 512, kMaxSplits}));
+        const int64_t blocks = p.one_tile ? 296 : 148;
+        if (!backward && units * p.q_tiles < blocks)
+            p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({blocks / (units * p.q_tiles), max_k / 512, kMaxSplits}));
     } else if (p.path == Path::simt) {
         p.simt = simt_plan(a, max_q, max_k);
         p.splits = p.simt.splits;
@@ -242,7 +246,7 @@ extern "C" int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e
     float2 *part_ml = static_cast<float2 *>(ws);
     float *part_o = reinterpret_cast<float *>(static_cast<char *>(ws) + plan.ml_bytes);
     bool ok = true;
-    if (plan.path == Path::tc) ok = tc_attention_forward(a, plan.q_tiles, plan.splits, part_o, part_ml, st);
+    if (plan.path == Path::tc) ok = tc_attention_forward(a, plan.q_tiles, plan.splits, plan.one_tile, part_o, part_ml, st);
     else if (plan.path == Path::simt) ok = simt_attention_forward(a, plan.simt, part_o, part_ml, st);
     else few_attention_forward(a, plan.few, Q->dtype, part_o, part_ml, st);
     if (!ok) return launch_refused("cross_attention_forward");

@@ -56,11 +56,10 @@ __device__ inline int64_t owner(const int64_t *ptr, int64_t n_seq, int64_t row)
     return row < ptr[lo + 1] ? lo : -1;
 }
 
-// attention_tc.cu: bf16, head_dim <= 128.  tiles: blocks of tc_fwd_rows() rows per sequence and key head (longer sequences go
-// round again); splits: stretches of the keys, whose results (out in fp32 and (maximum in powers of two, sum)) go to
+// attention_tc.cu: bf16, head_dim <= 128.  tiles: blocks of 256 rows (128 with one_tile) per sequence and key head, longer sequences go
+// round again; splits: stretches of the keys, whose results (out in fp32 and (maximum in powers of two, sum)) go to
 // part_o [splits x q_rows x heads x head_dim] and part_ml [splits x q_rows x heads] where splits > 1.
-int tc_fwd_rows();
-bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, float *part_o, float2 *part_ml, cudaStream_t st);
+bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, bool one_tile, float *part_o, float2 *part_ml, cudaStream_t st);
 // q_tiles, k_tiles: tiles of 128 rows and of 128 keys per sequence and key head; dots: [q_rows x heads] scratch
 bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st);
 

@@ -21,6 +21,7 @@ using bf16 = __nv_bfloat16;
 constexpr int kTile = 128;
 constexpr int kThreads = 12 * 32;                    // two warpgroups over scores, two loading warps, the products' warp; one idle
 constexpr int kLoaders = 2, kMmaWarp = 8 + kLoaders;
+constexpr int kSms = 148;
 constexpr int kBlockBytes = kTile * 128;             // 64 columns of 128 rows
 constexpr int kWordRing = 8;                         // tiles whose visibility words are kept
 
@@ -61,9 +62,64 @@ __device__ inline void tmem_load16_async(uint32_t taddr, uint32_t (&r)[16])
         : "r"(taddr));
 }
 
-// Registers are dealt out anew once the block runs: 384 threads x 168 at launch = 128 (copies and products) x 88 + 256 x 208.
-__device__ inline void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
-__device__ inline void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
+// Registers are dealt out anew once the block runs.  One block per SM: 384 threads x 168 at launch = 128 (copies and products) x 88 +
+// 256 x 208.  Two blocks per SM: 256 threads x 128 = 128 x 72 + 128 x 184.
+template <int kBlocks> __device__ inline void fewer_registers()
+{
+    if (kBlocks == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+}
+template <int kBlocks> __device__ inline void more_registers()
+{
+    if (kBlocks == 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+}
+
+// What a block works on: unit u of `units`, a stretch of the keys of a block of rows of one key head.  A block takes the units
+// blockIdx.x, blockIdx.x + gridDim.x, ...
+struct TcShape {
+    uint32_t units;
+    int tiles, splits;                               // blocks of rows (or keys) per sequence and key head; stretches of the keys
+};
+struct Work {
+    SeqRange rg;
+    int64_t rows, kb, ke;
+    int z, t0, h, n;                                 // n: tiles of keys
+};
+__device__ inline Work work_of(const AttnArgs &a, const TcShape &f, uint32_t u, bool report)
+{
+    Work x;
+    x.z = 0;
+    if (f.splits > 1) {
+        x.z = (int)(u % (uint32_t)f.splits);
+        u /= (uint32_t)f.splits;
+    }
+    x.t0 = 0;
+    if (f.tiles > 1) {
+        x.t0 = (int)(u % (uint32_t)f.tiles);
+        u /= (uint32_t)f.tiles;
+    }
+    const uint32_t s = u / (uint32_t)a.kv_heads;
+    x.h = (int)(u - s * (uint32_t)a.kv_heads);
+    x.rg = seq_range(a, s, report && x.z == 0 && x.t0 == 0 && x.h == 0);
+    x.rows = (x.rg.q1 - x.rg.q0) * a.group;
+    x.kb = x.rg.k0;
+    x.ke = x.rg.k1;
+    if (f.splits > 1) {
+        const int64_t per = ((x.rg.k1 - x.rg.k0 + f.splits - 1) / f.splits + kTile - 1) / kTile * kTile;
+        x.kb = min(x.rg.k0 + x.z * per, x.rg.k1);
+        x.ke = min(x.kb + per, x.rg.k1);
+    }
+    x.n = (int)((x.ke - x.kb + kTile - 1) / kTile);
+    return x;
+}
+// (query row, head) of row r of the key head's matrix
+__device__ inline void row_of(const AttnArgs &a, const Work &x, int64_t r, int64_t &row, int &head)
+{
+    const int64_t i = a.group == 1 ? r : (r >> 32 ? r / a.group : (int64_t)((uint32_t)r / (uint32_t)a.group));
+    row = x.rg.q0 + i;
+    head = x.h * a.group + (int)(r - i * a.group);
+}
 
 // 32 rows (a quarter of a tile) -> shared memory.  A lane keeps to one 16-byte chunk of the rows, 8 NB lanes side by side take a row;
 // chunks: those that the products read, of which `real` exist (the others are zeros); any: an address that may be named where
@@ -150,39 +206,31 @@ __device__ inline void row_steps(uint32_t d, uint32_t a, uint32_t second, uint64
 }
 
 // ------------------------------------------------------------------------------------------------- forward
-constexpr int kFwdRows = 2 * kTile;                  // rows of a block: one tile per softmax warpgroup
+// NT tiles of 128 rows per block, a softmax warpgroup each.  Two where a key head has more than 128 rows: they share the copies of
+// keys and values, and the products of one run beside the softmax of the other.  One, in half of the shared and tensor memory, where
+// the second would idle: two such blocks per SM overlap instead.
+template <int NB, int NT> struct Fwd {
+    static constexpr int kStages = NT == 2 ? (NB == 2 ? 5 : 8) : (NB == 2 ? 2 : 5);
+    static constexpr int kSoft = NT * 4, kMma = kSoft + kLoaders, kThreads = (kSoft + 4) * 32, kBlocks = 3 - NT;
+    static constexpr int kRows = NT * kTile, kTileBytes = NB * kBlockBytes, kColumns = NT * 256;
+    static constexpr size_t kSmem = 1024 + (size_t)(NT + kStages) * kTileBytes;
+};
 
-template <int NB> constexpr int fwd_stages() { return NB == 2 ? 5 : 8; }
-template <int NB> constexpr size_t fwd_smem() { return 1024 + (size_t)(2 + fwd_stages<NB>()) * NB * kBlockBytes; }
-
-template <int NB>
-__global__ void __launch_bounds__(kThreads, 1)
-attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, float *__restrict__ part_o, float2 *__restrict__ part_ml)
+template <int NB, int NT>
+__global__ void __launch_bounds__(Fwd<NB, NT>::kThreads, Fwd<NB, NT>::kBlocks)
+attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
 {
-    constexpr int kStages = NB == 2 ? 5 : 8, kTileBytes = NB * kBlockBytes;
+    using F = Fwd<NB, NT>;
+    constexpr int kStages = F::kStages, kTileBytes = F::kTileBytes, kRows = F::kRows, kSoft = F::kSoft;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], q_full, q_empty, s_full[2], p_full[2], o_full[2], o_empty[2];
+    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], q_full, q_empty, s_full[NT], p_full[NT], o_full[NT], o_empty[NT];
     __shared__ uint32_t words[kWordRing][4];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int64_t u = blockIdx.x;
-    const int z = (int)(u % splits);
-    u /= splits;
-    const int t0 = (int)(u % tiles);
-    u /= tiles;
-    const int h = (int)(u % a.kv_heads);
-    const SeqRange rg = seq_range(a, u / a.kv_heads, z == 0 && t0 == 0 && h == 0 && threadIdx.x == 0);
-    const int64_t rows = (rg.q1 - rg.q0) * a.group;
-    if ((int64_t)t0 * kFwdRows >= rows) return;
-    const int64_t klen = rg.k1 - rg.k0;
-    const int64_t per = ceil_div(ceil_div(klen, splits), kTile) * kTile;
-    const int64_t kb = min(rg.k0 + z * per, rg.k1), ke = min(kb + per, rg.k1);
-    const int n = (int)ceil_div(ke - kb, kTile);
-
     uint8_t *tiles_smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    const uint32_t q_smem = smem_u32(tiles_smem), kv_smem = q_smem + 2 * kTileBytes;
+    const uint32_t q_smem = smem_u32(tiles_smem), kv_smem = q_smem + NT * kTileBytes;
     const int ksteps = (a.head_dim + 15) / 16;
 
     if (threadIdx.x == 0) {
@@ -192,7 +240,7 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
         }
         mbar_init(&q_full, kTileArrivals);
         mbar_init(&q_empty, 1);
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < NT; ++t) {
             mbar_init(&s_full[t], 1);
             mbar_init(&p_full[t], 4);
             mbar_init(&o_full[t], 1);
@@ -202,210 +250,223 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == kMmaWarp) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
+    if (warp == F::kMma) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "n"(F::kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot;                  // scores (and p) of tile t: columns 128 t; outputs: 256 + 64 NB t
+    const uint32_t tmem = tmem_slot, tmem_o = tmem + NT * kTile;      // scores (and p) of tile t: columns 128 t; outputs: 64 NB each behind them
 
-    if (warp >= 8) {
-    fewer_registers();
-    if (warp < kMmaWarp) {
-        // ---- copies: queries of a block of rows, then keys and values in turn
-        const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8;
-        uint32_t g = 0, jj = 0, item = 0;
-        bool ok = true;
-        for (int64_t t = t0; t * kFwdRows < rows && n > 0 && ok; t += tiles, ++item) {
-            if (item > 0) ok = warp_wait(&q_empty, (item - 1) & 1u, &abort_flag);
-            if (!ok) break;
-            for (int b = w; b < kFwdRows / 32; b += kLoaders) {
-                const int64_t r = t * kFwdRows + b * 32 + lane;
-                const bf16 *src = nullptr;
-                if (r < rows) {
-                    const int64_t i = r / a.group;
-                    src = static_cast<const bf16 *>(a.q) + (rg.q0 + i) * a.ldq + (h * a.group + (int)(r - i * a.group)) * (int64_t)a.head_dim;
-                }
-                copy_each<NB>(q_smem + (b >> 2) * kTileBytes, b & 3, src, a.q, chunks, real, lane);
-            }
-            announce(&q_full, lane);
-            for (int j = 0; j < n && ok; ++j, ++jj) {
-                uint32_t word[4 / kLoaders];
-#pragma unroll
-                for (int b = 0; b < 4 / kLoaders; ++b) {
-                    const int64_t key = kb + (int64_t)j * kTile + (w + b * kLoaders) * 32 + lane;
-                    word[b] = __ballot_sync(0xFFFFFFFFu, key < ke && (!a.mask || a.mask[key]));
-                }
-                for (int v = 0; v < 2; ++v, ++g) {
-                    const uint32_t s = g % kStages;
-                    if (g >= kStages) ok = warp_wait(&kv_empty[s], (g / kStages - 1) & 1u, &abort_flag);
-                    if (!ok) break;
-#pragma unroll
-                    for (int b = 0; b < 4 / kLoaders; ++b) {
-                        const int part = w + b * kLoaders;
-                        const int64_t key = kb + (int64_t)j * kTile + part * 32, ld = v ? a.ldv : a.ldk;
-                        if (v == 0 && lane == 0) words[jj % kWordRing][part] = word[b];
-                        copy_rows<NB>(kv_smem + s * kTileBytes, part, static_cast<const bf16 *>(v ? a.v : a.k) + key * ld + h * (int64_t)a.head_dim, ld,
-                                      word[b], a.q, chunks, real, lane);
-                    }
-                    announce(&kv_full[s], lane);
-                }
-            }
-        }
-        cp_async_wait_all();
-    } else if (warp == kMmaWarp) {
-        // ---- products
-        if (elect_one()) {
-            const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
-            uint32_t g = 0, item = 0, pc[2] = {0, 0};
+    if (warp >= kSoft) {
+        fewer_registers<F::kBlocks>();
+        if (warp < F::kMma) {
+            // ---- copies: queries of a block of rows, then keys and values in turn
+            const int w = warp - kSoft, chunks = 2 * ksteps, real = a.head_dim / 8;
+            uint32_t g = 0, jj = 0, item = 0;
             bool ok = true;
-            for (int64_t t = t0; t * kFwdRows < rows && n > 0 && ok; t += tiles, ++item) {
-                const int nt = rows - t * kFwdRows > kTile ? 2 : 1;
-                ok = tile_ready(&q_full, item & 1u, &abort_flag);
-                if (item > 0)
-                    for (int q = 0; q < nt && ok; ++q) ok = mbar_wait(&o_empty[q], (item - 1) & 1u, &abort_flag);
+            for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
+                const Work x = work_of(a, f, u, w == 0 && lane == 0);
+                for (int64_t t = x.t0; t * kRows < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
+                    if (item > 0) ok = warp_wait(&q_empty, (item - 1) & 1u, &abort_flag);
+                    if (!ok) break;
+                    for (int b = w; b < kRows / 32; b += kLoaders) {
+                        const int64_t r = t * kRows + b * 32 + lane;
+                        int64_t row;
+                        int head;
+                        row_of(a, x, r, row, head);
+                        copy_each<NB>(q_smem + (b >> 2) * kTileBytes, b & 3,
+                                      r < x.rows ? static_cast<const bf16 *>(a.q) + row * a.ldq + (int64_t)head * a.head_dim : nullptr, a.q, chunks, real, lane);
+                    }
+                    announce(&q_full, lane);
+                    for (int j = 0; j < x.n && ok; ++j, ++jj) {
+                        uint32_t word[4 / kLoaders];
+#pragma unroll
+                        for (int b = 0; b < 4 / kLoaders; ++b) {
+                            const int64_t key = x.kb + (int64_t)j * kTile + (w + b * kLoaders) * 32 + lane;
+                            word[b] = __ballot_sync(0xFFFFFFFFu, key < x.ke && (!a.mask || a.mask[key]));
+                        }
+                        for (int v = 0; v < 2; ++v, ++g) {
+                            const uint32_t s = g % kStages;
+                            if (g >= kStages) ok = warp_wait(&kv_empty[s], (g / kStages - 1) & 1u, &abort_flag);
+                            if (!ok) break;
+#pragma unroll
+                            for (int b = 0; b < 4 / kLoaders; ++b) {
+                                const int part = w + b * kLoaders;
+                                const int64_t key = x.kb + (int64_t)j * kTile + part * 32, ld = v ? a.ldv : a.ldk;
+                                if (v == 0 && lane == 0) words[jj % kWordRing][part] = word[b];
+                                copy_rows<NB>(kv_smem + s * kTileBytes, part,
+                                              static_cast<const bf16 *>(v ? a.v : a.k) + key * ld + x.h * (int64_t)a.head_dim, ld, word[b], a.q, chunks,
+                                              real, lane);
+                            }
+                            announce(&kv_full[s], lane);
+                        }
+                    }
+                }
+            }
+            cp_async_wait_all();
+        } else if (warp == F::kMma) {
+            // ---- products
+            if (elect_one()) {
+                const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
+                uint32_t g = 0, item = 0, pc[NT] = {}, used[NT] = {};
+                bool ok = true;
                 auto scores = [&](uint32_t gk, int q) {
                     head_steps<NB>(tmem + q * kTile, make_smem_desc(q_smem + q * kTileBytes), make_smem_desc(kv_smem + (gk % kStages) * kTileBytes), id_s,
                                    ksteps);
                     umma_commit(&s_full[q]);
                 };
-                if (ok) ok = tile_ready(&kv_full[g % kStages], (g / kStages) & 1u, &abort_flag);
-                if (ok) {
-                    for (int q = 0; q < nt; ++q) scores(g, q);
-                    umma_commit(&kv_empty[g % kStages]);
-                }
-                for (int j = 0; j < n && ok; ++j, g += 2) {
-                    const uint32_t gv = g + 1, gk = g + 2;
-                    const uint64_t v_desc = make_smem_desc_mn(kv_smem + (gv % kStages) * kTileBytes, kBlockBytes);
-                    ok = tile_ready(&kv_full[gv % kStages], (gv / kStages) & 1u, &abort_flag);
-                    for (int q = 0; q < nt && ok; ++q) {
-                        ok = mbar_wait(&p_full[q], pc[q]++ & 1u, &abort_flag);
-                        if (!ok) break;
-                        tc_fence_after();
-                        row_steps(tmem + 256 + q * 64 * NB, tmem + q * kTile, 0, v_desc, id_o, j > 0);
-                        if (j + 1 < n) {
-                            if (q == 0) {
-                                ok = tile_ready(&kv_full[gk % kStages], (gk / kStages) & 1u, &abort_flag);
-                                if (!ok) break;
+                for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
+                    const Work x = work_of(a, f, u, false);
+                    for (int64_t t = x.t0; t * kRows < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
+                        const int nt = NT == 2 && x.rows - t * kRows > kTile ? 2 : 1;
+                        ok = tile_ready(&q_full, item & 1u, &abort_flag);
+                        if (ok) ok = tile_ready(&kv_full[g % kStages], (g / kStages) & 1u, &abort_flag);
+#pragma unroll
+                        for (int q = 0; q < NT; ++q)
+                            if (q < nt && ok) {
+                                // the outputs that the tile held last have been read
+                                if (used[q] > 0) ok = mbar_wait(&o_empty[q], (used[q] - 1) & 1u, &abort_flag);
+                                tc_fence_after();
+                                if (ok) scores(g, q);
+                                ++used[q];
                             }
-                            if (q == nt - 1) umma_commit(&kv_empty[gv % kStages]);
-                            scores(gk, q);
-                            if (q == nt - 1) umma_commit(&kv_empty[gk % kStages]);
-                        } else {
-                            umma_commit(&o_full[q]);
-                            if (q == nt - 1) {
-                                umma_commit(&kv_empty[gv % kStages]);
-                                umma_commit(&q_empty);
+                        if (ok) umma_commit(&kv_empty[g % kStages]);
+                        for (int j = 0; j < x.n && ok; ++j, g += 2) {
+                            const uint32_t gv = g + 1, gk = g + 2;
+                            const uint64_t v_desc = make_smem_desc_mn(kv_smem + (gv % kStages) * kTileBytes, kBlockBytes);
+                            ok = tile_ready(&kv_full[gv % kStages], (gv / kStages) & 1u, &abort_flag);
+#pragma unroll
+                            for (int q = 0; q < NT; ++q) {
+                                if (q >= nt || !ok) continue;
+                                ok = mbar_wait(&p_full[q], pc[q]++ & 1u, &abort_flag);
+                                if (!ok) continue;
+                                tc_fence_after();
+                                row_steps(tmem_o + q * 64 * NB, tmem + q * kTile, 0, v_desc, id_o, j > 0);
+                                if (j + 1 < x.n) {
+                                    if (q == nt - 1) umma_commit(&kv_empty[gv % kStages]);
+                                    if (q == 0) ok = tile_ready(&kv_full[gk % kStages], (gk / kStages) & 1u, &abort_flag);
+                                    if (!ok) continue;
+                                    scores(gk, q);
+                                    if (q == nt - 1) umma_commit(&kv_empty[gk % kStages]);
+                                } else {
+                                    umma_commit(&o_full[q]);
+                                    if (q == nt - 1) {
+                                        umma_commit(&kv_empty[gv % kStages]);
+                                        umma_commit(&q_empty);
+                                    }
+                                }
                             }
                         }
                     }
                 }
             }
         }
-    }
     } else {
-        more_registers();
+        more_registers<F::kBlocks>();
         // ---- softmax of tile `q`, one row per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
-        const uint32_t s_addr = tmem + lanes + q * kTile, o_addr = tmem + lanes + 256 + q * 64 * NB;
+        const uint32_t s_addr = tmem + lanes + q * kTile, o_addr = tmem_o + lanes + q * 64 * NB;
         const float c1 = a.scale * kLog2e;
         const int heads = a.kv_heads * a.group;
-        uint32_t jj = 0, item = 0, sc = 0, oc = 0;
+        uint32_t jj = 0, sc = 0, oc = 0;
         bool ok = true;
-        for (int64_t t = t0; t * kFwdRows < rows && ok; t += tiles, ++item) {
-            const int64_t r = t * kFwdRows + q * kTile + w * 32 + lane;
-            const bool active = rows - t * kFwdRows > q * kTile;
-            float m = -INFINITY, l = 0.f;
-            if (!active) jj += n;
-            for (int j = 0; j < n && active; ++j, ++jj) {
-                ok = mbar_wait(&s_full[q], sc++ & 1u, &abort_flag);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                tc_fence_after();
-                uint32_t word[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) word[c] = words[jj % kWordRing][c];
-                // the row's 128 scores stay in registers; four chains for the maximum
-                uint32_t v[4][32];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) tmem_load32_async(s_addr + c * 32, v[c]);
-                tmem_load_wait();
-                float tops[4];
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    if (word[c] != 0xFFFFFFFFu) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (!((word[c] >> i) & 1u)) v[c][i] = 0xFF800000u;
-                    }
-                    tops[c] = __uint_as_float(v[c][0]);
-#pragma unroll
-                    for (int i = 1; i < 32; ++i) tops[c] = fmaxf(tops[c], __uint_as_float(v[c][i]));
+        for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
+            const Work x = work_of(a, f, u, false);
+            for (int64_t t = x.t0; t * kRows < x.rows && ok; t += f.tiles) {
+                const int64_t r = t * kRows + q * kTile + w * 32 + lane;
+                if (x.rows - t * kRows <= q * kTile) {       // no rows for this warpgroup
+                    jj += x.n;
+                    continue;
                 }
-                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-                // The maximum that p and l refer to moves only where a score exceeds it by 8 in the exponent: p <= 2^8 loses
-                // nothing in floating point, and the sums so far are rescaled seldom.
-                const bool moves = top * c1 > m * c1 + 8.f || m == -INFINITY;
-                if (j > 0 && __any_sync(0xFFFFFFFFu, moves && top != -INFINITY)) {
-                    const float f = moves && top != -INFINITY ? exp2_approx((m - top) * c1) : 1.f;
-                    l *= f;
-                    for (int c = 0; c < NB * 4; ++c) {
-                        uint32_t x[16];
-                        tmem_load16_async(o_addr + c * 16, x);
-                        tmem_load_wait();
+                float m = -INFINITY, l = 0.f;
+                for (int j = 0; j < x.n; ++j, ++jj) {
+                    ok = warp_wait(&s_full[q], sc++ & 1u, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    uint32_t word[4];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
-                        tmem_store16(o_addr + c * 16, x);
+                    for (int c = 0; c < 4; ++c) word[c] = words[jj % kWordRing][c];
+                    // the row's 128 scores stay in registers; four chains for the maximum
+                    uint32_t v[4][32];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) tmem_load32_async(s_addr + c * 32, v[c]);
+                    tmem_load_wait();
+                    float tops[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        if (word[c] != 0xFFFFFFFFu) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i)
+                                if (!((word[c] >> i) & 1u)) v[c][i] = 0xFF800000u;
+                        }
+                        tops[c] = __uint_as_float(v[c][0]);
+#pragma unroll
+                        for (int i = 1; i < 32; ++i) tops[c] = fmaxf(tops[c], __uint_as_float(v[c][i]));
                     }
-                }
-                if (moves) m = top;
-                const float base = m == -INFINITY ? 0.f : m * c1;
-                const float2 scale2 = make_float2(c1, c1), base2 = make_float2(-base, -base);
-                float2 sums[4];
+                    const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                    // The maximum that p and l refer to moves only where a score exceeds it by 8 in the exponent: p <= 2^8 loses
+                    // nothing in floating point, and the sums so far are rescaled seldom.
+                    const bool moves = top * c1 > m * c1 + 8.f || m == -INFINITY;
+                    if (j > 0 && __any_sync(0xFFFFFFFFu, moves && top != -INFINITY)) {
+                        const float f = moves && top != -INFINITY ? exp2_approx((m - top) * c1) : 1.f;
+                        l *= f;
+                        for (int c = 0; c < NB * 4; ++c) {
+                            uint32_t x[16];
+                            tmem_load16_async(o_addr + c * 16, x);
+                            tmem_load_wait();
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t p[16];
-                    sums[c] = make_float2(0.f, 0.f);
-#pragma unroll
-                    for (int i = 0; i < 32; i += 2) {
-                        float2 x = __ffma2_rn(make_float2(__uint_as_float(v[c][i]), __uint_as_float(v[c][i + 1])), scale2, base2);
-                        x.x = exp2_approx(x.x);
-                        x.y = exp2_approx(x.y);
-                        sums[c] = __fadd2_rn(sums[c], x);
-                        p[i / 2] = pack_bf16(x.x, x.y);
+                            for (int i = 0; i < 16; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * f);
+                            tmem_store16(o_addr + c * 16, x);
+                        }
                     }
-                    tmem_store16(s_addr + c * 16, p);
+                    if (moves) m = top;
+                    const float base = m == -INFINITY ? 0.f : m * c1;
+                    const float2 scale2 = make_float2(c1, c1), base2 = make_float2(-base, -base);
+                    float2 sums[4];
+#pragma unroll
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t p[16];
+                        sums[c] = make_float2(0.f, 0.f);
+#pragma unroll
+                        for (int i = 0; i < 32; i += 2) {
+                            float2 x = __ffma2_rn(make_float2(__uint_as_float(v[c][i]), __uint_as_float(v[c][i + 1])), scale2, base2);
+                            x.x = exp2_approx(x.x);
+                            x.y = exp2_approx(x.y);
+                            sums[c] = __fadd2_rn(sums[c], x);
+                            p[i / 2] = pack_bf16(x.x, x.y);
+                        }
+                        tmem_store16(s_addr + c * 16, p);
+                    }
+                    const float sum = (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y) + ((sums[2].x + sums[2].y) + (sums[3].x + sums[3].y));
+                    l += sum;
+                    tmem_store_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_full[q]);
                 }
-                const float sum = (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y) + ((sums[2].x + sums[2].y) + (sums[3].x + sums[3].y));
-                l += sum;
-                tmem_store_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full[q]);
-            }
-            if (!ok) break;
-            if (active && n > 0) {
-                ok = mbar_wait(&o_full[q], oc++ & 1u, &abort_flag);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                tc_fence_after();
-            }
-            const int64_t i = r / a.group;
-            const int head = h * a.group + (int)(r - i * a.group);
-            const int64_t row = rg.q0 + i;
-            const bool live = r < rows;
-            const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
-            if (active)
+                if (!ok) break;
+                if (x.n > 0) {
+                    ok = warp_wait(&o_full[q], oc++ & 1u, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                int64_t row;
+                int head;
+                row_of(a, x, r, row, head);
+                const bool live = r < x.rows;
+                const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
                 for (int c = 0; c < NB * 2; ++c) {
                     uint32_t v[32];
-                    if (n > 0) {
+                    if (x.n > 0) {
                         tmem_load32_async(o_addr + c * 32, v);
                         tmem_load_wait();
                     }
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) v[e] = n > 0 && l != 0.f ? __float_as_uint(__uint_as_float(v[e]) * inv) : 0u;
-                    if (live && splits == 1) {
+                    for (int e = 0; e < 32; ++e) v[e] = x.n > 0 && l != 0.f ? __float_as_uint(__uint_as_float(v[e]) * inv) : 0u;
+                    if (live && f.splits == 1) {
                         bf16 *out = static_cast<bf16 *>(a.out) + row * a.ldo + (int64_t)head * a.head_dim + c * 32;
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
@@ -416,32 +477,35 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, int tiles, int splits, fl
                                 *reinterpret_cast<uint4 *>(out + e * 8) = make_uint4(p[0], p[1], p[2], p[3]);
                             }
                     } else if (live) {
-                        float *out = part_o + (((int64_t)z * a.q_rows + row) * heads + head) * a.head_dim + c * 32;
+                        float *out = part_o + (((int64_t)x.z * a.q_rows + row) * heads + head) * a.head_dim + c * 32;
 #pragma unroll
                         for (int e = 0; e < 8; ++e)
                             if (c * 32 + e * 4 < a.head_dim) *reinterpret_cast<uint4 *>(out + e * 4) = make_uint4(v[e * 4], v[e * 4 + 1], v[e * 4 + 2], v[e * 4 + 3]);
                     }
                 }
-            if (live && active) {
-                if (splits > 1) part_ml[((int64_t)z * a.q_rows + row) * heads + head] = make_float2(l == 0.f ? -INFINITY : m * c1, l);
-                else if (a.lse) a.lse[row * heads + head] = l == 0.f ? -INFINITY : (m * c1 + log2f(l)) * kLn2;
+                if (x.n > 0) {                               // the accumulator has been read: the next block of rows may use it
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&o_empty[q]);
+                }
+                if (live) {
+                    if (f.splits > 1) part_ml[((int64_t)x.z * a.q_rows + row) * heads + head] = make_float2(l == 0.f ? -INFINITY : m * c1, l);
+                    else if (a.lse) a.lse[row * heads + head] = l == 0.f ? -INFINITY : (m * c1 + log2f(l)) * kLn2;
+                }
             }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0 && n > 0 && active) mbar_arrive(&o_empty[q]);      // only the last block of rows may lack the second tile
         }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && abort_flag && a.status) atomicOr(reinterpret_cast<unsigned *>(a.status), E2EGREC_DEV_TIMEOUT);
-    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == F::kMma) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(F::kColumns) : "memory");
 }
 
 // ------------------------------------------------------------------------------------------------- backward
 // Two kernels, so that no gradient is added up by atomics: dQ goes over the keys of a tile of rows, dK and dV over the rows of a
 // tile of keys; the scores are formed in both.  Two warpgroups share a tile of 128 x 128: 64 columns each, one row per thread.
-template <int NB> constexpr size_t dq_smem() { return 1024 + (size_t)(2 + fwd_stages<NB>()) * NB * kBlockBytes; }
+template <int NB> constexpr size_t dq_smem() { return 1024 + (size_t)(2 + (NB == 2 ? 5 : 8)) * NB * kBlockBytes; }
 template <int NB> constexpr size_t dkv_smem() { return 1024 + (size_t)(2 + 4) * NB * kBlockBytes; }
 
 // 64 columns of p or dS of a thread's row as an operand in tensor memory: 32 packed columns
@@ -530,7 +594,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
     const uint32_t tmem = tmem_slot;                  // scores: columns 0 and 128 in turn; dP and dS: 256; dQ: 384
 
     if (warp >= 8) {
-    fewer_registers();
+    fewer_registers<1>();
     if (warp < kMmaWarp) {
         // ---- copies: Q and dO of a tile of rows, then keys and values in turn
         const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8;
@@ -620,7 +684,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
         }
     }
     } else {
-        more_registers();
+        more_registers<1>();
         // ---- p and dS: 64 columns of one row per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
@@ -758,7 +822,7 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
     const uint32_t tmem = tmem_slot;                  // S^T and P^T: columns 0; dP^T and dS^T: 128; dV: 256; dK: 384
 
     if (warp >= 8) {
-    fewer_registers();
+    fewer_registers<1>();
     if (warp < kMmaWarp) {
         // ---- copies: keys and values of a tile, then Q and dO of the rows in turn, with the rows' lse and D
         const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8, heads = a.kv_heads * a.group;
@@ -868,7 +932,7 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
         }
     }
     } else {
-        more_registers();
+        more_registers<1>();
         // ---- p and dS: 64 columns (rows of Q) of one key per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
@@ -963,18 +1027,25 @@ template <typename Kernel> bool allow_smem(Kernel kernel, size_t bytes, bool (&d
 
 }  // namespace
 
-int tc_fwd_rows() { return kFwdRows; }
+// Small units in numbers go to as many blocks as the machine holds, which prefetch from unit to unit; fewer units get a block each,
+// so that the hardware hands them out as blocks end.
+static uint32_t tc_grid(uint32_t units, int blocks) { return units >= 8u * kSms * blocks ? kSms * blocks : units; }
 
-bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, float *part_o, float2 *part_ml, cudaStream_t st)
+template <int NB, int NT> static bool launch_fwd(const AttnArgs &a, const TcShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    static bool done[2][kMaxDevices] = {};
-    const bool one = a.head_dim <= 64;
-    if (!(one ? allow_smem(attn_tc_fwd_kernel<1>, fwd_smem<1>(), done[0]) : allow_smem(attn_tc_fwd_kernel<2>, fwd_smem<2>(), done[1]))) return false;
-    const unsigned grid = (unsigned)(a.n_seq * a.kv_heads * tiles * splits);
+    static bool done[kMaxDevices] = {};
+    using F = Fwd<NB, NT>;
+    if (!allow_smem(attn_tc_fwd_kernel<NB, NT>, F::kSmem, done)) return false;
     note_launch();
-    if (one) attn_tc_fwd_kernel<1><<<grid, kThreads, fwd_smem<1>(), st>>>(a, (int)tiles, splits, part_o, part_ml);
-    else attn_tc_fwd_kernel<2><<<grid, kThreads, fwd_smem<2>(), st>>>(a, (int)tiles, splits, part_o, part_ml);
+    attn_tc_fwd_kernel<NB, NT><<<tc_grid(f.units, F::kBlocks), F::kThreads, F::kSmem, st>>>(a, f, part_o, part_ml);
     return true;
+}
+
+bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, bool one_tile, float *part_o, float2 *part_ml, cudaStream_t st)
+{
+    const TcShape f{(uint32_t)(a.n_seq * a.kv_heads * tiles * splits), (int)tiles, splits};
+    if (a.head_dim <= 64) return one_tile ? launch_fwd<1, 1>(a, f, part_o, part_ml, st) : launch_fwd<1, 2>(a, f, part_o, part_ml, st);
+    return one_tile ? launch_fwd<2, 1>(a, f, part_o, part_ml, st) : launch_fwd<2, 2>(a, f, part_o, part_ml, st);
 }
 
 bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st)
