@@ -145,7 +145,8 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     const int64_t rows = max_q * a.group, units = std::max<int64_t>(a.n_seq * a.kv_heads, 1);
     const size_t cells = (size_t)a.q_rows * a.kv_heads * a.group;
     const bool small = rows <= kFewRows || rows * max_k <= (dtype == E2EGREC_F32 ? 256 : (backward ? 800 : 2048));
-    p.path = small || a.head_dim > 128 ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
+    // (without rows on one side there is nothing to form a product of)
+    p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
     if (p.path == Path::tc) {
         const int64_t most = (kMaxRows - 1) / units;
         p.one_tile = rows <= 128;

@@ -3,15 +3,18 @@
 // The rows of a product are the (query, head of the group) pairs of one key head of one sequence; tiles are 128 x 128.  Every
 // operand tile lies in shared memory as blocks of 64 columns, 128 lines of 128 bytes each, 128-byte swizzled: the same bytes serve
 // as an operand whose K index is contiguous (Q, K, V, dO against head_dim) and as one whose N index is (V, K, Q, dO against rows).
-// Tiles are copied by cp.async, 16 bytes per lane, each loading warp half of the rows: rows behind a sequence's end and hidden keys are
-// filled with zeros without being read, which a box of a tensor map cannot do, and any offset, stride and head width
-// goes.  Scores and gradients of scores go back to the tensor cores through tensor memory (A operand), never through shared memory.
+// Tiles are TMA boxes of three-dimensional maps (columns of a head, heads, rows): columns behind a head's end read as zeros, a box of
+// G heads of 128 / G rows is the rows of G query heads.  Rows behind a sequence's end and hidden keys arrive as whatever they hold;
+// where such a row would meet p = 0 or dS = 0 in a product (0 x NaN), one warp overwrites it with zeros first.  Scores and gradients of
+// scores go back to the tensor cores through tensor memory (A operand), never through shared memory.
+// With cp.async for the tiles, zero-filled on the way, the two copying warps were the bound: 47 cycles per 512 bytes and warp.
 // Every wait is bounded; when one runs out the block reports E2EGREC_DEV_TIMEOUT, lets its copies land, frees its tensor memory
 // and returns.
 #include <algorithm>
 
 #include "attention.cuh"
 #include "tcgen05.cuh"
+#include "tensor_map.cuh"
 
 namespace e2egrec {
 namespace {
@@ -19,11 +22,9 @@ namespace {
 using bf16 = __nv_bfloat16;
 
 constexpr int kTile = 128;
-constexpr int kThreads = 12 * 32;                    // two warpgroups over scores, two loading warps, the products' warp; one idle
-constexpr int kLoaders = 2, kMmaWarp = 8 + kLoaders;
-constexpr int kSms = 148;
 constexpr int kBlockBytes = kTile * 128;             // 64 columns of 128 rows
 constexpr int kWordRing = 8;                         // tiles whose visibility words are kept
+constexpr int kSms = 148;
 
 __device__ inline float exp2_approx(float x)
 {
@@ -62,16 +63,12 @@ __device__ inline void tmem_load16_async(uint32_t taddr, uint32_t (&r)[16])
         : "r"(taddr));
 }
 
-// Registers are dealt out anew once the block runs.  One block per SM: 384 threads x 168 at launch = 128 (copies and products) x 88 +
-// 256 x 208.  Two blocks per SM: 256 threads x 128 = 128 x 72 + 128 x 184.
-template <int kBlocks> __device__ inline void fewer_registers()
-{
-    if (kBlocks == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-}
+// Registers are dealt out anew once the block runs.  One block per SM: 384 threads x 168 at launch = 128 (copies and products) x 72 +
+// 256 x 216.  Two blocks per SM: 256 threads x 128 = 128 x 72 + 128 x 184.
+template <int kBlocks> __device__ inline void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
 template <int kBlocks> __device__ inline void more_registers()
 {
-    if (kBlocks == 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+    if (kBlocks == 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     else asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
 }
 
@@ -80,6 +77,7 @@ template <int kBlocks> __device__ inline void more_registers()
 struct TcShape {
     uint32_t units;
     int tiles, splits;                               // blocks of rows (or keys) per sequence and key head; stretches of the keys
+    int boxes;                                       // rows of the group's heads come as boxes (the group divides 128)
 };
 struct Work {
     SeqRange rg;
@@ -121,60 +119,85 @@ __device__ inline void row_of(const AttnArgs &a, const Work &x, int64_t r, int64
     head = x.h * a.group + (int)(r - i * a.group);
 }
 
-// 32 rows (a quarter of a tile) -> shared memory.  A lane keeps to one 16-byte chunk of the rows, 8 NB lanes side by side take a row;
-// chunks: those that the products read, of which `real` exist (the others are zeros); any: an address that may be named where
-// nothing is read.  copy_rows: rows `stride` elements apart, those whose bit in `word` is off are zeros.  copy_each: the lane's own row
-// (its first element of the head), null for zeros.
-template <int NB> __device__ inline uint32_t chunk_place(uint32_t tile, int part, int lane)
+// One box of 64 columns x 128 rows: column x of head y, row z and on
+__device__ inline void tma_load_3d(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint64_t *bar)
 {
-    const int ch = lane & (8 * NB - 1), row = lane / (8 * NB);
-    return tile + (uint32_t)(ch >> 3) * kBlockBytes + (uint32_t)(part * 32 + row) * 128u + (uint32_t)(((ch & 7) ^ row) << 4);
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar))
+                 : "memory");
 }
+template <int NB> __device__ inline void load_tile(uint32_t dst, const CUtensorMap *map, int head, int64_t row, uint64_t *bar)
+{
+#pragma unroll
+    for (int b = 0; b < NB; ++b) tma_load_3d(dst + b * kBlockBytes, map, b * 64, head, (int)row, bar);
+}
+
+// The same tile by cp.async, for groups of heads that do not divide 128 (no box has their rows): 32 rows (a quarter) by one warp.  A
+// lane keeps to one 16-byte chunk of the rows, 8 NB lanes side by side take a row; mine: the lane's own row (its first element of the
+// head), null for zeros; any: an address that may be named where nothing is read.
 template <int NB>
-__device__ inline void copy_rows(uint32_t tile, int part, const bf16 *first, int64_t stride, uint32_t word, const void *any, int chunks, int real,
-                                 int lane)
+__device__ inline void copy_each(uint32_t tile, int part, const bf16 *mine, const void *any, int head_dim, int lane)
 {
     constexpr int kPer = 4 / NB;                          // rows per step
     const int ch = lane & (8 * NB - 1), row = lane / (8 * NB);
-    if (ch >= chunks) return;
-    const uint32_t dst = chunk_place<NB>(tile, part, lane);
-    const bf16 *src = first + row * stride + ch * 8;
-    const int64_t step = stride * kPer;
-    word = ch < real ? word >> row : 0u;
-#pragma unroll
-    for (int i = 0; i < 8 * NB; ++i) {
-        const bool on = (word >> (i * kPer)) & 1u;
-        // row * 128, and the swizzle's exclusive or of the row's low bits with the chunk
-        cp_async16((dst ^ (uint32_t)(((i * kPer) & 7) << 4)) + (uint32_t)(i * kPer) * 128u, on ? static_cast<const void *>(src) : any, on);
-        src += step;
-    }
-}
-template <int NB>
-__device__ inline void copy_each(uint32_t tile, int part, const bf16 *mine, const void *any, int chunks, int real, int lane)
-{
-    constexpr int kPer = 4 / NB;
-    const int ch = lane & (8 * NB - 1), row = lane / (8 * NB);
-    const uint32_t dst = chunk_place<NB>(tile, part, lane);
+    const uint32_t dst = tile + (uint32_t)(ch >> 3) * kBlockBytes + (uint32_t)(part * 32 + row) * 128u + (uint32_t)(((ch & 7) ^ row) << 4);
 #pragma unroll
     for (int i = 0; i < 8 * NB; ++i) {
         const uint64_t p = __shfl_sync(0xFFFFFFFFu, reinterpret_cast<uint64_t>(mine), row + i * kPer);
-        const bool on = p != 0 && ch < real;
-        if (ch < chunks)
-            cp_async16((dst ^ (uint32_t)(((i * kPer) & 7) << 4)) + (uint32_t)(i * kPer) * 128u,
-                       on ? static_cast<const void *>(reinterpret_cast<const bf16 *>(p) + ch * 8) : any, on);
+        const bool on = p != 0 && ch * 8 < head_dim;
+        // row * 128, and the swizzle's exclusive or of the row's low bits with the chunk
+        cp_async16((dst ^ (uint32_t)(((i * kPer) & 7) << 4)) + (uint32_t)(i * kPer) * 128u,
+                   on ? static_cast<const void *>(reinterpret_cast<const bf16 *>(p) + ch * 8) : any, on);
     }
 }
-
-// A tile's barrier is arrived at by every lane of the loading warps as soon as the lane's copies have landed, without anybody waiting
-// for them, and once more per warp for what it wrote itself (visibility words, statistics of rows).  The lane that issues the products
-// makes the landed bytes visible to the tensor cores (tile_ready).
-constexpr uint32_t kTileArrivals = kLoaders * 33;
-__device__ inline void announce(uint64_t *bar, int lane)
+// Arrivals at the barrier of a tile of rows: its box, or every lane of the copying warp once its copies have landed and the warp itself
+constexpr uint32_t kCopyArrivals = 33;
+__device__ inline void announce_copies(uint64_t *bar, int lane)
 {
     asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(bar)) : "memory");
     __syncwarp();
     if (lane == 0) mbar_arrive(bar);
 }
+
+// Zeros over the rows of a tile whose bit is off, by one warp, visible to the tensor cores
+template <int NB> __device__ inline void clear_rows(uint32_t tile, const uint32_t (&word)[4], int lane)
+{
+    const int ch = lane & (8 * NB - 1), row = lane / (8 * NB);
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        if (word[b] == 0xFFFFFFFFu) continue;
+        for (int i = 0; i < 8 * NB; ++i) {
+            const int r = i * (4 / NB) + row;
+            if (!((word[b] >> r) & 1u))
+                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(tile + (uint32_t)(ch >> 3) * kBlockBytes + (uint32_t)(b * 32 + r) * 128u +
+                                                                             (uint32_t)((ch & 7) << 4)),
+                             "r"(0)
+                             : "memory");
+        }
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+}
+__device__ inline bool all_seen(const uint32_t (&word)[4]) { return (word[0] & word[1] & word[2] & word[3]) == 0xFFFFFFFFu; }
+
+// Whether the 128 keys from j * 128 on are seen, one bit each; loads for the next tile go out a tile ahead (ahead, then now)
+struct Visible {
+    uint32_t next[4];
+    __device__ inline void ahead(const AttnArgs &a, const Work &x, int j, int lane)
+    {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int64_t key = x.kb + (int64_t)j * kTile + b * 32 + lane;
+            next[b] = key < x.ke ? (a.mask ? (uint32_t)a.mask[key] : 1u) : 0u;
+        }
+    }
+    __device__ inline void now(uint32_t (&word)[4]) const
+    {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) word[b] = __ballot_sync(0xFFFFFFFFu, next[b] != 0);
+    }
+};
+
+// the lane that issues the products: a tile has landed, whoever wrote it
 __device__ inline bool tile_ready(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
 {
     const bool ok = mbar_wait(bar, parity, abort_flag);
@@ -186,6 +209,12 @@ __device__ inline bool tile_ready(uint64_t *bar, uint32_t parity, volatile int *
 __device__ inline bool warp_wait(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
 {
     return __all_sync(0xFFFFFFFFu, mbar_wait(bar, parity, abort_flag));
+}
+// Giving up: the copies that were started into slots of a ring land before the shared memory is released
+__device__ inline void let_land(uint64_t *bars, uint32_t stages, uint32_t issued)
+{
+    int never = 0;
+    for (uint32_t j = issued > stages ? issued - stages : 0; j < issued; ++j) mbar_wait(&bars[j % stages], (j / stages) & 1u, &never);
 }
 
 // Products of one tile, K step by K step, with descriptors that move on by constants: the instruction stream of the one issuing lane
@@ -211,20 +240,21 @@ __device__ inline void row_steps(uint32_t d, uint32_t a, uint32_t second, uint64
 // the second would idle: two such blocks per SM overlap instead.
 template <int NB, int NT> struct Fwd {
     static constexpr int kStages = NT == 2 ? (NB == 2 ? 5 : 8) : (NB == 2 ? 2 : 5);
-    static constexpr int kSoft = NT * 4, kMma = kSoft + kLoaders, kThreads = (kSoft + 4) * 32, kBlocks = 3 - NT;
+    static constexpr int kSoft = NT * 4, kThreads = (kSoft + 4) * 32, kBlocks = 3 - NT;      // copies, zeros, products; one idle
     static constexpr int kRows = NT * kTile, kTileBytes = NB * kBlockBytes, kColumns = NT * 256;
     static constexpr size_t kSmem = 1024 + (size_t)(NT + kStages) * kTileBytes;
 };
 
 template <int NB, int NT>
 __global__ void __launch_bounds__(Fwd<NB, NT>::kThreads, Fwd<NB, NT>::kBlocks)
-attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
+attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                   const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
 {
     using F = Fwd<NB, NT>;
     constexpr int kStages = F::kStages, kTileBytes = F::kTileBytes, kRows = F::kRows, kSoft = F::kSoft;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], q_full, q_empty, s_full[NT], p_full[NT], o_full[NT], o_empty[NT];
-    __shared__ uint32_t words[kWordRing][4];
+    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], v_clean[kWordRing], q_full, q_empty, s_full[NT], p_full[NT], o_full[NT], o_empty[NT];
+    __shared__ __align__(16) uint32_t words[kWordRing][4];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
@@ -235,10 +265,11 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ T
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&kv_full[s], kTileArrivals);
+            mbar_init(&kv_full[s], 1);
             mbar_init(&kv_empty[s], 1);
         }
-        mbar_init(&q_full, kTileArrivals);
+        for (int s = 0; s < kWordRing; ++s) mbar_init(&v_clean[s], 1);
+        mbar_init(&q_full, f.boxes ? 1 : kCopyArrivals);
         mbar_init(&q_empty, 1);
         for (int t = 0; t < NT; ++t) {
             mbar_init(&s_full[t], 1);
@@ -250,7 +281,7 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ T
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == F::kMma) {
+    if (warp == kSoft + 2) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "n"(F::kColumns) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -261,56 +292,80 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ T
 
     if (warp >= kSoft) {
         fewer_registers<F::kBlocks>();
-        if (warp < F::kMma) {
+        if (warp == kSoft) {
             // ---- copies: queries of a block of rows, then keys and values in turn
-            const int w = warp - kSoft, chunks = 2 * ksteps, real = a.head_dim / 8;
-            uint32_t g = 0, jj = 0, item = 0;
+            uint32_t g = 0, jj = 0, item = 0, q_issued = 0;
             bool ok = true;
             for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
-                const Work x = work_of(a, f, u, w == 0 && lane == 0);
+                const Work x = work_of(a, f, u, lane == 0);
                 for (int64_t t = x.t0; t * kRows < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
+                    Visible seen;
+                    seen.ahead(a, x, 0, lane);
                     if (item > 0) ok = warp_wait(&q_empty, (item - 1) & 1u, &abort_flag);
                     if (!ok) break;
-                    for (int b = w; b < kRows / 32; b += kLoaders) {
-                        const int64_t r = t * kRows + b * 32 + lane;
-                        int64_t row;
-                        int head;
-                        row_of(a, x, r, row, head);
-                        copy_each<NB>(q_smem + (b >> 2) * kTileBytes, b & 3,
-                                      r < x.rows ? static_cast<const bf16 *>(a.q) + row * a.ldq + (int64_t)head * a.head_dim : nullptr, a.q, chunks, real, lane);
-                    }
-                    announce(&q_full, lane);
-                    for (int j = 0; j < x.n && ok; ++j, ++jj) {
-                        uint32_t word[4 / kLoaders];
-#pragma unroll
-                        for (int b = 0; b < 4 / kLoaders; ++b) {
-                            const int64_t key = x.kb + (int64_t)j * kTile + (w + b * kLoaders) * 32 + lane;
-                            word[b] = __ballot_sync(0xFFFFFFFFu, key < x.ke && (!a.mask || a.mask[key]));
+                    const int nt = NT == 2 && x.rows - t * kRows > kTile ? 2 : 1;
+                    if (f.boxes) {
+                        if (lane == 0) {
+                            mbar_expect_tx(&q_full, nt * kTileBytes);
+                            for (int q = 0; q < nt; ++q)
+                                load_tile<NB>(q_smem + q * kTileBytes, &map_q, x.h * a.group, x.rg.q0 + (t * kRows + q * kTile) / a.group, &q_full);
                         }
+                        ++q_issued;
+                    } else {
+                        for (int b = 0; b < nt * 4; ++b) {
+                            const int64_t r = t * kRows + b * 32 + lane;
+                            int64_t row;
+                            int head;
+                            row_of(a, x, r, row, head);
+                            copy_each<NB>(q_smem + (b >> 2) * kTileBytes, b & 3,
+                                          r < x.rows ? static_cast<const bf16 *>(a.q) + row * a.ldq + (int64_t)head * a.head_dim : nullptr, a.q, a.head_dim, lane);
+                        }
+                        announce_copies(&q_full, lane);
+                    }
+                    for (int j = 0; j < x.n && ok; ++j, ++jj) {
+                        uint32_t word[4];
+                        seen.now(word);
+                        if (j + 1 < x.n) seen.ahead(a, x, j + 1, lane);
                         for (int v = 0; v < 2; ++v, ++g) {
                             const uint32_t s = g % kStages;
                             if (g >= kStages) ok = warp_wait(&kv_empty[s], (g / kStages - 1) & 1u, &abort_flag);
                             if (!ok) break;
-#pragma unroll
-                            for (int b = 0; b < 4 / kLoaders; ++b) {
-                                const int part = w + b * kLoaders;
-                                const int64_t key = x.kb + (int64_t)j * kTile + part * 32, ld = v ? a.ldv : a.ldk;
-                                if (v == 0 && lane == 0) words[jj % kWordRing][part] = word[b];
-                                copy_rows<NB>(kv_smem + s * kTileBytes, part,
-                                              static_cast<const bf16 *>(v ? a.v : a.k) + key * ld + x.h * (int64_t)a.head_dim, ld, word[b], a.q, chunks,
-                                              real, lane);
+                            if (lane == 0) {
+                                if (v == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
+                                mbar_expect_tx(&kv_full[s], kTileBytes);
+                                load_tile<NB>(kv_smem + s * kTileBytes, v ? &map_v : &map_k, x.h, x.kb + (int64_t)j * kTile, &kv_full[s]);
                             }
-                            announce(&kv_full[s], lane);
                         }
                     }
                 }
             }
+            if (!ok && lane == 0) {
+                let_land(kv_full, kStages, g);
+                if (q_issued) let_land(&q_full, 1, q_issued);
+            }
             cp_async_wait_all();
-        } else if (warp == F::kMma) {
+        } else if (warp == kSoft + 1) {
+            // ---- zeros over hidden rows of the values
+            uint32_t g = 1, jj = 0;
+            bool ok = true;
+            for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
+                const Work x = work_of(a, f, u, false);
+                for (int64_t t = x.t0; t * kRows < x.rows && x.n > 0 && ok; t += f.tiles)
+                    for (int j = 0; j < x.n && ok; ++j, ++jj, g += 2) {
+                        ok = warp_wait(&kv_full[g % kStages], (g / kStages) & 1u, &abort_flag);
+                        if (!ok) break;
+                        const uint4 w4 = *reinterpret_cast<const uint4 *>(words[jj % kWordRing]);
+                        const uint32_t word[4] = {w4.x, w4.y, w4.z, w4.w};
+                        if (!all_seen(word)) clear_rows<NB>(kv_smem + (g % kStages) * kTileBytes, word, lane);
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&v_clean[jj % kWordRing]);
+                    }
+            }
+        } else if (warp == kSoft + 2) {
             // ---- products
             if (elect_one()) {
                 const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
-                uint32_t g = 0, item = 0, pc[NT] = {}, used[NT] = {};
+                uint32_t g = 0, jj = 0, item = 0, pc[NT] = {}, used[NT] = {};
                 bool ok = true;
                 auto scores = [&](uint32_t gk, int q) {
                     head_steps<NB>(tmem + q * kTile, make_smem_desc(q_smem + q * kTileBytes), make_smem_desc(kv_smem + (gk % kStages) * kTileBytes), id_s,
@@ -333,10 +388,11 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ T
                                 ++used[q];
                             }
                         if (ok) umma_commit(&kv_empty[g % kStages]);
-                        for (int j = 0; j < x.n && ok; ++j, g += 2) {
+                        for (int j = 0; j < x.n && ok; ++j, ++jj, g += 2) {
                             const uint32_t gv = g + 1, gk = g + 2;
                             const uint64_t v_desc = make_smem_desc_mn(kv_smem + (gv % kStages) * kTileBytes, kBlockBytes);
                             ok = tile_ready(&kv_full[gv % kStages], (gv / kStages) & 1u, &abort_flag);
+                            if (ok) ok = tile_ready(&v_clean[jj % kWordRing], (jj / kWordRing) & 1u, &abort_flag);
 #pragma unroll
                             for (int q = 0; q < NT; ++q) {
                                 if (q >= nt || !ok) continue;
@@ -499,16 +555,20 @@ attn_tc_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ T
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && abort_flag && a.status) atomicOr(reinterpret_cast<unsigned *>(a.status), E2EGREC_DEV_TIMEOUT);
-    if (warp == F::kMma) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(F::kColumns) : "memory");
+    if (warp == kSoft + 2) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(F::kColumns) : "memory");
 }
 
 // ------------------------------------------------------------------------------------------------- backward
 // Two kernels, so that no gradient is added up by atomics: dQ goes over the keys of a tile of rows, dK and dV over the rows of a
 // tile of keys; the scores are formed in both.  Two warpgroups share a tile of 128 x 128: 64 columns each, one row per thread.
-template <int NB> constexpr size_t dq_smem() { return 1024 + (size_t)(2 + (NB == 2 ? 5 : 8)) * NB * kBlockBytes; }
-template <int NB> constexpr size_t dkv_smem() { return 1024 + (size_t)(2 + 4) * NB * kBlockBytes; }
+template <int NB> struct Bwd {
+    static constexpr int kThreads = 12 * 32, kTileBytes = NB * kBlockBytes;      // copies, zeros, products; one idle
+    static constexpr int kKvStages = NB == 2 ? 5 : 8, kQgStages = NB == 2 ? 4 : 8;
+    static constexpr size_t kDqSmem = 1024 + (size_t)(2 + kKvStages) * kTileBytes, kDkvSmem = 1024 + (size_t)(2 + kQgStages) * kTileBytes;
+};
 
-// 64 columns of p or dS of a thread's row as an operand in tensor memory: 32 packed columns
+// 64 columns of p or dS of a thread's row as an operand in tensor memory: 32 packed columns (the second warpgroup's lie 64 behind the
+// first's: each half stays within the columns that its warpgroup has read)
 __device__ inline void store_operand(uint32_t taddr, const float (&v)[64])
 {
     uint32_t r[32];
@@ -516,7 +576,6 @@ __device__ inline void store_operand(uint32_t taddr, const float (&v)[64])
     for (int i = 0; i < 32; ++i) r[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
     tmem_store32(taddr, r);
 }
-// (the second warpgroup's 32 packed columns lie 64 behind the first's: each half stays within the columns that its warpgroup has read)
 
 // One row (up to 64 NB columns) of an accumulator -> out, times f; zeros where !keep
 template <int NB>
@@ -543,36 +602,28 @@ __device__ inline void store_row(uint32_t taddr, bf16 *out, int head_dim, float 
 
 // dQ, and D = dO . out of every row for the other kernel
 template <int NB>
-__global__ void __launch_bounds__(kThreads, 1)
-attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restrict__ dots)
+__global__ void __launch_bounds__(Bwd<NB>::kThreads, 1)
+attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_k,
+                  const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f, float *__restrict__ dots)
 {
-    constexpr int kStages = NB == 2 ? 5 : 8, kTileBytes = NB * kBlockBytes;
+    constexpr int kStages = Bwd<NB>::kKvStages, kTileBytes = Bwd<NB>::kTileBytes;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], q_full, q_empty, s_full[2], dp_full, ds_full, o_full, o_empty;
-    __shared__ uint32_t words[kWordRing][4];
+    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], k_clean[kWordRing], q_full, q_empty, s_full[2], dp_full, ds_full, o_full, o_empty;
+    __shared__ __align__(16) uint32_t words[kWordRing][4];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int64_t u = blockIdx.x;
-    const int t0 = (int)(u % tiles);
-    u /= tiles;
-    const int h = (int)(u % a.kv_heads);
-    const SeqRange rg = seq_range(a, u / a.kv_heads, t0 == 0 && h == 0 && threadIdx.x == 0);
-    const int64_t rows = (rg.q1 - rg.q0) * a.group;
-    if ((int64_t)t0 * kTile >= rows) return;
-    const int n = (int)ceil_div(rg.k1 - rg.k0, kTile);
-
     uint8_t *tiles_smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t q_smem = smem_u32(tiles_smem), g_smem = q_smem + kTileBytes, kv_smem = q_smem + 2 * kTileBytes;
     const int ksteps = (a.head_dim + 15) / 16;
-
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&kv_full[s], kTileArrivals);
+            mbar_init(&kv_full[s], 1);
             mbar_init(&kv_empty[s], 1);
         }
-        mbar_init(&q_full, kTileArrivals);
+        for (int s = 0; s < kWordRing; ++s) mbar_init(&k_clean[s], 1);
+        mbar_init(&q_full, f.boxes ? 1 : kCopyArrivals);
         mbar_init(&q_empty, 1);
         mbar_init(&s_full[0], 1);
         mbar_init(&s_full[1], 1);
@@ -584,7 +635,7 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == kMmaWarp) {
+    if (warp == 10) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -594,95 +645,128 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
     const uint32_t tmem = tmem_slot;                  // scores: columns 0 and 128 in turn; dP and dS: 256; dQ: 384
 
     if (warp >= 8) {
-    fewer_registers<1>();
-    if (warp < kMmaWarp) {
-        // ---- copies: Q and dO of a tile of rows, then keys and values in turn
-        const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8;
-        uint32_t g = 0, jj = 0, item = 0;
-        bool ok = true;
-        for (int64_t t = t0; t * kTile < rows && n > 0 && ok; t += tiles, ++item) {
-            if (item > 0) ok = warp_wait(&q_empty, (item - 1) & 1u, &abort_flag);
-            if (!ok) break;
-            for (int b = w; b < 4; b += kLoaders) {
-                const int64_t r = t * kTile + b * 32 + lane, i = r / a.group;
-                const int64_t col = (h * a.group + (int)(r - i * a.group)) * (int64_t)a.head_dim;
-                copy_each<NB>(q_smem, b, r < rows ? static_cast<const bf16 *>(a.q) + (rg.q0 + i) * a.ldq + col : nullptr, a.q, chunks, real, lane);
-                copy_each<NB>(g_smem, b, r < rows ? static_cast<const bf16 *>(a.dout) + (rg.q0 + i) * a.ldg + col : nullptr, a.q, chunks, real, lane);
-            }
-            announce(&q_full, lane);
-            for (int j = 0; j < n && ok; ++j, ++jj) {
-                uint32_t word[4 / kLoaders];
-#pragma unroll
-                for (int b = 0; b < 4 / kLoaders; ++b) {
-                    const int64_t key = rg.k0 + (int64_t)j * kTile + (w + b * kLoaders) * 32 + lane;
-                    word[b] = __ballot_sync(0xFFFFFFFFu, key < rg.k1 && (!a.mask || a.mask[key]));
-                }
-                for (int v = 0; v < 2; ++v, ++g) {
-                    const uint32_t s = g % kStages;
-                    if (g >= kStages) ok = warp_wait(&kv_empty[s], (g / kStages - 1) & 1u, &abort_flag);
-                    if (!ok) break;
-#pragma unroll
-                    for (int b = 0; b < 4 / kLoaders; ++b) {
-                        const int part = w + b * kLoaders;
-                        const int64_t key = rg.k0 + (int64_t)j * kTile + part * 32, ld = v ? a.ldv : a.ldk;
-                        if (v == 0 && lane == 0) words[jj % kWordRing][part] = word[b];
-                        copy_rows<NB>(kv_smem + s * kTileBytes, part, static_cast<const bf16 *>(v ? a.v : a.k) + key * ld + h * (int64_t)a.head_dim, ld,
-                                      word[b], a.q, chunks, real, lane);
-                    }
-                    announce(&kv_full[s], lane);
-                }
-            }
-        }
-        cp_async_wait_all();
-    } else if (warp == kMmaWarp) {
-        // ---- products.  S of the next tile goes out before dQ waits for dS, dP of the next tile behind dQ (whose operand it
-        // overwrites): the warpgroups form p of the next tile beside dQ and dP.
-        if (elect_one()) {
-            const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
-            uint32_t g = 0, item = 0, jj = 0;
+        fewer_registers<1>();
+        if (warp == 8) {
+            // ---- copies: Q and dO of a tile of rows, then keys and values in turn
+            uint32_t g = 0, jj = 0, item = 0, q_issued = 0;
             bool ok = true;
-            auto product = [&](uint32_t d, uint64_t a_desc, uint32_t slot) {
-                head_steps<NB>(d, a_desc, make_smem_desc(kv_smem + (slot % kStages) * kTileBytes), id_s, ksteps);
-            };
-            const uint64_t q_desc = make_smem_desc(q_smem), g_desc = make_smem_desc(g_smem);
-            auto full = [&](uint32_t slot) {
-                ok = ok && tile_ready(&kv_full[slot % kStages], (slot / kStages) & 1u, &abort_flag);
-                return ok;
-            };
-            for (int64_t t = t0; t * kTile < rows && n > 0 && ok; t += tiles, ++item) {
-                ok = tile_ready(&q_full, item & 1u, &abort_flag);
-                if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
-                if (!full(g)) break;
-                product(tmem + (jj & 1u) * kTile, q_desc, g);
-                umma_commit(&s_full[jj & 1u]);
-                if (!full(g + 1)) break;
-                product(tmem + 256, g_desc, g + 1);
-                umma_commit(&dp_full);
-                umma_commit(&kv_empty[(g + 1) % kStages]);
-                for (int j = 0; j < n; ++j, g += 2, ++jj) {
-                    if (j + 1 < n) {
-                        if (!full(g + 2)) break;
-                        product(tmem + ((jj + 1) & 1u) * kTile, q_desc, g + 2);
-                        umma_commit(&s_full[(jj + 1) & 1u]);
-                    }
-                    ok = mbar_wait(&ds_full, jj & 1u, &abort_flag);
+            for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
+                const Work x = work_of(a, f, u, lane == 0);
+                for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
+                    Visible seen;
+                    seen.ahead(a, x, 0, lane);
+                    if (item > 0) ok = warp_wait(&q_empty, (item - 1) & 1u, &abort_flag);
                     if (!ok) break;
-                    tc_fence_after();
-                    row_steps(tmem + 384, tmem + 256, 32, make_smem_desc_mn(kv_smem + (g % kStages) * kTileBytes, kBlockBytes), id_o, j > 0);
-                    umma_commit(&kv_empty[g % kStages]);
-                    if (j + 1 < n) {
-                        if (!full(g + 3)) break;
-                        product(tmem + 256, g_desc, g + 3);
-                        umma_commit(&dp_full);
-                        umma_commit(&kv_empty[(g + 3) % kStages]);
+                    if (f.boxes) {
+                        if (lane == 0) {
+                            mbar_expect_tx(&q_full, 2 * kTileBytes);
+                            load_tile<NB>(q_smem, &map_q, x.h * a.group, x.rg.q0 + t * kTile / a.group, &q_full);
+                            load_tile<NB>(g_smem, &map_g, x.h * a.group, x.rg.q0 + t * kTile / a.group, &q_full);
+                        }
+                        ++q_issued;
                     } else {
-                        umma_commit(&o_full);
-                        umma_commit(&q_empty);
+                        for (int b = 0; b < 4; ++b) {
+                            const int64_t r = t * kTile + b * 32 + lane;
+                            int64_t row;
+                            int head;
+                            row_of(a, x, r, row, head);
+                            const int64_t col = (int64_t)head * a.head_dim;
+                            copy_each<NB>(q_smem, b, r < x.rows ? static_cast<const bf16 *>(a.q) + row * a.ldq + col : nullptr, a.q, a.head_dim, lane);
+                            copy_each<NB>(g_smem, b, r < x.rows ? static_cast<const bf16 *>(a.dout) + row * a.ldg + col : nullptr, a.q, a.head_dim, lane);
+                        }
+                        announce_copies(&q_full, lane);
+                    }
+                    for (int j = 0; j < x.n && ok; ++j, ++jj) {
+                        uint32_t word[4];
+                        seen.now(word);
+                        if (j + 1 < x.n) seen.ahead(a, x, j + 1, lane);
+                        for (int v = 0; v < 2; ++v, ++g) {
+                            const uint32_t s = g % kStages;
+                            if (g >= kStages) ok = warp_wait(&kv_empty[s], (g / kStages - 1) & 1u, &abort_flag);
+                            if (!ok) break;
+                            if (lane == 0) {
+                                if (v == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
+                                mbar_expect_tx(&kv_full[s], kTileBytes);
+                                load_tile<NB>(kv_smem + s * kTileBytes, v ? &map_v : &map_k, x.h, x.kb + (int64_t)j * kTile, &kv_full[s]);
+                            }
+                        }
+                    }
+                }
+            }
+            if (!ok && lane == 0) {
+                let_land(kv_full, kStages, g);
+                if (q_issued) let_land(&q_full, 1, q_issued);
+            }
+            cp_async_wait_all();
+        } else if (warp == 9) {
+            // ---- zeros over hidden rows of the keys (the products with K as columns leave what they hold to the mask)
+            uint32_t g = 0, jj = 0;
+            bool ok = true;
+            for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
+                const Work x = work_of(a, f, u, false);
+                for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles)
+                    for (int j = 0; j < x.n && ok; ++j, ++jj, g += 2) {
+                        ok = warp_wait(&kv_full[g % kStages], (g / kStages) & 1u, &abort_flag);
+                        if (!ok) break;
+                        const uint4 w4 = *reinterpret_cast<const uint4 *>(words[jj % kWordRing]);
+                        const uint32_t word[4] = {w4.x, w4.y, w4.z, w4.w};
+                        if (!all_seen(word)) clear_rows<NB>(kv_smem + (g % kStages) * kTileBytes, word, lane);
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&k_clean[jj % kWordRing]);
+                    }
+            }
+        } else if (warp == 10) {
+            // ---- products.  S of the next tile goes out before dQ waits for dS, dP of the next tile behind dQ (whose operand it
+            // overwrites): the warpgroups form p of the next tile beside dQ and dP.
+            if (elect_one()) {
+                const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
+                const uint64_t q_desc = make_smem_desc(q_smem), g_desc = make_smem_desc(g_smem);
+                uint32_t g = 0, item = 0, jj = 0;
+                bool ok = true;
+                auto product = [&](uint32_t d, uint64_t a_desc, uint32_t slot) {
+                    head_steps<NB>(d, a_desc, make_smem_desc(kv_smem + (slot % kStages) * kTileBytes), id_s, ksteps);
+                };
+                auto full = [&](uint32_t slot) {
+                    ok = ok && tile_ready(&kv_full[slot % kStages], (slot / kStages) & 1u, &abort_flag);
+                    return ok;
+                };
+                for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
+                    const Work x = work_of(a, f, u, false);
+                    for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
+                        ok = tile_ready(&q_full, item & 1u, &abort_flag);
+                        if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
+                        if (!full(g)) break;
+                        product(tmem + (jj & 1u) * kTile, q_desc, g);
+                        umma_commit(&s_full[jj & 1u]);
+                        if (!full(g + 1)) break;
+                        product(tmem + 256, g_desc, g + 1);
+                        umma_commit(&dp_full);
+                        umma_commit(&kv_empty[(g + 1) % kStages]);
+                        for (int j = 0; j < x.n; ++j, g += 2, ++jj) {
+                            if (j + 1 < x.n) {
+                                if (!full(g + 2)) break;
+                                product(tmem + ((jj + 1) & 1u) * kTile, q_desc, g + 2);
+                                umma_commit(&s_full[(jj + 1) & 1u]);
+                            }
+                            ok = tile_ready(&k_clean[jj % kWordRing], (jj / kWordRing) & 1u, &abort_flag) && mbar_wait(&ds_full, jj & 1u, &abort_flag);
+                            if (!ok) break;
+                            tc_fence_after();
+                            row_steps(tmem + 384, tmem + 256, 32, make_smem_desc_mn(kv_smem + (g % kStages) * kTileBytes, kBlockBytes), id_o, j > 0);
+                            umma_commit(&kv_empty[g % kStages]);
+                            if (j + 1 < x.n) {
+                                if (!full(g + 3)) break;
+                                product(tmem + 256, g_desc, g + 3);
+                                umma_commit(&dp_full);
+                                umma_commit(&kv_empty[(g + 3) % kStages]);
+                            } else {
+                                umma_commit(&o_full);
+                                umma_commit(&q_empty);
+                            }
+                        }
                     }
                 }
             }
         }
-    }
     } else {
         more_registers<1>();
         // ---- p and dS: 64 columns of one row per thread
@@ -692,115 +776,116 @@ attn_tc_dq_kernel(const __grid_constant__ AttnArgs a, int tiles, float *__restri
         const int heads = a.kv_heads * a.group;
         uint32_t jj = 0, item = 0;
         bool ok = true;
-        for (int64_t t = t0; t * kTile < rows && ok; t += tiles, ++item) {
-            const int64_t r = t * kTile + w * 32 + lane, i = r / a.group;
-            const int head = h * a.group + (int)(r - i * a.group);
-            const int64_t row = rg.q0 + i, col = (int64_t)head * a.head_dim;
-            const bool live = r < rows;
-            float base = INFINITY, dot = 0.f;          // rows that saw no key: p = 0
-            if (live) {
-                const float l = a.lse[row * heads + head];
-                if (l != -INFINITY) base = l * kLog2e;
-                const bf16 *o = static_cast<const bf16 *>(a.o) + row * a.ldo + col, *gr = static_cast<const bf16 *>(a.dout) + row * a.ldg + col;
-                for (int e = 0; e < a.head_dim; e += 8) {
-                    float x[8], y[8];
-                    Chunk<bf16>::load(o + e, x);
-                    Chunk<bf16>::load(gr + e, y);
+        for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
+            const Work x = work_of(a, f, u, false);
+            for (int64_t t = x.t0; t * kTile < x.rows && ok; t += f.tiles) {
+                const int64_t r = t * kTile + w * 32 + lane;
+                int64_t row;
+                int head;
+                row_of(a, x, r, row, head);
+                const int64_t col = (int64_t)head * a.head_dim;
+                const bool live = r < x.rows;
+                float base = INFINITY, dot = 0.f;          // rows that saw no key: p = 0
+                if (live) {
+                    const float l = a.lse[row * heads + head];
+                    if (l != -INFINITY) base = l * kLog2e;
+                    const bf16 *o = static_cast<const bf16 *>(a.o) + row * a.ldo + col, *gr = static_cast<const bf16 *>(a.dout) + row * a.ldg + col;
+#pragma unroll 4
+                    for (int e = 0; e < a.head_dim; e += 8) {
+                        float xo[8], xg[8];
+                        Chunk<bf16>::load(o + e, xo);
+                        Chunk<bf16>::load(gr + e, xg);
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) dot += x[k] * y[k];
-                }
-                if (l == -INFINITY) dot = 0.f;
-                if (q == 0) dots[row * heads + head] = dot;
-            }
-            for (int j = 0; j < n; ++j, ++jj) {
-                ok = mbar_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                tc_fence_after();
-                float p[64];
-                uint32_t v0[2][32];
-                tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64, v0[0]);
-                tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64 + 32, v0[1]);
-                tmem_load_wait();
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const uint32_t word = words[jj % kWordRing][q * 2 + c];
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) p[c * 32 + e] = exp2_approx(fmaf(__uint_as_float(v0[c][e]), c1, -base));
-                    if (word != 0xFFFFFFFFu) {
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (!((word >> e) & 1u)) p[c * 32 + e] = 0.f;
+                        for (int k = 0; k < 8; ++k) dot += xo[k] * xg[k];
                     }
+                    if (l == -INFINITY) dot = 0.f;
+                    if (q == 0) dots[row * heads + head] = dot;
                 }
-                ok = mbar_wait(&dp_full, jj & 1u, &abort_flag);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                tc_fence_after();
-                uint32_t v1[2][32];
-                tmem_load32_async(tmem + lanes + 256 + q * 64, v1[0]);
-                tmem_load32_async(tmem + lanes + 256 + q * 64 + 32, v1[1]);
-                tmem_load_wait();
+                for (int j = 0; j < x.n; ++j, ++jj) {
+                    ok = warp_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    float p[64];
+                    {
+                        uint32_t v[2][32];
+                        tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64, v[0]);
+                        tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64 + 32, v[1]);
+                        tmem_load_wait();
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
+                        for (int e = 0; e < 64; ++e) p[e] = exp2_approx(fmaf(__uint_as_float(v[e >> 5][e & 31]), c1, -base));
+                    }
+                    ok = warp_wait(&dp_full, jj & 1u, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    {
+                        uint32_t v[2][32];
+                        tmem_load32_async(tmem + lanes + 256 + q * 64, v[0]);
+                        tmem_load32_async(tmem + lanes + 256 + q * 64 + 32, v[1]);
+                        tmem_load_wait();
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) p[c * 32 + e] *= __uint_as_float(v1[c][e]) - dot;
+                        for (int e = 0; e < 64; ++e) p[e] *= __uint_as_float(v[e >> 5][e & 31]) - dot;
+                    }
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const uint32_t word = words[jj % kWordRing][q * 2 + c];
+                        if (word != 0xFFFFFFFFu) {
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                if (!((word >> e) & 1u)) p[c * 32 + e] = 0.f;
+                        }
+                    }
+                    store_operand(tmem + lanes + 256 + q * 64, p);
+                    tmem_store_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&ds_full);
                 }
-                store_operand(tmem + lanes + 256 + q * 64, p);
-                tmem_store_wait();
+                if (!ok) break;
+                if (x.n > 0) {
+                    ok = warp_wait(&o_full, item++ & 1u, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                if (q == 0) store_row<NB>(tmem + lanes + 384, static_cast<bf16 *>(a.dq) + row * a.ldq2 + col, a.head_dim, a.scale, x.n > 0, base != INFINITY, live);
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&ds_full);
+                if (lane == 0 && x.n > 0) mbar_arrive(&o_empty);
             }
-            if (!ok) break;
-            if (n > 0) {
-                ok = mbar_wait(&o_full, item & 1u, &abort_flag);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                tc_fence_after();
-            }
-            if (q == 0) store_row<NB>(tmem + lanes + 384, static_cast<bf16 *>(a.dq) + row * a.ldq2 + col, a.head_dim, a.scale, n > 0, base != INFINITY, live);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0 && n > 0) mbar_arrive(&o_empty);
         }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && abort_flag && a.status) atomicOr(reinterpret_cast<unsigned *>(a.status), E2EGREC_DEV_TIMEOUT);
-    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == 10) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
 // dK and dV of a tile of keys: S^T = K Q^T and dP^T = V dO^T over the rows of the sequence
 template <int NB>
-__global__ void __launch_bounds__(kThreads, 1)
-attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *__restrict__ dots)
+__global__ void __launch_bounds__(Bwd<NB>::kThreads, 1)
+attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_k,
+                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f,
+                   const float *__restrict__ dots)
 {
-    constexpr int kStages = 4, kTileBytes = NB * kBlockBytes, kStatRing = 4;
+    constexpr int kStages = Bwd<NB>::kQgStages, kTileBytes = Bwd<NB>::kTileBytes;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t qg_full[kStages], qg_empty[kStages], kv_full, kv_empty, s_full, p_full, dp_full, ds_full, o_full, o_empty;
-    __shared__ __align__(16) float stat_lse[kStatRing][kTile], stat_dot[kStatRing][kTile];
+    __shared__ uint64_t qg_full[kStages], qg_clean[kStages], qg_empty[kStages], kv_full, kv_empty, s_full, p_full, dp_full, ds_full, o_full, o_empty;
+    __shared__ __align__(16) float stat_lse[kWordRing][kTile], stat_dot[kWordRing][kTile];
+    __shared__ __align__(16) uint32_t words[kWordRing][4];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    int64_t u = blockIdx.x;
-    const int t0 = (int)(u % tiles);
-    u /= tiles;
-    const int h = (int)(u % a.kv_heads);
-    const SeqRange rg = seq_range(a, u / a.kv_heads, t0 == 0 && h == 0 && threadIdx.x == 0);
-    const int64_t rows = (rg.q1 - rg.q0) * a.group, keys = rg.k1 - rg.k0;
-    if ((int64_t)t0 * kTile >= keys) return;
-    const int n = (int)ceil_div(rows, kTile);
-
     uint8_t *tiles_smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t k_smem = smem_u32(tiles_smem), v_smem = k_smem + kTileBytes, qg_smem = k_smem + 2 * kTileBytes;
     const int ksteps = (a.head_dim + 15) / 16;
-
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
-            mbar_init(&qg_full[s], kTileArrivals);
+            mbar_init(&qg_full[s], f.boxes ? 1 : kCopyArrivals);
+            mbar_init(&qg_clean[s], 1);
             mbar_init(&qg_empty[s], 1);
         }
-        mbar_init(&kv_full, kTileArrivals);
+        mbar_init(&kv_full, 1);
         mbar_init(&kv_empty, 1);
         mbar_init(&s_full, 1);
         mbar_init(&p_full, 8);
@@ -812,7 +897,7 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    if (warp == kMmaWarp) {
+    if (warp == 10) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(&tmem_slot)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -822,115 +907,169 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
     const uint32_t tmem = tmem_slot;                  // S^T and P^T: columns 0; dP^T and dS^T: 128; dV: 256; dK: 384
 
     if (warp >= 8) {
-    fewer_registers<1>();
-    if (warp < kMmaWarp) {
-        // ---- copies: keys and values of a tile, then Q and dO of the rows in turn, with the rows' lse and D
-        const int w = warp - 8, chunks = 2 * ksteps, real = a.head_dim / 8, heads = a.kv_heads * a.group;
-        uint32_t g = 0, jj = 0, item = 0;
-        bool ok = true;
-        for (int64_t t = t0; t * kTile < keys && n > 0 && ok; t += tiles, ++item) {
-            if (item > 0) ok = warp_wait(&kv_empty, (item - 1) & 1u, &abort_flag);
-            if (!ok) break;
-            for (int b = w; b < 4; b += kLoaders) {
-                const int64_t key = rg.k0 + t * kTile + b * 32 + lane;
-                const bool seen = key < rg.k1 && (!a.mask || a.mask[key]);
-                copy_each<NB>(k_smem, b, seen ? static_cast<const bf16 *>(a.k) + key * a.ldk + h * (int64_t)a.head_dim : nullptr, a.q, chunks, real, lane);
-                copy_each<NB>(v_smem, b, seen ? static_cast<const bf16 *>(a.v) + key * a.ldv + h * (int64_t)a.head_dim : nullptr, a.q, chunks, real, lane);
-            }
-            announce(&kv_full, lane);
-            for (int j = 0; j < n && ok; ++j, ++jj) {
-                int64_t row[4 / kLoaders], col[4 / kLoaders];
-                float l[4 / kLoaders], d[4 / kLoaders];
-#pragma unroll
-                for (int b = 0; b < 4 / kLoaders; ++b) {
-                    const int64_t r = (int64_t)j * kTile + (w + b * kLoaders) * 32 + lane, i = r / a.group;
-                    const int head = h * a.group + (int)(r - i * a.group);
-                    row[b] = rg.q0 + i;
-                    col[b] = (int64_t)head * a.head_dim;
-                    l[b] = INFINITY;
-                    d[b] = 0.f;
-                    if (r < rows) {
-                        const float x = a.lse[row[b] * heads + head];
-                        if (x != -INFINITY) {
-                            l[b] = x * kLog2e;
-                            d[b] = dots[row[b] * heads + head];
-                        }
-                    }
-                }
-                for (int v = 0; v < 2; ++v, ++g) {
-                    const uint32_t s = g % kStages;
-                    if (g >= kStages) ok = warp_wait(&qg_empty[s], (g / kStages - 1) & 1u, &abort_flag);
-                    if (!ok) break;
-#pragma unroll
-                    for (int b = 0; b < 4 / kLoaders; ++b) {
-                        const int part = w + b * kLoaders;
-                        if (v == 0) {
-                            stat_lse[jj % kStatRing][part * 32 + lane] = l[b];
-                            stat_dot[jj % kStatRing][part * 32 + lane] = d[b];
-                        }
-                        const bf16 *src = v ? static_cast<const bf16 *>(a.dout) + row[b] * a.ldg + col[b] : static_cast<const bf16 *>(a.q) + row[b] * a.ldq + col[b];
-                        copy_each<NB>(qg_smem + s * kTileBytes, part, l[b] != INFINITY ? src : nullptr, a.q, chunks, real, lane);
-                    }
-                    announce(&qg_full[s], lane);
-                }
-            }
-        }
-        cp_async_wait_all();
-    } else if (warp == kMmaWarp) {
-        // ---- products.  S^T of the next tile follows dV, whose operand it overwrites, dP^T follows dK: the warpgroups form dS
-        // beside dV and the next S^T, and the next p beside dK and the next dP^T.
-        if (elect_one()) {
-            const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
-            uint32_t g = 0, item = 0, jj = 0;
+        fewer_registers<1>();
+        if (warp == 8) {
+            // ---- copies: keys and values of a tile, then Q and dO of the rows in turn, with the rows' lse and D (fetched a tile ahead)
+            const int heads = a.kv_heads * a.group;
+            uint32_t g = 0, jj = 0, item = 0;
             bool ok = true;
-            auto product = [&](uint32_t d, uint64_t a_desc, uint32_t slot) {
-                head_steps<NB>(d, a_desc, make_smem_desc(qg_smem + (slot % kStages) * kTileBytes), id_s, ksteps);
-            };
-            auto gradient = [&](uint32_t d, uint32_t operand, uint32_t slot, bool add) {
-                row_steps(d, operand, 32, make_smem_desc_mn(qg_smem + (slot % kStages) * kTileBytes, kBlockBytes), id_o, add);
-            };
-            const uint64_t k_desc = make_smem_desc(k_smem), v_desc = make_smem_desc(v_smem);
-            auto full = [&](uint32_t slot) {
-                ok = ok && tile_ready(&qg_full[slot % kStages], (slot / kStages) & 1u, &abort_flag);
-                return ok;
-            };
-            for (int64_t t = t0; t * kTile < keys && n > 0 && ok; t += tiles, ++item) {
-                ok = tile_ready(&kv_full, item & 1u, &abort_flag);
-                if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
-                if (!full(g)) break;
-                product(tmem, k_desc, g);
-                umma_commit(&s_full);
-                if (!full(g + 1)) break;
-                product(tmem + 128, v_desc, g + 1);
-                umma_commit(&dp_full);
-                for (int j = 0; j < n; ++j, g += 2, ++jj) {
-                    ok = mbar_wait(&p_full, jj & 1u, &abort_flag);
-                    if (!ok) break;
-                    tc_fence_after();
-                    gradient(tmem + 256, tmem, g + 1, j > 0);
-                    umma_commit(&qg_empty[(g + 1) % kStages]);
-                    if (j + 1 < n) {
-                        if (!full(g + 2)) break;
-                        product(tmem, k_desc, g + 2);
-                        umma_commit(&s_full);
+            for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
+                const Work x = work_of(a, f, u, lane == 0);
+                const int64_t keys = x.ke - x.kb;
+                const int n = (int)((x.rows + kTile - 1) / kTile);
+                float lse[4], dot[4];
+                auto ahead = [&](int j) {
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) {
+                        const int64_t r = (int64_t)j * kTile + b * 32 + lane;
+                        int64_t row;
+                        int head;
+                        row_of(a, x, r, row, head);
+                        lse[b] = r < x.rows ? a.lse[row * heads + head] : -INFINITY;
+                        dot[b] = r < x.rows ? dots[row * heads + head] : 0.f;
                     }
-                    ok = mbar_wait(&ds_full, jj & 1u, &abort_flag);
+                };
+                for (int64_t t = x.t0; t * kTile < keys && n > 0 && ok; t += f.tiles, ++item) {
+                    ahead(0);
+                    if (item > 0) ok = warp_wait(&kv_empty, (item - 1) & 1u, &abort_flag);
                     if (!ok) break;
-                    tc_fence_after();
-                    gradient(tmem + 384, tmem + 128, g, j > 0);
-                    umma_commit(&qg_empty[g % kStages]);
-                    if (j + 1 < n) {
-                        if (!full(g + 3)) break;
-                        product(tmem + 128, v_desc, g + 3);
+                    if (lane == 0) {
+                        mbar_expect_tx(&kv_full, 2 * kTileBytes);
+                        load_tile<NB>(k_smem, &map_k, x.h, x.kb + t * kTile, &kv_full);
+                        load_tile<NB>(v_smem, &map_v, x.h, x.kb + t * kTile, &kv_full);
+                    }
+                    for (int j = 0; j < n && ok; ++j, ++jj) {
+                        float l[4], d[4];
+                        uint32_t word[4];
+#pragma unroll
+                        for (int b = 0; b < 4; ++b) {
+                            const bool on = lse[b] != -INFINITY;
+                            l[b] = on ? lse[b] * kLog2e : INFINITY;
+                            d[b] = on ? dot[b] : 0.f;
+                            word[b] = __ballot_sync(0xFFFFFFFFu, on);
+                        }
+                        if (j + 1 < n) ahead(j + 1);
+                        for (int v = 0; v < 2; ++v, ++g) {
+                            const uint32_t s = g % kStages;
+                            if (g >= kStages) ok = warp_wait(&qg_empty[s], (g / kStages - 1) & 1u, &abort_flag);
+                            if (!ok) break;
+                            if (v == 0) {
+#pragma unroll
+                                for (int b = 0; b < 4; ++b) {
+                                    stat_lse[jj % kWordRing][b * 32 + lane] = l[b];
+                                    stat_dot[jj % kWordRing][b * 32 + lane] = d[b];
+                                }
+                                if (lane == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
+                                __syncwarp();
+                            }
+                            if (f.boxes) {
+                                if (lane == 0) {
+                                    mbar_expect_tx(&qg_full[s], kTileBytes);
+                                    load_tile<NB>(qg_smem + s * kTileBytes, v ? &map_g : &map_q, x.h * a.group, x.rg.q0 + (int64_t)j * kTile / a.group,
+                                                  &qg_full[s]);
+                                }
+                            } else {
+                                for (int b = 0; b < 4; ++b) {
+                                    const int64_t r = (int64_t)j * kTile + b * 32 + lane;
+                                    int64_t row;
+                                    int head;
+                                    row_of(a, x, r, row, head);
+                                    const int64_t col = (int64_t)head * a.head_dim;
+                                    const bf16 *src = v ? static_cast<const bf16 *>(a.dout) + row * a.ldg + col : static_cast<const bf16 *>(a.q) + row * a.ldq + col;
+                                    copy_each<NB>(qg_smem + s * kTileBytes, b, (word[b] >> lane) & 1u ? src : nullptr, a.q, a.head_dim, lane);
+                                }
+                                announce_copies(&qg_full[s], lane);
+                            }
+                        }
+                    }
+                }
+            }
+            if (!ok && lane == 0) {
+                if (f.boxes) let_land(qg_full, kStages, g);
+                if (item) let_land(&kv_full, 1, item);
+            }
+            cp_async_wait_all();
+        } else if (warp == 9) {
+            // ---- zeros over rows behind the sequence's end and rows that saw no key
+            uint32_t g = 0, jj = 0;
+            bool ok = true;
+            for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
+                const Work x = work_of(a, f, u, false);
+                const int64_t keys = x.ke - x.kb;
+                const int n = (int)((x.rows + kTile - 1) / kTile);
+                for (int64_t t = x.t0; t * kTile < keys && n > 0 && ok; t += f.tiles)
+                    for (int j = 0; j < n && ok; ++j, ++jj)
+                        for (int v = 0; v < 2 && ok; ++v, ++g) {
+                            ok = warp_wait(&qg_full[g % kStages], (g / kStages) & 1u, &abort_flag);
+                            if (!ok) break;
+                            const uint4 w4 = *reinterpret_cast<const uint4 *>(words[jj % kWordRing]);
+                            const uint32_t word[4] = {w4.x, w4.y, w4.z, w4.w};
+                            if (!all_seen(word)) clear_rows<NB>(qg_smem + (g % kStages) * kTileBytes, word, lane);
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&qg_clean[g % kStages]);
+                        }
+            }
+        } else if (warp == 10) {
+            // ---- products.  S^T of the next tile follows dV, whose operand it overwrites, dP^T follows dK: the warpgroups form dS
+            // beside dV and the next S^T, and the next p beside dK and the next dP^T.
+            if (elect_one()) {
+                const uint32_t id_s = make_idesc(kTile, kTile), id_o = make_idesc(kTile, ksteps * 16, false, true);
+                const uint64_t k_desc = make_smem_desc(k_smem), v_desc = make_smem_desc(v_smem);
+                uint32_t g = 0, item = 0, jj = 0;
+                bool ok = true;
+                auto product = [&](uint32_t d, uint64_t a_desc, uint32_t slot) {
+                    head_steps<NB>(d, a_desc, make_smem_desc(qg_smem + (slot % kStages) * kTileBytes), id_s, ksteps);
+                };
+                auto gradient = [&](uint32_t d, uint32_t operand, uint32_t slot, bool add) {
+                    row_steps(d, operand, 32, make_smem_desc_mn(qg_smem + (slot % kStages) * kTileBytes, kBlockBytes), id_o, add);
+                };
+                auto full = [&](uint32_t slot) {
+                    ok = ok && tile_ready(&qg_full[slot % kStages], (slot / kStages) & 1u, &abort_flag) &&
+                         tile_ready(&qg_clean[slot % kStages], (slot / kStages) & 1u, &abort_flag);
+                    return ok;
+                };
+                for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
+                    const Work x = work_of(a, f, u, false);
+                    const int64_t keys = x.ke - x.kb;
+                    const int n = (int)((x.rows + kTile - 1) / kTile);
+                    for (int64_t t = x.t0; t * kTile < keys && n > 0 && ok; t += f.tiles, ++item) {
+                        ok = tile_ready(&kv_full, item & 1u, &abort_flag);
+                        if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
+                        if (!full(g)) break;
+                        product(tmem, k_desc, g);
+                        umma_commit(&s_full);
+                        if (!full(g + 1)) break;
+                        product(tmem + 128, v_desc, g + 1);
                         umma_commit(&dp_full);
-                    } else {
-                        umma_commit(&o_full);
-                        umma_commit(&kv_empty);
+                        for (int j = 0; j < n; ++j, g += 2, ++jj) {
+                            ok = mbar_wait(&p_full, jj & 1u, &abort_flag);
+                            if (!ok) break;
+                            tc_fence_after();
+                            gradient(tmem + 256, tmem, g + 1, j > 0);
+                            umma_commit(&qg_empty[(g + 1) % kStages]);
+                            if (j + 1 < n) {
+                                if (!full(g + 2)) break;
+                                product(tmem, k_desc, g + 2);
+                                umma_commit(&s_full);
+                            }
+                            ok = mbar_wait(&ds_full, jj & 1u, &abort_flag);
+                            if (!ok) break;
+                            tc_fence_after();
+                            gradient(tmem + 384, tmem + 128, g, j > 0);
+                            umma_commit(&qg_empty[g % kStages]);
+                            if (j + 1 < n) {
+                                if (!full(g + 3)) break;
+                                product(tmem + 128, v_desc, g + 3);
+                                umma_commit(&dp_full);
+                            } else {
+                                umma_commit(&o_full);
+                                umma_commit(&kv_empty);
+                            }
+                        }
                     }
                 }
             }
         }
-    }
     } else {
         more_registers<1>();
         // ---- p and dS: 64 columns (rows of Q) of one key per thread
@@ -939,81 +1078,85 @@ attn_tc_dkv_kernel(const __grid_constant__ AttnArgs a, int tiles, const float *_
         const float c1 = a.scale * kLog2e;
         uint32_t jj = 0, item = 0;
         bool ok = true;
-        for (int64_t t = t0; t * kTile < keys && ok; t += tiles, ++item) {
-            const int64_t key = rg.k0 + t * kTile + w * 32 + lane;
-            const bool live = key < rg.k1, seen = live && (!a.mask || a.mask[key]);
-            for (int j = 0; j < n; ++j, ++jj) {
-                ok = mbar_wait(&s_full, jj & 1u, &abort_flag);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                tc_fence_after();
-                const float4 *lse4 = reinterpret_cast<const float4 *>(stat_lse[jj % kStatRing] + q * 64);
-                const float4 *dot4 = reinterpret_cast<const float4 *>(stat_dot[jj % kStatRing] + q * 64);
-                float p[64];
-                uint32_t v0[2][32];
-                tmem_load32_async(tmem + lanes + q * 64, v0[0]);
-                tmem_load32_async(tmem + lanes + q * 64 + 32, v0[1]);
-                tmem_load_wait();
+        for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
+            const Work x = work_of(a, f, u, false);
+            const int64_t keys = x.ke - x.kb;
+            const int n = (int)((x.rows + kTile - 1) / kTile);
+            for (int64_t t = x.t0; t * kTile < keys && ok; t += f.tiles) {
+                const int64_t key = x.kb + t * kTile + w * 32 + lane;
+                const bool live = key < x.ke, seen = live && (!a.mask || a.mask[key]);
+                for (int j = 0; j < n; ++j, ++jj) {
+                    ok = warp_wait(&s_full, jj & 1u, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const float4 *lse4 = reinterpret_cast<const float4 *>(stat_lse[jj % kWordRing] + q * 64);
+                    const float4 *dot4 = reinterpret_cast<const float4 *>(stat_dot[jj % kWordRing] + q * 64);
+                    float p[64];
+                    {
+                        uint32_t v[2][32];
+                        tmem_load32_async(tmem + lanes + q * 64, v[0]);
+                        tmem_load32_async(tmem + lanes + q * 64 + 32, v[1]);
+                        tmem_load_wait();
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float4 l = lse4[c * 8 + e];
-                        p[c * 32 + 4 * e] = exp2_approx(fmaf(__uint_as_float(v0[c][4 * e]), c1, -l.x));
-                        p[c * 32 + 4 * e + 1] = exp2_approx(fmaf(__uint_as_float(v0[c][4 * e + 1]), c1, -l.y));
-                        p[c * 32 + 4 * e + 2] = exp2_approx(fmaf(__uint_as_float(v0[c][4 * e + 2]), c1, -l.z));
-                        p[c * 32 + 4 * e + 3] = exp2_approx(fmaf(__uint_as_float(v0[c][4 * e + 3]), c1, -l.w));
+                        for (int e = 0; e < 64; e += 4) {
+                            const float4 l = lse4[e / 4];
+                            p[e] = exp2_approx(fmaf(__uint_as_float(v[e >> 5][e & 31]), c1, -l.x));
+                            p[e + 1] = exp2_approx(fmaf(__uint_as_float(v[e >> 5][(e & 31) + 1]), c1, -l.y));
+                            p[e + 2] = exp2_approx(fmaf(__uint_as_float(v[e >> 5][(e & 31) + 2]), c1, -l.z));
+                            p[e + 3] = exp2_approx(fmaf(__uint_as_float(v[e >> 5][(e & 31) + 3]), c1, -l.w));
+                        }
                     }
+                    store_operand(tmem + lanes + q * 64, p);
+                    tmem_store_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&p_full);
+                    ok = warp_wait(&dp_full, jj & 1u, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                    {
+                        uint32_t v[2][32];
+                        tmem_load32_async(tmem + lanes + 128 + q * 64, v[0]);
+                        tmem_load32_async(tmem + lanes + 128 + q * 64 + 32, v[1]);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int e = 0; e < 64; e += 4) {
+                            const float4 d = dot4[e / 4];
+                            p[e] *= __uint_as_float(v[e >> 5][e & 31]) - d.x;
+                            p[e + 1] *= __uint_as_float(v[e >> 5][(e & 31) + 1]) - d.y;
+                            p[e + 2] *= __uint_as_float(v[e >> 5][(e & 31) + 2]) - d.z;
+                            p[e + 3] *= __uint_as_float(v[e >> 5][(e & 31) + 3]) - d.w;
+                        }
+                    }
+                    store_operand(tmem + lanes + 128 + q * 64, p);
+                    tmem_store_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&ds_full);
                 }
-                store_operand(tmem + lanes + q * 64, p);
-                tmem_store_wait();
+                if (!ok) break;
+                if (n > 0) {
+                    ok = warp_wait(&o_full, item++ & 1u, &abort_flag);
+                    if (!ok) break;
+                    tc_fence_after();
+                }
+                const int64_t col = x.h * (int64_t)a.head_dim;
+                if (q == 0) store_row<NB>(tmem + lanes + 256, static_cast<bf16 *>(a.dv) + key * a.ldv2 + col, a.head_dim, 1.f, n > 0, seen, live);
+                else store_row<NB>(tmem + lanes + 384, static_cast<bf16 *>(a.dk) + key * a.ldk2 + col, a.head_dim, a.scale, n > 0, seen, live);
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&p_full);
-                ok = mbar_wait(&dp_full, jj & 1u, &abort_flag);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                tc_fence_after();
-                uint32_t v1[2][32];
-                tmem_load32_async(tmem + lanes + 128 + q * 64, v1[0]);
-                tmem_load32_async(tmem + lanes + 128 + q * 64 + 32, v1[1]);
-                tmem_load_wait();
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float4 d = dot4[c * 8 + e];
-                        p[c * 32 + 4 * e] *= __uint_as_float(v1[c][4 * e]) - d.x;
-                        p[c * 32 + 4 * e + 1] *= __uint_as_float(v1[c][4 * e + 1]) - d.y;
-                        p[c * 32 + 4 * e + 2] *= __uint_as_float(v1[c][4 * e + 2]) - d.z;
-                        p[c * 32 + 4 * e + 3] *= __uint_as_float(v1[c][4 * e + 3]) - d.w;
-                    }
-                }
-                store_operand(tmem + lanes + 128 + q * 64, p);
-                tmem_store_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(&ds_full);
+                if (lane == 0 && n > 0) mbar_arrive(&o_empty);
             }
-            if (!ok) break;
-            if (n > 0) {
-                ok = mbar_wait(&o_full, item & 1u, &abort_flag);
-                if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
-                tc_fence_after();
-            }
-            const int64_t col = h * (int64_t)a.head_dim;
-            if (q == 0) store_row<NB>(tmem + lanes + 256, static_cast<bf16 *>(a.dv) + key * a.ldv2 + col, a.head_dim, 1.f, n > 0, seen, live);
-            else store_row<NB>(tmem + lanes + 384, static_cast<bf16 *>(a.dk) + key * a.ldk2 + col, a.head_dim, a.scale, n > 0, seen, live);
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0 && n > 0) mbar_arrive(&o_empty);
         }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
     if (threadIdx.x == 0 && abort_flag && a.status) atomicOr(reinterpret_cast<unsigned *>(a.status), E2EGREC_DEV_TIMEOUT);
-    if (warp == kMmaWarp) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    if (warp == 10) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
 }
 
+// ------------------------------------------------------------------------------------------------- host side
 constexpr int kMaxDevices = 64;
 template <typename Kernel> bool allow_smem(Kernel kernel, size_t bytes, bool (&done)[kMaxDevices])
 {
@@ -1025,48 +1168,79 @@ template <typename Kernel> bool allow_smem(Kernel kernel, size_t bytes, bool (&d
     return true;
 }
 
-}  // namespace
+// A matrix of heads as (column of a head, head, row); box: 64 columns of `box_heads` heads of 128 / box_heads rows, 128-byte swizzle
+bool make_map(CUtensorMap *map, const void *base, int64_t rows, int heads, int head_dim, int64_t ld, int box_heads)
+{
+    TensorMapEncodeFn fn = tensor_map_encode_fn();
+    if (!fn) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)head_dim, (cuuint64_t)heads, (cuuint64_t)rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)head_dim * 2, (cuuint64_t)ld * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)(kTile / box_heads)};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Maps of Q, K, V and (backward) dO; false where one cannot be made
+struct Maps {
+    CUtensorMap q, k, v, g;
+    int boxes;
+};
+bool make_maps(const AttnArgs &a, Maps &m)
+{
+    m.boxes = kTile % a.group == 0;
+    const int box = m.boxes ? a.group : 1, heads = a.kv_heads * a.group;
+    if (!make_map(&m.q, a.q, a.q_rows, heads, a.head_dim, a.ldq, box) || !make_map(&m.k, a.k, a.k_rows, a.kv_heads, a.head_dim, a.ldk, 1) ||
+        !make_map(&m.v, a.v, a.k_rows, a.kv_heads, a.head_dim, a.ldv, 1))
+        return false;
+    m.g = m.q;
+    return !a.dout || make_map(&m.g, a.dout, a.q_rows, heads, a.head_dim, a.ldg, box);
+}
 
 // Small units in numbers go to as many blocks as the machine holds, which prefetch from unit to unit; fewer units get a block each,
 // so that the hardware hands them out as blocks end.
-static uint32_t tc_grid(uint32_t units, int blocks) { return units >= 8u * kSms * blocks ? kSms * blocks : units; }
+uint32_t tc_grid(uint32_t units, int blocks) { return units >= 8u * kSms * blocks ? kSms * blocks : units; }
 
-template <int NB, int NT> static bool launch_fwd(const AttnArgs &a, const TcShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
+template <int NB, int NT> bool launch_fwd(const AttnArgs &a, const Maps &m, const TcShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
 {
     static bool done[kMaxDevices] = {};
     using F = Fwd<NB, NT>;
     if (!allow_smem(attn_tc_fwd_kernel<NB, NT>, F::kSmem, done)) return false;
     note_launch();
-    attn_tc_fwd_kernel<NB, NT><<<tc_grid(f.units, F::kBlocks), F::kThreads, F::kSmem, st>>>(a, f, part_o, part_ml);
+    attn_tc_fwd_kernel<NB, NT><<<tc_grid(f.units, F::kBlocks), F::kThreads, F::kSmem, st>>>(m.q, m.k, m.v, a, f, part_o, part_ml);
     return true;
 }
 
+template <int NB> bool launch_bwd(const AttnArgs &a, const Maps &m, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st)
+{
+    static bool done[2][kMaxDevices] = {};
+    using B = Bwd<NB>;
+    if (!allow_smem(attn_tc_dq_kernel<NB>, B::kDqSmem, done[0]) || !allow_smem(attn_tc_dkv_kernel<NB>, B::kDkvSmem, done[1])) return false;
+    const int64_t units = a.n_seq * a.kv_heads;
+    const TcShape fq{(uint32_t)(units * q_tiles), (int)q_tiles, 1, m.boxes}, fk{(uint32_t)(units * k_tiles), (int)k_tiles, 1, m.boxes};
+    note_launch();
+    attn_tc_dq_kernel<NB><<<tc_grid(fq.units, 1), B::kThreads, B::kDqSmem, st>>>(m.q, m.g, m.k, m.v, a, fq, dots);
+    note_launch();
+    attn_tc_dkv_kernel<NB><<<tc_grid(fk.units, 1), B::kThreads, B::kDkvSmem, st>>>(m.q, m.g, m.k, m.v, a, fk, dots);
+    return true;
+}
+
+}  // namespace
+
 bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, bool one_tile, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    const TcShape f{(uint32_t)(a.n_seq * a.kv_heads * tiles * splits), (int)tiles, splits};
-    if (a.head_dim <= 64) return one_tile ? launch_fwd<1, 1>(a, f, part_o, part_ml, st) : launch_fwd<1, 2>(a, f, part_o, part_ml, st);
-    return one_tile ? launch_fwd<2, 1>(a, f, part_o, part_ml, st) : launch_fwd<2, 2>(a, f, part_o, part_ml, st);
+    Maps m;
+    if (!make_maps(a, m)) return false;
+    const TcShape f{(uint32_t)(a.n_seq * a.kv_heads * tiles * splits), (int)tiles, splits, m.boxes};
+    if (a.head_dim <= 64) return one_tile ? launch_fwd<1, 1>(a, m, f, part_o, part_ml, st) : launch_fwd<1, 2>(a, m, f, part_o, part_ml, st);
+    return one_tile ? launch_fwd<2, 1>(a, m, f, part_o, part_ml, st) : launch_fwd<2, 2>(a, m, f, part_o, part_ml, st);
 }
 
 bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st)
 {
-    static bool done[4][kMaxDevices] = {};
-    const bool one = a.head_dim <= 64;
-    if (!(one ? allow_smem(attn_tc_dq_kernel<1>, dq_smem<1>(), done[0]) && allow_smem(attn_tc_dkv_kernel<1>, dkv_smem<1>(), done[1])
-              : allow_smem(attn_tc_dq_kernel<2>, dq_smem<2>(), done[2]) && allow_smem(attn_tc_dkv_kernel<2>, dkv_smem<2>(), done[3])))
-        return false;
-    const int64_t units = a.n_seq * a.kv_heads;
-    if (a.q_rows) {
-        note_launch();
-        if (one) attn_tc_dq_kernel<1><<<(unsigned)(units * q_tiles), kThreads, dq_smem<1>(), st>>>(a, (int)q_tiles, dots);
-        else attn_tc_dq_kernel<2><<<(unsigned)(units * q_tiles), kThreads, dq_smem<2>(), st>>>(a, (int)q_tiles, dots);
-    }
-    if (a.k_rows) {
-        note_launch();
-        if (one) attn_tc_dkv_kernel<1><<<(unsigned)(units * k_tiles), kThreads, dkv_smem<1>(), st>>>(a, (int)k_tiles, dots);
-        else attn_tc_dkv_kernel<2><<<(unsigned)(units * k_tiles), kThreads, dkv_smem<2>(), st>>>(a, (int)k_tiles, dots);
-    }
-    return true;
+    Maps m;
+    if (!make_maps(a, m)) return false;
+    return a.head_dim <= 64 ? launch_bwd<1>(a, m, q_tiles, k_tiles, dots, st) : launch_bwd<2>(a, m, q_tiles, k_tiles, dots, st);
 }
 
 }  // namespace e2egrec

@@ -59,10 +59,12 @@ class Problem:
         mk = int((self.k_ptr[1:] - self.k_ptr[:-1]).max()) if hints is True else hints
         return E.Sequences(self.q_ptr.cuda(), self.k_ptr.cuda(), mq, mk, None if self.mask is None else self.mask.cuda())
 
-    def run(self, E, hints=True, backward=True, wide=False):
+    def run(self, E, hints=True, backward=True, wide=0):
         cu = lambda t: t.cuda()
         if wide:          # column ranges of wider matrices, and results into such ranges
-            widen = lambda t: torch.cat([torch.full_like(t, float("nan")), t, torch.full_like(t, float("nan"))], 1).cuda()[:, t.shape[1]: 2 * t.shape[1]]
+            def widen(t):         # `wide` more columns on either side: the distance of two rows need not be a multiple of a head
+                side = torch.full((t.shape[0], wide), float("nan"), dtype=t.dtype)
+                return torch.cat([side, t, side], 1).cuda()[:, wide: wide + t.shape[1]]
         else:
             widen = cu
         q, k, v, g = widen(self.q_in), widen(self.k_in), widen(self.v_in), widen(self.g_in)
@@ -129,7 +131,8 @@ def test_column_ranges_hints_and_repetition(lengths, dtype):
     again = p.run(E)
     for name in first:
         assert torch.equal(first[name], again[name]), name
-    p.check(p.run(E, wide=True), want)
+    p.check(p.run(E, wide=8), want)
+    p.check(p.run(E, wide=128), want)
     p.check(p.run(E, hints=0), want)
     p.check(p.run(E, hints=1), want)
 
