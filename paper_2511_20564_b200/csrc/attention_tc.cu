@@ -516,6 +516,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);
                 for (int c = 0; c < NB * 2; ++c) {
                     uint32_t v[32];
+                    __syncwarp();                            // the loads of tensor memory are for a converged warp; the stores are not
                     if (x.n > 0) {
                         tmem_load32_async(o_addr + c * 32, v);
                         tmem_load_wait();
@@ -583,6 +584,7 @@ __device__ inline void store_row(uint32_t taddr, bf16 *out, int head_dim, float 
 {
     for (int c = 0; c < NB * 2; ++c) {
         uint32_t v[32];
+        __syncwarp();                                    // the loads of tensor memory are for a converged warp; the stores are not
         if (have) {
             tmem_load32_async(taddr + c * 32, v);
             tmem_load_wait();
