@@ -63,14 +63,11 @@ __device__ inline void tmem_load16_async(uint32_t taddr, uint32_t (&r)[16])
         : "r"(taddr));
 }
 
-// Registers are dealt out anew once the block runs.  One block per SM: 384 threads x 168 at launch = 128 (copies and products) x 72 +
-// 256 x 216.  Two blocks per SM: 256 threads x 128 = 128 x 72 + 128 x 184.
-template <int kBlocks> __device__ inline void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 72;"); }
-template <int kBlocks> __device__ inline void more_registers()
-{
-    if (kBlocks == 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-    else asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
-}
+// Registers are dealt out anew once the block runs, kCopies to the threads of copies and products, kScores to those of the scores.  One
+// block per SM: 384 threads x 168 at launch = 128 x 72 + 256 x 216 (forward) = 128 x 104 + 256 x 200 (backward, whose copies hold statistics
+// of rows a tile ahead; spilled, they were waited for).  Two blocks per SM: 256 threads x 128 = 128 x 72 + 128 x 184.
+template <int kRegisters> __device__ inline void fewer_registers() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegisters)); }
+template <int kRegisters> __device__ inline void more_registers() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegisters)); }
 
 // What a block works on: unit u of `units`, a stretch of the keys of a block of rows of one key head.  A block takes the units
 // blockIdx.x, blockIdx.x + gridDim.x, ...
@@ -179,6 +176,21 @@ template <int NB> __device__ inline void clear_rows(uint32_t tile, const uint32_
 }
 __device__ inline bool all_seen(const uint32_t (&word)[4]) { return (word[0] & word[1] & word[2] & word[3]) == 0xFFFFFFFFu; }
 
+// Loads that stay where they are written, a tile ahead of their use (the compiler moves plain ones down to it, where their latency
+// held up the copies: 2800 cycles a tile of the dK, dV kernel)
+__device__ inline float load_now(const float *p)
+{
+    float v;
+    asm volatile("ld.global.f32 %0, [%1];" : "=f"(v) : "l"(p) : "memory");
+    return v;
+}
+__device__ inline uint32_t load_now(const uint8_t *p)
+{
+    uint32_t v;
+    asm volatile("ld.global.u8 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
 // Whether the 128 keys from j * 128 on are seen, one bit each; loads for the next tile go out a tile ahead (ahead, then now)
 struct Visible {
     uint32_t next[4];
@@ -187,7 +199,7 @@ struct Visible {
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
             const int64_t key = x.kb + (int64_t)j * kTile + b * 32 + lane;
-            next[b] = key < x.ke ? (a.mask ? (uint32_t)a.mask[key] : 1u) : 0u;
+            next[b] = key < x.ke ? (a.mask ? load_now(a.mask + key) : 1u) : 0u;
         }
     }
     __device__ inline void now(uint32_t (&word)[4]) const
@@ -291,7 +303,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const uint32_t tmem = tmem_slot, tmem_o = tmem + NT * kTile;      // scores (and p) of tile t: columns 128 t; outputs: 64 NB each behind them
 
     if (warp >= kSoft) {
-        fewer_registers<F::kBlocks>();
+        fewer_registers<72>();
         if (warp == kSoft) {
             // ---- copies: queries of a block of rows, then keys and values in turn
             uint32_t g = 0, jj = 0, item = 0, q_issued = 0;
@@ -420,7 +432,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
         }
     } else {
-        more_registers<F::kBlocks>();
+        more_registers<F::kBlocks == 1 ? 216 : 184>();
         // ---- softmax of tile `q`, one row per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
@@ -647,7 +659,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     const uint32_t tmem = tmem_slot;                  // scores: columns 0 and 128 in turn; dP and dS: 256; dQ: 384
 
     if (warp >= 8) {
-        fewer_registers<1>();
+        fewer_registers<104>();
         if (warp == 8) {
             // ---- copies: Q and dO of a tile of rows, then keys and values in turn
             uint32_t g = 0, jj = 0, item = 0, q_issued = 0;
@@ -770,7 +782,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             }
         }
     } else {
-        more_registers<1>();
+        more_registers<200>();
         // ---- p and dS: 64 columns of one row per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
@@ -909,7 +921,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const uint32_t tmem = tmem_slot;                  // S^T and P^T: columns 0; dP^T and dS^T: 128; dV: 256; dK: 384
 
     if (warp >= 8) {
-        fewer_registers<1>();
+        fewer_registers<104>();
         if (warp == 8) {
             // ---- copies: keys and values of a tile, then Q and dO of the rows in turn, with the rows' lse and D (fetched a tile ahead)
             const int heads = a.kv_heads * a.group;
@@ -927,8 +939,8 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         int64_t row;
                         int head;
                         row_of(a, x, r, row, head);
-                        lse[b] = r < x.rows ? a.lse[row * heads + head] : -INFINITY;
-                        dot[b] = r < x.rows ? dots[row * heads + head] : 0.f;
+                        lse[b] = r < x.rows ? load_now(a.lse + row * heads + head) : -INFINITY;
+                        dot[b] = r < x.rows ? load_now(dots + row * heads + head) : 0.f;
                     }
                 };
                 for (int64_t t = x.t0; t * kTile < keys && n > 0 && ok; t += f.tiles, ++item) {
@@ -1073,7 +1085,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             }
         }
     } else {
-        more_registers<1>();
+        more_registers<200>();
         // ---- p and dS: 64 columns (rows of Q) of one key per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
