@@ -66,7 +66,7 @@ bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, 
 // attention_few.cu: streaming kernels, fp32 and bf16, head_dim <= 256
 struct FewPlan {
     int rows;                             // rows per unit
-    bool one_step;                        // a warp's step holds all keys of a sequence
+    int steps;                            // steps of keys in flight per warp
     bool both;                            // backward: one kernel for dQ, dK and dV
     int64_t batches;                      // units of rows per sequence and key head
     int warps, splits;                    // warps per unit, stretches of the keys

@@ -1,9 +1,10 @@
 // Attention where a sequence has few rows (query, head of the group) per key head: single tokens, a candidate, a stack of a few
 // tokens.  Every key and value is used a handful of times, so these kernels stream them: fp32 FMA, 16 bytes per lane and load.
 //
-// `lanes` neighbouring lanes share a key (16 bytes of the head each) and 32 / lanes keys are in a warp's step, kUnroll steps in flight.
-// Each lane group keeps its own running maximum, sum and outputs over the keys it meets; groups, then the warps of a unit, then the
-// stretches of a long list of keys are joined at the end, in a fixed order.  A unit is up to R rows of one sequence and key head.
+// `lanes` neighbouring lanes share a head's part of a key (16 bytes each), `heads` key heads lie side by side in a warp as they do in
+// memory, and the rest of the warp is further keys of the step; kUnroll steps are in flight.  Each lane group keeps its own running
+// maximum, sum and outputs over the keys it meets; groups, then the warps of a unit, then the stretches of a long list of keys are
+// joined at the end, in a fixed order.  A unit is up to R rows of one sequence and of each of its key heads.
 #include <algorithm>
 
 #include "attention.cuh"
@@ -12,7 +13,8 @@ namespace e2egrec {
 namespace {
 
 constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
-constexpr int kUnroll = 4;                           // steps of keys in flight per warp (1 where a step holds all keys of a sequence)
+constexpr int kUnroll = 4;                           // steps of keys in flight per warp (1 where a step holds all keys of a sequence, 2 for
+                                                     // more than two rows unless four steps hold all keys)
 
 template <typename T, int CPL> struct Piece {        // a lane's part of a head's row
     static constexpr int E = Chunk<T>::kElems * CPL;
@@ -80,7 +82,8 @@ template <int N> __device__ inline void key_sums(float (&v)[N], int lanes)
 }
 
 struct FewShape {
-    int lanes, chunks;                               // lanes per key (a power of two), 16-byte chunks of a head
+    int lanes, chunks;                               // lanes per head of a key (a power of two), 16-byte chunks of a head
+    int heads, head_groups;                          // key heads side by side in a warp (a power of two), groups of them
     int warps;                                       // warps per unit: a power of two, at most kFewWarps
     int batches;                                     // batches of R rows per sequence and key head
     int splits;                                      // stretches of the keys
@@ -97,8 +100,8 @@ __device__ inline float exp2_fast(float x)
 struct Unit {
     SeqRange rg;
     int64_t kb, ke, rows;
-    int z, h, first;
-    bool any;
+    int z, h, first;                                 // h: the lane's key head
+    bool any, on;                                    // there is such a unit; there is such a head
 };
 __device__ inline Unit few_unit(const AttnArgs &a, const FewShape &f, uint32_t u)            // fewer than 2^31 units: few_plan
 {
@@ -113,14 +116,15 @@ __device__ inline Unit few_unit(const AttnArgs &a, const FewShape &f, uint32_t u
         x.first = (int)(u % (uint32_t)f.batches);
         u /= (uint32_t)f.batches;
     }
-    const uint32_t s = u / (uint32_t)a.kv_heads;
-    x.h = (int)(u - s * (uint32_t)a.kv_heads);
+    const uint32_t s = u / (uint32_t)f.head_groups, hg = u - s * (uint32_t)f.head_groups;
+    x.h = (int)(hg * f.heads + (threadIdx.x & 31) / f.lanes % f.heads);
+    x.on = x.any && x.h < a.kv_heads;
     if (!x.any) {
         x.rows = x.kb = x.ke = 0;
         x.rg = SeqRange{0, 0, 0, 0};
         return x;
     }
-    x.rg = seq_range(a, s, (threadIdx.x & 31) == 0 && x.h == 0 && x.first == 0 && x.z == 0);
+    x.rg = seq_range(a, s, (threadIdx.x & 31) == 0 && hg == 0 && x.first == 0 && x.z == 0);
     x.rows = (x.rg.q1 - x.rg.q0) * a.group;
     x.kb = x.rg.k0;
     x.ke = x.rg.k1;
@@ -158,12 +162,12 @@ __global__ void __launch_bounds__(kFewThreads, CPL == 2 ? 1 : (R > 2 ? 2 : 3))
 attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
 {
     constexpr int E = Piece<T, CPL>::E;
-    __shared__ float2 join_ml[kFewWarps][R];
-    __shared__ float join_o[kFewWarps][kMaxAttnDim];
+    __shared__ float2 join_ml[kFewWarps][R][32];
+    __shared__ float join_o[kFewWarps][E * 32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wu = warp & (f.warps - 1);                                            // the warp's number in its unit
     const Unit x = few_unit(a, f, blockIdx.x * (uint32_t)(kFewWarps / f.warps) + warp / f.warps);
-    const int grp = lane / f.lanes, at = lane & (f.lanes - 1), kpw = 32 / f.lanes;
+    const int wide = f.lanes * f.heads, grp = lane / wide, at = lane & (f.lanes - 1), kpw = 32 / wide;
     const int heads = a.kv_heads * a.group;
     const int64_t koff = x.h * (int64_t)a.head_dim;
     const float c1 = a.scale * kLog2e;
@@ -177,7 +181,7 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         for (int r = 0; r < R; ++r, in.next(a)) {
             Piece<T, CPL> p;
             p.zero();
-            if (live && r0 + r < x.rows) p.load(static_cast<const T *>(a.q) + in.row * a.ldq + in.head(a, x) * (int64_t)a.head_dim, at, f.lanes, f.chunks);
+            if (live && x.on && r0 + r < x.rows) p.load(static_cast<const T *>(a.q) + in.row * a.ldq + in.head(a, x) * (int64_t)a.head_dim, at, f.lanes, f.chunks);
             p.widen(q[r]);
 #pragma unroll
             for (int e = 0; e < E; ++e) {
@@ -194,7 +198,7 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int64_t j = j0 + u * kpw + grp;
-                seen[u] = j < x.ke && (!a.mask || a.mask[j]);
+                seen[u] = x.on && j < x.ke && (!a.mask || a.mask[j]);
                 k[u].zero();
                 v[u].zero();
                 if (seen[u]) {
@@ -239,7 +243,7 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             }
         }
         // lane groups of the warp
-        for (int d = f.lanes; d < 32; d <<= 1)
+        for (int d = wide; d < 32; d <<= 1)
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 const float m2 = __shfl_xor_sync(0xFFFFFFFFu, m[r], d), l2 = __shfl_xor_sync(0xFFFFFFFFu, l[r], d), top = fmaxf(m[r], m2);
@@ -250,37 +254,29 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 for (int e = 0; e < E; ++e) o[r][e] = o[r][e] * c + __shfl_xor_sync(0xFFFFFFFFu, o[r][e], d) * c2;
             }
         if (f.warps > 1) {
-            if (lane == 0)
+            if (grp == 0 && at == 0)
 #pragma unroll
-                for (int r = 0; r < R; ++r) join_ml[warp][r] = make_float2(m[r], l[r]);
+                for (int r = 0; r < R; ++r) join_ml[warp][r][lane] = make_float2(m[r], l[r]);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 __syncthreads();
                 if (grp == 0)
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c)
-                        if (at + c * f.lanes < f.chunks)
-#pragma unroll
-                            for (int e = 0; e < Chunk<T>::kElems; ++e)
-                                join_o[warp][(at + c * f.lanes) * Chunk<T>::kElems + e] = o[r][c * Chunk<T>::kElems + e];
+                    for (int e = 0; e < E; ++e) join_o[warp][e * 32 + lane] = o[r][e];
                 __syncthreads();
                 if (wu == 0 && grp == 0) {
                     float top = -INFINITY;
-                    for (int w = 0; w < f.warps; ++w) top = fmaxf(top, join_ml[warp + w][r].x);
+                    for (int w = 0; w < f.warps; ++w) top = fmaxf(top, join_ml[warp + w][r][lane - at].x);
                     const float base = top == -INFINITY ? 0.f : top;
                     float sum = 0.f;
 #pragma unroll
                     for (int e = 0; e < E; ++e) o[r][e] = 0.f;
                     for (int w = 0; w < f.warps; ++w) {
-                        const float2 ml = join_ml[warp + w][r];
+                        const float2 ml = join_ml[warp + w][r][lane - at];
                         const float c = exp2_fast(ml.x - base);
                         sum += ml.y * c;
 #pragma unroll
-                        for (int k = 0; k < CPL; ++k)
-                            if (at + k * f.lanes < f.chunks)
-#pragma unroll
-                                for (int e = 0; e < Chunk<T>::kElems; ++e)
-                                    o[r][k * Chunk<T>::kElems + e] += c * join_o[warp + w][(at + k * f.lanes) * Chunk<T>::kElems + e];
+                        for (int e = 0; e < E; ++e) o[r][e] += c * join_o[warp + w][e * 32 + lane];
                     }
                     m[r] = top;
                     l[r] = sum;
@@ -288,7 +284,7 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             }
         }
         RowWalk out(a, x, r0);
-        if (wu == 0 && grp == 0 && live)
+        if (wu == 0 && grp == 0 && live && x.on)
 #pragma unroll
             for (int r = 0; r < R; ++r, out.next(a))
                 if (r0 + r < x.rows) {
@@ -317,11 +313,11 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 // formed from the stored outputs.
 constexpr int kKeys = 2;
 template <typename T, int CPL>
-__device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int h, int64_t j0, int64_t end, int grp, int at, const FewShape &f,
+__device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int h, bool on, int64_t j0, int64_t end, int grp, int at, const FewShape &f,
                                       const float *dots)
 {
     constexpr int E = Piece<T, CPL>::E;
-    const int kpw = 32 / f.lanes, heads = a.kv_heads * a.group;
+    const int kpw = 32 / (f.lanes * f.heads), heads = a.kv_heads * a.group;
     const int64_t koff = h * (int64_t)a.head_dim;
     const float c1 = a.scale * kLog2e;
     float k[kKeys][E], v[kKeys][E], dk[kKeys][E], dv[kKeys][E];
@@ -329,7 +325,7 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
 #pragma unroll
     for (int n = 0; n < kKeys; ++n) {
         const int64_t j = j0 + n * kpw + grp;
-        seen[n] = j < end && (!a.mask || a.mask[j]);
+        seen[n] = on && j < end && (!a.mask || a.mask[j]);
         Piece<T, CPL> p, t;
         p.zero();
         t.zero();
@@ -344,13 +340,18 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
     }
     for (int64_t row = rg.q0; row < rg.q1; ++row)
         for (int g = 0; g < a.group; ++g) {
-            const int head = h * a.group + g;
+            const int head = (on ? h : 0) * a.group + g;
             const float l = __ldg(a.lse + row * heads + head);
-            if (l == -INFINITY) continue;
+            if (__all_sync(0xFFFFFFFFu, l == -INFINITY)) continue;
+            const bool live = l != -INFINITY;
             const int64_t col = (int64_t)head * a.head_dim;
             Piece<T, CPL> p, t;
-            p.load(static_cast<const T *>(a.q) + row * a.ldq + col, at, f.lanes, f.chunks);
-            t.load(static_cast<const T *>(a.dout) + row * a.ldg + col, at, f.lanes, f.chunks);
+            p.zero();
+            t.zero();
+            if (live) {
+                p.load(static_cast<const T *>(a.q) + row * a.ldq + col, at, f.lanes, f.chunks);
+                t.load(static_cast<const T *>(a.dout) + row * a.ldg + col, at, f.lanes, f.chunks);
+            }
             float q[E], go[E], s[2 * kKeys], d[1];
             p.widen(q);
             t.widen(go);
@@ -358,7 +359,8 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
                 d[0] = __ldg(dots + row * heads + head);
             } else {
                 Piece<T, CPL> o;
-                o.load(static_cast<const T *>(a.o) + row * a.ldo + col, at, f.lanes, f.chunks);
+                o.zero();
+                if (live) o.load(static_cast<const T *>(a.o) + row * a.ldo + col, at, f.lanes, f.chunks);
                 float y[E];
                 o.widen(y);
                 d[0] = dot<E>(go, y);
@@ -372,15 +374,15 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
             key_sums<2 * kKeys>(s, f.lanes);
 #pragma unroll
             for (int n = 0; n < kKeys; ++n) {
-                const float pr = seen[n] ? exp2_fast(fmaf(s[n], c1, -l * kLog2e)) : 0.f;
+                const float pr = seen[n] && live ? exp2_fast(fmaf(s[n], c1, -l * kLog2e)) : 0.f;
                 axpy<E>(dv[n], pr, go);
-                axpy<E>(dk[n], seen[n] ? pr * (s[kKeys + n] - d[0]) : 0.f, q);
+                axpy<E>(dk[n], seen[n] && live ? pr * (s[kKeys + n] - d[0]) : 0.f, q);
             }
         }
 #pragma unroll
     for (int n = 0; n < kKeys; ++n) {
         const int64_t j = j0 + n * kpw + grp;
-        if (j < end) {
+        if (on && j < end) {
             store_piece<T, CPL>(static_cast<T *>(a.dk) + j * a.ldk2 + koff, at, f.lanes, f.chunks, dk[n], a.scale);
             store_piece<T, CPL>(static_cast<T *>(a.dv) + j * a.ldv2 + koff, at, f.lanes, f.chunks, dv[n], 1.f);
         }
@@ -397,11 +399,11 @@ __global__ void __launch_bounds__(kFewThreads)
 attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_dq, float *__restrict__ dots)
 {
     constexpr int E = Piece<T, CPL>::E;
-    __shared__ float join[kFewWarps][kMaxAttnDim];
+    __shared__ float join[kFewWarps][E * 32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wu = warp & (f.warps - 1);
     const Unit x = few_unit(a, f, blockIdx.x * (uint32_t)(kFewWarps / f.warps) + warp / f.warps);
-    const int grp = lane / f.lanes, at = lane & (f.lanes - 1), kpw = 32 / f.lanes;
+    const int wide = f.lanes * f.heads, grp = lane / wide, at = lane & (f.lanes - 1), kpw = 32 / wide;
     const int heads = a.kv_heads * a.group;
     const int64_t koff = x.h * (int64_t)a.head_dim;
     const float c1 = a.scale * kLog2e;
@@ -422,7 +424,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             t.zero();
             lse[r] = INFINITY;
             d[r] = 0.f;
-            if (live && r0 + r < x.rows) {
+            if (live && x.on && r0 + r < x.rows) {
                 const int64_t row = in.row;
                 const int head = in.head(a, x);
                 const int64_t col = (int64_t)head * a.head_dim;
@@ -453,7 +455,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int64_t j = j0 + u * kpw + grp;
-                seen[u] = j < x.ke && (!a.mask || a.mask[j]);
+                seen[u] = x.on && j < x.ke && (!a.mask || a.mask[j]);
                 k[u].zero();
                 v[u].zero();
                 if (seen[u]) {
@@ -482,7 +484,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     float t = 0.f;
 #pragma unroll
                     for (int u = 0; u < U; ++u) t += seen[u] ? s[r * U + u] * s[(R + r) * U + u] : 0.f;
-                    for (int o = f.lanes; o < 32; o <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
+                    for (int o = wide; o < 32; o <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
                     d[r] = t;
                 }
 #pragma unroll
@@ -495,7 +497,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
                 for (int r = 0; r < R; ++r) axpy<E>(dq[r], s[(R + r) * U + u], w);
                 const int64_t j = j0 + u * kpw + grp;
-                if (kBoth && whole && j < x.ke) {
+                if (kBoth && whole && x.on && j < x.ke) {
                     float dk[E], dv[E];
 #pragma unroll
                     for (int e = 0; e < E; ++e) dk[e] = dv[e] = 0.f;
@@ -509,7 +511,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 }
             }
         }
-        for (int o = f.lanes; o < 32; o <<= 1)
+        for (int o = wide; o < 32; o <<= 1)
 #pragma unroll
             for (int r = 0; r < R; ++r)
 #pragma unroll
@@ -521,20 +523,14 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 __syncthreads();
                 if (grp == 0)
 #pragma unroll
-                    for (int c = 0; c < CPL; ++c)
-                        if (at + c * f.lanes < f.chunks)
-#pragma unroll
-                            for (int e = 0; e < Chunk<T>::kElems; ++e) join[warp][(at + c * f.lanes) * Chunk<T>::kElems + e] = dq[r][c * Chunk<T>::kElems + e];
+                    for (int e = 0; e < E; ++e) join[warp][e * 32 + lane] = dq[r][e];
                 __syncthreads();
                 if (wu == 0 && grp == 0)
                     for (int w = 1; w < f.warps; ++w)
 #pragma unroll
-                        for (int c = 0; c < CPL; ++c)
-                            if (at + c * f.lanes < f.chunks)
-#pragma unroll
-                                for (int e = 0; e < Chunk<T>::kElems; ++e) dq[r][c * Chunk<T>::kElems + e] += join[warp + w][(at + c * f.lanes) * Chunk<T>::kElems + e];
+                        for (int e = 0; e < E; ++e) dq[r][e] += join[warp + w][e * 32 + lane];
             }
-            if (wu == 0 && grp == 0 && live && r0 + r < x.rows) {
+            if (wu == 0 && grp == 0 && live && x.on && r0 + r < x.rows) {
                 const int64_t row = out.row;
                 const int head = out.head(a, x);
                 if (!kBoth && x.z == 0 && at == 0) dots[row * heads + head] = d[r];
@@ -554,7 +550,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     }
     if (kBoth && x.any && !whole)
         for (int64_t j0 = x.kb + (int64_t)wu * kKeys * kpw; j0 < x.ke; j0 += (int64_t)f.warps * kKeys * kpw)
-            keys_gradients<T, CPL>(a, x.rg, x.h, j0, x.ke, grp, at, f, nullptr);
+            keys_gradients<T, CPL>(a, x.rg, x.h, x.on, j0, x.ke, grp, at, f, nullptr);
 }
 
 // dK and dV where the rows of a sequence do not fit one unit
@@ -567,11 +563,12 @@ attn_few_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     if (u >= f.units) return;
     const int first = (int)(u % (uint32_t)f.batches);
     u /= (uint32_t)f.batches;
-    const int h = (int)(u % (uint32_t)a.kv_heads);
-    const SeqRange rg = seq_range(a, u / (uint32_t)a.kv_heads, lane == 0 && h == 0 && first == 0);
-    const int64_t step = (int64_t)kKeys * (32 / f.lanes);
+    const uint32_t s = u / (uint32_t)f.head_groups, hg = u - s * (uint32_t)f.head_groups;
+    const int wide = f.lanes * f.heads, h = (int)(hg * f.heads + lane / f.lanes % f.heads);
+    const SeqRange rg = seq_range(a, s, lane == 0 && hg == 0 && first == 0);
+    const int64_t step = (int64_t)kKeys * (32 / wide);
     for (int64_t j0 = rg.k0 + first * step; j0 < rg.k1; j0 += f.batches * step)
-        keys_gradients<T, CPL>(a, rg, h, j0, rg.k1, lane / f.lanes, lane & (f.lanes - 1), f, dots);
+        keys_gradients<T, CPL>(a, rg, h, h < a.kv_heads, j0, rg.k1, lane / wide, lane & (f.lanes - 1), f, dots);
 }
 
 FewShape few_shape(const AttnArgs &a, int es)
@@ -580,13 +577,16 @@ FewShape few_shape(const AttnArgs &a, int es)
     f.chunks = a.head_dim * es / 16;
     f.lanes = 1;
     while (f.lanes < f.chunks && f.lanes < 32) f.lanes <<= 1;
+    f.heads = 1;
+    while (f.heads * 2 <= a.kv_heads && f.heads * 2 * f.lanes <= 32) f.heads *= 2;
+    f.head_groups = (a.kv_heads + f.heads - 1) / f.heads;
     f.warps = f.batches = f.splits = 1;
     return f;
 }
 
 unsigned few_grid(const AttnArgs &a, FewShape &f)
 {
-    f.units = (uint32_t)(a.n_seq * a.kv_heads * f.batches * f.splits);
+    f.units = (uint32_t)(a.n_seq * f.head_groups * f.batches * f.splits);
     return (unsigned)ceil_div(f.units, kFewWarps / f.warps);
 }
 
@@ -599,42 +599,42 @@ void launch_fwd(const AttnArgs &a, FewShape f, float *part_o, float2 *part_ml, c
     else if constexpr (sizeof(T) == 4) attn_few_fwd_kernel<T, R, U, 2><<<grid, kFewThreads, 0, st>>>(a, f, part_o, part_ml);
 }
 
-template <typename T, int R, bool kBoth>
-void launch_bwd(const AttnArgs &a, FewShape f, bool one_step, float *part_dq, float *dots, cudaStream_t st)
+template <typename T, int R, int U, bool kBoth>
+void launch_bwd(const AttnArgs &a, FewShape f, float *part_dq, float *dots, cudaStream_t st)
 {
-    constexpr int U = R > 2 ? 2 : kUnroll;
     note_launch();
     const unsigned grid = few_grid(a, f);
-    if (f.chunks <= 32) {
-        if (one_step) attn_few_bwd_kernel<T, R, 1, 1, kBoth><<<grid, kFewThreads, 0, st>>>(a, f, part_dq, dots);
-        else attn_few_bwd_kernel<T, R, U, 1, kBoth><<<grid, kFewThreads, 0, st>>>(a, f, part_dq, dots);
-    } else if constexpr (sizeof(T) == 4) {
-        attn_few_bwd_kernel<T, R, U, 2, kBoth><<<grid, kFewThreads, 0, st>>>(a, f, part_dq, dots);
-    }
+    if (f.chunks <= 32) attn_few_bwd_kernel<T, R, U, 1, kBoth><<<grid, kFewThreads, 0, st>>>(a, f, part_dq, dots);
+    else if constexpr (sizeof(T) == 4) attn_few_bwd_kernel<T, R, U, 2, kBoth><<<grid, kFewThreads, 0, st>>>(a, f, part_dq, dots);
+}
+
+template <typename T, int R> void forward_rows(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
+{
+    if (p.steps == 1) launch_fwd<T, R, 1>(a, f, part_o, part_ml, st);
+    else if (p.steps == 2) launch_fwd<T, R, 2>(a, f, part_o, part_ml, st);
+    else launch_fwd<T, R, kUnroll>(a, f, part_o, part_ml, st);
 }
 
 template <typename T> void forward_of(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    if (p.one_step) {
-        if (p.rows == 1) launch_fwd<T, 1, 1>(a, f, part_o, part_ml, st);
-        else if (p.rows == 2) launch_fwd<T, 2, 1>(a, f, part_o, part_ml, st);
-        else launch_fwd<T, 4, 1>(a, f, part_o, part_ml, st);
-    } else {
-        if (p.rows == 1) launch_fwd<T, 1, kUnroll>(a, f, part_o, part_ml, st);
-        else if (p.rows == 2) launch_fwd<T, 2, kUnroll>(a, f, part_o, part_ml, st);
-        else launch_fwd<T, 4, 2>(a, f, part_o, part_ml, st);
-    }
+    if (p.rows == 1) forward_rows<T, 1>(a, p, f, part_o, part_ml, st);
+    else if (p.rows == 2) forward_rows<T, 2>(a, p, f, part_o, part_ml, st);
+    else forward_rows<T, 4>(a, p, f, part_o, part_ml, st);
+}
+
+template <typename T, int R, bool kBoth> void backward_rows(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_dq, float *dots, cudaStream_t st)
+{
+    if (p.steps == 1) launch_bwd<T, R, 1, kBoth>(a, f, part_dq, dots, st);
+    else if (p.steps == 2) launch_bwd<T, R, 2, kBoth>(a, f, part_dq, dots, st);
+    else launch_bwd<T, R, kUnroll, kBoth>(a, f, part_dq, dots, st);
 }
 
 template <typename T> void backward_of(const AttnArgs &a, const FewPlan &p, FewShape f, float *part_dq, float *dots, cudaStream_t st)
 {
-    if (p.both) {
-        if (p.rows == 1) launch_bwd<T, 1, true>(a, f, p.one_step, part_dq, dots, st);
-        else if (p.rows == 2) launch_bwd<T, 2, true>(a, f, p.one_step, part_dq, dots, st);
-        else launch_bwd<T, 4, true>(a, f, p.one_step, part_dq, dots, st);
-    } else {
-        launch_bwd<T, 4, false>(a, f, p.one_step, part_dq, dots, st);
-    }
+    if (!p.both) backward_rows<T, 4, false>(a, p, f, part_dq, dots, st);
+    else if (p.rows == 1) backward_rows<T, 1, true>(a, p, f, part_dq, dots, st);
+    else if (p.rows == 2) backward_rows<T, 2, true>(a, p, f, part_dq, dots, st);
+    else backward_rows<T, 4, true>(a, p, f, part_dq, dots, st);
     if (f.splits > 1 && a.q_rows) join_dq(a, f.splits, sizeof(T) == 4 ? E2EGREC_F32 : E2EGREC_BF16, part_dq, st);
     if (!p.both && a.k_rows) {
         note_launch();
@@ -654,12 +654,12 @@ FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool b
 {
     FewPlan p{};
     const FewShape f = few_shape(a, es);
-    const int64_t rows = max_q * a.group, units0 = std::max<int64_t>(a.n_seq * a.kv_heads, 1), most = (((int64_t)1 << 31) - 1) / units0;
-    const int64_t step = 32 / f.lanes;
+    const int64_t rows = max_q * a.group, units0 = std::max<int64_t>(a.n_seq * f.head_groups, 1), most = (((int64_t)1 << 31) - 1) / units0;
+    const int64_t step = 32 / (f.lanes * f.heads);
     p.rows = rows <= 1 ? 1 : (rows <= 2 ? 2 : 4);
     p.both = backward && rows <= p.rows;
-    p.one_step = max_k <= step && f.chunks <= 32;
-    const int64_t turn = step * (p.one_step ? 1 : (p.rows > 2 ? 2 : kUnroll));
+    p.steps = max_k <= step ? 1 : (p.rows > 2 && max_k > kUnroll * step ? 2 : kUnroll);
+    const int64_t turn = step * p.steps;
     p.batches = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, p.rows), most));
     const int64_t want = std::max<int64_t>(1, std::min(ceil_div(148 * 24, units0 * p.batches), ceil_div(max_k, turn)));
     p.warps = 1;
