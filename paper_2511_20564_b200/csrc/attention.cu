@@ -121,11 +121,10 @@ int32_t check_heads(const e2egrec_mat *m, int32_t heads, int32_t head_dim, int32
 
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
 
-// The kernels of a call.  A sequence's keys and rows stream (attention_few.cu) where a key head has up to kFewRows rows, or where a
-// sequence is so small that the set-up of a tile costs more than its products; bf16 heads of up to 128 go to the tensor cores
-// otherwise, fp32 ones to tiles of fp32 FMA, wider heads always stream.
+// The kernels of a call.  A sequence's keys and rows stream (attention_few.cu) where a key head has up to two rows (four in the
+// backward pass), or where a sequence is so small that the set-up of a tile costs more than its products; bf16 heads of up to 128
+// go to the tensor cores otherwise, fp32 ones to tiles of fp32 FMA, wider heads always stream.
 enum class Path { few, tc, simt };
-constexpr int64_t kFewRows = 4;
 
 struct Plan {
     Path path;
@@ -144,7 +143,7 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     const int64_t max_q = s.max_q ? std::min(s.max_q, a.q_rows) : a.q_rows, max_k = s.max_k ? std::min(s.max_k, a.k_rows) : a.k_rows;
     const int64_t rows = max_q * a.group, units = std::max<int64_t>(a.n_seq * a.kv_heads, 1);
     const size_t cells = (size_t)a.q_rows * a.kv_heads * a.group;
-    const bool small = rows <= kFewRows || rows * max_k <= (dtype == E2EGREC_F32 ? 256 : (backward ? 800 : 2048));
+    const bool small = rows <= (backward ? 4 : 2) || rows * max_k <= (dtype == E2EGREC_F32 ? 256 : 800);
     // (without rows on one side there is nothing to form a product of)
     p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
     if (p.path == Path::tc) {
@@ -249,7 +248,7 @@ extern "C" int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e
     bool ok = true;
     if (plan.path == Path::tc) ok = tc_attention_forward(a, plan.q_tiles, plan.splits, plan.one_tile, part_o, part_ml, st);
     else if (plan.path == Path::simt) ok = simt_attention_forward(a, plan.simt, part_o, part_ml, st);
-    else few_attention_forward(a, plan.few, Q->dtype, part_o, part_ml, st);
+    else ok = few_attention_forward(a, plan.few, Q->dtype, part_o, part_ml, st);
     if (!ok) return launch_refused("cross_attention_forward");
     if (plan.splits > 1) {
         note_launch();
@@ -306,7 +305,7 @@ extern "C" int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, con
         ok = simt_attention_backward(a, plan.simt, part_dq, dots, st);
         if (ok && plan.splits > 1 && a.q_rows) join_dq(a, plan.splits, Q->dtype, part_dq, st);
     } else {
-        few_attention_backward(a, plan.few, Q->dtype, part_dq, dots, st);
+        ok = few_attention_backward(a, plan.few, Q->dtype, part_dq, dots, st);
     }
     if (!ok) return launch_refused("cross_attention_backward");
     return check_launch("cross_attention_backward");

@@ -6,7 +6,7 @@
 namespace e2egrec {
 
 constexpr int kMaxAttnDim = 256;
-constexpr int kMaxSplits = 64;               // stretches of the keys, at most
+constexpr int kMaxSplits = 256;              // stretches of the keys, at most
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // Rows (query i, head g of its group) of one key head count as the rows of one matrix: row i * group + g.
@@ -73,9 +73,9 @@ struct FewPlan {
     int64_t key_batches;                  // units of keys of the dK, dV kernel
 };
 FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool backward);
-void few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_o, float2 *part_ml, cudaStream_t st);
+bool few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_o, float2 *part_ml, cudaStream_t st);
 // part_dq: [splits x q_rows x heads x head_dim] where splits > 1; dots: [q_rows x heads] where !both
-void few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st);
+bool few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st);
 
 // dQ of stretches of the keys -> dQ, in order
 void join_dq(const AttnArgs &a, int splits, int32_t dtype, const float *part_dq, cudaStream_t st);

@@ -2,19 +2,23 @@
 // tokens.  Every key and value is used a handful of times, so these kernels stream them: fp32 FMA, 16 bytes per lane and load.
 //
 // `lanes` neighbouring lanes share a head's part of a key (16 bytes each), `heads` key heads lie side by side in a warp as they do in
-// memory, and the rest of the warp is further keys of the step; kUnroll steps are in flight.  Each lane group keeps its own running
-// maximum, sum and outputs over the keys it meets; groups, then the warps of a unit, then the stretches of a long list of keys are
+// memory, and the rest of the warp is further keys of the step; a turn is up to kUnroll steps.  Keys and values come through a ring of
+// kStages turns per warp in shared memory, filled by bulk copies (one per turn where the rows follow one another, else one per row):
+// what is under way costs no registers, and a turn's latency passes beside the turns before it (with loads into registers, four
+// steps of them, two rows to 4096 x 100 keys of 4 heads of 64 took 186 us, this way 74).  Each lane group keeps its own running maximum, sum and outputs over the keys it meets; groups, then the warps of a unit, then the stretches of a long list of keys are
 // joined at the end, in a fixed order.  A unit is up to R rows of one sequence and of each of its key heads.
 #include <algorithm>
 
 #include "attention.cuh"
+#include "tcgen05.cuh"
 
 namespace e2egrec {
 namespace {
 
-constexpr int kFewThreads = 256, kFewWarps = kFewThreads / 32;
-constexpr int kUnroll = 4;                           // steps of keys in flight per warp (1 where a step holds all keys of a sequence, 2 for
-                                                     // more than two rows unless four steps hold all keys)
+constexpr int kFewThreads = 128, kFewWarps = kFewThreads / 32;
+constexpr int kUnroll = 4;                           // steps of a turn (fewer where they hold all keys of a sequence, for many keys a
+                                                     // step, and 2 for more than two rows, whose registers four would take)
+constexpr int kStages = 3;
 
 template <typename T, int CPL> struct Piece {        // a lane's part of a head's row
     static constexpr int E = Chunk<T>::kElems * CPL;
@@ -31,6 +35,16 @@ template <typename T, int CPL> struct Piece {        // a lane's part of a head'
         for (int c = 0; c < CPL; ++c)
             if (at + c * lanes < chunks) raw[c] = __ldg(reinterpret_cast<const uint4 *>(row) + at + c * lanes);
             else raw[c] = make_uint4(0, 0, 0, 0);
+    }
+    // the same from shared memory
+    __device__ inline void load_shared(uint32_t row, int at, int lanes, int chunks)
+    {
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) {
+            raw[c] = make_uint4(0, 0, 0, 0);
+            if (at + c * lanes < chunks)
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(raw[c].x), "=r"(raw[c].y), "=r"(raw[c].z), "=r"(raw[c].w) : "r"(row + (at + c * lanes) * 16));
+        }
     }
     __device__ inline void widen(float (&v)[E]) const
     {
@@ -73,6 +87,126 @@ template <int E> __device__ inline void axpy(float (&y)[E], float s, const float
     }
 }
 
+struct FewShape {
+    int lanes, chunks;                               // lanes per head of a key (a power of two), 16-byte chunks of a head
+    int heads, head_groups;                          // key heads side by side in a warp (a power of two), groups of them
+    int warps;                                       // warps per unit: a power of two, at most kFewWarps
+    int batches;                                     // batches of R rows per sequence and key head
+    int splits;                                      // stretches of the keys
+    uint32_t units;
+    int slice, packed;                               // bytes of a row's heads of a warp; whether those of consecutive rows are one stretch
+};
+
+// A warp's ring: turns of `keys` rows of K and of V (its heads' slice of them), visible rows as bits beside them.  Turn t of the warp is
+// the rows (t * warps + its number) * keys and on; a hidden row may come along or not, its bit keeps it out.
+struct Ring {
+    const char *k, *v;                               // row kb, slice of the heads
+    const uint8_t *mask;                             // of row kb
+    int64_t ldk, ldv;                                // bytes
+    uint32_t base, half;                             // shared memory; bytes of a turn's keys
+    uint64_t *bar;
+    uint32_t *seen;
+    int keys, stride, first, n, turns, slice, own, packed, lane;      // stride, first: rows; own: bytes of a row that are copied
+    uint32_t used;                                   // turns that went through the ring so far: stage and phase
+    uint32_t next_mask;
+    bool ok;
+    __device__ inline uint32_t mask_of(int t) const
+    {
+        const int j = first + t * stride + lane;
+        uint32_t m = 1;
+        if (mask && lane < keys && j < n) asm volatile("ld.global.u8 %0, [%1];" : "=r"(m) : "l"(mask + j) : "memory");
+        return m;
+    }
+    // turn t into the stage of use `use`
+    __device__ inline void fill(int t, uint32_t use)
+    {
+        const int j0 = first + t * stride, count = min(keys, n - j0);
+        const uint32_t word = __ballot_sync(0xFFFFFFFFu, lane < count && next_mask != 0);
+        if (t + 1 < turns) next_mask = mask_of(t + 1);
+        const uint32_t s = use % kStages, dst = base + s * 2 * half, b = smem_u32(bar + s);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // the stage was read through the generic proxy
+        if (lane == 0) {
+            seen[s] = word;
+            mbar_expect_tx(bar + s, packed ? 2u * count * slice : 2u * __popc(word) * own);
+            if (packed) {
+                copy(dst, k + j0 * ldk, (uint32_t)(count * slice), b);
+                copy(dst + half, v + j0 * ldv, (uint32_t)(count * slice), b);
+            }
+        }
+        __syncwarp();
+        if (!packed && (word >> lane & 1u)) {
+            copy(dst + lane * slice, k + (j0 + lane) * ldk, own, b);
+            copy(dst + half + lane * slice, v + (j0 + lane) * ldv, own, b);
+        }
+    }
+    static __device__ inline void copy(uint32_t dst, const char *src, uint32_t bytes, uint32_t b)
+    {
+        asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(b) : "memory");
+    }
+    __device__ inline void start()
+    {
+        next_mask = turns > 0 ? mask_of(0) : 0;
+        for (int t = 0; t < turns && t < kStages; ++t) fill(t, used + t);
+    }
+    // waits for turn t; its stage's address, and which of its rows are seen
+    __device__ inline uint32_t wait(uint32_t &word, int t, volatile int *abort_flag)
+    {
+        const uint32_t use = used + t;
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar + use % kStages, use / kStages & 1u, abort_flag));
+        word = ok ? seen[use % kStages] : 0u;
+        return base + use % kStages * 2 * half;
+    }
+    // giving up after turn t: the copies behind it land before the shared memory is released
+    __device__ inline void land(int t)
+    {
+        int never = 0;
+        for (int i = t + 1; i < turns && i < t + kStages; ++i) mbar_wait(bar + (used + i) % kStages, (used + i) / kStages & 1u, &never);
+    }
+    // turn t has been read by the whole warp
+    __device__ inline void done(int t)
+    {
+        __syncwarp();
+        if (t + kStages < turns && ok) fill(t + kStages, used + t + kStages);
+    }
+};
+
+template <int U> __device__ inline Ring ring_of(const AttnArgs &a, const FewShape &f, int es, uint8_t *smem, uint64_t *bars, uint32_t *seen, int warp, int lane)
+{
+    Ring r;
+    r.keys = U * (32 / (f.lanes * f.heads));
+    r.slice = f.slice;
+    r.half = (uint32_t)(r.keys * f.slice);
+    r.base = smem_u32(smem) + (uint32_t)warp * kStages * 2 * r.half;
+    r.bar = bars + warp * kStages;
+    r.seen = seen + warp * kStages;
+    r.ldk = a.ldk * es;
+    r.ldv = a.ldv * es;
+    r.packed = f.packed;
+    r.lane = lane;
+    r.used = 0;
+    r.ok = true;
+    if (lane == 0) {
+        for (int s = 0; s < kStages; ++s) mbar_init(r.bar + s, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncwarp();
+    return r;
+}
+// the keys kb .. ke of a unit, head group hg; wu: the warp's number in the unit
+__device__ inline void ring_keys(Ring &r, const AttnArgs &a, const FewShape &f, int es, int64_t kb, int64_t ke, int hg, int wu)
+{
+    const int64_t col = (int64_t)hg * f.slice;
+    r.k = static_cast<const char *>(a.k) + kb * r.ldk + col;
+    r.v = static_cast<const char *>(a.v) + kb * r.ldv + col;
+    r.mask = a.mask ? a.mask + kb : nullptr;
+    r.n = (int)(ke - kb);
+    r.stride = f.warps * r.keys;
+    r.first = wu * r.keys;
+    r.turns = r.n > r.first ? (r.n - r.first + r.stride - 1) / r.stride : 0;
+    r.own = min(f.heads, a.kv_heads - hg * f.heads) * a.head_dim * es;
+}
+
 // sums over the lanes of a key, N values at once
 template <int N> __device__ inline void key_sums(float (&v)[N], int lanes)
 {
@@ -81,14 +215,6 @@ template <int N> __device__ inline void key_sums(float (&v)[N], int lanes)
         for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
 }
 
-struct FewShape {
-    int lanes, chunks;                               // lanes per head of a key (a power of two), 16-byte chunks of a head
-    int heads, head_groups;                          // key heads side by side in a warp (a power of two), groups of them
-    int warps;                                       // warps per unit: a power of two, at most kFewWarps
-    int batches;                                     // batches of R rows per sequence and key head
-    int splits;                                      // stretches of the keys
-    uint32_t units;
-};
 
 __device__ inline float exp2_fast(float x)
 {
@@ -100,7 +226,7 @@ __device__ inline float exp2_fast(float x)
 struct Unit {
     SeqRange rg;
     int64_t kb, ke, rows;
-    int z, h, first;                                 // h: the lane's key head
+    int z, h, hg, first;                             // h: the lane's key head, hg: the warp's group of them
     bool any, on;                                    // there is such a unit; there is such a head
 };
 __device__ inline Unit few_unit(const AttnArgs &a, const FewShape &f, uint32_t u)            // fewer than 2^31 units: few_plan
@@ -117,6 +243,7 @@ __device__ inline Unit few_unit(const AttnArgs &a, const FewShape &f, uint32_t u
         u /= (uint32_t)f.batches;
     }
     const uint32_t s = u / (uint32_t)f.head_groups, hg = u - s * (uint32_t)f.head_groups;
+    x.hg = (int)hg;
     x.h = (int)(hg * f.heads + (threadIdx.x & 31) / f.lanes % f.heads);
     x.on = x.any && x.h < a.kv_heads;
     if (!x.any) {
@@ -158,10 +285,14 @@ struct RowWalk {
 
 // kb .. ke in turns of warps * kUnroll * (32 / lanes) keys
 template <typename T, int R, int U, int CPL>
-__global__ void __launch_bounds__(kFewThreads, CPL == 2 ? 1 : (R > 2 ? 2 : 3))
+__global__ void __launch_bounds__(kFewThreads, CPL == 2 ? 2 : (R > 2 ? 3 : 4))
 attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
 {
     constexpr int E = Piece<T, CPL>::E;
+    extern __shared__ __align__(16) uint8_t ring_smem[];
+    __shared__ uint64_t bars[kFewWarps * kStages];
+    __shared__ uint32_t seen_words[kFewWarps * kStages];
+    __shared__ int abort_flag;
     __shared__ float2 join_ml[kFewWarps][R][32];
     __shared__ float join_o[kFewWarps][E * 32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -169,12 +300,17 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     const Unit x = few_unit(a, f, blockIdx.x * (uint32_t)(kFewWarps / f.warps) + warp / f.warps);
     const int wide = f.lanes * f.heads, grp = lane / wide, at = lane & (f.lanes - 1), kpw = 32 / wide;
     const int heads = a.kv_heads * a.group;
-    const int64_t koff = x.h * (int64_t)a.head_dim;
     const float c1 = a.scale * kLog2e;
+    if (threadIdx.x == 0) abort_flag = 0;
+    Ring ring = ring_of<U>(a, f, sizeof(T), ring_smem, bars, seen_words, warp, lane);
+    ring_keys(ring, a, f, sizeof(T), x.kb, x.ke, x.hg, wu);
+    const uint32_t mine = (uint32_t)(lane / f.lanes % f.heads * a.head_dim * (int)sizeof(T));       // the lane's head in a slice
+    __syncthreads();
     for (int64_t n = 0;; ++n) {
         const int64_t r0 = (x.first + n * f.batches) * R;
         const bool live = x.any && r0 < x.rows;
         if (f.warps == 1 ? !live : !__syncthreads_or((int)live)) break;      // barriers inside: all warps of the block go on, or none
+        if (live) ring.start();
         float q[R][E], o[R][E], m[R], l[R];
         RowWalk in(a, x, r0);
 #pragma unroll
@@ -191,26 +327,24 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             m[r] = -INFINITY;
             l[r] = 0.f;
         }
-        const int64_t step = (int64_t)f.warps * U * kpw;
-        for (int64_t j0 = x.kb + (int64_t)wu * U * kpw; live && j0 < x.ke; j0 += step) {
-            Piece<T, CPL> k[U], v[U];
+        for (int t = 0; live && t < ring.turns && ring.ok; ++t) {
+            uint32_t word;
+            const uint32_t at_k = ring.wait(word, t, &abort_flag) + grp * f.slice + mine, at_v = at_k + ring.half;
+            if (!ring.ok) {
+                ring.land(t);
+                break;
+            }
             bool seen[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t j = j0 + u * kpw + grp;
-                seen[u] = x.on && j < x.ke && (!a.mask || a.mask[j]);
-                k[u].zero();
-                v[u].zero();
-                if (seen[u]) {
-                    k[u].load(static_cast<const T *>(a.k) + j * a.ldk + koff, at, f.lanes, f.chunks);
-                    v[u].load(static_cast<const T *>(a.v) + j * a.ldv + koff, at, f.lanes, f.chunks);
-                }
-            }
+            for (int u = 0; u < U; ++u) seen[u] = x.on && (word >> (u * kpw + grp) & 1u);
             float s[R * U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                Piece<T, CPL> k;
                 float w[E];
-                k[u].widen(w);
+                k.zero();
+                if (seen[u]) k.load_shared(at_k + u * kpw * f.slice, at, f.lanes, f.chunks);
+                k.widen(w);
 #pragma unroll
                 for (int r = 0; r < R; ++r) s[r * U + u] = dot<E>(q[r], w);
             }
@@ -236,12 +370,17 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                Piece<T, CPL> v;
                 float w[E];
-                v[u].widen(w);
+                v.zero();
+                if (seen[u]) v.load_shared(at_v + u * kpw * f.slice, at, f.lanes, f.chunks);
+                v.widen(w);
 #pragma unroll
                 for (int r = 0; r < R; ++r) axpy<E>(o[r], s[r * U + u], w);
             }
+            ring.done(t);
         }
+        if (live) ring.used += ring.turns;
         // lane groups of the warp
         for (int d = wide; d < 32; d <<= 1)
 #pragma unroll
@@ -307,6 +446,7 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 }
         if (f.warps > 1) __syncthreads();
     }
+    if (!ring.ok && lane == 0 && a.status) atomicOr(reinterpret_cast<unsigned *>(a.status), E2EGREC_DEV_TIMEOUT);
 }
 
 // dK and dV of kKeys keys per lane group (j0 and on), over all rows of the sequence.  dots: D of every row, or null where it is to be
@@ -395,10 +535,14 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
 // Where all keys are in one turn of the warp, D = sum_j p_j dP_j is formed from what the registers hold instead of the stored
 // outputs: with a handful of keys dP - D cancels, and the rounding of 16-bit outputs showed (dQ of three keys 3.1e-3 off, 2.0e-3 so).
 template <typename T, int R, int U, int CPL, bool kBoth>
-__global__ void __launch_bounds__(kFewThreads)
+__global__ void __launch_bounds__(kFewThreads, CPL == 2 || R > 2 ? 2 : (R == 1 ? 4 : 3))
 attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_dq, float *__restrict__ dots)
 {
     constexpr int E = Piece<T, CPL>::E;
+    extern __shared__ __align__(16) uint8_t ring_smem[];
+    __shared__ uint64_t bars[kFewWarps * kStages];
+    __shared__ uint32_t seen_words[kFewWarps * kStages];
+    __shared__ int abort_flag;
     __shared__ float join[kFewWarps][E * 32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wu = warp & (f.warps - 1);
@@ -408,13 +552,18 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     const int64_t koff = x.h * (int64_t)a.head_dim;
     const float c1 = a.scale * kLog2e;
     const bool whole = kBoth && x.rows <= R;
+    if (threadIdx.x == 0) abort_flag = 0;
+    Ring ring = ring_of<U>(a, f, sizeof(T), ring_smem, bars, seen_words, warp, lane);
+    ring_keys(ring, a, f, sizeof(T), x.kb, x.ke, x.hg, wu);
+    const uint32_t mine = (uint32_t)(lane / f.lanes % f.heads * a.head_dim * (int)sizeof(T));       // the lane's head in a slice
+    __syncthreads();
     for (int64_t n = 0;; ++n) {
         const int64_t r0 = (x.first + n * f.batches) * R;
         // with kBoth the keys' gradients are written even where there is no row at all
         const bool live = x.any && (r0 < x.rows || (kBoth && n == 0));
         if (f.warps == 1 ? !live : !__syncthreads_or((int)live)) break;
+        if (live) ring.start();
         float q[R][E], g[R][E], dq[R][E], lse[R], d[R];
-        const int64_t step = (int64_t)f.warps * U * kpw;
         const bool one_turn = f.warps == 1 && f.splits == 1 && x.ke - x.kb <= U * kpw;
         RowWalk in(a, x, r0);
 #pragma unroll
@@ -449,26 +598,29 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             for (int e = 0; e < E; ++e) dq[r][e] = 0.f;
         }
         key_sums<R>(d, f.lanes);
-        for (int64_t j0 = x.kb + (int64_t)wu * U * kpw; live && j0 < x.ke; j0 += step) {
-            Piece<T, CPL> k[U], v[U];
+        for (int t = 0; live && t < ring.turns && ring.ok; ++t) {
+            uint32_t word;
+            const uint32_t at_k = ring.wait(word, t, &abort_flag) + grp * f.slice + mine, at_v = at_k + ring.half;
+            if (!ring.ok) {
+                ring.land(t);
+                break;
+            }
             bool seen[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t j = j0 + u * kpw + grp;
-                seen[u] = x.on && j < x.ke && (!a.mask || a.mask[j]);
-                k[u].zero();
-                v[u].zero();
-                if (seen[u]) {
-                    k[u].load(static_cast<const T *>(a.k) + j * a.ldk + koff, at, f.lanes, f.chunks);
-                    v[u].load(static_cast<const T *>(a.v) + j * a.ldv + koff, at, f.lanes, f.chunks);
-                }
-            }
+            for (int u = 0; u < U; ++u) seen[u] = x.on && (word >> (u * kpw + grp) & 1u);
             float s[2 * R * U];                                                     // scores, then p; dP, then dS
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                Piece<T, CPL> k, v;
                 float w[E], y[E];
-                k[u].widen(w);
-                v[u].widen(y);
+                k.zero();
+                v.zero();
+                if (seen[u]) {
+                    k.load_shared(at_k + u * kpw * f.slice, at, f.lanes, f.chunks);
+                    v.load_shared(at_v + u * kpw * f.slice, at, f.lanes, f.chunks);
+                }
+                k.widen(w);
+                v.widen(y);
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     s[r * U + u] = dot<E>(q[r], w);
@@ -492,11 +644,14 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
+                Piece<T, CPL> k;
                 float w[E];
-                k[u].widen(w);
+                k.zero();
+                if (seen[u]) k.load_shared(at_k + u * kpw * f.slice, at, f.lanes, f.chunks);
+                k.widen(w);
 #pragma unroll
                 for (int r = 0; r < R; ++r) axpy<E>(dq[r], s[(R + r) * U + u], w);
-                const int64_t j = j0 + u * kpw + grp;
+                const int64_t j = x.kb + ring.first + t * ring.stride + u * kpw + grp;
                 if (kBoth && whole && x.on && j < x.ke) {
                     float dk[E], dv[E];
 #pragma unroll
@@ -510,7 +665,9 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     store_piece<T, CPL>(static_cast<T *>(a.dv) + j * a.ldv2 + koff, at, f.lanes, f.chunks, dv, 1.f);
                 }
             }
+            ring.done(t);
         }
+        if (live) ring.used += ring.turns;
         for (int o = wide; o < 32; o <<= 1)
 #pragma unroll
             for (int r = 0; r < R; ++r)
@@ -548,6 +705,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         }
         if (f.warps > 1) __syncthreads();
     }
+    if (!ring.ok && lane == 0 && a.status) atomicOr(reinterpret_cast<unsigned *>(a.status), E2EGREC_DEV_TIMEOUT);
     if (kBoth && x.any && !whole)
         for (int64_t j0 = x.kb + (int64_t)wu * kKeys * kpw; j0 < x.ke; j0 += (int64_t)f.warps * kKeys * kpw)
             keys_gradients<T, CPL>(a, x.rg, x.h, x.on, j0, x.ke, grp, at, f, nullptr);
@@ -580,6 +738,8 @@ FewShape few_shape(const AttnArgs &a, int es)
     f.heads = 1;
     while (f.heads * 2 <= a.kv_heads && f.heads * 2 * f.lanes <= 32) f.heads *= 2;
     f.head_groups = (a.kv_heads + f.heads - 1) / f.heads;
+    f.slice = f.heads * a.head_dim * es;
+    f.packed = f.head_groups == 1 && f.heads == a.kv_heads && a.ldk * es == f.slice && a.ldv * es == f.slice;
     f.warps = f.batches = f.splits = 1;
     return f;
 }
@@ -590,51 +750,80 @@ unsigned few_grid(const AttnArgs &a, FewShape &f)
     return (unsigned)ceil_div(f.units, kFewWarps / f.warps);
 }
 
-template <typename T, int R, int U>
-void launch_fwd(const AttnArgs &a, FewShape f, float *part_o, float2 *part_ml, cudaStream_t st)
+template <int U> size_t few_smem(const FewShape &f) { return (size_t)kFewWarps * kStages * 2 * U * (32 / (f.lanes * f.heads)) * f.slice; }
+
+constexpr int kMaxDevices = 64;
+template <typename Kernel> bool allow_smem(Kernel kernel, bool (&done)[kMaxDevices])
 {
-    note_launch();
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return false;
+    if (done[dev]) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != cudaSuccess) return false;
+    done[dev] = true;
+    return true;
+}
+
+template <typename T, int R, int U>
+bool launch_fwd(const AttnArgs &a, FewShape f, float *part_o, float2 *part_ml, cudaStream_t st)
+{
+    static bool done[2][kMaxDevices] = {};
     const unsigned grid = few_grid(a, f);
-    if (f.chunks <= 32) attn_few_fwd_kernel<T, R, U, 1><<<grid, kFewThreads, 0, st>>>(a, f, part_o, part_ml);
-    else if constexpr (sizeof(T) == 4) attn_few_fwd_kernel<T, R, U, 2><<<grid, kFewThreads, 0, st>>>(a, f, part_o, part_ml);
+    note_launch();
+    if (f.chunks <= 32) {
+        if (!allow_smem(attn_few_fwd_kernel<T, R, U, 1>, done[0])) return false;
+        attn_few_fwd_kernel<T, R, U, 1><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_o, part_ml);
+    } else if constexpr (sizeof(T) == 4) {
+        if (!allow_smem(attn_few_fwd_kernel<T, R, U, 2>, done[1])) return false;
+        attn_few_fwd_kernel<T, R, U, 2><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_o, part_ml);
+    }
+    return true;
 }
 
 template <typename T, int R, int U, bool kBoth>
-void launch_bwd(const AttnArgs &a, FewShape f, float *part_dq, float *dots, cudaStream_t st)
+bool launch_bwd(const AttnArgs &a, FewShape f, float *part_dq, float *dots, cudaStream_t st)
 {
-    note_launch();
+    static bool done[2][kMaxDevices] = {};
     const unsigned grid = few_grid(a, f);
-    if (f.chunks <= 32) attn_few_bwd_kernel<T, R, U, 1, kBoth><<<grid, kFewThreads, 0, st>>>(a, f, part_dq, dots);
-    else if constexpr (sizeof(T) == 4) attn_few_bwd_kernel<T, R, U, 2, kBoth><<<grid, kFewThreads, 0, st>>>(a, f, part_dq, dots);
+    note_launch();
+    if (f.chunks <= 32) {
+        if (!allow_smem(attn_few_bwd_kernel<T, R, U, 1, kBoth>, done[0])) return false;
+        attn_few_bwd_kernel<T, R, U, 1, kBoth><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_dq, dots);
+    } else if constexpr (sizeof(T) == 4) {
+        if (!allow_smem(attn_few_bwd_kernel<T, R, U, 2, kBoth>, done[1])) return false;
+        attn_few_bwd_kernel<T, R, U, 2, kBoth><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_dq, dots);
+    }
+    return true;
 }
 
-template <typename T, int R> void forward_rows(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
+template <typename T, int R> bool forward_rows(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    if (p.steps == 1) launch_fwd<T, R, 1>(a, f, part_o, part_ml, st);
-    else if (p.steps == 2) launch_fwd<T, R, 2>(a, f, part_o, part_ml, st);
-    else launch_fwd<T, R, kUnroll>(a, f, part_o, part_ml, st);
+    if (p.steps == 1) return launch_fwd<T, R, 1>(a, f, part_o, part_ml, st);
+    if (p.steps == 2) return launch_fwd<T, R, 2>(a, f, part_o, part_ml, st);
+    return launch_fwd<T, R, kUnroll>(a, f, part_o, part_ml, st);
 }
 
-template <typename T> void forward_of(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
+template <typename T> bool forward_of(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    if (p.rows == 1) forward_rows<T, 1>(a, p, f, part_o, part_ml, st);
-    else if (p.rows == 2) forward_rows<T, 2>(a, p, f, part_o, part_ml, st);
-    else forward_rows<T, 4>(a, p, f, part_o, part_ml, st);
+    if (p.rows == 1) return forward_rows<T, 1>(a, p, f, part_o, part_ml, st);
+    if (p.rows == 2) return forward_rows<T, 2>(a, p, f, part_o, part_ml, st);
+    return forward_rows<T, 4>(a, p, f, part_o, part_ml, st);
 }
 
-template <typename T, int R, bool kBoth> void backward_rows(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_dq, float *dots, cudaStream_t st)
+template <typename T, int R, bool kBoth> bool backward_rows(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_dq, float *dots, cudaStream_t st)
 {
-    if (p.steps == 1) launch_bwd<T, R, 1, kBoth>(a, f, part_dq, dots, st);
-    else if (p.steps == 2) launch_bwd<T, R, 2, kBoth>(a, f, part_dq, dots, st);
-    else launch_bwd<T, R, kUnroll, kBoth>(a, f, part_dq, dots, st);
+    if (p.steps == 1) return launch_bwd<T, R, 1, kBoth>(a, f, part_dq, dots, st);
+    if (p.steps == 2) return launch_bwd<T, R, 2, kBoth>(a, f, part_dq, dots, st);
+    return launch_bwd<T, R, kUnroll, kBoth>(a, f, part_dq, dots, st);
 }
 
-template <typename T> void backward_of(const AttnArgs &a, const FewPlan &p, FewShape f, float *part_dq, float *dots, cudaStream_t st)
+template <typename T> bool backward_of(const AttnArgs &a, const FewPlan &p, FewShape f, float *part_dq, float *dots, cudaStream_t st)
 {
-    if (!p.both) backward_rows<T, 4, false>(a, p, f, part_dq, dots, st);
-    else if (p.rows == 1) backward_rows<T, 1, true>(a, p, f, part_dq, dots, st);
-    else if (p.rows == 2) backward_rows<T, 2, true>(a, p, f, part_dq, dots, st);
-    else backward_rows<T, 4, true>(a, p, f, part_dq, dots, st);
+    bool ok;
+    if (!p.both) ok = backward_rows<T, 4, false>(a, p, f, part_dq, dots, st);
+    else if (p.rows == 1) ok = backward_rows<T, 1, true>(a, p, f, part_dq, dots, st);
+    else if (p.rows == 2) ok = backward_rows<T, 2, true>(a, p, f, part_dq, dots, st);
+    else ok = backward_rows<T, 4, true>(a, p, f, part_dq, dots, st);
+    if (!ok) return false;
     if (f.splits > 1 && a.q_rows) join_dq(a, f.splits, sizeof(T) == 4 ? E2EGREC_F32 : E2EGREC_BF16, part_dq, st);
     if (!p.both && a.k_rows) {
         note_launch();
@@ -645,6 +834,7 @@ template <typename T> void backward_of(const AttnArgs &a, const FewPlan &p, FewS
         if (f.chunks <= 32) attn_few_dkv_kernel<T, 1><<<grid, kFewThreads, 0, st>>>(a, f, dots);
         else if constexpr (sizeof(T) == 4) attn_few_dkv_kernel<T, 2><<<grid, kFewThreads, 0, st>>>(a, f, dots);
     }
+    return true;
 }
 
 }  // namespace
@@ -658,7 +848,8 @@ FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool b
     const int64_t step = 32 / (f.lanes * f.heads);
     p.rows = rows <= 1 ? 1 : (rows <= 2 ? 2 : 4);
     p.both = backward && rows <= p.rows;
-    p.steps = max_k <= step ? 1 : (p.rows > 2 && max_k > kUnroll * step ? 2 : kUnroll);
+    p.steps = max_k <= step ? 1 : (max_k <= 2 * step || (p.rows > 2 && max_k > kUnroll * step) ? 2 : kUnroll);
+    while (p.steps * step > 32) p.steps /= 2;        // a turn's rows are the bits of a word
     const int64_t turn = step * p.steps;
     p.batches = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, p.rows), most));
     const int64_t want = std::max<int64_t>(1, std::min(ceil_div(148 * 24, units0 * p.batches), ceil_div(max_k, turn)));
@@ -678,16 +869,16 @@ static FewShape planned(const AttnArgs &a, const FewPlan &p, int32_t dtype)
     return f;
 }
 
-void few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_o, float2 *part_ml, cudaStream_t st)
+bool few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    if (dtype == E2EGREC_F32) forward_of<float>(a, p, planned(a, p, dtype), part_o, part_ml, st);
-    else forward_of<__nv_bfloat16>(a, p, planned(a, p, dtype), part_o, part_ml, st);
+    return dtype == E2EGREC_F32 ? forward_of<float>(a, p, planned(a, p, dtype), part_o, part_ml, st)
+                                : forward_of<__nv_bfloat16>(a, p, planned(a, p, dtype), part_o, part_ml, st);
 }
 
-void few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st)
+bool few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st)
 {
-    if (dtype == E2EGREC_F32) backward_of<float>(a, p, planned(a, p, dtype), part_dq, dots, st);
-    else backward_of<__nv_bfloat16>(a, p, planned(a, p, dtype), part_dq, dots, st);
+    return dtype == E2EGREC_F32 ? backward_of<float>(a, p, planned(a, p, dtype), part_dq, dots, st)
+                                : backward_of<__nv_bfloat16>(a, p, planned(a, p, dtype), part_dq, dots, st);
 }
 
 }  // namespace e2egrec
