@@ -4,11 +4,14 @@
 //   over the pairs (a, b) = (i, i + rot / 2) or (2 i, 2 i + 1), i < rot / 2; elements behind rot are passed through as g.
 // Gradient, with u = the inverse rotation of dy:  dw = sum u n,  dx = (u w - n mean(u w n)) / sqrt(mean(x^2) + eps).
 //
-// What bounds these kernels is memory: a row is read once and written once (the gradient reads x and dy).  A thread takes one
-// unit of 16 bytes and its partner 16 bytes (the other elements of the pairs) of one row and goes over the heads of the row, so
-// that the angles of its pairs are formed once per row; the lanes of one head are neighbours, and a head's sum of squares is a
-// handful of shuffles.  Angles: pos * f / 2 pi in 64 bits, whole turns taken off, then sine and cosine in 32: exact to 2^-31 of
-// a turn for every 32-bit position, where a product in 32 bits has no digit left beyond position 2^23.
+// What bounds these kernels is memory: a row is read once and written once (the gradient reads x and dy).  A thread takes one unit of
+// 16 bytes and its partner 16 bytes (the other elements of the pairs) of one row and goes over the heads of the row, so that the
+// angles of its pairs are formed once per row; the lanes of one head are neighbours, and a head's sum of squares is a handful of
+// shuffles.  (One thread per unit and head, whose accesses are whole lines, forms every angle once per head: 21 us instead of 15
+// for 65 536 rows of 4 heads of 64 bf16 values.)
+// Angles: a frequency becomes a 64-bit fraction of a turn, once per block and pair; its product with a 32-bit position modulo one turn
+// is two integer products, exact to 2^-32 of a turn wherever the position lies, where a product in 32-bit floating point has no digit
+// left beyond position 2^23.
 #include <algorithm>
 
 #include "common.cuh"
@@ -17,9 +20,10 @@ namespace e2egrec {
 namespace {
 
 constexpr int kRotThreads = 256;
-constexpr int kHeadUnroll = 4;            // heads of a row whose loads are in flight together
+constexpr int kHeadUnroll = 2;            // heads of a row whose loads are in flight together
 constexpr int kMaxHeadDim = 256;
-constexpr int kGradBlocks = 148 * 4;      // blocks (per operand) that sum up the gains' gradients: fixed, so that the order is
+constexpr int kGradUnroll = 1;            // the same in the gradient's kernel
+constexpr int kGradBlocks = 148 * 4;      // blocks that sum up the gains' gradients, at most
 
 // V values of a row as they lie in memory (16, 8, 4 or 2 bytes)
 template <int BYTES> struct RawOf;
@@ -31,18 +35,38 @@ template <typename T, int V> using Raw = typename RawOf<V * (int)sizeof(T)>::typ
 
 template <typename T, int V> __device__ inline void widen(const Raw<T, V> &r, float *v)
 {
-    T e[V];
-    memcpy(e, &r, sizeof(r));
+    if constexpr (sizeof(T) == 2 && V > 1) {         // two bf16 values of a word: a shift and a mask
+        uint32_t w[V / 2];
+        memcpy(w, &r, sizeof(r));
 #pragma unroll
-    for (int i = 0; i < V; ++i) v[i] = to_float<T>(e[i]);
+        for (int i = 0; i < V / 2; ++i) {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+    } else {
+        T e[V];
+        memcpy(e, &r, sizeof(r));
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = to_float<T>(e[i]);
+    }
 }
 template <typename T, int V> __device__ inline Raw<T, V> narrow(const float *v)
 {
-    T e[V];
-#pragma unroll
-    for (int i = 0; i < V; ++i) e[i] = from_float<T>(v[i]);
     Raw<T, V> r;
-    memcpy(&r, e, sizeof(r));
+    if constexpr (sizeof(T) == 2 && V > 1) {
+        uint32_t w[V / 2];
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+            memcpy(&w[i], &h, 4);
+        }
+        memcpy(&r, w, sizeof(r));
+    } else {
+        T e[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) e[i] = from_float<T>(v[i]);
+        memcpy(&r, e, sizeof(r));
+    }
     return r;
 }
 
@@ -54,7 +78,7 @@ struct Operand {
     int32_t heads;
     const float *w;
     const int32_t *pos;
-    float *dw;                            // partial sums of the gain's gradient, [kGradBlocks x head_dim], or null
+    float *dw;                            // partial sums of the gain's gradient, [blocks x head_dim], or null
 };
 
 struct RotArgs {
@@ -90,21 +114,40 @@ template <int V, bool kInter> struct Places {
     }
 };
 
+// The block's table of turns per position, 2^64 to a turn: high and low words
+__device__ inline void make_turns(const RotArgs &r, uint2 *turns)
+{
+    for (int f = threadIdx.x; f < r.half; f += kRotThreads) {
+        const double t = __ldg(r.freqs + f) * 0.15915494309189533577;
+        const unsigned long long n = __double2ull_rz((t - floor(t)) * 18446744073709551616.0);
+        turns[f] = make_uint2((uint32_t)(n >> 32), (uint32_t)n);
+    }
+    __syncthreads();
+}
+
 // scale * (cos, sin) of pair f at position p; (1, 0) for pairs that are not rotated.  With 16-bit results the hardware's sine and
-// cosine of the reduced angle are off by 2^-21, a 2^12th of the result's own rounding; 32-bit results take the library's.
-template <typename T> __device__ inline void angle(const RotArgs &r, int f, double p, float &c, float &s)
+// cosine of the angle to 2^-24 of a turn are off by 2^-20, a 2^11th of the result's own rounding.  For 32-bit results the angle is
+// taken to the nearest quarter turn, |x| <= pi / 4, and the Taylor series of sine and cosine broken off behind x^9 and x^8 (the next terms
+// are below 2^-28 and 2^-25); the quarter turns swap the two and set signs.
+template <typename T> __device__ inline void angle(const RotArgs &r, const uint2 *turns, int f, int p, float &c, float &s)
 {
     c = 1.f;
     s = 0.f;
     if (f >= r.half) return;
-    const double t = p * __ldg(r.freqs + f) * 0.15915494309189533577;
-    const float turn = (float)(t - rint(t));
+    const uint2 t = turns[f];
+    const uint32_t frac = t.x * (uint32_t)p + __umulhi(t.y, (uint32_t)p) - (p < 0 ? t.y : 0u);      // of 2^32, modulo a turn
     if (sizeof(T) == 2) {
-        const float a = turn * 6.28318530718f;
+        // 1.5 + the signed fraction of a turn, from the bits
+        const float a = (__uint_as_float(0x3F800000u | ((frac + 0x80000000u) >> 9)) - 1.5f) * 6.28318530718f;
         c = __cosf(a);
         s = __sinf(a);
     } else {
-        sincospif(2.f * turn, &s, &c);
+        const uint32_t quarter = (frac + 0x20000000u) >> 30;
+        const float x = (float)(int32_t)(frac - (quarter << 30)) * 1.46291807926715968105e-9f, x2 = x * x;      // 2 pi / 2^32
+        const float sx = fmaf(fmaf(fmaf(fmaf(1.f / 362880.f, x2, -1.f / 5040.f), x2, 1.f / 120.f), x2, -1.f / 6.f) * x2, x, x);
+        const float cx = fmaf(fmaf(fmaf(fmaf(1.f / 40320.f, x2, -1.f / 720.f), x2, 1.f / 24.f), x2, -0.5f), x2, 1.f);
+        s = __uint_as_float(__float_as_uint(quarter & 1u ? cx : sx) ^ ((quarter & 2u) << 30));
+        c = __uint_as_float(__float_as_uint(quarter & 1u ? sx : cx) ^ (((quarter + 1u) & 2u) << 30));
     }
     c *= r.scale;
     s *= r.scale * r.sign;
@@ -140,7 +183,7 @@ __device__ inline float lanes_sum(float v, int lanes)
 
 // Forward: rotation, with kNorm the norm before it.
 template <typename T, int V, bool kInter, bool kNorm>
-__global__ void __launch_bounds__(kRotThreads)
+__global__ void __launch_bounds__(kRotThreads, 3)
 rotary_kernel(const __grid_constant__ RotArgs r)
 {
     constexpr int E = Chunk<T>::kElems, NU = E / V;
@@ -151,7 +194,9 @@ rotary_kernel(const __grid_constant__ RotArgs r)
     const int lane = threadIdx.x & (r.lanes - 1);
     const int64_t row = (int64_t)(blockIdx.x - (second ? r.blocks0 : 0)) * (kRotThreads / r.lanes) + threadIdx.x / r.lanes;
     const bool live = row < op.rows;
-    const double p = !live ? 0. : (op.pos ? (double)__ldg(op.pos + row) : (double)row);
+    const int p = !live ? 0 : (op.pos ? __ldg(op.pos + row) : (int)row);
+    __shared__ uint2 turns[kMaxHeadDim / 2];
+    make_turns(r, turns);
 
     int pa[NU], pb[NU];
     float c[E], s[E], wa[E], wb[E];
@@ -162,7 +207,7 @@ rotary_kernel(const __grid_constant__ RotArgs r)
         pb[j] = live ? at.b : -1;
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            angle<T>(r, at.f + i, p, c[j * V + i], s[j * V + i]);
+            angle<T>(r, turns, at.f + i, p, c[j * V + i], s[j * V + i]);
             if (kNorm) {
                 wa[j * V + i] = op.w && at.a >= 0 ? __ldg(op.w + at.a + i) : 1.f;
                 wb[j * V + i] = op.w && at.b >= 0 ? __ldg(op.w + at.b + i) : 1.f;
@@ -212,15 +257,19 @@ rotary_kernel(const __grid_constant__ RotArgs r)
     }
 }
 
-// Gradient of the normed form.  A fixed number of blocks goes over the rows of each operand; a thread's share of the gains'
+// Gradient of the normed form.  The blocks of an operand go over its rows in rounds; a thread's share of the gains'
 // gradient stays in registers, the block adds its threads' up in a fixed order and leaves one row of partial sums.
 template <typename T, int V, bool kInter>
-__global__ void __launch_bounds__(kRotThreads)
+__global__ void __launch_bounds__(kRotThreads, 2)
 qk_norm_grad_kernel(const __grid_constant__ RotArgs r)
 {
     constexpr int E = Chunk<T>::kElems, NU = E / V;
     __shared__ float part[kRotThreads / 32][kMaxHeadDim];
-    const Operand &op = r.op[blockIdx.y];
+    __shared__ uint2 turns[kMaxHeadDim / 2];
+    make_turns(r, turns);
+    const bool second = (int)blockIdx.x >= r.blocks0;
+    const Operand &op = r.op[second];
+    const int block = (int)blockIdx.x - (second ? r.blocks0 : 0), blocks = second ? (int)gridDim.x - r.blocks0 : r.blocks0;
     const int lane = threadIdx.x & (r.lanes - 1), per_block = kRotThreads / r.lanes;
     int pa[NU], pb[NU], pf[NU];
     float wa[E], wb[E], ga[E], gb[E];
@@ -237,58 +286,74 @@ qk_norm_grad_kernel(const __grid_constant__ RotArgs r)
             ga[j * V + i] = gb[j * V + i] = 0.f;
         }
     }
-    const int64_t turns = ceil_div(ceil_div(op.rows, per_block), gridDim.x);
-    for (int64_t n = 0; n < turns; ++n) {
-        const int64_t row = (n * gridDim.x + blockIdx.x) * per_block + threadIdx.x / r.lanes;
+    const int64_t rounds = ceil_div(ceil_div(op.rows, per_block), blocks);
+    for (int64_t n = 0; n < rounds; ++n) {
+        const int64_t row = (n * blocks + block) * per_block + threadIdx.x / r.lanes;
         const bool live = row < op.rows;
-        const double p = !live ? 0. : (op.pos ? (double)__ldg(op.pos + row) : (double)row);
-        float c[E], s[E];
-#pragma unroll
-        for (int j = 0; j < NU; ++j)
-#pragma unroll
-            for (int i = 0; i < V; ++i) angle<T>(r, pf[j] + i, p, c[j * V + i], s[j * V + i]);
+        const int p = !live ? 0 : (op.pos ? __ldg(op.pos + row) : (int)row);
         const T *x = static_cast<const T *>(op.x) + row * op.ldx, *dy = static_cast<const T *>(op.dy) + row * op.ldd;
         T *dx = static_cast<T *>(op.y) + row * op.ldy;
-        for (int h = 0; h < op.heads; ++h) {
-            float a[E], b[E], da[E], db[E];
+        float c[E], s[E];
+        for (int h = 0; h < op.heads; h += kGradUnroll) {
+            Raw<T, V> r0[kGradUnroll][NU], r1[kGradUnroll][NU], r2[kGradUnroll][NU], r3[kGradUnroll][NU];
 #pragma unroll
-            for (int j = 0; j < NU; ++j) {
-                Raw<T, V> r0{}, r1{}, r2{}, r3{};
-                if (live && pa[j] >= 0) {
-                    r0 = *reinterpret_cast<const Raw<T, V> *>(x + (int64_t)h * r.head_dim + pa[j]);
-                    r2 = *reinterpret_cast<const Raw<T, V> *>(dy + (int64_t)h * r.head_dim + pa[j]);
+            for (int u = 0; u < kGradUnroll; ++u) {
+                const bool on = live && h + u < op.heads;
+                const int64_t off = (int64_t)(h + u) * r.head_dim;
+#pragma unroll
+                for (int j = 0; j < NU; ++j) {
+                    r0[u][j] = r1[u][j] = r2[u][j] = r3[u][j] = Raw<T, V>{};
+                    if (on && pa[j] >= 0) {
+                        r0[u][j] = *reinterpret_cast<const Raw<T, V> *>(x + off + pa[j]);
+                        r2[u][j] = *reinterpret_cast<const Raw<T, V> *>(dy + off + pa[j]);
+                    }
+                    if (on && pb[j] >= 0) {
+                        r1[u][j] = *reinterpret_cast<const Raw<T, V> *>(x + off + pb[j]);
+                        r3[u][j] = *reinterpret_cast<const Raw<T, V> *>(dy + off + pb[j]);
+                    }
                 }
-                if (live && pb[j] >= 0) {
-                    r1 = *reinterpret_cast<const Raw<T, V> *>(x + (int64_t)h * r.head_dim + pb[j]);
-                    r3 = *reinterpret_cast<const Raw<T, V> *>(dy + (int64_t)h * r.head_dim + pb[j]);
+            }
+            if (h == 0) {
+#pragma unroll
+                for (int j = 0; j < NU; ++j)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) angle<T>(r, turns, pf[j] + i, p, c[j * V + i], s[j * V + i]);
+            }
+#pragma unroll
+            for (int u = 0; u < kGradUnroll; ++u) {
+                if (h + u >= op.heads) break;
+                const int64_t off = (int64_t)(h + u) * r.head_dim;
+                float a[E], b[E], da[E], db[E];
+#pragma unroll
+                for (int j = 0; j < NU; ++j) {
+                    widen<T, V>(r0[u][j], a + j * V);
+                    widen<T, V>(r1[u][j], b + j * V);
+                    widen<T, V>(r2[u][j], da + j * V);
+                    widen<T, V>(r3[u][j], db + j * V);
+                    turn_unit<kInter, V>(da + j * V, db + j * V, c + j * V, s + j * V);
                 }
-                widen<T, V>(r0, a + j * V);
-                widen<T, V>(r1, b + j * V);
-                widen<T, V>(r2, da + j * V);
-                widen<T, V>(r3, db + j * V);
-                turn_unit<kInter, V>(da + j * V, db + j * V, c + j * V, s + j * V);
-            }
-            float q = 0.f, d = 0.f;
+                float q = 0.f, d = 0.f;
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                q += a[i] * a[i] + b[i] * b[i];
-                d += da[i] * wa[i] * a[i] + db[i] * wb[i] * b[i];
-            }
-            q = lanes_sum(q, r.lanes);
-            d = lanes_sum(d, r.lanes);
-            const float rs = rsqrtf(q / (float)r.head_dim + r.eps);
-            const float m = d * rs * rs * rs / (float)r.head_dim;
+                for (int i = 0; i < E; ++i) {
+                    q += a[i] * a[i] + b[i] * b[i];
+                    d += da[i] * wa[i] * a[i] + db[i] * wb[i] * b[i];
+                }
+                q = lanes_sum(q, r.lanes);
+                d = lanes_sum(d, r.lanes);
+                const float rs = rsqrtf(q / (float)r.head_dim + r.eps);
+                const float m = d * rs * rs * rs / (float)r.head_dim;
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                ga[i] += da[i] * a[i] * rs;
-                gb[i] += db[i] * b[i] * rs;
-                a[i] = da[i] * wa[i] * rs - a[i] * m;
-                b[i] = db[i] * wb[i] * rs - b[i] * m;
-            }
+                for (int i = 0; i < E; ++i) {
+                    ga[i] += da[i] * a[i] * rs;
+                    gb[i] += db[i] * b[i] * rs;
+                    a[i] = da[i] * wa[i] * rs - a[i] * m;
+                    b[i] = db[i] * wb[i] * rs - b[i] * m;
+                }
 #pragma unroll
-            for (int j = 0; j < NU; ++j) {
-                if (live && pa[j] >= 0) *reinterpret_cast<Raw<T, V> *>(dx + (int64_t)h * r.head_dim + pa[j]) = narrow<T, V>(a + j * V);
-                if (live && pb[j] >= 0) *reinterpret_cast<Raw<T, V> *>(dx + (int64_t)h * r.head_dim + pb[j]) = narrow<T, V>(b + j * V);
+                for (int j = 0; j < NU; ++j) {
+                    if (live && pa[j] >= 0) *reinterpret_cast<Raw<T, V> *>(dx + off + pa[j]) = narrow<T, V>(a + j * V);
+                    if (live && pb[j] >= 0) *reinterpret_cast<Raw<T, V> *>(dx + off + pb[j]) = narrow<T, V>(b + j * V);
+                }
             }
         }
     }
@@ -313,29 +378,32 @@ qk_norm_grad_kernel(const __grid_constant__ RotArgs r)
     for (int i = threadIdx.x; i < r.head_dim; i += kRotThreads) {
         float t = 0.f;
         for (int w = 0; w < kRotThreads / 32; ++w) t += part[w][i];
-        op.dw[(int64_t)blockIdx.x * r.head_dim + i] = t;
+        op.dw[(int64_t)block * r.head_dim + i] = t;
     }
 }
 
-// Partial sums of the blocks -> dw, element by element: 256 threads per 32 elements, eight stretches of blocks each
-__global__ void __launch_bounds__(kRotThreads)
-gain_grad_kernel(const float *__restrict__ part0, const float *__restrict__ part1, int blocks, int head_dim, float *__restrict__ dw0,
+// Partial sums of the blocks -> dw, in a fixed order: 32 stretches of blocks per element (with eight, 592 blocks took 10 us, 4 now)
+constexpr int kGainThreads = 1024;
+__global__ void __launch_bounds__(kGainThreads)
+gain_grad_kernel(const float *__restrict__ part0, const float *__restrict__ part1, int blocks0, int blocks1, int head_dim, float *__restrict__ dw0,
                  float *__restrict__ dw1)
 {
-    __shared__ float red[8][32];
+    __shared__ float red[32][33];
     const float *part = blockIdx.y ? part1 : part0;
     float *dw = blockIdx.y ? dw1 : dw0;
+    const int blocks = blockIdx.y ? blocks1 : blocks0;
     const int e = blockIdx.x * 32 + (threadIdx.x & 31), g = threadIdx.x >> 5;
     if (!dw) return;
     float t = 0.f;
-    if (e < head_dim)
-        for (int b = g; b < blocks; b += 8) t += part[(int64_t)b * head_dim + e];
-    red[g][threadIdx.x & 31] = t;
-    __syncthreads();
-    if (g == 0 && e < head_dim) {
-        for (int i = 1; i < 8; ++i) t += red[i][threadIdx.x];
-        dw[e] = t;
+    if (e < head_dim) {
+#pragma unroll 8
+        for (int b = g; b < blocks; b += 32) t += part[(int64_t)b * head_dim + e];
     }
+    red[threadIdx.x & 31][g] = t;
+    __syncthreads();
+    t = red[g][threadIdx.x & 31];                    // element g of this block, stretch = lane
+    t = lanes_sum(t, 32);
+    if ((threadIdx.x & 31) == 0 && (int)blockIdx.x * 32 + g < head_dim) dw[blockIdx.x * 32 + g] = t;
 }
 
 // frequencies of the pairs, in radians per position
@@ -547,7 +615,7 @@ extern "C" int32_t e2egrec_qk_norm_rotary_backward(const e2egrec_mat *dQn, const
     int32_t hd = 0;
     int32_t rc = check_qk(Q, K, n_heads, n_kv_heads, eps, freqs, rot_dim, scale, flags, &hd);
     if (rc != E2EGREC_OK && (ws || rc != E2EGREC_ERR_NULL)) return rc;
-    const size_t one = align_up((size_t)kGradBlocks * kMaxHeadDim * sizeof(float), 256), need = 2 * one;
+    const size_t one = align_up((size_t)(kGradBlocks + 1) * kMaxHeadDim * sizeof(float), 256), need = 2 * one;
     if (!ws) { *ws_bytes = need; return E2EGREC_OK; }
     if (*ws_bytes < need) { *ws_bytes = need; return E2EGREC_ERR_WORKSPACE; }
     if (reinterpret_cast<uintptr_t>(ws) % 256) return E2EGREC_ERR_ALIGN;
@@ -582,13 +650,18 @@ extern "C" int32_t e2egrec_qk_norm_rotary_backward(const e2egrec_mat *dQn, const
     const bool inter = flags & E2EGREC_ROTARY_INTERLEAVED, f32 = Q->dtype == E2EGREC_F32;
     set_lanes(r, f32 ? 4 : 2);
     const int v = stretch(f32 ? 4 : 2, r.half, inter);
-    const int blocks = (int)std::min<int64_t>(kGradBlocks, ceil_div(rows, kRotThreads / r.lanes));
-    const dim3 grid(blocks, K ? 2 : 1);
+    // the blocks are shared by the operands as their heads are, so that all of them end together
+    const int64_t per = kRotThreads / r.lanes, need0 = ceil_div(Q->rows, per), need1 = K ? ceil_div(K->rows, per) : 0;
+    const int64_t heads0 = Q->rows * n_heads, heads1 = K ? K->rows * n_kv_heads : 0, all = std::min<int64_t>(kGradBlocks, need0 + need1);
+    const int64_t b0 = need0 ? std::min(need0, std::max<int64_t>(1, all * heads0 / (heads0 + heads1))) : 0;
+    const int64_t b1 = need1 ? std::min(need1, std::max<int64_t>(1, all - b0)) : 0;
+    r.blocks0 = (int32_t)b0;
+    const dim3 grid((unsigned)(b0 + b1));
     if (f32) launch_grad<float>(r, v, inter, grid, st);
     else launch_grad<__nv_bfloat16>(r, v, inter, grid, st);
     if (dwq || dwk) {
         note_launch();
-        gain_grad_kernel<<<dim3((unsigned)ceil_div(hd, 32), K ? 2 : 1), kRotThreads, 0, st>>>(part0, part1, blocks, hd, dwq, dwk);
+        gain_grad_kernel<<<dim3((unsigned)ceil_div(hd, 32), K ? 2 : 1), kGainThreads, 0, st>>>(part0, part1, (int)b0, (int)b1, hd, dwq, dwk);
     }
     return check_launch("qk_norm_rotary_backward");
 }

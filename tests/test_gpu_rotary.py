@@ -21,8 +21,8 @@ def _held(got, want, bound, what):
 
 
 def _trig(dtype):
-    # sine and cosine: the hardware's of the reduced angle for 16-bit results (2^-20 with the reduction's rounding), the
-    # library's (2 units in the last place, 2^-22) for 32-bit ones; products and their sum add two roundings
+    # sine and cosine: the hardware's of the reduced angle for 16-bit results (2^-20 with the reduction's rounding), series of five
+    # terms in 32 bits for 32-bit ones (some four roundings of 2^-24 and 2^-25 of truncation); products and their sum add two roundings
     return 2.0 ** -20 if dtype == BF16 else 2.0 ** -21
 
 
