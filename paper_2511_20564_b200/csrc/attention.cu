@@ -143,7 +143,7 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     const int64_t max_q = s.max_q ? std::min(s.max_q, a.q_rows) : a.q_rows, max_k = s.max_k ? std::min(s.max_k, a.k_rows) : a.k_rows;
     const int64_t rows = max_q * a.group, units = std::max<int64_t>(a.n_seq * a.kv_heads, 1);
     const size_t cells = (size_t)a.q_rows * a.kv_heads * a.group;
-    const bool small = rows <= (backward ? 4 : 2) || rows * max_k <= (dtype == E2EGREC_F32 ? 256 : 800);
+    const bool small = rows <= (backward ? 4 : 2) || rows * max_k <= (dtype == E2EGREC_F32 ? 256 : backward ? 700 : 800);
     // (without rows on one side there is nothing to form a product of)
     p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
     if (p.path == Path::tc) {

@@ -855,7 +855,8 @@ FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool b
     const int64_t want = std::max<int64_t>(1, std::min(ceil_div(148 * 24, units0 * p.batches), ceil_div(max_k, turn)));
     p.warps = 1;
     while (p.warps < kFewWarps && p.warps < want) p.warps *= 2;
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want / p.warps, kMaxSplits, most / p.batches}));
+    // a stretch is worth its join where every warp has four turns of it
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want / p.warps, max_k / (turn * p.warps * 4), kMaxSplits, most / p.batches}));
     p.key_batches = std::max<int64_t>(1, std::min(ceil_div(max_k, step * kKeys), most));
     return p;
 }
