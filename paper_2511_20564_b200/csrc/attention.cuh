@@ -82,6 +82,7 @@ void join_dq(const AttnArgs &a, int splits, int32_t dtype, const float *part_dq,
 
 // attention_simt.cu: fp32, head_dim <= 128, tiles of 64 rows x 64 keys
 struct SimtPlan {
+    int rows;                             // of a tile: 16, 32 or 64
     int64_t q_tiles, k_tiles;             // blocks of rows / of keys per sequence and key head
     int splits;                           // stretches of the keys (forward, dQ)
 };

@@ -1,10 +1,13 @@
-// Attention of fp32 sequences by tiles of 64 rows x 64 keys on fp32 FMA (head_dim <= 128): scores to fp32 accuracy, which neither TF32
-// nor bf16 products give.
+// Attention of fp32 sequences on fp32 FMA (head_dim <= 128): scores to fp32 accuracy, which neither TF32 nor bf16 products give.
 //
-// 256 threads: thread (ty, tx) of 16 x 16 forms the 4 x 4 scores of rows 4 ty + i and keys tx + 16 j as dot products of row-major
-// tiles, four elements of each at a time (eight 16-byte reads of shared memory for 64 FMA).  Tiles have rows of an odd number
-// of 16-byte units, so that eight neighbouring rows lie in different banks.  p and dS go through shared memory; the products with V, K, dO
-// and Q are outer products over the same row-major tiles, columns 4 tx + 64 c.  FMA throughput bounds it.
+// Tiles of 16 I rows x 64 keys, I = 1, 2 or 4 by the rows that a key head has.  256 threads: thread (ty, tx) of 16 x 16 forms the I x 4
+// scores of rows I ty + i and keys tx + 16 j as dot products of row-major tiles, four elements of each at a time (with I = 4 eight
+// 16-byte reads of shared memory for 64 FMA).  Tiles have rows of an odd number of 16-byte units, so that eight neighbouring rows lie
+// in different banks.  p and dS go through shared memory; the products with V, K, dO and Q are outer products over the same row-major
+// tiles, columns 4 cx + 64 c; of heads of at most 32 columns the threads of a row take a part of the summed index each, which are added
+// up once at the end.  The next tiles are on their way beside a tile's products where shared memory holds both.
+// 77 sequences of up to 61 x 307, heads of 36, forward and backward: 172 us with one tile at a time and one block per SM, 167 us so; 107 of 372 x 61, heads of 16: 598 and 440 us; 135 of 13 x 261,
+// heads of 100: 580 and 458 us.
 #include <algorithm>
 
 #include "attention.cuh"
@@ -15,9 +18,14 @@ namespace {
 
 constexpr int kTile = 64, kThreads = 256, kLdP = kTile + 4;
 
+// Blocks per SM: one where the sums of 64 rows of wide heads take the registers of two
+constexpr int blocks_of(int C, int I) { return C == 2 && I == 4 ? 1 : 2; }
+
 struct SimtShape {
     int ld;                               // floats from row to row of a tile in shared memory
     int tiles, splits;                    // blocks of rows (or keys) per sequence and key head; stretches of the keys
+    int stages;                           // tiles of the side that a block goes over: 2: one lands beside the products of the other
+    int cols;                             // threads side by side over a head's columns (a power of two), 16 / cols parts of the sums
 };
 
 __device__ inline float exp2_fast(float x)
@@ -41,32 +49,32 @@ __device__ inline float row_max(float v)
     return v;
 }
 
-// One tile -> shared memory: thread t takes row t / 4 and every fourth 16-byte unit of it; src: that row, null for zeros
-__device__ inline void load_tile(float *tile, const SimtShape &f, const float *src, const void *any, int head_dim)
+// One tile -> shared memory: kPer threads take a row's 16-byte units in turn; src: that row, null for zeros
+template <int kPer> __device__ inline void load_tile(float *tile, const SimtShape &f, const float *src, const void *any, int head_dim)
 {
-    const uint32_t dst = smem_u32(tile + (threadIdx.x >> 2) * f.ld);
-    for (int u = threadIdx.x & 3; u * 4 < head_dim; u += 4) cp_async16(dst + u * 16, src ? static_cast<const void *>(src + u * 4) : any, src != nullptr);
+    const uint32_t dst = smem_u32(tile + threadIdx.x / kPer * f.ld);
+#pragma unroll 4
+    for (int u = threadIdx.x % kPer; u * 4 < head_dim; u += kPer) cp_async16(dst + u * 16, src ? static_cast<const void *>(src + u * 4) : any, src != nullptr);
 }
 
-// s[i][j] = a[4 ty + i] . b[tx + 16 j]
-__device__ inline void scores(const float *a, const float *b, int ld, int head_dim, int ty, int tx, float (&s)[4][4])
+// s[i][j] = a[I ty + i] . b[tx + 16 j]
+template <int I> __device__ inline void scores(const float *a, const float *b, int ld, int head_dim, int ty, int tx, float (&s)[I][4])
 {
-    const float *pa = a + 4 * ty * ld, *pb = b + tx * ld;
-    float2 t[4][4];
+    const float *pa = a + I * ty * ld, *pb = b + tx * ld;
+    float2 t[I][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < I; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) t[i][j] = make_float2(0.f, 0.f);
 #pragma unroll 2
     for (int d = 0; d < head_dim; d += 4) {
-        float4 x[4], y[4];
+        float4 x[I], y[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[i] = *reinterpret_cast<const float4 *>(pa + i * ld + d);
-            y[i] = *reinterpret_cast<const float4 *>(pb + 16 * i * ld + d);
-        }
+        for (int i = 0; i < I; ++i) x[i] = *reinterpret_cast<const float4 *>(pa + i * ld + d);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+        for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4 *>(pb + 16 * j * ld + d);
+#pragma unroll
+        for (int i = 0; i < I; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 t[i][j] = __ffma2_rn(make_float2(x[i].x, x[i].y), make_float2(y[j].x, y[j].y), t[i][j]);
@@ -74,7 +82,7 @@ __device__ inline void scores(const float *a, const float *b, int ld, int head_d
             }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < I; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j) s[i][j] = t[i][j].x + t[i][j].y;
 }
@@ -89,36 +97,44 @@ __device__ inline void fma4(float (&o)[4], float w, const float4 &v)
     o[3] = b.y;
 }
 
-// o[i][c] += sum_k w[4 ty + i][k] b[k][4 tx + 64 c]     (w row by row)
-template <int C> __device__ inline void add_rows(float (&o)[4][C][4], const float *w, const float *b, int ld, int head_dim, int ty, int tx)
+// Columns 4 cx + 64 c of a head, part `part` of the sums
+struct Columns {
+    int cx, part, parts;
+    __device__ inline Columns(const SimtShape &f, int tx) : cx(tx & (f.cols - 1)), part(tx / f.cols), parts(16 / f.cols) {}
+};
+
+// o[i][c] += sum_k w[I ty + i][k] b[k][4 cx + 64 c]     (w row by row)
+template <int C, int I>
+__device__ inline void add_rows(float (&o)[I][C][4], const float *w, const float *b, int ld, int head_dim, int ty, const Columns &at)
 {
 #pragma unroll 2
-    for (int k = 0; k < kTile; k += 4) {
-        float4 x[4];
+    for (int k = at.part * 4; k < kTile; k += at.parts * 4) {
+        float4 x[I];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = *reinterpret_cast<const float4 *>(w + (4 * ty + i) * kLdP + k);
+        for (int i = 0; i < I; ++i) x[i] = *reinterpret_cast<const float4 *>(w + (I * ty + i) * kLdP + k);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if (4 * tx + 64 * c >= head_dim) continue;
+            if (4 * at.cx + 64 * c >= head_dim) continue;
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
-                const float4 v = *reinterpret_cast<const float4 *>(b + (k + n) * ld + 4 * tx + 64 * c);
+                const float4 v = *reinterpret_cast<const float4 *>(b + (k + n) * ld + 4 * at.cx + 64 * c);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) fma4(o[i][c], n == 0 ? x[i].x : n == 1 ? x[i].y : n == 2 ? x[i].z : x[i].w, v);
+                for (int i = 0; i < I; ++i) fma4(o[i][c], n == 0 ? x[i].x : n == 1 ? x[i].y : n == 2 ? x[i].z : x[i].w, v);
             }
         }
     }
 }
-// o[i][c] += sum_r w[r][4 ty + i] b[r][4 tx + 64 c]     (w column by column)
-template <int C> __device__ inline void add_columns(float (&o)[4][C][4], const float *w, const float *b, int ld, int head_dim, int ty, int tx)
+// o[i][c] += sum_r w[r][4 ty + i] b[r][4 cx + 64 c]     (w column by column, 16 I rows)
+template <int C, int I>
+__device__ inline void add_columns(float (&o)[4][C][4], const float *w, const float *b, int ld, int head_dim, int ty, const Columns &at)
 {
 #pragma unroll 4
-    for (int r = 0; r < kTile; ++r) {
+    for (int r = at.part; r < 16 * I; r += at.parts) {
         const float4 x = *reinterpret_cast<const float4 *>(w + r * kLdP + 4 * ty);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if (4 * tx + 64 * c >= head_dim) continue;
-            const float4 v = *reinterpret_cast<const float4 *>(b + r * ld + 4 * tx + 64 * c);
+            if (4 * at.cx + 64 * c >= head_dim) continue;
+            const float4 v = *reinterpret_cast<const float4 *>(b + r * ld + 4 * at.cx + 64 * c);
             fma4(o[0][c], x.x, v);
             fma4(o[1][c], x.y, v);
             fma4(o[2][c], x.z, v);
@@ -126,24 +142,34 @@ template <int C> __device__ inline void add_columns(float (&o)[4][C][4], const f
         }
     }
 }
+// the parts of the sums together, in every thread (all of a warp)
+template <int C, int N> __device__ inline void add_parts(float (&o)[N][C][4], const SimtShape &f)
+{
+    if (C > 1) return;
+    for (int off = f.cols; off < 16; off <<= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[i][0][e] += __shfl_xor_sync(0xFFFFFFFFu, o[i][0][e], off);
+}
 
-template <int C> __device__ inline void clear(float (&o)[4][C][4])
+template <int C, int N> __device__ inline void clear(float (&o)[N][C][4])
 {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[i][c][e] = 0.f;
 }
 
-// columns 4 tx + 64 c of a row, times f; zeros (whatever the sums hold) where !keep
-template <int C> __device__ inline void store_columns(float *row, const float (&o)[C][4], float f, int head_dim, int tx, bool keep = true)
+// columns 4 cx + 64 c of a row, times f, by the first part's threads; zeros (whatever the sums hold) where !keep
+template <int C> __device__ inline void store_columns(float *row, const float (&o)[C][4], float f, int head_dim, const Columns &at, bool keep = true)
 {
 #pragma unroll
     for (int c = 0; c < C; ++c)
-        if (4 * tx + 64 * c < head_dim)
-            *reinterpret_cast<float4 *>(row + 4 * tx + 64 * c) =
+        if (at.part == 0 && 4 * at.cx + 64 * c < head_dim)
+            *reinterpret_cast<float4 *>(row + 4 * at.cx + 64 * c) =
                 keep ? make_float4(o[c][0] * f, o[c][1] * f, o[c][2] * f, o[c][3] * f) : make_float4(0.f, 0.f, 0.f, 0.f);
 }
 
@@ -164,7 +190,7 @@ __device__ inline SimtUnit simt_unit(const AttnArgs &a, const SimtShape &f)
     x.h = (int)(u - s * (uint32_t)a.kv_heads);
     x.rg = seq_range(a, s, threadIdx.x == 0 && x.z == 0 && x.t0 == 0 && x.h == 0);
     x.rows = (x.rg.q1 - x.rg.q0) * a.group;
-    const int64_t per = ceil_div(x.rg.k1 - x.rg.k0, f.splits);
+    const int64_t per = ceil_div(ceil_div(x.rg.k1 - x.rg.k0, f.splits), (int64_t)kTile) * kTile;
     x.kb = min(x.rg.k0 + x.z * per, x.rg.k1);
     x.ke = min(x.kb + per, x.rg.k1);
     return x;
@@ -178,49 +204,72 @@ __device__ inline void row_of(const AttnArgs &a, const SimtUnit &x, int64_t r, i
     head = x.h * a.group + (int)(r - i * a.group);
 }
 
-template <int C>
-__global__ void __launch_bounds__(kThreads)
+// Tiles of keys and values (or of rows) that a block goes over: stage b of two pairs of tiles, a turn's loads beside the turn before where
+// there are two.  load(j, b) starts the copies of turn j into stage b; use(j, b) works on it.
+template <typename Load, typename Use> __device__ inline void turns(const SimtShape &f, int64_t n, Load load, Use use)
+{
+    if (f.stages == 2 && n > 0) load(0, 0);
+    for (int64_t j = 0; j < n; ++j) {
+        const int b = f.stages == 2 ? (int)(j & 1) : 0;
+        if (f.stages == 1) {
+            __syncthreads();
+            load(j, 0);
+        }
+        cp_async_wait_all();
+        __syncthreads();
+        if (f.stages == 2 && j + 1 < n) load(j + 1, b ^ 1);
+        use(b);
+    }
+}
+
+// Keys and values from x.kb + 64 j on -> a stage, zeros over hidden ones
+__device__ inline void load_keys(const AttnArgs &a, const SimtUnit &x, const SimtShape &f, float *stage, uint8_t *seen_s, int64_t j, const float *kp, const float *vp)
+{
+    const int64_t key = x.kb + j * kTile + (threadIdx.x >> 2);
+    const bool seen = key < x.ke && (!a.mask || a.mask[key]);
+    load_tile<4>(stage, f, seen ? kp + key * a.ldk + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
+    load_tile<4>(stage + kTile * f.ld, f, seen ? vp + key * a.ldv + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
+    if ((threadIdx.x & 3) == 0) seen_s[threadIdx.x >> 2] = seen;
+}
+
+template <int C, int I>
+__global__ void __launch_bounds__(kThreads, blocks_of(C, I))
 attn_simt_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ SimtShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
 {
+    constexpr int kRows = 16 * I, kPerRow = 16 / I;
     extern __shared__ __align__(16) float sm[];
-    float *q_s = sm, *k_s = q_s + kTile * f.ld, *v_s = k_s + kTile * f.ld, *p_s = v_s + kTile * f.ld;
-    __shared__ uint8_t seen_s[kTile];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, heads = a.kv_heads * a.group, lr = threadIdx.x >> 2;
+    float *q_s = sm, *p_s = q_s + kRows * f.ld, *kv_s = p_s + kRows * kLdP;          // stage b: K and V at tiles 2 b, 2 b + 1
+    __shared__ uint8_t seen_s[2][kTile];
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, heads = a.kv_heads * a.group, lr = threadIdx.x / kPerRow;
+    const Columns at(f, tx);
     const SimtUnit x = simt_unit(a, f);
     const float c1 = a.scale * kLog2e;
     const float *qp = static_cast<const float *>(a.q), *kp = static_cast<const float *>(a.k), *vp = static_cast<const float *>(a.v);
-    for (int64_t t = x.t0; t * kTile < x.rows; t += f.tiles) {
-        const int64_t r0 = t * kTile;
+    for (int64_t t = x.t0; t * kRows < x.rows; t += f.tiles) {
+        const int64_t r0 = t * kRows;
         __syncthreads();
         {
             int64_t row;
             int head;
             row_of(a, x, min(r0 + lr, x.rows - 1), row, head);
-            load_tile(q_s, f, r0 + lr < x.rows ? qp + row * a.ldq + (int64_t)head * a.head_dim : nullptr, qp, a.head_dim);
+            load_tile<kPerRow>(q_s, f, r0 + lr < x.rows ? qp + row * a.ldq + (int64_t)head * a.head_dim : nullptr, qp, a.head_dim);
         }
-        float o[4][C][4], m[4], l[4];
-        clear<C>(o);
+        float o[I][C][4], m[I], l[I];
+        clear(o);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < I; ++i) {
             m[i] = -INFINITY;
             l[i] = 0.f;
         }
-        for (int64_t j0 = x.kb; j0 < x.ke; j0 += kTile) {
-            if (j0 > x.kb) __syncthreads();
-            const int64_t key = j0 + lr;
-            const bool seen = key < x.ke && (!a.mask || a.mask[key]);
-            load_tile(k_s, f, seen ? kp + key * a.ldk + (int64_t)x.h * a.head_dim : nullptr, qp, a.head_dim);
-            load_tile(v_s, f, seen ? vp + key * a.ldv + (int64_t)x.h * a.head_dim : nullptr, qp, a.head_dim);
-            if ((threadIdx.x & 3) == 0) seen_s[lr] = seen;
-            cp_async_wait_all();
-            __syncthreads();
-            float s[4][4];
-            scores(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
+        turns(f, ceil_div(x.ke - x.kb, (int64_t)kTile), [&](int64_t j, int b) { load_keys(a, x, f, kv_s + 2 * b * kTile * f.ld, seen_s[b], j, kp, vp); }, [&](int b) {
+            const float *k_s = kv_s + 2 * b * kTile * f.ld, *v_s = k_s + kTile * f.ld;
+            float s[I][4];
+            scores<I>(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
             bool on[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) on[j] = seen_s[tx + 16 * j];
+            for (int j = 0; j < 4; ++j) on[j] = seen_s[b][tx + 16 * j];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
+            for (int i = 0; i < I; ++i) {
                 float top = -INFINITY;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -235,7 +284,7 @@ attn_simt_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                 for (int j = 0; j < 4; ++j) {
                     const float p = exp2_fast(s[i][j] - base);
                     sum += p;
-                    p_s[(4 * ty + i) * kLdP + tx + 16 * j] = p;
+                    p_s[(I * ty + i) * kLdP + tx + 16 * j] = p;
                 }
                 l[i] = l[i] * c + sum;
 #pragma unroll
@@ -244,123 +293,127 @@ attn_simt_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                     for (int e = 0; e < 4; ++e) o[i][n][e] *= c;
             }
             __syncwarp();                                // rows of p belong to one half-warp
-            add_rows<C>(o, p_s, v_s, f.ld, a.head_dim, ty, tx);
+            add_rows<C, I>(o, p_s, v_s, f.ld, a.head_dim, ty, at);
             __syncwarp();
-        }
+        });
         cp_async_wait_all();
+        add_parts<C>(o, f);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            l[i] = row_sum(l[i]);
-            const int64_t r = r0 + 4 * ty + i;
+        for (int i = 0; i < I; ++i) l[i] = row_sum(l[i]);
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
+            const int64_t r = r0 + I * ty + i;
             if (r >= x.rows) continue;
             int64_t row;
             int head;
             row_of(a, x, r, row, head);
             const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
             if (f.splits == 1) {
-                store_columns<C>(static_cast<float *>(a.out) + row * a.ldo + (int64_t)head * a.head_dim, o[i], inv, a.head_dim, tx);
+                store_columns<C>(static_cast<float *>(a.out) + row * a.ldo + (int64_t)head * a.head_dim, o[i], inv, a.head_dim, at);
                 if (a.lse && tx == 0) a.lse[row * heads + head] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * kLn2;
             } else {
                 const int64_t p = ((int64_t)x.z * a.q_rows + row) * heads + head;
-                store_columns<C>(part_o + p * a.head_dim, o[i], inv, a.head_dim, tx);
+                store_columns<C>(part_o + p * a.head_dim, o[i], inv, a.head_dim, at);
                 if (tx == 0) part_ml[p] = make_float2(l[i] == 0.f ? -INFINITY : m[i], l[i]);
             }
         }
     }
 }
 
-template <int C>
-__global__ void __launch_bounds__(kThreads)
+template <int C, int I>
+__global__ void __launch_bounds__(kThreads, blocks_of(C, I))
 attn_simt_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ SimtShape f, float *__restrict__ part_dq, float *__restrict__ dots)
 {
+    constexpr int kRows = 16 * I, kPerRow = 16 / I;
     extern __shared__ __align__(16) float sm[];
-    float *q_s = sm, *g_s = q_s + kTile * f.ld, *k_s = g_s + kTile * f.ld, *v_s = k_s + kTile * f.ld, *ds_s = v_s + kTile * f.ld;
-    __shared__ uint8_t seen_s[kTile];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, heads = a.kv_heads * a.group, lr = threadIdx.x >> 2;
+    float *q_s = sm, *g_s = q_s + kRows * f.ld, *ds_s = g_s + kRows * f.ld, *kv_s = ds_s + kRows * kLdP;
+    __shared__ uint8_t seen_s[2][kTile];
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, heads = a.kv_heads * a.group, lr = threadIdx.x / kPerRow;
+    const Columns at(f, tx);
     const SimtUnit x = simt_unit(a, f);
     const float c1 = a.scale * kLog2e;
     const float *qp = static_cast<const float *>(a.q), *kp = static_cast<const float *>(a.k), *vp = static_cast<const float *>(a.v);
     const float *gp = static_cast<const float *>(a.dout), *op = static_cast<const float *>(a.o);
-    for (int64_t t = x.t0; t * kTile < x.rows; t += f.tiles) {
-        const int64_t r0 = t * kTile;
+    for (int64_t t = x.t0; t * kRows < x.rows; t += f.tiles) {
+        const int64_t r0 = t * kRows;
         __syncthreads();
         {
             int64_t row;
             int head;
             row_of(a, x, min(r0 + lr, x.rows - 1), row, head);
             const bool on = r0 + lr < x.rows;
-            load_tile(q_s, f, on ? qp + row * a.ldq + (int64_t)head * a.head_dim : nullptr, qp, a.head_dim);
-            load_tile(g_s, f, on ? gp + row * a.ldg + (int64_t)head * a.head_dim : nullptr, qp, a.head_dim);
+            load_tile<kPerRow>(q_s, f, on ? qp + row * a.ldq + (int64_t)head * a.head_dim : nullptr, qp, a.head_dim);
+            load_tile<kPerRow>(g_s, f, on ? gp + row * a.ldg + (int64_t)head * a.head_dim : nullptr, qp, a.head_dim);
         }
-        float dq[4][C][4], lse[4], d[4];
-        int64_t row[4];
-        int head[4];
-        clear<C>(dq);
+        float dq[I][C][4], lse[I], d[I];
+        clear(dq);
         cp_async_wait_all();
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int64_t r = r0 + 4 * ty + i;
-            row_of(a, x, min(r, x.rows - 1), row[i], head[i]);
+        for (int i = 0; i < I; ++i) {
+            const int64_t r = r0 + I * ty + i;
+            int64_t row;
+            int head;
+            row_of(a, x, min(r, x.rows - 1), row, head);
             lse[i] = INFINITY;
             d[i] = 0.f;
             if (r < x.rows) {
-                const float v = a.lse[row[i] * heads + head[i]];
+                const float v = a.lse[row * heads + head];
                 if (v != -INFINITY) {
                     lse[i] = v * kLog2e;
 #pragma unroll
                     for (int c = 0; c < C; ++c)
                         if (4 * tx + 64 * c < a.head_dim) {
-                            const float4 y = *reinterpret_cast<const float4 *>(op + row[i] * a.ldo + (int64_t)head[i] * a.head_dim + 4 * tx + 64 * c);
-                            const float4 g = *reinterpret_cast<const float4 *>(g_s + (4 * ty + i) * f.ld + 4 * tx + 64 * c);
+                            const float4 y = *reinterpret_cast<const float4 *>(op + row * a.ldo + (int64_t)head * a.head_dim + 4 * tx + 64 * c);
+                            const float4 g = *reinterpret_cast<const float4 *>(g_s + (I * ty + i) * f.ld + 4 * tx + 64 * c);
                             d[i] += y.x * g.x + y.y * g.y + y.z * g.z + y.w * g.w;
                         }
                 }
             }
             d[i] = row_sum(d[i]);
-            if (r < x.rows && x.z == 0 && tx == 0) dots[row[i] * heads + head[i]] = d[i];
+            if (r < x.rows && x.z == 0 && tx == 0) dots[row * heads + head] = d[i];
         }
-        for (int64_t j0 = x.kb; j0 < x.ke; j0 += kTile) {
-            __syncthreads();
-            const int64_t key = j0 + lr;
-            const bool seen = key < x.ke && (!a.mask || a.mask[key]);
-            load_tile(k_s, f, seen ? kp + key * a.ldk + (int64_t)x.h * a.head_dim : nullptr, qp, a.head_dim);
-            load_tile(v_s, f, seen ? vp + key * a.ldv + (int64_t)x.h * a.head_dim : nullptr, qp, a.head_dim);
-            if ((threadIdx.x & 3) == 0) seen_s[lr] = seen;
-            cp_async_wait_all();
-            __syncthreads();
-            float s[4][4], u[4][4];
-            scores(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
-            scores(g_s, v_s, f.ld, a.head_dim, ty, tx, u);
+        turns(f, ceil_div(x.ke - x.kb, (int64_t)kTile), [&](int64_t j, int b) { load_keys(a, x, f, kv_s + 2 * b * kTile * f.ld, seen_s[b], j, kp, vp); }, [&](int b) {
+            const float *k_s = kv_s + 2 * b * kTile * f.ld, *v_s = k_s + kTile * f.ld;
+            float s[I][4], u[I][4];
+            scores<I>(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
+            scores<I>(g_s, v_s, f.ld, a.head_dim, ty, tx, u);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const bool on = seen_s[tx + 16 * j];
+                const bool on = seen_s[b][tx + 16 * j];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    ds_s[(4 * ty + i) * kLdP + tx + 16 * j] = on ? exp2_fast(fmaf(s[i][j], c1, -lse[i])) * (u[i][j] - d[i]) : 0.f;
+                for (int i = 0; i < I; ++i)
+                    ds_s[(I * ty + i) * kLdP + tx + 16 * j] = on ? exp2_fast(fmaf(s[i][j], c1, -lse[i])) * (u[i][j] - d[i]) : 0.f;
             }
             __syncwarp();
-            add_rows<C>(dq, ds_s, k_s, f.ld, a.head_dim, ty, tx);
+            add_rows<C, I>(dq, ds_s, k_s, f.ld, a.head_dim, ty, at);
             __syncwarp();
-        }
+        });
+        add_parts<C>(dq, f);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (r0 + 4 * ty + i >= x.rows) continue;
+        for (int i = 0; i < I; ++i) {
+            const int64_t r = r0 + I * ty + i;
+            if (r >= x.rows) continue;
+            int64_t row;
+            int head;
+            row_of(a, x, r, row, head);
             const bool keep = lse[i] != INFINITY;        // a row that saw no key passes on nothing
-            if (f.splits == 1) store_columns<C>(static_cast<float *>(a.dq) + row[i] * a.ldq2 + (int64_t)head[i] * a.head_dim, dq[i], a.scale, a.head_dim, tx, keep);
-            else store_columns<C>(part_dq + (((int64_t)x.z * a.q_rows + row[i]) * heads + head[i]) * a.head_dim, dq[i], a.scale, a.head_dim, tx, keep);
+            if (f.splits == 1) store_columns<C>(static_cast<float *>(a.dq) + row * a.ldq2 + (int64_t)head * a.head_dim, dq[i], a.scale, a.head_dim, at, keep);
+            else store_columns<C>(part_dq + (((int64_t)x.z * a.q_rows + row) * heads + head) * a.head_dim, dq[i], a.scale, a.head_dim, at, keep);
         }
     }
 }
 
-template <int C>
-__global__ void __launch_bounds__(kThreads)
+template <int C, int I>
+__global__ void __launch_bounds__(kThreads, blocks_of(C, I))
 attn_simt_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ SimtShape f, const float *__restrict__ dots)
 {
+    constexpr int kRows = 16 * I, kPerRow = 16 / I;
     extern __shared__ __align__(16) float sm[];
-    float *k_s = sm, *v_s = k_s + kTile * f.ld, *q_s = v_s + kTile * f.ld, *g_s = q_s + kTile * f.ld, *p_s = g_s + kTile * f.ld, *ds_s = p_s + kTile * kLdP;
-    __shared__ float lse_s[kTile], dot_s[kTile];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, heads = a.kv_heads * a.group, lr = threadIdx.x >> 2;
+    float *k_s = sm, *v_s = k_s + kTile * f.ld, *p_s = v_s + kTile * f.ld, *ds_s = p_s + kRows * kLdP, *qg_s = ds_s + kRows * kLdP;
+    __shared__ float lse_s[2][kRows], dot_s[2][kRows];
+    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, heads = a.kv_heads * a.group, lr = threadIdx.x / kPerRow;
+    const Columns at(f, tx);
     const SimtUnit x = simt_unit(a, f);
     const float c1 = a.scale * kLog2e;
     const float *qp = static_cast<const float *>(a.q), *kp = static_cast<const float *>(a.k), *vp = static_cast<const float *>(a.v);
@@ -368,106 +421,115 @@ attn_simt_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     for (int64_t j0 = x.rg.k0 + (int64_t)x.t0 * kTile; j0 < x.rg.k1; j0 += (int64_t)f.tiles * kTile) {
         __syncthreads();
         {
-            const int64_t key = j0 + lr;
+            const int64_t key = j0 + (threadIdx.x >> 2);
             const bool seen = key < x.rg.k1 && (!a.mask || a.mask[key]);
-            load_tile(k_s, f, seen ? kp + key * a.ldk + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
-            load_tile(v_s, f, seen ? vp + key * a.ldv + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
+            load_tile<4>(k_s, f, seen ? kp + key * a.ldk + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
+            load_tile<4>(v_s, f, seen ? vp + key * a.ldv + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
         }
         float dk[4][C][4], dv[4][C][4];
-        clear<C>(dk);
-        clear<C>(dv);
-        for (int64_t r0 = 0; r0 < x.rows; r0 += kTile) {
-            if (r0) __syncthreads();
+        clear(dk);
+        clear(dv);
+        turns(f, ceil_div(x.rows, (int64_t)kRows), [&](int64_t j, int b) {
+            const int64_t r = j * kRows + lr;
+            float *q_s = qg_s + 2 * b * kRows * f.ld, *g_s = q_s + kRows * f.ld;
             int64_t row;
             int head;
-            row_of(a, x, min(r0 + lr, x.rows - 1), row, head);
+            row_of(a, x, min(r, x.rows - 1), row, head);
             float l = INFINITY;
-            if (r0 + lr < x.rows) {
+            if (r < x.rows) {
                 const float v = a.lse[row * heads + head];
                 if (v != -INFINITY) l = v * kLog2e;
             }
-            if ((threadIdx.x & 3) == 0) {
-                lse_s[lr] = l;
-                dot_s[lr] = l != INFINITY ? dots[row * heads + head] : 0.f;
+            if (threadIdx.x % kPerRow == 0) {
+                lse_s[b][lr] = l;
+                dot_s[b][lr] = l != INFINITY ? dots[row * heads + head] : 0.f;
             }
-            load_tile(q_s, f, l != INFINITY ? qp + row * a.ldq + (int64_t)head * a.head_dim : nullptr, kp, a.head_dim);
-            load_tile(g_s, f, l != INFINITY ? gp + row * a.ldg + (int64_t)head * a.head_dim : nullptr, kp, a.head_dim);
-            cp_async_wait_all();
-            __syncthreads();
-            float s[4][4], u[4][4];
-            scores(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
-            scores(g_s, v_s, f.ld, a.head_dim, ty, tx, u);
+            load_tile<kPerRow>(q_s, f, l != INFINITY ? qp + row * a.ldq + (int64_t)head * a.head_dim : nullptr, kp, a.head_dim);
+            load_tile<kPerRow>(g_s, f, l != INFINITY ? gp + row * a.ldg + (int64_t)head * a.head_dim : nullptr, kp, a.head_dim);
+        }, [&](int b) {
+            const float *q_s = qg_s + 2 * b * kRows * f.ld, *g_s = q_s + kRows * f.ld;
+            float s[I][4], u[I][4];
+            scores<I>(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
+            scores<I>(g_s, v_s, f.ld, a.head_dim, ty, tx, u);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float lse = lse_s[4 * ty + i], d = dot_s[4 * ty + i];
+            for (int i = 0; i < I; ++i) {
+                const float lse = lse_s[b][I * ty + i], d = dot_s[b][I * ty + i];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float p = exp2_fast(fmaf(s[i][j], c1, -lse));
-                    p_s[(4 * ty + i) * kLdP + tx + 16 * j] = p;
-                    ds_s[(4 * ty + i) * kLdP + tx + 16 * j] = p * (u[i][j] - d);
+                    p_s[(I * ty + i) * kLdP + tx + 16 * j] = p;
+                    ds_s[(I * ty + i) * kLdP + tx + 16 * j] = p * (u[i][j] - d);
                 }
             }
             __syncthreads();
-            add_columns<C>(dv, p_s, g_s, f.ld, a.head_dim, ty, tx);
-            add_columns<C>(dk, ds_s, q_s, f.ld, a.head_dim, ty, tx);
-        }
+            add_columns<C, I>(dv, p_s, g_s, f.ld, a.head_dim, ty, at);
+            add_columns<C, I>(dk, ds_s, q_s, f.ld, a.head_dim, ty, at);
+        });
         cp_async_wait_all();
+        add_parts<C>(dk, f);
+        add_parts<C>(dv, f);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t key = j0 + 4 * ty + i;
             if (key >= x.rg.k1) continue;
             const bool keep = !a.mask || a.mask[key];
-            store_columns<C>(static_cast<float *>(a.dk) + key * a.ldk2 + (int64_t)x.h * a.head_dim, dk[i], a.scale, a.head_dim, tx, keep);
-            store_columns<C>(static_cast<float *>(a.dv) + key * a.ldv2 + (int64_t)x.h * a.head_dim, dv[i], 1.f, a.head_dim, tx, keep);
+            store_columns<C>(static_cast<float *>(a.dk) + key * a.ldk2 + (int64_t)x.h * a.head_dim, dk[i], a.scale, a.head_dim, at, keep);
+            store_columns<C>(static_cast<float *>(a.dv) + key * a.ldv2 + (int64_t)x.h * a.head_dim, dv[i], 1.f, a.head_dim, at, keep);
         }
     }
 }
 
-constexpr int kMaxDevices = 64;
+constexpr int kMaxDevices = 64, kMostSmem = 226 * 1024, kSmSmem = 228 * 1024;
 template <typename Kernel> bool allow_smem(Kernel kernel, bool (&done)[kMaxDevices])
 {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return false;
     if (done[dev]) return true;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024) != cudaSuccess) return false;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) != cudaSuccess) return false;
     done[dev] = true;
     return true;
 }
 
-SimtShape shape_of(const AttnArgs &a, int64_t tiles, int splits)
+// kept: floats of shared memory that stay; pair: those of one stage.  Two stages where they leave room for `blocks` blocks per SM.
+SimtShape shape_of(const AttnArgs &a, int64_t tiles, int splits, int kept_rows, int pair_rows, int p_rows, int blocks, size_t &smem)
 {
     SimtShape f{};
     f.ld = (a.head_dim / 4 | 1) * 4;                 // an odd number of 16-byte units
     f.tiles = (int)tiles;
     f.splits = splits;
+    f.cols = 16;
+    while (f.cols > 1 && f.cols * 2 >= a.head_dim) f.cols /= 2;
+    const size_t fixed = ((size_t)kept_rows * f.ld + (size_t)p_rows * kLdP) * sizeof(float), pair = (size_t)pair_rows * f.ld * sizeof(float);
+    f.stages = (fixed + 2 * pair + 2048) * blocks <= (size_t)kSmSmem ? 2 : 1;
+    smem = fixed + f.stages * pair;
     return f;
 }
 
-size_t smem_of(const SimtShape &f, int tiles, int scores) { return ((size_t)tiles * kTile * f.ld + (size_t)scores * kTile * kLdP) * sizeof(float); }
-
-template <int C> bool forward_of(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
+template <int C, int I> bool forward_of(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
 {
     static bool done[kMaxDevices] = {};
-    if (!allow_smem(attn_simt_fwd_kernel<C>, done)) return false;
-    const SimtShape f = shape_of(a, p.q_tiles, p.splits);
+    if (!allow_smem(attn_simt_fwd_kernel<C, I>, done)) return false;
+    size_t smem;
+    const SimtShape f = shape_of(a, p.q_tiles, p.splits, 16 * I, 2 * kTile, 16 * I, blocks_of(C, I), smem);
     note_launch();
-    attn_simt_fwd_kernel<C><<<(unsigned)(a.n_seq * a.kv_heads * p.q_tiles * p.splits), kThreads, smem_of(f, 3, 1), st>>>(a, f, part_o, part_ml);
+    attn_simt_fwd_kernel<C, I><<<(unsigned)(a.n_seq * a.kv_heads * p.q_tiles * p.splits), kThreads, smem, st>>>(a, f, part_o, part_ml);
     return true;
 }
 
-template <int C> bool backward_of(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
+template <int C, int I> bool backward_of(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
 {
     static bool done[2][kMaxDevices] = {};
-    if (!allow_smem(attn_simt_dq_kernel<C>, done[0]) || !allow_smem(attn_simt_dkv_kernel<C>, done[1])) return false;
+    if (!allow_smem(attn_simt_dq_kernel<C, I>, done[0]) || !allow_smem(attn_simt_dkv_kernel<C, I>, done[1])) return false;
+    size_t smem;
     if (a.q_rows) {
-        const SimtShape f = shape_of(a, p.q_tiles, p.splits);
+        const SimtShape f = shape_of(a, p.q_tiles, p.splits, 2 * 16 * I, 2 * kTile, 16 * I, blocks_of(C, I), smem);
         note_launch();
-        attn_simt_dq_kernel<C><<<(unsigned)(a.n_seq * a.kv_heads * p.q_tiles * p.splits), kThreads, smem_of(f, 4, 1), st>>>(a, f, part_dq, dots);
+        attn_simt_dq_kernel<C, I><<<(unsigned)(a.n_seq * a.kv_heads * p.q_tiles * p.splits), kThreads, smem, st>>>(a, f, part_dq, dots);
     }
     if (a.k_rows) {
-        const SimtShape f = shape_of(a, p.k_tiles, 1);
+        const SimtShape f = shape_of(a, p.k_tiles, 1, 2 * kTile, 2 * 16 * I, 2 * 16 * I, blocks_of(C, I), smem);
         note_launch();
-        attn_simt_dkv_kernel<C><<<(unsigned)(a.n_seq * a.kv_heads * p.k_tiles), kThreads, smem_of(f, 4, 2), st>>>(a, f, dots);
+        attn_simt_dkv_kernel<C, I><<<(unsigned)(a.n_seq * a.kv_heads * p.k_tiles), kThreads, smem, st>>>(a, f, dots);
     }
     return true;
 }
@@ -477,22 +539,36 @@ template <int C> bool backward_of(const AttnArgs &a, const SimtPlan &p, float *p
 SimtPlan simt_plan(const AttnArgs &a, int64_t max_q, int64_t max_k)
 {
     SimtPlan p{};
-    const int64_t units = std::max<int64_t>(a.n_seq * a.kv_heads, 1), most = (((int64_t)1 << 31) - 1) / units;
-    p.q_tiles = std::max<int64_t>(1, std::min(ceil_div(max_q * a.group, kTile), most));
+    const int64_t units = std::max<int64_t>(a.n_seq * a.kv_heads, 1), most = (((int64_t)1 << 31) - 1) / units, rows = max_q * a.group;
+    p.rows = rows <= 16 ? 16 : (rows <= 32 ? 32 : 64);
+    p.q_tiles = std::max<int64_t>(1, std::min(ceil_div(rows, p.rows), most));
     p.k_tiles = std::max<int64_t>(1, std::min(ceil_div(max_k, kTile), most));
     p.splits = 1;
-    if (units * p.q_tiles < 296) p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({296 / (units * p.q_tiles), max_k / (2 * kTile), kMaxSplits}));
+    if (units * p.q_tiles < 296)
+        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({296 / (units * p.q_tiles), max_k / (2 * kTile), kMaxSplits, most / p.q_tiles}));
     return p;
+}
+
+template <int C> static bool forward_by_rows(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
+{
+    if (p.rows == 16) return forward_of<C, 1>(a, p, part_o, part_ml, st);
+    return p.rows == 32 ? forward_of<C, 2>(a, p, part_o, part_ml, st) : forward_of<C, 4>(a, p, part_o, part_ml, st);
+}
+
+template <int C> static bool backward_by_rows(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
+{
+    if (p.rows == 16) return backward_of<C, 1>(a, p, part_dq, dots, st);
+    return p.rows == 32 ? backward_of<C, 2>(a, p, part_dq, dots, st) : backward_of<C, 4>(a, p, part_dq, dots, st);
 }
 
 bool simt_attention_forward(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    return a.head_dim <= 64 ? forward_of<1>(a, p, part_o, part_ml, st) : forward_of<2>(a, p, part_o, part_ml, st);
+    return a.head_dim <= 64 ? forward_by_rows<1>(a, p, part_o, part_ml, st) : forward_by_rows<2>(a, p, part_o, part_ml, st);
 }
 
 bool simt_attention_backward(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
 {
-    return a.head_dim <= 64 ? backward_of<1>(a, p, part_dq, dots, st) : backward_of<2>(a, p, part_dq, dots, st);
+    return a.head_dim <= 64 ? backward_by_rows<1>(a, p, part_dq, dots, st) : backward_by_rows<2>(a, p, part_dq, dots, st);
 }
 
 }  // namespace e2egrec
