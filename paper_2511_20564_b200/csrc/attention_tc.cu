@@ -33,6 +33,9 @@ __device__ inline float exp2_approx(float x)
     return y;
 }
 
+__device__ inline float2 exp2_pair(float2 x) { return make_float2(exp2_approx(x.x), exp2_approx(x.y)); }
+__device__ inline float2 pair_of(uint32_t x, uint32_t y) { return make_float2(__uint_as_float(x), __uint_as_float(y)); }
+
 __device__ inline uint32_t pack_bf16(float lo, float hi)
 {
     __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
@@ -239,11 +242,11 @@ template <int NB> __device__ inline void head_steps(uint32_t d, uint64_t a, uint
     for (int k = 0; k < 4 * NB; ++k)
         if (k < ksteps) umma(d, desc_at(a, (k >> 2) * kBlockBytes + (k & 3) * 32), desc_at(b, (k >> 2) * kBlockBytes + (k & 3) * 32), idesc, k > 0);
 }
-__device__ inline void row_steps(uint32_t d, uint32_t a, uint32_t second, uint64_t b, uint32_t idesc, bool add)
+__device__ inline void row_steps(uint32_t d, uint32_t a, uint32_t second, uint64_t b, uint32_t idesc, bool add, int from = 0, int to = kTile / 16)
 {
 #pragma unroll
     for (int k = 0; k < kTile / 16; ++k)
-        umma_ts(d, a + k * 8 + (k >= 4 ? second : 0), desc_at(b, k * 2048), idesc, k > 0 ? 1u : (uint32_t)add);
+        if (k >= from && k < to) umma_ts(d, a + k * 8 + (k >= 4 ? second : 0), desc_at(b, k * 2048), idesc, k > 0 ? 1u : (uint32_t)add);
 }
 
 // ------------------------------------------------------------------------------------------------- forward
@@ -254,6 +257,9 @@ template <int NB, int NT> struct Fwd {
     static constexpr int kStages = NT == 2 ? (NB == 2 ? 5 : 8) : (NB == 2 ? 2 : 5);
     static constexpr int kSoft = NT * 4, kThreads = (kSoft + 4) * 32, kBlocks = 3 - NT;      // copies, zeros, products; one idle
     static constexpr int kRows = NT * kTile, kTileBytes = NB * kBlockBytes, kColumns = NT * 256;
+    // p goes to the product in halves where heads take up to 64 columns, the second formed beside the product of the first: 37 x 256 x 8192
+    // with 4 heads of 64 158 -> 141 us, one-tile blocks 55 -> 48 us; with heads of 128 158 -> 167 us, so whole there
+    static constexpr int kParts = NB == 1 ? 2 : 1;
     static constexpr size_t kSmem = 1024 + (size_t)(NT + kStages) * kTileBytes;
 };
 
@@ -265,7 +271,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     using F = Fwd<NB, NT>;
     constexpr int kStages = F::kStages, kTileBytes = F::kTileBytes, kRows = F::kRows, kSoft = F::kSoft;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], v_clean[kWordRing], q_full, q_empty, s_full[NT], p_full[NT], o_full[NT], o_empty[NT];
+    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], v_clean[kWordRing], q_full, q_empty, s_full[NT], p_full[NT][F::kParts], o_full[NT], o_empty[NT];
     __shared__ __align__(16) uint32_t words[kWordRing][4];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
@@ -285,7 +291,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         mbar_init(&q_empty, 1);
         for (int t = 0; t < NT; ++t) {
             mbar_init(&s_full[t], 1);
-            mbar_init(&p_full[t], 4);
+            for (int part = 0; part < F::kParts; ++part) mbar_init(&p_full[t][part], 4);
             mbar_init(&o_full[t], 1);
             mbar_init(&o_empty[t], 4);
         }
@@ -408,10 +414,16 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                             for (int q = 0; q < NT; ++q) {
                                 if (q >= nt || !ok) continue;
-                                ok = mbar_wait(&p_full[q], pc[q]++ & 1u, &abort_flag);
+#pragma unroll
+                                for (int part = 0; part < F::kParts; ++part) {
+                                    if (!ok) continue;
+                                    ok = mbar_wait(&p_full[q][part], pc[q] & 1u, &abort_flag);
+                                    if (!ok) continue;
+                                    tc_fence_after();
+                                    row_steps(tmem_o + q * 64 * NB, tmem + q * kTile, 0, v_desc, id_o, j > 0, part * (8 / F::kParts), (part + 1) * (8 / F::kParts));
+                                }
+                                ++pc[q];
                                 if (!ok) continue;
-                                tc_fence_after();
-                                row_steps(tmem_o + q * 64 * NB, tmem + q * kTile, 0, v_desc, id_o, j > 0);
                                 if (j + 1 < x.n) {
                                     if (q == nt - 1) umma_commit(&kv_empty[gv % kStages]);
                                     if (q == 0) ok = tile_ready(&kv_full[gk % kStages], (gk / kStages) & 1u, &abort_flag);
@@ -481,6 +493,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (j > 0 && __any_sync(0xFFFFFFFFu, moves && top != -INFINITY)) {
                         const float f = moves && top != -INFINITY ? exp2_approx((m - top) * c1) : 1.f;
                         l *= f;
+                        __syncwarp();
                         for (int c = 0; c < NB * 4; ++c) {
                             uint32_t x[16];
                             tmem_load16_async(o_addr + c * 16, x);
@@ -507,13 +520,16 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             p[i / 2] = pack_bf16(x.x, x.y);
                         }
                         tmem_store16(s_addr + c * 16, p);
+                        if ((c + 1) % (4 / F::kParts) == 0) {
+                            tmem_store_wait();
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&p_full[q][(c + 1) / (4 / F::kParts) - 1]);
+                            __syncwarp();                    // the stores to tensor memory are for a converged warp
+                        }
                     }
                     const float sum = (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y) + ((sums[2].x + sums[2].y) + (sums[3].x + sums[3].y));
                     l += sum;
-                    tmem_store_wait();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&p_full[q]);
                 }
                 if (!ok) break;
                 if (x.n > 0) {
@@ -826,7 +842,11 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                         tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64 + 32, v[1]);
                         tmem_load_wait();
 #pragma unroll
-                        for (int e = 0; e < 64; ++e) p[e] = exp2_approx(fmaf(__uint_as_float(v[e >> 5][e & 31]), c1, -base));
+                        for (int e = 0; e < 64; e += 2) {
+                            const float2 y = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(c1, c1), make_float2(-base, -base)));
+                            p[e] = y.x;
+                            p[e + 1] = y.y;
+                        }
                     }
                     ok = warp_wait(&dp_full, jj & 1u, &abort_flag);
                     if (!ok) break;
@@ -837,7 +857,12 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                         tmem_load32_async(tmem + lanes + 256 + q * 64 + 32, v[1]);
                         tmem_load_wait();
 #pragma unroll
-                        for (int e = 0; e < 64; ++e) p[e] *= __uint_as_float(v[e >> 5][e & 31]) - dot;
+                        for (int e = 0; e < 64; e += 2) {
+                            const float2 y = __fmul2_rn(__fadd2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(-dot, -dot)),
+                                                        make_float2(p[e], p[e + 1]));
+                            p[e] = y.x;
+                            p[e + 1] = y.y;
+                        }
                     }
 #pragma unroll
                     for (int c = 0; c < 2; ++c) {
@@ -970,8 +995,8 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             if (v == 0) {
 #pragma unroll
                                 for (int b = 0; b < 4; ++b) {
-                                    stat_lse[jj % kWordRing][b * 32 + lane] = l[b];
-                                    stat_dot[jj % kWordRing][b * 32 + lane] = d[b];
+                                    stat_lse[jj % kWordRing][b * 32 + lane] = -l[b];
+                                    stat_dot[jj % kWordRing][b * 32 + lane] = -d[b];
                                 }
                                 if (lane == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
                                 __syncwarp();
@@ -1113,11 +1138,13 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         tmem_load_wait();
 #pragma unroll
                         for (int e = 0; e < 64; e += 4) {
-                            const float4 l = lse4[e / 4];
-                            p[e] = exp2_approx(fmaf(__uint_as_float(v[e >> 5][e & 31]), c1, -l.x));
-                            p[e + 1] = exp2_approx(fmaf(__uint_as_float(v[e >> 5][(e & 31) + 1]), c1, -l.y));
-                            p[e + 2] = exp2_approx(fmaf(__uint_as_float(v[e >> 5][(e & 31) + 2]), c1, -l.z));
-                            p[e + 3] = exp2_approx(fmaf(__uint_as_float(v[e >> 5][(e & 31) + 3]), c1, -l.w));
+                            const float4 l = lse4[e / 4];            // negated, as the sums of products below
+                            const float2 y0 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(c1, c1), make_float2(l.x, l.y)));
+                            const float2 y1 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][(e & 31) + 2], v[e >> 5][(e & 31) + 3]), make_float2(c1, c1), make_float2(l.z, l.w)));
+                            p[e] = y0.x;
+                            p[e + 1] = y0.y;
+                            p[e + 2] = y1.x;
+                            p[e + 3] = y1.y;
                         }
                     }
                     store_operand(tmem + lanes + q * 64, p);
@@ -1136,10 +1163,12 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                         for (int e = 0; e < 64; e += 4) {
                             const float4 d = dot4[e / 4];
-                            p[e] *= __uint_as_float(v[e >> 5][e & 31]) - d.x;
-                            p[e + 1] *= __uint_as_float(v[e >> 5][(e & 31) + 1]) - d.y;
-                            p[e + 2] *= __uint_as_float(v[e >> 5][(e & 31) + 2]) - d.z;
-                            p[e + 3] *= __uint_as_float(v[e >> 5][(e & 31) + 3]) - d.w;
+                            const float2 y0 = __fmul2_rn(__fadd2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(d.x, d.y)), make_float2(p[e], p[e + 1]));
+                            const float2 y1 = __fmul2_rn(__fadd2_rn(pair_of(v[e >> 5][(e & 31) + 2], v[e >> 5][(e & 31) + 3]), make_float2(d.z, d.w)), make_float2(p[e + 2], p[e + 3]));
+                            p[e] = y0.x;
+                            p[e + 1] = y0.y;
+                            p[e + 2] = y1.x;
+                            p[e + 3] = y1.y;
                         }
                     }
                     store_operand(tmem + lanes + 128 + q * 64, p);
