@@ -84,27 +84,50 @@ attn_join_kernel(const __grid_constant__ AttnArgs a, int splits, int warps, cons
     if (a.lse && lane == 0) a.lse[unit] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// dQ of stretches of the keys -> dQ, in order: one thread per four elements, its loads eight at a time
+// dQ of stretches of the keys -> dQ: a block per (query, head), a thread per four elements and part of the stretches (a power of two of
+// threads side by side over the elements), the parts added up in order.  fit: the sums of p k of every stretch and of dS follow
+// (attention_few.cu).  One row of 4 x 24 000 keys, two heads of 128: 125 us with a thread going over all stretches, 60 us so.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads)
-attn_join_dq_kernel(const __grid_constant__ AttnArgs a, int splits, const float *__restrict__ part)
+attn_join_dq_kernel(const __grid_constant__ AttnArgs a, int splits, int wide, bool fit, const float *__restrict__ part)
 {
-    const int heads = a.kv_heads * a.group, units = a.head_dim / 4;
-    const int64_t n = (int64_t)blockIdx.x * kRowThreads + threadIdx.x, cell = n / units, stride = a.q_rows * heads * units;
-    const int64_t row = cell / heads;
-    if (row >= a.q_rows || owner(a.q_ptr, a.n_seq, row) < 0) return;
-    const float4 *p = reinterpret_cast<const float4 *>(part) + n;
-    float4 t = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-    for (int z = 0; z < splits; ++z) {
-        const float4 v = p[z * stride];
-        t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+    __shared__ float4 sums[2][kRowThreads];
+    __shared__ float rests[kRowThreads];
+    const int heads = a.kv_heads * a.group, units = a.head_dim / 4, at = threadIdx.x & (wide - 1), first = threadIdx.x / wide, parts = kRowThreads / wide;
+    const int64_t cell = blockIdx.x, cells = a.q_rows * heads, row = cell / heads;
+    if (owner(a.q_ptr, a.n_seq, row) < 0) return;
+    const float4 *p = reinterpret_cast<const float4 *>(part) + cell * units + at;
+    const float *rest = part + 2 * splits * cells * a.head_dim + cell;
+    float4 t = make_float4(0.f, 0.f, 0.f, 0.f), m = t;
+    float r = 0.f;
+    if (at < units) {
+#pragma unroll 4
+        for (int z = first; z < splits; z += parts) {
+            const float4 v = p[z * cells * units];
+            t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+            if (fit) {
+                const float4 w = p[(splits + z) * cells * units];
+                m.x += w.x; m.y += w.y; m.z += w.z; m.w += w.w;
+                r += rest[z * cells];
+            }
+        }
     }
-    T *out = static_cast<T *>(a.dq) + row * a.ldq2 + (cell - row * heads) * a.head_dim + (n - cell * units) * 4;
-    out[0] = from_float<T>(t.x);
-    out[1] = from_float<T>(t.y);
-    out[2] = from_float<T>(t.z);
-    out[3] = from_float<T>(t.w);
+    sums[0][threadIdx.x] = t;
+    sums[1][threadIdx.x] = m;
+    rests[threadIdx.x] = r;
+    __syncthreads();
+    if (first || at >= units) return;
+    for (int i = 1; i < parts; ++i) {
+        const float4 v = sums[0][i * wide + at], w = sums[1][i * wide + at];
+        t.x += v.x; t.y += v.y; t.z += v.z; t.w += v.w;
+        m.x += w.x; m.y += w.y; m.z += w.z; m.w += w.w;
+        r += rests[i * wide + at];
+    }
+    T *out = static_cast<T *>(a.dq) + row * a.ldq2 + (cell - row * heads) * a.head_dim + at * 4;
+    out[0] = from_float<T>(t.x - r * m.x);
+    out[1] = from_float<T>(t.y - r * m.y);
+    out[2] = from_float<T>(t.z - r * m.z);
+    out[3] = from_float<T>(t.w - r * m.w);
 }
 
 // Shapes, types and alignment of one matrix of heads
@@ -163,7 +186,8 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     }
     if (backward && !(p.path == Path::few && p.few.both)) p.dot_bytes = align_up(cells * sizeof(float), 256);
     if (p.splits > 1) {
-        p.part_bytes = align_up(p.splits * cells * a.head_dim * sizeof(float), 256);
+        const bool fit = backward && p.path == Path::few && dtype == E2EGREC_BF16;       // as attn_few_bwd_kernel's kFit
+        p.part_bytes = align_up(p.splits * cells * (fit ? 2 * a.head_dim + 1 : a.head_dim) * sizeof(float), 256);
         if (!backward) p.ml_bytes = align_up(p.splits * cells * sizeof(float2), 256);
     }
     return p;
@@ -203,12 +227,14 @@ int32_t check_shape(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_se
 
 }  // namespace
 
-void join_dq(const AttnArgs &a, int splits, int32_t dtype, const float *part_dq, cudaStream_t st)
+void join_dq(const AttnArgs &a, int splits, int32_t dtype, bool fit, const float *part_dq, cudaStream_t st)
 {
     note_launch();
-    const unsigned grid = (unsigned)ceil_div(a.q_rows * a.kv_heads * a.group * (a.head_dim / 4), kRowThreads);
-    if (dtype == E2EGREC_F32) attn_join_dq_kernel<float><<<grid, kRowThreads, 0, st>>>(a, splits, part_dq);
-    else attn_join_dq_kernel<__nv_bfloat16><<<grid, kRowThreads, 0, st>>>(a, splits, part_dq);
+    const unsigned grid = (unsigned)(a.q_rows * a.kv_heads * a.group);
+    int wide = 1;
+    while (wide * 4 < a.head_dim) wide *= 2;
+    if (dtype == E2EGREC_F32) attn_join_dq_kernel<float><<<grid, kRowThreads, 0, st>>>(a, splits, wide, fit, part_dq);
+    else attn_join_dq_kernel<__nv_bfloat16><<<grid, kRowThreads, 0, st>>>(a, splits, wide, fit, part_dq);
 }
 
 }  // namespace e2egrec
@@ -303,7 +329,7 @@ extern "C" int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, con
         ok = tc_attention_backward(a, plan.q_tiles, plan.k_tiles, dots, st);
     } else if (plan.path == Path::simt) {
         ok = simt_attention_backward(a, plan.simt, part_dq, dots, st);
-        if (ok && plan.splits > 1 && a.q_rows) join_dq(a, plan.splits, Q->dtype, part_dq, st);
+        if (ok && plan.splits > 1 && a.q_rows) join_dq(a, plan.splits, Q->dtype, false, part_dq, st);
     } else {
         ok = few_attention_backward(a, plan.few, Q->dtype, part_dq, dots, st);
     }

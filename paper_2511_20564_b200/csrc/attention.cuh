@@ -74,11 +74,11 @@ struct FewPlan {
 };
 FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool backward);
 bool few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_o, float2 *part_ml, cudaStream_t st);
-// part_dq: [splits x q_rows x heads x head_dim] where splits > 1; dots: [q_rows x heads] where !both
+// part_dq: [splits x q_rows x heads x head_dim] where splits > 1, with bf16 twice that and [splits x q_rows x heads]; dots: [q_rows x heads] where !both
 bool few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st);
 
 // dQ of stretches of the keys -> dQ, in order
-void join_dq(const AttnArgs &a, int splits, int32_t dtype, const float *part_dq, cudaStream_t st);
+void join_dq(const AttnArgs &a, int splits, int32_t dtype, bool fit, const float *part_dq, cudaStream_t st);
 
 // attention_simt.cu: fp32, head_dim <= 128, tiles of 64 rows x 64 keys
 struct SimtPlan {

@@ -534,6 +534,8 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
 // that is longer than the launch was sized for has its rows done batch by batch and its keys' gradients apart.
 // Where all keys are in one turn of the warp, D = sum_j p_j dP_j is formed from what the registers hold instead of the stored
 // outputs: with a handful of keys dP - D cancels, and the rounding of 16-bit outputs showed (dQ of three keys 3.1e-3 off, 2.0e-3 so).
+// Over more keys D comes from the stored outputs, and what 16-bit ones lack, sum_j dS_j (0 with the exact D), is taken out at the end:
+// dQ = sum_j dS_j k_j - (sum_j dS_j) (sum_j p_j k_j).  dQ of rows that see 12 000 keys was 3.4e-3 off without it, a rounding 1.7e-3.
 template <typename T, int R, int U, int CPL, bool kBoth>
 __global__ void __launch_bounds__(kFewThreads, CPL == 2 || R > 2 ? 2 : (R == 1 ? 4 : 3))
 attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_dq, float *__restrict__ dots)
@@ -544,6 +546,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     __shared__ uint32_t seen_words[kFewWarps * kStages];
     __shared__ int abort_flag;
     __shared__ float join[kFewWarps][E * 32];
+    constexpr bool kFit = sizeof(T) == 2;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wu = warp & (f.warps - 1);
     const Unit x = few_unit(a, f, blockIdx.x * (uint32_t)(kFewWarps / f.warps) + warp / f.warps);
@@ -564,6 +567,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         if (f.warps == 1 ? !live : !__syncthreads_or((int)live)) break;
         if (live) ring.start();
         float q[R][E], g[R][E], dq[R][E], lse[R], d[R];
+        float mean[kFit ? R : 1][E], rest[R];             // sum_j p_j k_j; what D lacked
         const bool one_turn = f.warps == 1 && f.splits == 1 && x.ke - x.kb <= U * kpw;
         RowWalk in(a, x, r0);
 #pragma unroll
@@ -596,6 +600,10 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             t.widen(g[r]);
 #pragma unroll
             for (int e = 0; e < E; ++e) dq[r][e] = 0.f;
+            rest[r] = 0.f;
+            if constexpr (kFit)
+#pragma unroll
+                for (int e = 0; e < E; ++e) mean[r][e] = 0.f;
         }
         key_sums<R>(d, f.lanes);
         for (int t = 0; live && t < ring.turns && ring.ok; ++t) {
@@ -640,7 +648,10 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     d[r] = t;
                 }
 #pragma unroll
-                for (int u = 0; u < U; ++u) s[(R + r) * U + u] = seen[u] ? s[r * U + u] * (s[(R + r) * U + u] - d[r]) : 0.f;
+                for (int u = 0; u < U; ++u) {
+                    s[(R + r) * U + u] = seen[u] ? s[r * U + u] * (s[(R + r) * U + u] - d[r]) : 0.f;
+                    rest[r] += s[(R + r) * U + u];
+                }
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -651,6 +662,10 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 k.widen(w);
 #pragma unroll
                 for (int r = 0; r < R; ++r) axpy<E>(dq[r], s[(R + r) * U + u], w);
+                if constexpr (kFit)
+                    if (!one_turn)
+#pragma unroll
+                        for (int r = 0; r < R; ++r) axpy<E>(mean[r], s[r * U + u], w);
                 const int64_t j = x.kb + ring.first + t * ring.stride + u * kpw + grp;
                 if (kBoth && whole && x.on && j < x.ke) {
                     float dk[E], dv[E];
@@ -670,36 +685,62 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         if (live) ring.used += ring.turns;
         for (int o = wide; o < 32; o <<= 1)
 #pragma unroll
-            for (int r = 0; r < R; ++r)
+            for (int r = 0; r < R; ++r) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) dq[r][e] += __shfl_xor_sync(0xFFFFFFFFu, dq[r][e], o);
+                if constexpr (kFit) {
+                    rest[r] += __shfl_xor_sync(0xFFFFFFFFu, rest[r], o);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) mean[r][e] += __shfl_xor_sync(0xFFFFFFFFu, mean[r][e], o);
+                }
+            }
+        // the warps' sums of N values per lane together, in the first warp
+        auto join_warps = [&](auto &v, int n) {
+            __syncthreads();
+            if (grp == 0)
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (e < n) join[warp][e * 32 + lane] = v[e];
+            __syncthreads();
+            if (wu == 0 && grp == 0)
+                for (int w = 1; w < f.warps; ++w)
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        if (e < n) v[e] += join[warp + w][e * 32 + lane];
+        };
         RowWalk out(a, x, r0);
 #pragma unroll
         for (int r = 0; r < R; ++r, out.next(a)) {
             if (f.warps > 1) {
-                __syncthreads();
-                if (grp == 0)
-#pragma unroll
-                    for (int e = 0; e < E; ++e) join[warp][e * 32 + lane] = dq[r][e];
-                __syncthreads();
-                if (wu == 0 && grp == 0)
-                    for (int w = 1; w < f.warps; ++w)
-#pragma unroll
-                        for (int e = 0; e < E; ++e) dq[r][e] += join[warp + w][e * 32 + lane];
+                join_warps(dq[r], E);
+                if constexpr (kFit) {
+                    join_warps(mean[r], E);
+                    float one[E];
+                    one[0] = rest[r];
+                    join_warps(one, 1);
+                    rest[r] = one[0];
+                }
             }
             if (wu == 0 && grp == 0 && live && x.on && r0 + r < x.rows) {
                 const int64_t row = out.row;
                 const int head = out.head(a, x);
                 if (!kBoth && x.z == 0 && at == 0) dots[row * heads + head] = d[r];
                 if (f.splits == 1) {
+                    if constexpr (kFit)
+                        if (!one_turn) axpy<E>(dq[r], -rest[r], mean[r]);
                     store_piece<T, CPL>(static_cast<T *>(a.dq) + row * a.ldq2 + (int64_t)head * a.head_dim, at, f.lanes, f.chunks, dq[r], a.scale);
                 } else {
-                    const int64_t p = (((int64_t)x.z * a.q_rows + row) * heads + head) * a.head_dim;
+                    const int64_t cells = a.q_rows * heads, cell = (x.z * a.q_rows + row) * heads + head, means = f.splits * cells * a.head_dim;
 #pragma unroll
                     for (int c = 0; c < CPL; ++c)
                         if (at + c * f.lanes < f.chunks)
 #pragma unroll
-                            for (int e = 0; e < Chunk<T>::kElems; ++e) part_dq[p + (at + c * f.lanes) * Chunk<T>::kElems + e] = dq[r][c * Chunk<T>::kElems + e] * a.scale;
+                            for (int e = 0; e < Chunk<T>::kElems; ++e) {
+                                const int64_t p = cell * a.head_dim + (at + c * f.lanes) * Chunk<T>::kElems + e;
+                                part_dq[p] = dq[r][c * Chunk<T>::kElems + e] * a.scale;
+                                if constexpr (kFit) part_dq[means + p] = mean[r][c * Chunk<T>::kElems + e] * a.scale;
+                            }
+                    if (kFit && at == 0) part_dq[2 * means + cell] = rest[r];
                 }
             }
         }
@@ -824,7 +865,7 @@ template <typename T> bool backward_of(const AttnArgs &a, const FewPlan &p, FewS
     else if (p.rows == 2) ok = backward_rows<T, 2, true>(a, p, f, part_dq, dots, st);
     else ok = backward_rows<T, 4, true>(a, p, f, part_dq, dots, st);
     if (!ok) return false;
-    if (f.splits > 1 && a.q_rows) join_dq(a, f.splits, sizeof(T) == 4 ? E2EGREC_F32 : E2EGREC_BF16, part_dq, st);
+    if (f.splits > 1 && a.q_rows) join_dq(a, f.splits, sizeof(T) == 4 ? E2EGREC_F32 : E2EGREC_BF16, sizeof(T) == 2, part_dq, st);
     if (!p.both && a.k_rows) {
         note_launch();
         f.batches = (int)p.key_batches;
