@@ -509,9 +509,9 @@ typedef struct e2egrec_sequences {
 /* Attention of every sequence's queries to its keys and values, of another length:  for query row i of sequence s and head h,
  *     out_ih = sum_j p_ij v_jg,   p_ij = exp(scale q_ih . k_jg - lse_ih),   lse_ih = log sum_j exp(scale q_ih . k_jg)
  * over the visible keys j of s;  g = h / (n_heads / n_kv_heads) (n_heads a multiple of n_kv_heads: neighbouring query heads share
- * a key head).  A query that sees no key gets out = 0 and lse = -inf, and passes on no gradient.  What hidden keys and rows outside
+ * a key head); out overlaps no input.  A query that sees no key gets out = 0 and lse = -inf, and passes on no gradient.  What hidden keys and rows outside
  * the sequences hold (infinities, NaN) has no influence; rows of out, lse and of the gradients outside every sequence are left as
- * they were.  Q, out: [rows x n_heads head_dim]; K, V: [rows x n_kv_heads head_dim] of one number of rows; scale > 0.
+ * they were.  Q, out: [rows x n_heads head_dim]; K, V: [rows x n_kv_heads head_dim] of one number of rows; 0 < scale <= 1e38.
  *   lse     device float[Q rows x n_heads], row-major; may be NULL (serving: nothing is kept for a backward pass)
  *   status  optional device int32, receives E2EGREC_DEV_RANGE (or-ed) if offsets decrease or leave the matrices (the rows at fault
  *           are skipped) and E2EGREC_DEV_TIMEOUT if a wait inside a kernel ran out

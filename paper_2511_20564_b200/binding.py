@@ -809,6 +809,8 @@ def _elsewhere(t, stream):
 
 def _heads_mat(t, dev, name):
     """A matrix of heads as the library takes it: two dimensions, elements of a row side by side, on the call's device."""
+    if t is None:
+        raise E2EGrecError(f"{name}: a matrix is wanted, got None")
     shape, strides = t.shape, t.stride()
     if len(shape) != 2 or t.dtype not in _DTYPES or t.get_device() != dev or (strides[1] != 1 and shape[1] > 1):
         raise E2EGrecError(f"{name}: a [rows x heads * head_dim] float32 or bfloat16 matrix with adjacent columns on device {dev} is wanted, "
@@ -907,12 +909,13 @@ def qk_norm_rotary_backward(dQn, dKn, Q, K, n_heads: int, n_kv_heads: int, wq=No
         with ctx:
             return qk_norm_rotary_backward(dQn, dKn, Q, K, n_heads, n_kv_heads, wq, wk, freqs, pos_q, pos_k, eps, scale, interleaved, dQ, dK,
                                            gains, ws)
-    dev, hd = Q.get_device(), Q.shape[1] // max(n_heads, 1)
+    dev = Q.get_device()
+    q, hd = _heads_mat(Q, dev, "Q"), Q.shape[-1] // max(n_heads, 1)
     dQ = _packed_like(Q) if dQ is None else dQ
     dK = _packed_like(K) if dK is None and K is not None else dK
     dw = Q.new_empty((2, hd), dtype=torch.float32) if gains else None
     dwq, dwk = (None, None) if dw is None else (dw[0], None if K is None else dw[1])
-    q, gq, dq = _heads_mat(Q, dev, "Q"), _heads_mat(dQn, dev, "dQn"), _heads_mat(dQ, dev, "dQ")
+    gq, dq = _heads_mat(dQn, dev, "dQn"), _heads_mat(dQ, dev, "dQ")
     k, gk, dk = (None, None, None) if K is None else (_heads_mat(K, dev, "K"), _heads_mat(dKn, dev, "dKn"), _heads_mat(dK, dev, "dK"))
     args = _qk_arguments(Q, K, n_heads, n_kv_heads, wq, wk, eps, freqs, pos_q, pos_k, scale, interleaved, dev)
 
@@ -961,8 +964,8 @@ def cross_attention_forward(Q, K, V, seqs: Sequences, n_heads: int, n_kv_heads: 
         with ctx:
             return cross_attention_forward(Q, K, V, seqs, n_heads, n_kv_heads, scale, out, lse, keep_lse, status, ws)
     dev, rows = Q.get_device(), Q.shape[0]
-    s = seqs.check(dev, K.shape[0])
     q, k, v = _heads_mat(Q, dev, "Q"), _heads_mat(K, dev, "K"), _heads_mat(V, dev, "V")
+    s = seqs.check(dev, K.shape[0])
     out = _packed_like(Q) if out is None else out
     if lse is None and keep_lse:
         lse = Q.new_empty((rows, n_heads), dtype=torch.float32)
@@ -990,8 +993,8 @@ def cross_attention_backward(dOut, Q, K, V, out, lse, seqs: Sequences, n_heads: 
         with ctx:
             return cross_attention_backward(dOut, Q, K, V, out, lse, seqs, n_heads, n_kv_heads, scale, dQ, dK, dV, status, ws)
     dev = Q.get_device()
-    s = seqs.check(dev, K.shape[0])
     g, q, k, v, o = (_heads_mat(t, dev, n) for t, n in ((dOut, "dOut"), (Q, "Q"), (K, "K"), (V, "V"), (out, "out")))
+    s = seqs.check(dev, K.shape[0])
     dQ = _packed_like(Q) if dQ is None else dQ
     dK = _packed_like(K) if dK is None else dK
     dV = _packed_like(K) if dV is None else dV

@@ -210,7 +210,7 @@ int32_t check_shape(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_se
     if (n_kv_heads < 1 || n_heads < n_kv_heads || n_heads % n_kv_heads || Q->dim < 1 || Q->dim % n_heads) return E2EGREC_ERR_ARG;
     if (Q->rows < 0 || K->rows < 0 || Q->rows >= kMaxRows || K->rows >= kMaxRows) return E2EGREC_ERR_ARG;
     if (seqs->n_seq < 0 || seqs->n_seq > (kMaxRows - 1) / n_kv_heads || seqs->max_q < 0 || seqs->max_k < 0) return E2EGREC_ERR_ARG;
-    if (!(scale > 0.f) || !(scale <= 3.0e38f)) return E2EGREC_ERR_ARG;
+    if (!(scale > 0.f) || !(scale <= 1.0e38f)) return E2EGREC_ERR_ARG;
     if (Q->dim / n_heads > kMaxAttnDim) return E2EGREC_ERR_UNSUPPORTED;
     a.n_seq = seqs->n_seq;
     a.q_ptr = seqs->q_ptr;

@@ -8,6 +8,7 @@
 // steps of them, two rows to 4096 x 100 keys of 4 heads of 64 took 186 us, this way 74).  Each lane group keeps its own running maximum, sum and outputs over the keys it meets; groups, then the warps of a unit, then the stretches of a long list of keys are
 // joined at the end, in a fixed order.  A unit is up to R rows of one sequence and of each of its key heads.
 #include <algorithm>
+#include <atomic>
 
 #include "attention.cuh"
 #include "tcgen05.cuh"
@@ -794,7 +795,7 @@ unsigned few_grid(const AttnArgs &a, FewShape &f)
 template <int U> size_t few_smem(const FewShape &f) { return (size_t)kFewWarps * kStages * 2 * U * (32 / (f.lanes * f.heads)) * f.slice; }
 
 constexpr int kMaxDevices = 64;
-template <typename Kernel> bool allow_smem(Kernel kernel, bool (&done)[kMaxDevices])
+template <typename Kernel> bool allow_smem(Kernel kernel, std::atomic<bool> (&done)[kMaxDevices])
 {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return false;
@@ -807,7 +808,7 @@ template <typename Kernel> bool allow_smem(Kernel kernel, bool (&done)[kMaxDevic
 template <typename T, int R, int U>
 bool launch_fwd(const AttnArgs &a, FewShape f, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    static bool done[2][kMaxDevices] = {};
+    static std::atomic<bool> done[2][kMaxDevices] = {};
     const unsigned grid = few_grid(a, f);
     note_launch();
     if (f.chunks <= 32) {
@@ -823,7 +824,7 @@ bool launch_fwd(const AttnArgs &a, FewShape f, float *part_o, float2 *part_ml, c
 template <typename T, int R, int U, bool kBoth>
 bool launch_bwd(const AttnArgs &a, FewShape f, float *part_dq, float *dots, cudaStream_t st)
 {
-    static bool done[2][kMaxDevices] = {};
+    static std::atomic<bool> done[2][kMaxDevices] = {};
     const unsigned grid = few_grid(a, f);
     note_launch();
     if (f.chunks <= 32) {

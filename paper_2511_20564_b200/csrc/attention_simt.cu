@@ -9,6 +9,7 @@
 // 77 sequences of up to 61 x 307, heads of 36, forward and backward: 172 us with one tile at a time and one block per SM, 167 us so; 107 of 372 x 61, heads of 16: 598 and 440 us; 135 of 13 x 261,
 // heads of 100: 580 and 458 us.
 #include <algorithm>
+#include <atomic>
 
 #include "attention.cuh"
 #include "tcgen05.cuh"
@@ -480,7 +481,7 @@ attn_simt_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
 }
 
 constexpr int kMaxDevices = 64, kMostSmem = 226 * 1024, kSmSmem = 228 * 1024;
-template <typename Kernel> bool allow_smem(Kernel kernel, bool (&done)[kMaxDevices])
+template <typename Kernel> bool allow_smem(Kernel kernel, std::atomic<bool> (&done)[kMaxDevices])
 {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return false;
@@ -507,7 +508,7 @@ SimtShape shape_of(const AttnArgs &a, int64_t tiles, int splits, int kept_rows, 
 
 template <int C, int I> bool forward_of(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    static bool done[kMaxDevices] = {};
+    static std::atomic<bool> done[kMaxDevices] = {};
     if (!allow_smem(attn_simt_fwd_kernel<C, I>, done)) return false;
     size_t smem;
     const SimtShape f = shape_of(a, p.q_tiles, p.splits, 16 * I, 2 * kTile, 16 * I, blocks_of(C, I), smem);
@@ -518,7 +519,7 @@ template <int C, int I> bool forward_of(const AttnArgs &a, const SimtPlan &p, fl
 
 template <int C, int I> bool backward_of(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
 {
-    static bool done[2][kMaxDevices] = {};
+    static std::atomic<bool> done[2][kMaxDevices] = {};
     if (!allow_smem(attn_simt_dq_kernel<C, I>, done[0]) || !allow_smem(attn_simt_dkv_kernel<C, I>, done[1])) return false;
     size_t smem;
     if (a.q_rows) {

@@ -11,6 +11,7 @@
 // Every wait is bounded; when one runs out the block reports E2EGREC_DEV_TIMEOUT, lets its copies land, frees its tensor memory
 // and returns.
 #include <algorithm>
+#include <atomic>
 
 #include "attention.cuh"
 #include "tcgen05.cuh"
@@ -1201,7 +1202,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
 // ------------------------------------------------------------------------------------------------- host side
 constexpr int kMaxDevices = 64;
-template <typename Kernel> bool allow_smem(Kernel kernel, size_t bytes, bool (&done)[kMaxDevices])
+template <typename Kernel> bool allow_smem(Kernel kernel, size_t bytes, std::atomic<bool> (&done)[kMaxDevices])
 {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return false;
@@ -1246,7 +1247,7 @@ uint32_t tc_grid(uint32_t units, int blocks) { return units >= 8u * kSms * block
 
 template <int NB, int NT> bool launch_fwd(const AttnArgs &a, const Maps &m, const TcShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    static bool done[kMaxDevices] = {};
+    static std::atomic<bool> done[kMaxDevices] = {};
     using F = Fwd<NB, NT>;
     if (!allow_smem(attn_tc_fwd_kernel<NB, NT>, F::kSmem, done)) return false;
     note_launch();
@@ -1256,7 +1257,7 @@ template <int NB, int NT> bool launch_fwd(const AttnArgs &a, const Maps &m, cons
 
 template <int NB> bool launch_bwd(const AttnArgs &a, const Maps &m, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st)
 {
-    static bool done[2][kMaxDevices] = {};
+    static std::atomic<bool> done[2][kMaxDevices] = {};
     using B = Bwd<NB>;
     if (!allow_smem(attn_tc_dq_kernel<NB>, B::kDqSmem, done[0]) || !allow_smem(attn_tc_dkv_kernel<NB>, B::kDkvSmem, done[1])) return false;
     const int64_t units = a.n_seq * a.kv_heads;

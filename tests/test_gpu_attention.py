@@ -149,6 +149,44 @@ def test_sharp_and_rising_scores(lengths, dtype):
     p.check(p.run(E), p.want())
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv_heads,hd", [(130, 1, 8), (21, 3, 16), (48, 2, 128)])
+def test_many_query_heads_per_key_head(heads, kv_heads, hd, dtype):
+    """Groups larger than a tile has rows, and groups that do not divide its rows."""
+    import paper_2511_20564_b200 as E
+    p = Problem([3, 1, 0, 20], [70, 200, 9, 131], heads, kv_heads, hd, dtype, True)
+    p.check(p.run(E), p.want())
+
+
+def test_two_threads_at_once():
+    """Calls from two host threads on streams of their own, kernels of every kind used for the first time by both."""
+    import threading
+    import paper_2511_20564_b200 as E
+    problems = [Problem([3, 1, 40], [50, 260, 140], 4, 2, hd, dtype, seed=i, gap=0) for i, (hd, dtype) in enumerate([(48, BF16), (24, F32), (8, BF16), (112, F32)])]
+    results, errors = {}, []
+
+    def work(side):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(3):
+                    for i, p in enumerate(problems):
+                        results[side, i] = p.run(E)
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:          # handed to the test's own thread
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(side,)) for side in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
+    for i, p in enumerate(problems):
+        p.check(results[0, i], p.want())
+        for name, value in results[0, i].items():
+            assert torch.equal(value, results[1, i][name])
+
+
 def test_no_sequences_no_rows_no_lse():
     import paper_2511_20564_b200 as E
     x = _randn(4, 64, seed=1, dtype=BF16).cuda()

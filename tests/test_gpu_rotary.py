@@ -131,3 +131,18 @@ def test_many_rows_of_gains():
     n = h / (h.square().mean(-1, keepdim=True) + 1e-6).sqrt()
     terms = g.double().view(rows, heads, hd) * n
     assert ((dw - terms.sum((0, 1))).abs() <= (rows * heads / (148 * 4) + 700) * E24 * terms.abs().sum((0, 1))).all()
+
+
+def test_wrong_matrices_are_errors():
+    import paper_2511_20564_b200 as E
+    x, line, half = torch.zeros(4, 64, device="cuda"), torch.zeros(64, device="cuda"), torch.zeros(4, 64, device="cuda", dtype=torch.float16)
+    ptr = torch.tensor([0, 4], device="cuda")
+    seqs = E.Sequences(ptr, ptr)
+    lse = torch.zeros(4, 2, device="cuda")
+    for bad in (line, half, x.cpu(), x.t(), None):
+        for call in (lambda: E.qk_norm_rotary_backward(bad, None, x, None, 2, 1), lambda: E.qk_norm_rotary_forward(x, x, 2, 2, Qn=x if bad is None else bad, Kn=line),
+                     lambda: E.cross_attention_forward(x, bad, x, seqs, 2, 2, 1.0), lambda: E.cross_attention_backward(x, x, x, bad, x, lse, seqs, 2, 2, 1.0)):
+            with pytest.raises(E.E2EGrecError):
+                call()
+    with pytest.raises(E.E2EGrecError):
+        E.qk_norm_rotary_backward(line, None, line, None, 2, 1)
