@@ -793,6 +793,9 @@ def gate_fusion_backward(dFused: torch.Tensor, F: torch.Tensor, n_rows: int, gat
 ROTARY_INTERLEAVED, ROTARY_INVERSE = 1, 2
 _NO_WS = 256            # a workspace of this size is one that the library does not use
 _NO_WS_BUFFER = {}
+_ERR_WORKSPACE = -5
+_GAINS_WS = [_NO_WS]     # what the norms' backward pass takes, once a call has asked: the same for all sizes
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 # the current stream's handle without a stream object around it (that object costs half as much as a small call)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -802,7 +805,7 @@ def _elsewhere(t, stream):
     caller's stream on it, current (allocations inside belong to that stream)."""
     if not t.is_cuda:
         raise E2EGrecError("a tensor is not on a CUDA device")
-    if stream is None and torch.cuda.current_device() == t.get_device():
+    if stream is None and _current_device() == t.get_device():
         return None
     return torch.cuda.stream(torch.cuda.current_stream(t.device) if stream is None else stream)
 
@@ -842,6 +845,21 @@ def _scratch(need: int, device):
     if device not in _NO_WS_BUFFER:
         _NO_WS_BUFFER[device] = torch.empty(_NO_WS, dtype=torch.uint8, device=device)
     return _NO_WS_BUFFER[device]
+
+
+def _with_scratch(call, ws, device, what, need=_NO_WS):
+    """call(address, size) with the caller's workspace, or with one of the size that the library asks for: most calls need none,
+    so the first try, with `need` bytes, is also the size query."""
+    if ws is not None:
+        _check(call(ws.data_ptr(), C.c_size_t(ws.numel())), what)
+        return ws
+    ws, n = _scratch(need, device), C.c_size_t(need)
+    rc = call(ws.data_ptr(), n)
+    if rc == _ERR_WORKSPACE:
+        ws = _scratch(n.value, device)
+        rc = call(ws.data_ptr(), n)
+    _check(rc, what)
+    return ws
 
 
 def rotary_frequencies(rot_dim: int, base=10000.0, factor=1.0, trained_len=0.0, low=1.0, high=32.0, device="cuda", stream=None):
@@ -914,21 +932,23 @@ def qk_norm_rotary_backward(dQn, dKn, Q, K, n_heads: int, n_kv_heads: int, wq=No
     dQ = _packed_like(Q) if dQ is None else dQ
     dK = _packed_like(K) if dK is None and K is not None else dK
     dw = Q.new_empty((2, hd), dtype=torch.float32) if gains else None
-    dwq, dwk = (None, None) if dw is None else (dw[0], None if K is None else dw[1])
+    dwq, dwk = (None, None) if dw is None else dw.unbind()
+    if K is None:
+        dwk = None
     gq, dq = _heads_mat(dQn, dev, "dQn"), _heads_mat(dQ, dev, "dQ")
     k, gk, dk = (None, None, None) if K is None else (_heads_mat(K, dev, "K"), _heads_mat(dKn, dev, "dKn"), _heads_mat(dK, dev, "dK"))
     args = _qk_arguments(Q, K, n_heads, n_kv_heads, wq, wk, eps, freqs, pos_q, pos_k, scale, interleaved, dev)
 
     def call(ws_ptr, n):
-        _check(lib().e2egrec_qk_norm_rotary_backward(C.byref(gq), _ref(gk), C.byref(q), _ref(k), *args, C.byref(dq), _ref(dk),
+        return lib().e2egrec_qk_norm_rotary_backward(C.byref(gq), _ref(gk), C.byref(q), _ref(k), *args, C.byref(dq), _ref(dk),
                                                      None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(),
-                                                     ws_ptr, C.byref(n), _raw_stream(dev)), "e2egrec_qk_norm_rotary_backward")
+                                                     ws_ptr, C.byref(n), _raw_stream(dev))
 
     if ws is None:
-        n = C.c_size_t(0)
-        call(None, n)
-        ws = _scratch(n.value, Q.device)
-    call(ws.data_ptr(), C.c_size_t(ws.numel()))
+        ws = _with_scratch(call, None, Q.device, "e2egrec_qk_norm_rotary_backward", _GAINS_WS[0])
+        _GAINS_WS[0] = ws.numel()
+    else:
+        _with_scratch(call, ws, Q.device, "e2egrec_qk_norm_rotary_backward")
     return dQ, dK, dwq, dwk, ws
 
 
@@ -973,14 +993,10 @@ def cross_attention_forward(Q, K, V, seqs: Sequences, n_heads: int, n_kv_heads: 
     lp, sp = _vector(lse, dev, torch.float32, rows * n_heads, "lse"), _vector(status, dev, torch.int32, 1, "status")
 
     def call(ws_ptr, n):
-        _check(lib().e2egrec_cross_attention_forward(C.byref(q), C.byref(k), C.byref(v), s, n_heads, n_kv_heads, scale, C.byref(o), lp, sp,
-                                                     ws_ptr, C.byref(n), _raw_stream(dev)), "e2egrec_cross_attention_forward")
+        return lib().e2egrec_cross_attention_forward(C.byref(q), C.byref(k), C.byref(v), s, n_heads, n_kv_heads, scale, C.byref(o), lp, sp,
+                                                     ws_ptr, C.byref(n), _raw_stream(dev))
 
-    if ws is None:
-        n = C.c_size_t(0)
-        call(None, n)
-        ws = _scratch(n.value, Q.device)
-    call(ws.data_ptr(), C.c_size_t(ws.numel()))
+    ws = _with_scratch(call, ws, Q.device, "e2egrec_cross_attention_forward")
     return out, lse, ws
 
 
@@ -1002,13 +1018,8 @@ def cross_attention_backward(dOut, Q, K, V, out, lse, seqs: Sequences, n_heads: 
     lp, sp = _vector(lse, dev, torch.float32, Q.shape[0] * n_heads, "lse"), _vector(status, dev, torch.int32, 1, "status")
 
     def call(ws_ptr, n):
-        _check(lib().e2egrec_cross_attention_backward(C.byref(g), C.byref(q), C.byref(k), C.byref(v), C.byref(o), lp, s, n_heads, n_kv_heads, scale,
-                                                      C.byref(dq), C.byref(dk), C.byref(dv), sp, ws_ptr, C.byref(n), _raw_stream(dev)),
-               "e2egrec_cross_attention_backward")
+        return lib().e2egrec_cross_attention_backward(C.byref(g), C.byref(q), C.byref(k), C.byref(v), C.byref(o), lp, s, n_heads, n_kv_heads, scale,
+                                                      C.byref(dq), C.byref(dk), C.byref(dv), sp, ws_ptr, C.byref(n), _raw_stream(dev))
 
-    if ws is None:
-        n = C.c_size_t(0)
-        call(None, n)
-        ws = _scratch(n.value, Q.device)
-    call(ws.data_ptr(), C.c_size_t(ws.numel()))
+    ws = _with_scratch(call, ws, Q.device, "e2egrec_cross_attention_backward")
     return dQ, dK, dV, ws
