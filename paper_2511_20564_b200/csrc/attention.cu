@@ -186,7 +186,7 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     }
     if (backward && !(p.path == Path::few && p.few.both)) p.dot_bytes = align_up(cells * sizeof(float), 256);
     if (p.splits > 1) {
-        const bool fit = backward && p.path == Path::few && dtype == E2EGREC_BF16;       // as attn_few_bwd_kernel's kFit
+        const bool fit = backward && p.path == Path::few && p.few.fit;
         p.part_bytes = align_up(p.splits * cells * (fit ? 2 * a.head_dim + 1 : a.head_dim) * sizeof(float), 256);
         if (!backward) p.ml_bytes = align_up(p.splits * cells * sizeof(float2), 256);
     }

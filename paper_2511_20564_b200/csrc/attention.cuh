@@ -68,13 +68,14 @@ struct FewPlan {
     int rows;                             // rows per unit
     int steps;                            // steps of keys in flight per warp
     bool both;                            // backward: one kernel for dQ, dK and dV
+    bool fit;                             // backward, bf16, more keys than one turn: dQ without what D of the stored outputs lacks
     int64_t batches;                      // units of rows per sequence and key head
     int warps, splits;                    // warps per unit, stretches of the keys
     int64_t key_batches;                  // units of keys of the dK, dV kernel
 };
 FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool backward);
 bool few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_o, float2 *part_ml, cudaStream_t st);
-// part_dq: [splits x q_rows x heads x head_dim] where splits > 1, with bf16 twice that and [splits x q_rows x heads]; dots: [q_rows x heads] where !both
+// part_dq: [splits x q_rows x heads x head_dim] where splits > 1, twice that and [splits x q_rows x heads] with fit; dots: [q_rows x heads] where !both
 bool few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st);
 
 // dQ of stretches of the keys -> dQ, in order

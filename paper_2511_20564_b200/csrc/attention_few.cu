@@ -535,9 +535,10 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
 // that is longer than the launch was sized for has its rows done batch by batch and its keys' gradients apart.
 // Where all keys are in one turn of the warp, D = sum_j p_j dP_j is formed from what the registers hold instead of the stored
 // outputs: with a handful of keys dP - D cancels, and the rounding of 16-bit outputs showed (dQ of three keys 3.1e-3 off, 2.0e-3 so).
-// Over more keys D comes from the stored outputs, and what 16-bit ones lack, sum_j dS_j (0 with the exact D), is taken out at the end:
-// dQ = sum_j dS_j k_j - (sum_j dS_j) (sum_j p_j k_j).  dQ of rows that see 12 000 keys was 3.4e-3 off without it, a rounding 1.7e-3.
-template <typename T, int R, int U, int CPL, bool kBoth>
+// Over more keys (kFit) D comes from the stored outputs, and what 16-bit ones lack, sum_j dS_j (0 with the exact D), is taken out at the end:
+// dQ = sum_j dS_j k_j - (sum_j dS_j) (sum_j p_j k_j).  dQ of rows that see 12 000 keys was 3.4e-3 off without it, 1.8e-3 so (a rounding:
+// 1.7e-3).
+template <typename T, int R, int U, int CPL, bool kBoth, bool kFit>
 __global__ void __launch_bounds__(kFewThreads, CPL == 2 || R > 2 ? 2 : (R == 1 ? 4 : 3))
 attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_dq, float *__restrict__ dots)
 {
@@ -547,7 +548,6 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     __shared__ uint32_t seen_words[kFewWarps * kStages];
     __shared__ int abort_flag;
     __shared__ float join[kFewWarps][E * 32];
-    constexpr bool kFit = sizeof(T) == 2;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wu = warp & (f.warps - 1);
     const Unit x = few_unit(a, f, blockIdx.x * (uint32_t)(kFewWarps / f.warps) + warp / f.warps);
@@ -689,12 +689,16 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             for (int r = 0; r < R; ++r) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) dq[r][e] += __shfl_xor_sync(0xFFFFFFFFu, dq[r][e], o);
-                if constexpr (kFit) {
-                    rest[r] += __shfl_xor_sync(0xFFFFFFFFu, rest[r], o);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) mean[r][e] += __shfl_xor_sync(0xFFFFFFFFu, mean[r][e], o);
-                }
             }
+        if constexpr (kFit)
+            if (!one_turn)
+                for (int o = wide; o < 32; o <<= 1)
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        rest[r] += __shfl_xor_sync(0xFFFFFFFFu, rest[r], o);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) mean[r][e] += __shfl_xor_sync(0xFFFFFFFFu, mean[r][e], o);
+                    }
         // the warps' sums of N values per lane together, in the first warp
         auto join_warps = [&](auto &v, int n) {
             __syncthreads();
@@ -821,18 +825,18 @@ bool launch_fwd(const AttnArgs &a, FewShape f, float *part_o, float2 *part_ml, c
     return true;
 }
 
-template <typename T, int R, int U, bool kBoth>
+template <typename T, int R, int U, bool kBoth, bool kFit>
 bool launch_bwd(const AttnArgs &a, FewShape f, float *part_dq, float *dots, cudaStream_t st)
 {
     static std::atomic<bool> done[2][kMaxDevices] = {};
     const unsigned grid = few_grid(a, f);
     note_launch();
     if (f.chunks <= 32) {
-        if (!allow_smem(attn_few_bwd_kernel<T, R, U, 1, kBoth>, done[0])) return false;
-        attn_few_bwd_kernel<T, R, U, 1, kBoth><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_dq, dots);
+        if (!allow_smem(attn_few_bwd_kernel<T, R, U, 1, kBoth, kFit>, done[0])) return false;
+        attn_few_bwd_kernel<T, R, U, 1, kBoth, kFit><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_dq, dots);
     } else if constexpr (sizeof(T) == 4) {
-        if (!allow_smem(attn_few_bwd_kernel<T, R, U, 2, kBoth>, done[1])) return false;
-        attn_few_bwd_kernel<T, R, U, 2, kBoth><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_dq, dots);
+        if (!allow_smem(attn_few_bwd_kernel<T, R, U, 2, kBoth, kFit>, done[1])) return false;
+        attn_few_bwd_kernel<T, R, U, 2, kBoth, kFit><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_dq, dots);
     }
     return true;
 }
@@ -851,11 +855,19 @@ template <typename T> bool forward_of(const AttnArgs &a, const FewPlan &p, const
     return forward_rows<T, 4>(a, p, f, part_o, part_ml, st);
 }
 
+template <typename T, int R, bool kBoth, bool kFit>
+bool backward_steps(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_dq, float *dots, cudaStream_t st)
+{
+    if (p.steps == 1) return launch_bwd<T, R, 1, kBoth, kFit>(a, f, part_dq, dots, st);
+    if (p.steps == 2) return launch_bwd<T, R, 2, kBoth, kFit>(a, f, part_dq, dots, st);
+    return launch_bwd<T, R, kUnroll, kBoth, kFit>(a, f, part_dq, dots, st);
+}
+
 template <typename T, int R, bool kBoth> bool backward_rows(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_dq, float *dots, cudaStream_t st)
 {
-    if (p.steps == 1) return launch_bwd<T, R, 1, kBoth>(a, f, part_dq, dots, st);
-    if (p.steps == 2) return launch_bwd<T, R, 2, kBoth>(a, f, part_dq, dots, st);
-    return launch_bwd<T, R, kUnroll, kBoth>(a, f, part_dq, dots, st);
+    if constexpr (sizeof(T) == 2)
+        if (p.fit) return backward_steps<T, R, kBoth, true>(a, p, f, part_dq, dots, st);
+    return backward_steps<T, R, kBoth, false>(a, p, f, part_dq, dots, st);
 }
 
 template <typename T> bool backward_of(const AttnArgs &a, const FewPlan &p, FewShape f, float *part_dq, float *dots, cudaStream_t st)
@@ -866,7 +878,7 @@ template <typename T> bool backward_of(const AttnArgs &a, const FewPlan &p, FewS
     else if (p.rows == 2) ok = backward_rows<T, 2, true>(a, p, f, part_dq, dots, st);
     else ok = backward_rows<T, 4, true>(a, p, f, part_dq, dots, st);
     if (!ok) return false;
-    if (f.splits > 1 && a.q_rows) join_dq(a, f.splits, sizeof(T) == 4 ? E2EGREC_F32 : E2EGREC_BF16, sizeof(T) == 2, part_dq, st);
+    if (f.splits > 1 && a.q_rows) join_dq(a, f.splits, sizeof(T) == 4 ? E2EGREC_F32 : E2EGREC_BF16, p.fit, part_dq, st);
     if (!p.both && a.k_rows) {
         note_launch();
         f.batches = (int)p.key_batches;
@@ -893,6 +905,7 @@ FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool b
     p.steps = max_k <= step ? 1 : (max_k <= 2 * step || (p.rows > 2 && max_k > kUnroll * step) ? 2 : kUnroll);
     while (p.steps * step > 32) p.steps /= 2;        // a turn's rows are the bits of a word
     const int64_t turn = step * p.steps;
+    p.fit = backward && es == 2 && max_k > turn;
     p.batches = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, p.rows), most));
     const int64_t want = std::max<int64_t>(1, std::min(ceil_div(148 * 24, units0 * p.batches), ceil_div(max_k, turn)));
     p.warps = 1;
