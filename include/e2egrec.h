@@ -521,7 +521,7 @@ typedef struct e2egrec_sequences {
  *     dV_jg = sum_ih p_ij dOut_ih,  dS_ij = p_ij (dOut_ih . v_jg - dOut_ih . out_ih),  dQ_ih = scale sum_j dS_ij k_jg,
  *     dK_jg = scale sum_ih dS_ij q_ih   (i over the queries of s, h over the query heads of g).
  * Rows of hidden keys get zeros.  dOut, dQ have Q's shape, dK, dV that of K; none may overlap an input.  No floating-point atomics:
- * results are the same bits from run to run.  With bf16, p and dS are rounded to bf16 where the products run on the tensor cores.
+ * results are the same bits from run to run.  With bf16, p and dS are rounded to bf16 where the products run on the tensor cores (dS of dQ to two such values).
  * Every matrix of both calls: heads as above. */
 int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V, const e2egrec_sequences *seqs,
                                         int32_t n_heads, int32_t n_kv_heads, float scale, const e2egrec_mat *out, float *lse,

@@ -607,6 +607,20 @@ __device__ inline void store_operand(uint32_t taddr, const float (&v)[64])
     tmem_store32(taddr, r);
 }
 
+// The same, and what the rounding to bf16 leaves out as a second operand
+__device__ inline void store_operand_and_rest(uint32_t taddr, uint32_t rest, float (&v)[64])
+{
+    uint32_t r[32];
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        r[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+        v[2 * i] -= __uint_as_float(r[i] << 16);
+        v[2 * i + 1] -= __uint_as_float(r[i] & 0xFFFF0000u);
+    }
+    tmem_store32(taddr, r);
+    store_operand(rest, v);
+}
+
 // One row (up to 64 NB columns) of an accumulator -> out, times f; zeros where !keep
 template <int NB>
 __device__ inline void store_row(uint32_t taddr, bf16 *out, int head_dim, float f, bool have, bool keep, bool write)
@@ -631,7 +645,9 @@ __device__ inline void store_row(uint32_t taddr, bf16 *out, int head_dim, float 
     }
 }
 
-// dQ, and D = dO . out of every row for the other kernel
+// dQ, and D = dO . out of every row for the other kernel.  dS goes into its product as two bf16 operands, its rounding and the rest: D comes
+// from 16-bit outputs already, and with dS rounded as well dQ was 2.5 to 2.7e-3 off in the mean (a rounding of the result: 1.8e-3),
+// at most 2.4e-3 so, dK included; the training case's backward pass takes 550 us with one operand, 585 us so.
 template <int NB>
 __global__ void __launch_bounds__(Bwd<NB>::kThreads, 1)
 attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_k,
@@ -782,14 +798,18 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                             ok = tile_ready(&k_clean[jj % kWordRing], (jj / kWordRing) & 1u, &abort_flag) && mbar_wait(&ds_full, jj & 1u, &abort_flag);
                             if (!ok) break;
                             tc_fence_after();
-                            row_steps(tmem + 384, tmem + 256, 32, make_smem_desc_mn(kv_smem + (g % kStages) * kTileBytes, kBlockBytes), id_o, j > 0);
-                            umma_commit(&kv_empty[g % kStages]);
+                            const uint64_t k_desc = make_smem_desc_mn(kv_smem + (g % kStages) * kTileBytes, kBlockBytes);
+                            row_steps(tmem + 384, tmem + 256, 32, k_desc, id_o, j > 0);
                             if (j + 1 < x.n) {
                                 if (!full(g + 3)) break;
                                 product(tmem + 256, g_desc, g + 3);
                                 umma_commit(&dp_full);
                                 umma_commit(&kv_empty[(g + 3) % kStages]);
-                            } else {
+                            }
+                            // the rest of dS, where the scores were: behind dP, which the warpgroups wait for
+                            row_steps(tmem + 384, tmem + (jj & 1u) * kTile, 32, k_desc, id_o, true);
+                            umma_commit(&kv_empty[g % kStages]);
+                            if (j + 1 == x.n) {
                                 umma_commit(&o_full);
                                 umma_commit(&q_empty);
                             }
@@ -874,7 +894,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                                 if (!((word >> e) & 1u)) p[c * 32 + e] = 0.f;
                         }
                     }
-                    store_operand(tmem + lanes + 256 + q * 64, p);
+                    store_operand_and_rest(tmem + lanes + 256 + q * 64, tmem + lanes + (jj & 1u) * kTile + q * 64, p);
                     tmem_store_wait();
                     tc_fence_before();
                     __syncwarp();
