@@ -509,9 +509,10 @@ typedef struct e2egrec_sequences {
 /* Attention of every sequence's queries to its keys and values, of another length:  for query row i of sequence s and head h,
  *     out_ih = sum_j p_ij v_jg,   p_ij = exp(scale q_ih . k_jg - lse_ih),   lse_ih = log sum_j exp(scale q_ih . k_jg)
  * over the visible keys j of s;  g = h / (n_heads / n_kv_heads) (n_heads a multiple of n_kv_heads: neighbouring query heads share
- * a key head); out overlaps no input.  A query that sees no key gets out = 0 and lse = -inf, and passes on no gradient.  What hidden keys and rows outside
- * the sequences hold (infinities, NaN) has no influence; rows of out, lse and of the gradients outside every sequence are left as
- * they were.  Q, out: [rows x n_heads head_dim]; K, V: [rows x n_kv_heads head_dim] of one number of rows; 0 < scale <= 1e38.
+ * a key head); out overlaps no input.  A query that sees no key gets out = 0 and lse = -inf, and passes on no gradient.  What
+ * hidden keys and rows outside the sequences hold (infinities, NaN) has no influence; rows of out, lse and of the gradients outside
+ * every sequence are left as they were.  Q, out: [rows x n_heads head_dim]; K, V: [rows x n_kv_heads head_dim] of one number of
+ * rows; 0 < scale <= 1e38.
  *   lse     device float[Q rows x n_heads], row-major; may be NULL (serving: nothing is kept for a backward pass)
  *   status  optional device int32, receives E2EGREC_DEV_RANGE (or-ed) if offsets decrease or leave the matrices (the rows at fault
  *           are skipped) and E2EGREC_DEV_TIMEOUT if a wait inside a kernel ran out
@@ -521,8 +522,8 @@ typedef struct e2egrec_sequences {
  *     dV_jg = sum_ih p_ij dOut_ih,  dS_ij = p_ij (dOut_ih . v_jg - dOut_ih . out_ih),  dQ_ih = scale sum_j dS_ij k_jg,
  *     dK_jg = scale sum_ih dS_ij q_ih   (i over the queries of s, h over the query heads of g).
  * Rows of hidden keys get zeros.  dOut, dQ have Q's shape, dK, dV that of K; none may overlap an input.  No floating-point atomics:
- * results are the same bits from run to run.  With bf16, p and dS are rounded to bf16 where the products run on the tensor cores (dS of dQ to two such values).
- * Every matrix of both calls: heads as above. */
+ * results are the same bits from run to run.  With bf16, p and dS are rounded to bf16 where the products run on the tensor cores
+ * (dS of dQ to two such values).  Every matrix of both calls: heads as above. */
 int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V, const e2egrec_sequences *seqs,
                                         int32_t n_heads, int32_t n_kv_heads, float scale, const e2egrec_mat *out, float *lse,
                                         int32_t *status, void *ws, size_t *ws_bytes, void *stream);
