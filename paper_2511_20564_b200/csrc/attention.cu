@@ -144,8 +144,8 @@ int32_t check_heads(const e2egrec_mat *m, int32_t heads, int32_t head_dim, int32
 
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
 
-// The kernels of a call.  A sequence's keys and rows stream (attention_few.cu) where a key head has up to two rows (four in the
-// backward pass), or where a sequence is so small that the set-up of a tile costs more than its products; bf16 heads of up to 128
+// The kernels of a call.  A sequence's keys and rows stream (attention_few.cu) where a key head has up to two rows (fp32 three: 300 of
+// 3 x 200, 88 us against 113; four in the backward pass), or where a sequence is so small that the set-up of a tile costs more than its products; bf16 heads of up to 128
 // go to the tensor cores otherwise, fp32 ones to tiles of fp32 FMA, wider heads always stream.
 enum class Path { few, tc, simt };
 
@@ -166,7 +166,7 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     const int64_t max_q = s.max_q ? std::min(s.max_q, a.q_rows) : a.q_rows, max_k = s.max_k ? std::min(s.max_k, a.k_rows) : a.k_rows;
     const int64_t rows = max_q * a.group, units = std::max<int64_t>(a.n_seq * a.kv_heads, 1);
     const size_t cells = (size_t)a.q_rows * a.kv_heads * a.group;
-    const bool small = rows <= (backward ? 4 : 2) || rows * max_k <= (dtype == E2EGREC_F32 ? 256 : backward ? 700 : 800);
+    const bool small = rows <= (backward ? 4 : dtype == E2EGREC_F32 ? 3 : 2) || rows * max_k <= (dtype == E2EGREC_F32 ? 256 : backward ? 700 : 800);
     // (without rows on one side there is nothing to form a product of)
     p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
     if (p.path == Path::tc) {

@@ -1,13 +1,15 @@
 // Attention of fp32 sequences on fp32 FMA (head_dim <= 128): scores to fp32 accuracy, which neither TF32 nor bf16 products give.
 //
-// Tiles of 16 I rows x 64 keys, I = 1, 2 or 4 by the rows that a key head has.  256 threads: thread (ty, tx) of 16 x 16 forms the I x 4
-// scores of rows I ty + i and keys tx + 16 j as dot products of row-major tiles, four elements of each at a time (with I = 4 eight
-// 16-byte reads of shared memory for 64 FMA).  Tiles have rows of an odd number of 16-byte units, so that eight neighbouring rows lie
-// in different banks.  p and dS go through shared memory; the products with V, K, dO and Q are outer products over the same row-major
-// tiles, columns 4 cx + 64 c; of heads of at most 32 columns the threads of a row take a part of the summed index each, which are added
-// up once at the end.  The next tiles are on their way beside a tile's products where shared memory holds both.
-// 77 sequences of up to 61 x 307, heads of 36, forward and backward: 172 us with one tile at a time and one block per SM, 167 us so; 107 of 372 x 61, heads of 16: 598 and 440 us; 135 of 13 x 261,
-// heads of 100: 580 and 458 us.
+// Tiles of 16 I rows x 64 keys, I = 1, 2 or 4 by the rows that a key head has.  16 x TX threads: thread (ty, tx) forms the scores of
+// rows ty + 16 i and keys tx + TX j as dot products of row-major tiles, four elements of each at a time.  TX = 8 where there are up to 32
+// rows (more scores per thread, whose reads of shared memory are whole lines) and in the forward pass of heads of up to 32 columns,
+// TX = 16 else, which leaves the schedulers twice the warps.  Tiles have rows of an odd number of 16-byte units, so that eight neighbouring
+// rows lie in different banks.  p and dS go through shared memory; the products with V, K, dO and Q are outer products over the same
+// row-major tiles, columns 4 cx + 4 TX c; of narrow heads the threads of a row take a part of the summed index each, which are added up
+// once at the end.  The next tiles are on their way beside a tile's products where shared memory holds both.
+// Reads of shared memory and their latency bound it (8 x 512 x 2048, heads of 64: their pipe 65 %, FMA 48 %; tiles by bulk copies instead
+// of cp.async change nothing).  Forward and backward, us with TX = 16 everywhere and with this rule: 107 of 372 x 61, heads of 16: 440,
+// 417; 300 of 8 x 200, heads of 64: 467, 435; 1000 of 8 x 40, heads of 64: 424, 374.  77 of up to 61 x 307, heads of 36: 166.
 #include <algorithm>
 #include <atomic>
 
@@ -17,16 +19,16 @@
 namespace e2egrec {
 namespace {
 
-constexpr int kTile = 64, kThreads = 256, kLdP = kTile + 4;
+constexpr int kTile = 64, kLdP = kTile + 4;
 
-// Blocks per SM: one where the sums of 64 rows of wide heads take the registers of two
-constexpr int blocks_of(int C, int I) { return C == 2 && I == 4 ? 1 : 2; }
+// Blocks per SM, by the registers that the sums take; C columns per thread, in fours
+constexpr int blocks_of(int TX, int C, int I) { return TX == 8 ? 3 : (C == 2 && I == 4 ? 1 : 2); }
 
 struct SimtShape {
     int ld;                               // floats from row to row of a tile in shared memory
     int tiles, splits;                    // blocks of rows (or keys) per sequence and key head; stretches of the keys
     int stages;                           // tiles of the side that a block goes over: 2: one lands beside the products of the other
-    int cols;                             // threads side by side over a head's columns (a power of two), 16 / cols parts of the sums
+    int cols;                             // threads side by side over a head's columns (a power of two), TX / cols parts of the sums
 };
 
 __device__ inline float exp2_fast(float x)
@@ -36,17 +38,17 @@ __device__ inline float exp2_fast(float x)
     return y;
 }
 
-// sums and maxima over the 16 threads that share rows
-__device__ inline float row_sum(float v)
+// sums and maxima over the TX threads that share rows
+template <int TX> __device__ inline float row_sum(float v)
 {
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    for (int o = TX / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
     return v;
 }
-__device__ inline float row_max(float v)
+template <int TX> __device__ inline float row_max(float v)
 {
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    for (int o = TX / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
     return v;
 }
 
@@ -58,34 +60,36 @@ template <int kPer> __device__ inline void load_tile(float *tile, const SimtShap
     for (int u = threadIdx.x % kPer; u * 4 < head_dim; u += kPer) cp_async16(dst + u * 16, src ? static_cast<const void *>(src + u * 4) : any, src != nullptr);
 }
 
-// s[i][j] = a[I ty + i] . b[tx + 16 j]
-template <int I> __device__ inline void scores(const float *a, const float *b, int ld, int head_dim, int ty, int tx, float (&s)[I][4])
+// s[i][j] = a[ty + 16 i] . b[tx + TX j]
+template <int TX, int I> __device__ inline void scores(const float *a, const float *b, int ld, int head_dim, int ty, int tx, float (&s)[I][kTile / TX])
 {
-    const float *pa = a + I * ty * ld, *pb = b + tx * ld;
-    float2 t[I][4];
+    constexpr int J = kTile / TX;
+    const float *pa = a + ty * ld, *pb = b + tx * ld;
+    float2 t[I][J];
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) t[i][j] = make_float2(0.f, 0.f);
+        for (int j = 0; j < J; ++j) t[i][j] = make_float2(0.f, 0.f);
 #pragma unroll 2
     for (int d = 0; d < head_dim; d += 4) {
-        float4 x[I], y[4];
+        float4 x[I], y[J];
 #pragma unroll
-        for (int i = 0; i < I; ++i) x[i] = *reinterpret_cast<const float4 *>(pa + i * ld + d);
+        for (int i = 0; i < I; ++i) x[i] = *reinterpret_cast<const float4 *>(pa + 16 * i * ld + d);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4 *>(pb + 16 * j * ld + d);
+        for (int j = 0; j < J; ++j) y[j] = *reinterpret_cast<const float4 *>(pb + TX * j * ld + d);
 #pragma unroll
         for (int i = 0; i < I; ++i)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                t[i][j] = __ffma2_rn(make_float2(x[i].x, x[i].y), make_float2(y[j].x, y[j].y), t[i][j]);
-                t[i][j] = __ffma2_rn(make_float2(x[i].z, x[i].w), make_float2(y[j].z, y[j].w), t[i][j]);
-            }
+            for (int j = 0; j < J; ++j) t[i][j] = __ffma2_rn(make_float2(x[i].x, x[i].y), make_float2(y[j].x, y[j].y), t[i][j]);
+#pragma unroll
+        for (int i = 0; i < I; ++i)
+#pragma unroll
+            for (int j = 0; j < J; ++j) t[i][j] = __ffma2_rn(make_float2(x[i].z, x[i].w), make_float2(y[j].z, y[j].w), t[i][j]);
     }
 #pragma unroll
     for (int i = 0; i < I; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[i][j] = t[i][j].x + t[i][j].y;
+        for (int j = 0; j < J; ++j) s[i][j] = t[i][j].x + t[i][j].y;
 }
 
 __device__ inline void fma4(float (&o)[4], float w, const float4 &v)
@@ -98,44 +102,44 @@ __device__ inline void fma4(float (&o)[4], float w, const float4 &v)
     o[3] = b.y;
 }
 
-// Columns 4 cx + 64 c of a head, part `part` of the sums
-struct Columns {
+// Columns 4 cx + 4 TX c of a head, part `part` of the sums
+template <int TX> struct Columns {
     int cx, part, parts;
-    __device__ inline Columns(const SimtShape &f, int tx) : cx(tx & (f.cols - 1)), part(tx / f.cols), parts(16 / f.cols) {}
+    __device__ inline Columns(const SimtShape &f, int tx) : cx(tx & (f.cols - 1)), part(tx / f.cols), parts(TX / f.cols) {}
 };
 
-// o[i][c] += sum_k w[I ty + i][k] b[k][4 cx + 64 c]     (w row by row)
-template <int C, int I>
-__device__ inline void add_rows(float (&o)[I][C][4], const float *w, const float *b, int ld, int head_dim, int ty, const Columns &at)
+// o[i][c] += sum_k w[ty + 16 i][k] b[k][4 cx + 4 TX c]     (w row by row)
+template <int C, int I, int TX>
+__device__ inline void add_rows(float (&o)[I][C][4], const float *w, const float *b, int ld, int head_dim, int ty, const Columns<TX> &at)
 {
 #pragma unroll 2
     for (int k = at.part * 4; k < kTile; k += at.parts * 4) {
         float4 x[I];
 #pragma unroll
-        for (int i = 0; i < I; ++i) x[i] = *reinterpret_cast<const float4 *>(w + (I * ty + i) * kLdP + k);
+        for (int i = 0; i < I; ++i) x[i] = *reinterpret_cast<const float4 *>(w + (ty + 16 * i) * kLdP + k);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if (4 * at.cx + 64 * c >= head_dim) continue;
+            if (4 * at.cx + 4 * TX * c >= head_dim) continue;
 #pragma unroll
             for (int n = 0; n < 4; ++n) {
-                const float4 v = *reinterpret_cast<const float4 *>(b + (k + n) * ld + 4 * at.cx + 64 * c);
+                const float4 v = *reinterpret_cast<const float4 *>(b + (k + n) * ld + 4 * at.cx + 4 * TX * c);
 #pragma unroll
                 for (int i = 0; i < I; ++i) fma4(o[i][c], n == 0 ? x[i].x : n == 1 ? x[i].y : n == 2 ? x[i].z : x[i].w, v);
             }
         }
     }
 }
-// o[i][c] += sum_r w[r][4 ty + i] b[r][4 cx + 64 c]     (w column by column, 16 I rows)
-template <int C, int I>
-__device__ inline void add_columns(float (&o)[4][C][4], const float *w, const float *b, int ld, int head_dim, int ty, const Columns &at)
+// o[i][c] += sum_r w[r][4 ty + i] b[r][4 cx + 4 TX c]     (w column by column, 16 I rows)
+template <int C, int I, int TX>
+__device__ inline void add_columns(float (&o)[4][C][4], const float *w, const float *b, int ld, int head_dim, int ty, const Columns<TX> &at)
 {
 #pragma unroll 4
     for (int r = at.part; r < 16 * I; r += at.parts) {
         const float4 x = *reinterpret_cast<const float4 *>(w + r * kLdP + 4 * ty);
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if (4 * at.cx + 64 * c >= head_dim) continue;
-            const float4 v = *reinterpret_cast<const float4 *>(b + r * ld + 4 * at.cx + 64 * c);
+            if (4 * at.cx + 4 * TX * c >= head_dim) continue;
+            const float4 v = *reinterpret_cast<const float4 *>(b + r * ld + 4 * at.cx + 4 * TX * c);
             fma4(o[0][c], x.x, v);
             fma4(o[1][c], x.y, v);
             fma4(o[2][c], x.z, v);
@@ -144,14 +148,14 @@ __device__ inline void add_columns(float (&o)[4][C][4], const float *w, const fl
     }
 }
 // the parts of the sums together, in every thread (all of a warp)
-template <int C, int N> __device__ inline void add_parts(float (&o)[N][C][4], const SimtShape &f)
+template <int TX, int C, int N> __device__ inline void add_parts(float (&o)[N][C][4], const SimtShape &f)
 {
-    if (C > 1) return;
-    for (int off = f.cols; off < 16; off <<= 1)
+    if constexpr (C == 1)
+        for (int off = f.cols; off < TX; off <<= 1)
 #pragma unroll
-        for (int i = 0; i < N; ++i)
+            for (int i = 0; i < N; ++i)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[i][0][e] += __shfl_xor_sync(0xFFFFFFFFu, o[i][0][e], off);
+                for (int e = 0; e < 4; ++e) o[i][0][e] += __shfl_xor_sync(0xFFFFFFFFu, o[i][0][e], off);
 }
 
 template <int C, int N> __device__ inline void clear(float (&o)[N][C][4])
@@ -164,13 +168,13 @@ template <int C, int N> __device__ inline void clear(float (&o)[N][C][4])
             for (int e = 0; e < 4; ++e) o[i][c][e] = 0.f;
 }
 
-// columns 4 cx + 64 c of a row, times f, by the first part's threads; zeros (whatever the sums hold) where !keep
-template <int C> __device__ inline void store_columns(float *row, const float (&o)[C][4], float f, int head_dim, const Columns &at, bool keep = true)
+// columns 4 cx + 4 TX c of a row, times f, by the first part's threads; zeros (whatever the sums hold) where !keep
+template <int C, int TX> __device__ inline void store_columns(float *row, const float (&o)[C][4], float f, int head_dim, const Columns<TX> &at, bool keep = true)
 {
 #pragma unroll
     for (int c = 0; c < C; ++c)
-        if (at.part == 0 && 4 * at.cx + 64 * c < head_dim)
-            *reinterpret_cast<float4 *>(row + 4 * at.cx + 64 * c) =
+        if (at.part == 0 && 4 * at.cx + 4 * TX * c < head_dim)
+            *reinterpret_cast<float4 *>(row + 4 * at.cx + 4 * TX * c) =
                 keep ? make_float4(o[c][0] * f, o[c][1] * f, o[c][2] * f, o[c][3] * f) : make_float4(0.f, 0.f, 0.f, 0.f);
 }
 
@@ -224,25 +228,25 @@ template <typename Load, typename Use> __device__ inline void turns(const SimtSh
 }
 
 // Keys and values from x.kb + 64 j on -> a stage, zeros over hidden ones
-__device__ inline void load_keys(const AttnArgs &a, const SimtUnit &x, const SimtShape &f, float *stage, uint8_t *seen_s, int64_t j, const float *kp, const float *vp)
+template <int TX> __device__ inline void load_keys(const AttnArgs &a, const SimtUnit &x, const SimtShape &f, float *stage, uint8_t *seen_s, int64_t j, const float *kp, const float *vp)
 {
-    const int64_t key = x.kb + j * kTile + (threadIdx.x >> 2);
+    const int64_t key = x.kb + j * kTile + threadIdx.x / (TX / 4);
     const bool seen = key < x.ke && (!a.mask || a.mask[key]);
-    load_tile<4>(stage, f, seen ? kp + key * a.ldk + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
-    load_tile<4>(stage + kTile * f.ld, f, seen ? vp + key * a.ldv + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
-    if ((threadIdx.x & 3) == 0) seen_s[threadIdx.x >> 2] = seen;
+    load_tile<TX / 4>(stage, f, seen ? kp + key * a.ldk + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
+    load_tile<TX / 4>(stage + kTile * f.ld, f, seen ? vp + key * a.ldv + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
+    if (threadIdx.x % (TX / 4) == 0) seen_s[threadIdx.x / (TX / 4)] = seen;
 }
 
-template <int C, int I>
-__global__ void __launch_bounds__(kThreads, blocks_of(C, I))
+template <int TX, int C, int I>
+__global__ void __launch_bounds__(16 * TX, blocks_of(TX, C, I))
 attn_simt_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ SimtShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
 {
-    constexpr int kRows = 16 * I, kPerRow = 16 / I;
+    constexpr int kRows = 16 * I, kPerRow = TX / I, J = kTile / TX;
     extern __shared__ __align__(16) float sm[];
     float *q_s = sm, *p_s = q_s + kRows * f.ld, *kv_s = p_s + kRows * kLdP;          // stage b: K and V at tiles 2 b, 2 b + 1
     __shared__ uint8_t seen_s[2][kTile];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, heads = a.kv_heads * a.group, lr = threadIdx.x / kPerRow;
-    const Columns at(f, tx);
+    const int tx = threadIdx.x % TX, ty = threadIdx.x / TX, heads = a.kv_heads * a.group, lr = threadIdx.x / kPerRow;
+    const Columns<TX> at(f, tx);
     const SimtUnit x = simt_unit(a, f);
     const float c1 = a.scale * kLog2e;
     const float *qp = static_cast<const float *>(a.q), *kp = static_cast<const float *>(a.k), *vp = static_cast<const float *>(a.v);
@@ -262,30 +266,30 @@ attn_simt_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             m[i] = -INFINITY;
             l[i] = 0.f;
         }
-        turns(f, ceil_div(x.ke - x.kb, (int64_t)kTile), [&](int64_t j, int b) { load_keys(a, x, f, kv_s + 2 * b * kTile * f.ld, seen_s[b], j, kp, vp); }, [&](int b) {
+        turns(f, ceil_div(x.ke - x.kb, (int64_t)kTile), [&](int64_t j, int b) { load_keys<TX>(a, x, f, kv_s + 2 * b * kTile * f.ld, seen_s[b], j, kp, vp); }, [&](int b) {
             const float *k_s = kv_s + 2 * b * kTile * f.ld, *v_s = k_s + kTile * f.ld;
-            float s[I][4];
-            scores<I>(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
-            bool on[4];
+            float s[I][J];
+            scores<TX, I>(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
+            bool on[J];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) on[j] = seen_s[b][tx + 16 * j];
+            for (int j = 0; j < J; ++j) on[j] = seen_s[b][tx + TX * j];
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 float top = -INFINITY;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < J; ++j) {
                     s[i][j] = on[j] ? s[i][j] * c1 : -INFINITY;
                     top = fmaxf(top, s[i][j]);
                 }
-                top = fmaxf(m[i], row_max(top));
+                top = fmaxf(m[i], row_max<TX>(top));
                 const float base = top == -INFINITY ? 0.f : top, c = exp2_fast(m[i] - base);
                 m[i] = top;
                 float sum = 0.f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < J; ++j) {
                     const float p = exp2_fast(s[i][j] - base);
                     sum += p;
-                    p_s[(I * ty + i) * kLdP + tx + 16 * j] = p;
+                    p_s[(ty + 16 * i) * kLdP + tx + TX * j] = p;
                 }
                 l[i] = l[i] * c + sum;
 #pragma unroll
@@ -294,43 +298,43 @@ attn_simt_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
                     for (int e = 0; e < 4; ++e) o[i][n][e] *= c;
             }
             __syncwarp();                                // rows of p belong to one half-warp
-            add_rows<C, I>(o, p_s, v_s, f.ld, a.head_dim, ty, at);
+            add_rows<C, I, TX>(o, p_s, v_s, f.ld, a.head_dim, ty, at);
             __syncwarp();
         });
         cp_async_wait_all();
-        add_parts<C>(o, f);
+        add_parts<TX, C>(o, f);
 #pragma unroll
-        for (int i = 0; i < I; ++i) l[i] = row_sum(l[i]);
+        for (int i = 0; i < I; ++i) l[i] = row_sum<TX>(l[i]);
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int64_t r = r0 + I * ty + i;
+            const int64_t r = r0 + ty + 16 * i;
             if (r >= x.rows) continue;
             int64_t row;
             int head;
             row_of(a, x, r, row, head);
             const float inv = l[i] == 0.f ? 0.f : 1.f / l[i];
             if (f.splits == 1) {
-                store_columns<C>(static_cast<float *>(a.out) + row * a.ldo + (int64_t)head * a.head_dim, o[i], inv, a.head_dim, at);
+                store_columns<C, TX>(static_cast<float *>(a.out) + row * a.ldo + (int64_t)head * a.head_dim, o[i], inv, a.head_dim, at);
                 if (a.lse && tx == 0) a.lse[row * heads + head] = l[i] == 0.f ? -INFINITY : (m[i] + log2f(l[i])) * kLn2;
             } else {
                 const int64_t p = ((int64_t)x.z * a.q_rows + row) * heads + head;
-                store_columns<C>(part_o + p * a.head_dim, o[i], inv, a.head_dim, at);
+                store_columns<C, TX>(part_o + p * a.head_dim, o[i], inv, a.head_dim, at);
                 if (tx == 0) part_ml[p] = make_float2(l[i] == 0.f ? -INFINITY : m[i], l[i]);
             }
         }
     }
 }
 
-template <int C, int I>
-__global__ void __launch_bounds__(kThreads, blocks_of(C, I))
+template <int TX, int C, int I>
+__global__ void __launch_bounds__(16 * TX, blocks_of(TX, C, I))
 attn_simt_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ SimtShape f, float *__restrict__ part_dq, float *__restrict__ dots)
 {
-    constexpr int kRows = 16 * I, kPerRow = 16 / I;
+    constexpr int kRows = 16 * I, kPerRow = TX / I, J = kTile / TX;
     extern __shared__ __align__(16) float sm[];
     float *q_s = sm, *g_s = q_s + kRows * f.ld, *ds_s = g_s + kRows * f.ld, *kv_s = ds_s + kRows * kLdP;
     __shared__ uint8_t seen_s[2][kTile];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, heads = a.kv_heads * a.group, lr = threadIdx.x / kPerRow;
-    const Columns at(f, tx);
+    const int tx = threadIdx.x % TX, ty = threadIdx.x / TX, heads = a.kv_heads * a.group, lr = threadIdx.x / kPerRow;
+    const Columns<TX> at(f, tx);
     const SimtUnit x = simt_unit(a, f);
     const float c1 = a.scale * kLog2e;
     const float *qp = static_cast<const float *>(a.q), *kp = static_cast<const float *>(a.k), *vp = static_cast<const float *>(a.v);
@@ -352,7 +356,7 @@ attn_simt_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int64_t r = r0 + I * ty + i;
+            const int64_t r = r0 + ty + 16 * i;
             int64_t row;
             int head;
             row_of(a, x, min(r, x.rows - 1), row, head);
@@ -364,57 +368,57 @@ attn_simt_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     lse[i] = v * kLog2e;
 #pragma unroll
                     for (int c = 0; c < C; ++c)
-                        if (4 * tx + 64 * c < a.head_dim) {
-                            const float4 y = *reinterpret_cast<const float4 *>(op + row * a.ldo + (int64_t)head * a.head_dim + 4 * tx + 64 * c);
-                            const float4 g = *reinterpret_cast<const float4 *>(g_s + (I * ty + i) * f.ld + 4 * tx + 64 * c);
+                        if (4 * tx + 4 * TX * c < a.head_dim) {
+                            const float4 y = *reinterpret_cast<const float4 *>(op + row * a.ldo + (int64_t)head * a.head_dim + 4 * tx + 4 * TX * c);
+                            const float4 g = *reinterpret_cast<const float4 *>(g_s + (ty + 16 * i) * f.ld + 4 * tx + 4 * TX * c);
                             d[i] += y.x * g.x + y.y * g.y + y.z * g.z + y.w * g.w;
                         }
                 }
             }
-            d[i] = row_sum(d[i]);
+            d[i] = row_sum<TX>(d[i]);
             if (r < x.rows && x.z == 0 && tx == 0) dots[row * heads + head] = d[i];
         }
-        turns(f, ceil_div(x.ke - x.kb, (int64_t)kTile), [&](int64_t j, int b) { load_keys(a, x, f, kv_s + 2 * b * kTile * f.ld, seen_s[b], j, kp, vp); }, [&](int b) {
+        turns(f, ceil_div(x.ke - x.kb, (int64_t)kTile), [&](int64_t j, int b) { load_keys<TX>(a, x, f, kv_s + 2 * b * kTile * f.ld, seen_s[b], j, kp, vp); }, [&](int b) {
             const float *k_s = kv_s + 2 * b * kTile * f.ld, *v_s = k_s + kTile * f.ld;
-            float s[I][4], u[I][4];
-            scores<I>(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
-            scores<I>(g_s, v_s, f.ld, a.head_dim, ty, tx, u);
+            float s[I][J], u[I][J];
+            scores<TX, I>(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
+            scores<TX, I>(g_s, v_s, f.ld, a.head_dim, ty, tx, u);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const bool on = seen_s[b][tx + 16 * j];
+            for (int j = 0; j < J; ++j) {
+                const bool on = seen_s[b][tx + TX * j];
 #pragma unroll
                 for (int i = 0; i < I; ++i)
-                    ds_s[(I * ty + i) * kLdP + tx + 16 * j] = on ? exp2_fast(fmaf(s[i][j], c1, -lse[i])) * (u[i][j] - d[i]) : 0.f;
+                    ds_s[(ty + 16 * i) * kLdP + tx + TX * j] = on ? exp2_fast(fmaf(s[i][j], c1, -lse[i])) * (u[i][j] - d[i]) : 0.f;
             }
             __syncwarp();
-            add_rows<C, I>(dq, ds_s, k_s, f.ld, a.head_dim, ty, at);
+            add_rows<C, I, TX>(dq, ds_s, k_s, f.ld, a.head_dim, ty, at);
             __syncwarp();
         });
-        add_parts<C>(dq, f);
+        add_parts<TX, C>(dq, f);
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const int64_t r = r0 + I * ty + i;
+            const int64_t r = r0 + ty + 16 * i;
             if (r >= x.rows) continue;
             int64_t row;
             int head;
             row_of(a, x, r, row, head);
             const bool keep = lse[i] != INFINITY;        // a row that saw no key passes on nothing
-            if (f.splits == 1) store_columns<C>(static_cast<float *>(a.dq) + row * a.ldq2 + (int64_t)head * a.head_dim, dq[i], a.scale, a.head_dim, at, keep);
-            else store_columns<C>(part_dq + (((int64_t)x.z * a.q_rows + row) * heads + head) * a.head_dim, dq[i], a.scale, a.head_dim, at, keep);
+            if (f.splits == 1) store_columns<C, TX>(static_cast<float *>(a.dq) + row * a.ldq2 + (int64_t)head * a.head_dim, dq[i], a.scale, a.head_dim, at, keep);
+            else store_columns<C, TX>(part_dq + (((int64_t)x.z * a.q_rows + row) * heads + head) * a.head_dim, dq[i], a.scale, a.head_dim, at, keep);
         }
     }
 }
 
-template <int C, int I>
-__global__ void __launch_bounds__(kThreads, blocks_of(C, I))
+template <int TX, int C, int I>
+__global__ void __launch_bounds__(16 * TX, blocks_of(TX, C, I))
 attn_simt_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ SimtShape f, const float *__restrict__ dots)
 {
-    constexpr int kRows = 16 * I, kPerRow = 16 / I;
+    constexpr int kRows = 16 * I, kPerRow = TX / I, J = kTile / TX;
     extern __shared__ __align__(16) float sm[];
     float *k_s = sm, *v_s = k_s + kTile * f.ld, *p_s = v_s + kTile * f.ld, *ds_s = p_s + kRows * kLdP, *qg_s = ds_s + kRows * kLdP;
     __shared__ float lse_s[2][kRows], dot_s[2][kRows];
-    const int tx = threadIdx.x & 15, ty = threadIdx.x >> 4, heads = a.kv_heads * a.group, lr = threadIdx.x / kPerRow;
-    const Columns at(f, tx);
+    const int tx = threadIdx.x % TX, ty = threadIdx.x / TX, heads = a.kv_heads * a.group, lr = threadIdx.x / kPerRow;
+    const Columns<TX> at(f, tx);
     const SimtUnit x = simt_unit(a, f);
     const float c1 = a.scale * kLog2e;
     const float *qp = static_cast<const float *>(a.q), *kp = static_cast<const float *>(a.k), *vp = static_cast<const float *>(a.v);
@@ -422,10 +426,10 @@ attn_simt_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     for (int64_t j0 = x.rg.k0 + (int64_t)x.t0 * kTile; j0 < x.rg.k1; j0 += (int64_t)f.tiles * kTile) {
         __syncthreads();
         {
-            const int64_t key = j0 + (threadIdx.x >> 2);
+            const int64_t key = j0 + threadIdx.x / (TX / 4);
             const bool seen = key < x.rg.k1 && (!a.mask || a.mask[key]);
-            load_tile<4>(k_s, f, seen ? kp + key * a.ldk + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
-            load_tile<4>(v_s, f, seen ? vp + key * a.ldv + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
+            load_tile<TX / 4>(k_s, f, seen ? kp + key * a.ldk + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
+            load_tile<TX / 4>(v_s, f, seen ? vp + key * a.ldv + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
         }
         float dk[4][C][4], dv[4][C][4];
         clear(dk);
@@ -449,38 +453,38 @@ attn_simt_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             load_tile<kPerRow>(g_s, f, l != INFINITY ? gp + row * a.ldg + (int64_t)head * a.head_dim : nullptr, kp, a.head_dim);
         }, [&](int b) {
             const float *q_s = qg_s + 2 * b * kRows * f.ld, *g_s = q_s + kRows * f.ld;
-            float s[I][4], u[I][4];
-            scores<I>(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
-            scores<I>(g_s, v_s, f.ld, a.head_dim, ty, tx, u);
+            float s[I][J], u[I][J];
+            scores<TX, I>(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
+            scores<TX, I>(g_s, v_s, f.ld, a.head_dim, ty, tx, u);
 #pragma unroll
             for (int i = 0; i < I; ++i) {
-                const float lse = lse_s[b][I * ty + i], d = dot_s[b][I * ty + i];
+                const float lse = lse_s[b][ty + 16 * i], d = dot_s[b][ty + 16 * i];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
+                for (int j = 0; j < J; ++j) {
                     const float p = exp2_fast(fmaf(s[i][j], c1, -lse));
-                    p_s[(I * ty + i) * kLdP + tx + 16 * j] = p;
-                    ds_s[(I * ty + i) * kLdP + tx + 16 * j] = p * (u[i][j] - d);
+                    p_s[(ty + 16 * i) * kLdP + tx + TX * j] = p;
+                    ds_s[(ty + 16 * i) * kLdP + tx + TX * j] = p * (u[i][j] - d);
                 }
             }
             __syncthreads();
-            add_columns<C, I>(dv, p_s, g_s, f.ld, a.head_dim, ty, at);
-            add_columns<C, I>(dk, ds_s, q_s, f.ld, a.head_dim, ty, at);
+            add_columns<C, I, TX>(dv, p_s, g_s, f.ld, a.head_dim, ty, at);
+            add_columns<C, I, TX>(dk, ds_s, q_s, f.ld, a.head_dim, ty, at);
         });
         cp_async_wait_all();
-        add_parts<C>(dk, f);
-        add_parts<C>(dv, f);
+        add_parts<TX, C>(dk, f);
+        add_parts<TX, C>(dv, f);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t key = j0 + 4 * ty + i;
             if (key >= x.rg.k1) continue;
             const bool keep = !a.mask || a.mask[key];
-            store_columns<C>(static_cast<float *>(a.dk) + key * a.ldk2 + (int64_t)x.h * a.head_dim, dk[i], a.scale, a.head_dim, at, keep);
-            store_columns<C>(static_cast<float *>(a.dv) + key * a.ldv2 + (int64_t)x.h * a.head_dim, dv[i], 1.f, a.head_dim, at, keep);
+            store_columns<C, TX>(static_cast<float *>(a.dk) + key * a.ldk2 + (int64_t)x.h * a.head_dim, dk[i], a.scale, a.head_dim, at, keep);
+            store_columns<C, TX>(static_cast<float *>(a.dv) + key * a.ldv2 + (int64_t)x.h * a.head_dim, dv[i], 1.f, a.head_dim, at, keep);
         }
     }
 }
 
-constexpr int kMaxDevices = 64, kMostSmem = 226 * 1024, kSmSmem = 228 * 1024;
+constexpr int kMaxDevices = 64, kMostSmem = 224 * 1024, kSmSmem = 228 * 1024;
 template <typename Kernel> bool allow_smem(Kernel kernel, std::atomic<bool> (&done)[kMaxDevices])
 {
     int dev = 0;
@@ -492,13 +496,13 @@ template <typename Kernel> bool allow_smem(Kernel kernel, std::atomic<bool> (&do
 }
 
 // kept: floats of shared memory that stay; pair: those of one stage.  Two stages where they leave room for `blocks` blocks per SM.
-SimtShape shape_of(const AttnArgs &a, int64_t tiles, int splits, int kept_rows, int pair_rows, int p_rows, int blocks, size_t &smem)
+SimtShape shape_of(const AttnArgs &a, int64_t tiles, int splits, int kept_rows, int pair_rows, int p_rows, int TX, int blocks, size_t &smem)
 {
     SimtShape f{};
     f.ld = (a.head_dim / 4 | 1) * 4;                 // an odd number of 16-byte units
     f.tiles = (int)tiles;
     f.splits = splits;
-    f.cols = 16;
+    f.cols = TX;
     while (f.cols > 1 && f.cols * 2 >= a.head_dim) f.cols /= 2;
     const size_t fixed = ((size_t)kept_rows * f.ld + (size_t)p_rows * kLdP) * sizeof(float), pair = (size_t)pair_rows * f.ld * sizeof(float);
     f.stages = (fixed + 2 * pair + 2048) * blocks <= (size_t)kSmSmem ? 2 : 1;
@@ -506,31 +510,31 @@ SimtShape shape_of(const AttnArgs &a, int64_t tiles, int splits, int kept_rows, 
     return f;
 }
 
-template <int C, int I> bool forward_of(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
+template <int TX, int C, int I> bool forward_of(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
 {
     static std::atomic<bool> done[kMaxDevices] = {};
-    if (!allow_smem(attn_simt_fwd_kernel<C, I>, done)) return false;
+    if (!allow_smem(attn_simt_fwd_kernel<TX, C, I>, done)) return false;
     size_t smem;
-    const SimtShape f = shape_of(a, p.q_tiles, p.splits, 16 * I, 2 * kTile, 16 * I, blocks_of(C, I), smem);
+    const SimtShape f = shape_of(a, p.q_tiles, p.splits, 16 * I, 2 * kTile, 16 * I, TX, blocks_of(TX, C, I), smem);
     note_launch();
-    attn_simt_fwd_kernel<C, I><<<(unsigned)(a.n_seq * a.kv_heads * p.q_tiles * p.splits), kThreads, smem, st>>>(a, f, part_o, part_ml);
+    attn_simt_fwd_kernel<TX, C, I><<<(unsigned)(a.n_seq * a.kv_heads * p.q_tiles * p.splits), 16 * TX, smem, st>>>(a, f, part_o, part_ml);
     return true;
 }
 
-template <int C, int I> bool backward_of(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
+template <int TX, int C, int I> bool backward_of(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
 {
     static std::atomic<bool> done[2][kMaxDevices] = {};
-    if (!allow_smem(attn_simt_dq_kernel<C, I>, done[0]) || !allow_smem(attn_simt_dkv_kernel<C, I>, done[1])) return false;
+    if (!allow_smem(attn_simt_dq_kernel<TX, C, I>, done[0]) || !allow_smem(attn_simt_dkv_kernel<TX, C, I>, done[1])) return false;
     size_t smem;
     if (a.q_rows) {
-        const SimtShape f = shape_of(a, p.q_tiles, p.splits, 2 * 16 * I, 2 * kTile, 16 * I, blocks_of(C, I), smem);
+        const SimtShape f = shape_of(a, p.q_tiles, p.splits, 2 * 16 * I, 2 * kTile, 16 * I, TX, blocks_of(TX, C, I), smem);
         note_launch();
-        attn_simt_dq_kernel<C, I><<<(unsigned)(a.n_seq * a.kv_heads * p.q_tiles * p.splits), kThreads, smem, st>>>(a, f, part_dq, dots);
+        attn_simt_dq_kernel<TX, C, I><<<(unsigned)(a.n_seq * a.kv_heads * p.q_tiles * p.splits), 16 * TX, smem, st>>>(a, f, part_dq, dots);
     }
     if (a.k_rows) {
-        const SimtShape f = shape_of(a, p.k_tiles, 1, 2 * kTile, 2 * 16 * I, 2 * 16 * I, blocks_of(C, I), smem);
+        const SimtShape f = shape_of(a, p.k_tiles, 1, 2 * kTile, 2 * 16 * I, 2 * 16 * I, TX, blocks_of(TX, C, I), smem);
         note_launch();
-        attn_simt_dkv_kernel<C, I><<<(unsigned)(a.n_seq * a.kv_heads * p.k_tiles), kThreads, smem, st>>>(a, f, dots);
+        attn_simt_dkv_kernel<TX, C, I><<<(unsigned)(a.n_seq * a.kv_heads * p.k_tiles), 16 * TX, smem, st>>>(a, f, dots);
     }
     return true;
 }
@@ -550,26 +554,32 @@ SimtPlan simt_plan(const AttnArgs &a, int64_t max_q, int64_t max_k)
     return p;
 }
 
-template <int C> static bool forward_by_rows(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
+// heads of up to 32, 64, 128 columns, with 8 or 16 threads side by side
+template <int I, int TX> static bool forward_wide(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    if (p.rows == 16) return forward_of<C, 1>(a, p, part_o, part_ml, st);
-    return p.rows == 32 ? forward_of<C, 2>(a, p, part_o, part_ml, st) : forward_of<C, 4>(a, p, part_o, part_ml, st);
+    if (a.head_dim > 64) return forward_of<16, 2, I>(a, p, part_o, part_ml, st);
+    if (a.head_dim > 32) return forward_of<TX, 64 / (4 * TX), I>(a, p, part_o, part_ml, st);
+    return forward_of<8, 1, I>(a, p, part_o, part_ml, st);
 }
 
-template <int C> static bool backward_by_rows(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
+template <int I, int TX> static bool backward_wide(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
 {
-    if (p.rows == 16) return backward_of<C, 1>(a, p, part_dq, dots, st);
-    return p.rows == 32 ? backward_of<C, 2>(a, p, part_dq, dots, st) : backward_of<C, 4>(a, p, part_dq, dots, st);
+    if (a.head_dim > 64) return backward_of<16, 2, I>(a, p, part_dq, dots, st);
+    if constexpr (TX == 8)
+        if (a.head_dim <= 32) return backward_of<8, 1, I>(a, p, part_dq, dots, st);
+    return backward_of<TX, 64 / (4 * TX), I>(a, p, part_dq, dots, st);
 }
 
 bool simt_attention_forward(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    return a.head_dim <= 64 ? forward_by_rows<1>(a, p, part_o, part_ml, st) : forward_by_rows<2>(a, p, part_o, part_ml, st);
+    if (p.rows == 16) return forward_wide<1, 8>(a, p, part_o, part_ml, st);
+    return p.rows == 32 ? forward_wide<2, 8>(a, p, part_o, part_ml, st) : forward_wide<4, 16>(a, p, part_o, part_ml, st);
 }
 
 bool simt_attention_backward(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
 {
-    return a.head_dim <= 64 ? backward_by_rows<1>(a, p, part_dq, dots, st) : backward_by_rows<2>(a, p, part_dq, dots, st);
+    if (p.rows == 16) return backward_wide<1, 8>(a, p, part_dq, dots, st);
+    return p.rows == 32 ? backward_wide<2, 8>(a, p, part_dq, dots, st) : backward_wide<4, 16>(a, p, part_dq, dots, st);
 }
 
 }  // namespace e2egrec
