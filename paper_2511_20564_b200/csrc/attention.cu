@@ -145,8 +145,8 @@ int32_t check_heads(const e2egrec_mat *m, int32_t heads, int32_t head_dim, int32
 constexpr int64_t kMaxRows = (int64_t)1 << 31;
 
 // The kernels of a call.  A sequence's keys and rows stream (attention_few.cu) where a key head has up to two rows (fp32 three: 300 of
-// 3 x 200, 88 us against 113; four in the backward pass), or where a sequence is so small that the set-up of a tile costs more than its products; bf16 heads of up to 128
-// go to the tensor cores otherwise, fp32 ones to tiles of fp32 FMA, wider heads always stream.
+// 3 x 200, 88 us against 113; four in the backward pass), or where a sequence is so small that the set-up of a tile costs more than its
+// products; bf16 heads of up to 128 go to the tensor cores otherwise, fp32 ones to tiles of fp32 FMA, wider heads always stream.
 enum class Path { few, tc, simt };
 
 struct Plan {
