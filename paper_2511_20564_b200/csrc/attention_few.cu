@@ -536,6 +536,8 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
 // that is longer than the launch was sized for has its rows done batch by batch and its keys' gradients apart.
 // Where all keys are in one turn of the warp, D = sum_j p_j dP_j is formed from what the registers hold instead of the stored
 // outputs: with a handful of keys dP - D cancels, and the rounding of 16-bit outputs showed (dQ of three keys 3.1e-3 off, 2.0e-3 so).
+// p is divided by its sum there, which lse, rounded on its own, leaves a few 2^-23 off 1; a p that is the whole sum becomes 1 exactly, and
+// dS of a lone key 0.
 // Over more keys (kFit) D comes from the stored outputs, and what 16-bit ones lack, sum_j dS_j (0 with the exact D), is taken out at the end:
 // dQ = sum_j dS_j k_j - (sum_j dS_j) (sum_j p_j k_j).  dQ of rows that see 12 000 keys was 3.4e-3 off without it, 1.8e-3 so (a rounding:
 // 1.7e-3).
@@ -643,9 +645,16 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
                 for (int u = 0; u < U; ++u) s[r * U + u] = seen[u] ? exp2_fast(fmaf(s[r * U + u], c1, -lse[r])) : 0.f;
                 if (one_turn) {
-                    float t = 0.f;
+                    float sum = 0.f, t = 0.f;
 #pragma unroll
-                    for (int u = 0; u < U; ++u) t += seen[u] ? s[r * U + u] * s[(R + r) * U + u] : 0.f;
+                    for (int u = 0; u < U; ++u) sum += s[r * U + u];
+                    for (int o = wide; o < 32; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+                    const float lone = lse[r] == INFINITY ? 0.f : 1.f, inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        s[r * U + u] = s[r * U + u] == sum ? lone : s[r * U + u] * inv;
+                        t += seen[u] ? s[r * U + u] * s[(R + r) * U + u] : 0.f;
+                    }
                     for (int o = wide; o < 32; o <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
                     d[r] = t;
                 }

@@ -92,6 +92,19 @@ template <int TX, int I> __device__ inline void scores(const float *a, const flo
         for (int j = 0; j < J; ++j) s[i][j] = t[i][j].x + t[i][j].y;
 }
 
+// a . b, added up in the order of one of the scores above: D of a row whose softmax is one key's alone is that key's dP to the last bit
+__device__ inline float dot_as_scores(const float *a, const float *b, int head_dim)
+{
+    float2 t = make_float2(0.f, 0.f);
+#pragma unroll 4
+    for (int d = 0; d < head_dim; d += 4) {
+        const float4 x = *reinterpret_cast<const float4 *>(a + d), y = *reinterpret_cast<const float4 *>(b + d);
+        t = __ffma2_rn(make_float2(x.x, x.y), make_float2(y.x, y.y), t);
+        t = __ffma2_rn(make_float2(x.z, x.w), make_float2(y.z, y.w), t);
+    }
+    return t.x + t.y;
+}
+
 __device__ inline void fma4(float (&o)[4], float w, const float4 &v)
 {
     const float2 w2 = make_float2(w, w);
@@ -350,7 +363,7 @@ attn_simt_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             load_tile<kPerRow>(q_s, f, on ? qp + row * a.ldq + (int64_t)head * a.head_dim : nullptr, qp, a.head_dim);
             load_tile<kPerRow>(g_s, f, on ? gp + row * a.ldg + (int64_t)head * a.head_dim : nullptr, qp, a.head_dim);
         }
-        float dq[I][C][4], lse[I], d[I];
+        float dq[I][C][4], lse[I], d[I], mine = 0.f;
         clear(dq);
         cp_async_wait_all();
         __syncthreads();
@@ -361,23 +374,15 @@ attn_simt_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             int head;
             row_of(a, x, min(r, x.rows - 1), row, head);
             lse[i] = INFINITY;
-            d[i] = 0.f;
             if (r < x.rows) {
                 const float v = a.lse[row * heads + head];
-                if (v != -INFINITY) {
-                    lse[i] = v * kLog2e;
-#pragma unroll
-                    for (int c = 0; c < C; ++c)
-                        if (4 * tx + 4 * TX * c < a.head_dim) {
-                            const float4 y = *reinterpret_cast<const float4 *>(op + row * a.ldo + (int64_t)head * a.head_dim + 4 * tx + 4 * TX * c);
-                            const float4 g = *reinterpret_cast<const float4 *>(g_s + (ty + 16 * i) * f.ld + 4 * tx + 4 * TX * c);
-                            d[i] += y.x * g.x + y.y * g.y + y.z * g.z + y.w * g.w;
-                        }
-                }
+                if (v != -INFINITY) lse[i] = v * kLog2e;
             }
-            d[i] = row_sum<TX>(d[i]);
-            if (r < x.rows && x.z == 0 && tx == 0) dots[row * heads + head] = d[i];
+            if (tx == i && lse[i] != INFINITY) mine = dot_as_scores(g_s + (ty + 16 * i) * f.ld, op + row * a.ldo + (int64_t)head * a.head_dim, a.head_dim);
+            if (tx == i && r < x.rows && x.z == 0) dots[row * heads + head] = mine;
         }
+#pragma unroll
+        for (int i = 0; i < I; ++i) d[i] = __shfl_sync(0xFFFFFFFFu, mine, i, TX);
         turns(f, ceil_div(x.ke - x.kb, (int64_t)kTile), [&](int64_t j, int b) { load_keys<TX>(a, x, f, kv_s + 2 * b * kTile * f.ld, seen_s[b], j, kp, vp); }, [&](int b) {
             const float *k_s = kv_s + 2 * b * kTile * f.ld, *v_s = k_s + kTile * f.ld;
             float s[I][J], u[I][J];

@@ -645,7 +645,8 @@ __device__ inline void store_row(uint32_t taddr, bf16 *out, int head_dim, float 
     }
 }
 
-// dQ, and D = dO . out of every row for the other kernel.  dS goes into its product as two bf16 operands, its rounding and the rest: D comes
+// dQ, and D = dO . out of every row for the other kernel.  Where one tile holds all keys, what the stored out's D lacks, the sum of
+// p (dP - D), is added to it: dS of a lone key is 0 then, and the rounding of out does not show.  dS goes into its product as two bf16 operands, its rounding and the rest: D comes
 // from 16-bit outputs already, and with dS rounded as well dQ was 2.5 to 2.7e-3 off in the mean (a rounding of the result: 1.8e-3),
 // at most 2.4e-3 so, dK included; the training case's backward pass takes 550 us with one operand, 585 us so.
 template <int NB>
@@ -655,7 +656,8 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 {
     constexpr int kStages = Bwd<NB>::kKvStages, kTileBytes = Bwd<NB>::kTileBytes;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], k_clean[kWordRing], q_full, q_empty, s_full[2], dp_full, ds_full, o_full, o_empty;
+    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], k_clean[kWordRing], q_full, q_empty, s_full[2], dp_full, ds_full, o_full, o_empty, rest_full;
+    __shared__ float rests[2][kTile];                 // sums of p (dP - D) over each warpgroup's columns
     __shared__ __align__(16) uint32_t words[kWordRing][4];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
@@ -678,6 +680,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         mbar_init(&ds_full, 8);
         mbar_init(&o_full, 1);
         mbar_init(&o_empty, 8);
+        mbar_init(&rest_full, 8);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -825,7 +828,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
         const float c1 = a.scale * kLog2e;
         const int heads = a.kv_heads * a.group;
-        uint32_t jj = 0, item = 0;
+        uint32_t jj = 0, item = 0, alone = 0;
         bool ok = true;
         for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
             const Work x = work_of(a, f, u, false);
@@ -850,7 +853,6 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                         for (int k = 0; k < 8; ++k) dot += xo[k] * xg[k];
                     }
                     if (l == -INFINITY) dot = 0.f;
-                    if (q == 0) dots[row * heads + head] = dot;
                 }
                 for (int j = 0; j < x.n; ++j, ++jj) {
                     ok = warp_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
@@ -872,6 +874,25 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     ok = warp_wait(&dp_full, jj & 1u, &abort_flag);
                     if (!ok) break;
                     tc_fence_after();
+                    if (x.n == 1) {
+                        uint32_t v[2][32];
+                        tmem_load32_async(tmem + lanes + 256 + q * 64, v[0]);
+                        tmem_load32_async(tmem + lanes + 256 + q * 64 + 32, v[1]);
+                        tmem_load_wait();
+                        float rest = 0.f;
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const uint32_t word = words[jj % kWordRing][q * 2 + c];
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) rest += (word >> e) & 1u ? p[c * 32 + e] * (__uint_as_float(v[c][e]) - dot) : 0.f;
+                        }
+                        rests[q][w * 32 + lane] = rest;
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&rest_full);
+                        ok = warp_wait(&rest_full, alone++ & 1u, &abort_flag);
+                        if (!ok) break;
+                        if (base != INFINITY) dot += rests[0][w * 32 + lane] + rests[1][w * 32 + lane];
+                    }
                     {
                         uint32_t v[2][32];
                         tmem_load32_async(tmem + lanes + 256 + q * 64, v[0]);
@@ -901,6 +922,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     if (lane == 0) mbar_arrive(&ds_full);
                 }
                 if (!ok) break;
+                if (live && q == 0) dots[row * heads + head] = dot;
                 if (x.n > 0) {
                     ok = warp_wait(&o_full, item++ & 1u, &abort_flag);
                     if (!ok) break;
