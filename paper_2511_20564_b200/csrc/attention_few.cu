@@ -531,6 +531,75 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
     }
 }
 
+// What D of the stored outputs lacks, the sum of p (dP - D) over the keys, for R rows of unit u from r0 on.  For sequences of more keys than the
+// caller named; apart from the kernel below, whose registers it would take (inlined: 72 -> 80 us for 8192 requests of three tokens).
+template <int R> struct RowSums {
+    float of[R];
+};
+template <typename T, int R, int CPL> __device__ __noinline__ RowSums<R> lacking(const AttnArgs &a, const FewShape &f, uint32_t unit, int64_t r0)
+{
+    constexpr int E = Piece<T, CPL>::E;
+    const int lane = threadIdx.x & 31, wide = f.lanes * f.heads, grp = lane / wide, at = lane & (f.lanes - 1), kpw = 32 / wide, heads = a.kv_heads * a.group;
+    const Unit x = few_unit(a, f, unit);
+    const int64_t koff = x.h * (int64_t)a.head_dim;
+    const float c1 = a.scale * kLog2e;
+    float q[R][E], g[R][E], lse[R], d[R];
+    RowSums<R> sums;
+    RowWalk in(a, x, r0);
+#pragma unroll
+    for (int r = 0; r < R; ++r, in.next(a)) {
+        Piece<T, CPL> p, t, o;
+        p.zero();
+        t.zero();
+        o.zero();
+        lse[r] = INFINITY;
+        if (x.on && r0 + r < x.rows) {
+            const int head = in.head(a, x);
+            const int64_t col = (int64_t)head * a.head_dim;
+            const float v = a.lse[in.row * heads + head];
+            if (v != -INFINITY) {
+                lse[r] = v * kLog2e;
+                p.load(static_cast<const T *>(a.q) + in.row * a.ldq + col, at, f.lanes, f.chunks);
+                t.load(static_cast<const T *>(a.dout) + in.row * a.ldg + col, at, f.lanes, f.chunks);
+                o.load(static_cast<const T *>(a.o) + in.row * a.ldo + col, at, f.lanes, f.chunks);
+            }
+        }
+        float y[E];
+        p.widen(q[r]);
+        t.widen(g[r]);
+        o.widen(y);
+        d[r] = dot<E>(g[r], y);
+        sums.of[r] = 0.f;
+    }
+    key_sums<R>(d, f.lanes);
+    for (int64_t j0 = x.kb; j0 < x.ke; j0 += kpw) {
+        const int64_t j = j0 + grp;
+        const bool on = x.on && j < x.ke && (!a.mask || a.mask[j]);
+        Piece<T, CPL> k, v;
+        float w[E], y[E], s[2 * R];
+        k.zero();
+        v.zero();
+        if (on) {
+            k.load(static_cast<const T *>(a.k) + j * a.ldk + koff, at, f.lanes, f.chunks);
+            v.load(static_cast<const T *>(a.v) + j * a.ldv + koff, at, f.lanes, f.chunks);
+        }
+        k.widen(w);
+        v.widen(y);
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            s[r] = dot<E>(q[r], w);
+            s[R + r] = dot<E>(g[r], y);
+        }
+        key_sums<2 * R>(s, f.lanes);
+#pragma unroll
+        for (int r = 0; r < R; ++r) sums.of[r] += on ? exp2_fast(fmaf(s[r], c1, -lse[r])) * (s[R + r] - d[r]) : 0.f;
+    }
+    for (int o = wide; o < 32; o <<= 1)
+#pragma unroll
+        for (int r = 0; r < R; ++r) sums.of[r] += __shfl_xor_sync(0xFFFFFFFFu, sums.of[r], o);
+    return sums;
+}
+
 // Backward pass of up to R rows over a stretch of the keys.  kBoth: the unit holds every row of its sequence and key head, so dK and
 // dV of a key are complete as soon as its own step is done and everything is read once; else only dQ (and D, in dots).  A sequence
 // that is longer than the launch was sized for has its rows done batch by batch and its keys' gradients apart.
@@ -540,7 +609,7 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
 // dS of a lone key 0.
 // Over more keys (kFit) D comes from the stored outputs, and what 16-bit ones lack, sum_j dS_j (0 with the exact D), is taken out at the end:
 // dQ = sum_j dS_j k_j - (sum_j dS_j) (sum_j p_j k_j).  dQ of rows that see 12 000 keys was 3.4e-3 off without it, 1.8e-3 so (a rounding:
-// 1.7e-3).
+// 1.7e-3).  Without kFit (a turn holds all keys, the caller said) longer sequences go over their keys twice (lacking).
 template <typename T, int R, int U, int CPL, bool kBoth, bool kFit>
 __global__ void __launch_bounds__(kFewThreads, CPL == 2 || R > 2 ? 2 : (R == 1 ? 4 : 3))
 attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_dq, float *__restrict__ dots)
@@ -553,7 +622,8 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     __shared__ float join[kFewWarps][E * 32];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int wu = warp & (f.warps - 1);
-    const Unit x = few_unit(a, f, blockIdx.x * (uint32_t)(kFewWarps / f.warps) + warp / f.warps);
+    const uint32_t unit = blockIdx.x * (uint32_t)(kFewWarps / f.warps) + warp / f.warps;
+    const Unit x = few_unit(a, f, unit);
     const int wide = f.lanes * f.heads, grp = lane / wide, at = lane & (f.lanes - 1), kpw = 32 / wide;
     const int heads = a.kv_heads * a.group;
     const int64_t koff = x.h * (int64_t)a.head_dim;
@@ -573,6 +643,9 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         float q[R][E], g[R][E], dq[R][E], lse[R], d[R];
         float mean[kFit ? R : 1][E], rest[R];             // sum_j p_j k_j; what D lacked
         const bool one_turn = f.warps == 1 && f.splits == 1 && x.ke - x.kb <= U * kpw;
+        RowSums<R> lack = {};
+        if constexpr (sizeof(T) == 2 && !kFit)
+            if (live && !one_turn) lack = lacking<T, R, CPL>(a, f, unit, r0);       // one warp per unit and one stretch: few_plan
         RowWalk in(a, x, r0);
 #pragma unroll
         for (int r = 0; r < R; ++r, in.next(a)) {
@@ -610,6 +683,9 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 for (int e = 0; e < E; ++e) mean[r][e] = 0.f;
         }
         key_sums<R>(d, f.lanes);
+        if constexpr (sizeof(T) == 2 && !kFit)
+#pragma unroll
+            for (int r = 0; r < R; ++r) d[r] += lack.of[r];
         for (int t = 0; live && t < ring.turns && ring.ok; ++t) {
             uint32_t word;
             const uint32_t at_k = ring.wait(word, t, &abort_flag) + grp * f.slice + mine, at_v = at_k + ring.half;
