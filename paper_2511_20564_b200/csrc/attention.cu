@@ -163,25 +163,30 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
 {
     Plan p{};
     p.splits = 1;
-    const int64_t max_q = s.max_q ? std::min(s.max_q, a.q_rows) : a.q_rows, max_k = s.max_k ? std::min(s.max_k, a.k_rows) : a.k_rows;
-    const int64_t rows = max_q * a.group, units = std::max<int64_t>(a.n_seq * a.kv_heads, 1);
+    auto lengths = [&](int64_t hint, int64_t all) {
+        Lengths l{hint ? std::min(hint, all) : all, ceil_div(all, std::max<int64_t>(a.n_seq, 1)), 0};
+        l.mean = std::min(l.mean, l.longest);
+        l.typical = hint ? l.longest : l.mean;
+        return l;
+    };
+    const Lengths q = lengths(s.max_q, a.q_rows), k = lengths(s.max_k, a.k_rows);
+    const int64_t rows = q.typical * a.group, units = std::max<int64_t>(a.n_seq * a.kv_heads, 1);
     const size_t cells = (size_t)a.q_rows * a.kv_heads * a.group;
-    const bool small = rows <= (backward ? 4 : dtype == E2EGREC_F32 ? 3 : 2) || rows * max_k <= (dtype == E2EGREC_F32 ? 256 : backward ? 700 : 800);
+    const bool small = rows <= (backward ? 4 : dtype == E2EGREC_F32 ? 3 : 2) || rows * k.typical <= (dtype == E2EGREC_F32 ? 256 : backward ? 700 : 800);
     // (without rows on one side there is nothing to form a product of)
     p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
     if (p.path == Path::tc) {
-        const int64_t most = (kMaxRows - 1) / units;
         p.one_tile = rows <= 128;
-        p.q_tiles = std::max<int64_t>(1, std::min(ceil_div(rows, backward || p.one_tile ? 128 : 256), most));
-        p.k_tiles = std::max<int64_t>(1, std::min(ceil_div(max_k, 128), most));
+        p.q_tiles = blocks_per_unit(q, a.group, backward || p.one_tile ? 128 : 256, units);
+        p.k_tiles = blocks_per_unit(k, 1, 128, units);
         const int64_t blocks = p.one_tile ? 296 : 148;
         if (!backward && units * p.q_tiles < blocks)
-            p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({blocks / (units * p.q_tiles), max_k / 512, kMaxSplits}));
+            p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({blocks / (units * p.q_tiles), k.longest / 512, kMaxSplits}));
     } else if (p.path == Path::simt) {
-        p.simt = simt_plan(a, max_q, max_k);
+        p.simt = simt_plan(a, q, k);
         p.splits = p.simt.splits;
     } else {
-        p.few = few_plan(a, max_q, max_k, (int)dtype_size(dtype), backward);
+        p.few = few_plan(a, q, k, (int)dtype_size(dtype), backward);
         p.splits = p.few.splits;
     }
     if (backward && !(p.path == Path::few && p.few.both)) p.dot_bytes = align_up(cells * sizeof(float), 256);

@@ -1,6 +1,8 @@
 // What the attention kernels share: their arguments, the ranges of a sequence, and the launchers of the translation units.
 #pragma once
 
+#include <algorithm>
+
 #include "common.cuh"
 
 namespace e2egrec {
@@ -56,6 +58,22 @@ __device__ inline int64_t owner(const int64_t *ptr, int64_t n_seq, int64_t row)
     return row < ptr[lo + 1] ? lo : -1;
 }
 
+// Lengths that a call is planned by: the longest that a sequence can have (the caller's hint, else all rows), the mean, and the one that
+// the kernels are chosen for: the hint, without one the mean.
+struct Lengths {
+    int64_t longest, mean, typical;
+};
+
+// Blocks per unit (a key head of a sequence) for pieces of `per` rows, which walk sequences of more pieces in rounds: as many as a sequence of
+// twice the mean takes, or kSpread in all if that is more.  Sized by the longest alone, the units of many sequences are nearly all empty
+// ones (4096 of one token and 62 states, longest unknown: 32 million of them, 104 ms, 0.4 so).
+constexpr int64_t kSpread = 148 * 64;
+inline int64_t blocks_per_unit(const Lengths &l, int64_t factor, int64_t per, int64_t units)
+{
+    const int64_t want = std::max(ceil_div(2 * l.mean * factor, per), ceil_div(kSpread, units));
+    return std::max<int64_t>(1, std::min({ceil_div(l.longest * factor, per), want, (((int64_t)1 << 31) - 1) / units}));
+}
+
 // attention_tc.cu: bf16, head_dim <= 128.  tiles: blocks of 256 rows (128 with one_tile) per sequence and key head, longer sequences go
 // round again; splits: stretches of the keys, whose results (out in fp32 and (maximum in powers of two, sum)) go to
 // part_o [splits x q_rows x heads x head_dim] and part_ml [splits x q_rows x heads] where splits > 1.
@@ -73,7 +91,7 @@ struct FewPlan {
     int warps, splits;                    // warps per unit, stretches of the keys
     int64_t key_batches;                  // units of keys of the dK, dV kernel
 };
-FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool backward);
+FewPlan few_plan(const AttnArgs &a, const Lengths &q, const Lengths &k, int es, bool backward);
 bool few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_o, float2 *part_ml, cudaStream_t st);
 // part_dq: [splits x q_rows x heads x head_dim] where splits > 1, twice that and [splits x q_rows x heads] with fit; dots: [q_rows x heads] where !both
 bool few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st);
@@ -87,7 +105,7 @@ struct SimtPlan {
     int64_t q_tiles, k_tiles;             // blocks of rows / of keys per sequence and key head
     int splits;                           // stretches of the keys (forward, dQ)
 };
-SimtPlan simt_plan(const AttnArgs &a, int64_t max_q, int64_t max_k);
+SimtPlan simt_plan(const AttnArgs &a, const Lengths &q, const Lengths &k);
 bool simt_attention_forward(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st);
 bool simt_attention_backward(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st);
 

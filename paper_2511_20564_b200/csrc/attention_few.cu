@@ -980,11 +980,12 @@ template <typename T> bool backward_of(const AttnArgs &a, const FewPlan &p, FewS
 }  // namespace
 
 // Rows per unit, warps per unit and stretches of the keys.  The aim is 24 warps per SM; a warp gets a turn of keys at least.
-FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool backward)
+FewPlan few_plan(const AttnArgs &a, const Lengths &q, const Lengths &k, int es, bool backward)
 {
     FewPlan p{};
     const FewShape f = few_shape(a, es);
-    const int64_t rows = max_q * a.group, units0 = std::max<int64_t>(a.n_seq * f.head_groups, 1), most = (((int64_t)1 << 31) - 1) / units0;
+    // (backward: rows that fit one unit have their keys' gradients in the same pass, which has to hold for every sequence)
+    const int64_t rows = (backward ? q.longest : q.typical) * a.group, max_k = k.longest, units0 = std::max<int64_t>(a.n_seq * f.head_groups, 1), most = (((int64_t)1 << 31) - 1) / units0;
     const int64_t step = 32 / (f.lanes * f.heads);
     p.rows = rows <= 1 ? 1 : (rows <= 2 ? 2 : 4);
     p.both = backward && rows <= p.rows;
@@ -992,13 +993,13 @@ FewPlan few_plan(const AttnArgs &a, int64_t max_q, int64_t max_k, int es, bool b
     while (p.steps * step > 32) p.steps /= 2;        // a turn's rows are the bits of a word
     const int64_t turn = step * p.steps;
     p.fit = backward && es == 2 && max_k > turn;
-    p.batches = std::max<int64_t>(1, std::min<int64_t>(ceil_div(rows, p.rows), most));
+    p.batches = blocks_per_unit(q, a.group, p.rows, units0);
     const int64_t want = std::max<int64_t>(1, std::min(ceil_div(148 * 24, units0 * p.batches), ceil_div(max_k, turn)));
     p.warps = 1;
     while (p.warps < kFewWarps && p.warps < want) p.warps *= 2;
     // a stretch is worth its join where every warp has four turns of it
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want / p.warps, max_k / (turn * p.warps * 4), kMaxSplits, most / p.batches}));
-    p.key_batches = std::max<int64_t>(1, std::min(ceil_div(max_k, step * kKeys), most));
+    p.key_batches = blocks_per_unit(k, 1, step * kKeys, units0);
     return p;
 }
 

@@ -546,16 +546,16 @@ template <int TX, int C, int I> bool backward_of(const AttnArgs &a, const SimtPl
 
 }  // namespace
 
-SimtPlan simt_plan(const AttnArgs &a, int64_t max_q, int64_t max_k)
+SimtPlan simt_plan(const AttnArgs &a, const Lengths &q, const Lengths &k)
 {
     SimtPlan p{};
-    const int64_t units = std::max<int64_t>(a.n_seq * a.kv_heads, 1), most = (((int64_t)1 << 31) - 1) / units, rows = max_q * a.group;
+    const int64_t units = std::max<int64_t>(a.n_seq * a.kv_heads, 1), most = (((int64_t)1 << 31) - 1) / units, rows = q.typical * a.group;
     p.rows = rows <= 16 ? 16 : (rows <= 32 ? 32 : 64);
-    p.q_tiles = std::max<int64_t>(1, std::min(ceil_div(rows, p.rows), most));
-    p.k_tiles = std::max<int64_t>(1, std::min(ceil_div(max_k, kTile), most));
+    p.q_tiles = blocks_per_unit(q, a.group, p.rows, units);
+    p.k_tiles = blocks_per_unit(k, 1, kTile, units);
     p.splits = 1;
     if (units * p.q_tiles < 296)
-        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({296 / (units * p.q_tiles), max_k / (2 * kTile), kMaxSplits, most / p.q_tiles}));
+        p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({296 / (units * p.q_tiles), k.longest / (2 * kTile), kMaxSplits, most / p.q_tiles}));
     return p;
 }
 
