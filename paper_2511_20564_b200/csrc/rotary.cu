@@ -340,7 +340,7 @@ qk_norm_grad_kernel(const __grid_constant__ RotArgs r)
                 }
                 q = lanes_sum(q, r.lanes);
                 d = lanes_sum(d, r.lanes);
-                const float rs = rsqrtf(q / (float)r.head_dim + r.eps);
+                const float rs = live ? rsqrtf(q / (float)r.head_dim + r.eps) : 0.f;      // (with eps = 0 no inverse of the zeros of no row)
                 const float m = d * rs * rs * rs / (float)r.head_dim;
 #pragma unroll
                 for (int i = 0; i < E; ++i) {
