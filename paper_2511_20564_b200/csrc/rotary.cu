@@ -153,19 +153,22 @@ template <typename T> __device__ inline void angle(const RotArgs &r, const uint2
     s *= r.scale * r.sign;
 }
 
-template <bool kInter, int V> __device__ inline void turn_unit(float *a, float *b, const float *c, const float *s)
+// The stretches of V values from pa and pb on; what lies behind the rotated part stays as it is (a product with sin 0 = 0 would pass on
+// infinities and NaN of a neighbour).
+template <bool kInter, int V> __device__ inline void turn_unit(float *a, float *b, const float *c, const float *s, int pa, int pb, int half)
 {
     if (kInter) {
 #pragma unroll
         for (int i = 0; i < V; i += 2) {
             const float u = a[i] * c[i / 2] - a[i + 1] * s[i / 2], v = a[i + 1] * c[i / 2] + a[i] * s[i / 2];
-            a[i] = u;
-            a[i + 1] = v;
             const float w = b[i] * c[V / 2 + i / 2] - b[i + 1] * s[V / 2 + i / 2], x = b[i + 1] * c[V / 2 + i / 2] + b[i] * s[V / 2 + i / 2];
-            b[i] = w;
-            b[i + 1] = x;
+            const bool first = pa + i < 2 * half, second = pb + i < 2 * half;
+            a[i] = first ? u : a[i];
+            a[i + 1] = first ? v : a[i + 1];
+            b[i] = second ? w : b[i];
+            b[i + 1] = second ? x : b[i + 1];
         }
-    } else {
+    } else if (pa < half) {
 #pragma unroll
         for (int i = 0; i < V; ++i) {
             const float u = a[i] * c[i] - b[i] * s[i], v = b[i] * c[i] + a[i] * s[i];
@@ -249,7 +252,7 @@ rotary_kernel(const __grid_constant__ RotArgs r)
             }
 #pragma unroll
             for (int j = 0; j < NU; ++j) {
-                turn_unit<kInter, V>(a + j * V, b + j * V, c + j * V, s + j * V);
+                turn_unit<kInter, V>(a + j * V, b + j * V, c + j * V, s + j * V, pa[j], pb[j], r.half);
                 if (pa[j] >= 0) *reinterpret_cast<Raw<T, V> *>(y + (int64_t)(h + u) * r.head_dim + pa[j]) = narrow<T, V>(a + j * V);
                 if (pb[j] >= 0) *reinterpret_cast<Raw<T, V> *>(y + (int64_t)(h + u) * r.head_dim + pb[j]) = narrow<T, V>(b + j * V);
             }
@@ -330,7 +333,7 @@ qk_norm_grad_kernel(const __grid_constant__ RotArgs r)
                     widen<T, V>(r1[u][j], b + j * V);
                     widen<T, V>(r2[u][j], da + j * V);
                     widen<T, V>(r3[u][j], db + j * V);
-                    turn_unit<kInter, V>(da + j * V, db + j * V, c + j * V, s + j * V);
+                    turn_unit<kInter, V>(da + j * V, db + j * V, c + j * V, s + j * V, pa[j], pb[j], r.half);
                 }
                 float q = 0.f, d = 0.f;
 #pragma unroll
