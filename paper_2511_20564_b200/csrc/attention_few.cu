@@ -12,6 +12,7 @@
 #include <atomic>
 
 #include "attention.cuh"
+#include "ring_turns.h"
 #include "tcgen05.cuh"
 
 namespace e2egrec {
@@ -20,7 +21,7 @@ namespace {
 constexpr int kFewThreads = 128, kFewWarps = kFewThreads / 32;
 constexpr int kUnroll = 4;                           // steps of a turn (fewer where they hold all keys of a sequence, for many keys a
                                                      // step, and 2 for more than two rows, whose registers four would take)
-constexpr int kStages = 3;
+constexpr int kStages = kRingStages;
 
 template <typename T, int CPL> struct Piece {        // a lane's part of a head's row
     static constexpr int E = Chunk<T>::kElems * CPL;
@@ -148,7 +149,7 @@ struct Ring {
     __device__ inline void start()
     {
         next_mask = turns > 0 ? mask_of(0) : 0;
-        for (int t = 0; t < turns && t < kStages; ++t) fill(t, used + t);
+        for (int t = 0; t < ring_first(turns, ok); ++t) fill(t, used + t);
     }
     // waits for turn t; its stage's address, and which of its rows are seen
     __device__ inline uint32_t wait(uint32_t &word, int t, volatile int *abort_flag)
@@ -158,17 +159,18 @@ struct Ring {
         word = ok ? seen[use % kStages] : 0u;
         return base + use % kStages * 2 * half;
     }
-    // giving up after turn t: the copies behind it land before the shared memory is released
+    // the wait for turn t is given up: copies on their way land before the shared memory is released, and start() starts no others
     __device__ inline void land(int t)
     {
         int never = 0;
-        for (int i = t + 1; i < turns && i < t + kStages; ++i) mbar_wait(bar + (used + i) % kStages, (used + i) / kStages & 1u, &never);
+        for (int i = t; i < ring_pending(t, turns); ++i) mbar_wait(bar + (used + i) % kStages, (used + i) / kStages & 1u, &never);
     }
     // turn t has been read by the whole warp
     __device__ inline void done(int t)
     {
         __syncwarp();
-        if (t + kStages < turns && ok) fill(t + kStages, used + t + kStages);
+        const int next = ring_next(t, turns, ok);
+        if (next >= 0) fill(next, used + next);
     }
 };
 
