@@ -512,7 +512,7 @@ typedef struct e2egrec_sequences {
  * a key head); out overlaps no input.  A query that sees no key gets out = 0 and lse = -inf, and passes on no gradient.  What
  * hidden keys and rows outside the sequences hold (infinities, NaN) has no influence; rows of out, lse and of the gradients outside
  * every sequence are left as they were.  Q, out: [rows x n_heads head_dim]; K, V: [rows x n_kv_heads head_dim] of one number of
- * rows; 0 < scale <= 1e38.
+ * rows; 0 < scale <= 1e38; at most 2^31 - 65536 rows each.
  *   lse     device float[Q rows x n_heads], row-major; may be NULL (serving: nothing is kept for a backward pass)
  *   status  optional device int32, receives E2EGREC_DEV_RANGE (or-ed) if offsets decrease or leave the matrices (the rows at fault
  *           are skipped) and E2EGREC_DEV_TIMEOUT if a wait inside a kernel ran out

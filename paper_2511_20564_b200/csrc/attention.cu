@@ -142,7 +142,8 @@ int32_t check_heads(const e2egrec_mat *m, int32_t heads, int32_t head_dim, int32
     return E2EGREC_OK;
 }
 
-constexpr int64_t kMaxRows = (int64_t)1 << 31;
+constexpr int64_t kMaxUnits = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMaxRows = ((int64_t)1 << 31) - (1 << 16);      // the kernels step some hundred rows beyond a sequence's end in 32 bits
 
 // The kernels of a call.  A sequence's keys and rows stream (attention_few.cu) where a key head has up to two rows (fp32 three: 300 of
 // 3 x 200, 88 us against 113; four in the backward pass), or where a sequence is so small that the set-up of a tile costs more than its
@@ -213,8 +214,8 @@ int32_t check_shape(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_se
     if (!Q || !K || !seqs) return E2EGREC_ERR_NULL;
     if (Q->dtype != E2EGREC_F32 && Q->dtype != E2EGREC_BF16) return E2EGREC_ERR_DTYPE;
     if (n_kv_heads < 1 || n_heads < n_kv_heads || n_heads % n_kv_heads || Q->dim < 1 || Q->dim % n_heads) return E2EGREC_ERR_ARG;
-    if (Q->rows < 0 || K->rows < 0 || Q->rows >= kMaxRows || K->rows >= kMaxRows) return E2EGREC_ERR_ARG;
-    if (seqs->n_seq < 0 || seqs->n_seq > (kMaxRows - 1) / n_kv_heads || seqs->max_q < 0 || seqs->max_k < 0) return E2EGREC_ERR_ARG;
+    if (Q->rows < 0 || K->rows < 0 || Q->rows > kMaxRows || K->rows > kMaxRows) return E2EGREC_ERR_ARG;
+    if (seqs->n_seq < 0 || seqs->n_seq > kMaxUnits / n_kv_heads || seqs->max_q < 0 || seqs->max_k < 0) return E2EGREC_ERR_ARG;
     if (!(scale > 0.f) || !(scale <= 1.0e38f)) return E2EGREC_ERR_ARG;
     if (Q->dim / n_heads > kMaxAttnDim) return E2EGREC_ERR_UNSUPPORTED;
     a.n_seq = seqs->n_seq;
