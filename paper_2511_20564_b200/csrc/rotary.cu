@@ -9,8 +9,9 @@
 // angles of its pairs are formed once per row; the lanes of one head are neighbours, and a head's sum of squares is a handful of
 // shuffles.  (One thread per unit and head, whose accesses are whole lines, forms every angle once per head: 21 us instead of 15
 // for 65 536 rows of 4 heads of 64 bf16 values.)
-// Angles: a frequency becomes a 64-bit fraction of a turn, once per block and pair; its product with a 32-bit position modulo one turn
-// is two integer products, exact to 2^-32 of a turn wherever the position lies, where a product in 32-bit floating point has no digit
+// Angles: a frequency becomes a 64-bit fraction of a turn, once per block and pair (1 / 2 pi and the product in two doubles: what one
+// product loses a far position multiplies, 2^-25 of a turn for 1 radian per position and 2^-15 for a thousand); its product with a 32-bit
+// position modulo one turn is two integer products, exact to 2^-32 of a turn wherever the position lies, where a product in 32-bit floating point has no digit
 // left beyond position 2^23.
 #include <algorithm>
 
@@ -118,15 +119,16 @@ template <int V, bool kInter> struct Places {
 __device__ inline void make_turns(const RotArgs &r, uint2 *turns)
 {
     for (int f = threadIdx.x; f < r.half; f += kRotThreads) {
-        const double t = __ldg(r.freqs + f) * 0.15915494309189533577;
-        const unsigned long long n = __double2ull_rz((t - floor(t)) * 18446744073709551616.0);
+        const double freq = __ldg(r.freqs + f), hi = 0.15915494309189535, lo = -9.839338337591243e-18;      // 1 / 2 pi = hi + lo
+        const double t = freq * hi, rest = fma(freq, lo, fma(freq, hi, -t));
+        const unsigned long long n = __double2ull_rz((t - floor(t)) * 18446744073709551616.0) + (unsigned long long)__double2ll_rn(rest * 18446744073709551616.0);
         turns[f] = make_uint2((uint32_t)(n >> 32), (uint32_t)n);
     }
     __syncthreads();
 }
 
 // scale * (cos, sin) of pair f at position p; (1, 0) for pairs that are not rotated.  With 16-bit results the hardware's sine and
-// cosine of the angle to 2^-24 of a turn are off by 2^-20, a 2^11th of the result's own rounding.  For 32-bit results the angle is
+// cosine of the angle to 2^-24 of a turn are off by less than 2^-19.8, a 2^10th of the result's own rounding.  For 32-bit results the angle is
 // taken to the nearest quarter turn, |x| <= pi / 4, and the Taylor series of sine and cosine broken off behind x^9 and x^8 (the next terms
 // are below 2^-28 and 2^-25); the quarter turns swap the two and set signs.
 template <typename T> __device__ inline void angle(const RotArgs &r, const uint2 *turns, int f, int p, float &c, float &s)
@@ -137,8 +139,8 @@ template <typename T> __device__ inline void angle(const RotArgs &r, const uint2
     const uint2 t = turns[f];
     const uint32_t frac = t.x * (uint32_t)p + __umulhi(t.y, (uint32_t)p) - (p < 0 ? t.y : 0u);      // of 2^32, modulo a turn
     if (sizeof(T) == 2) {
-        // 1.5 + the signed fraction of a turn, from the bits
-        const float a = (__uint_as_float(0x3F800000u | ((frac + 0x80000000u) >> 9)) - 1.5f) * 6.28318530718f;
+        // 1.5 + the signed fraction of a turn, from the bits, rounded to 23 of them (half a turn up may come out as half a turn down)
+        const float a = (__uint_as_float(0x3F800000u | ((frac + 0x80000100u) >> 9)) - 1.5f) * 6.28318530718f;
         c = __cosf(a);
         s = __sinf(a);
     } else {
