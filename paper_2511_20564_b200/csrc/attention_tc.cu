@@ -16,6 +16,7 @@
 #include "attention.cuh"
 #include "tcgen05.cuh"
 #include "tensor_map.cuh"
+#include "tile_ring.h"
 
 namespace e2egrec {
 namespace {
@@ -24,7 +25,6 @@ using bf16 = __nv_bfloat16;
 
 constexpr int kTile = 128;
 constexpr int kBlockBytes = kTile * 128;             // 64 columns of 128 rows
-constexpr int kWordRing = 8;                         // tiles whose visibility words are kept
 constexpr int kSms = 148;
 
 __device__ inline float exp2_approx(float x)
@@ -232,6 +232,12 @@ __device__ inline void let_land(uint64_t *bars, uint32_t stages, uint32_t issued
     int never = 0;
     for (uint32_t j = issued > stages ? issued - stages : 0; j < issued; ++j) mbar_wait(&bars[j % stages], (j / stages) & 1u, &never);
 }
+// the same for the copies of a ring of two sides, 0 .. g - 1
+template <typename R> __device__ inline void let_land_both(uint64_t *bars, uint32_t g)
+{
+    int never = 0;
+    for (uint32_t j = g > R::kSlots ? g - R::kSlots : 0; j < g; ++j) mbar_wait(&bars[R::full(j)], R::parity(j), &never);
+}
 
 // Products of one tile, K step by K step, with descriptors that move on by constants: the instruction stream of the one issuing lane
 // is what feeds the tensor cores (with descriptors built anew for every step an instruction took 122 cycles, its execution 64).
@@ -255,13 +261,13 @@ __device__ inline void row_steps(uint32_t d, uint32_t a, uint32_t second, uint64
 // keys and values, and the products of one run beside the softmax of the other.  One, in half of the shared and tensor memory, where
 // the second would idle: two such blocks per SM overlap instead.
 template <int NB, int NT> struct Fwd {
-    static constexpr int kStages = NT == 2 ? (NB == 2 ? 5 : 8) : (NB == 2 ? 2 : 5);
+    using Ring = TileRing<NT == 2 ? (NB == 2 ? 5 : 8) : (NB == 2 ? 2 : 5)>;      // keys and values
     static constexpr int kSoft = NT * 4, kThreads = (kSoft + 4) * 32, kBlocks = 3 - NT;      // copies, zeros, products; one idle
     static constexpr int kRows = NT * kTile, kTileBytes = NB * kBlockBytes, kColumns = NT * 256;
     // p goes to the product in halves where heads take up to 64 columns, the second formed beside the product of the first: 37 x 256 x 8192
     // with 4 heads of 64 158 -> 141 us, one-tile blocks 55 -> 48 us; with heads of 128 158 -> 167 us, so whole there
     static constexpr int kParts = NB == 1 ? 2 : 1;
-    static constexpr size_t kSmem = 1024 + (size_t)(NT + kStages) * kTileBytes;
+    static constexpr size_t kSmem = 1024 + (size_t)(NT + Ring::kSlots) * kTileBytes;
 };
 
 template <int NB, int NT>
@@ -270,9 +276,10 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                    const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
 {
     using F = Fwd<NB, NT>;
-    constexpr int kStages = F::kStages, kTileBytes = F::kTileBytes, kRows = F::kRows, kSoft = F::kSoft;
+    using R = typename F::Ring;
+    constexpr int kTileBytes = F::kTileBytes, kRows = F::kRows, kSoft = F::kSoft;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], v_clean[kWordRing], q_full, q_empty, s_full[NT], p_full[NT][F::kParts], o_full[NT], o_empty[NT];
+    __shared__ uint64_t kv_full[R::kBarriers], kv_empty[R::kSlots], v_clean[kWordRing], q_full, q_empty, s_full[NT], p_full[NT][F::kParts], o_full[NT], o_empty[NT];
     __shared__ __align__(16) uint32_t words[kWordRing][4];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
@@ -283,10 +290,8 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     const int ksteps = (a.head_dim + 15) / 16;
 
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            mbar_init(&kv_full[s], 1);
-            mbar_init(&kv_empty[s], 1);
-        }
+        for (int s = 0; s < R::kBarriers; ++s) mbar_init(&kv_full[s], 1);
+        for (int s = 0; s < R::kSlots; ++s) mbar_init(&kv_empty[s], 1);
         for (int s = 0; s < kWordRing; ++s) mbar_init(&v_clean[s], 1);
         mbar_init(&q_full, f.boxes ? 1 : kCopyArrivals);
         mbar_init(&q_empty, 1);
@@ -346,20 +351,20 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         seen.now(word);
                         if (j + 1 < x.n) seen.ahead(a, x, j + 1, lane);
                         for (int v = 0; v < 2; ++v, ++g) {
-                            const uint32_t s = g % kStages;
-                            if (g >= kStages) ok = warp_wait(&kv_empty[s], (g / kStages - 1) & 1u, &abort_flag);
+                            const uint32_t s = R::slot(g);
+                            if (g >= R::kSlots) ok = warp_wait(&kv_empty[s], (R::use(g) - 1) & 1u, &abort_flag);
                             if (!ok) break;
                             if (lane == 0) {
                                 if (v == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
-                                mbar_expect_tx(&kv_full[s], kTileBytes);
-                                load_tile<NB>(kv_smem + s * kTileBytes, v ? &map_v : &map_k, x.h, x.kb + (int64_t)j * kTile, &kv_full[s]);
+                                mbar_expect_tx(&kv_full[R::full(g)], kTileBytes);
+                                load_tile<NB>(kv_smem + s * kTileBytes, v ? &map_v : &map_k, x.h, x.kb + (int64_t)j * kTile, &kv_full[R::full(g)]);
                             }
                         }
                     }
                 }
             }
             if (!ok && lane == 0) {
-                let_land(kv_full, kStages, g);
+                let_land_both<R>(kv_full, g);
                 if (q_issued) let_land(&q_full, 1, q_issued);
             }
             cp_async_wait_all();
@@ -371,11 +376,11 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const Work x = work_of(a, f, u, false);
                 for (int64_t t = x.t0; t * kRows < x.rows && x.n > 0 && ok; t += f.tiles)
                     for (int j = 0; j < x.n && ok; ++j, ++jj, g += 2) {
-                        ok = warp_wait(&kv_full[g % kStages], (g / kStages) & 1u, &abort_flag);
+                        ok = warp_wait(&kv_full[R::full(g)], R::parity(g), &abort_flag);
                         if (!ok) break;
                         const uint4 w4 = *reinterpret_cast<const uint4 *>(words[jj % kWordRing]);
                         const uint32_t word[4] = {w4.x, w4.y, w4.z, w4.w};
-                        if (!all_seen(word)) clear_rows<NB>(kv_smem + (g % kStages) * kTileBytes, word, lane);
+                        if (!all_seen(word)) clear_rows<NB>(kv_smem + R::slot(g) * kTileBytes, word, lane);
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&v_clean[jj % kWordRing]);
                     }
@@ -387,7 +392,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 uint32_t g = 0, jj = 0, item = 0, pc[NT] = {}, used[NT] = {};
                 bool ok = true;
                 auto scores = [&](uint32_t gk, int q) {
-                    head_steps<NB>(tmem + q * kTile, make_smem_desc(q_smem + q * kTileBytes), make_smem_desc(kv_smem + (gk % kStages) * kTileBytes), id_s,
+                    head_steps<NB>(tmem + q * kTile, make_smem_desc(q_smem + q * kTileBytes), make_smem_desc(kv_smem + R::slot(gk) * kTileBytes), id_s,
                                    ksteps);
                     umma_commit(&s_full[q]);
                 };
@@ -396,7 +401,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     for (int64_t t = x.t0; t * kRows < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                         const int nt = NT == 2 && x.rows - t * kRows > kTile ? 2 : 1;
                         ok = tile_ready(&q_full, item & 1u, &abort_flag);
-                        if (ok) ok = tile_ready(&kv_full[g % kStages], (g / kStages) & 1u, &abort_flag);
+                        if (ok) ok = tile_ready(&kv_full[R::full(g)], R::parity(g), &abort_flag);
 #pragma unroll
                         for (int q = 0; q < NT; ++q)
                             if (q < nt && ok) {
@@ -406,11 +411,11 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                                 if (ok) scores(g, q);
                                 ++used[q];
                             }
-                        if (ok) umma_commit(&kv_empty[g % kStages]);
+                        if (ok) umma_commit(&kv_empty[R::slot(g)]);
                         for (int j = 0; j < x.n && ok; ++j, ++jj, g += 2) {
                             const uint32_t gv = g + 1, gk = g + 2;
-                            const uint64_t v_desc = make_smem_desc_mn(kv_smem + (gv % kStages) * kTileBytes, kBlockBytes);
-                            ok = tile_ready(&kv_full[gv % kStages], (gv / kStages) & 1u, &abort_flag);
+                            const uint64_t v_desc = make_smem_desc_mn(kv_smem + R::slot(gv) * kTileBytes, kBlockBytes);
+                            ok = tile_ready(&kv_full[R::full(gv)], R::parity(gv), &abort_flag);
                             if (ok) ok = tile_ready(&v_clean[jj % kWordRing], (jj / kWordRing) & 1u, &abort_flag);
 #pragma unroll
                             for (int q = 0; q < NT; ++q) {
@@ -426,15 +431,15 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                                 ++pc[q];
                                 if (!ok) continue;
                                 if (j + 1 < x.n) {
-                                    if (q == nt - 1) umma_commit(&kv_empty[gv % kStages]);
-                                    if (q == 0) ok = tile_ready(&kv_full[gk % kStages], (gk / kStages) & 1u, &abort_flag);
+                                    if (q == nt - 1) umma_commit(&kv_empty[R::slot(gv)]);
+                                    if (q == 0) ok = tile_ready(&kv_full[R::full(gk)], R::parity(gk), &abort_flag);
                                     if (!ok) continue;
                                     scores(gk, q);
-                                    if (q == nt - 1) umma_commit(&kv_empty[gk % kStages]);
+                                    if (q == nt - 1) umma_commit(&kv_empty[R::slot(gk)]);
                                 } else {
                                     umma_commit(&o_full[q]);
                                     if (q == nt - 1) {
-                                        umma_commit(&kv_empty[gv % kStages]);
+                                        umma_commit(&kv_empty[R::slot(gv)]);
                                         umma_commit(&q_empty);
                                     }
                                 }
@@ -593,8 +598,9 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 // tile of keys; the scores are formed in both.  Two warpgroups share a tile of 128 x 128: 64 columns each, one row per thread.
 template <int NB> struct Bwd {
     static constexpr int kThreads = 12 * 32, kTileBytes = NB * kBlockBytes;      // copies, zeros, products; one idle
-    static constexpr int kKvStages = NB == 2 ? 5 : 8, kQgStages = NB == 2 ? 4 : 8;
-    static constexpr size_t kDqSmem = 1024 + (size_t)(2 + kKvStages) * kTileBytes, kDkvSmem = 1024 + (size_t)(2 + kQgStages) * kTileBytes;
+    using KvRing = TileRing<NB == 2 ? 5 : 8>;
+    static constexpr int kQgStages = NB == 2 ? 4 : 8;
+    static constexpr size_t kDqSmem = 1024 + (size_t)(2 + KvRing::kSlots) * kTileBytes, kDkvSmem = 1024 + (size_t)(2 + kQgStages) * kTileBytes;
 };
 
 // 64 columns of p or dS of a thread's row as an operand in tensor memory: 32 packed columns (the second warpgroup's lie 64 behind the
@@ -654,9 +660,10 @@ __global__ void __launch_bounds__(Bwd<NB>::kThreads, 1)
 attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_k,
                   const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f, float *__restrict__ dots)
 {
-    constexpr int kStages = Bwd<NB>::kKvStages, kTileBytes = Bwd<NB>::kTileBytes;
+    using R = typename Bwd<NB>::KvRing;
+    constexpr int kTileBytes = Bwd<NB>::kTileBytes;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kv_full[kStages], kv_empty[kStages], k_clean[kWordRing], q_full, q_empty, s_full[2], dp_full, ds_full, o_full, o_empty, rest_full;
+    __shared__ uint64_t kv_full[R::kBarriers], kv_empty[R::kSlots], k_clean[kWordRing], q_full, q_empty, s_full[2], dp_full, ds_full, o_full, o_empty, rest_full;
     __shared__ float rests[2][kTile];                 // sums of p (dP - D) over each warpgroup's columns
     __shared__ __align__(16) uint32_t words[kWordRing][4];
     __shared__ uint32_t tmem_slot;
@@ -667,10 +674,8 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     const uint32_t q_smem = smem_u32(tiles_smem), g_smem = q_smem + kTileBytes, kv_smem = q_smem + 2 * kTileBytes;
     const int ksteps = (a.head_dim + 15) / 16;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < kStages; ++s) {
-            mbar_init(&kv_full[s], 1);
-            mbar_init(&kv_empty[s], 1);
-        }
+        for (int s = 0; s < R::kBarriers; ++s) mbar_init(&kv_full[s], 1);
+        for (int s = 0; s < R::kSlots; ++s) mbar_init(&kv_empty[s], 1);
         for (int s = 0; s < kWordRing; ++s) mbar_init(&k_clean[s], 1);
         mbar_init(&q_full, f.boxes ? 1 : kCopyArrivals);
         mbar_init(&q_empty, 1);
@@ -731,20 +736,20 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                         seen.now(word);
                         if (j + 1 < x.n) seen.ahead(a, x, j + 1, lane);
                         for (int v = 0; v < 2; ++v, ++g) {
-                            const uint32_t s = g % kStages;
-                            if (g >= kStages) ok = warp_wait(&kv_empty[s], (g / kStages - 1) & 1u, &abort_flag);
+                            const uint32_t s = R::slot(g);
+                            if (g >= R::kSlots) ok = warp_wait(&kv_empty[s], (R::use(g) - 1) & 1u, &abort_flag);
                             if (!ok) break;
                             if (lane == 0) {
                                 if (v == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
-                                mbar_expect_tx(&kv_full[s], kTileBytes);
-                                load_tile<NB>(kv_smem + s * kTileBytes, v ? &map_v : &map_k, x.h, x.kb + (int64_t)j * kTile, &kv_full[s]);
+                                mbar_expect_tx(&kv_full[R::full(g)], kTileBytes);
+                                load_tile<NB>(kv_smem + s * kTileBytes, v ? &map_v : &map_k, x.h, x.kb + (int64_t)j * kTile, &kv_full[R::full(g)]);
                             }
                         }
                     }
                 }
             }
             if (!ok && lane == 0) {
-                let_land(kv_full, kStages, g);
+                let_land_both<R>(kv_full, g);
                 if (q_issued) let_land(&q_full, 1, q_issued);
             }
             cp_async_wait_all();
@@ -756,11 +761,11 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 const Work x = work_of(a, f, u, false);
                 for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles)
                     for (int j = 0; j < x.n && ok; ++j, ++jj, g += 2) {
-                        ok = warp_wait(&kv_full[g % kStages], (g / kStages) & 1u, &abort_flag);
+                        ok = warp_wait(&kv_full[R::full(g)], R::parity(g), &abort_flag);
                         if (!ok) break;
                         const uint4 w4 = *reinterpret_cast<const uint4 *>(words[jj % kWordRing]);
                         const uint32_t word[4] = {w4.x, w4.y, w4.z, w4.w};
-                        if (!all_seen(word)) clear_rows<NB>(kv_smem + (g % kStages) * kTileBytes, word, lane);
+                        if (!all_seen(word)) clear_rows<NB>(kv_smem + R::slot(g) * kTileBytes, word, lane);
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&k_clean[jj % kWordRing]);
                     }
@@ -774,10 +779,10 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 uint32_t g = 0, item = 0, jj = 0;
                 bool ok = true;
                 auto product = [&](uint32_t d, uint64_t a_desc, uint32_t slot) {
-                    head_steps<NB>(d, a_desc, make_smem_desc(kv_smem + (slot % kStages) * kTileBytes), id_s, ksteps);
+                    head_steps<NB>(d, a_desc, make_smem_desc(kv_smem + R::slot(slot) * kTileBytes), id_s, ksteps);
                 };
                 auto full = [&](uint32_t slot) {
-                    ok = ok && tile_ready(&kv_full[slot % kStages], (slot / kStages) & 1u, &abort_flag);
+                    ok = ok && tile_ready(&kv_full[R::full(slot)], R::parity(slot), &abort_flag);
                     return ok;
                 };
                 for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
@@ -791,7 +796,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                         if (!full(g + 1)) break;
                         product(tmem + 256, g_desc, g + 1);
                         umma_commit(&dp_full);
-                        umma_commit(&kv_empty[(g + 1) % kStages]);
+                        umma_commit(&kv_empty[R::slot(g + 1)]);
                         for (int j = 0; j < x.n; ++j, g += 2, ++jj) {
                             if (j + 1 < x.n) {
                                 if (!full(g + 2)) break;
@@ -801,17 +806,17 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                             ok = tile_ready(&k_clean[jj % kWordRing], (jj / kWordRing) & 1u, &abort_flag) && mbar_wait(&ds_full, jj & 1u, &abort_flag);
                             if (!ok) break;
                             tc_fence_after();
-                            const uint64_t k_desc = make_smem_desc_mn(kv_smem + (g % kStages) * kTileBytes, kBlockBytes);
+                            const uint64_t k_desc = make_smem_desc_mn(kv_smem + R::slot(g) * kTileBytes, kBlockBytes);
                             row_steps(tmem + 384, tmem + 256, 32, k_desc, id_o, j > 0);
                             if (j + 1 < x.n) {
                                 if (!full(g + 3)) break;
                                 product(tmem + 256, g_desc, g + 3);
                                 umma_commit(&dp_full);
-                                umma_commit(&kv_empty[(g + 3) % kStages]);
+                                umma_commit(&kv_empty[R::slot(g + 3)]);
                             }
                             // the rest of dS, where the scores were: behind dP, which the warpgroups wait for
                             row_steps(tmem + 384, tmem + (jj & 1u) * kTile, 32, k_desc, id_o, true);
-                            umma_commit(&kv_empty[g % kStages]);
+                            umma_commit(&kv_empty[R::slot(g)]);
                             if (j + 1 == x.n) {
                                 umma_commit(&o_full);
                                 umma_commit(&q_empty);
