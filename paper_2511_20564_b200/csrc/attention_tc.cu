@@ -651,10 +651,16 @@ __device__ inline void store_row(uint32_t taddr, bf16 *out, int head_dim, float 
     }
 }
 
-// dQ, and D = dO . out of every row for the other kernel.  Where one tile holds all keys, what the stored out's D lacks, the sum of
-// p (dP - D), is added to it: dS of a lone key is 0 then, and the rounding of out does not show.  dS goes into its product as two bf16 operands, its rounding and the rest: D comes
+// dQ, and D = dO . out of every row for the other kernel.  What the stored out's D lacks is the sum of p (dP - D) over the keys; it meets
+// sum p k in dQ, which does not get smaller with the number of keys, as dQ does.  Where one tile holds all keys it is added to D before dS is
+// formed: dS of a lone key is 0 then.  Over more than 32 head_dim keys it comes from a pass over them that forms p and dP alone (dQ of 26 000
+// keys and heads of 16: 9.6e-3 off without, 1.7e-3 so; 20 000 and 64: 5.3e-3, 1.6e-3; 8 x 512 x 16 384, four heads of 64, backward: 505 us,
+// 684 so); in between it is left out, about a rounding of the result for values whose mean is a quarter of their spread.  dS goes into its product as two bf16 operands, its rounding and the rest: D comes
 // from 16-bit outputs already, and with dS rounded as well dQ was 2.5 to 2.7e-3 off in the mean (a rounding of the result: 1.8e-3),
 // at most 2.4e-3 so, dK included; the training case's backward pass takes 550 us with one operand, 585 us so.
+// Passes over the keys
+__device__ inline int passes_of(const Work &x, int head_dim) { return (int64_t)x.n * kTile > 32 * head_dim ? 2 : 1; }
+
 template <int NB>
 __global__ void __launch_bounds__(Bwd<NB>::kThreads, 1)
 attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_k,
@@ -707,6 +713,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             bool ok = true;
             for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
                 const Work x = work_of(a, f, u, lane == 0);
+                const int steps = x.n * passes_of(x, a.head_dim);
                 for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                     Visible seen;
                     seen.ahead(a, x, 0, lane);
@@ -731,10 +738,11 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                         }
                         announce_copies(&q_full, lane);
                     }
-                    for (int j = 0; j < x.n && ok; ++j, ++jj) {
+                    for (int j = 0, tile = 0; j < steps && ok; ++j, ++jj) {
+                        const int next = tile + 1 < x.n ? tile + 1 : 0;
                         uint32_t word[4];
                         seen.now(word);
-                        if (j + 1 < x.n) seen.ahead(a, x, j + 1, lane);
+                        if (j + 1 < steps) seen.ahead(a, x, next, lane);
                         for (int v = 0; v < 2; ++v, ++g) {
                             const uint32_t s = R::slot(g);
                             if (g >= R::kSlots) ok = warp_wait(&kv_empty[s], (R::use(g) - 1) & 1u, &abort_flag);
@@ -742,9 +750,10 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                             if (lane == 0) {
                                 if (v == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
                                 mbar_expect_tx(&kv_full[R::full(g)], kTileBytes);
-                                load_tile<NB>(kv_smem + s * kTileBytes, v ? &map_v : &map_k, x.h, x.kb + (int64_t)j * kTile, &kv_full[R::full(g)]);
+                                load_tile<NB>(kv_smem + s * kTileBytes, v ? &map_v : &map_k, x.h, x.kb + (int64_t)tile * kTile, &kv_full[R::full(g)]);
                             }
                         }
+                        tile = next;
                     }
                 }
             }
@@ -759,8 +768,9 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             bool ok = true;
             for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
                 const Work x = work_of(a, f, u, false);
+                const int steps = x.n * passes_of(x, a.head_dim);
                 for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles)
-                    for (int j = 0; j < x.n && ok; ++j, ++jj, g += 2) {
+                    for (int j = 0; j < steps && ok; ++j, ++jj, g += 2) {
                         ok = warp_wait(&kv_full[R::full(g)], R::parity(g), &abort_flag);
                         if (!ok) break;
                         const uint4 w4 = *reinterpret_cast<const uint4 *>(words[jj % kWordRing]);
@@ -787,6 +797,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 };
                 for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
                     const Work x = work_of(a, f, u, false);
+                    const int steps = x.n * passes_of(x, a.head_dim), first = steps - x.n;      // of the last pass
                     for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                         ok = tile_ready(&q_full, item & 1u, &abort_flag);
                         if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
@@ -797,8 +808,8 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                         product(tmem + 256, g_desc, g + 1);
                         umma_commit(&dp_full);
                         umma_commit(&kv_empty[R::slot(g + 1)]);
-                        for (int j = 0; j < x.n; ++j, g += 2, ++jj) {
-                            if (j + 1 < x.n) {
+                        for (int j = 0; j < steps; ++j, g += 2, ++jj) {
+                            if (j + 1 < steps) {
                                 if (!full(g + 2)) break;
                                 product(tmem + ((jj + 1) & 1u) * kTile, q_desc, g + 2);
                                 umma_commit(&s_full[(jj + 1) & 1u]);
@@ -807,17 +818,17 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                             if (!ok) break;
                             tc_fence_after();
                             const uint64_t k_desc = make_smem_desc_mn(kv_smem + R::slot(g) * kTileBytes, kBlockBytes);
-                            row_steps(tmem + 384, tmem + 256, 32, k_desc, id_o, j > 0);
-                            if (j + 1 < x.n) {
+                            if (j >= first) row_steps(tmem + 384, tmem + 256, 32, k_desc, id_o, j > first);
+                            if (j + 1 < steps) {
                                 if (!full(g + 3)) break;
                                 product(tmem + 256, g_desc, g + 3);
                                 umma_commit(&dp_full);
                                 umma_commit(&kv_empty[R::slot(g + 3)]);
                             }
                             // the rest of dS, where the scores were: behind dP, which the warpgroups wait for
-                            row_steps(tmem + 384, tmem + (jj & 1u) * kTile, 32, k_desc, id_o, true);
+                            if (j >= first) row_steps(tmem + 384, tmem + (jj & 1u) * kTile, 32, k_desc, id_o, true);
                             umma_commit(&kv_empty[R::slot(g)]);
-                            if (j + 1 == x.n) {
+                            if (j + 1 == steps) {
                                 umma_commit(&o_full);
                                 umma_commit(&q_empty);
                             }
@@ -833,10 +844,11 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
         const float c1 = a.scale * kLog2e;
         const int heads = a.kv_heads * a.group;
-        uint32_t jj = 0, item = 0, alone = 0;
+        uint32_t jj = 0, item = 0, corrected = 0;
         bool ok = true;
         for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
             const Work x = work_of(a, f, u, false);
+            const int steps = x.n * passes_of(x, a.head_dim), first = steps - x.n;
             for (int64_t t = x.t0; t * kTile < x.rows && ok; t += f.tiles) {
                 const int64_t r = t * kTile + w * 32 + lane;
                 int64_t row;
@@ -859,7 +871,8 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     }
                     if (l == -INFINITY) dot = 0.f;
                 }
-                for (int j = 0; j < x.n; ++j, ++jj) {
+                float rest = 0.f;
+                for (int j = 0; j < steps; ++j, ++jj) {
                     ok = warp_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
                     if (!ok) break;
                     tc_fence_after();
@@ -879,24 +892,34 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     ok = warp_wait(&dp_full, jj & 1u, &abort_flag);
                     if (!ok) break;
                     tc_fence_after();
-                    if (x.n == 1) {
+                    if (j < first || x.n == 1) {
                         uint32_t v[2][32];
                         tmem_load32_async(tmem + lanes + 256 + q * 64, v[0]);
                         tmem_load32_async(tmem + lanes + 256 + q * 64 + 32, v[1]);
                         tmem_load_wait();
-                        float rest = 0.f;
+                        float sums[4] = {};
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
                             const uint32_t word = words[jj % kWordRing][q * 2 + c];
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) rest += (word >> e) & 1u ? p[c * 32 + e] * (__uint_as_float(v[c][e]) - dot) : 0.f;
+                            for (int e = 0; e < 32; ++e) sums[e & 3] += (word >> e) & 1u ? p[c * 32 + e] * (__uint_as_float(v[c][e]) - dot) : 0.f;
                         }
-                        rests[q][w * 32 + lane] = rest;
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(&rest_full);
-                        ok = warp_wait(&rest_full, alone++ & 1u, &abort_flag);
-                        if (!ok) break;
-                        if (base != INFINITY) dot += rests[0][w * 32 + lane] + rests[1][w * 32 + lane];
+                        rest += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+                        if (j + 1 == x.n) {                  // all keys: the other warpgroup's columns as well
+                            rests[q][w * 32 + lane] = rest;
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&rest_full);
+                            ok = warp_wait(&rest_full, corrected++ & 1u, &abort_flag);
+                            if (!ok) break;
+                            if (base != INFINITY) dot += rests[0][w * 32 + lane] + rests[1][w * 32 + lane];
+                            __syncwarp();                    // the loads of tensor memory are for a converged warp
+                        }
+                        if (j < first) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(&ds_full);
+                            continue;
+                        }
                     }
                     {
                         uint32_t v[2][32];
