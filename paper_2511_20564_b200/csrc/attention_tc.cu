@@ -236,7 +236,7 @@ __device__ inline void let_land(uint64_t *bars, uint32_t stages, uint32_t issued
 template <typename R> __device__ inline void let_land_both(uint64_t *bars, uint32_t g)
 {
     int never = 0;
-    for (uint32_t j = g > R::kSlots ? g - R::kSlots : 0; j < g; ++j) mbar_wait(&bars[R::full(j)], R::parity(j), &never);
+    for (uint32_t j = g > R::kSlots ? g - R::kSlots : 0; j < g; ++j) mbar_wait(&bars[R::full(j & 1u, j >> 1)], R::parity(j >> 1), &never);
 }
 
 // Products of one tile, K step by K step, with descriptors that move on by constants: the instruction stream of the one issuing lane
@@ -356,8 +356,8 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                             if (!ok) break;
                             if (lane == 0) {
                                 if (v == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
-                                mbar_expect_tx(&kv_full[R::full(g)], kTileBytes);
-                                load_tile<NB>(kv_smem + s * kTileBytes, v ? &map_v : &map_k, x.h, x.kb + (int64_t)j * kTile, &kv_full[R::full(g)]);
+                                mbar_expect_tx(&kv_full[R::full(v, jj)], kTileBytes);
+                                load_tile<NB>(kv_smem + s * kTileBytes, v ? &map_v : &map_k, x.h, x.kb + (int64_t)j * kTile, &kv_full[R::full(v, jj)]);
                             }
                         }
                     }
@@ -376,7 +376,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const Work x = work_of(a, f, u, false);
                 for (int64_t t = x.t0; t * kRows < x.rows && x.n > 0 && ok; t += f.tiles)
                     for (int j = 0; j < x.n && ok; ++j, ++jj, g += 2) {
-                        ok = warp_wait(&kv_full[R::full(g)], R::parity(g), &abort_flag);
+                        ok = warp_wait(&kv_full[R::full(1, jj)], R::parity(jj), &abort_flag);
                         if (!ok) break;
                         const uint4 w4 = *reinterpret_cast<const uint4 *>(words[jj % kWordRing]);
                         const uint32_t word[4] = {w4.x, w4.y, w4.z, w4.w};
@@ -401,7 +401,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     for (int64_t t = x.t0; t * kRows < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                         const int nt = NT == 2 && x.rows - t * kRows > kTile ? 2 : 1;
                         ok = tile_ready(&q_full, item & 1u, &abort_flag);
-                        if (ok) ok = tile_ready(&kv_full[R::full(g)], R::parity(g), &abort_flag);
+                        if (ok) ok = tile_ready(&kv_full[R::full(0, jj)], R::parity(jj), &abort_flag);
 #pragma unroll
                         for (int q = 0; q < NT; ++q)
                             if (q < nt && ok) {
@@ -415,7 +415,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         for (int j = 0; j < x.n && ok; ++j, ++jj, g += 2) {
                             const uint32_t gv = g + 1, gk = g + 2;
                             const uint64_t v_desc = make_smem_desc_mn(kv_smem + R::slot(gv) * kTileBytes, kBlockBytes);
-                            ok = tile_ready(&kv_full[R::full(gv)], R::parity(gv), &abort_flag);
+                            ok = tile_ready(&kv_full[R::full(1, jj)], R::parity(jj), &abort_flag);
                             if (ok) ok = tile_ready(&v_clean[jj % kWordRing], (jj / kWordRing) & 1u, &abort_flag);
 #pragma unroll
                             for (int q = 0; q < NT; ++q) {
@@ -432,7 +432,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                                 if (!ok) continue;
                                 if (j + 1 < x.n) {
                                     if (q == nt - 1) umma_commit(&kv_empty[R::slot(gv)]);
-                                    if (q == 0) ok = tile_ready(&kv_full[R::full(gk)], R::parity(gk), &abort_flag);
+                                    if (q == 0) ok = tile_ready(&kv_full[R::full(0, jj + 1)], R::parity(jj + 1), &abort_flag);
                                     if (!ok) continue;
                                     scores(gk, q);
                                     if (q == nt - 1) umma_commit(&kv_empty[R::slot(gk)]);
@@ -749,8 +749,8 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                             if (!ok) break;
                             if (lane == 0) {
                                 if (v == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
-                                mbar_expect_tx(&kv_full[R::full(g)], kTileBytes);
-                                load_tile<NB>(kv_smem + s * kTileBytes, v ? &map_v : &map_k, x.h, x.kb + (int64_t)tile * kTile, &kv_full[R::full(g)]);
+                                mbar_expect_tx(&kv_full[R::full(v, jj)], kTileBytes);
+                                load_tile<NB>(kv_smem + s * kTileBytes, v ? &map_v : &map_k, x.h, x.kb + (int64_t)tile * kTile, &kv_full[R::full(v, jj)]);
                             }
                         }
                         tile = next;
@@ -771,7 +771,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 const int steps = x.n * passes_of(x, a.head_dim);
                 for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles)
                     for (int j = 0; j < steps && ok; ++j, ++jj, g += 2) {
-                        ok = warp_wait(&kv_full[R::full(g)], R::parity(g), &abort_flag);
+                        ok = warp_wait(&kv_full[R::full(0, jj)], R::parity(jj), &abort_flag);
                         if (!ok) break;
                         const uint4 w4 = *reinterpret_cast<const uint4 *>(words[jj % kWordRing]);
                         const uint32_t word[4] = {w4.x, w4.y, w4.z, w4.w};
@@ -791,8 +791,8 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 auto product = [&](uint32_t d, uint64_t a_desc, uint32_t slot) {
                     head_steps<NB>(d, a_desc, make_smem_desc(kv_smem + R::slot(slot) * kTileBytes), id_s, ksteps);
                 };
-                auto full = [&](uint32_t slot) {
-                    ok = ok && tile_ready(&kv_full[R::full(slot)], R::parity(slot), &abort_flag);
+                auto full = [&](uint32_t side, uint32_t tile) {
+                    ok = ok && tile_ready(&kv_full[R::full(side, tile)], R::parity(tile), &abort_flag);
                     return ok;
                 };
                 for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
@@ -801,16 +801,16 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                         ok = tile_ready(&q_full, item & 1u, &abort_flag);
                         if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
-                        if (!full(g)) break;
+                        if (!full(0, jj)) break;
                         product(tmem + (jj & 1u) * kTile, q_desc, g);
                         umma_commit(&s_full[jj & 1u]);
-                        if (!full(g + 1)) break;
+                        if (!full(1, jj)) break;
                         product(tmem + 256, g_desc, g + 1);
                         umma_commit(&dp_full);
                         umma_commit(&kv_empty[R::slot(g + 1)]);
                         for (int j = 0; j < steps; ++j, g += 2, ++jj) {
                             if (j + 1 < steps) {
-                                if (!full(g + 2)) break;
+                                if (!full(0, jj + 1)) break;
                                 product(tmem + ((jj + 1) & 1u) * kTile, q_desc, g + 2);
                                 umma_commit(&s_full[(jj + 1) & 1u]);
                             }
@@ -820,7 +820,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                             const uint64_t k_desc = make_smem_desc_mn(kv_smem + R::slot(g) * kTileBytes, kBlockBytes);
                             if (j >= first) row_steps(tmem + 384, tmem + 256, 32, k_desc, id_o, j > first);
                             if (j + 1 < steps) {
-                                if (!full(g + 3)) break;
+                                if (!full(1, jj + 1)) break;
                                 product(tmem + 256, g_desc, g + 3);
                                 umma_commit(&dp_full);
                                 umma_commit(&kv_empty[R::slot(g + 3)]);

@@ -8,9 +8,13 @@ template <int SLOTS> struct BySlot {
     static constexpr int kSlots = SLOTS;
     static uint32_t slot(uint32_t g) { return g % SLOTS; }
     static uint32_t use(uint32_t g) { return g / SLOTS; }
-    static uint32_t full(uint32_t g) { return slot(g); }
-    static uint32_t parity(uint32_t g) { return use(g) & 1u; }
+    static uint32_t full(uint32_t side, uint32_t tile) { return slot(2 * tile + side); }
+    static uint32_t parity(uint32_t) { return 0; }
 };
+// the barrier of copy g and the parity that is waited for
+template <typename R> uint32_t full(uint32_t g) { return R::full(g & 1u, g >> 1); }
+template <int S> uint32_t parity(TileRing<S>, uint32_t g) { return TileRing<S>::parity(g >> 1); }
+template <int S> uint32_t parity(BySlot<S>, uint32_t g) { return BySlot<S>::use(g) & 1u; }
 
 // `tiles` tiles through ring R, steps in random order.  Copies are started in order, each once its slot's last use was consumed, and land in
 // any order.  Products: a tile's side is consumed once it landed, side `side` only after the waiter of that side, too; side 1 of a tile after
@@ -29,18 +33,18 @@ template <typename R> int walk(int tiles, int side, unsigned seed)
         switch (rand() % 4) {
         case 0:                                          // start a copy
             if (next < 2 * tiles && consumed[R::slot(next)] == (int)R::use(next)) {
-                if (under_way[R::full(next)]++) return -3;
+                if (under_way[full<R>(next)]++) return -3;
                 in_flight[next++] = true, idle = 0;
             }
             break;
         case 1: {                                        // one of those on their way lands
             const int g = next - 1 - rand() % 16;
-            if (g >= 0 && in_flight[g]) in_flight[g] = false, done[g] = true, ++phases[R::full(g)], --under_way[R::full(g)], idle = 0;
+            if (g >= 0 && in_flight[g]) in_flight[g] = false, done[g] = true, ++phases[full<R>(g)], --under_way[full<R>(g)], idle = 0;
             break;
         }
         case 2: {                                        // the waiter of one side
             const uint32_t g = 2 * waiter + side;
-            if (waiter < tiles && (uint32_t)(phases[R::full(g)] & 1) != R::parity(g)) {
+            if (waiter < tiles && (uint32_t)(phases[full<R>(g)] & 1) != parity(R(), g)) {
                 if (!done[g]) return waiter;
                 ++waiter, idle = 0;
             }
@@ -82,9 +86,9 @@ def test_every_phase_of_a_barrier_is_one_side_in_turn(tmp_path):
 using R = TileRing<5>;
 int phases[R::kBarriers] = {}, uses[R::kSlots] = {};
 for (uint32_t g = 0; g < 1000; ++g) {
-    const uint32_t f = R::full(g);
+    const uint32_t f = R::full(g & 1u, g >> 1);
     if (f >= R::kBarriers || (g & 1u) != (f >= kWordRing)) return 1;           // a side's own barriers
-    if (R::parity(g) != (uint32_t)(phases[f]++ & 1)) return 2;
+    if (R::parity(g >> 1) != (uint32_t)(phases[f]++ & 1)) return 2;
     if (R::use(g) != (uint32_t)uses[R::slot(g)]++) return 3;
 }
 """, "tile_ring.h")
