@@ -497,8 +497,8 @@ int32_t e2egrec_qk_norm_rotary_backward(const e2egrec_mat *dQn, const e2egrec_ma
 
 /* Packed ragged sequences: sequence s owns rows q_ptr[s] .. q_ptr[s+1]-1 of the queries and k_ptr[s] .. k_ptr[s+1]-1 of the
  * keys and values.  q_ptr, k_ptr: device int64[n_seq+1], not decreasing, within the matrices' rows; lengths may be 0.
- * max_q, max_k: the longest of each, as far as the caller knows them (0: unknown); they size the launches, longer sequences are
- * still right, only slower.  k_mask: NULL or device uint8[rows of K], 0 = hidden from every query (padding, filtered entries). */
+ * max_q, max_k: the longest of each, as far as the caller knows them (0: unknown, the mean length decides); they choose the kernels and
+ * size the launches, longer sequences are still right, only slower.  k_mask: NULL or device uint8[rows of K], 0 = hidden from every query (padding, filtered entries). */
 typedef struct e2egrec_sequences {
     int64_t        n_seq;
     const int64_t *q_ptr, *k_ptr;
@@ -514,16 +514,20 @@ typedef struct e2egrec_sequences {
  * every sequence are left as they were.  Q, out: [rows x n_heads head_dim]; K, V: [rows x n_kv_heads head_dim] of one number of
  * rows; 0 < scale <= 1e38; at most 2^31 - 65536 rows each.
  *   lse     device float[Q rows x n_heads], row-major; may be NULL (serving: nothing is kept for a backward pass)
- *   status  optional device int32, receives E2EGREC_DEV_RANGE (or-ed) if offsets decrease or leave the matrices (the rows at fault
- *           are skipped) and E2EGREC_DEV_TIMEOUT if a wait inside a kernel ran out
+ *   status  optional device int32, receives E2EGREC_DEV_RANGE (or-ed) if offsets decrease or leave the matrices (such sequences are
+ *           cut to the matrices' rows; what the rows of them and of those they overlap get is not defined) and E2EGREC_DEV_TIMEOUT
+ *           if a wait inside a kernel ran out
  *   ws      scratch, 256-byte aligned (size query with ws == NULL; goes by the shapes, n_seq, max_q and max_k).  Nothing in it
  *           has to start at zero and nothing is kept in it; calls that may run at the same time need one each.
  * e2egrec_cross_attention_backward: gradients dQ, dK, dV for dOut, from the forward call's inputs, out and lse:
  *     dV_jg = sum_ih p_ij dOut_ih,  dS_ij = p_ij (dOut_ih . v_jg - dOut_ih . out_ih),  dQ_ih = scale sum_j dS_ij k_jg,
  *     dK_jg = scale sum_ih dS_ij q_ih   (i over the queries of s, h over the query heads of g).
  * Rows of hidden keys get zeros.  dOut, dQ have Q's shape, dK, dV that of K; none may overlap an input.  No floating-point atomics:
- * results are the same bits from run to run.  With bf16, p and dS are rounded to bf16 where the products run on the tensor cores
- * (dS of dQ to two such values).  Every matrix of both calls: heads as above. */
+ * results are the same bits from run to run.  A key that is the only visible one of its sequence gets exactly zero from dS (bf16 on
+ * the tensor cores: of up to 128 keys).  With bf16, p and dS are rounded to bf16 where the products run on the tensor cores (heads up to
+ * 128; dS of dQ to two such values), and dOut . out is formed from the stored out; what its rounding takes is made good in dQ (heads over 128
+ * and few rows: always where more than a handful of keys are seen; tensor cores: up to 128 keys, and over 32 head_dim), elsewhere it is about
+ * a rounding of the result.  Heads over 128 go through kernels for few rows, four at a time.  Every matrix of both calls: heads as above. */
 int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V, const e2egrec_sequences *seqs,
                                         int32_t n_heads, int32_t n_kv_heads, float scale, const e2egrec_mat *out, float *lse,
                                         int32_t *status, void *ws, size_t *ws_bytes, void *stream);

@@ -651,16 +651,17 @@ __device__ inline void store_row(uint32_t taddr, bf16 *out, int head_dim, float 
     }
 }
 
-// dQ, and D = dO . out of every row for the other kernel.  What the stored out's D lacks is the sum of p (dP - D) over the keys; it meets
-// sum p k in dQ, which does not get smaller with the number of keys, as dQ does.  Where one tile holds all keys it is added to D before dS is
-// formed: dS of a lone key is 0 then.  Over more than 32 head_dim keys it comes from a pass over them that forms p and dP alone (dQ of 26 000
-// keys and heads of 16: 9.6e-3 off without, 1.7e-3 so; 20 000 and 64: 5.3e-3, 1.6e-3; 8 x 512 x 16 384, four heads of 64, backward: 505 us,
-// 684 so); in between it is left out, about a rounding of the result for values whose mean is a quarter of their spread.  dS goes into its product as two bf16 operands, its rounding and the rest: D comes
-// from 16-bit outputs already, and with dS rounded as well dQ was 2.5 to 2.7e-3 off in the mean (a rounding of the result: 1.8e-3),
-// at most 2.4e-3 so, dK included; the training case's backward pass takes 550 us with one operand, 585 us so.
 // Passes over the keys
 __device__ inline int passes_of(const Work &x, int head_dim) { return (int64_t)x.n * kTile > 32 * head_dim ? 2 : 1; }
 
+// dQ, and D = dO . out of every row for the other kernel.  What the stored out's D lacks is the sum of p (dP - D) over the keys; it meets
+// sum p k in dQ, which does not get smaller with the number of keys, as dQ does.  Where one tile holds all keys it is added to D before dS is
+// formed: dS of a lone key is 0 then (2000 of 32 x 100, four heads of 64, backward: 610 -> 641 us).  Over more than 32 head_dim keys it comes
+// from a pass over them that forms p and dP alone (dQ of 26 000 keys and heads of 16: 9.6e-3 off without, 1.7e-3 so; 20 000 and 64:
+// 5.3e-3, 1.6e-3; 8 x 512 x 16 384, four heads of 64, backward: 505 -> 684 us).  In between it is left out, about a rounding of the result
+// for values whose mean is a quarter of their spread.
+// dS goes into its product as two bf16 operands, its rounding and the rest: with dS rounded once dQ was 2.5 to 2.7e-3 off in the mean (a
+// rounding of the result: 1.8e-3), at most 2.4e-3 so; the training case's backward pass takes 550 us with one operand, 585 us so.
 template <int NB>
 __global__ void __launch_bounds__(Bwd<NB>::kThreads, 1)
 attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_k,
