@@ -497,8 +497,9 @@ int32_t e2egrec_qk_norm_rotary_backward(const e2egrec_mat *dQn, const e2egrec_ma
 
 /* Packed ragged sequences: sequence s owns rows q_ptr[s] .. q_ptr[s+1]-1 of the queries and k_ptr[s] .. k_ptr[s+1]-1 of the
  * keys and values.  q_ptr, k_ptr: device int64[n_seq+1], not decreasing, within the matrices' rows; lengths may be 0.
- * max_q, max_k: the longest of each, as far as the caller knows them (0: unknown, the mean length decides); they choose the kernels and
- * size the launches, longer sequences are still right, only slower.  k_mask: NULL or device uint8[rows of K], 0 = hidden from every query (padding, filtered entries). */
+ * max_q, max_k: the longest of each, as far as the caller knows them (0: unknown, the mean length decides); they choose the
+ * kernels and size the launches, longer sequences are still right, only slower.  k_mask: NULL or device uint8[rows of K], 0 = hidden
+ * from every query (padding, filtered entries). */
 typedef struct e2egrec_sequences {
     int64_t        n_seq;
     const int64_t *q_ptr, *k_ptr;
