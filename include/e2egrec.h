@@ -526,9 +526,11 @@ typedef struct e2egrec_sequences {
  * Rows of hidden keys get zeros.  dOut, dQ have Q's shape, dK, dV that of K; none may overlap an input.  No floating-point atomics:
  * results are the same bits from run to run.  A key that is the only visible one of its sequence gets exactly zero from dS (bf16 on
  * the tensor cores: of up to 128 keys).  With bf16, p and dS are rounded to bf16 where the products run on the tensor cores (heads up to
- * 128; dS of dQ to two such values), and dOut . out is formed from the stored out; what its rounding takes is made good in dQ (heads over 128
- * and few rows: always where more than a handful of keys are seen; tensor cores: up to 128 keys, and over 32 head_dim), elsewhere it is about
- * a rounding of the result.  Heads over 128 go through kernels for few rows, four at a time.  Every matrix of both calls: heads as above. */
+ * 128; dS of dQ to two such values), and dOut . out is formed from the stored out.  What its rounding takes, up to 2^-8 of the sum of
+ * |dOut out|, meets scale sum_j p_ij k_jg in dQ.  It is made good where the streaming kernels run (few rows, heads over 128), on the tensor
+ * cores for sequences of up to 128 keys and of over 32 head_dim; in between it is about a rounding of dQ where keys are spread around zero, and
+ * some times that where they have more in common than they differ by.  Heads over 128 stream four rows at a time, which suits few rows.
+ * Every matrix of both calls: heads as above. */
 int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V, const e2egrec_sequences *seqs,
                                         int32_t n_heads, int32_t n_kv_heads, float scale, const e2egrec_mat *out, float *lse,
                                         int32_t *status, void *ws, size_t *ws_bytes, void *stream);
