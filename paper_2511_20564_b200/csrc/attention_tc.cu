@@ -658,7 +658,7 @@ __device__ inline int passes_of(const Work &x, int head_dim) { return (int64_t)x
 // sum p k in dQ, which does not get smaller with the number of keys, as dQ does.  Where one tile holds all keys it is added to D before dS is
 // formed: dS of a lone key is 0 then (2000 of 32 x 100, four heads of 64, backward: 610 -> 641 us).  Over more than 32 head_dim keys it comes
 // from a pass over them that forms p and dP alone (dQ of 26 000 keys and heads of 16: 9.6e-3 off without, 1.7e-3 so; 20 000 and 64:
-// 5.3e-3, 1.6e-3; 8 x 512 x 16 384, four heads of 64, backward: 505 -> 684 us).  In between it is left out, about a rounding of the result
+// 5.3e-3, 1.6e-3; 8 x 512 x 16 384, four heads of 64, backward: 505 -> 668 us).  In between it is left out, about a rounding of the result
 // for values whose mean is a quarter of their spread.
 // dS goes into its product as two bf16 operands, its rounding and the rest: with dS rounded once dQ was 2.5 to 2.7e-3 off in the mean (a
 // rounding of the result: 1.8e-3), at most 2.4e-3 so; the training case's backward pass takes 550 us with one operand, 585 us so.
@@ -898,14 +898,24 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                         tmem_load32_async(tmem + lanes + 256 + q * 64, v[0]);
                         tmem_load32_async(tmem + lanes + 256 + q * 64 + 32, v[1]);
                         tmem_load_wait();
-                        float sums[4] = {};
+                        float2 sums[2] = {};
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
                             const uint32_t word = words[jj % kWordRing][q * 2 + c];
+                            if (word != 0xFFFFFFFFu) {       // whatever hidden keys hold
 #pragma unroll
-                            for (int e = 0; e < 32; ++e) sums[e & 3] += (word >> e) & 1u ? p[c * 32 + e] * (__uint_as_float(v[c][e]) - dot) : 0.f;
+                                for (int e = 0; e < 32; ++e)
+                                    if (!((word >> e) & 1u)) {
+                                        p[c * 32 + e] = 0.f;
+                                        v[c][e] = 0u;
+                                    }
+                            }
+#pragma unroll
+                            for (int e = 0; e < 32; e += 2)
+                                sums[e / 2 & 1] = __ffma2_rn(make_float2(p[c * 32 + e], p[c * 32 + e + 1]),
+                                                             __fadd2_rn(pair_of(v[c][e], v[c][e + 1]), make_float2(-dot, -dot)), sums[e / 2 & 1]);
                         }
-                        rest += (sums[0] + sums[1]) + (sums[2] + sums[3]);
+                        rest += (sums[0].x + sums[0].y) + (sums[1].x + sums[1].y);
                         if (j + 1 == x.n) {                  // all keys: the other warpgroup's columns as well
                             rests[q][w * 32 + lane] = rest;
                             __syncwarp();
