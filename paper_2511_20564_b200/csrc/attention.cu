@@ -89,7 +89,7 @@ attn_join_kernel(const __grid_constant__ AttnArgs a, int splits, int warps, cons
 // (attention_few.cu).  One row of 4 x 24 000 keys, two heads of 128: 125 us with a thread going over all stretches, 60 us so.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads)
-attn_join_dq_kernel(const __grid_constant__ AttnArgs a, int splits, int wide, bool fit, const float *__restrict__ part)
+attn_join_dq_kernel(const __grid_constant__ AttnArgs a, int splits, int wide, bool fit, const float *__restrict__ part, float *__restrict__ dots)
 {
     __shared__ float4 sums[2][kRowThreads];
     __shared__ float rests[kRowThreads];
@@ -123,6 +123,7 @@ attn_join_dq_kernel(const __grid_constant__ AttnArgs a, int splits, int wide, bo
         m.x += w.x; m.y += w.y; m.z += w.z; m.w += w.w;
         r += rests[i * wide + at];
     }
+    if (fit && dots && at == 0) dots[cell] += r;
     T *out = static_cast<T *>(a.dq) + row * a.ldq2 + (cell - row * heads) * a.head_dim + at * 4;
     out[0] = from_float<T>(t.x - r * m.x);
     out[1] = from_float<T>(t.y - r * m.y);
@@ -233,14 +234,14 @@ int32_t check_shape(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_se
 
 }  // namespace
 
-void join_dq(const AttnArgs &a, int splits, int32_t dtype, bool fit, const float *part_dq, cudaStream_t st)
+void join_dq(const AttnArgs &a, int splits, int32_t dtype, bool fit, const float *part_dq, float *dots, cudaStream_t st)
 {
     note_launch();
     const unsigned grid = (unsigned)(a.q_rows * a.kv_heads * a.group);
     int wide = 1;
     while (wide * 4 < a.head_dim) wide *= 2;
-    if (dtype == E2EGREC_F32) attn_join_dq_kernel<float><<<grid, kRowThreads, 0, st>>>(a, splits, wide, fit, part_dq);
-    else attn_join_dq_kernel<__nv_bfloat16><<<grid, kRowThreads, 0, st>>>(a, splits, wide, fit, part_dq);
+    if (dtype == E2EGREC_F32) attn_join_dq_kernel<float><<<grid, kRowThreads, 0, st>>>(a, splits, wide, fit, part_dq, dots);
+    else attn_join_dq_kernel<__nv_bfloat16><<<grid, kRowThreads, 0, st>>>(a, splits, wide, fit, part_dq, dots);
 }
 
 }  // namespace e2egrec
@@ -335,7 +336,7 @@ extern "C" int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, con
         ok = tc_attention_backward(a, plan.q_tiles, plan.k_tiles, dots, st);
     } else if (plan.path == Path::simt) {
         ok = simt_attention_backward(a, plan.simt, part_dq, dots, st);
-        if (ok && plan.splits > 1 && a.q_rows) join_dq(a, plan.splits, Q->dtype, false, part_dq, st);
+        if (ok && plan.splits > 1 && a.q_rows) join_dq(a, plan.splits, Q->dtype, false, part_dq, nullptr, st);
     } else {
         ok = few_attention_backward(a, plan.few, Q->dtype, part_dq, dots, st);
     }

@@ -96,8 +96,8 @@ bool few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, f
 // part_dq: [splits x q_rows x heads x head_dim] where splits > 1, twice that and [splits x q_rows x heads] with fit; dots: [q_rows x heads] where !both
 bool few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st);
 
-// dQ of stretches of the keys -> dQ, in order
-void join_dq(const AttnArgs &a, int splits, int32_t dtype, bool fit, const float *part_dq, cudaStream_t st);
+// dQ of stretches of the keys -> dQ, in order; with fit what D lacks is added to dots (where there are any)
+void join_dq(const AttnArgs &a, int splits, int32_t dtype, bool fit, const float *part_dq, float *dots, cudaStream_t st);
 
 // attention_simt.cu: fp32, head_dim <= 128, tiles of 64 rows x 64 keys
 struct SimtPlan {

@@ -647,7 +647,8 @@ template <typename T, int U, int CPL> __device__ __noinline__ void clear_hidden(
 // dS of a lone key 0.
 // Over more keys (kFit) D comes from the stored outputs, and what 16-bit ones lack, sum_j dS_j (0 with the exact D), is taken out at the end:
 // dQ = sum_j dS_j k_j - (sum_j dS_j) (sum_j p_j k_j).  dQ of rows that see 12 000 keys was 3.4e-3 off without it, 1.8e-3 so (a rounding:
-// 1.7e-3).  Without kFit (a turn holds all keys, the caller said) longer sequences go over their keys twice (lacking).
+// 1.7e-3), and the sum goes to D for the kernel of dK and dV where that is another (dK of sharp softmaxes 5e-3 off, 2e-3 so).  Without kFit
+// (a turn holds all keys, the caller said) longer sequences go over their keys twice (lacking).
 template <typename T, int R, int U, int CPL, bool kBoth, bool kFit>
 __global__ void __launch_bounds__(kFewThreads, CPL == 2 || R > 2 ? 2 : (R == 1 ? 4 : 3))
 attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_dq, float *__restrict__ dots)
@@ -853,7 +854,8 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             if (wu == 0 && grp == 0 && live && x.on && r0 + r < x.rows) {
                 const int64_t row = out.row;
                 const int head = out.head(a, x);
-                if (!kBoth && x.z == 0 && at == 0) dots[row * heads + head] = d[r];
+                // (with stretches of the keys the join adds what D lacks)
+                if (!kBoth && x.z == 0 && at == 0) dots[row * heads + head] = kFit && !one_turn && f.splits == 1 ? d[r] + rest[r] : d[r];
                 if (f.splits == 1) {
                     if constexpr (kFit)
                         if (!one_turn) axpy<E>(dq[r], -rest[r], mean[r]);
@@ -1003,7 +1005,7 @@ template <typename T> bool backward_of(const AttnArgs &a, const FewPlan &p, FewS
     else if (p.rows == 2) ok = backward_rows<T, 2, true>(a, p, f, part_dq, dots, st);
     else ok = backward_rows<T, 4, true>(a, p, f, part_dq, dots, st);
     if (!ok) return false;
-    if (f.splits > 1 && a.q_rows) join_dq(a, f.splits, sizeof(T) == 4 ? E2EGREC_F32 : E2EGREC_BF16, p.fit, part_dq, st);
+    if (f.splits > 1 && a.q_rows) join_dq(a, f.splits, sizeof(T) == 4 ? E2EGREC_F32 : E2EGREC_BF16, p.fit, part_dq, p.both ? nullptr : dots, st);
     if (!p.both && a.k_rows) {
         note_launch();
         f.batches = (int)p.key_batches;
