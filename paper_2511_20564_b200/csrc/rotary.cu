@@ -11,8 +11,8 @@
 // for 65 536 rows of 4 heads of 64 bf16 values.)
 // Angles: a frequency becomes a 64-bit fraction of a turn, once per block and pair (1 / 2 pi and the product in two doubles: what one
 // product loses a far position multiplies, 2^-25 of a turn for 1 radian per position and 2^-15 for a thousand); its product with a 32-bit
-// position modulo one turn is two integer products, exact to 2^-32 of a turn wherever the position lies, where a product in 32-bit floating point has no digit
-// left beyond position 2^23.
+// position modulo one turn is two integer products, exact to 2^-32 of a turn wherever the position lies, where a product in 32-bit
+// floating point has no digit left beyond position 2^23.
 #include <algorithm>
 
 #include "common.cuh"
