@@ -539,6 +539,42 @@ int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, const e2egrec_
                                          int32_t n_kv_heads, float scale, const e2egrec_mat *dQ, const e2egrec_mat *dK,
                                          const e2egrec_mat *dV, int32_t *status, void *ws, size_t *ws_bytes, void *stream);
 
+/* What stands around the attention of a fusion layer (Sec. 4.3.2; Sec. 5.1 trains with dropout): dropout from a counter-based generator and
+ * layer norm of x, or of residual + dropout(x), with their gradients.
+ *
+ * Plan of a dropout: element (row, col) of a matrix is dropped where its 16 random bits lie below t = round(p 2^16) (at most 65535), else
+ * multiplied by 2^16 / (2^16 - t).  The bits are half col % 8 (of a word first the low one) of Philox4x32-10 with key (seed low, seed high) and
+ * counter (col / 8, row, 2^31 + place, step): a function of the plan and the element's place alone, the same for either dtype, any ld, stream
+ * and launch.  No mask is stored: the backward pass forms it again.  NaN and infinities that are dropped are 0.
+ *   p         0 <= p < 1
+ *   seed, place, step   place < 2^31 tells the dropouts of one step apart, step the steps
+ *   step_dev  NULL, or device uint32 that is added to step (mod 2^32): for callers that record a step once (a CUDA graph) and replay it
+ * e2egrec_dropout_apply: Y = dropout(X), or residual + dropout(X) (NULL for none).  The gradient with respect to X is the same call on dY
+ *   without a residual.  drop may be NULL (p = 0).  Y may be X or the residual.
+ * e2egrec_layer_norm_forward: z = residual + dropout(X) (residual, drop: NULL for none), Y = gain (z - m) s + shift with m the mean of a row of z
+ *   and s = 1 / sqrt(mean((z - m)^2) + eps).  gain, shift: device float[dim], 16-byte aligned, NULL for ones and zeros.  Z: NULL, or receives z (a
+ *   layer that norms its input carries the sum on).  stats: NULL, or device float[2 rows], 8-byte aligned, receives (m, s) of every row, all
+ *   that the backward call needs besides the inputs.  Y or Z may be X or the residual.  dim <= 8192, eps > 0.
+ * e2egrec_layer_norm_backward: with g = dY gain, n = (z - m) s:  dz = s (g - mean(g) - n mean(g n)) + dZ (the gradient that comes back along Z,
+ *   NULL for none);  dR = dz, the gradient with respect to the residual (NULL to skip: without dropout it equals dX);  dX = dropout(dz);
+ *   dgain = sum dY n, dshift = sum dY over the rows (device float[dim], overwritten; NULL to skip).  X, residual, drop, gain and stats as in the
+ *   forward call; z is formed again.  dX or dR may be dY or dZ, dX and dR are apart.  Sums run in a fixed order.  ws: scratch, 256-byte aligned
+ *   (size query with ws == NULL), nothing in it has to start at zero.
+ * Sums, means and s are fp32; results are rounded once. */
+typedef struct e2egrec_dropout {
+    double          p;
+    uint64_t        seed;
+    uint32_t        place, step;
+    const uint32_t *step_dev;
+} e2egrec_dropout;
+
+int32_t e2egrec_dropout_apply(const e2egrec_mat *X, const e2egrec_mat *residual, const e2egrec_dropout *drop, const e2egrec_mat *Y, void *stream);
+int32_t e2egrec_layer_norm_forward(const e2egrec_mat *X, const e2egrec_mat *residual, const e2egrec_dropout *drop, const float *gain,
+                                   const float *shift, float eps, const e2egrec_mat *Y, const e2egrec_mat *Z, float *stats, void *stream);
+int32_t e2egrec_layer_norm_backward(const e2egrec_mat *dY, const e2egrec_mat *dZ, const e2egrec_mat *X, const e2egrec_mat *residual,
+                                    const e2egrec_dropout *drop, const float *gain, const float *stats, const e2egrec_mat *dX,
+                                    const e2egrec_mat *dR, float *dgain, float *dshift, void *ws, size_t *ws_bytes, void *stream);
+
 /* e2egrec_aggregate_forward without a workspace argument (the paper has no counterpart; this is a
  * packaging variant of the call above: it enqueues the same kernels with the same launch shapes, so its
  * output equals that call's bit for bit).

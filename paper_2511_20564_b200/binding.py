@@ -46,6 +46,10 @@ class SequencesStruct(C.Structure):
                 ("k_mask", C.c_void_p)]
 
 
+class DropoutStruct(C.Structure):
+    _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("place", C.c_uint32), ("step", C.c_uint32), ("step_dev", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -154,12 +158,15 @@ def lib():
             fn.argtypes = [C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(Mat),
                            C.POINTER(Mat), C.c_void_p, C.POINTER(C.c_size_t), C.c_void_p]
         P, M, i32, f32 = C.c_void_p, C.POINTER(Mat), C.c_int32, C.c_float
-        sizes, seqs = C.POINTER(C.c_size_t), C.POINTER(SequencesStruct)
+        sizes, seqs, drop = C.POINTER(C.c_size_t), C.POINTER(SequencesStruct), C.POINTER(DropoutStruct)
         for name, args in (
                 ("e2egrec_rotary_frequencies", [i32] + [C.c_double] * 5 + [P, P]),
                 ("e2egrec_rotary", [M, i32, P, i32, P, f32, C.c_uint32, M, P]),
                 ("e2egrec_qk_norm_rotary_forward", [M, M, i32, i32, P, P, f32, P, i32, P, P, f32, C.c_uint32, M, M, P]),
                 ("e2egrec_qk_norm_rotary_backward", [M, M, M, M, i32, i32, P, P, f32, P, i32, P, P, f32, C.c_uint32, M, M, P, P, P, sizes, P]),
+                ("e2egrec_dropout_apply", [M, M, drop, M, P]),
+                ("e2egrec_layer_norm_forward", [M, M, drop, P, P, f32, M, M, P, P]),
+                ("e2egrec_layer_norm_backward", [M, M, M, M, drop, P, P, M, M, P, P, P, sizes, P]),
                 ("e2egrec_cross_attention_forward", [M, M, M, seqs, i32, i32, f32, M, P, P, P, sizes, P]),
                 ("e2egrec_cross_attention_backward", [M, M, M, M, M, P, seqs, i32, i32, f32, M, M, M, P, P, sizes, P])):
             fn = getattr(L, name)
@@ -1023,3 +1030,98 @@ def cross_attention_backward(dOut, Q, K, V, out, lse, seqs: Sequences, n_heads: 
 
     ws = _with_scratch(call, ws, Q.device, "e2egrec_cross_attention_backward")
     return dQ, dK, dV, ws
+
+
+# ------------------------------------------------------------------------------------------ dropout and layer norm
+
+class Dropout:
+    """Plan of a dropout (see e2egrec_dropout): the mask is a function of (seed, place, step) and an element's row and column, so the
+    forward and the backward call take the same plan.  step_dev: a device int32 or uint32 that is added to step, for captured steps."""
+
+    def __init__(self, p: float, seed: int, place=0, step=0, step_dev=None):
+        if not 0.0 <= p < 1.0 or not 0 <= int(place) < 1 << 31:
+            raise E2EGrecError(f"a rate of 0 or more and below 1 and a place below 2^31 are wanted, got {p}, {place}")
+        if step_dev is not None and (step_dev.dtype not in (torch.int32, torch.uint32) or step_dev.numel() != 1):
+            raise E2EGrecError(f"step_dev: one int32 or uint32 is wanted, got {tuple(step_dev.shape)} {step_dev.dtype}")
+        self.p, self.step_dev = p, step_dev
+        self.c = DropoutStruct(p, int(seed) & 0xFFFFFFFFFFFFFFFF, int(place), int(step) & 0xFFFFFFFF, None if step_dev is None else step_dev.data_ptr())
+
+    def check(self, dev):
+        if self.step_dev is not None and self.step_dev.get_device() != dev:
+            raise E2EGrecError(f"step_dev belongs on device {dev}")
+        return C.byref(self.c)
+
+
+def _plan(drop, dev):
+    return None if drop is None else drop.check(dev)
+
+
+def _beside(t, dev, name):
+    return None if t is None else C.byref(_heads_mat(t, dev, name))
+
+
+def dropout(X: torch.Tensor, drop, residual=None, out=None, stream=None):
+    """Enqueues dropout(X), or residual + dropout(X) (see e2egrec_dropout_apply), and returns the result; out may be X or the residual.
+    The gradient with respect to X is dropout of the result's gradient with the same plan."""
+    ctx = _elsewhere(X, stream)
+    if ctx is not None:
+        with ctx:
+            return dropout(X, drop, residual, out)
+    dev = X.get_device()
+    x = _heads_mat(X, dev, "X")
+    if out is None:
+        out = _packed_like(X)
+    _check(lib().e2egrec_dropout_apply(C.byref(x), _beside(residual, dev, "residual"), _plan(drop, dev), C.byref(_heads_mat(out, dev, "out")),
+                                       _raw_stream(dev)), "e2egrec_dropout_apply")
+    return out
+
+
+def layer_norm_forward(X: torch.Tensor, gain=None, shift=None, residual=None, drop=None, eps=1e-5, keep_sum=False, keep_stats=True, Y=None, Z=None,
+                       stats=None, stream=None):
+    """Enqueues the layer norm of z = residual + dropout(X) (see e2egrec_layer_norm_forward); returns (Y, Z, stats).  keep_sum: z is
+    stored (Z, else None).  keep_stats=False: nothing is kept for a backward pass."""
+    ctx = _elsewhere(X, stream)
+    if ctx is not None:
+        with ctx:
+            return layer_norm_forward(X, gain, shift, residual, drop, eps, keep_sum, keep_stats, Y, Z, stats)
+    dev = X.get_device()
+    x = _heads_mat(X, dev, "X")
+    if Y is None:
+        Y = _packed_like(X)
+    if Z is None and keep_sum:
+        Z = _packed_like(X)
+    if stats is None and keep_stats:
+        stats = X.new_empty((x.rows, 2), dtype=torch.float32)
+    _check(lib().e2egrec_layer_norm_forward(
+        C.byref(x), _beside(residual, dev, "residual"), _plan(drop, dev), _vector(gain, dev, torch.float32, x.dim, "gain"),
+        _vector(shift, dev, torch.float32, x.dim, "shift"), eps, C.byref(_heads_mat(Y, dev, "Y")), _beside(Z, dev, "Z"),
+        _vector(stats, dev, torch.float32, 2 * x.rows, "stats"), _raw_stream(dev)), "e2egrec_layer_norm_forward")
+    return Y, Z, stats
+
+
+def layer_norm_backward(dY: torch.Tensor, X: torch.Tensor, stats, gain=None, residual=None, drop=None, dZ=None, dX=None, dR=None, gains=True, ws=None,
+                        stream=None):
+    """Enqueues the gradient of layer_norm_forward (see e2egrec_layer_norm_backward) from its inputs and stats; returns
+    (dX, dR, dgain, dshift, ws).  dZ: the gradient that comes back along Z.  dR is the gradient with respect to the residual: None where
+    there is none, dX itself where nothing was dropped.  gains=False skips dgain and dshift."""
+    ctx = _elsewhere(X, stream)
+    if ctx is not None:
+        with ctx:
+            return layer_norm_backward(dY, X, stats, gain, residual, drop, dZ, dX, dR, gains, ws)
+    dev = X.get_device()
+    x = _heads_mat(X, dev, "X")
+    if dX is None:
+        dX = _packed_like(X)
+    if dR is None and residual is not None and drop is not None:
+        dR = _packed_like(X)
+    dw = X.new_empty((2, x.dim), dtype=torch.float32) if gains else None
+    dgain, dshift = (None, None) if dw is None else dw.unbind()
+    args = (_beside(dY, dev, "dY"), _beside(dZ, dev, "dZ"), C.byref(x), _beside(residual, dev, "residual"), _plan(drop, dev),
+            _vector(gain, dev, torch.float32, x.dim, "gain"), _vector(stats, dev, torch.float32, 2 * x.rows, "stats"), _beside(dX, dev, "dX"),
+            _beside(dR, dev, "dR"), None if dgain is None else dgain.data_ptr(), None if dshift is None else dshift.data_ptr())
+
+    def call(ws_ptr, n):
+        return lib().e2egrec_layer_norm_backward(*args, ws_ptr, C.byref(n), _raw_stream(dev))
+
+    ws = _with_scratch(call, ws, X.device, "e2egrec_layer_norm_backward")
+    return dX, dX if dR is None and residual is not None else dR, dgain, dshift, ws
