@@ -539,6 +539,39 @@ int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, const e2egrec_
                                          int32_t n_kv_heads, float scale, const e2egrec_mat *dQ, const e2egrec_mat *dK,
                                          const e2egrec_mat *dV, int32_t *status, void *ws, size_t *ws_bytes, void *stream);
 
+/* The same attention with a learned bias per head and bucket of the distance between a query's and a key's position (the age of an entry of a
+ * user's history, places in a sequence):
+ *     score_ij = scale q_ih . k_jg + table[b(pos_k[j] - pos_q[i])][h],   b(d) = number of edges that are not above d.
+ *   n_buckets   1 .. 128; n_buckets * n_heads <= 65536
+ *   edges       device int32[n_buckets - 1], ascending, above -2^31 (unordered ones give buckets that are not defined, nothing worse)
+ *   table       device float[n_buckets x n_heads], row-major.  An entry of -1e30 and less hides its pairs: they get no weight (the value
+ *               is still multiplied by zero: rows that hold infinities or NaN are k_mask's to hide).  A query that sees no key so gets
+ *               out = 0 and lse = -inf.
+ *   pos_q, pos_k  device int32[rows of Q], [rows of K], any values (distances are cut to 32 bits), or NULL: a row's number in its sequence
+ * Everything else is as in the calls without a bias.  e2egrec_biased_attention_backward also writes dtable (device float[n_buckets x
+ * n_heads], overwritten; NULL to skip): dtable_bh = sum of dS_ijh over the pairs in bucket b, in a fixed order.  D = dOut . out is made good
+ * for the rounding of the stored out wherever it goes into dtable.  The size query of the backward call goes by n_buckets too.
+ * e2egrec_relative_edges: edges of the usual buckets, written to host memory: on the side of the past (distances <= 0) bucket numbers are
+ *   distances up to buckets / 2, from there on they go evenly by the logarithm up to `far`, all beyond that in one; with `both` != 0 the same
+ *   widths from distance 1 on the other side.  edges: host int32[buckets - 1], or [2 buckets - 2] with both; n_buckets is one more.
+ *   1 <= far <= 2^30. */
+typedef struct e2egrec_relative_bias {
+    int32_t        n_buckets;
+    const int32_t *edges;
+    const float   *table;
+    const int32_t *pos_q, *pos_k;
+} e2egrec_relative_bias;
+
+int32_t e2egrec_relative_edges(int32_t buckets, int64_t far, int32_t both, int32_t *edges);
+int32_t e2egrec_biased_attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V, const e2egrec_sequences *seqs,
+                                         const e2egrec_relative_bias *bias, int32_t n_heads, int32_t n_kv_heads, float scale,
+                                         const e2egrec_mat *out, float *lse, int32_t *status, void *ws, size_t *ws_bytes, void *stream);
+int32_t e2egrec_biased_attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V,
+                                          const e2egrec_mat *out, const float *lse, const e2egrec_sequences *seqs,
+                                          const e2egrec_relative_bias *bias, int32_t n_heads, int32_t n_kv_heads, float scale,
+                                          const e2egrec_mat *dQ, const e2egrec_mat *dK, const e2egrec_mat *dV, float *dtable, int32_t *status,
+                                          void *ws, size_t *ws_bytes, void *stream);
+
 /* What stands around the attention of a fusion layer (Sec. 4.3.2; Sec. 5.1 trains with dropout): dropout from a counter-based generator and
  * layer norm of x, or of residual + dropout(x), with their gradients.
  *

@@ -9,5 +9,6 @@ from .binding import (  # noqa: F401
     BF16, F32, Blocks, JointStep, E2EGrecError, launch_count, lib, profile_tap, sample_join, sample_khop, blocks_transpose, sample_khop_workspace, sampler_scratch_init, sampler_set_step,
     sage_backward, sage_backward_multi, sage_ctx_views, sage_forward, status_string, ssl_loss, gradient_norm, gradient_norms, gradnorm_update, gate_fusion_forward, gate_fusion_backward,
     rotary, rotary_frequencies, qk_norm_rotary_forward, qk_norm_rotary_backward, Sequences, cross_attention_forward, cross_attention_backward,
+    RelativeBias, relative_edges, biased_attention_forward, biased_attention_backward,
     Dropout, dropout, layer_norm_forward, layer_norm_backward,
 )

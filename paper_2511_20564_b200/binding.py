@@ -50,6 +50,10 @@ class DropoutStruct(C.Structure):
     _fields_ = [("p", C.c_double), ("seed", C.c_uint64), ("place", C.c_uint32), ("step", C.c_uint32), ("step_dev", C.c_void_p)]
 
 
+class RelativeBiasStruct(C.Structure):
+    _fields_ = [("n_buckets", C.c_int32), ("edges", C.c_void_p), ("table", C.c_void_p), ("pos_q", C.c_void_p), ("pos_k", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -158,12 +162,15 @@ def lib():
             fn.argtypes = [C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(Mat),
                            C.POINTER(Mat), C.c_void_p, C.POINTER(C.c_size_t), C.c_void_p]
         P, M, i32, f32 = C.c_void_p, C.POINTER(Mat), C.c_int32, C.c_float
-        sizes, seqs, drop = C.POINTER(C.c_size_t), C.POINTER(SequencesStruct), C.POINTER(DropoutStruct)
+        sizes, seqs, drop, bias = C.POINTER(C.c_size_t), C.POINTER(SequencesStruct), C.POINTER(DropoutStruct), C.POINTER(RelativeBiasStruct)
         for name, args in (
                 ("e2egrec_rotary_frequencies", [i32] + [C.c_double] * 5 + [P, P]),
                 ("e2egrec_rotary", [M, i32, P, i32, P, f32, C.c_uint32, M, P]),
                 ("e2egrec_qk_norm_rotary_forward", [M, M, i32, i32, P, P, f32, P, i32, P, P, f32, C.c_uint32, M, M, P]),
                 ("e2egrec_qk_norm_rotary_backward", [M, M, M, M, i32, i32, P, P, f32, P, i32, P, P, f32, C.c_uint32, M, M, P, P, P, sizes, P]),
+                ("e2egrec_relative_edges", [i32, C.c_int64, i32, P]),
+                ("e2egrec_biased_attention_forward", [M, M, M, seqs, bias, i32, i32, f32, M, P, P, P, sizes, P]),
+                ("e2egrec_biased_attention_backward", [M, M, M, M, M, P, seqs, bias, i32, i32, f32, M, M, M, P, P, P, sizes, P]),
                 ("e2egrec_dropout_apply", [M, M, drop, M, P]),
                 ("e2egrec_layer_norm_forward", [M, M, drop, P, P, f32, M, M, P, P]),
                 ("e2egrec_layer_norm_backward", [M, M, M, M, drop, P, P, M, M, P, P, P, sizes, P]),
@@ -1030,6 +1037,88 @@ def cross_attention_backward(dOut, Q, K, V, out, lse, seqs: Sequences, n_heads: 
 
     ws = _with_scratch(call, ws, Q.device, "e2egrec_cross_attention_backward")
     return dQ, dK, dV, ws
+
+
+def relative_edges(buckets: int, far: int, both=False, device="cuda"):
+    """Edges (int32, ascending) of the usual buckets of distances (see e2egrec_relative_edges); RelativeBias takes one bucket more."""
+    buckets = int(buckets)
+    edges = torch.zeros(max(2 * buckets - 2 if both else buckets - 1, 0), dtype=torch.int32)
+    _check(lib().e2egrec_relative_edges(buckets, int(far), int(bool(both)), edges.data_ptr()), "e2egrec_relative_edges")
+    return edges.to(device)
+
+
+class RelativeBias:
+    """Bias of scores by head and bucket of the distance pos_k - pos_q (see e2egrec_relative_bias): table float32 [n_buckets x n_heads], edges
+    int32 [n_buckets - 1], ascending, positions int32 per row of Q and of K (None: a row's number in its sequence)."""
+
+    def __init__(self, table: torch.Tensor, edges: torch.Tensor, pos_q=None, pos_k=None):
+        if table.dim() != 2 or table.dtype != torch.float32 or not table.is_contiguous() or edges.dtype != torch.int32 or not edges.is_contiguous() or \
+                edges.numel() + 1 != table.shape[0]:
+            raise E2EGrecError(f"a contiguous float32 table [n_buckets x n_heads] and n_buckets - 1 contiguous int32 edges are wanted, got "
+                               f"{tuple(table.shape)} {table.dtype} and {tuple(edges.shape)} {edges.dtype}")
+        self.table, self.edges, self.pos_q, self.pos_k = table, edges, pos_q, pos_k
+        address = lambda t: None if t is None else t.data_ptr()
+        self.c = RelativeBiasStruct(table.shape[0], address(edges), address(table), address(pos_q), address(pos_k))
+
+    def check(self, dev, n_heads, q_rows, k_rows):
+        if self.table.get_device() != dev or self.edges.get_device() != dev or self.table.shape[1] != n_heads:
+            raise E2EGrecError(f"the table of {n_heads} heads and its edges belong on device {dev}, got {tuple(self.table.shape)} on {self.table.device}")
+        _vector(self.pos_q, dev, torch.int32, q_rows, "pos_q")
+        _vector(self.pos_k, dev, torch.int32, k_rows, "pos_k")
+        return C.byref(self.c)
+
+
+def biased_attention_forward(Q, K, V, seqs: Sequences, bias: RelativeBias, n_heads: int, n_kv_heads: int, scale: float, out=None, lse=None,
+                             keep_lse=True, status=None, ws=None, stream=None):
+    """cross_attention_forward with a bias of the scores (see e2egrec_biased_attention_forward); returns (out, lse, ws)."""
+    ctx = _elsewhere(Q, stream)
+    if ctx is not None:
+        with ctx:
+            return biased_attention_forward(Q, K, V, seqs, bias, n_heads, n_kv_heads, scale, out, lse, keep_lse, status, ws)
+    dev, rows = Q.get_device(), Q.shape[0]
+    q, k, v = _heads_mat(Q, dev, "Q"), _heads_mat(K, dev, "K"), _heads_mat(V, dev, "V")
+    s, b = seqs.check(dev, K.shape[0]), bias.check(dev, n_heads, rows, K.shape[0])
+    out = _packed_like(Q) if out is None else out
+    if lse is None and keep_lse:
+        lse = Q.new_empty((rows, n_heads), dtype=torch.float32)
+    o = _heads_mat(out, dev, "out")
+    lp, sp = _vector(lse, dev, torch.float32, rows * n_heads, "lse"), _vector(status, dev, torch.int32, 1, "status")
+
+    def call(ws_ptr, n):
+        return lib().e2egrec_biased_attention_forward(C.byref(q), C.byref(k), C.byref(v), s, b, n_heads, n_kv_heads, scale, C.byref(o), lp, sp,
+                                                      ws_ptr, C.byref(n), _raw_stream(dev))
+
+    ws = _with_scratch(call, ws, Q.device, "e2egrec_biased_attention_forward")
+    return out, lse, ws
+
+
+def biased_attention_backward(dOut, Q, K, V, out, lse, seqs: Sequences, bias: RelativeBias, n_heads: int, n_kv_heads: int, scale: float, dQ=None,
+                              dK=None, dV=None, dtable=None, table_grad=True, status=None, ws=None, stream=None):
+    """Enqueues the gradient of biased_attention_forward (see e2egrec_biased_attention_backward); returns (dQ, dK, dV, dtable, ws).
+    table_grad=False skips dtable."""
+    ctx = _elsewhere(Q, stream)
+    if ctx is not None:
+        with ctx:
+            return biased_attention_backward(dOut, Q, K, V, out, lse, seqs, bias, n_heads, n_kv_heads, scale, dQ, dK, dV, dtable, table_grad,
+                                             status, ws)
+    dev = Q.get_device()
+    g, q, k, v, o = (_heads_mat(t, dev, n) for t, n in ((dOut, "dOut"), (Q, "Q"), (K, "K"), (V, "V"), (out, "out")))
+    s, b = seqs.check(dev, K.shape[0]), bias.check(dev, n_heads, Q.shape[0], K.shape[0])
+    dQ = _packed_like(Q) if dQ is None else dQ
+    dK = _packed_like(K) if dK is None else dK
+    dV = _packed_like(K) if dV is None else dV
+    if dtable is None and table_grad:
+        dtable = torch.empty_like(bias.table)
+    dq, dk, dv = _heads_mat(dQ, dev, "dQ"), _heads_mat(dK, dev, "dK"), _heads_mat(dV, dev, "dV")
+    lp, sp = _vector(lse, dev, torch.float32, Q.shape[0] * n_heads, "lse"), _vector(status, dev, torch.int32, 1, "status")
+    tp = _vector(dtable, dev, torch.float32, bias.table.numel(), "dtable")
+
+    def call(ws_ptr, n):
+        return lib().e2egrec_biased_attention_backward(C.byref(g), C.byref(q), C.byref(k), C.byref(v), C.byref(o), lp, s, b, n_heads, n_kv_heads,
+                                                       scale, C.byref(dq), C.byref(dk), C.byref(dv), tp, sp, ws_ptr, C.byref(n), _raw_stream(dev))
+
+    ws = _with_scratch(call, ws, Q.device, "e2egrec_biased_attention_backward")
+    return dQ, dK, dV, dtable, ws
 
 
 # ------------------------------------------------------------------------------------------ dropout and layer norm

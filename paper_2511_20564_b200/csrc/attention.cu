@@ -1,8 +1,10 @@
 // Attention of ragged sequences of tokens to ragged sequences of states: argument checks, the choice of kernels, and the join of
 // results that were formed over stretches of the keys.
 #include <algorithm>
+#include <cmath>
 
 #include "attention.cuh"
+#include "gemm_simt.cuh"
 
 namespace e2egrec {
 namespace {
@@ -143,6 +145,7 @@ int32_t check_heads(const e2egrec_mat *m, int32_t heads, int32_t head_dim, int32
     return E2EGREC_OK;
 }
 
+constexpr int64_t kMaxTable = 1 << 16;         // entries of a table of biases
 constexpr int64_t kMaxUnits = ((int64_t)1 << 31) - 1;
 constexpr int64_t kMaxRows = ((int64_t)1 << 31) - (1 << 16);      // the kernels step some hundred rows beyond a sequence's end in 32 bits
 
@@ -155,10 +158,13 @@ struct Plan {
     Path path;
     FewPlan few;
     SimtPlan simt;
+    TablePlan table;
     bool one_tile;                        // tensor cores: a key head's rows fit one tile
     int64_t q_tiles, k_tiles;             // blocks of rows / tiles of keys per sequence and key head
     int splits;                           // stretches of the keys
     size_t part_bytes, ml_bytes, dot_bytes;
+    int64_t table_rows;                   // backward with a bias: rows of partial gradients of the table
+    size_t table_bytes;
 };
 
 Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, bool backward)
@@ -176,7 +182,7 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     const size_t cells = (size_t)a.q_rows * a.kv_heads * a.group;
     const bool small = rows <= (backward ? 4 : dtype == E2EGREC_F32 ? 3 : 2) || rows * k.typical <= (dtype == E2EGREC_F32 ? 256 : backward ? 700 : 800);
     // (without rows on one side there is nothing to form a product of)
-    p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
+    p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows || a.bias.buckets ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
     if (p.path == Path::tc) {
         p.one_tile = rows <= 128;
         p.q_tiles = blocks_per_unit(q, a.group, backward || p.one_tile ? 128 : 256, units);
@@ -196,6 +202,11 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
         const bool fit = backward && p.path == Path::few && p.few.fit;
         p.part_bytes = align_up(p.splits * cells * (fit ? 2 * a.head_dim + 1 : a.head_dim) * sizeof(float), 256);
         if (!backward) p.ml_bytes = align_up(p.splits * cells * sizeof(float2), 256);
+    }
+    if (backward && a.bias.buckets) {
+        p.table = few_table_plan(a, dtype);
+        p.table_rows = p.table.seq_slices * p.table.row_slices;
+        p.table_bytes = align_up((size_t)p.table_rows * a.bias.buckets * a.kv_heads * a.group * sizeof(float), 256);
     }
     return p;
 }
@@ -232,6 +243,32 @@ int32_t check_shape(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_se
     return E2EGREC_OK;
 }
 
+// A bias, or none
+int32_t check_bias(const e2egrec_relative_bias *b, AttnArgs &a)
+{
+    if (!b) return E2EGREC_OK;
+    if (b->n_buckets < 1) return E2EGREC_ERR_ARG;
+    if (b->n_buckets > kMaxBuckets || (int64_t)b->n_buckets * a.kv_heads * a.group > kMaxTable) return E2EGREC_ERR_UNSUPPORTED;
+    for (const void *p : {(const void *)b->table, (const void *)b->edges, (const void *)b->pos_q, (const void *)b->pos_k})
+        if (reinterpret_cast<uintptr_t>(p) % 4) return E2EGREC_ERR_ALIGN;
+    a.bias.table = b->table;
+    a.bias.edges = b->edges;
+    a.bias.pos_q = b->pos_q;
+    a.bias.pos_k = b->pos_k;
+    a.bias.buckets = b->n_buckets;
+    a.bias.top = 0;
+    for (int s = 1; s < b->n_buckets; s *= 2) a.bias.top = s;
+    return E2EGREC_OK;
+}
+// The same where work is enqueued: its pointers are there
+bool bias_missing(const e2egrec_relative_bias *b) { return b && (!b->table || (b->n_buckets > 1 && !b->edges)); }
+
+__global__ void zero_table_kernel(float *t, int n)
+{
+    const int i = blockIdx.x * blockDim.x + threadIdx.x;
+    if (i < n) t[i] = 0.f;
+}
+
 }  // namespace
 
 void join_dq(const AttnArgs &a, int splits, int32_t dtype, bool fit, const float *part_dq, float *dots, cudaStream_t st)
@@ -248,14 +285,14 @@ void join_dq(const AttnArgs &a, int splits, int32_t dtype, bool fit, const float
 
 using namespace e2egrec;
 
-extern "C" int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V,
-                                                   const e2egrec_sequences *seqs, int32_t n_heads, int32_t n_kv_heads, float scale,
-                                                   const e2egrec_mat *out, float *lse, int32_t *status, void *ws, size_t *ws_bytes,
-                                                   void *stream)
+static int32_t attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V, const e2egrec_sequences *seqs,
+                                 const e2egrec_relative_bias *bias, int32_t n_heads, int32_t n_kv_heads, float scale, const e2egrec_mat *out,
+                                 float *lse, int32_t *status, void *ws, size_t *ws_bytes, void *stream)
 {
     if (!ws_bytes) return E2EGREC_ERR_NULL;
     AttnArgs a{};
     int32_t rc = check_shape(Q, K, seqs, n_heads, n_kv_heads, scale, a);
+    if (rc == E2EGREC_OK) rc = check_bias(bias, a);
     if (rc != E2EGREC_OK) return rc;
     const Plan plan = make_plan(a, *seqs, Q->dtype, false);
     const size_t need = 256 + plan.part_bytes + plan.ml_bytes;
@@ -267,7 +304,7 @@ extern "C" int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e
     if (rc == E2EGREC_OK) rc = check_heads(V, n_kv_heads, a.head_dim, Q->dtype, a.k_rows);
     if (rc == E2EGREC_OK) rc = check_heads(out, n_heads, a.head_dim, Q->dtype, a.q_rows);
     if (rc != E2EGREC_OK) return rc;
-    if (a.n_seq && (!a.q_ptr || !a.k_ptr)) return E2EGREC_ERR_NULL;
+    if ((a.n_seq && (!a.q_ptr || !a.k_ptr)) || bias_missing(bias)) return E2EGREC_ERR_NULL;
     if (a.n_seq == 0 || a.q_rows == 0) return E2EGREC_OK;
     a.q = Q->data; a.ldq = Q->ld;
     a.k = K->data; a.ldk = K->ld;
@@ -282,7 +319,7 @@ extern "C" int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e
     if (plan.path == Path::tc) ok = tc_attention_forward(a, plan.q_tiles, plan.splits, plan.one_tile, part_o, part_ml, st);
     else if (plan.path == Path::simt) ok = simt_attention_forward(a, plan.simt, part_o, part_ml, st);
     else ok = few_attention_forward(a, plan.few, Q->dtype, part_o, part_ml, st);
-    if (!ok) return launch_refused("cross_attention_forward");
+    if (!ok) return launch_refused("attention_forward");
     if (plan.splits > 1) {
         note_launch();
         const int warps = plan.splits > 8 ? kRowThreads / 32 : 1;
@@ -290,21 +327,21 @@ extern "C" int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e
         if (Q->dtype == E2EGREC_F32) attn_join_kernel<float><<<grid, kRowThreads, 0, st>>>(a, plan.splits, warps, part_o, part_ml);
         else attn_join_kernel<__nv_bfloat16><<<grid, kRowThreads, 0, st>>>(a, plan.splits, warps, part_o, part_ml);
     }
-    return check_launch("cross_attention_forward");
+    return check_launch("attention_forward");
 }
 
-extern "C" int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q, const e2egrec_mat *K,
-                                                    const e2egrec_mat *V, const e2egrec_mat *out, const float *lse,
-                                                    const e2egrec_sequences *seqs, int32_t n_heads, int32_t n_kv_heads, float scale,
-                                                    const e2egrec_mat *dQ, const e2egrec_mat *dK, const e2egrec_mat *dV,
-                                                    int32_t *status, void *ws, size_t *ws_bytes, void *stream)
+static int32_t attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V,
+                                  const e2egrec_mat *out, const float *lse, const e2egrec_sequences *seqs, const e2egrec_relative_bias *bias,
+                                  int32_t n_heads, int32_t n_kv_heads, float scale, const e2egrec_mat *dQ, const e2egrec_mat *dK,
+                                  const e2egrec_mat *dV, float *dtable, int32_t *status, void *ws, size_t *ws_bytes, void *stream)
 {
     if (!ws_bytes) return E2EGREC_ERR_NULL;
     AttnArgs a{};
     int32_t rc = check_shape(Q, K, seqs, n_heads, n_kv_heads, scale, a);
+    if (rc == E2EGREC_OK) rc = check_bias(bias, a);
     if (rc != E2EGREC_OK) return rc;
     const Plan plan = make_plan(a, *seqs, Q->dtype, true);
-    const size_t need = 256 + plan.part_bytes + plan.dot_bytes;
+    const size_t need = 256 + plan.part_bytes + plan.dot_bytes + plan.table_bytes;
     if (!ws) { *ws_bytes = need; return E2EGREC_OK; }
     if (*ws_bytes < need) { *ws_bytes = need; return E2EGREC_ERR_WORKSPACE; }
     if (reinterpret_cast<uintptr_t>(ws) % 256) return E2EGREC_ERR_ALIGN;
@@ -316,9 +353,17 @@ extern "C" int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, con
         rc = check_heads(m, n_kv_heads, a.head_dim, Q->dtype, a.k_rows);
         if (rc != E2EGREC_OK) return rc;
     }
-    if (a.n_seq && (!a.q_ptr || !a.k_ptr)) return E2EGREC_ERR_NULL;
+    if ((a.n_seq && (!a.q_ptr || !a.k_ptr)) || bias_missing(bias)) return E2EGREC_ERR_NULL;
     if (a.q_rows && !lse) return E2EGREC_ERR_NULL;
-    if (a.n_seq == 0 || (a.q_rows == 0 && a.k_rows == 0)) return E2EGREC_OK;
+    if (reinterpret_cast<uintptr_t>(dtable) % 4) return E2EGREC_ERR_ALIGN;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const int table_size = a.bias.buckets * n_heads;
+    if (dtable && (a.n_seq == 0 || a.q_rows == 0)) {
+        note_launch();
+        zero_table_kernel<<<(unsigned)ceil_div(table_size, 256), 256, 0, st>>>(dtable, table_size);
+        dtable = nullptr;
+    }
+    if (a.n_seq == 0 || (a.q_rows == 0 && a.k_rows == 0)) return check_launch("attention_backward");
     a.q = Q->data; a.ldq = Q->ld;
     a.k = K->data; a.ldk = K->ld;
     a.v = V->data; a.ldv = V->ld;
@@ -329,7 +374,7 @@ extern "C" int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, con
     a.dv = dV->data; a.ldv2 = dV->ld;
     a.lse = const_cast<float *>(lse);
     a.status = status;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    float *table_part = reinterpret_cast<float *>(static_cast<char *>(ws) + plan.dot_bytes + plan.part_bytes);
     float *dots = static_cast<float *>(ws), *part_dq = reinterpret_cast<float *>(static_cast<char *>(ws) + plan.dot_bytes);
     bool ok = true;
     if (plan.path == Path::tc) {
@@ -340,6 +385,71 @@ extern "C" int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, con
     } else {
         ok = few_attention_backward(a, plan.few, Q->dtype, part_dq, dots, st);
     }
-    if (!ok) return launch_refused("cross_attention_backward");
-    return check_launch("cross_attention_backward");
+    if (ok && dtable) {
+        ok = few_attention_table(a, plan.table, Q->dtype, table_part, st);
+        if (ok) launch_colsum<float>(table_part, table_size, nullptr, nullptr, plan.table_rows, table_size, 0, dtable, st);
+    }
+    if (!ok) return launch_refused("attention_backward");
+    return check_launch("attention_backward");
+}
+
+extern "C" int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V,
+                                                   const e2egrec_sequences *seqs, int32_t n_heads, int32_t n_kv_heads, float scale,
+                                                   const e2egrec_mat *out, float *lse, int32_t *status, void *ws, size_t *ws_bytes,
+                                                   void *stream)
+{
+    return attention_forward(Q, K, V, seqs, nullptr, n_heads, n_kv_heads, scale, out, lse, status, ws, ws_bytes, stream);
+}
+
+extern "C" int32_t e2egrec_cross_attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q, const e2egrec_mat *K,
+                                                    const e2egrec_mat *V, const e2egrec_mat *out, const float *lse,
+                                                    const e2egrec_sequences *seqs, int32_t n_heads, int32_t n_kv_heads, float scale,
+                                                    const e2egrec_mat *dQ, const e2egrec_mat *dK, const e2egrec_mat *dV,
+                                                    int32_t *status, void *ws, size_t *ws_bytes, void *stream)
+{
+    return attention_backward(dOut, Q, K, V, out, lse, seqs, nullptr, n_heads, n_kv_heads, scale, dQ, dK, dV, nullptr, status, ws, ws_bytes,
+                              stream);
+}
+
+extern "C" int32_t e2egrec_biased_attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V,
+                                                    const e2egrec_sequences *seqs, const e2egrec_relative_bias *bias, int32_t n_heads,
+                                                    int32_t n_kv_heads, float scale, const e2egrec_mat *out, float *lse, int32_t *status,
+                                                    void *ws, size_t *ws_bytes, void *stream)
+{
+    if (!bias) return E2EGREC_ERR_NULL;
+    return attention_forward(Q, K, V, seqs, bias, n_heads, n_kv_heads, scale, out, lse, status, ws, ws_bytes, stream);
+}
+
+extern "C" int32_t e2egrec_biased_attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q, const e2egrec_mat *K,
+                                                     const e2egrec_mat *V, const e2egrec_mat *out, const float *lse,
+                                                     const e2egrec_sequences *seqs, const e2egrec_relative_bias *bias, int32_t n_heads,
+                                                     int32_t n_kv_heads, float scale, const e2egrec_mat *dQ, const e2egrec_mat *dK,
+                                                     const e2egrec_mat *dV, float *dtable, int32_t *status, void *ws, size_t *ws_bytes,
+                                                     void *stream)
+{
+    if (!bias) return E2EGREC_ERR_NULL;
+    return attention_backward(dOut, Q, K, V, out, lse, seqs, bias, n_heads, n_kv_heads, scale, dQ, dK, dV, dtable, status, ws, ws_bytes, stream);
+}
+
+// Smallest distances of the buckets 1 .. n - 1 of one side: their numbers up to n / 2, from there on half (far / half)^((i - half) / (n - half)),
+// rounded up, at least one apart.
+extern "C" int32_t e2egrec_relative_edges(int32_t buckets, int64_t far, int32_t both, int32_t *edges)
+{
+    if (buckets < 1 || far < 1 || far > (1 << 30)) return E2EGREC_ERR_ARG;
+    if ((both ? 2 * buckets - 1 : buckets) > kMaxBuckets) return E2EGREC_ERR_UNSUPPORTED;
+    if (!edges) return buckets == 1 ? E2EGREC_OK : E2EGREC_ERR_NULL;
+    const int half = std::max(buckets / 2, 1);
+    int64_t last = 0;
+    for (int i = 1; i < buckets; ++i) {
+        int64_t t = i;
+        if (i >= half) {
+            const double x = half * std::pow((double)std::max<int64_t>(far, half + 1) / half, (double)(i - half) / std::max(buckets - half, 1));
+            const double whole = std::nearbyint(x);
+            t = (int64_t)(std::fabs(x - whole) < 1e-9 * x ? whole : std::ceil(x));       // a whole number that pow missed by a rounding
+        }
+        last = std::max(t, last + 1);
+        edges[buckets - 1 - i] = (int32_t)(1 - last);
+        if (both) edges[buckets - 2 + i] = (int32_t)last;
+    }
+    return E2EGREC_OK;
 }

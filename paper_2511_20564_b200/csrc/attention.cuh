@@ -11,6 +11,18 @@ constexpr int kMaxAttnDim = 256;
 constexpr int kMaxSplits = 256;              // stretches of the keys, at most
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
+constexpr int kMaxBuckets = 128;
+constexpr float kHides = -1.0e30f;           // a bias of this and less hides the pair
+
+// Bias of a score by the bucket of the distance pos_k - pos_q: the number of edges that are not above it.
+struct BiasArgs {
+    const float *table;                   // [buckets x heads]
+    const int32_t *edges;                 // [buckets - 1], ascending
+    const int32_t *pos_q, *pos_k;         // null: a row's number in its sequence
+    float *dtable;                        // backward; may be null
+    int32_t buckets, top;                 // top: the largest power of two that is not above buckets - 1 (0: one bucket)
+};
+
 // Rows (query i, head g of its group) of one key head count as the rows of one matrix: row i * group + g.
 struct AttnArgs {
     const void *q, *k, *v, *o, *dout;     // o, dout: backward only
@@ -24,6 +36,7 @@ struct AttnArgs {
     int64_t n_seq, q_rows, k_rows;
     int32_t kv_heads, group, head_dim;
     float scale;
+    BiasArgs bias;                        // table null: none
 };
 
 struct SeqRange {
@@ -57,6 +70,28 @@ __device__ inline int64_t owner(const int64_t *ptr, int64_t n_seq, int64_t row)
     }
     return row < ptr[lo + 1] ? lo : -1;
 }
+
+// pos_k - pos_q, cut to 32 bits (no edge is the lowest number, so a bucket is not another for it)
+__device__ __forceinline__ int apart(int pos_k, int pos_q)
+{
+    int d;
+    asm("sub.sat.s32 %0, %1, %2;" : "=r"(d) : "r"(pos_k), "r"(pos_q));
+    return d;
+}
+// The bucket of a distance.  Steps by powers of two: 0 .. buckets - 1 whatever the edges hold.
+__device__ __forceinline__ int bucket_of(const BiasArgs &b, const int32_t *edges, int d)
+{
+    int at = 0;
+    for (int s = b.top; s; s >>= 1) {
+        const int m = at + s;
+        if (m < b.buckets && edges[m - 1] <= d) at = m;
+    }
+    return at;
+}
+// A bias in powers of two, as the scores are
+__device__ __forceinline__ float bias_value(float b) { return b <= kHides ? -INFINITY : b * kLog2e; }
+__device__ __forceinline__ float bias_at(const BiasArgs &b, int heads, int bucket, int head) { return bias_value(__ldg(b.table + bucket * heads + head)); }
+__device__ __forceinline__ int pos_of(const int32_t *pos, int64_t row, int64_t first) { return pos ? __ldg(pos + row) : (int)(row - first); }
 
 // Lengths that a call is planned by: the longest that a sequence can have (the caller's hint, else all rows), the mean, and the one that
 // the kernels are chosen for: the hint, without one the mean.
@@ -95,6 +130,13 @@ FewPlan few_plan(const AttnArgs &a, const Lengths &q, const Lengths &k, int es, 
 bool few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_o, float2 *part_ml, cudaStream_t st);
 // part_dq: [splits x q_rows x heads x head_dim] where splits > 1, twice that and [splits x q_rows x heads] with fit; dots: [q_rows x heads] where !both
 bool few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st);
+
+// Gradient of the table of biases: part [slices x buckets x heads], one row per slice of the sequences' rows, which the caller adds up
+struct TablePlan {
+    int64_t seq_slices, row_slices;       // slices of the sequences, and of each one's rows
+};
+TablePlan few_table_plan(const AttnArgs &a, int32_t dtype);
+bool few_attention_table(const AttnArgs &a, const TablePlan &p, int32_t dtype, float *part, cudaStream_t st);
 
 // dQ of stretches of the keys -> dQ, in order; with fit what D lacks is added to dots (where there are any)
 void join_dq(const AttnArgs &a, int splits, int32_t dtype, bool fit, const float *part_dq, float *dots, cudaStream_t st);

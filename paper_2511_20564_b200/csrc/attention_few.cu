@@ -267,6 +267,34 @@ __device__ inline Unit few_unit(const AttnArgs &a, const FewShape &f, uint32_t u
     return x;
 }
 
+// Biases of the scores of a turn: lane i finds the buckets of the turn's key i, which the lanes of that key then ask it for.  Positions of the
+// keys are fetched a turn ahead.
+template <int R> struct TurnBias {
+    int pos[R], col[R], buckets[R];                  // the rows' positions and heads
+    int next;
+    __device__ inline void row(const AttnArgs &a, const Unit &x, bool on, int r, int64_t row, int head)
+    {
+        pos[r] = on ? pos_of(a.bias.pos_q, row, x.rg.q0) : 0;
+        col[r] = on ? head : 0;
+    }
+    __device__ inline void fetch(const AttnArgs &a, const Unit &x, const Ring &ring, int t)
+    {
+        const int j = ring.first + t * ring.stride + ring.lane;
+        next = ring.lane < ring.keys && j < ring.n ? pos_of(a.bias.pos_k, x.kb + j, x.rg.k0) : 0;
+    }
+    __device__ inline void turn(const AttnArgs &a, const Unit &x, const Ring &ring, int t)
+    {
+        const int mine = next;
+        if (t + 1 < ring.turns) fetch(a, x, ring, t + 1);
+#pragma unroll
+        for (int r = 0; r < R; ++r) buckets[r] = bucket_of(a.bias, a.bias.edges, apart(mine, pos[r]));
+    }
+    __device__ inline float of(const AttnArgs &a, int r, int key) const
+    {
+        return bias_at(a.bias, a.kv_heads * a.group, __shfl_sync(0xFFFFFFFFu, buckets[r], key), col[r]);
+    }
+};
+
 // Rows of a unit one after the other: query row and head of (query, head of the group) pair r0, r0 + 1, ...
 struct RowWalk {
     int64_t row;
@@ -288,7 +316,7 @@ struct RowWalk {
 };
 
 // kb .. ke in turns of warps * kUnroll * (32 / lanes) keys
-template <typename T, int R, int U, int CPL>
+template <typename T, int R, int U, int CPL, bool kBias>
 __global__ void __launch_bounds__(kFewThreads, CPL == 2 ? 2 : (R > 2 ? 3 : 4))
 attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
 {
@@ -316,11 +344,15 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         if (f.warps == 1 ? !live : !__syncthreads_or((int)live)) break;      // barriers inside: all warps of the block go on, or none
         if (live) ring.start();
         float q[R][E], o[R][E], m[R], l[R];
+        TurnBias<R> bias;
+        if constexpr (kBias)
+            if (live) bias.fetch(a, x, ring, 0);
         RowWalk in(a, x, r0);
 #pragma unroll
         for (int r = 0; r < R; ++r, in.next(a)) {
             Piece<T, CPL> p;
             p.zero();
+            if constexpr (kBias) bias.row(a, x, live && x.on && r0 + r < x.rows, r, in.row, in.head(a, x));
             if (live && x.on && r0 + r < x.rows) p.load(static_cast<const T *>(a.q) + in.row * a.ldq + in.head(a, x) * (int64_t)a.head_dim, at, f.lanes, f.chunks);
             p.widen(q[r]);
 #pragma unroll
@@ -353,6 +385,11 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 for (int r = 0; r < R; ++r) s[r * U + u] = dot<E>(q[r], w);
             }
             key_sums<R * U>(s, f.lanes);
+            if constexpr (kBias) {
+                bias.turn(a, x, ring, t);
+#pragma unroll
+                for (int i = 0; i < R * U; ++i) s[i] += bias.of(a, i / U, i % U * kpw + grp);
+            }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float top = m[r];
@@ -456,7 +493,7 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 // dK and dV of kKeys keys per lane group (j0 and on), over all rows of the sequence.  dots: D of every row, or null where it is to be
 // formed from the stored outputs.
 constexpr int kKeys = 2;
-template <typename T, int CPL>
+template <typename T, int CPL, bool kBias>
 __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int h, bool on, int64_t j0, int64_t end, int grp, int at, const FewShape &f,
                                       const float *dots)
 {
@@ -466,10 +503,12 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
     const float c1 = a.scale * kLog2e;
     float k[kKeys][E], v[kKeys][E], dk[kKeys][E], dv[kKeys][E];
     bool seen[kKeys];
+    int pos[kKeys];
 #pragma unroll
     for (int n = 0; n < kKeys; ++n) {
         const int64_t j = j0 + n * kpw + grp;
         seen[n] = on && j < end && (!a.mask || a.mask[j]);
+        if constexpr (kBias) pos[n] = seen[n] ? pos_of(a.bias.pos_k, j, rg.k0) : 0;
         Piece<T, CPL> p, t;
         p.zero();
         t.zero();
@@ -516,9 +555,13 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
                 s[kKeys + n] = dot<E>(go, v[n]);
             }
             key_sums<2 * kKeys>(s, f.lanes);
+            int pos_q = 0;
+            if constexpr (kBias) pos_q = pos_of(a.bias.pos_q, row, rg.q0);
 #pragma unroll
             for (int n = 0; n < kKeys; ++n) {
-                const float pr = seen[n] && live ? exp2_fast(fmaf(s[n], c1, -l * kLog2e)) : 0.f;
+                float base = -l * kLog2e;
+                if constexpr (kBias) base += bias_at(a.bias, heads, bucket_of(a.bias, a.bias.edges, apart(pos[n], pos_q)), head);
+                const float pr = seen[n] && live ? exp2_fast(fmaf(s[n], c1, base)) : 0.f;
                 axpy<E>(dv[n], pr, go);
                 axpy<E>(dk[n], seen[n] && live ? pr * (s[kKeys + n] - d[0]) : 0.f, q);
             }
@@ -541,7 +584,7 @@ __device__ inline void keys_gradients(const AttnArgs &a, const SeqRange &rg, int
 template <int R> struct RowSums {
     float of[R];
 };
-template <typename T, int R, int CPL> __device__ __noinline__ RowSums<R> lacking(const AttnArgs &a, const FewShape &f, uint32_t unit, int64_t r0)
+template <typename T, int R, int CPL, bool kBias> __device__ __noinline__ RowSums<R> lacking(const AttnArgs &a, const FewShape &f, uint32_t unit, int64_t r0)
 {
     constexpr int E = Piece<T, CPL>::E;
     const int lane = threadIdx.x & 31, wide = f.lanes * f.heads, grp = lane / wide, at = lane & (f.lanes - 1), kpw = 32 / wide, heads = a.kv_heads * a.group;
@@ -549,6 +592,7 @@ template <typename T, int R, int CPL> __device__ __noinline__ RowSums<R> lacking
     const int64_t koff = x.h * (int64_t)a.head_dim;
     const float c1 = a.scale * kLog2e;
     float q[R][E], g[R][E], lse[R], d[R];
+    int pos[R], col[R];
     RowSums<R> sums;
     RowWalk in(a, x, r0);
 #pragma unroll
@@ -558,15 +602,20 @@ template <typename T, int R, int CPL> __device__ __noinline__ RowSums<R> lacking
         t.zero();
         o.zero();
         lse[r] = INFINITY;
+        pos[r] = col[r] = 0;
         if (x.on && r0 + r < x.rows) {
             const int head = in.head(a, x);
-            const int64_t col = (int64_t)head * a.head_dim;
+            const int64_t off = (int64_t)head * a.head_dim;
             const float v = a.lse[in.row * heads + head];
+            if constexpr (kBias) {
+                pos[r] = pos_of(a.bias.pos_q, in.row, x.rg.q0);
+                col[r] = head;
+            }
             if (v != -INFINITY) {
                 lse[r] = v * kLog2e;
-                p.load(static_cast<const T *>(a.q) + in.row * a.ldq + col, at, f.lanes, f.chunks);
-                t.load(static_cast<const T *>(a.dout) + in.row * a.ldg + col, at, f.lanes, f.chunks);
-                o.load(static_cast<const T *>(a.o) + in.row * a.ldo + col, at, f.lanes, f.chunks);
+                p.load(static_cast<const T *>(a.q) + in.row * a.ldq + off, at, f.lanes, f.chunks);
+                t.load(static_cast<const T *>(a.dout) + in.row * a.ldg + off, at, f.lanes, f.chunks);
+                o.load(static_cast<const T *>(a.o) + in.row * a.ldo + off, at, f.lanes, f.chunks);
             }
         }
         float y[E];
@@ -597,7 +646,12 @@ template <typename T, int R, int CPL> __device__ __noinline__ RowSums<R> lacking
         }
         key_sums<2 * R>(s, f.lanes);
 #pragma unroll
-        for (int r = 0; r < R; ++r) sums.of[r] += on ? exp2_fast(fmaf(s[r], c1, -lse[r])) * (s[R + r] - d[r]) : 0.f;
+        for (int r = 0; r < R; ++r) {
+            float base = -lse[r];
+            if constexpr (kBias)
+                if (on) base += bias_at(a.bias, heads, bucket_of(a.bias, a.bias.edges, apart(pos_of(a.bias.pos_k, j, x.rg.k0), pos[r])), col[r]);
+            sums.of[r] += on ? exp2_fast(fmaf(s[r], c1, base)) * (s[R + r] - d[r]) : 0.f;
+        }
     }
     for (int o = wide; o < 32; o <<= 1)
 #pragma unroll
@@ -649,7 +703,7 @@ template <typename T, int U, int CPL> __device__ __noinline__ void clear_hidden(
 // dQ = sum_j dS_j k_j - (sum_j dS_j) (sum_j p_j k_j).  dQ of rows that see 12 000 keys was 3.4e-3 off without it, 1.8e-3 so (a rounding:
 // 1.7e-3), and the sum goes to D for the kernel of dK and dV where that is another (dK of sharp softmaxes 5e-3 off, 2e-3 so).  Without kFit
 // (a turn holds all keys, the caller said) longer sequences go over their keys twice (lacking).
-template <typename T, int R, int U, int CPL, bool kBoth, bool kFit>
+template <typename T, int R, int U, int CPL, bool kBoth, bool kFit, bool kBias>
 __global__ void __launch_bounds__(kFewThreads, CPL == 2 || R > 2 ? 2 : (R == 1 ? 4 : 3))
 attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_dq, float *__restrict__ dots)
 {
@@ -682,9 +736,12 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         float q[R][E], g[R][E], dq[R][E], lse[R], d[R];
         float mean[kFit ? R : 1][E], rest[R];             // sum_j p_j k_j; what D lacked
         const bool one_turn = f.warps == 1 && f.splits == 1 && x.ke - x.kb <= U * kpw;
+        TurnBias<R> bias;
+        if constexpr (kBias)
+            if (live) bias.fetch(a, x, ring, 0);
         RowSums<R> lack = {};
         if constexpr (sizeof(T) == 2 && !kFit)
-            if (live && !one_turn) lack = lacking<T, R, CPL>(a, f, unit, r0);       // one warp per unit and one stretch: few_plan
+            if (live && !one_turn) lack = lacking<T, R, CPL, kBias>(a, f, unit, r0);       // one warp per unit and one stretch: few_plan
         RowWalk in(a, x, r0);
 #pragma unroll
         for (int r = 0; r < R; ++r, in.next(a)) {
@@ -693,6 +750,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             t.zero();
             lse[r] = INFINITY;
             d[r] = 0.f;
+            if constexpr (kBias) bias.row(a, x, live && x.on && r0 + r < x.rows, r, in.row, in.head(a, x));
             if (live && x.on && r0 + r < x.rows) {
                 const int64_t row = in.row;
                 const int head = in.head(a, x);
@@ -755,10 +813,15 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 }
             }
             key_sums<2 * R * U>(s, f.lanes);
+            if constexpr (kBias) bias.turn(a, x, ring, t);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
 #pragma unroll
-                for (int u = 0; u < U; ++u) s[r * U + u] = seen[u] ? exp2_fast(fmaf(s[r * U + u], c1, -lse[r])) : 0.f;
+                for (int u = 0; u < U; ++u) {
+                    float base = -lse[r];
+                    if constexpr (kBias) base += bias.of(a, r, u * kpw + grp);
+                    s[r * U + u] = seen[u] ? exp2_fast(fmaf(s[r * U + u], c1, base)) : 0.f;
+                }
                 if (one_turn) {
                     float sum = 0.f, t = 0.f;
 #pragma unroll
@@ -881,11 +944,11 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     if (kBoth && x.any && whole && a.mask) clear_hidden<T, U, CPL>(a, f, unit);
     if (kBoth && x.any && !whole)
         for (int64_t j0 = x.kb + (int64_t)wu * kKeys * kpw; j0 < x.ke; j0 += (int64_t)f.warps * kKeys * kpw)
-            keys_gradients<T, CPL>(a, x.rg, x.h, x.on, j0, x.ke, grp, at, f, nullptr);
+            keys_gradients<T, CPL, kBias>(a, x.rg, x.h, x.on, j0, x.ke, grp, at, f, nullptr);
 }
 
 // dK and dV where the rows of a sequence do not fit one unit
-template <typename T, int CPL>
+template <typename T, int CPL, bool kBias>
 __global__ void __launch_bounds__(kFewThreads)
 attn_few_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, const float *__restrict__ dots)
 {
@@ -899,7 +962,140 @@ attn_few_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     const SeqRange rg = seq_range(a, s, lane == 0 && hg == 0 && first == 0);
     const int64_t step = (int64_t)kKeys * (32 / wide);
     for (int64_t j0 = rg.k0 + first * step; j0 < rg.k1; j0 += f.batches * step)
-        keys_gradients<T, CPL>(a, rg, h, h < a.kv_heads, j0, rg.k1, lane / wide, lane & (f.lanes - 1), f, dots);
+        keys_gradients<T, CPL, kBias>(a, rg, h, h < a.kv_heads, j0, rg.k1, lane / wide, lane & (f.lanes - 1), f, dots);
+}
+
+// Gradient of the table of biases: dtable_bh = sum of dS over the pairs whose distance is in bucket b.  A warp takes every slices-th row of
+// a slice of the sequences, of its head group's key heads and one query head g of theirs.  Of a row it adds up, by bucket, a = sum p (dP - D)
+// with D from the stored out, and m = sum p; what D lacks, r = sum a / sum m over all buckets, is known at the row's end, and a - r m is the
+// row's part.  Lane groups (a key each) have bins of their own and keep the bucket that they are in in registers, so no two lanes meet.
+template <typename T, int CPL>
+__global__ void __launch_bounds__(kFewThreads)
+attn_few_table_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, int64_t seq_slices, int64_t row_slices, float *__restrict__ part)
+{
+    constexpr int E = Piece<T, CPL>::E, U = 4;
+    extern __shared__ float2 bins_smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wide = f.lanes * f.heads, grp = lane / wide, at = lane & (f.lanes - 1), kpw = 32 / wide;
+    const int heads = a.kv_heads * a.group, nb = a.bias.buckets, local = lane / f.lanes % f.heads;
+    uint32_t u = blockIdx.x * (uint32_t)kFewWarps + warp;
+    if (u >= f.units) return;
+    const int g = (int)(u % (uint32_t)a.group);
+    u /= (uint32_t)a.group;
+    const int hg = (int)(u % (uint32_t)f.head_groups);
+    u /= (uint32_t)f.head_groups;
+    const int64_t slice = u, s0 = slice / row_slices, r0 = slice % row_slices;
+    const int h = hg * f.heads + local, head = h * a.group + g;
+    const bool on = h < a.kv_heads;
+    const int64_t koff = h * (int64_t)a.head_dim, qoff = head * (int64_t)a.head_dim;
+    const float c1 = a.scale * kLog2e;
+    // bins of (bucket, key of a step, head): float2 (a, m); behind them the warp's sums of the rows, (bucket, head)
+    float2 *bins = bins_smem + (size_t)warp * nb * (32 / f.lanes);
+    float *sums = reinterpret_cast<float *>(bins_smem + (size_t)kFewWarps * nb * (32 / f.lanes)) + (size_t)warp * nb * f.heads;
+    for (int i = lane; i < nb * (32 / f.lanes); i += 32) bins[i] = make_float2(0.f, 0.f);
+    for (int i = lane; i < nb * f.heads; i += 32) sums[i] = 0.f;
+    __syncwarp();
+    float2 *mine = bins + lane / f.lanes;                // stride 32 / lanes
+    for (int64_t s = s0; s < a.n_seq; s += seq_slices) {
+        const SeqRange rg = seq_range(a, s, false);
+        for (int64_t row = rg.q0 + r0; row < rg.q1; row += row_slices) {
+            const float l = on ? a.lse[row * heads + head] : -INFINITY;
+            if (__all_sync(0xFFFFFFFFu, l == -INFINITY)) continue;
+            Piece<T, CPL> p, t, o;
+            p.zero();
+            t.zero();
+            o.zero();
+            if (l != -INFINITY) {
+                p.load(static_cast<const T *>(a.q) + row * a.ldq + qoff, at, f.lanes, f.chunks);
+                t.load(static_cast<const T *>(a.dout) + row * a.ldg + qoff, at, f.lanes, f.chunks);
+                o.load(static_cast<const T *>(a.o) + row * a.ldo + qoff, at, f.lanes, f.chunks);
+            }
+            float q[E], go[E], y[E], d[1];
+            p.widen(q);
+            t.widen(go);
+            o.widen(y);
+            d[0] = dot<E>(go, y);
+            key_sums<1>(d, f.lanes);
+            const int pos_q = pos_of(a.bias.pos_q, row, rg.q0);
+            const float lse = l == -INFINITY ? INFINITY : l * kLog2e;
+            float run_a = 0.f, run_m = 0.f, all_a = 0.f, all_m = 0.f;
+            int cur = -1;
+            for (int64_t j0 = rg.k0; j0 < rg.k1; j0 += U * kpw) {
+                float sc[2 * U];
+                int pos[U];
+                bool seen[U];
+#pragma unroll
+                for (int n = 0; n < U; ++n) {
+                    const int64_t j = j0 + n * kpw + grp;
+                    seen[n] = on && j < rg.k1 && (!a.mask || a.mask[j]);
+                    pos[n] = seen[n] ? pos_of(a.bias.pos_k, j, rg.k0) : 0;
+                    Piece<T, CPL> k, v;
+                    float w[E], x[E];
+                    k.zero();
+                    v.zero();
+                    if (seen[n]) {
+                        k.load(static_cast<const T *>(a.k) + j * a.ldk + koff, at, f.lanes, f.chunks);
+                        v.load(static_cast<const T *>(a.v) + j * a.ldv + koff, at, f.lanes, f.chunks);
+                    }
+                    k.widen(w);
+                    v.widen(x);
+                    sc[n] = dot<E>(q, w);
+                    sc[U + n] = dot<E>(go, x);
+                }
+                key_sums<2 * U>(sc, f.lanes);
+#pragma unroll
+                for (int n = 0; n < U; ++n) {
+                    if (!seen[n]) continue;
+                    const int b = bucket_of(a.bias, a.bias.edges, apart(pos[n], pos_q));
+                    const float pr = exp2_fast(fmaf(sc[n], c1, bias_at(a.bias, heads, b, head) - lse)), v = pr * (sc[U + n] - d[0]);
+                    if (b != cur) {
+                        if (at == 0 && cur >= 0) {
+                            float2 &bin = mine[cur * (32 / f.lanes)];
+                            bin = make_float2(bin.x + run_a, bin.y + run_m);
+                        }
+                        all_a += run_a;
+                        all_m += run_m;
+                        run_a = run_m = 0.f;
+                        cur = b;
+                    }
+                    run_a += v;
+                    run_m += pr;
+                }
+            }
+            if (at == 0 && cur >= 0) {
+                float2 &bin = mine[cur * (32 / f.lanes)];
+                bin = make_float2(bin.x + run_a, bin.y + run_m);
+            }
+            all_a += run_a;
+            all_m += run_m;
+            for (int i = wide; i < 32; i <<= 1) {
+                all_a += __shfl_xor_sync(0xFFFFFFFFu, all_a, i);
+                all_m += __shfl_xor_sync(0xFFFFFFFFu, all_m, i);
+            }
+            const float rest = all_m == 0.f ? 0.f : all_a / all_m;
+            __syncwarp();
+            // the row's bins -> the warp's sums: a lane per (bucket, head), whose rest the head's first lane has
+            for (int i0 = 0; i0 < nb * f.heads; i0 += 32) {
+                const int i = i0 + lane, hl = i & (f.heads - 1);
+                const float r = __shfl_sync(0xFFFFFFFFu, rest, hl * f.lanes);
+                if (i < nb * f.heads) {
+                    float v = 0.f, m = 0.f;
+                    for (int k = 0; k < kpw; ++k) {
+                        float2 &bin = bins[i / f.heads * (32 / f.lanes) + k * f.heads + hl];
+                        v += bin.x;
+                        m += bin.y;
+                        bin = make_float2(0.f, 0.f);
+                    }
+                    sums[i] += v - r * m;
+                }
+            }
+            __syncwarp();
+        }
+    }
+    __syncwarp();
+    for (int i = lane; i < nb * f.heads; i += 32) {
+        const int hl = i & (f.heads - 1), b = i / f.heads, to = hg * f.heads + hl;
+        if (to < a.kv_heads) part[(slice * nb + b) * heads + to * a.group + g] = sums[i];
+    }
 }
 
 FewShape few_shape(const AttnArgs &a, int es)
@@ -925,46 +1121,58 @@ unsigned few_grid(const AttnArgs &a, FewShape &f)
 
 template <int U> size_t few_smem(const FewShape &f) { return (size_t)kFewWarps * kStages * 2 * U * (32 / (f.lanes * f.heads)) * f.slice; }
 
-constexpr int kMaxDevices = 64;
+constexpr int kMaxDevices = 64, kMostSmem = 160 * 1024;
 template <typename Kernel> bool allow_smem(Kernel kernel, std::atomic<bool> (&done)[kMaxDevices])
 {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kMaxDevices) return false;
     if (done[dev]) return true;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024) != cudaSuccess) return false;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostSmem) != cudaSuccess) return false;
     done[dev] = true;
+    return true;
+}
+
+template <typename T, int R, int U, int CPL, bool kBias>
+bool launch_fwd_of(const AttnArgs &a, const FewShape &f, unsigned grid, float *part_o, float2 *part_ml, cudaStream_t st)
+{
+    static std::atomic<bool> done[kMaxDevices] = {};
+    if (!allow_smem(attn_few_fwd_kernel<T, R, U, CPL, kBias>, done)) return false;
+    note_launch();
+    attn_few_fwd_kernel<T, R, U, CPL, kBias><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_o, part_ml);
     return true;
 }
 
 template <typename T, int R, int U>
 bool launch_fwd(const AttnArgs &a, FewShape f, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    static std::atomic<bool> done[2][kMaxDevices] = {};
     const unsigned grid = few_grid(a, f);
+    if (f.chunks <= 32)
+        return a.bias.table ? launch_fwd_of<T, R, U, 1, true>(a, f, grid, part_o, part_ml, st) : launch_fwd_of<T, R, U, 1, false>(a, f, grid, part_o, part_ml, st);
+    if constexpr (sizeof(T) == 4)
+        return a.bias.table ? launch_fwd_of<T, R, U, 2, true>(a, f, grid, part_o, part_ml, st) : launch_fwd_of<T, R, U, 2, false>(a, f, grid, part_o, part_ml, st);
+    return true;
+}
+
+template <typename T, int R, int U, int CPL, bool kBoth, bool kFit, bool kBias>
+bool launch_bwd_of(const AttnArgs &a, const FewShape &f, unsigned grid, float *part_dq, float *dots, cudaStream_t st)
+{
+    static std::atomic<bool> done[kMaxDevices] = {};
+    if (!allow_smem(attn_few_bwd_kernel<T, R, U, CPL, kBoth, kFit, kBias>, done)) return false;
     note_launch();
-    if (f.chunks <= 32) {
-        if (!allow_smem(attn_few_fwd_kernel<T, R, U, 1>, done[0])) return false;
-        attn_few_fwd_kernel<T, R, U, 1><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_o, part_ml);
-    } else if constexpr (sizeof(T) == 4) {
-        if (!allow_smem(attn_few_fwd_kernel<T, R, U, 2>, done[1])) return false;
-        attn_few_fwd_kernel<T, R, U, 2><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_o, part_ml);
-    }
+    attn_few_bwd_kernel<T, R, U, CPL, kBoth, kFit, kBias><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_dq, dots);
     return true;
 }
 
 template <typename T, int R, int U, bool kBoth, bool kFit>
 bool launch_bwd(const AttnArgs &a, FewShape f, float *part_dq, float *dots, cudaStream_t st)
 {
-    static std::atomic<bool> done[2][kMaxDevices] = {};
     const unsigned grid = few_grid(a, f);
-    note_launch();
-    if (f.chunks <= 32) {
-        if (!allow_smem(attn_few_bwd_kernel<T, R, U, 1, kBoth, kFit>, done[0])) return false;
-        attn_few_bwd_kernel<T, R, U, 1, kBoth, kFit><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_dq, dots);
-    } else if constexpr (sizeof(T) == 4) {
-        if (!allow_smem(attn_few_bwd_kernel<T, R, U, 2, kBoth, kFit>, done[1])) return false;
-        attn_few_bwd_kernel<T, R, U, 2, kBoth, kFit><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_dq, dots);
-    }
+    if (f.chunks <= 32)
+        return a.bias.table ? launch_bwd_of<T, R, U, 1, kBoth, kFit, true>(a, f, grid, part_dq, dots, st)
+                            : launch_bwd_of<T, R, U, 1, kBoth, kFit, false>(a, f, grid, part_dq, dots, st);
+    if constexpr (sizeof(T) == 4)
+        return a.bias.table ? launch_bwd_of<T, R, U, 2, kBoth, kFit, true>(a, f, grid, part_dq, dots, st)
+                            : launch_bwd_of<T, R, U, 2, kBoth, kFit, false>(a, f, grid, part_dq, dots, st);
     return true;
 }
 
@@ -1012,8 +1220,10 @@ template <typename T> bool backward_of(const AttnArgs &a, const FewPlan &p, FewS
         f.splits = 1;
         f.warps = 1;
         const unsigned grid = few_grid(a, f);
-        if (f.chunks <= 32) attn_few_dkv_kernel<T, 1><<<grid, kFewThreads, 0, st>>>(a, f, dots);
-        else if constexpr (sizeof(T) == 4) attn_few_dkv_kernel<T, 2><<<grid, kFewThreads, 0, st>>>(a, f, dots);
+        auto *kernel = a.bias.table ? attn_few_dkv_kernel<T, 1, true> : attn_few_dkv_kernel<T, 1, false>;
+        if constexpr (sizeof(T) == 4)
+            if (f.chunks > 32) kernel = a.bias.table ? attn_few_dkv_kernel<T, 2, true> : attn_few_dkv_kernel<T, 2, false>;
+        kernel<<<grid, kFewThreads, 0, st>>>(a, f, dots);
     }
     return true;
 }
@@ -1042,6 +1252,45 @@ FewPlan few_plan(const AttnArgs &a, const Lengths &q, const Lengths &k, int es, 
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want / p.warps, max_k / (turn * p.warps * 4), kMaxSplits, most / p.batches}));
     p.key_batches = blocks_per_unit(k, 1, step * kKeys, units0);
     return p;
+}
+
+// The table's kernel: its bins and sums fit shared memory with one key head side by side at least (32 keys of a step, 128 buckets: 130 KB)
+static size_t table_smem(const AttnArgs &a, const FewShape &f)
+{
+    return (size_t)kFewWarps * a.bias.buckets * (32 / f.lanes * sizeof(float2) + f.heads * sizeof(float));
+}
+static FewShape table_shape(const AttnArgs &a, int32_t dtype)
+{
+    FewShape f = few_shape(a, (int)dtype_size(dtype));
+    while (f.heads > 1 && table_smem(a, f) > (size_t)kMostSmem) f.heads /= 2;
+    f.head_groups = (a.kv_heads + f.heads - 1) / f.heads;
+    return f;
+}
+
+// Warps enough for 16 per SM, each with a slice of the sequences; of their rows where there are fewer sequences than that.
+TablePlan few_table_plan(const AttnArgs &a, int32_t dtype)
+{
+    const FewShape f = table_shape(a, dtype);
+    const int64_t want = std::max<int64_t>(1, 148 * 16 / ((int64_t)f.head_groups * a.group)), n = std::max<int64_t>(a.n_seq, 1);
+    TablePlan p{std::min(n, want), 1};
+    p.row_slices = std::max<int64_t>(1, std::min(want / p.seq_slices, ceil_div(a.q_rows, n)));
+    return p;
+}
+
+bool few_attention_table(const AttnArgs &a, const TablePlan &p, int32_t dtype, float *part, cudaStream_t st)
+{
+    static std::atomic<bool> done[3][kMaxDevices] = {};
+    FewShape f = table_shape(a, dtype);
+    f.units = (uint32_t)(p.seq_slices * p.row_slices * f.head_groups * a.group);
+    const unsigned grid = (unsigned)ceil_div(f.units, kFewWarps);
+    auto launch = [&](auto *kernel, int i) {
+        if (!allow_smem(kernel, done[i])) return false;
+        note_launch();
+        kernel<<<grid, kFewThreads, table_smem(a, f), st>>>(a, f, p.seq_slices, p.row_slices, part);
+        return true;
+    };
+    if (dtype == E2EGREC_BF16) return launch(attn_few_table_kernel<__nv_bfloat16, 1>, 0);
+    return f.chunks <= 32 ? launch(attn_few_table_kernel<float, 1>, 1) : launch(attn_few_table_kernel<float, 2>, 2);
 }
 
 static FewShape planned(const AttnArgs &a, const FewPlan &p, int32_t dtype)
