@@ -163,6 +163,7 @@ struct Plan {
     int64_t q_tiles, k_tiles;             // blocks of rows / tiles of keys per sequence and key head
     int splits;                           // stretches of the keys
     size_t part_bytes, ml_bytes, dot_bytes;
+    bool table_fused;                     // the kernel of dQ forms them
     int64_t table_rows;                   // backward with a bias: rows of partial gradients of the table
     size_t table_bytes;
 };
@@ -180,9 +181,10 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     const Lengths q = lengths(s.max_q, a.q_rows), k = lengths(s.max_k, a.k_rows);
     const int64_t rows = q.typical * a.group, units = std::max<int64_t>(a.n_seq * a.kv_heads, 1);
     const size_t cells = (size_t)a.q_rows * a.kv_heads * a.group;
+    const int n_heads = a.kv_heads * a.group;
     const bool small = rows <= (backward ? 4 : dtype == E2EGREC_F32 ? 3 : 2) || rows * k.typical <= (dtype == E2EGREC_F32 ? 256 : backward ? 700 : 800);
     // (without rows on one side there is nothing to form a product of)
-    p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows || a.bias.buckets ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
+    p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows || (a.bias.buckets && dtype == E2EGREC_F32) || a.bias.buckets * n_heads > kTcTable ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
     if (p.path == Path::tc) {
         p.one_tile = rows <= 128;
         p.q_tiles = blocks_per_unit(q, a.group, backward || p.one_tile ? 128 : 256, units);
@@ -205,7 +207,8 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     }
     if (backward && a.bias.buckets) {
         p.table = few_table_plan(a, dtype);
-        p.table_rows = p.table.seq_slices * p.table.row_slices;
+        p.table_fused = p.path == Path::tc && a.bias.buckets * a.group <= kTcBins;
+        p.table_rows = p.table_fused ? a.n_seq * p.q_tiles : p.table.seq_slices * p.table.row_slices;
         p.table_bytes = align_up((size_t)p.table_rows * a.bias.buckets * a.kv_heads * a.group * sizeof(float), 256);
     }
     return p;
@@ -378,7 +381,7 @@ static int32_t attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q,
     float *dots = static_cast<float *>(ws), *part_dq = reinterpret_cast<float *>(static_cast<char *>(ws) + plan.dot_bytes);
     bool ok = true;
     if (plan.path == Path::tc) {
-        ok = tc_attention_backward(a, plan.q_tiles, plan.k_tiles, dots, st);
+        ok = tc_attention_backward(a, plan.q_tiles, plan.k_tiles, dots, plan.table_fused && dtable ? table_part : nullptr, st);
     } else if (plan.path == Path::simt) {
         ok = simt_attention_backward(a, plan.simt, part_dq, dots, st);
         if (ok && plan.splits > 1 && a.q_rows) join_dq(a, plan.splits, Q->dtype, false, part_dq, nullptr, st);
@@ -386,7 +389,7 @@ static int32_t attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q,
         ok = few_attention_backward(a, plan.few, Q->dtype, part_dq, dots, st);
     }
     if (ok && dtable) {
-        ok = few_attention_table(a, plan.table, Q->dtype, table_part, st);
+        if (!plan.table_fused) ok = few_attention_table(a, plan.table, Q->dtype, table_part, st);
         if (ok) launch_colsum<float>(table_part, table_size, nullptr, nullptr, plan.table_rows, table_size, 0, dtable, st);
     }
     if (!ok) return launch_refused("attention_backward");

@@ -12,6 +12,7 @@
 // and returns.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "attention.cuh"
 #include "tcgen05.cuh"
@@ -195,6 +196,13 @@ __device__ inline uint32_t load_now(const uint8_t *p)
     return v;
 }
 
+__device__ inline int load_now(const int32_t *p)
+{
+    int v;
+    asm volatile("ld.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+    return v;
+}
+
 // Whether the 128 keys from j * 128 on are seen, one bit each; loads for the next tile go out a tile ahead (ahead, then now)
 struct Visible {
     uint32_t next[4];
@@ -212,6 +220,185 @@ struct Visible {
         for (int b = 0; b < 4; ++b) word[b] = __ballot_sync(0xFFFFFFFFu, next[b] != 0);
     }
 };
+
+// ---- Bias by distance.  Buckets are monotone in the distance, so the lowest and the highest position of 32 neighbouring columns give
+// the buckets that a thread's row (or key) meets in them: where it is one, as it nearly always is, the bias is a constant of the 32 scores,
+// else each score's bucket is found by comparing it with the few edges in between.  Positions need not be sorted for that.
+struct BiasShared {
+    int32_t pos[kWordRing][kTile];                   // of the tile's columns: keys (forward pass, dQ), rows of Q (dK, dV)
+    int2 range[kWordRing][4];                        // lowest and highest of each 32 columns that count; lowest > highest: none
+    int32_t edges[kMaxBuckets];
+};
+struct NoBiasShared {};
+template <bool kBias> using BiasShared_ = typename std::conditional<kBias, BiasShared, NoBiasShared>::type;
+
+// The table in shared memory, [heads x buckets] in powers of two, and the edges, by all threads of a block
+__device__ inline void stage_bias(const AttnArgs &a, BiasShared &s, float *table)
+{
+    const int heads = a.kv_heads * a.group, nb = a.bias.buckets;
+    for (int i = threadIdx.x; i < nb - 1; i += blockDim.x) s.edges[i] = __ldg(a.bias.edges + i);
+    for (int i = threadIdx.x; i < nb * heads; i += blockDim.x) table[i % heads * nb + i / heads] = bias_value(__ldg(a.bias.table + i));
+}
+
+// Positions of 4 x 32 columns, a lane each -> shared memory; word: which of them count
+__device__ inline void place(BiasShared &s, uint32_t slot, const int (&pos)[4], const uint32_t (&word)[4], int lane)
+{
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+        const bool on = word[b] >> lane & 1u;
+        const int lo = __reduce_min_sync(0xFFFFFFFFu, on ? pos[b] : INT32_MAX), hi = __reduce_max_sync(0xFFFFFFFFu, on ? pos[b] : INT32_MIN);
+        s.pos[slot][b * 32 + lane] = pos[b];
+        if (lane == 0) s.range[slot][b] = make_int2(lo, hi);
+    }
+    __syncwarp();
+}
+// the keys' positions, a tile ahead as Visible's words
+struct KeyPlaces {
+    int next[4];
+    __device__ inline void ahead(const AttnArgs &a, const Work &x, int j, int lane)
+    {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            const int64_t key = x.kb + (int64_t)j * kTile + b * 32 + lane;
+            next[b] = key < x.ke ? (a.bias.pos_k ? load_now(a.bias.pos_k + key) : (int)(key - x.rg.k0)) : 0;
+        }
+    }
+};
+
+// kKey: the thread's own position is the key's, the columns' are the queries'
+template <bool kKey> __device__ inline int distance(int own, int column) { return kKey ? apart(own, column) : apart(column, own); }
+
+// The buckets lo .. hi that the thread meets in each of N times 32 columns
+template <int N, bool kKey>
+__device__ inline void spans(const BiasArgs &b, const int32_t *edges, const int2 *range, int own, int (&lo)[N], int (&hi)[N])
+{
+    int2 r[N], all = make_int2(INT32_MAX, INT32_MIN);
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        r[c] = range[c];
+        all = make_int2(min(all.x, r[c].x), max(all.y, r[c].y));
+        if (kKey) r[c] = make_int2(r[c].y, r[c].x);
+        lo[c] = hi[c] = 0;
+    }
+    if (all.x > all.y) return;
+    if (kKey) all = make_int2(all.y, all.x);
+    const int first = bucket_of(b, edges, distance<kKey>(own, all.x)), last = bucket_of(b, edges, distance<kKey>(own, all.y));
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        lo[c] = hi[c] = first;
+        if (first == last) continue;
+        const int near = distance<kKey>(own, r[c].x), far = distance<kKey>(own, r[c].y);
+        while (lo[c] < last && edges[lo[c]] <= near) ++lo[c];
+        hi[c] = lo[c];
+        while (hi[c] < last && edges[hi[c]] <= far) ++hi[c];
+    }
+}
+
+// 32 products -> scores in powers of two with their biases.  table: of the row's head, or (kKey, group > 1) of the key head's first, g0 the
+// first column's head of the group.
+template <bool kKey>
+__device__ inline void add_bias(uint32_t (&v)[32], float c1, const BiasArgs &b, const int32_t *edges, const float *table, const int32_t *pos, int own, int lo,
+                                int hi, int group, int g0)
+{
+    if (!kKey || group == 1) {
+        const float t = table[lo];
+        if (lo == hi) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) {
+                const float2 x = __ffma2_rn(pair_of(v[i], v[i + 1]), make_float2(c1, c1), make_float2(t, t));
+                v[i] = __float_as_uint(x.x);
+                v[i + 1] = __float_as_uint(x.y);
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            const int4 p = *reinterpret_cast<const int4 *>(pos + i);
+            const int d[4] = {distance<kKey>(own, p.x), distance<kKey>(own, p.y), distance<kKey>(own, p.z), distance<kKey>(own, p.w)};
+            float w[4] = {t, t, t, t};
+            for (int e = lo; e < hi; ++e) {
+                const int edge = edges[e];
+                const float next = table[e + 1];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = d[k] >= edge ? next : w[k];
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) v[i + k] = __float_as_uint(fmaf(__uint_as_float(v[i + k]), c1, w[k]));
+        }
+        return;
+    }
+    int g = g0;
+#pragma unroll
+    for (int i = 0; i < 32; i += 4) {
+        const int4 p = *reinterpret_cast<const int4 *>(pos + i);
+        const int d[4] = {distance<kKey>(own, p.x), distance<kKey>(own, p.y), distance<kKey>(own, p.z), distance<kKey>(own, p.w)};
+        int at[4] = {lo, lo, lo, lo};
+        for (int e = lo; e < hi; ++e) {
+            const int edge = edges[e];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) at[k] += d[k] >= edge;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[i + k] = __float_as_uint(fmaf(__uint_as_float(v[i + k]), c1, table[g * b.buckets + at[k]]));
+            g = g + 1 == group ? 0 : g + 1;
+        }
+    }
+}
+
+// Sums of dS by bucket and head of the group, of one warp: bins [buckets x group].  Rows of a warp follow one another, so lane i has head
+// (g0 + i) mod group; lanes of one head are added up in a fixed order.
+__device__ inline void add_to_bin(float *bins, int bucket, int group, int g0, float s, int lane)
+{
+    __syncwarp();
+    if (group >= 32) {                                   // no two lanes of one head
+        const int g = g0 + lane;
+        bins[bucket * group + (g >= group ? g - group : g)] += s;
+    } else if ((group & (group - 1)) == 0) {
+        for (int o = 16; o >= group; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+        if (lane < group) bins[bucket * group + lane] += s;      // g0 = 0: rows of a warp begin at a multiple of 32
+    } else {
+        float sum = s;
+        for (int o = group; o < 32; o += group) {
+            const float other = __shfl_down_sync(0xFFFFFFFFu, s, o);
+            if (lane + o < 32) sum += other;
+        }
+        const int g = g0 + lane;
+        if (lane < group) bins[bucket * group + (g >= group ? g - group : g)] += sum;
+    }
+}
+// The dS of a thread's row in 32 columns.  run, cur: sum of the bucket that the warp is in, kept in registers until it leaves it.
+__device__ inline void bin_columns(float *bins, const BiasArgs &b, const int32_t *edges, const int32_t *pos, const int2 &range, const float *ds, int own,
+                                   int lo, int hi, bool live, int group, int g0, float &run, int &cur, int lane)
+{
+    if (range.x > range.y) return;                       // no key is seen
+    float2 s2 = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < 32; i += 2) s2 = __fadd2_rn(s2, make_float2(ds[i], ds[i + 1]));
+    float all = live ? s2.x + s2.y : 0.f;
+    const int first = __reduce_min_sync(0xFFFFFFFFu, lo), last = __reduce_max_sync(0xFFFFFFFFu, hi);
+    if (first != cur || first != last) {
+        if (cur >= 0) add_to_bin(bins, cur, group, g0, run, lane);
+        run = 0.f;
+        cur = first == last ? first : -1;
+    }
+    if (first == last) {
+        run += all;
+        return;
+    }
+    for (int e = first; e <= last; ++e) {
+        const int from = e == first ? INT32_MIN : edges[e - 1], to = e == last ? INT32_MAX : edges[e] - 1;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            const int4 p = *reinterpret_cast<const int4 *>(pos + i);
+            const int d[4] = {apart(p.x, own), apart(p.y, own), apart(p.z, own), apart(p.w, own)};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) s += d[k] >= from && d[k] <= to ? ds[i + k] : 0.f;
+        }
+        add_to_bin(bins, e, group, g0, live ? s : 0.f, lane);
+    }
+}
 
 // the lane that issues the products: a tile has landed, whoever wrote it
 __device__ inline bool tile_ready(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
@@ -260,8 +447,8 @@ __device__ inline void row_steps(uint32_t d, uint32_t a, uint32_t second, uint64
 // NT tiles of 128 rows per block, a softmax warpgroup each.  Two where a key head has more than 128 rows: they share the copies of
 // keys and values, and the products of one run beside the softmax of the other.  One, in half of the shared and tensor memory, where
 // the second would idle: two such blocks per SM overlap instead.
-template <int NB, int NT> struct Fwd {
-    using Ring = TileRing<NT == 2 ? (NB == 2 ? 5 : 8) : (NB == 2 ? 2 : 5)>;      // keys and values
+template <int NB, int NT, bool kBias> struct Fwd {
+    using Ring = TileRing<NT == 2 ? (NB == 2 ? 5 - kBias : 8 - kBias) : (NB == 2 ? 2 : 5 - kBias)>;      // keys and values
     static constexpr int kSoft = NT * 4, kThreads = (kSoft + 4) * 32, kBlocks = 3 - NT;      // copies, zeros, products; one idle
     static constexpr int kRows = NT * kTile, kTileBytes = NB * kBlockBytes, kColumns = NT * 256;
     // p goes to the product in halves where heads take up to 64 columns, the second formed beside the product of the first: 37 x 256 x 8192
@@ -270,12 +457,12 @@ template <int NB, int NT> struct Fwd {
     static constexpr size_t kSmem = 1024 + (size_t)(NT + Ring::kSlots) * kTileBytes;
 };
 
-template <int NB, int NT>
-__global__ void __launch_bounds__(Fwd<NB, NT>::kThreads, Fwd<NB, NT>::kBlocks)
+template <int NB, int NT, bool kBias>
+__global__ void __launch_bounds__(Fwd<NB, NT, kBias>::kThreads, Fwd<NB, NT, kBias>::kBlocks)
 attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                    const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
 {
-    using F = Fwd<NB, NT>;
+    using F = Fwd<NB, NT, kBias>;
     using R = typename F::Ring;
     constexpr int kTileBytes = F::kTileBytes, kRows = F::kRows, kSoft = F::kSoft;
     extern __shared__ uint8_t smem_raw[];
@@ -283,11 +470,14 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     __shared__ __align__(16) uint32_t words[kWordRing][4];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
+    __shared__ __align__(16) BiasShared_<kBias> bias_s;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t *tiles_smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t q_smem = smem_u32(tiles_smem), kv_smem = q_smem + NT * kTileBytes;
     const int ksteps = (a.head_dim + 15) / 16;
+    float *table_s = reinterpret_cast<float *>(tiles_smem + (NT + R::kSlots) * kTileBytes);
+    if constexpr (kBias) stage_bias(a, bias_s, table_s);
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < R::kBarriers; ++s) mbar_init(&kv_full[s], 1);
@@ -324,7 +514,9 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const Work x = work_of(a, f, u, lane == 0);
                 for (int64_t t = x.t0; t * kRows < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                     Visible seen;
+                    KeyPlaces places;
                     seen.ahead(a, x, 0, lane);
+                    if constexpr (kBias) places.ahead(a, x, 0, lane);
                     if (item > 0) ok = warp_wait(&q_empty, (item - 1) & 1u, &abort_flag);
                     if (!ok) break;
                     const int nt = NT == 2 && x.rows - t * kRows > kTile ? 2 : 1;
@@ -348,12 +540,21 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     }
                     for (int j = 0; j < x.n && ok; ++j, ++jj) {
                         uint32_t word[4];
+                        int pos[4];
                         seen.now(word);
-                        if (j + 1 < x.n) seen.ahead(a, x, j + 1, lane);
+                        if constexpr (kBias)
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) pos[b] = places.next[b];
+                        if (j + 1 < x.n) {
+                            seen.ahead(a, x, j + 1, lane);
+                            if constexpr (kBias) places.ahead(a, x, j + 1, lane);
+                        }
                         for (int v = 0; v < 2; ++v, ++g) {
                             const uint32_t s = R::slot(g);
                             if (g >= R::kSlots) ok = warp_wait(&kv_empty[s], (R::use(g) - 1) & 1u, &abort_flag);
                             if (!ok) break;
+                            if constexpr (kBias)
+                                if (v == 0) place(bias_s, jj % kWordRing, pos, word, lane);
                             if (lane == 0) {
                                 if (v == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
                                 mbar_expect_tx(&kv_full[R::full(v, jj)], kTileBytes);
@@ -455,7 +656,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
         const uint32_t s_addr = tmem + lanes + q * kTile, o_addr = tmem_o + lanes + q * 64 * NB;
-        const float c1 = a.scale * kLog2e;
+        const float c1 = a.scale * kLog2e, c2 = kBias ? 1.f : c1;      // c2: of what the scores are once they have their bias
         const int heads = a.kv_heads * a.group;
         uint32_t jj = 0, sc = 0, oc = 0;
         bool ok = true;
@@ -468,6 +669,15 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     continue;
                 }
                 float m = -INFINITY, l = 0.f;
+                int pos_q = 0;
+                const float *table = table_s;
+                if constexpr (kBias) {
+                    int64_t row;
+                    int head;
+                    row_of(a, x, r, row, head);
+                    if (r < x.rows) pos_q = pos_of(a.bias.pos_q, row, x.rg.q0);
+                    table += head * a.bias.buckets;
+                }
                 for (int j = 0; j < x.n; ++j, ++jj) {
                     ok = warp_wait(&s_full[q], sc++ & 1u, &abort_flag);
                     if (!ok) break;
@@ -477,9 +687,18 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     for (int c = 0; c < 4; ++c) word[c] = words[jj % kWordRing][c];
                     // the row's 128 scores stay in registers; four chains for the maximum
                     uint32_t v[4][32];
+                    int lo[4], hi[4];
+                    if constexpr (kBias) {
+                        spans<4, false>(a.bias, bias_s.edges, bias_s.range[jj % kWordRing], pos_q, lo, hi);
+                        __syncwarp();                        // the loads of tensor memory are for a converged warp
+                    }
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_load32_async(s_addr + c * 32, v[c]);
                     tmem_load_wait();
+                    if constexpr (kBias)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            add_bias<false>(v[c], c1, a.bias, bias_s.edges, table, bias_s.pos[jj % kWordRing] + c * 32, pos_q, lo[c], hi[c], 1, 0);
                     float tops[4];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -495,9 +714,9 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                     // The maximum that p and l refer to moves only where a score exceeds it by 8 in the exponent: p <= 2^8 loses
                     // nothing in floating point, and the sums so far are rescaled seldom.
-                    const bool moves = top * c1 > m * c1 + 8.f || m == -INFINITY;
+                    const bool moves = top * c2 > m * c2 + 8.f || m == -INFINITY;
                     if (j > 0 && __any_sync(0xFFFFFFFFu, moves && top != -INFINITY)) {
-                        const float f = moves && top != -INFINITY ? exp2_approx((m - top) * c1) : 1.f;
+                        const float f = moves && top != -INFINITY ? exp2_approx((m - top) * c2) : 1.f;
                         l *= f;
                         __syncwarp();
                         for (int c = 0; c < NB * 4; ++c) {
@@ -510,8 +729,9 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         }
                     }
                     if (moves) m = top;
-                    const float base = m == -INFINITY ? 0.f : m * c1;
-                    const float2 scale2 = make_float2(c1, c1), base2 = make_float2(-base, -base);
+                    const float base = m == -INFINITY ? 0.f : m * c2;
+                    if constexpr (kBias) __syncwarp();       // the stores to tensor memory are for a converged warp
+                    const float2 scale2 = make_float2(c2, c2), base2 = make_float2(-base, -base);
                     float2 sums[4];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -580,8 +800,8 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (lane == 0) mbar_arrive(&o_empty[q]);
                 }
                 if (live) {
-                    if (f.splits > 1) part_ml[((int64_t)x.z * a.q_rows + row) * heads + head] = make_float2(l == 0.f ? -INFINITY : m * c1, l);
-                    else if (a.lse) a.lse[row * heads + head] = l == 0.f ? -INFINITY : (m * c1 + log2f(l)) * kLn2;
+                    if (f.splits > 1) part_ml[((int64_t)x.z * a.q_rows + row) * heads + head] = make_float2(l == 0.f ? -INFINITY : m * c2, l);
+                    else if (a.lse) a.lse[row * heads + head] = l == 0.f ? -INFINITY : (m * c2 + log2f(l)) * kLn2;
                 }
             }
         }
@@ -596,9 +816,9 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 // ------------------------------------------------------------------------------------------------- backward
 // Two kernels, so that no gradient is added up by atomics: dQ goes over the keys of a tile of rows, dK and dV over the rows of a
 // tile of keys; the scores are formed in both.  Two warpgroups share a tile of 128 x 128: 64 columns each, one row per thread.
-template <int NB> struct Bwd {
+template <int NB, bool kBias> struct Bwd {
     static constexpr int kThreads = 12 * 32, kTileBytes = NB * kBlockBytes;      // copies, zeros, products; one idle
-    using KvRing = TileRing<NB == 2 ? 5 : 8>;
+    using KvRing = TileRing<NB == 2 ? 5 - kBias : 8 - 2 * kBias>;
     static constexpr int kQgStages = NB == 2 ? 4 : 8;
     static constexpr size_t kDqSmem = 1024 + (size_t)(2 + KvRing::kSlots) * kTileBytes, kDkvSmem = 1024 + (size_t)(2 + kQgStages) * kTileBytes;
 };
@@ -652,7 +872,7 @@ __device__ inline void store_row(uint32_t taddr, bf16 *out, int head_dim, float 
 }
 
 // Passes over the keys
-__device__ inline int passes_of(const Work &x, int head_dim) { return (int64_t)x.n * kTile > 32 * head_dim ? 2 : 1; }
+template <bool kBias> __device__ inline int passes_of(const Work &x, int head_dim) { return kBias ? min(x.n, 2) : ((int64_t)x.n * kTile > 32 * head_dim ? 2 : 1); }
 
 // dQ, and D = dO . out of every row for the other kernel.  What the stored out's D lacks is the sum of p (dP - D) over the keys; it meets
 // sum p k in dQ, which does not get smaller with the number of keys, as dQ does.  Where one tile holds all keys it is added to D before dS is
@@ -662,15 +882,19 @@ __device__ inline int passes_of(const Work &x, int head_dim) { return (int64_t)x
 // for values whose mean is a quarter of their spread.
 // dS goes into its product as two bf16 operands, its rounding and the rest: with dS rounded once dQ was 2.5 to 2.7e-3 off in the mean (a
 // rounding of the result: 1.8e-3), at most 2.4e-3 so; the training case's backward pass takes 550 us with one operand, 585 us so.
-template <int NB>
-__global__ void __launch_bounds__(Bwd<NB>::kThreads, 1)
+// With a bias all sequences of more than one tile take the second pass: the table's gradient, sums of dS that are left from what cancels, needs
+// D as it is.  Each warp adds up its rows' dS by bucket in bins of its own; a unit's bins, in the order of the warps, are a row of part
+// [sequences x tiles, buckets x heads], which the caller adds up.
+template <int NB, bool kBias>
+__global__ void __launch_bounds__(Bwd<NB, kBias>::kThreads, 1)
 attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_k,
-                  const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f, float *__restrict__ dots)
+                  const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f, float *__restrict__ dots,
+                  float *__restrict__ table_part)
 {
-    using R = typename Bwd<NB>::KvRing;
-    constexpr int kTileBytes = Bwd<NB>::kTileBytes;
+    using R = typename Bwd<NB, kBias>::KvRing;
+    constexpr int kTileBytes = Bwd<NB, kBias>::kTileBytes;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kv_full[R::kBarriers], kv_empty[R::kSlots], k_clean[kWordRing], q_full, q_empty, s_full[2], dp_full, ds_full, o_full, o_empty, rest_full;
+    __shared__ uint64_t kv_full[R::kBarriers], kv_empty[R::kSlots], k_clean[kWordRing], q_full, q_empty, s_full[2], dp_full, ds_full, o_full, o_empty, rest_full, bins_full;
     __shared__ float rests[2][kTile];                 // sums of p (dP - D) over each warpgroup's columns
     __shared__ __align__(16) uint32_t words[kWordRing][4];
     __shared__ uint32_t tmem_slot;
@@ -680,6 +904,13 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     uint8_t *tiles_smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t q_smem = smem_u32(tiles_smem), g_smem = q_smem + kTileBytes, kv_smem = q_smem + 2 * kTileBytes;
     const int ksteps = (a.head_dim + 15) / 16;
+    __shared__ __align__(16) BiasShared_<kBias> bias_s;
+    float *table_s = reinterpret_cast<float *>(tiles_smem + (2 + R::kSlots) * kTileBytes), *bins_s = table_s + a.bias.buckets * a.kv_heads * a.group;
+    if constexpr (kBias) {
+        stage_bias(a, bias_s, table_s);
+        if (table_part)
+            for (int i = threadIdx.x; i < 8 * a.bias.buckets * a.group; i += blockDim.x) bins_s[i] = 0.f;
+    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < R::kBarriers; ++s) mbar_init(&kv_full[s], 1);
         for (int s = 0; s < R::kSlots; ++s) mbar_init(&kv_empty[s], 1);
@@ -693,6 +924,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         mbar_init(&o_full, 1);
         mbar_init(&o_empty, 8);
         mbar_init(&rest_full, 8);
+        mbar_init(&bins_full, 8);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -714,10 +946,12 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             bool ok = true;
             for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
                 const Work x = work_of(a, f, u, lane == 0);
-                const int steps = x.n * passes_of(x, a.head_dim);
+                const int steps = x.n * passes_of<kBias>(x, a.head_dim);
                 for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                     Visible seen;
+                    KeyPlaces places;
                     seen.ahead(a, x, 0, lane);
+                    if constexpr (kBias) places.ahead(a, x, 0, lane);
                     if (item > 0) ok = warp_wait(&q_empty, (item - 1) & 1u, &abort_flag);
                     if (!ok) break;
                     if (f.boxes) {
@@ -742,12 +976,21 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     for (int j = 0, tile = 0; j < steps && ok; ++j, ++jj) {
                         const int next = tile + 1 < x.n ? tile + 1 : 0;
                         uint32_t word[4];
+                        int pos[4];
                         seen.now(word);
-                        if (j + 1 < steps) seen.ahead(a, x, next, lane);
+                        if constexpr (kBias)
+#pragma unroll
+                            for (int b = 0; b < 4; ++b) pos[b] = places.next[b];
+                        if (j + 1 < steps) {
+                            seen.ahead(a, x, next, lane);
+                            if constexpr (kBias) places.ahead(a, x, next, lane);
+                        }
                         for (int v = 0; v < 2; ++v, ++g) {
                             const uint32_t s = R::slot(g);
                             if (g >= R::kSlots) ok = warp_wait(&kv_empty[s], (R::use(g) - 1) & 1u, &abort_flag);
                             if (!ok) break;
+                            if constexpr (kBias)
+                                if (v == 0) place(bias_s, jj % kWordRing, pos, word, lane);
                             if (lane == 0) {
                                 if (v == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
                                 mbar_expect_tx(&kv_full[R::full(v, jj)], kTileBytes);
@@ -769,7 +1012,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             bool ok = true;
             for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
                 const Work x = work_of(a, f, u, false);
-                const int steps = x.n * passes_of(x, a.head_dim);
+                const int steps = x.n * passes_of<kBias>(x, a.head_dim);
                 for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles)
                     for (int j = 0; j < steps && ok; ++j, ++jj, g += 2) {
                         ok = warp_wait(&kv_full[R::full(0, jj)], R::parity(jj), &abort_flag);
@@ -798,7 +1041,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 };
                 for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
                     const Work x = work_of(a, f, u, false);
-                    const int steps = x.n * passes_of(x, a.head_dim), first = steps - x.n;      // of the last pass
+                    const int steps = x.n * passes_of<kBias>(x, a.head_dim), first = steps - x.n;      // of the last pass
                     for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                         ok = tile_ready(&q_full, item & 1u, &abort_flag);
                         if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
@@ -843,13 +1086,14 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         // ---- p and dS: 64 columns of one row per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
-        const float c1 = a.scale * kLog2e;
+        const float c1 = a.scale * kLog2e, c2 = kBias ? 1.f : c1;
         const int heads = a.kv_heads * a.group;
-        uint32_t jj = 0, item = 0, corrected = 0;
+        uint32_t jj = 0, item = 0, corrected = 0, binned = 0;
         bool ok = true;
+        float *bins = bins_s + warp * a.bias.buckets * a.group;
         for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
             const Work x = work_of(a, f, u, false);
-            const int steps = x.n * passes_of(x, a.head_dim), first = steps - x.n;
+            const int steps = x.n * passes_of<kBias>(x, a.head_dim), first = steps - x.n;
             for (int64_t t = x.t0; t * kTile < x.rows && ok; t += f.tiles) {
                 const int64_t r = t * kTile + w * 32 + lane;
                 int64_t row;
@@ -872,20 +1116,37 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     }
                     if (l == -INFINITY) dot = 0.f;
                 }
-                float rest = 0.f;
+                float rest = 0.f, run = 0.f;
+                int pos_q = 0, cur = -1;
+                const int g0 = kBias ? (int)((t * kTile + w * 32) % a.group) : 0;
+                const float *table = table_s;
+                if constexpr (kBias) {
+                    if (live) pos_q = pos_of(a.bias.pos_q, row, x.rg.q0);
+                    table += head * a.bias.buckets;
+                }
                 for (int j = 0; j < steps; ++j, ++jj) {
+                    int lo[2], hi[2];
                     ok = warp_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
                     if (!ok) break;
                     tc_fence_after();
                     float p[64];
                     {
                         uint32_t v[2][32];
+                        if constexpr (kBias) {
+                            spans<2, false>(a.bias, bias_s.edges, bias_s.range[jj % kWordRing] + q * 2, pos_q, lo, hi);
+                            __syncwarp();                    // the loads of tensor memory are for a converged warp
+                        }
                         tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64, v[0]);
                         tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64 + 32, v[1]);
                         tmem_load_wait();
+                        if constexpr (kBias) {
+#pragma unroll
+                            for (int c = 0; c < 2; ++c)
+                                add_bias<false>(v[c], c1, a.bias, bias_s.edges, table, bias_s.pos[jj % kWordRing] + q * 64 + c * 32, pos_q, lo[c], hi[c], 1, 0);
+                        }
 #pragma unroll
                         for (int e = 0; e < 64; e += 2) {
-                            const float2 y = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(c1, c1), make_float2(-base, -base)));
+                            const float2 y = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(c2, c2), make_float2(-base, -base)));
                             p[e] = y.x;
                             p[e + 1] = y.y;
                         }
@@ -954,6 +1215,14 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                                 if (!((word >> e) & 1u)) p[c * 32 + e] = 0.f;
                         }
                     }
+                    if constexpr (kBias)
+                        if (table_part) {
+#pragma unroll
+                            for (int c = 0; c < 2; ++c)
+                                bin_columns(bins, a.bias, bias_s.edges, bias_s.pos[jj % kWordRing] + q * 64 + c * 32, bias_s.range[jj % kWordRing][q * 2 + c],
+                                            p + c * 32, pos_q, lo[c], hi[c], live && base != INFINITY, a.group, g0, run, cur, lane);
+                            __syncwarp();
+                        }
                     store_operand_and_rest(tmem + lanes + 256 + q * 64, tmem + lanes + (jj & 1u) * kTile + q * 64, p);
                     tmem_store_wait();
                     tc_fence_before();
@@ -961,6 +1230,8 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     if (lane == 0) mbar_arrive(&ds_full);
                 }
                 if (!ok) break;
+                if constexpr (kBias)
+                    if (table_part && cur >= 0) add_to_bin(bins, cur, a.group, g0, run, lane);
                 if (live && q == 0) dots[row * heads + head] = dot;
                 if (x.n > 0) {
                     ok = warp_wait(&o_full, item++ & 1u, &abort_flag);
@@ -972,6 +1243,28 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 __syncwarp();
                 if (lane == 0 && x.n > 0) mbar_arrive(&o_empty);
             }
+            if constexpr (kBias)
+                if (table_part && ok) {                      // the unit's bins: all warps have added theirs, and then all have read them
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bins_full);
+                    ok = warp_wait(&bins_full, binned++ & 1u, &abort_flag);
+                    if (!ok) break;
+                    const int size = a.bias.buckets * a.group;
+                    const uint32_t seq = u / (uint32_t)f.tiles / (uint32_t)a.kv_heads;
+                    float *part = table_part + ((int64_t)seq * f.tiles + x.t0) * a.bias.buckets * heads + x.h * a.group;
+                    for (int i = threadIdx.x; i < size; i += 256) {
+                        float s = 0.f;
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) s += bins_s[k * size + i];
+                        part[i / a.group * heads + i % a.group] = s;
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bins_full);
+                    ok = warp_wait(&bins_full, binned++ & 1u, &abort_flag);
+                    if (!ok) break;
+                    for (int i = lane; i < size; i += 32) bins[i] = 0.f;
+                    __syncwarp();
+                }
         }
     }
     __syncwarp();
@@ -982,13 +1275,13 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 }
 
 // dK and dV of a tile of keys: S^T = K Q^T and dP^T = V dO^T over the rows of the sequence
-template <int NB>
-__global__ void __launch_bounds__(Bwd<NB>::kThreads, 1)
+template <int NB, bool kBias>
+__global__ void __launch_bounds__(Bwd<NB, kBias>::kThreads, 1)
 attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f,
                    const float *__restrict__ dots)
 {
-    constexpr int kStages = Bwd<NB>::kQgStages, kTileBytes = Bwd<NB>::kTileBytes;
+    constexpr int kStages = Bwd<NB, kBias>::kQgStages, kTileBytes = Bwd<NB, kBias>::kTileBytes;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t qg_full[kStages], qg_clean[kStages], qg_empty[kStages], kv_full, kv_empty, s_full, p_full, dp_full, ds_full, o_full, o_empty;
     __shared__ __align__(16) float stat_lse[kWordRing][kTile], stat_dot[kWordRing][kTile];
@@ -1000,6 +1293,9 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     uint8_t *tiles_smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t k_smem = smem_u32(tiles_smem), v_smem = k_smem + kTileBytes, qg_smem = k_smem + 2 * kTileBytes;
     const int ksteps = (a.head_dim + 15) / 16;
+    __shared__ __align__(16) BiasShared_<kBias> bias_s;
+    float *table_s = reinterpret_cast<float *>(tiles_smem + (2 + kStages) * kTileBytes);
+    if constexpr (kBias) stage_bias(a, bias_s, table_s);
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
             mbar_init(&qg_full[s], f.boxes ? 1 : kCopyArrivals);
@@ -1039,6 +1335,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const int64_t keys = x.ke - x.kb;
                 const int n = (int)((x.rows + kTile - 1) / kTile);
                 float lse[4], dot[4];
+                int pos[4];
                 auto ahead = [&](int j) {
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
@@ -1048,6 +1345,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         row_of(a, x, r, row, head);
                         lse[b] = r < x.rows ? load_now(a.lse + row * heads + head) : -INFINITY;
                         dot[b] = r < x.rows ? load_now(dots + row * heads + head) : 0.f;
+                        if constexpr (kBias) pos[b] = r < x.rows ? (a.bias.pos_q ? load_now(a.bias.pos_q + row) : (int)(row - x.rg.q0)) : 0;
                     }
                 };
                 for (int64_t t = x.t0; t * kTile < keys && n > 0 && ok; t += f.tiles, ++item) {
@@ -1062,9 +1360,11 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     for (int j = 0; j < n && ok; ++j, ++jj) {
                         float l[4], d[4];
                         uint32_t word[4];
+                        int here[4];
 #pragma unroll
                         for (int b = 0; b < 4; ++b) {
                             const bool on = lse[b] != -INFINITY;
+                            if constexpr (kBias) here[b] = pos[b];
                             l[b] = on ? lse[b] * kLog2e : INFINITY;
                             d[b] = on ? dot[b] : 0.f;
                             word[b] = __ballot_sync(0xFFFFFFFFu, on);
@@ -1081,6 +1381,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                                     stat_dot[jj % kWordRing][b * 32 + lane] = -d[b];
                                 }
                                 if (lane == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
+                                if constexpr (kBias) place(bias_s, jj % kWordRing, here, word, lane);
                                 __syncwarp();
                             }
                             if (f.boxes) {
@@ -1196,7 +1497,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // ---- p and dS: 64 columns (rows of Q) of one key per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
-        const float c1 = a.scale * kLog2e;
+        const float c1 = a.scale * kLog2e, c2 = kBias ? 1.f : c1;
         uint32_t jj = 0, item = 0;
         bool ok = true;
         for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
@@ -1206,6 +1507,9 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             for (int64_t t = x.t0; t * kTile < keys && ok; t += f.tiles) {
                 const int64_t key = x.kb + t * kTile + w * 32 + lane;
                 const bool live = key < x.ke, seen = live && (!a.mask || a.mask[key]);
+                int pos_k = 0;
+                if constexpr (kBias)
+                    if (live) pos_k = pos_of(a.bias.pos_k, key, x.rg.k0);
                 for (int j = 0; j < n; ++j, ++jj) {
                     ok = warp_wait(&s_full, jj & 1u, &abort_flag);
                     if (!ok) break;
@@ -1215,20 +1519,34 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     float p[64];
                     {
                         uint32_t v[2][32];
+                        int lo[2], hi[2];
+                        if constexpr (kBias) {
+                            spans<2, true>(a.bias, bias_s.edges, bias_s.range[jj % kWordRing] + q * 2, pos_k, lo, hi);
+                            __syncwarp();                    // the loads of tensor memory are for a converged warp
+                        }
                         tmem_load32_async(tmem + lanes + q * 64, v[0]);
                         tmem_load32_async(tmem + lanes + q * 64 + 32, v[1]);
                         tmem_load_wait();
+                        if constexpr (kBias) {
+#pragma unroll
+                            for (int c = 0; c < 2; ++c) {
+                                const int at = q * 64 + c * 32, g0 = a.group == 1 ? 0 : (int)(((int64_t)j * kTile + at) % a.group);
+                                add_bias<true>(v[c], c1, a.bias, bias_s.edges, table_s + x.h * a.group * a.bias.buckets, bias_s.pos[jj % kWordRing] + at, pos_k,
+                                               lo[c], hi[c], a.group, g0);
+                            }
+                        }
 #pragma unroll
                         for (int e = 0; e < 64; e += 4) {
                             const float4 l = lse4[e / 4];            // negated, as the sums of products below
-                            const float2 y0 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(c1, c1), make_float2(l.x, l.y)));
-                            const float2 y1 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][(e & 31) + 2], v[e >> 5][(e & 31) + 3]), make_float2(c1, c1), make_float2(l.z, l.w)));
+                            const float2 y0 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(c2, c2), make_float2(l.x, l.y)));
+                            const float2 y1 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][(e & 31) + 2], v[e >> 5][(e & 31) + 3]), make_float2(c2, c2), make_float2(l.z, l.w)));
                             p[e] = y0.x;
                             p[e + 1] = y0.y;
                             p[e + 2] = y1.x;
                             p[e + 3] = y1.y;
                         }
                     }
+                    if constexpr (kBias) __syncwarp();       // the stores to tensor memory are for a converged warp
                     store_operand(tmem + lanes + q * 64, p);
                     tmem_store_wait();
                     tc_fence_before();
@@ -1326,28 +1644,40 @@ bool make_maps(const AttnArgs &a, Maps &m)
 // so that the hardware hands them out as blocks end.
 uint32_t tc_grid(uint32_t units, int blocks) { return units >= 8u * kSms * blocks ? kSms * blocks : units; }
 
-template <int NB, int NT> bool launch_fwd(const AttnArgs &a, const Maps &m, const TcShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
+template <int NB, int NT, bool kBias> bool launch_fwd(const AttnArgs &a, const Maps &m, const TcShape &f, float *part_o, float2 *part_ml, cudaStream_t st)
 {
     static std::atomic<bool> done[kMaxDevices] = {};
-    using F = Fwd<NB, NT>;
-    if (!allow_smem(attn_tc_fwd_kernel<NB, NT>, F::kSmem, done)) return false;
+    using F = Fwd<NB, NT, kBias>;
+    const size_t most = F::kSmem + (kBias ? kTcTable * sizeof(float) : 0), smem = F::kSmem + (size_t)a.bias.buckets * a.kv_heads * a.group * sizeof(float);
+    if (!allow_smem(attn_tc_fwd_kernel<NB, NT, kBias>, most, done)) return false;
     note_launch();
-    attn_tc_fwd_kernel<NB, NT><<<tc_grid(f.units, F::kBlocks), F::kThreads, F::kSmem, st>>>(m.q, m.k, m.v, a, f, part_o, part_ml);
+    attn_tc_fwd_kernel<NB, NT, kBias><<<tc_grid(f.units, F::kBlocks), F::kThreads, smem, st>>>(m.q, m.k, m.v, a, f, part_o, part_ml);
     return true;
 }
 
-template <int NB> bool launch_bwd(const AttnArgs &a, const Maps &m, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st)
+template <int NB, bool kBias>
+bool launch_bwd(const AttnArgs &a, const Maps &m, int64_t q_tiles, int64_t k_tiles, float *dots, float *table_part, cudaStream_t st)
 {
     static std::atomic<bool> done[2][kMaxDevices] = {};
-    using B = Bwd<NB>;
-    if (!allow_smem(attn_tc_dq_kernel<NB>, B::kDqSmem, done[0]) || !allow_smem(attn_tc_dkv_kernel<NB>, B::kDkvSmem, done[1])) return false;
+    using B = Bwd<NB, kBias>;
+    const size_t table = (size_t)a.bias.buckets * a.kv_heads * a.group * sizeof(float), bins = table_part ? 8 * (size_t)a.bias.buckets * a.group * sizeof(float) : 0;
+    if (!allow_smem(attn_tc_dq_kernel<NB, kBias>, B::kDqSmem + (kBias ? (kTcTable + 8 * kTcBins) * sizeof(float) : 0), done[0]) ||
+        !allow_smem(attn_tc_dkv_kernel<NB, kBias>, B::kDkvSmem + (kBias ? kTcTable * sizeof(float) : 0), done[1]))
+        return false;
     const int64_t units = a.n_seq * a.kv_heads;
     const TcShape fq{(uint32_t)(units * q_tiles), (int)q_tiles, 1, m.boxes}, fk{(uint32_t)(units * k_tiles), (int)k_tiles, 1, m.boxes};
     note_launch();
-    attn_tc_dq_kernel<NB><<<tc_grid(fq.units, 1), B::kThreads, B::kDqSmem, st>>>(m.q, m.g, m.k, m.v, a, fq, dots);
+    attn_tc_dq_kernel<NB, kBias><<<tc_grid(fq.units, 1), B::kThreads, B::kDqSmem + table + bins, st>>>(m.q, m.g, m.k, m.v, a, fq, dots, table_part);
     note_launch();
-    attn_tc_dkv_kernel<NB><<<tc_grid(fk.units, 1), B::kThreads, B::kDkvSmem, st>>>(m.q, m.g, m.k, m.v, a, fk, dots);
+    attn_tc_dkv_kernel<NB, kBias><<<tc_grid(fk.units, 1), B::kThreads, B::kDkvSmem + table, st>>>(m.q, m.g, m.k, m.v, a, fk, dots);
     return true;
+}
+
+template <bool kBias>
+bool forward_of(const AttnArgs &a, const Maps &m, const TcShape &f, bool one_tile, float *part_o, float2 *part_ml, cudaStream_t st)
+{
+    if (a.head_dim <= 64) return one_tile ? launch_fwd<1, 1, kBias>(a, m, f, part_o, part_ml, st) : launch_fwd<1, 2, kBias>(a, m, f, part_o, part_ml, st);
+    return one_tile ? launch_fwd<2, 1, kBias>(a, m, f, part_o, part_ml, st) : launch_fwd<2, 2, kBias>(a, m, f, part_o, part_ml, st);
 }
 
 }  // namespace
@@ -1357,15 +1687,16 @@ bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, bool one
     Maps m;
     if (!make_maps(a, m)) return false;
     const TcShape f{(uint32_t)(a.n_seq * a.kv_heads * tiles * splits), (int)tiles, splits, m.boxes};
-    if (a.head_dim <= 64) return one_tile ? launch_fwd<1, 1>(a, m, f, part_o, part_ml, st) : launch_fwd<1, 2>(a, m, f, part_o, part_ml, st);
-    return one_tile ? launch_fwd<2, 1>(a, m, f, part_o, part_ml, st) : launch_fwd<2, 2>(a, m, f, part_o, part_ml, st);
+    return a.bias.table ? forward_of<true>(a, m, f, one_tile, part_o, part_ml, st) : forward_of<false>(a, m, f, one_tile, part_o, part_ml, st);
 }
 
-bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st)
+bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, float *table_part, cudaStream_t st)
 {
     Maps m;
     if (!make_maps(a, m)) return false;
-    return a.head_dim <= 64 ? launch_bwd<1>(a, m, q_tiles, k_tiles, dots, st) : launch_bwd<2>(a, m, q_tiles, k_tiles, dots, st);
+    if (a.bias.table)
+        return a.head_dim <= 64 ? launch_bwd<1, true>(a, m, q_tiles, k_tiles, dots, table_part, st) : launch_bwd<2, true>(a, m, q_tiles, k_tiles, dots, table_part, st);
+    return a.head_dim <= 64 ? launch_bwd<1, false>(a, m, q_tiles, k_tiles, dots, nullptr, st) : launch_bwd<2, false>(a, m, q_tiles, k_tiles, dots, nullptr, st);
 }
 
 }  // namespace e2egrec
