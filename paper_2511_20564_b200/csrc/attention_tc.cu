@@ -68,6 +68,20 @@ __device__ inline void tmem_load16_async(uint32_t taddr, uint32_t (&r)[16])
         : "r"(taddr));
 }
 
+__device__ inline void tmem_load8_async(uint32_t taddr, uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr));
+}
+
+__device__ inline void tmem_store8(uint32_t taddr, const uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+                 : "memory");
+}
+
 // Registers are dealt out anew once the block runs, kCopies to the threads of copies and products, kScores to those of the scores.  One
 // block per SM: 384 threads x 168 at launch = 128 x 72 + 256 x 216 (forward) = 128 x 104 + 256 x 200 (backward, whose copies hold statistics
 // of rows a tile ahead; spilled, they were waited for).  Two blocks per SM: 256 threads x 128 = 128 x 72 + 128 x 184.
@@ -221,13 +235,18 @@ struct Visible {
     }
 };
 
-// ---- Bias by distance.  Buckets are monotone in the distance, so the lowest and the highest position of 32 neighbouring columns give
-// the buckets that a thread's row (or key) meets in them: where it is one, as it nearly always is, the bias is a constant of the 32 scores,
-// else each score's bucket is found by comparing it with the few edges in between.  Positions need not be sorted for that.
+// ---- Bias by distance.  Buckets are monotone in the distance, so the lowest and the highest position of neighbouring columns give the buckets
+// that a thread's row (or key) meets in them.  Where that is one for a whole tile, its bias goes into the exponent's argument and costs
+// nothing per score.  Else the scores get their biases in tensor memory, 32 columns at a time: one bucket, or a few with the edges between
+// them, each a threshold that the columns' positions are compared with; where they are more than four (close to the diagonal), every score
+// looks its bucket up.  Positions need not be sorted for that, but where they are the next columns' bucket is the last one's or its neighbour.
+// What decides is the code's size: with the scores' biases in the registers that hold a row of 128 scores, four copies of it, the forward pass of
+// 8 x 2048 x 2048 took 690 us, 5 of 6 stalls for instructions.
 struct BiasShared {
     int32_t pos[kWordRing][kTile];                   // of the tile's columns: keys (forward pass, dQ), rows of Q (dK, dV)
     int2 range[kWordRing][4];                        // lowest and highest of each 32 columns that count; lowest > highest: none
-    int32_t edges[kMaxBuckets];
+    int4 halves[kWordRing];                          // the same of each 64
+    int32_t edges[kMaxBuckets];                      // beyond the last: the highest number
 };
 struct NoBiasShared {};
 template <bool kBias> using BiasShared_ = typename std::conditional<kBias, BiasShared, NoBiasShared>::type;
@@ -236,20 +255,22 @@ template <bool kBias> using BiasShared_ = typename std::conditional<kBias, BiasS
 __device__ inline void stage_bias(const AttnArgs &a, BiasShared &s, float *table)
 {
     const int heads = a.kv_heads * a.group, nb = a.bias.buckets;
-    for (int i = threadIdx.x; i < nb - 1; i += blockDim.x) s.edges[i] = __ldg(a.bias.edges + i);
+    for (int i = threadIdx.x; i < kMaxBuckets; i += blockDim.x) s.edges[i] = i < nb - 1 ? __ldg(a.bias.edges + i) : INT32_MAX;
     for (int i = threadIdx.x; i < nb * heads; i += blockDim.x) table[i % heads * nb + i / heads] = bias_value(__ldg(a.bias.table + i));
 }
 
 // Positions of 4 x 32 columns, a lane each -> shared memory; word: which of them count
 __device__ inline void place(BiasShared &s, uint32_t slot, const int (&pos)[4], const uint32_t (&word)[4], int lane)
 {
+    int2 r[4];
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
         const bool on = word[b] >> lane & 1u;
-        const int lo = __reduce_min_sync(0xFFFFFFFFu, on ? pos[b] : INT32_MAX), hi = __reduce_max_sync(0xFFFFFFFFu, on ? pos[b] : INT32_MIN);
+        r[b] = make_int2(__reduce_min_sync(0xFFFFFFFFu, on ? pos[b] : INT32_MAX), __reduce_max_sync(0xFFFFFFFFu, on ? pos[b] : INT32_MIN));
         s.pos[slot][b * 32 + lane] = pos[b];
-        if (lane == 0) s.range[slot][b] = make_int2(lo, hi);
+        if (lane == 0) s.range[slot][b] = r[b];
     }
+    if (lane == 0) s.halves[slot] = make_int4(min(r[0].x, r[1].x), max(r[0].y, r[1].y), min(r[2].x, r[3].x), max(r[2].y, r[3].y));
     __syncwarp();
 }
 // the keys' positions, a tile ahead as Visible's words
@@ -268,82 +289,165 @@ struct KeyPlaces {
 // kKey: the thread's own position is the key's, the columns' are the queries'
 template <bool kKey> __device__ inline int distance(int own, int column) { return kKey ? apart(own, column) : apart(column, own); }
 
-// The buckets lo .. hi that the thread meets in each of N times 32 columns
-template <int N, bool kKey>
-__device__ inline void spans(const BiasArgs &b, const int32_t *edges, const int2 *range, int own, int (&lo)[N], int (&hi)[N])
+// The buckets of N distances side by side.  Steps by powers of two over the edges in shared memory; those behind the last are passed by the
+// highest distance alone, whose bucket is the last.
+template <int N> __device__ inline void look_up(const BiasArgs &b, const int32_t *edges, const int (&d)[N], int (&at)[N])
 {
-    int2 r[N], all = make_int2(INT32_MAX, INT32_MIN);
 #pragma unroll
-    for (int c = 0; c < N; ++c) {
-        r[c] = range[c];
-        all = make_int2(min(all.x, r[c].x), max(all.y, r[c].y));
-        if (kKey) r[c] = make_int2(r[c].y, r[c].x);
-        lo[c] = hi[c] = 0;
-    }
-    if (all.x > all.y) return;
-    if (kKey) all = make_int2(all.y, all.x);
-    const int first = bucket_of(b, edges, distance<kKey>(own, all.x)), last = bucket_of(b, edges, distance<kKey>(own, all.y));
+    for (int i = 0; i < N; ++i) at[i] = 0;
+    for (int s = b.top; s; s >>= 1)
 #pragma unroll
-    for (int c = 0; c < N; ++c) {
-        lo[c] = hi[c] = first;
-        if (first == last) continue;
-        const int near = distance<kKey>(own, r[c].x), far = distance<kKey>(own, r[c].y);
-        while (lo[c] < last && edges[lo[c]] <= near) ++lo[c];
-        hi[c] = lo[c];
-        while (hi[c] < last && edges[hi[c]] <= far) ++hi[c];
-    }
+        for (int i = 0; i < N; ++i) at[i] += edges[at[i] + s - 1] <= d[i] ? s : 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) at[i] = min(at[i], b.buckets - 1);
 }
 
-// 32 products -> scores in powers of two with their biases.  table: of the row's head, or (kKey, group > 1) of the key head's first, g0 the
-// first column's head of the group.
-template <bool kKey>
-__device__ inline void add_bias(uint32_t (&v)[32], float c1, const BiasArgs &b, const int32_t *edges, const float *table, const int32_t *pos, int own, int lo,
-                                int hi, int group, int g0)
-{
-    if (!kKey || group == 1) {
-        const float t = table[lo];
-        if (lo == hi) {
+// The bucket that a thread is in: its number and the distances low .. top that are in it
+struct Bucket {
+    int at, low, top;
+    __device__ inline void unknown() { at = 0, low = 1, top = 0; }
+    __device__ inline void up(const BiasArgs &b, const int32_t *edges)
+    {
+        ++at;
+        low = top + 1;
+        top = at < b.buckets - 1 ? edges[at] - 1 : INT32_MAX;
+    }
+    __device__ inline void seek(const BiasArgs &b, const int32_t *edges, int d)
+    {
+        const int one[1] = {d};
+        int found[1];
+        look_up<1>(b, edges, one, found);
+        at = found[0];
+        low = at ? edges[at - 1] : INT32_MIN;
+        top = at < b.buckets - 1 ? edges[at] - 1 : INT32_MAX;
+    }
+    __device__ inline void to(const BiasArgs &b, const int32_t *edges, int d)
+    {
+        if (d > top && low <= top) up(b, edges);
+        if (d > top || d < low) seek(b, edges, d);
+    }
+};
+
+// The buckets that a thread meets in 32 columns: at, .. at + n.  kMost edges at most are kept as thresholds: column position p is beyond edge k
+// where p > limit[k] (kKey: p < limit[k]); n > kMost: there are more.  A limit of a bucket that is not met is never passed.
+constexpr int kMost = 3;
+template <bool kKey> struct Span {
+    int at, n, limit[kMost];
+    __device__ inline void find(const BiasArgs &b, const int32_t *edges, const int2 &range, int own, Bucket &s)
+    {
+        n = 0;
+        at = s.at;
 #pragma unroll
-            for (int i = 0; i < 32; i += 2) {
-                const float2 x = __ffma2_rn(pair_of(v[i], v[i + 1]), make_float2(c1, c1), make_float2(t, t));
-                v[i] = __float_as_uint(x.x);
-                v[i + 1] = __float_as_uint(x.y);
+        for (int k = 0; k < kMost; ++k) limit[k] = kKey ? INT32_MIN : INT32_MAX;
+        if (range.x > range.y) return;                   // no column counts
+        const int near = distance<kKey>(own, kKey ? range.y : range.x), far = distance<kKey>(own, kKey ? range.x : range.y);
+        s.to(b, edges, near);
+        at = s.at;
+#pragma unroll
+        for (int k = 0; k < kMost; ++k)
+            if (far > s.top) {
+                limit[k] = kKey ? own - s.top : own + s.top;      // a column lies on either side, so it is a position
+                ++n;
+                s.up(b, edges);
             }
-            return;
+        if (far > s.top) {
+            s.seek(b, edges, far);
+            n = s.at - at;
         }
+    }
+    __device__ inline bool beyond(int k, int p) const { return kKey ? p < limit[k] : p > limit[k]; }
+};
+
+// What a tile's scores are to be multiplied by and what is to be added to them
+struct Scale {
+    float factor, add;
+};
+
+// Biases of 32 N columns of a thread's row (kKey: key) from column 32 c0 of a tile on, whose products are at taddr.  Where they are one number
+// for every row of the warp it is returned with c1, else the products are replaced by scores in powers of two.  table: of the row's head, or
+// (kKey) of the key head's first, g0 the first column's head of the group.  All lanes of a warp take one way.
+template <bool kKey, int N>
+__device__ inline Scale add_bias(uint32_t taddr, float c1, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c0, const float *table, int own,
+                                 Bucket &bucket, int group, int g0)
+{
+    const int32_t *edges = sh.edges;
+    if (!kKey || group == 1) {
+        const int4 h = sh.halves[slot];
+        const int2 r = N == 4 ? make_int2(min(h.x, h.z), max(h.y, h.w)) : (c0 ? make_int2(h.z, h.w) : make_int2(h.x, h.y));
+        Bucket s = bucket;
+        bool one = true;
+        if (r.x <= r.y) {
+            s.to(b, edges, distance<kKey>(own, kKey ? r.y : r.x));
+            one = distance<kKey>(own, kKey ? r.x : r.y) <= s.top;
+        }
+        if (__all_sync(0xFFFFFFFFu, one)) {
+            bucket = s;
+            return Scale{c1, table[s.at]};
+        }
+    }
+    const float2 scale2 = make_float2(c1, c1);
+    int g = g0;
+#pragma unroll 1
+    for (int c = 0; c < N; ++c) {
+        Span<kKey> s;
+        s.find(b, edges, sh.range[slot][c0 + c], own, bucket);
+        const bool many = __any_sync(0xFFFFFFFFu, s.n > kMost), two = __any_sync(0xFFFFFFFFu, s.n > 1);
+        const int32_t *pos = sh.pos[slot] + (c0 + c) * 32;
+        const uint32_t at = taddr + c * 32;
+        if (many || (kKey && group > 1)) {
+#pragma unroll 1
+            for (int i = 0; i < 32; i += 8) {
+                uint32_t v[8];
+                __syncwarp();
+                tmem_load8_async(at + i, v);
+                tmem_load_wait();
+                int d[8], at8[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) d[k] = distance<kKey>(own, pos[i + k]);
+                if (many) {
+                    look_up<8>(b, edges, d, at8);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) at8[k] = s.at + s.beyond(0, pos[i + k]) + s.beyond(1, pos[i + k]) + s.beyond(2, pos[i + k]);
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    v[k] = __float_as_uint(fmaf(__uint_as_float(v[k]), c1, table[(kKey ? g * b.buckets : 0) + at8[k]]));
+                    if (kKey) g = g + 1 == group ? 0 : g + 1;
+                }
+                __syncwarp();
+                tmem_store8(at + i, v);
+            }
+            continue;
+        }
+        const float t0 = table[s.at], t1 = table[s.at + min(s.n, 1)], t2 = table[s.at + min(s.n, 2)], t3 = table[s.at + min(s.n, 3)];
+        uint32_t v[32];
+        __syncwarp();
+        tmem_load32_async(at, v);
+        tmem_load_wait();
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
-            const int4 p = *reinterpret_cast<const int4 *>(pos + i);
-            const int d[4] = {distance<kKey>(own, p.x), distance<kKey>(own, p.y), distance<kKey>(own, p.z), distance<kKey>(own, p.w)};
-            float w[4] = {t, t, t, t};
-            for (int e = lo; e < hi; ++e) {
-                const int edge = edges[e];
-                const float next = table[e + 1];
+            const int4 p4 = *reinterpret_cast<const int4 *>(pos + i);
+            const int p[4] = {p4.x, p4.y, p4.z, p4.w};
+            float w[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = d[k] >= edge ? next : w[k];
+            for (int k = 0; k < 4; ++k) w[k] = s.beyond(0, p[k]) ? t1 : t0;
+            if (two)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) w[k] = s.beyond(2, p[k]) ? t3 : (s.beyond(1, p[k]) ? t2 : w[k]);
+#pragma unroll
+            for (int k = 0; k < 4; k += 2) {
+                const float2 x = __ffma2_rn(pair_of(v[i + k], v[i + k + 1]), scale2, make_float2(w[k], w[k + 1]));
+                v[i + k] = __float_as_uint(x.x);
+                v[i + k + 1] = __float_as_uint(x.y);
             }
-#pragma unroll
-            for (int k = 0; k < 4; ++k) v[i + k] = __float_as_uint(fmaf(__uint_as_float(v[i + k]), c1, w[k]));
         }
-        return;
+        __syncwarp();
+        tmem_store32(at, v);
     }
-    int g = g0;
-#pragma unroll
-    for (int i = 0; i < 32; i += 4) {
-        const int4 p = *reinterpret_cast<const int4 *>(pos + i);
-        const int d[4] = {distance<kKey>(own, p.x), distance<kKey>(own, p.y), distance<kKey>(own, p.z), distance<kKey>(own, p.w)};
-        int at[4] = {lo, lo, lo, lo};
-        for (int e = lo; e < hi; ++e) {
-            const int edge = edges[e];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) at[k] += d[k] >= edge;
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            v[i + k] = __float_as_uint(fmaf(__uint_as_float(v[i + k]), c1, table[g * b.buckets + at[k]]));
-            g = g + 1 == group ? 0 : g + 1;
-        }
-    }
+    tmem_store_wait();
+    __syncwarp();
+    return Scale{1.f, 0.f};
 }
 
 // Sums of dS by bucket and head of the group, of one warp: bins [buckets x group].  Rows of a warp follow one another, so lane i has head
@@ -367,36 +471,87 @@ __device__ inline void add_to_bin(float *bins, int bucket, int group, int g0, fl
         if (lane < group) bins[bucket * group + (g >= group ? g - group : g)] += sum;
     }
 }
-// The dS of a thread's row in 32 columns.  run, cur: sum of the bucket that the warp is in, kept in registers until it leaves it.
-__device__ inline void bin_columns(float *bins, const BiasArgs &b, const int32_t *edges, const int32_t *pos, const int2 &range, const float *ds, int own,
-                                   int lo, int hi, bool live, int group, int g0, float &run, int &cur, int lane)
+// The dS of a thread's row in the 64 columns of half q of a tile.  run, cur: sum of the bucket that the warp is in, kept in registers until it
+// leaves it.  Every bucket is summed up by itself (as differences of sums of what lies beyond its edges, a bucket of few pairs had the
+// rounding of all).
+__device__ inline void bin_columns(float *bins, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int q, const float (&ds)[64], int own, Bucket &bucket,
+                                   bool live, int group, int g0, float &run, int &cur, int lane)
 {
-    if (range.x > range.y) return;                       // no key is seen
-    float2 s2 = make_float2(0.f, 0.f);
+    const int4 h = sh.halves[slot];
+    const int2 all = q ? make_int2(h.z, h.w) : make_int2(h.x, h.y);
+    if (all.x > all.y) return;                           // no key is seen
+    const int32_t *edges = sh.edges;
+    Bucket at = bucket;
+    at.to(b, edges, apart(all.x, own));
+    const bool one = __all_sync(0xFFFFFFFFu, apart(all.y, own) <= at.top);
+#pragma unroll 1
+    for (int c = 0; c < 2; ++c) {
+        float x[32];
+        Span<false> s;
+        if (one) {
 #pragma unroll
-    for (int i = 0; i < 32; i += 2) s2 = __fadd2_rn(s2, make_float2(ds[i], ds[i + 1]));
-    float all = live ? s2.x + s2.y : 0.f;
-    const int first = __reduce_min_sync(0xFFFFFFFFu, lo), last = __reduce_max_sync(0xFFFFFFFFu, hi);
-    if (first != cur || first != last) {
-        if (cur >= 0) add_to_bin(bins, cur, group, g0, run, lane);
-        run = 0.f;
-        cur = first == last ? first : -1;
-    }
-    if (first == last) {
-        run += all;
-        return;
-    }
-    for (int e = first; e <= last; ++e) {
-        const int from = e == first ? INT32_MIN : edges[e - 1], to = e == last ? INT32_MAX : edges[e] - 1;
-        float s = 0.f;
+            for (int i = 0; i < 32; ++i) x[i] = ds[i] + ds[32 + i];
+            s.at = at.at;
+            s.n = 0;
+            bucket = at;
+        } else {
 #pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            const int4 p = *reinterpret_cast<const int4 *>(pos + i);
-            const int d[4] = {apart(p.x, own), apart(p.y, own), apart(p.z, own), apart(p.w, own)};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) s += d[k] >= from && d[k] <= to ? ds[i + k] : 0.f;
+            for (int i = 0; i < 32; ++i) x[i] = c ? ds[32 + i] : ds[i];
+            const int2 range = sh.range[slot][q * 2 + c];
+            if (range.x > range.y) continue;
+            s.find(b, edges, range, own, bucket);
         }
-        add_to_bin(bins, e, group, g0, live ? s : 0.f, lane);
+        const int32_t *pos = sh.pos[slot] + q * 64 + c * 32;
+        const int most = __reduce_max_sync(0xFFFFFFFFu, s.n), first = __reduce_min_sync(0xFFFFFFFFu, s.at), last = __reduce_max_sync(0xFFFFFFFFu, s.at + s.n);
+        if (first != cur || first != last) {
+            if (cur >= 0) add_to_bin(bins, cur, group, g0, run, lane);
+            run = 0.f;
+            cur = first == last ? first : -1;
+        }
+        float sums[kMost + 1] = {};
+        if (most == 0) {
+            float2 s2 = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) s2 = __fadd2_rn(s2, make_float2(x[i], x[i + 1]));
+            sums[0] = live ? s2.x + s2.y : 0.f;
+        } else if (most <= kMost) {
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                const int4 p4 = *reinterpret_cast<const int4 *>(pos + i);
+                const int p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const bool b0 = s.beyond(0, p[k]), b1 = s.beyond(1, p[k]), b2 = s.beyond(2, p[k]);
+                    if (!b0) sums[0] += x[i + k];
+                    if (b0 && !b1) sums[1] += x[i + k];
+                    if (b1 && !b2) sums[2] += x[i + k];
+                    if (b2) sums[3] += x[i + k];
+                }
+            }
+        }
+        if (first == last) {
+            run += sums[0];
+        } else {
+#pragma unroll 1
+            for (int e = first; e <= last; ++e) {
+                float v = 0.f;
+                if (most <= kMost) {
+                    const int k = e - s.at;
+                    v = k == 0 ? sums[0] : k == 1 ? sums[1] : k == 2 ? sums[2] : k == 3 ? sums[3] : 0.f;
+                } else {
+                    const int from = e == first ? INT32_MIN : edges[e - 1], to = e == last ? INT32_MAX : edges[e] - 1;
+#pragma unroll
+                    for (int i = 0; i < 32; i += 4) {
+                        const int4 p = *reinterpret_cast<const int4 *>(pos + i);
+                        const int d[4] = {apart(p.x, own), apart(p.y, own), apart(p.z, own), apart(p.w, own)};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) v += d[k] >= from && d[k] <= to ? x[i + k] : 0.f;
+                    }
+                }
+                add_to_bin(bins, e, group, g0, live ? v : 0.f, lane);
+            }
+        }
+        if (one) break;
     }
 }
 
@@ -656,7 +811,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
         const uint32_t s_addr = tmem + lanes + q * kTile, o_addr = tmem_o + lanes + q * 64 * NB;
-        const float c1 = a.scale * kLog2e, c2 = kBias ? 1.f : c1;      // c2: of what the scores are once they have their bias
+        const float c1 = a.scale * kLog2e, c2 = kBias ? 1.f : c1;      // c2: of the maximum, which has its bias
         const int heads = a.kv_heads * a.group;
         uint32_t jj = 0, sc = 0, oc = 0;
         bool ok = true;
@@ -671,6 +826,8 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 float m = -INFINITY, l = 0.f;
                 int pos_q = 0;
                 const float *table = table_s;
+                Bucket bucket;
+                bucket.unknown();
                 if constexpr (kBias) {
                     int64_t row;
                     int head;
@@ -686,19 +843,12 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                     for (int c = 0; c < 4; ++c) word[c] = words[jj % kWordRing][c];
                     // the row's 128 scores stay in registers; four chains for the maximum
+                    Scale scale{c1, 0.f};
+                    if constexpr (kBias) scale = add_bias<false, 4>(s_addr, c1, a.bias, bias_s, jj % kWordRing, 0, table, pos_q, bucket, 1, 0);
                     uint32_t v[4][32];
-                    int lo[4], hi[4];
-                    if constexpr (kBias) {
-                        spans<4, false>(a.bias, bias_s.edges, bias_s.range[jj % kWordRing], pos_q, lo, hi);
-                        __syncwarp();                        // the loads of tensor memory are for a converged warp
-                    }
 #pragma unroll
                     for (int c = 0; c < 4; ++c) tmem_load32_async(s_addr + c * 32, v[c]);
                     tmem_load_wait();
-                    if constexpr (kBias)
-#pragma unroll
-                        for (int c = 0; c < 4; ++c)
-                            add_bias<false>(v[c], c1, a.bias, bias_s.edges, table, bias_s.pos[jj % kWordRing] + c * 32, pos_q, lo[c], hi[c], 1, 0);
                     float tops[4];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -711,7 +861,8 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 #pragma unroll
                         for (int i = 1; i < 32; ++i) tops[c] = fmaxf(tops[c], __uint_as_float(v[c][i]));
                     }
-                    const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                    float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+                    if constexpr (kBias) top = fmaf(top, scale.factor, scale.add);
                     // The maximum that p and l refer to moves only where a score exceeds it by 8 in the exponent: p <= 2^8 loses
                     // nothing in floating point, and the sums so far are rescaled seldom.
                     const bool moves = top * c2 > m * c2 + 8.f || m == -INFINITY;
@@ -731,7 +882,8 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (moves) m = top;
                     const float base = m == -INFINITY ? 0.f : m * c2;
                     if constexpr (kBias) __syncwarp();       // the stores to tensor memory are for a converged warp
-                    const float2 scale2 = make_float2(c2, c2), base2 = make_float2(-base, -base);
+                    const float factor = kBias ? scale.factor : c1, add = kBias ? scale.add - base : -base;
+                    const float2 scale2 = make_float2(factor, factor), base2 = make_float2(add, add);
                     float2 sums[4];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
@@ -1086,7 +1238,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         // ---- p and dS: 64 columns of one row per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
-        const float c1 = a.scale * kLog2e, c2 = kBias ? 1.f : c1;
+        const float c1 = a.scale * kLog2e;
         const int heads = a.kv_heads * a.group;
         uint32_t jj = 0, item = 0, corrected = 0, binned = 0;
         bool ok = true;
@@ -1118,6 +1270,9 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 }
                 float rest = 0.f, run = 0.f;
                 int pos_q = 0, cur = -1;
+                Bucket bucket, place_of;                 // of the scores, of the sums by bucket
+                bucket.unknown();
+                place_of.unknown();
                 const int g0 = kBias ? (int)((t * kTile + w * 32) % a.group) : 0;
                 const float *table = table_s;
                 if constexpr (kBias) {
@@ -1125,28 +1280,24 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     table += head * a.bias.buckets;
                 }
                 for (int j = 0; j < steps; ++j, ++jj) {
-                    int lo[2], hi[2];
+                    if (j == first) bucket.unknown();
                     ok = warp_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
                     if (!ok) break;
                     tc_fence_after();
                     float p[64];
                     {
+                        Scale scale{c1, 0.f};
+                        if constexpr (kBias)
+                            scale = add_bias<false, 2>(tmem + lanes + (jj & 1u) * kTile + q * 64, c1, a.bias, bias_s, jj % kWordRing, q * 2, table, pos_q,
+                                                       bucket, 1, 0);
+                        const float factor = kBias ? scale.factor : c1, add = kBias ? scale.add - base : -base;
                         uint32_t v[2][32];
-                        if constexpr (kBias) {
-                            spans<2, false>(a.bias, bias_s.edges, bias_s.range[jj % kWordRing] + q * 2, pos_q, lo, hi);
-                            __syncwarp();                    // the loads of tensor memory are for a converged warp
-                        }
                         tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64, v[0]);
                         tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64 + 32, v[1]);
                         tmem_load_wait();
-                        if constexpr (kBias) {
-#pragma unroll
-                            for (int c = 0; c < 2; ++c)
-                                add_bias<false>(v[c], c1, a.bias, bias_s.edges, table, bias_s.pos[jj % kWordRing] + q * 64 + c * 32, pos_q, lo[c], hi[c], 1, 0);
-                        }
 #pragma unroll
                         for (int e = 0; e < 64; e += 2) {
-                            const float2 y = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(c2, c2), make_float2(-base, -base)));
+                            const float2 y = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(factor, factor), make_float2(add, add)));
                             p[e] = y.x;
                             p[e + 1] = y.y;
                         }
@@ -1217,10 +1368,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     }
                     if constexpr (kBias)
                         if (table_part) {
-#pragma unroll
-                            for (int c = 0; c < 2; ++c)
-                                bin_columns(bins, a.bias, bias_s.edges, bias_s.pos[jj % kWordRing] + q * 64 + c * 32, bias_s.range[jj % kWordRing][q * 2 + c],
-                                            p + c * 32, pos_q, lo[c], hi[c], live && base != INFINITY, a.group, g0, run, cur, lane);
+                            bin_columns(bins, a.bias, bias_s, jj % kWordRing, q, p, pos_q, place_of, live && base != INFINITY, a.group, g0, run, cur, lane);
                             __syncwarp();
                         }
                     store_operand_and_rest(tmem + lanes + 256 + q * 64, tmem + lanes + (jj & 1u) * kTile + q * 64, p);
@@ -1497,7 +1645,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         // ---- p and dS: 64 columns (rows of Q) of one key per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
-        const float c1 = a.scale * kLog2e, c2 = kBias ? 1.f : c1;
+        const float c1 = a.scale * kLog2e;
         uint32_t jj = 0, item = 0;
         bool ok = true;
         for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
@@ -1508,6 +1656,8 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const int64_t key = x.kb + t * kTile + w * 32 + lane;
                 const bool live = key < x.ke, seen = live && (!a.mask || a.mask[key]);
                 int pos_k = 0;
+                Bucket bucket;
+                bucket.unknown();
                 if constexpr (kBias)
                     if (live) pos_k = pos_of(a.bias.pos_k, key, x.rg.k0);
                 for (int j = 0; j < n; ++j, ++jj) {
@@ -1518,28 +1668,26 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     const float4 *dot4 = reinterpret_cast<const float4 *>(stat_dot[jj % kWordRing] + q * 64);
                     float p[64];
                     {
-                        uint32_t v[2][32];
-                        int lo[2], hi[2];
+                        Scale scale{c1, 0.f};
                         if constexpr (kBias) {
-                            spans<2, true>(a.bias, bias_s.edges, bias_s.range[jj % kWordRing] + q * 2, pos_k, lo, hi);
-                            __syncwarp();                    // the loads of tensor memory are for a converged warp
+                            const int g0 = a.group == 1 ? 0 : (int)(((int64_t)j * kTile + q * 64) % a.group);
+                            scale = add_bias<true, 2>(tmem + lanes + q * 64, c1, a.bias, bias_s, jj % kWordRing, q * 2,
+                                                      table_s + x.h * a.group * a.bias.buckets, pos_k, bucket, a.group, g0);
                         }
+                        const float2 factor = make_float2(scale.factor, scale.factor), add = make_float2(scale.add, scale.add);
+                        uint32_t v[2][32];
                         tmem_load32_async(tmem + lanes + q * 64, v[0]);
                         tmem_load32_async(tmem + lanes + q * 64 + 32, v[1]);
                         tmem_load_wait();
-                        if constexpr (kBias) {
-#pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                const int at = q * 64 + c * 32, g0 = a.group == 1 ? 0 : (int)(((int64_t)j * kTile + at) % a.group);
-                                add_bias<true>(v[c], c1, a.bias, bias_s.edges, table_s + x.h * a.group * a.bias.buckets, bias_s.pos[jj % kWordRing] + at, pos_k,
-                                               lo[c], hi[c], a.group, g0);
-                            }
-                        }
 #pragma unroll
                         for (int e = 0; e < 64; e += 4) {
-                            const float4 l = lse4[e / 4];            // negated, as the sums of products below
-                            const float2 y0 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(c2, c2), make_float2(l.x, l.y)));
-                            const float2 y1 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][(e & 31) + 2], v[e >> 5][(e & 31) + 3]), make_float2(c2, c2), make_float2(l.z, l.w)));
+                            float4 l = lse4[e / 4];                  // negated, as the sums of products below
+                            if constexpr (kBias) {
+                                const float2 l0 = __fadd2_rn(make_float2(l.x, l.y), add), l1 = __fadd2_rn(make_float2(l.z, l.w), add);
+                                l = make_float4(l0.x, l0.y, l1.x, l1.y);
+                            }
+                            const float2 y0 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), factor, make_float2(l.x, l.y)));
+                            const float2 y1 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][(e & 31) + 2], v[e >> 5][(e & 31) + 3]), factor, make_float2(l.z, l.w)));
                             p[e] = y0.x;
                             p[e + 1] = y0.y;
                             p[e + 2] = y1.x;
