@@ -236,17 +236,20 @@ struct Visible {
 };
 
 // ---- Bias by distance.  Buckets are monotone in the distance, so the lowest and the highest position of neighbouring columns give the buckets
-// that a thread's row (or key) meets in them.  Where that is one for a whole tile, its bias goes into the exponent's argument and costs
-// nothing per score.  Else the scores get their biases in tensor memory, 32 columns at a time: one bucket, or a few with the edges between
-// them, each a threshold that the columns' positions are compared with; where they are more than four (close to the diagonal), every score
-// looks its bucket up.  Positions need not be sorted for that, but where they are the next columns' bucket is the last one's or its neighbour.
-// What decides is the code's size: with the scores' biases in the registers that hold a row of 128 scores, four copies of it, the forward pass of
-// 8 x 2048 x 2048 took 690 us, 5 of 6 stalls for instructions.
+// that a thread's row (or key) meets in them; positions need not be sorted for that, but where they are the next columns' bucket is the last
+// one's or its neighbour.  One bucket for a whole tile: its bias goes into the exponent's argument and costs nothing per score.  Two in 32
+// columns: the edge between them is a threshold that the columns' positions are compared with.  More (close to the diagonal): every score looks
+// its bucket up, in a table of the distances up to kNear, or by bisection, and gets its bias in tensor memory beforehand.  The buckets are found while the
+// tile's products are on their way: positions are there a tile ahead.
+// What decides is latency and the code's size.  Forward pass of 8 x 2048 x 2048, heads of 128 (123 us without a bias): 690 us with all ways in the
+// registers that hold a row of 128 scores (stalls for instructions), 270 with biases in tensor memory, 32 columns after 32.
+constexpr int kNear = 2048;
 struct BiasShared {
     int32_t pos[kWordRing][kTile];                   // of the tile's columns: keys (forward pass, dQ), rows of Q (dK, dV)
     int2 range[kWordRing][4];                        // lowest and highest of each 32 columns that count; lowest > highest: none
     int4 halves[kWordRing];                          // the same of each 64
     int32_t edges[kMaxBuckets];                      // beyond the last: the highest number
+    uint8_t near[2 * kNear];                         // buckets of the distances -kNear .. kNear - 1
 };
 struct NoBiasShared {};
 template <bool kBias> using BiasShared_ = typename std::conditional<kBias, BiasShared, NoBiasShared>::type;
@@ -273,16 +276,39 @@ __device__ inline void place(BiasShared &s, uint32_t slot, const int (&pos)[4], 
     if (lane == 0) s.halves[slot] = make_int4(min(r[0].x, r[1].x), max(r[0].y, r[1].y), min(r[2].x, r[3].x), max(r[2].y, r[3].y));
     __syncwarp();
 }
-// the keys' positions, a tile ahead as Visible's words
-struct KeyPlaces {
-    int next[4];
-    __device__ inline void ahead(const AttnArgs &a, const Work &x, int j, int lane)
+// The positions of keys, by the copying warp: those of tile j + 1 are written before the copies of tile j are announced, so whoever has seen a tile's
+// scores can read the next one's.  `steps` tiles in all; loads go out a tile before that.
+struct Ahead {
+    uint32_t seen[4];                                    // of the tile after the one that is copied
+    int pos[4];
+    __device__ inline void fetch(const AttnArgs &a, const Work &x, int tile, int lane)
     {
 #pragma unroll
         for (int b = 0; b < 4; ++b) {
-            const int64_t key = x.kb + (int64_t)j * kTile + b * 32 + lane;
-            next[b] = key < x.ke ? (a.bias.pos_k ? load_now(a.bias.pos_k + key) : (int)(key - x.rg.k0)) : 0;
+            const int64_t key = x.kb + (int64_t)tile * kTile + b * 32 + lane;
+            seen[b] = key < x.ke ? (a.mask ? load_now(a.mask + key) : 1u) : 0u;
+            pos[b] = key < x.ke ? (a.bias.pos_k ? load_now(a.bias.pos_k + key) : (int)(key - x.rg.k0)) : 0;
         }
+    }
+    __device__ inline void put(BiasShared &s, uint32_t slot, int lane) const
+    {
+        uint32_t word[4];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) word[b] = __ballot_sync(0xFFFFFFFFu, seen[b] != 0);
+        place(s, slot, pos, word, lane);
+    }
+    // tile jj begins a walk over `steps` tiles (its places were read eight tiles ago)
+    __device__ inline void begin(const AttnArgs &a, const Work &x, BiasShared &s, int steps, uint32_t jj, int lane)
+    {
+        fetch(a, x, 0, lane);
+        put(s, jj % kWordRing, lane);
+        if (steps > 1) fetch(a, x, x.n > 1 ? 1 : 0, lane);
+    }
+    // step j is about to be copied; next: the tile of step j + 2, or -1
+    __device__ inline void step(const AttnArgs &a, const Work &x, BiasShared &s, int j, int next, int steps, uint32_t jj, int lane)
+    {
+        if (j + 1 < steps) put(s, (jj + 1) % kWordRing, lane);
+        if (next >= 0) fetch(a, x, next, lane);
     }
 };
 
@@ -328,127 +354,200 @@ struct Bucket {
     }
 };
 
-// The buckets that a thread meets in 32 columns: at, .. at + n.  kMost edges at most are kept as thresholds: column position p is beyond edge k
-// where p > limit[k] (kKey: p < limit[k]); n > kMost: there are more.  A limit of a bucket that is not met is never passed.
+// The buckets of near distances, by the 32 W threads of W warps that have nothing else to do while the first tiles are on their way; the edges
+// are there.  A barrier of their own.
+template <int W> __device__ inline void stage_near(const BiasArgs &b, BiasShared &sh)
+{
+    for (int i0 = threadIdx.x * 8; i0 < 2 * kNear; i0 += W * 32 * 8) {
+        int d[8], at[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) d[k] = i0 + k - kNear;
+        look_up<8>(b, sh.edges, d, at);
+        *reinterpret_cast<uint2 *>(sh.near + i0) = make_uint2(at[0] | at[1] << 8 | at[2] << 16 | at[3] << 24, at[4] | at[5] << 8 | at[6] << 16 | at[7] << 24);
+    }
+    asm volatile("bar.sync 1, %0;" ::"n"(W * 32) : "memory");
+}
+
+// The buckets that a thread meets in 32 columns: at .. at + n.  Up to three edges are thresholds: a column's position p is beyond edge k where
+// p > limit[k] (kKey: p < limit[k]); a limit of a bucket that is not met is never passed.
 constexpr int kMost = 3;
 template <bool kKey> struct Span {
     int at, n, limit[kMost];
+    bool away;                                           // further than kNear from a column
     __device__ inline void find(const BiasArgs &b, const int32_t *edges, const int2 &range, int own, Bucket &s)
     {
         n = 0;
-        at = s.at;
 #pragma unroll
         for (int k = 0; k < kMost; ++k) limit[k] = kKey ? INT32_MIN : INT32_MAX;
+        at = s.at;
+        away = false;
         if (range.x > range.y) return;                   // no column counts
         const int near = distance<kKey>(own, kKey ? range.y : range.x), far = distance<kKey>(own, kKey ? range.x : range.y);
+        away = near < -kNear || far >= kNear;
         s.to(b, edges, near);
         at = s.at;
 #pragma unroll
         for (int k = 0; k < kMost; ++k)
             if (far > s.top) {
                 limit[k] = kKey ? own - s.top : own + s.top;      // a column lies on either side, so it is a position
-                ++n;
                 s.up(b, edges);
             }
-        if (far > s.top) {
-            s.seek(b, edges, far);
-            n = s.at - at;
-        }
+        if (far > s.top) s.seek(b, edges, far);
+        n = s.at - at;
     }
     __device__ inline bool beyond(int k, int p) const { return kKey ? p < limit[k] : p > limit[k]; }
 };
 
-// What a tile's scores are to be multiplied by and what is to be added to them
-struct Scale {
-    float factor, add;
-};
-
-// Biases of 32 N columns of a thread's row (kKey: key) from column 32 c0 of a tile on, whose products are at taddr.  Where they are one number
-// for every row of the warp it is returned with c1, else the products are replaced by scores in powers of two.  table: of the row's head, or
-// (kKey) of the key head's first, g0 the first column's head of the group.  All lanes of a warp take one way.
-template <bool kKey, int N>
-__device__ inline Scale add_bias(uint32_t taddr, float c1, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c0, const float *table, int own,
-                                 Bucket &bucket, int group, int g0)
-{
-    const int32_t *edges = sh.edges;
-    if (!kKey || group == 1) {
+// The buckets of 32 N columns of a thread's row (kKey: key), from column 32 c0 of a tile on.  Loops over the columns' 32s stay loops, their
+// results are put in place by selection.
+template <bool kKey, int N> struct TileSpans {
+    Span<kKey> s[N];
+    int at;                                              // `one`: the bucket
+    uint32_t two, more, many, apart;                     // a bit per 32 columns: some lane meets two buckets and more in them, three, over four;
+                                                         // is further than kNear from one of them
+    bool one;                                            // every lane meets one bucket in the tile
+    // alive: the warp has a row (key) that counts
+    __device__ inline void find(const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c0, int own, bool alive, Bucket &bucket)
+    {
+        at = 0;
+        one = true;
+        if (!alive) return;
         const int4 h = sh.halves[slot];
         const int2 r = N == 4 ? make_int2(min(h.x, h.z), max(h.y, h.w)) : (c0 ? make_int2(h.z, h.w) : make_int2(h.x, h.y));
-        Bucket s = bucket;
-        bool one = true;
+        Bucket next = bucket;
+        bool mine = true;
+        two = more = many = apart = 0;
         if (r.x <= r.y) {
-            s.to(b, edges, distance<kKey>(own, kKey ? r.y : r.x));
-            one = distance<kKey>(own, kKey ? r.x : r.y) <= s.top;
+            next.to(b, sh.edges, distance<kKey>(own, kKey ? r.y : r.x));
+            mine = distance<kKey>(own, kKey ? r.x : r.y) <= next.top;
         }
-        if (__all_sync(0xFFFFFFFFu, one)) {
-            bucket = s;
-            return Scale{c1, table[s.at]};
+        at = next.at;
+        one = __all_sync(0xFFFFFFFFu, mine);
+        if (one) {
+            bucket = next;
+            return;
+        }
+#pragma unroll 1
+        for (int c = 0; c < N; ++c) {
+            Span<kKey> x;
+            x.find(b, sh.edges, sh.range[slot][c0 + c], own, bucket);
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (c == k) s[k] = x;
+            two |= __any_sync(0xFFFFFFFFu, x.n > 0) ? 1u << c : 0u;
+            more |= __any_sync(0xFFFFFFFFu, x.n > 1) ? 1u << c : 0u;
+            many |= __any_sync(0xFFFFFFFFu, x.n > kMost) ? 1u << c : 0u;
+            apart |= __any_sync(0xFFFFFFFFu, x.away) ? 1u << c : 0u;
         }
     }
-    const float2 scale2 = make_float2(c1, c1);
-    int g = g0;
-#pragma unroll 1
-    for (int c = 0; c < N; ++c) {
-        Span<kKey> s;
-        s.find(b, edges, sh.range[slot][c0 + c], own, bucket);
-        const bool many = __any_sync(0xFFFFFFFFu, s.n > kMost), two = __any_sync(0xFFFFFFFFu, s.n > 1);
-        const int32_t *pos = sh.pos[slot] + (c0 + c) * 32;
-        const uint32_t at = taddr + c * 32;
-        if (many || (kKey && group > 1)) {
-#pragma unroll 1
-            for (int i = 0; i < 32; i += 8) {
-                uint32_t v[8];
-                __syncwarp();
-                tmem_load8_async(at + i, v);
-                tmem_load_wait();
-                int d[8], at8[8];
+    __device__ inline Span<kKey> of(int c) const
+    {
+        Span<kKey> x = s[0];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) d[k] = distance<kKey>(own, pos[i + k]);
-                if (many) {
-                    look_up<8>(b, edges, d, at8);
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) at8[k] = s.at + s.beyond(0, pos[i + k]) + s.beyond(1, pos[i + k]) + s.beyond(2, pos[i + k]);
-                }
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    v[k] = __float_as_uint(fmaf(__uint_as_float(v[k]), c1, table[(kKey ? g * b.buckets : 0) + at8[k]]));
-                    if (kKey) g = g + 1 == group ? 0 : g + 1;
-                }
-                __syncwarp();
-                tmem_store8(at + i, v);
-            }
-            continue;
-        }
-        const float t0 = table[s.at], t1 = table[s.at + min(s.n, 1)], t2 = table[s.at + min(s.n, 2)], t3 = table[s.at + min(s.n, 3)];
-        uint32_t v[32];
-        __syncwarp();
-        tmem_load32_async(at, v);
-        tmem_load_wait();
-#pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            const int4 p4 = *reinterpret_cast<const int4 *>(pos + i);
-            const int p[4] = {p4.x, p4.y, p4.z, p4.w};
-            float w[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) w[k] = s.beyond(0, p[k]) ? t1 : t0;
-            if (two)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) w[k] = s.beyond(2, p[k]) ? t3 : (s.beyond(1, p[k]) ? t2 : w[k]);
-#pragma unroll
-            for (int k = 0; k < 4; k += 2) {
-                const float2 x = __ffma2_rn(pair_of(v[i + k], v[i + k + 1]), scale2, make_float2(w[k], w[k + 1]));
-                v[i + k] = __float_as_uint(x.x);
-                v[i + k + 1] = __float_as_uint(x.y);
-            }
-        }
-        __syncwarp();
-        tmem_store32(at, v);
+        for (int k = 1; k < N; ++k)
+            if (c == k) x = s[k];
+        return x;
     }
-    tmem_store_wait();
-    __syncwarp();
-    return Scale{1.f, 0.f};
-}
+    // 32 products, of column 32 c and on -> scores in powers of two with their biases; apart_at() is false.  table: of the row's head
+    __device__ inline void add_to(uint32_t (&v)[32], int c, float c1, const BiasShared &sh, uint32_t slot, int c0, int own, const float *table) const
+    {
+        const int4 *pos = reinterpret_cast<const int4 *>(sh.pos[slot] + (c0 + c) * 32);
+        const float2 scale2 = make_float2(c1, c1);
+        auto put = [&](int i, float t0, float t1) {
+            const float2 x = __ffma2_rn(pair_of(v[i], v[i + 1]), scale2, make_float2(t0, t1));
+            v[i] = __float_as_uint(x.x);
+            v[i + 1] = __float_as_uint(x.y);
+        };
+        if (!(many >> c & 1u)) {
+            const Span<kKey> x = of(c);
+            const float t0 = table[x.at], t1 = table[x.at + min(x.n, 1)];
+            if (!(more >> c & 1u)) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    const int4 p = pos[i / 4];
+                    put(i, x.beyond(0, p.x) ? t1 : t0, x.beyond(0, p.y) ? t1 : t0);
+                    put(i + 2, x.beyond(0, p.z) ? t1 : t0, x.beyond(0, p.w) ? t1 : t0);
+                }
+            } else {
+                const float t2 = table[x.at + min(x.n, 2)], t3 = table[x.at + min(x.n, 3)];
+                auto pick = [&](int p) {
+                    float w = x.beyond(0, p) ? t1 : t0;
+                    w = x.beyond(1, p) ? t2 : w;
+                    return x.beyond(2, p) ? t3 : w;
+                };
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    const int4 p = pos[i / 4];
+                    put(i, pick(p.x), pick(p.y));
+                    put(i + 2, pick(p.z), pick(p.w));
+                }
+            }
+        } else {                                         // (columns that do not count may lie anywhere)
+            auto look = [&](int p) { return table[sh.near[min((uint32_t)((kKey ? own - p : p - own) + kNear), 2u * kNear - 1)]]; };
+#pragma unroll
+            for (int i = 0; i < 32; i += 4) {
+                const int4 p = pos[i / 4];
+                put(i, look(p.x), look(p.y));
+                put(i + 2, look(p.z), look(p.w));
+            }
+        }
+    }
+    // The same in tensor memory, where buckets have to be found by bisection or every column has its own head: eight columns at a time
+    __device__ inline bool apart_at(int c, int group) const { return (kKey && group > 1) || (many & apart) >> c & 1u; }
+    __device__ inline void one_by_one(uint32_t taddr, int c, float c1, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c0, int own,
+                                      const float *table, int group, int g) const
+    {
+#pragma unroll 1
+        for (int i = 0; i < 32; i += 8) {
+            const int4 *pos = reinterpret_cast<const int4 *>(sh.pos[slot] + (c0 + c) * 32 + i);
+            const int4 p = pos[0], o = pos[1];
+            int at8[8], d[8] = {distance<kKey>(own, p.x), distance<kKey>(own, p.y), distance<kKey>(own, p.z), distance<kKey>(own, p.w),
+                                distance<kKey>(own, o.x), distance<kKey>(own, o.y), distance<kKey>(own, o.z), distance<kKey>(own, o.w)};
+            if (one) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) at8[k] = at;
+            } else if (!(apart >> c & 1u)) {
+#pragma unroll
+                for (int k = 0; k < 8; ++k) at8[k] = sh.near[min((uint32_t)(d[k] + kNear), 2u * kNear - 1)];
+            } else {
+                look_up<8>(b, sh.edges, d, at8);
+            }
+            uint32_t v[8];
+            __syncwarp();                                // tensor memory is for a converged warp
+            tmem_load8_async(taddr + i, v);
+            tmem_load_wait();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                v[k] = __float_as_uint(fmaf(__uint_as_float(v[k]), c1, table[(kKey ? g * b.buckets : 0) + at8[k]]));
+                if (kKey) g = g + 1 == group ? 0 : g + 1;
+            }
+            __syncwarp();
+            tmem_store8(taddr + i, v);
+        }
+        tmem_store_wait();
+    }
+    // The same for all products of the tile, in tensor memory
+    __device__ inline void in_place(uint32_t taddr, float c1, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c0, int own, const float *table,
+                                    int group, int g0) const
+    {
+#pragma unroll 1
+        for (int c = 0; c < N; ++c) {
+            if (apart_at(c, group)) {
+                one_by_one(taddr + c * 32, c, c1, b, sh, slot, c0, own, table, group, kKey && group > 1 ? (g0 + c * 32) % group : 0);
+                continue;
+            }
+            uint32_t v[32];
+            __syncwarp();                                // tensor memory is for a converged warp
+            tmem_load32_async(taddr + c * 32, v);
+            tmem_load_wait();
+            add_to(v, c, c1, sh, slot, c0, own, table);
+            __syncwarp();
+            tmem_store32(taddr + c * 32, v);
+        }
+        tmem_store_wait();
+        __syncwarp();
+    }
+};
 
 // Sums of dS by bucket and head of the group, of one warp: bins [buckets x group].  Rows of a warp follow one another, so lane i has head
 // (g0 + i) mod group; lanes of one head are added up in a fixed order.
@@ -471,87 +570,133 @@ __device__ inline void add_to_bin(float *bins, int bucket, int group, int g0, fl
         if (lane < group) bins[bucket * group + (g >= group ? g - group : g)] += sum;
     }
 }
+// The same for the buckets first .. first + 3 at once, of those up to `last`.  One head: lanes give away half of what they hold at each of two
+// steps, so six exchanges do for four sums.
+__device__ inline void add_to_bins(float *bins, int first, int last, int group, int g0, const float (&s)[4], int lane)
+{
+    if (group != 1) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (first + k <= last) add_to_bin(bins, first + k, group, g0, s[k], lane);
+        return;
+    }
+    const bool high = lane & 2, odd = lane & 1;
+    float a = high ? s[2] : s[0], b = high ? s[3] : s[1];
+    a += __shfl_xor_sync(0xFFFFFFFFu, high ? s[0] : s[2], 2);
+    b += __shfl_xor_sync(0xFFFFFFFFu, high ? s[1] : s[3], 2);
+    float c = odd ? b : a;
+    c += __shfl_xor_sync(0xFFFFFFFFu, odd ? a : b, 1);
+#pragma unroll
+    for (int o = 16; o >= 4; o >>= 1) c += __shfl_xor_sync(0xFFFFFFFFu, c, o);
+    __syncwarp();
+    if (lane < 4 && first + lane <= last) bins[first + lane] += c;
+}
 // The dS of a thread's row in the 64 columns of half q of a tile.  run, cur: sum of the bucket that the warp is in, kept in registers until it
 // leaves it.  Every bucket is summed up by itself (as differences of sums of what lies beyond its edges, a bucket of few pairs had the
 // rounding of all).
-__device__ inline void bin_columns(float *bins, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int q, const float (&ds)[64], int own, Bucket &bucket,
-                                   bool live, int group, int g0, float &run, int &cur, int lane)
+__device__ inline void bin_columns(float *bins, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int q, const float (&ds)[64], int own,
+                                   const TileSpans<false, 2> &spans, bool live, int group, int g0, float &run, int &cur, int lane)
 {
-    const int4 h = sh.halves[slot];
-    const int2 all = q ? make_int2(h.z, h.w) : make_int2(h.x, h.y);
-    if (all.x > all.y) return;                           // no key is seen
-    const int32_t *edges = sh.edges;
-    Bucket at = bucket;
-    at.to(b, edges, apart(all.x, own));
-    const bool one = __all_sync(0xFFFFFFFFu, apart(all.y, own) <= at.top);
+    if (!__any_sync(0xFFFFFFFFu, live)) return;
 #pragma unroll 1
     for (int c = 0; c < 2; ++c) {
         float x[32];
-        Span<false> s;
-        if (one) {
+        Span<false> s1{};
+        if (spans.one) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) x[i] = ds[i] + ds[32 + i];
-            s.at = at.at;
-            s.n = 0;
-            bucket = at;
+            s1.at = spans.at;
+            s1.n = 0;
         } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i) x[i] = c ? ds[32 + i] : ds[i];
-            const int2 range = sh.range[slot][q * 2 + c];
-            if (range.x > range.y) continue;
-            s.find(b, edges, range, own, bucket);
+            s1 = spans.of(c);
         }
         const int32_t *pos = sh.pos[slot] + q * 64 + c * 32;
-        const int most = __reduce_max_sync(0xFFFFFFFFu, s.n), first = __reduce_min_sync(0xFFFFFFFFu, s.at), last = __reduce_max_sync(0xFFFFFFFFu, s.at + s.n);
+        const bool many = !spans.one && (spans.many >> c & 1u), more = !spans.one && (spans.more >> c & 1u);
+        const int first = __reduce_min_sync(0xFFFFFFFFu, s1.at), last = __reduce_max_sync(0xFFFFFFFFu, s1.at + s1.n);
         if (first != cur || first != last) {
             if (cur >= 0) add_to_bin(bins, cur, group, g0, run, lane);
             run = 0.f;
             cur = first == last ? first : -1;
         }
-        float sums[kMost + 1] = {};
-        if (most == 0) {
-            float2 s2 = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int i = 0; i < 32; i += 2) s2 = __fadd2_rn(s2, make_float2(x[i], x[i + 1]));
-            sums[0] = live ? s2.x + s2.y : 0.f;
-        } else if (most <= kMost) {
+        float part[kMost + 1] = {};                      // by bucket from at on
+        if (more && !many) {
 #pragma unroll
             for (int i = 0; i < 32; i += 4) {
                 const int4 p4 = *reinterpret_cast<const int4 *>(pos + i);
                 const int p[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const bool b0 = s.beyond(0, p[k]), b1 = s.beyond(1, p[k]), b2 = s.beyond(2, p[k]);
-                    if (!b0) sums[0] += x[i + k];
-                    if (b0 && !b1) sums[1] += x[i + k];
-                    if (b1 && !b2) sums[2] += x[i + k];
-                    if (b2) sums[3] += x[i + k];
+                    const bool b0 = s1.beyond(0, p[k]), b1 = s1.beyond(1, p[k]), b2 = s1.beyond(2, p[k]);
+                    if (!b0) part[0] += x[i + k];
+                    if (b0 && !b1) part[1] += x[i + k];
+                    if (b1 && !b2) part[2] += x[i + k];
+                    if (b2) part[3] += x[i + k];
                 }
             }
+        } else if (!many) {
+            float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
+            if (!spans.one && (spans.two >> c & 1u)) {
+#pragma unroll
+                for (int i = 0; i < 32; i += 4) {
+                    const int4 p = *reinterpret_cast<const int4 *>(pos + i);
+                    const bool b0 = s1.beyond(0, p.x), b1 = s1.beyond(0, p.y), b2 = s1.beyond(0, p.z), b3 = s1.beyond(0, p.w);
+                    s2 = __fadd2_rn(s2, make_float2(b0 ? 0.f : x[i], b1 ? 0.f : x[i + 1]));
+                    t2 = __fadd2_rn(t2, make_float2(b0 ? x[i] : 0.f, b1 ? x[i + 1] : 0.f));
+                    s2 = __fadd2_rn(s2, make_float2(b2 ? 0.f : x[i + 2], b3 ? 0.f : x[i + 3]));
+                    t2 = __fadd2_rn(t2, make_float2(b2 ? x[i + 2] : 0.f, b3 ? x[i + 3] : 0.f));
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; i += 2) s2 = __fadd2_rn(s2, make_float2(x[i], x[i + 1]));
+            }
+            part[0] = s2.x + s2.y;
+            part[1] = t2.x + t2.y;
         }
+#pragma unroll
+        for (int k = 0; k <= kMost; ++k) part[k] = live ? part[k] : 0.f;
         if (first == last) {
-            run += sums[0];
+            run += part[0];
         } else {
 #pragma unroll 1
-            for (int e = first; e <= last; ++e) {
-                float v = 0.f;
-                if (most <= kMost) {
-                    const int k = e - s.at;
-                    v = k == 0 ? sums[0] : k == 1 ? sums[1] : k == 2 ? sums[2] : k == 3 ? sums[3] : 0.f;
+            for (int e = first; e <= last; e += 4) {
+                float s[4];
+                if (!many) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int m = e + k - s1.at;
+                        s[k] = m == 0 ? part[0] : m == 1 ? part[1] : m == 2 ? part[2] : m == 3 ? part[3] : 0.f;
+                    }
                 } else {
-                    const int from = e == first ? INT32_MIN : edges[e - 1], to = e == last ? INT32_MAX : edges[e] - 1;
+                    int top[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        s[k] = 0.f;
+                        top[k] = e + k >= last ? INT32_MAX : sh.edges[e + k] - 1;
+                    }
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
-                        const int4 p = *reinterpret_cast<const int4 *>(pos + i);
-                        const int d[4] = {apart(p.x, own), apart(p.y, own), apart(p.z, own), apart(p.w, own)};
+                        const int4 p4 = *reinterpret_cast<const int4 *>(pos + i);
+                        const int d[4] = {apart(p4.x, own), apart(p4.y, own), apart(p4.z, own), apart(p4.w, own)};
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) v += d[k] >= from && d[k] <= to ? x[i + k] : 0.f;
+                        for (int k = 0; k < 4; ++k) {                       // what is in the buckets below is gone already
+                            const float v = x[i + k];
+                            const bool b0 = d[k] <= top[0], b1 = d[k] <= top[1], b2 = d[k] <= top[2], b3 = d[k] <= top[3];
+                            if (b0) s[0] += v;
+                            if (b1 && !b0) s[1] += v;
+                            if (b2 && !b1) s[2] += v;
+                            if (b3 && !b2) s[3] += v;
+                            if (b3) x[i + k] = 0.f;
+                        }
                     }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) s[k] = live ? s[k] : 0.f;
                 }
-                add_to_bin(bins, e, group, g0, live ? v : 0.f, lane);
+                add_to_bins(bins, e, last, group, g0, s, lane);
             }
         }
-        if (one) break;
+        if (spans.one) break;
     }
 }
 
@@ -669,9 +814,9 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const Work x = work_of(a, f, u, lane == 0);
                 for (int64_t t = x.t0; t * kRows < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                     Visible seen;
-                    KeyPlaces places;
+                    Ahead places;
                     seen.ahead(a, x, 0, lane);
-                    if constexpr (kBias) places.ahead(a, x, 0, lane);
+                    if constexpr (kBias) places.begin(a, x, bias_s, x.n, jj, lane);
                     if (item > 0) ok = warp_wait(&q_empty, (item - 1) & 1u, &abort_flag);
                     if (!ok) break;
                     const int nt = NT == 2 && x.rows - t * kRows > kTile ? 2 : 1;
@@ -695,21 +840,14 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     }
                     for (int j = 0; j < x.n && ok; ++j, ++jj) {
                         uint32_t word[4];
-                        int pos[4];
                         seen.now(word);
-                        if constexpr (kBias)
-#pragma unroll
-                            for (int b = 0; b < 4; ++b) pos[b] = places.next[b];
-                        if (j + 1 < x.n) {
-                            seen.ahead(a, x, j + 1, lane);
-                            if constexpr (kBias) places.ahead(a, x, j + 1, lane);
-                        }
+                        if (j + 1 < x.n) seen.ahead(a, x, j + 1, lane);
                         for (int v = 0; v < 2; ++v, ++g) {
                             const uint32_t s = R::slot(g);
                             if (g >= R::kSlots) ok = warp_wait(&kv_empty[s], (R::use(g) - 1) & 1u, &abort_flag);
                             if (!ok) break;
                             if constexpr (kBias)
-                                if (v == 0) place(bias_s, jj % kWordRing, pos, word, lane);
+                                if (v == 0) places.step(a, x, bias_s, j, j + 2 < x.n ? j + 2 : -1, x.n, jj, lane);
                             if (lane == 0) {
                                 if (v == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
                                 mbar_expect_tx(&kv_full[R::full(v, jj)], kTileBytes);
@@ -807,6 +945,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
     } else {
         more_registers<F::kBlocks == 1 ? 216 : 184>();
+        if constexpr (kBias) stage_near<kSoft>(a.bias, bias_s);
         // ---- softmax of tile `q`, one row per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
@@ -832,37 +971,77 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     int64_t row;
                     int head;
                     row_of(a, x, r, row, head);
-                    if (r < x.rows) pos_q = pos_of(a.bias.pos_q, row, x.rg.q0);
                     table += head * a.bias.buckets;
+                    row_of(a, x, min(r, x.rows - 1), row, head);      // rows that there are not are where the last one is
+                    pos_q = pos_of(a.bias.pos_q, row, x.rg.q0);
                 }
+                const bool alive = r - lane < x.rows;
+                TileSpans<false, 4> spans;
                 for (int j = 0; j < x.n; ++j, ++jj) {
-                    ok = warp_wait(&s_full[q], sc++ & 1u, &abort_flag);
+                    if constexpr (kBias) {                   // positions are a tile ahead of the products, the first tile's are not
+                        if (j == 0) ok = warp_wait(&s_full[q], sc & 1u, &abort_flag);
+                        if (!ok) break;
+                        spans.find(a.bias, bias_s, jj % kWordRing, 0, pos_q, alive, bucket);
+                        __syncwarp();
+                    }
+                    if (!kBias || j > 0) ok = warp_wait(&s_full[q], sc & 1u, &abort_flag);
+                    ++sc;
                     if (!ok) break;
                     tc_fence_after();
                     uint32_t word[4];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) word[c] = words[jj % kWordRing][c];
-                    // the row's 128 scores stay in registers; four chains for the maximum
-                    Scale scale{c1, 0.f};
-                    if constexpr (kBias) scale = add_bias<false, 4>(s_addr, c1, a.bias, bias_s, jj % kWordRing, 0, table, pos_q, bucket, 1, 0);
-                    uint32_t v[4][32];
+                    // the row's 128 scores stay in registers; four chains for the maximum.  With a bias they are read twice, 32 at a time, as the
+                    // code of the biases is there once.
+                    uint32_t v[kBias ? 1 : 4][32];
+                    float tops[4], factor = c1, add = 0.f;            // factor, add: of the scores in powers of two
+                    if constexpr (kBias) {
+                        if (spans.one) add = table[spans.at];
+                        else factor = 1.f;
+                        float highest = -INFINITY;
+#pragma unroll 1
+                        for (int c = 0; c < 4; ++c) {
+                            const bool apart = !spans.one && spans.apart_at(c, 1);
+                            if (apart) spans.one_by_one(s_addr + c * 32, c, c1, a.bias, bias_s, jj % kWordRing, 0, pos_q, table, 1, 0);
+                            __syncwarp();                    // tensor memory is for a converged warp
+                            tmem_load32_async(s_addr + c * 32, v[0]);
+                            tmem_load_wait();
+                            if (!spans.one && !apart) spans.add_to(v[0], c, c1, bias_s, jj % kWordRing, 0, pos_q, table);
+                            const uint32_t seen = words[jj % kWordRing][c];
+                            if (seen != 0xFFFFFFFFu) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) tmem_load32_async(s_addr + c * 32, v[c]);
-                    tmem_load_wait();
-                    float tops[4];
+                                for (int i = 0; i < 32; ++i)
+                                    if (!((seen >> i) & 1u)) v[0][i] = 0xFF800000u;
+                            }
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        if (word[c] != 0xFFFFFFFFu) {
+                            for (int i = 0; i < 4; ++i) tops[i] = __uint_as_float(v[0][i]);
 #pragma unroll
-                            for (int i = 0; i < 32; ++i)
-                                if (!((word[c] >> i) & 1u)) v[c][i] = 0xFF800000u;
+                            for (int i = 4; i < 32; ++i) tops[i & 3] = fmaxf(tops[i & 3], __uint_as_float(v[0][i]));
+                            highest = fmaxf(highest, fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])));
+                            if (!spans.one || seen != 0xFFFFFFFFu) {
+                                __syncwarp();
+                                tmem_store32(s_addr + c * 32, v[0]);
+                            }
                         }
-                        tops[c] = __uint_as_float(v[c][0]);
+                        tmem_store_wait();
+                        tops[0] = fmaf(highest, factor, add);
+                    } else {
 #pragma unroll
-                        for (int i = 1; i < 32; ++i) tops[c] = fmaxf(tops[c], __uint_as_float(v[c][i]));
+                        for (int c = 0; c < 4; ++c) tmem_load32_async(s_addr + c * 32, v[c]);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            if (word[c] != 0xFFFFFFFFu) {
+#pragma unroll
+                                for (int i = 0; i < 32; ++i)
+                                    if (!((word[c] >> i) & 1u)) v[c][i] = 0xFF800000u;
+                            }
+                            tops[c] = __uint_as_float(v[c][0]);
+#pragma unroll
+                            for (int i = 1; i < 32; ++i) tops[c] = fmaxf(tops[c], __uint_as_float(v[c][i]));
+                        }
                     }
-                    float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-                    if constexpr (kBias) top = fmaf(top, scale.factor, scale.add);
+                    const float top = kBias ? tops[0] : fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
                     // The maximum that p and l refer to moves only where a score exceeds it by 8 in the exponent: p <= 2^8 loses
                     // nothing in floating point, and the sums so far are rescaled seldom.
                     const bool moves = top * c2 > m * c2 + 8.f || m == -INFINITY;
@@ -882,16 +1061,20 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     if (moves) m = top;
                     const float base = m == -INFINITY ? 0.f : m * c2;
                     if constexpr (kBias) __syncwarp();       // the stores to tensor memory are for a converged warp
-                    const float factor = kBias ? scale.factor : c1, add = kBias ? scale.add - base : -base;
+                    add = kBias ? add - base : -base;
                     const float2 scale2 = make_float2(factor, factor), base2 = make_float2(add, add);
                     float2 sums[4];
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         uint32_t p[16];
                         sums[c] = make_float2(0.f, 0.f);
+                        if constexpr (kBias) {
+                            tmem_load32_async(s_addr + c * 32, v[0]);
+                            tmem_load_wait();
+                        }
 #pragma unroll
                         for (int i = 0; i < 32; i += 2) {
-                            float2 x = __ffma2_rn(make_float2(__uint_as_float(v[c][i]), __uint_as_float(v[c][i + 1])), scale2, base2);
+                            float2 x = __ffma2_rn(pair_of(v[kBias ? 0 : c][i], v[kBias ? 0 : c][i + 1]), scale2, base2);
                             x.x = exp2_approx(x.x);
                             x.y = exp2_approx(x.y);
                             sums[c] = __fadd2_rn(sums[c], x);
@@ -1101,9 +1284,9 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 const int steps = x.n * passes_of<kBias>(x, a.head_dim);
                 for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                     Visible seen;
-                    KeyPlaces places;
+                    Ahead places;
                     seen.ahead(a, x, 0, lane);
-                    if constexpr (kBias) places.ahead(a, x, 0, lane);
+                    if constexpr (kBias) places.begin(a, x, bias_s, steps, jj, lane);
                     if (item > 0) ok = warp_wait(&q_empty, (item - 1) & 1u, &abort_flag);
                     if (!ok) break;
                     if (f.boxes) {
@@ -1128,21 +1311,14 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     for (int j = 0, tile = 0; j < steps && ok; ++j, ++jj) {
                         const int next = tile + 1 < x.n ? tile + 1 : 0;
                         uint32_t word[4];
-                        int pos[4];
                         seen.now(word);
-                        if constexpr (kBias)
-#pragma unroll
-                            for (int b = 0; b < 4; ++b) pos[b] = places.next[b];
-                        if (j + 1 < steps) {
-                            seen.ahead(a, x, next, lane);
-                            if constexpr (kBias) places.ahead(a, x, next, lane);
-                        }
+                        if (j + 1 < steps) seen.ahead(a, x, next, lane);
                         for (int v = 0; v < 2; ++v, ++g) {
                             const uint32_t s = R::slot(g);
                             if (g >= R::kSlots) ok = warp_wait(&kv_empty[s], (R::use(g) - 1) & 1u, &abort_flag);
                             if (!ok) break;
                             if constexpr (kBias)
-                                if (v == 0) place(bias_s, jj % kWordRing, pos, word, lane);
+                                if (v == 0) places.step(a, x, bias_s, j, j + 2 < steps ? (next + 1 < x.n ? next + 1 : 0) : -1, steps, jj, lane);
                             if (lane == 0) {
                                 if (v == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
                                 mbar_expect_tx(&kv_full[R::full(v, jj)], kTileBytes);
@@ -1235,6 +1411,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         }
     } else {
         more_registers<200>();
+        if constexpr (kBias) stage_near<8>(a.bias, bias_s);
         // ---- p and dS: 64 columns of one row per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
@@ -1270,31 +1447,43 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 }
                 float rest = 0.f, run = 0.f;
                 int pos_q = 0, cur = -1;
-                Bucket bucket, place_of;                 // of the scores, of the sums by bucket
+                Bucket bucket;
                 bucket.unknown();
-                place_of.unknown();
                 const int g0 = kBias ? (int)((t * kTile + w * 32) % a.group) : 0;
                 const float *table = table_s;
                 if constexpr (kBias) {
-                    if (live) pos_q = pos_of(a.bias.pos_q, row, x.rg.q0);
+                    int64_t near;
+                    int any;
+                    row_of(a, x, min(r, x.rows - 1), near, any);      // rows that there are not are where the last one is
+                    pos_q = pos_of(a.bias.pos_q, near, x.rg.q0);
                     table += head * a.bias.buckets;
                 }
+                const bool alive = r - lane < x.rows;
+                TileSpans<false, 2> spans;
                 for (int j = 0; j < steps; ++j, ++jj) {
-                    if (j == first) bucket.unknown();
-                    ok = warp_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
+                    if constexpr (kBias) {                   // positions are a tile ahead of the products, the first tile's are not
+                        if (j == 0) ok = warp_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
+                        if (!ok) break;
+                        if (j == first) bucket.unknown();
+                        spans.find(a.bias, bias_s, jj % kWordRing, q * 2, pos_q, alive, bucket);
+                        __syncwarp();
+                    }
+                    if (!kBias || j > 0) ok = warp_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
                     if (!ok) break;
                     tc_fence_after();
                     float p[64];
                     {
-                        Scale scale{c1, 0.f};
                         if constexpr (kBias)
-                            scale = add_bias<false, 2>(tmem + lanes + (jj & 1u) * kTile + q * 64, c1, a.bias, bias_s, jj % kWordRing, q * 2, table, pos_q,
-                                                       bucket, 1, 0);
-                        const float factor = kBias ? scale.factor : c1, add = kBias ? scale.add - base : -base;
+                            if (!spans.one) spans.in_place(tmem + lanes + (jj & 1u) * kTile + q * 64, c1, a.bias, bias_s, jj % kWordRing, q * 2, pos_q, table, 1, 0);
                         uint32_t v[2][32];
                         tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64, v[0]);
                         tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64 + 32, v[1]);
                         tmem_load_wait();
+                        float factor = c1, add = -base;
+                        if constexpr (kBias) {
+                            if (spans.one) add += table[spans.at];
+                            else factor = 1.f;
+                        }
 #pragma unroll
                         for (int e = 0; e < 64; e += 2) {
                             const float2 y = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(factor, factor), make_float2(add, add)));
@@ -1368,7 +1557,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     }
                     if constexpr (kBias)
                         if (table_part) {
-                            bin_columns(bins, a.bias, bias_s, jj % kWordRing, q, p, pos_q, place_of, live && base != INFINITY, a.group, g0, run, cur, lane);
+                            bin_columns(bins, a.bias, bias_s, jj % kWordRing, q, p, pos_q, spans, live && base != INFINITY, a.group, g0, run, cur, lane);
                             __syncwarp();
                         }
                     store_operand_and_rest(tmem + lanes + 256 + q * 64, tmem + lanes + (jj & 1u) * kTile + q * 64, p);
@@ -1642,6 +1831,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
     } else {
         more_registers<200>();
+        if constexpr (kBias) stage_near<8>(a.bias, bias_s);
         // ---- p and dS: 64 columns (rows of Q) of one key per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
@@ -1658,27 +1848,36 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 int pos_k = 0;
                 Bucket bucket;
                 bucket.unknown();
-                if constexpr (kBias)
-                    if (live) pos_k = pos_of(a.bias.pos_k, key, x.rg.k0);
+                if constexpr (kBias) pos_k = pos_of(a.bias.pos_k, min(key, x.ke - 1), x.rg.k0);
+                const bool alive = key - lane < x.ke;
+                TileSpans<true, 2> spans;
                 for (int j = 0; j < n; ++j, ++jj) {
                     ok = warp_wait(&s_full, jj & 1u, &abort_flag);
                     if (!ok) break;
                     tc_fence_after();
+                    if constexpr (kBias) {
+                        spans.find(a.bias, bias_s, jj % kWordRing, q * 2, pos_k, alive, bucket);
+                        __syncwarp();
+                    }
                     const float4 *lse4 = reinterpret_cast<const float4 *>(stat_lse[jj % kWordRing] + q * 64);
                     const float4 *dot4 = reinterpret_cast<const float4 *>(stat_dot[jj % kWordRing] + q * 64);
                     float p[64];
                     {
-                        Scale scale{c1, 0.f};
-                        if constexpr (kBias) {
-                            const int g0 = a.group == 1 ? 0 : (int)(((int64_t)j * kTile + q * 64) % a.group);
-                            scale = add_bias<true, 2>(tmem + lanes + q * 64, c1, a.bias, bias_s, jj % kWordRing, q * 2,
-                                                      table_s + x.h * a.group * a.bias.buckets, pos_k, bucket, a.group, g0);
-                        }
-                        const float2 factor = make_float2(scale.factor, scale.factor), add = make_float2(scale.add, scale.add);
+                        const float *table = table_s + x.h * a.group * a.bias.buckets;
+                        if constexpr (kBias)
+                            if (a.group > 1 || !spans.one) {
+                                const int g0 = a.group == 1 ? 0 : (int)(((int64_t)j * kTile + q * 64) % a.group);
+                                spans.in_place(tmem + lanes + q * 64, c1, a.bias, bias_s, jj % kWordRing, q * 2, pos_k, table, a.group, g0);
+                            }
                         uint32_t v[2][32];
                         tmem_load32_async(tmem + lanes + q * 64, v[0]);
                         tmem_load32_async(tmem + lanes + q * 64 + 32, v[1]);
                         tmem_load_wait();
+                        float2 factor = make_float2(c1, c1), add = make_float2(0.f, 0.f);
+                        if constexpr (kBias) {
+                            if (a.group > 1 || !spans.one) factor = make_float2(1.f, 1.f);
+                            else add = make_float2(table[spans.at], table[spans.at]);
+                        }
 #pragma unroll
                         for (int e = 0; e < 64; e += 4) {
                             float4 l = lse4[e / 4];                  // negated, as the sums of products below
