@@ -88,6 +88,19 @@ __device__ __forceinline__ int bucket_of(const BiasArgs &b, const int32_t *edges
     }
     return at;
 }
+// The buckets of N distances side by side.  Steps by powers of two over the edges in shared memory; those behind the last are passed by the
+// highest distance alone, whose bucket is the last.
+template <int N> __device__ inline void look_up(const BiasArgs &b, const int32_t *edges, const int (&d)[N], int (&at)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) at[i] = 0;
+    for (int s = b.top; s; s >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) at[i] += edges[at[i] + s - 1] <= d[i] ? s : 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) at[i] = min(at[i], b.buckets - 1);
+}
+
 // A bias in powers of two, as the scores are
 __device__ __forceinline__ float bias_value(float b) { return b <= kHides ? -INFINITY : b * kLog2e; }
 __device__ __forceinline__ float bias_at(const BiasArgs &b, int heads, int bucket, int head) { return bias_value(__ldg(b.table + bucket * heads + head)); }
@@ -145,6 +158,7 @@ bool few_attention_table(const AttnArgs &a, const TablePlan &p, int32_t dtype, f
 void join_dq(const AttnArgs &a, int splits, int32_t dtype, bool fit, const float *part_dq, float *dots, cudaStream_t st);
 
 // attention_simt.cu: fp32, head_dim <= 128, tiles of 64 rows x 64 keys
+constexpr int kSimtTable = 4096;             // entries of a table of biases, buckets x heads of a group, that fit beside the tiles
 struct SimtPlan {
     int rows;                             // of a tile: 16, 32 or 64
     int64_t q_tiles, k_tiles;             // blocks of rows / of keys per sequence and key head
@@ -152,6 +166,8 @@ struct SimtPlan {
 };
 SimtPlan simt_plan(const AttnArgs &a, const Lengths &q, const Lengths &k);
 bool simt_attention_forward(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st);
-bool simt_attention_backward(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st);
+// table_part: with a bias [n_seq x q_tiles x splits, buckets x heads], or null where the kernel of dQ does not form the table's gradient
+bool simt_attention_backward(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, float *table_part, cudaStream_t st);
+bool simt_forms_table(const AttnArgs &a, const SimtPlan &p);      // groups that divide 16, bins that fit
 
 }  // namespace e2egrec

@@ -29,6 +29,7 @@ struct SimtShape {
     int tiles, splits;                    // blocks of rows (or keys) per sequence and key head; stretches of the keys
     int stages;                           // tiles of the side that a block goes over: 2: one lands beside the products of the other
     int cols;                             // threads side by side over a head's columns (a power of two), TX / cols parts of the sums
+    int tile_floats;                      // of all tiles; what a bias takes follows
 };
 
 __device__ inline float exp2_fast(float x)
@@ -222,6 +223,30 @@ __device__ inline void row_of(const AttnArgs &a, const SimtUnit &x, int64_t r, i
     head = x.h * a.group + (int)(r - i * a.group);
 }
 
+// ---- Bias by distance: positions of a tile's keys (and rows) lie beside it, every score looks its bucket up by bisection, the J of a row side by
+// side.  The gradient of the table is formed beside dQ: every thread has bins of its own in shared memory, [buckets x threads], added up at
+// the unit's end in a fixed order.  That wants a thread's rows to be of one head: groups that divide 16.
+struct SimtBias {
+    int32_t *edges;                                      // kMaxBuckets, beyond the last the highest number
+    float *table;                                        // [heads of the group x buckets], in powers of two
+    float *bins;
+};
+// where they lie: behind `floats` floats of shared memory
+__device__ inline SimtBias bias_of(float *sm, size_t floats, const AttnArgs &a)
+{
+    SimtBias s;
+    s.edges = reinterpret_cast<int32_t *>(sm + floats);
+    s.table = sm + floats + kMaxBuckets;
+    s.bins = s.table + a.bias.buckets * a.group;
+    return s;
+}
+__device__ inline void stage_bias(const AttnArgs &a, const SimtBias &s, int h)
+{
+    const int nb = a.bias.buckets, heads = a.kv_heads * a.group;
+    for (int i = threadIdx.x; i < kMaxBuckets; i += blockDim.x) s.edges[i] = i < nb - 1 ? __ldg(a.bias.edges + i) : INT32_MAX;
+    for (int i = threadIdx.x; i < nb * a.group; i += blockDim.x) s.table[i] = bias_at(a.bias, heads, i % nb, h * a.group + i / nb);
+}
+
 // Tiles of keys and values (or of rows) that a block goes over: stage b of two pairs of tiles, a turn's loads beside the turn before where
 // there are two.  load(j, b) starts the copies of turn j into stage b; use(j, b) works on it.
 template <typename Load, typename Use> __device__ inline void turns(const SimtShape &f, int64_t n, Load load, Use use)
@@ -240,17 +265,39 @@ template <typename Load, typename Use> __device__ inline void turns(const SimtSh
     }
 }
 
+// position of row r, and where its head's biases begin
+__device__ inline void place_row(const AttnArgs &a, const SimtUnit &x, int64_t r, int &pos, int &own)
+{
+    int64_t row;
+    int head;
+    row_of(a, x, min(r, x.rows - 1), row, head);
+    pos = pos_of(a.bias.pos_q, row, x.rg.q0);
+    own = (head - x.h * a.group) * a.bias.buckets;
+}
+// buckets of a row at pos_q and the thread's keys tx + TX j
+template <int TX> __device__ inline void buckets_of(const AttnArgs &a, const SimtBias &s, const int32_t *pos, int tx, int pos_q, int (&bucket)[kTile / TX])
+{
+    int d[kTile / TX];
+#pragma unroll
+    for (int j = 0; j < kTile / TX; ++j) d[j] = apart(pos[tx + TX * j], pos_q);
+    look_up<kTile / TX>(a.bias, s.edges, d, bucket);
+}
+
 // Keys and values from x.kb + 64 j on -> a stage, zeros over hidden ones
-template <int TX> __device__ inline void load_keys(const AttnArgs &a, const SimtUnit &x, const SimtShape &f, float *stage, uint8_t *seen_s, int64_t j, const float *kp, const float *vp)
+template <int TX, bool kBias>
+__device__ inline void load_keys(const AttnArgs &a, const SimtUnit &x, const SimtShape &f, float *stage, uint8_t *seen_s, int32_t *pos_s, int64_t j, const float *kp,
+                                 const float *vp)
 {
     const int64_t key = x.kb + j * kTile + threadIdx.x / (TX / 4);
     const bool seen = key < x.ke && (!a.mask || a.mask[key]);
     load_tile<TX / 4>(stage, f, seen ? kp + key * a.ldk + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
     load_tile<TX / 4>(stage + kTile * f.ld, f, seen ? vp + key * a.ldv + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
     if (threadIdx.x % (TX / 4) == 0) seen_s[threadIdx.x / (TX / 4)] = seen;
+    if constexpr (kBias)
+        if (threadIdx.x % (TX / 4) == 0) pos_s[threadIdx.x / (TX / 4)] = seen ? pos_of(a.bias.pos_k, key, x.rg.k0) : 0;
 }
 
-template <int TX, int C, int I>
+template <int TX, int C, int I, bool kBias>
 __global__ void __launch_bounds__(16 * TX, blocks_of(TX, C, I))
 attn_simt_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ SimtShape f, float *__restrict__ part_o, float2 *__restrict__ part_ml)
 {
@@ -258,11 +305,14 @@ attn_simt_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     extern __shared__ __align__(16) float sm[];
     float *q_s = sm, *p_s = q_s + kRows * f.ld, *kv_s = p_s + kRows * kLdP;          // stage b: K and V at tiles 2 b, 2 b + 1
     __shared__ uint8_t seen_s[2][kTile];
+    __shared__ int32_t pos_s[kBias ? 2 : 1][kTile];
     const int tx = threadIdx.x % TX, ty = threadIdx.x / TX, heads = a.kv_heads * a.group, lr = threadIdx.x / kPerRow;
     const Columns<TX> at(f, tx);
     const SimtUnit x = simt_unit(a, f);
     const float c1 = a.scale * kLog2e;
     const float *qp = static_cast<const float *>(a.q), *kp = static_cast<const float *>(a.k), *vp = static_cast<const float *>(a.v);
+    const SimtBias bias = bias_of(sm, f.tile_floats, a);
+    if constexpr (kBias) stage_bias(a, bias, x.h);
     for (int64_t t = x.t0; t * kRows < x.rows; t += f.tiles) {
         const int64_t r0 = t * kRows;
         __syncthreads();
@@ -273,13 +323,15 @@ attn_simt_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             load_tile<kPerRow>(q_s, f, r0 + lr < x.rows ? qp + row * a.ldq + (int64_t)head * a.head_dim : nullptr, qp, a.head_dim);
         }
         float o[I][C][4], m[I], l[I];
+        int pos_q[I], own[I];                            // own: the row's table
         clear(o);
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             m[i] = -INFINITY;
             l[i] = 0.f;
+            if constexpr (kBias) place_row(a, x, r0 + ty + 16 * i, pos_q[i], own[i]);
         }
-        turns(f, ceil_div(x.ke - x.kb, (int64_t)kTile), [&](int64_t j, int b) { load_keys<TX>(a, x, f, kv_s + 2 * b * kTile * f.ld, seen_s[b], j, kp, vp); }, [&](int b) {
+        turns(f, ceil_div(x.ke - x.kb, (int64_t)kTile), [&](int64_t j, int b) { load_keys<TX, kBias>(a, x, f, kv_s + 2 * b * kTile * f.ld, seen_s[b], pos_s[kBias ? b : 0], j, kp, vp); }, [&](int b) {
             const float *k_s = kv_s + 2 * b * kTile * f.ld, *v_s = k_s + kTile * f.ld;
             float s[I][J];
             scores<TX, I>(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
@@ -289,9 +341,12 @@ attn_simt_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 float top = -INFINITY;
+                int bucket[J];
+                if constexpr (kBias) buckets_of<TX>(a, bias, pos_s[b], tx, pos_q[i], bucket);
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    s[i][j] = on[j] ? s[i][j] * c1 : -INFINITY;
+                    if constexpr (kBias) s[i][j] = on[j] ? fmaf(s[i][j], c1, bias.table[own[i] + bucket[j]]) : -INFINITY;
+                    else s[i][j] = on[j] ? s[i][j] * c1 : -INFINITY;
                     top = fmaxf(top, s[i][j]);
                 }
                 top = fmaxf(m[i], row_max<TX>(top));
@@ -338,20 +393,29 @@ attn_simt_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     }
 }
 
-template <int TX, int C, int I>
+template <int TX, int C, int I, bool kBias>
 __global__ void __launch_bounds__(16 * TX, blocks_of(TX, C, I))
-attn_simt_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ SimtShape f, float *__restrict__ part_dq, float *__restrict__ dots)
+attn_simt_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ SimtShape f, float *__restrict__ part_dq, float *__restrict__ dots,
+                    float *__restrict__ table_part)
 {
     constexpr int kRows = 16 * I, kPerRow = TX / I, J = kTile / TX;
     extern __shared__ __align__(16) float sm[];
     float *q_s = sm, *g_s = q_s + kRows * f.ld, *ds_s = g_s + kRows * f.ld, *kv_s = ds_s + kRows * kLdP;
     __shared__ uint8_t seen_s[2][kTile];
+    __shared__ int32_t pos_s[kBias ? 2 : 1][kTile];
     const int tx = threadIdx.x % TX, ty = threadIdx.x / TX, heads = a.kv_heads * a.group, lr = threadIdx.x / kPerRow;
     const Columns<TX> at(f, tx);
     const SimtUnit x = simt_unit(a, f);
     const float c1 = a.scale * kLog2e;
     const float *qp = static_cast<const float *>(a.q), *kp = static_cast<const float *>(a.k), *vp = static_cast<const float *>(a.v);
     const float *gp = static_cast<const float *>(a.dout), *op = static_cast<const float *>(a.o);
+    const SimtBias bias = bias_of(sm, f.tile_floats, a);
+    float *mine_s = bias.bins + threadIdx.x;             // the thread's bins, 16 TX apart
+    if constexpr (kBias) {
+        stage_bias(a, bias, x.h);
+        if (table_part)
+            for (int i = 0; i < a.bias.buckets; ++i) mine_s[i * 16 * TX] = 0.f;
+    }
     for (int64_t t = x.t0; t * kRows < x.rows; t += f.tiles) {
         const int64_t r0 = t * kRows;
         __syncthreads();
@@ -364,6 +428,10 @@ attn_simt_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             load_tile<kPerRow>(g_s, f, on ? gp + row * a.ldg + (int64_t)head * a.head_dim : nullptr, qp, a.head_dim);
         }
         float dq[I][C][4], lse[I], d[I], mine = 0.f;
+        int pos_q[I], own[I];
+        if constexpr (kBias)
+#pragma unroll
+            for (int i = 0; i < I; ++i) place_row(a, x, r0 + ty + 16 * i, pos_q[i], own[i]);
         clear(dq);
         cp_async_wait_all();
         __syncthreads();
@@ -383,17 +451,32 @@ attn_simt_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         }
 #pragma unroll
         for (int i = 0; i < I; ++i) d[i] = __shfl_sync(0xFFFFFFFFu, mine, i, TX);
-        turns(f, ceil_div(x.ke - x.kb, (int64_t)kTile), [&](int64_t j, int b) { load_keys<TX>(a, x, f, kv_s + 2 * b * kTile * f.ld, seen_s[b], j, kp, vp); }, [&](int b) {
+        turns(f, ceil_div(x.ke - x.kb, (int64_t)kTile), [&](int64_t j, int b) { load_keys<TX, kBias>(a, x, f, kv_s + 2 * b * kTile * f.ld, seen_s[b], pos_s[kBias ? b : 0], j, kp, vp); }, [&](int b) {
             const float *k_s = kv_s + 2 * b * kTile * f.ld, *v_s = k_s + kTile * f.ld;
             float s[I][J], u[I][J];
             scores<TX, I>(q_s, k_s, f.ld, a.head_dim, ty, tx, s);
             scores<TX, I>(g_s, v_s, f.ld, a.head_dim, ty, tx, u);
+            if constexpr (kBias) {
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const bool on = seen_s[b][tx + TX * j];
+                for (int i = 0; i < I; ++i) {
+                    int bucket[J];
+                    buckets_of<TX>(a, bias, pos_s[b], tx, pos_q[i], bucket);
 #pragma unroll
-                for (int i = 0; i < I; ++i)
-                    ds_s[(ty + 16 * i) * kLdP + tx + TX * j] = on ? exp2_fast(fmaf(s[i][j], c1, -lse[i])) * (u[i][j] - d[i]) : 0.f;
+                    for (int j = 0; j < J; ++j) {
+                        const float v = exp2_fast(fmaf(s[i][j], c1, bias.table[own[i] + bucket[j]] - lse[i])) * (u[i][j] - d[i]);
+                        const float ds = seen_s[b][tx + TX * j] && lse[i] != INFINITY ? v : 0.f;
+                        ds_s[(ty + 16 * i) * kLdP + tx + TX * j] = ds;
+                        if (table_part) mine_s[bucket[j] * 16 * TX] += ds;
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const bool on = seen_s[b][tx + TX * j];
+#pragma unroll
+                    for (int i = 0; i < I; ++i)
+                        ds_s[(ty + 16 * i) * kLdP + tx + TX * j] = on ? exp2_fast(fmaf(s[i][j], c1, -lse[i])) * (u[i][j] - d[i]) : 0.f;
+                }
             }
             __syncwarp();
             add_rows<C, I, TX>(dq, ds_s, k_s, f.ld, a.head_dim, ty, at);
@@ -412,9 +495,33 @@ attn_simt_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             else store_columns<C, TX>(part_dq + (((int64_t)x.z * a.q_rows + row) * heads + head) * a.head_dim, dq[i], a.scale, a.head_dim, at, keep);
         }
     }
+    if constexpr (kBias)
+        if (table_part) {                                // thread ty, tx has the head ty % group: lanes of one head by exchange, then the warps
+            __syncthreads();
+            constexpr int kWarps = 16 * TX / 32;
+            const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nb = a.bias.buckets;
+            const uint32_t u = blockIdx.x;
+            const int64_t seq = u / (uint32_t)f.splits / (uint32_t)f.tiles / (uint32_t)a.kv_heads;
+            float *part = table_part + ((seq * f.tiles + x.t0) * f.splits + x.z) * nb * heads + x.h * a.group;
+            for (int k = warp; k < nb; k += kWarps) {
+                for (int g0 = 0; g0 < a.group; g0 += 32 / TX) {
+                    // a warp's lanes have the rows 32 / TX w + lane / TX of a step, of heads that follow one another
+                    float v = 0.f;
+                    for (int w = 0; w < kWarps; ++w) {
+                        const int first = w * (32 / TX) % a.group;
+                        if (a.group <= 32 / TX || first == g0) v += bias.bins[k * 16 * TX + w * 32 + lane];
+                    }
+                    const int stop = a.group <= 32 / TX ? TX * a.group : 32;
+                    for (int o = 16; o >= stop; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+                    for (int o = TX / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+                    const int g = g0 + lane / TX;
+                    if (lane % TX == 0 && lane < stop && g < a.group) part[k * heads + g] = v;
+                }
+            }
+        }
 }
 
-template <int TX, int C, int I>
+template <int TX, int C, int I, bool kBias>
 __global__ void __launch_bounds__(16 * TX, blocks_of(TX, C, I))
 attn_simt_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ SimtShape f, const float *__restrict__ dots)
 {
@@ -422,12 +529,15 @@ attn_simt_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
     extern __shared__ __align__(16) float sm[];
     float *k_s = sm, *v_s = k_s + kTile * f.ld, *p_s = v_s + kTile * f.ld, *ds_s = p_s + kRows * kLdP, *qg_s = ds_s + kRows * kLdP;
     __shared__ float lse_s[2][kRows], dot_s[2][kRows];
+    __shared__ int32_t pos_s[kBias ? 2 : 1][kRows], own_s[kBias ? 2 : 1][kRows], key_s[kTile];
     const int tx = threadIdx.x % TX, ty = threadIdx.x / TX, heads = a.kv_heads * a.group, lr = threadIdx.x / kPerRow;
     const Columns<TX> at(f, tx);
     const SimtUnit x = simt_unit(a, f);
     const float c1 = a.scale * kLog2e;
     const float *qp = static_cast<const float *>(a.q), *kp = static_cast<const float *>(a.k), *vp = static_cast<const float *>(a.v);
     const float *gp = static_cast<const float *>(a.dout);
+    const SimtBias bias = bias_of(sm, f.tile_floats, a);
+    if constexpr (kBias) stage_bias(a, bias, x.h);
     for (int64_t j0 = x.rg.k0 + (int64_t)x.t0 * kTile; j0 < x.rg.k1; j0 += (int64_t)f.tiles * kTile) {
         __syncthreads();
         {
@@ -435,6 +545,8 @@ attn_simt_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             const bool seen = key < x.rg.k1 && (!a.mask || a.mask[key]);
             load_tile<TX / 4>(k_s, f, seen ? kp + key * a.ldk + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
             load_tile<TX / 4>(v_s, f, seen ? vp + key * a.ldv + (int64_t)x.h * a.head_dim : nullptr, kp, a.head_dim);
+            if constexpr (kBias)
+                if (threadIdx.x % (TX / 4) == 0) key_s[threadIdx.x / (TX / 4)] = seen ? pos_of(a.bias.pos_k, key, x.rg.k0) : 0;
         }
         float dk[4][C][4], dv[4][C][4];
         clear(dk);
@@ -453,6 +565,7 @@ attn_simt_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
             if (threadIdx.x % kPerRow == 0) {
                 lse_s[b][lr] = l;
                 dot_s[b][lr] = l != INFINITY ? dots[row * heads + head] : 0.f;
+                if constexpr (kBias) place_row(a, x, r, pos_s[b][lr], own_s[b][lr]);
             }
             load_tile<kPerRow>(q_s, f, l != INFINITY ? qp + row * a.ldq + (int64_t)head * a.head_dim : nullptr, kp, a.head_dim);
             load_tile<kPerRow>(g_s, f, l != INFINITY ? gp + row * a.ldg + (int64_t)head * a.head_dim : nullptr, kp, a.head_dim);
@@ -464,9 +577,16 @@ attn_simt_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__
 #pragma unroll
             for (int i = 0; i < I; ++i) {
                 const float lse = lse_s[b][ty + 16 * i], d = dot_s[b][ty + 16 * i];
+                int bucket[J], own = 0;
+                if constexpr (kBias) {
+                    buckets_of<TX>(a, bias, key_s, tx, pos_s[b][ty + 16 * i], bucket);
+                    own = own_s[b][ty + 16 * i];
+                }
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    const float p = exp2_fast(fmaf(s[i][j], c1, -lse));
+                    float add = -lse;
+                    if constexpr (kBias) add += bias.table[own + bucket[j]];
+                    const float p = exp2_fast(fmaf(s[i][j], c1, add));
                     p_s[(ty + 16 * i) * kLdP + tx + TX * j] = p;
                     ds_s[(ty + 16 * i) * kLdP + tx + TX * j] = p * (u[i][j] - d);
                 }
@@ -501,7 +621,8 @@ template <typename Kernel> bool allow_smem(Kernel kernel, std::atomic<bool> (&do
 }
 
 // kept: floats of shared memory that stay; pair: those of one stage.  Two stages where they leave room for `blocks` blocks per SM.
-SimtShape shape_of(const AttnArgs &a, int64_t tiles, int splits, int kept_rows, int pair_rows, int p_rows, int TX, int blocks, size_t &smem)
+// bins: threads that have bins of their own.
+SimtShape shape_of(const AttnArgs &a, int64_t tiles, int splits, int kept_rows, int pair_rows, int p_rows, int TX, int blocks, int bins, size_t &smem)
 {
     SimtShape f{};
     f.ld = (a.head_dim / 4 | 1) * 4;                 // an odd number of 16-byte units
@@ -510,38 +631,51 @@ SimtShape shape_of(const AttnArgs &a, int64_t tiles, int splits, int kept_rows, 
     f.cols = TX;
     while (f.cols > 1 && f.cols * 2 >= a.head_dim) f.cols /= 2;
     const size_t fixed = ((size_t)kept_rows * f.ld + (size_t)p_rows * kLdP) * sizeof(float), pair = (size_t)pair_rows * f.ld * sizeof(float);
-    f.stages = (fixed + 2 * pair + 2048) * blocks <= (size_t)kSmSmem ? 2 : 1;
-    smem = fixed + f.stages * pair;
+    const size_t beside = a.bias.buckets ? ((size_t)kMaxBuckets + (size_t)a.bias.buckets * (a.group + bins)) * sizeof(float) : 0;
+    f.stages = (fixed + 2 * pair + beside + 2048) * blocks <= (size_t)kSmSmem ? 2 : 1;
+    f.tile_floats = (int)((fixed + f.stages * pair) / sizeof(float));
+    smem = fixed + f.stages * pair + beside;
     return f;
+}
+
+template <int TX, int C, int I, bool kBias> bool launch_fwd(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
+{
+    static std::atomic<bool> done[kMaxDevices] = {};
+    if (!allow_smem(attn_simt_fwd_kernel<TX, C, I, kBias>, done)) return false;
+    size_t smem;
+    const SimtShape f = shape_of(a, p.q_tiles, p.splits, 16 * I, 2 * kTile, 16 * I, TX, blocks_of(TX, C, I), 0, smem);
+    note_launch();
+    attn_simt_fwd_kernel<TX, C, I, kBias><<<(unsigned)(a.n_seq * a.kv_heads * p.q_tiles * p.splits), 16 * TX, smem, st>>>(a, f, part_o, part_ml);
+    return true;
+}
+
+template <int TX, int C, int I, bool kBias>
+bool launch_bwd(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, float *table_part, cudaStream_t st)
+{
+    static std::atomic<bool> done[2][kMaxDevices] = {};
+    if (!allow_smem(attn_simt_dq_kernel<TX, C, I, kBias>, done[0]) || !allow_smem(attn_simt_dkv_kernel<TX, C, I, kBias>, done[1])) return false;
+    size_t smem;
+    if (a.q_rows) {
+        const SimtShape f = shape_of(a, p.q_tiles, p.splits, 2 * 16 * I, 2 * kTile, 16 * I, TX, blocks_of(TX, C, I), table_part ? 16 * TX : 0, smem);
+        note_launch();
+        attn_simt_dq_kernel<TX, C, I, kBias><<<(unsigned)(a.n_seq * a.kv_heads * p.q_tiles * p.splits), 16 * TX, smem, st>>>(a, f, part_dq, dots, table_part);
+    }
+    if (a.k_rows) {
+        const SimtShape f = shape_of(a, p.k_tiles, 1, 2 * kTile, 2 * 16 * I, 2 * 16 * I, TX, blocks_of(TX, C, I), 0, smem);
+        note_launch();
+        attn_simt_dkv_kernel<TX, C, I, kBias><<<(unsigned)(a.n_seq * a.kv_heads * p.k_tiles), 16 * TX, smem, st>>>(a, f, dots);
+    }
+    return true;
 }
 
 template <int TX, int C, int I> bool forward_of(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
 {
-    static std::atomic<bool> done[kMaxDevices] = {};
-    if (!allow_smem(attn_simt_fwd_kernel<TX, C, I>, done)) return false;
-    size_t smem;
-    const SimtShape f = shape_of(a, p.q_tiles, p.splits, 16 * I, 2 * kTile, 16 * I, TX, blocks_of(TX, C, I), smem);
-    note_launch();
-    attn_simt_fwd_kernel<TX, C, I><<<(unsigned)(a.n_seq * a.kv_heads * p.q_tiles * p.splits), 16 * TX, smem, st>>>(a, f, part_o, part_ml);
-    return true;
+    return a.bias.table ? launch_fwd<TX, C, I, true>(a, p, part_o, part_ml, st) : launch_fwd<TX, C, I, false>(a, p, part_o, part_ml, st);
 }
-
-template <int TX, int C, int I> bool backward_of(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
+template <int TX, int C, int I>
+bool backward_of(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, float *table_part, cudaStream_t st)
 {
-    static std::atomic<bool> done[2][kMaxDevices] = {};
-    if (!allow_smem(attn_simt_dq_kernel<TX, C, I>, done[0]) || !allow_smem(attn_simt_dkv_kernel<TX, C, I>, done[1])) return false;
-    size_t smem;
-    if (a.q_rows) {
-        const SimtShape f = shape_of(a, p.q_tiles, p.splits, 2 * 16 * I, 2 * kTile, 16 * I, TX, blocks_of(TX, C, I), smem);
-        note_launch();
-        attn_simt_dq_kernel<TX, C, I><<<(unsigned)(a.n_seq * a.kv_heads * p.q_tiles * p.splits), 16 * TX, smem, st>>>(a, f, part_dq, dots);
-    }
-    if (a.k_rows) {
-        const SimtShape f = shape_of(a, p.k_tiles, 1, 2 * kTile, 2 * 16 * I, 2 * 16 * I, TX, blocks_of(TX, C, I), smem);
-        note_launch();
-        attn_simt_dkv_kernel<TX, C, I><<<(unsigned)(a.n_seq * a.kv_heads * p.k_tiles), 16 * TX, smem, st>>>(a, f, dots);
-    }
-    return true;
+    return a.bias.table ? launch_bwd<TX, C, I, true>(a, p, part_dq, dots, table_part, st) : launch_bwd<TX, C, I, false>(a, p, part_dq, dots, nullptr, st);
 }
 
 }  // namespace
@@ -567,12 +701,21 @@ template <int I, int TX> static bool forward_wide(const AttnArgs &a, const SimtP
     return forward_of<8, 1, I>(a, p, part_o, part_ml, st);
 }
 
-template <int I, int TX> static bool backward_wide(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
+template <int I, int TX> static bool backward_wide(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, float *table_part, cudaStream_t st)
 {
-    if (a.head_dim > 64) return backward_of<16, 2, I>(a, p, part_dq, dots, st);
+    if (a.head_dim > 64) return backward_of<16, 2, I>(a, p, part_dq, dots, table_part, st);
     if constexpr (TX == 8)
-        if (a.head_dim <= 32) return backward_of<8, 1, I>(a, p, part_dq, dots, st);
-    return backward_of<TX, 64 / (4 * TX), I>(a, p, part_dq, dots, st);
+        if (a.head_dim <= 32) return backward_of<8, 1, I>(a, p, part_dq, dots, table_part, st);
+    return backward_of<TX, 64 / (4 * TX), I>(a, p, part_dq, dots, table_part, st);
+}
+
+// The bins of all threads fit beside one stage of tiles
+bool simt_forms_table(const AttnArgs &a, const SimtPlan &p)
+{
+    const int TX = a.head_dim > 64 || p.rows == 64 ? 16 : 8;
+    size_t smem;
+    shape_of(a, 1, 1, 2 * p.rows, 2 * kTile, p.rows, TX, 1 << 20, 16 * TX, smem);       // (one stage where two leave no room for that many blocks)
+    return 16 % a.group == 0 && smem <= (size_t)kMostSmem;
 }
 
 bool simt_attention_forward(const AttnArgs &a, const SimtPlan &p, float *part_o, float2 *part_ml, cudaStream_t st)
@@ -581,10 +724,10 @@ bool simt_attention_forward(const AttnArgs &a, const SimtPlan &p, float *part_o,
     return p.rows == 32 ? forward_wide<2, 8>(a, p, part_o, part_ml, st) : forward_wide<4, 16>(a, p, part_o, part_ml, st);
 }
 
-bool simt_attention_backward(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, cudaStream_t st)
+bool simt_attention_backward(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, float *table_part, cudaStream_t st)
 {
-    if (p.rows == 16) return backward_wide<1, 8>(a, p, part_dq, dots, st);
-    return p.rows == 32 ? backward_wide<2, 8>(a, p, part_dq, dots, st) : backward_wide<4, 16>(a, p, part_dq, dots, st);
+    if (p.rows == 16) return backward_wide<1, 8>(a, p, part_dq, dots, table_part, st);
+    return p.rows == 32 ? backward_wide<2, 8>(a, p, part_dq, dots, table_part, st) : backward_wide<4, 16>(a, p, part_dq, dots, table_part, st);
 }
 
 }  // namespace e2egrec

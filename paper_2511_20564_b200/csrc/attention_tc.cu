@@ -315,19 +315,6 @@ struct Ahead {
 // kKey: the thread's own position is the key's, the columns' are the queries'
 template <bool kKey> __device__ inline int distance(int own, int column) { return kKey ? apart(own, column) : apart(column, own); }
 
-// The buckets of N distances side by side.  Steps by powers of two over the edges in shared memory; those behind the last are passed by the
-// highest distance alone, whose bucket is the last.
-template <int N> __device__ inline void look_up(const BiasArgs &b, const int32_t *edges, const int (&d)[N], int (&at)[N])
-{
-#pragma unroll
-    for (int i = 0; i < N; ++i) at[i] = 0;
-    for (int s = b.top; s; s >>= 1)
-#pragma unroll
-        for (int i = 0; i < N; ++i) at[i] += edges[at[i] + s - 1] <= d[i] ? s : 0;
-#pragma unroll
-    for (int i = 0; i < N; ++i) at[i] = min(at[i], b.buckets - 1);
-}
-
 // The bucket that a thread is in: its number and the distances low .. top that are in it
 struct Bucket {
     int at, low, top;
