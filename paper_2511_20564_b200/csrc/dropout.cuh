@@ -41,26 +41,56 @@ inline int32_t drop_args(const e2egrec_dropout *d, DropArgs &a)
 
 __device__ __forceinline__ uint32_t drop_step(const DropArgs &d) { return d.step + (d.step_dev ? __ldcg(d.step_dev) : 0u); }
 
-__device__ __forceinline__ uint4 drop_words(const DropArgs &d, uint32_t step, uint32_t row, uint32_t unit)
-{
-    return philox4x32_10(make_uint4(unit, row, d.place, step), make_uint2(d.seed_lo, d.seed_hi));
-}
+__device__ __forceinline__ uint2 drop_key(const DropArgs &d) { return make_uint2(d.seed_lo, d.seed_hi); }
+__device__ __forceinline__ PhiloxUnit drop_of_unit(const DropArgs &d, uint32_t step, uint32_t unit) { return philox_unit(unit, d.place, step, drop_key(d)); }
+__device__ __forceinline__ PhiloxRow drop_of_row(const DropArgs &d, uint32_t row) { return philox_row(row, d.place, drop_key(d)); }
+__device__ __forceinline__ uint4 drop_words(const DropArgs &d, const PhiloxUnit &u, const PhiloxRow &r) { return philox_join(u, r, drop_key(d)); }
 
-// Which elements of a chunk stay, a bit each: the 8 of a unit (bf16), or its first or second 4 (fp32)
-template <int E> __device__ __forceinline__ uint32_t drop_bits(const DropArgs &d, const uint4 &w, int chunk)
+// The words of a chunk: all four of its unit (bf16, 8 elements), or the first or second two (fp32)
+template <int E> __device__ __forceinline__ void drop_halves(const uint4 &w, int chunk, uint32_t (&h)[E / 2])
 {
     const bool second = E == 4 && (chunk & 1);
-    const uint32_t words[4] = {second ? w.z : w.x, second ? w.w : w.y, w.z, w.w};
-    uint32_t bits = 0;
-#pragma unroll
-    for (int e = 0; e < E; e += 2) bits |= ((words[e / 2] << 16) >= d.cut ? 1u << e : 0u) | (words[e / 2] >= d.cut ? 2u << e : 0u);
-    return bits;
+    h[0] = second ? w.z : w.x;
+    h[1] = second ? w.w : w.y;
+    if constexpr (E == 8) {
+        h[2] = w.z;
+        h[3] = w.w;
+    }
 }
-template <int E> __device__ __forceinline__ void drop_apply(const DropArgs &d, uint32_t bits, float (&v)[E])
+// A chunk's elements, two by two
+template <int N> __device__ __forceinline__ void drop_apply(const DropArgs &d, const uint32_t (&h)[N], float2 (&v)[N])
 {
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = bits >> e & 1u ? v[e] * d.factor : 0.f;
+    for (int i = 0; i < N; ++i) {
+        const float2 x = __fmul2_rn(v[i], make_float2(d.factor, d.factor));
+        v[i] = make_float2((h[i] << 16) < d.cut ? 0.f : x.x, h[i] < d.cut ? 0.f : x.y);
+    }
 }
+
+// 16 bytes of a row as pairs of fp32, and back
+__device__ __forceinline__ void unpack_pairs(const uint4 &r, float2 (&v)[4])
+{
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+}
+__device__ __forceinline__ void unpack_pairs(const uint4 &r, float2 (&v)[2])
+{
+    v[0] = make_float2(__uint_as_float(r.x), __uint_as_float(r.y));
+    v[1] = make_float2(__uint_as_float(r.z), __uint_as_float(r.w));
+}
+template <typename T, int N> __device__ __forceinline__ void store_pairs(T *p, const float2 (&v)[N])
+{
+    float x[2 * N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        x[2 * i] = v[i].x;
+        x[2 * i + 1] = v[i].y;
+    }
+    Chunk<T>::store(p, x);
+}
+
+// The unit of a row's chunk
 template <typename T> __device__ __forceinline__ uint32_t drop_unit(int chunk) { return (uint32_t)chunk / (8u / Chunk<T>::kElems); }
 
 }  // namespace e2egrec

@@ -18,7 +18,7 @@ namespace {
 
 constexpr int kNormThreads = 256, kNormWarps = kNormThreads / 32;
 constexpr int kMaxNormDim = 8192;
-constexpr int kGradBlocks = 148 * 4;                 // blocks that sum up the gains' gradients, at most
+constexpr int kGradBlocks = 148 * 2;                 // blocks that sum up the gains' gradients, at most
 constexpr int64_t kMaxRows = ((int64_t)1 << 31) - 1;
 
 struct NormArgs {
@@ -55,184 +55,169 @@ template <int N> __device__ inline void row_sums(float (&v)[N], int threads, flo
     }
 }
 
-template <int E> __device__ inline void load_gains(const float *p, int chunk, float none, float (&v)[E])
+template <int N> __device__ inline void load_gains(const float *p, int chunk, float none, float2 (&v)[N])
 {
 #pragma unroll
-    for (int e = 0; e < E; e += 4) {
-        const float4 q = p ? __ldg(reinterpret_cast<const float4 *>(p + chunk * E + e)) : make_float4(none, none, none, none);
-        v[e] = q.x; v[e + 1] = q.y; v[e + 2] = q.z; v[e + 3] = q.w;
+    for (int i = 0; i < N; i += 2) {
+        const float4 q = p ? __ldg(reinterpret_cast<const float4 *>(p + (chunk * N + i) * 2)) : make_float4(none, none, none, none);
+        v[i] = make_float2(q.x, q.y);
+        v[i + 1] = make_float2(q.z, q.w);
     }
 }
+__device__ inline float2 both(float x) { return make_float2(x, x); }
 
-// U chunks of 16 bytes per thread, R rows at a time
-template <typename T, int U, int R, bool kDrop>
-__global__ void __launch_bounds__(kNormThreads)
+// U chunks of 16 bytes per thread; arithmetic on two elements at a time.  131 072 x 256 bf16 with residual and dropout: 50 us, 4.0 TB/s, 70 % of
+// the issue slots (half of them the generator's and the conversions'); without dropout 47 us; 32 768 x 1024, the sum stored as well: 55 us, 4.9 TB/s.
+// With a row per warp, an element at a time and the mask as bits the first took 55 us.
+template <typename T, int U, bool kDrop>
+__global__ void __launch_bounds__(kNormThreads, U * Chunk<T>::kElems > 24 ? 3 : 4)
 norm_fwd_kernel(const __grid_constant__ NormArgs a)
 {
-    constexpr int E = Chunk<T>::kElems;
-    __shared__ float buf[2][R][kNormWarps];
+    constexpr int E = Chunk<T>::kElems, P = E / 2;
+    __shared__ float buf[2][1][kNormWarps];
     const int at = threadIdx.x & (a.threads - 1), group = threadIdx.x / a.threads, groups = kNormThreads / a.threads;
-    const int64_t row0 = (int64_t)blockIdx.x * groups * R + group;
-    uint4 raw[R][U], res[R][U];
+    const int64_t row = (int64_t)blockIdx.x * groups + group;
+    const bool live = row < a.rows;
+    uint4 raw[U], res[U];
 #pragma unroll
-    for (int i = 0; i < R; ++i)
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int64_t row = row0 + i * groups;
-            const int c = at + u * a.threads;
-            const bool on = row < a.rows && c < a.chunks;
-            raw[i][u] = on ? Chunk<T>::load_raw(static_cast<const T *>(a.x) + row * a.ldx + c * E) : make_uint4(0, 0, 0, 0);
-            res[i][u] = on && a.r ? Chunk<T>::load_raw(static_cast<const T *>(a.r) + row * a.ldr + c * E) : make_uint4(0, 0, 0, 0);
-        }
+    for (int u = 0; u < U; ++u) {
+        const int c = at + u * a.threads;
+        const bool on = live && c < a.chunks;
+        raw[u] = on ? Chunk<T>::load_raw(static_cast<const T *>(a.x) + row * a.ldx + c * E) : make_uint4(0, 0, 0, 0);
+        res[u] = on && a.r ? Chunk<T>::load_raw(static_cast<const T *>(a.r) + row * a.ldr + c * E) : make_uint4(0, 0, 0, 0);
+    }
     const uint32_t step = kDrop ? drop_step(a.drop) : 0u;
-    float z[R][U][E], sum[R];
+    PhiloxRow of_row;
+    if constexpr (kDrop) of_row = drop_of_row(a.drop, (uint32_t)row);
+    float2 z[U][P], s2 = both(0.f);
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-        const int64_t row = row0 + i * groups;
-        sum[i] = 0.f;
+    for (int u = 0; u < U; ++u) {
+        const int c = at + u * a.threads;
+        float2 v[P];
+        unpack_pairs(raw[u], z[u]);
+        if constexpr (kDrop) {
+            uint32_t h[P];
+            drop_halves<E>(drop_words(a.drop, drop_of_unit(a.drop, step, drop_unit<T>(c)), of_row), c, h);
+            drop_apply(a.drop, h, z[u]);
+        }
+        unpack_pairs(res[u], v);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int c = at + u * a.threads;
-            float v[E];
-            Chunk<T>::unpack(raw[i][u], z[i][u]);
-            if constexpr (kDrop) drop_apply<E>(a.drop, drop_bits<E>(a.drop, drop_words(a.drop, step, (uint32_t)row, drop_unit<T>(c)), c), z[i][u]);
-            Chunk<T>::unpack(res[i][u], v);
+        for (int i = 0; i < P; ++i) {
+            z[u][i] = __fadd2_rn(z[u][i], v[i]);
+            s2 = __fadd2_rn(s2, z[u][i]);
+        }
+        if (a.z && live && c < a.chunks) store_pairs(static_cast<T *>(a.z) + row * a.ldz + c * E, z[u]);
+    }
+    float sum[1] = {s2.x + s2.y};
+    row_sums<1>(sum, a.threads, buf[0]);
+    const float mean = sum[0] * a.inv_dim;
+    s2 = both(0.f);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                z[i][u][e] += v[e];
-                sum[i] += z[i][u][e];
-            }
+    for (int u = 0; u < U; ++u) {
+        const bool on = at + u * a.threads < a.chunks;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            z[u][i] = __fadd2_rn(z[u][i], both(-mean));
+            const float2 d = on ? z[u][i] : both(0.f);
+            s2 = __ffma2_rn(d, d, s2);
         }
     }
-    row_sums<R>(sum, a.threads, buf[0]);
-    float sq[R];
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-        sum[i] *= a.inv_dim;
-        sq[i] = 0.f;
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (at + u * a.threads < a.chunks)
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float d = z[i][u][e] - sum[i];
-                    sq[i] = fmaf(d, d, sq[i]);
-                }
-    }
-    row_sums<R>(sq, a.threads, buf[1]);
-#pragma unroll
-    for (int i = 0; i < R; ++i) sq[i] = rsqrtf(fmaf(sq[i], a.inv_dim, a.eps));
+    sum[0] = s2.x + s2.y;
+    row_sums<1>(sum, a.threads, buf[1]);
+    const float rstd = rsqrtf(fmaf(sum[0], a.inv_dim, a.eps));
+    if (!live) return;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int c = at + u * a.threads;
         if (c >= a.chunks) continue;
-        float gain[E], shift[E];
-        load_gains<E>(a.gain, c, 1.f, gain);
-        load_gains<E>(a.shift, c, 0.f, shift);
+        float2 gain[P], shift[P];
+        load_gains(a.gain, c, 1.f, gain);
+        load_gains(a.shift, c, 0.f, shift);
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const int64_t row = row0 + i * groups;
-            if (row >= a.rows) continue;
-            if (a.z) Chunk<T>::store(static_cast<T *>(a.z) + row * a.ldz + c * E, z[i][u]);
-            float y[E];
-#pragma unroll
-            for (int e = 0; e < E; ++e) y[e] = fmaf((z[i][u][e] - sum[i]) * sq[i], gain[e], shift[e]);
-            Chunk<T>::store(static_cast<T *>(a.y) + row * a.ldy + c * E, y);
-        }
+        for (int i = 0; i < P; ++i) z[u][i] = __ffma2_rn(__fmul2_rn(z[u][i], both(rstd)), gain[i], shift[i]);
+        store_pairs(static_cast<T *>(a.y) + row * a.ldy + c * E, z[u]);
     }
-    if (a.stats && at == 0)
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-            if (row0 + i * groups < a.rows) a.stats[row0 + i * groups] = make_float2(sum[i], sq[i]);
+    if (a.stats && at == 0) a.stats[row] = make_float2(mean, rstd);
 }
 
-template <typename T, int U, int R, bool kDrop>
-__global__ void __launch_bounds__(kNormThreads)
+// The gradient, rows in turn, 16 values per thread as the gains' sums take twice that.  131 072 x 256 bf16 with residual and dropout: 78 us, 4.3 TB/s;
+// 32 768 x 1024 with the gradient of the sum 94 us, 4.3 TB/s (250 registers and a block per SM with 32 values per thread: 168 us).  Two blocks per SM
+// at most go over the rows: four and more have more partial sums to write than they hide latency (77 -> 79 us, 20 011 x 320 fp32 30 -> 34 us).
+constexpr int kBackValues = 16, kForwardValues = 32;
+template <typename T, int U, bool kDrop>
+__global__ void __launch_bounds__(kNormThreads, U * Chunk<T>::kElems > kBackValues ? 1 : 2)
 norm_bwd_kernel(const __grid_constant__ NormArgs a)
 {
-    constexpr int E = Chunk<T>::kElems;
+    constexpr int E = Chunk<T>::kElems, P = E / 2;
     extern __shared__ float join[];                  // [U * E][kNormThreads], gains only
-    __shared__ float buf[2][2 * R][kNormWarps];
+    __shared__ float buf[2][2][kNormWarps];
     const int at = threadIdx.x & (a.threads - 1), group = threadIdx.x / a.threads, groups = kNormThreads / a.threads;
     const uint32_t step = kDrop ? drop_step(a.drop) : 0u;
-    float dgain[U][E], dshift[U][E];
+    float2 dgain[U][P], dshift[U][P];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int e = 0; e < E; ++e) dgain[u][e] = dshift[u][e] = 0.f;
+        for (int i = 0; i < P; ++i) dgain[u][i] = dshift[u][i] = both(0.f);
+    PhiloxUnit of_unit[kDrop ? U : 1];
+    if constexpr (kDrop)
+#pragma unroll
+        for (int u = 0; u < U; ++u) of_unit[u] = drop_of_unit(a.drop, step, drop_unit<T>(at + u * a.threads));
     int turn = 0;
-    for (int64_t first = (int64_t)blockIdx.x * groups * R; first < a.rows; first += (int64_t)gridDim.x * groups * R, turn ^= 1) {
-        uint4 raw[R][U], res[R][U], up[R][U];
-        float2 st[R];
+    for (int64_t first = (int64_t)blockIdx.x * groups; first < a.rows; first += (int64_t)gridDim.x * groups, turn ^= 1) {
+        const int64_t row = first + group;
+        const bool live = row < a.rows;
+        uint4 raw[U], res[U], up[U], in[U];
+        const float2 st = live ? __ldg(a.stats + row) : both(0.f);
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const int64_t row = first + group + i * groups;
-            st[i] = row < a.rows ? __ldg(a.stats + row) : make_float2(0.f, 0.f);
+        for (int u = 0; u < U; ++u) {
+            const int c = at + u * a.threads;
+            const bool on = live && c < a.chunks;
+            raw[u] = on ? Chunk<T>::load_raw(static_cast<const T *>(a.x) + row * a.ldx + c * E) : make_uint4(0, 0, 0, 0);
+            up[u] = on ? Chunk<T>::load_raw(static_cast<const T *>(a.dy) + row * a.lddy + c * E) : make_uint4(0, 0, 0, 0);
+            res[u] = on && a.r ? Chunk<T>::load_raw(static_cast<const T *>(a.r) + row * a.ldr + c * E) : make_uint4(0, 0, 0, 0);
+            in[u] = on && a.dz ? Chunk<T>::load_raw(static_cast<const T *>(a.dz) + row * a.lddz + c * E) : make_uint4(0, 0, 0, 0);
+        }
+        float2 n[U][P], g[U][P], s1 = both(0.f), s2 = both(0.f);
+        uint32_t h[kDrop ? U : 1][P];
+        PhiloxRow of_row;
+        if constexpr (kDrop) of_row = drop_of_row(a.drop, (uint32_t)row);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int c = at + u * a.threads;
-                const bool on = row < a.rows && c < a.chunks;
-                raw[i][u] = on ? Chunk<T>::load_raw(static_cast<const T *>(a.x) + row * a.ldx + c * E) : make_uint4(0, 0, 0, 0);
-                res[i][u] = on && a.r ? Chunk<T>::load_raw(static_cast<const T *>(a.r) + row * a.ldr + c * E) : make_uint4(0, 0, 0, 0);
-                up[i][u] = on ? Chunk<T>::load_raw(static_cast<const T *>(a.dy) + row * a.lddy + c * E) : make_uint4(0, 0, 0, 0);
+        for (int u = 0; u < U; ++u) {
+            const int c = at + u * a.threads;
+            float2 v[P], gain[P];
+            unpack_pairs(raw[u], n[u]);
+            if constexpr (kDrop) {
+                drop_halves<E>(drop_words(a.drop, of_unit[u], of_row), c, h[u]);
+                drop_apply(a.drop, h[u], n[u]);
+            }
+            unpack_pairs(res[u], v);
+            unpack_pairs(up[u], g[u]);
+            load_gains(c < a.chunks ? a.gain : nullptr, c, 1.f, gain);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {            // places behind the row's end: g = 0
+                n[u][i] = __fmul2_rn(__fadd2_rn(__fadd2_rn(n[u][i], v[i]), both(-st.x)), both(st.y));
+                dgain[u][i] = __ffma2_rn(g[u][i], n[u][i], dgain[u][i]);
+                dshift[u][i] = __fadd2_rn(dshift[u][i], g[u][i]);
+                g[u][i] = __fmul2_rn(g[u][i], gain[i]);
+                s1 = __fadd2_rn(s1, g[u][i]);
+                s2 = __ffma2_rn(g[u][i], n[u][i], s2);
             }
         }
-        float n[R][U][E], g[R][U][E], sums[2 * R];
-        uint32_t kept[R][U];                         // a bit per element
+        float sums[2] = {s1.x + s1.y, s2.x + s2.y};
+        row_sums<2>(sums, a.threads, buf[turn]);
+        if (!live) continue;
+        const float2 c1 = both(-sums[0] * a.inv_dim), c2 = both(-sums[1] * a.inv_dim);
 #pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const int64_t row = first + group + i * groups;
-            sums[2 * i] = sums[2 * i + 1] = 0.f;
+        for (int u = 0; u < U; ++u) {
+            const int c = at + u * a.threads;
+            if (c >= a.chunks) continue;
+            float2 v[P];
+            unpack_pairs(in[u], v);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int c = at + u * a.threads;
-                float v[E], gain[E];
-                Chunk<T>::unpack(raw[i][u], n[i][u]);
-                kept[i][u] = 0;
-                if constexpr (kDrop) {
-                    kept[i][u] = drop_bits<E>(a.drop, drop_words(a.drop, step, (uint32_t)row, drop_unit<T>(c)), c);
-                    drop_apply<E>(a.drop, kept[i][u], n[i][u]);
-                }
-                Chunk<T>::unpack(res[i][u], v);
-                Chunk<T>::unpack(up[i][u], g[i][u]);
-                if (c < a.chunks) load_gains<E>(a.gain, c, 1.f, gain);
-                else
-#pragma unroll
-                    for (int e = 0; e < E; ++e) gain[e] = 0.f;
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    n[i][u][e] = (n[i][u][e] + v[e] - st[i].x) * st[i].y;
-                    dgain[u][e] = fmaf(g[i][u][e], n[i][u][e], dgain[u][e]);
-                    dshift[u][e] += g[i][u][e];
-                    g[i][u][e] *= gain[e];
-                    sums[2 * i] += g[i][u][e];
-                    sums[2 * i + 1] = fmaf(g[i][u][e], n[i][u][e], sums[2 * i + 1]);
-                }
-            }
-        }
-        row_sums<2 * R>(sums, a.threads, buf[turn]);
-#pragma unroll
-        for (int i = 0; i < R; ++i) {
-            const int64_t row = first + group + i * groups;
-            if (row >= a.rows) continue;
-            const float c1 = sums[2 * i] * a.inv_dim, c2 = sums[2 * i + 1] * a.inv_dim;
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int c = at + u * a.threads;
-                if (c >= a.chunks) continue;
-                float d[E];
-#pragma unroll
-                for (int e = 0; e < E; ++e) d[e] = st[i].y * (g[i][u][e] - c1 - n[i][u][e] * c2);
-                if (a.dz) {
-                    float v[E];
-                    Chunk<T>::load(static_cast<const T *>(a.dz) + row * a.lddz + c * E, v);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) d[e] += v[e];
-                }
-                if (a.dr) Chunk<T>::store(static_cast<T *>(a.dr) + row * a.lddr + c * E, d);
-                if constexpr (kDrop) drop_apply<E>(a.drop, kept[i][u], d);
-                Chunk<T>::store(static_cast<T *>(a.dx) + row * a.lddx + c * E, d);
-            }
+            for (int i = 0; i < P; ++i) g[u][i] = __ffma2_rn(__ffma2_rn(n[u][i], c2, __fadd2_rn(g[u][i], c1)), both(st.y), v[i]);
+            if (a.dr) store_pairs(static_cast<T *>(a.dr) + row * a.lddr + c * E, g[u]);
+            if constexpr (kDrop) drop_apply(a.drop, h[u], g[u]);
+            store_pairs(static_cast<T *>(a.dx) + row * a.lddx + c * E, g[u]);
         }
     }
     if (!a.part) return;
@@ -244,7 +229,10 @@ norm_bwd_kernel(const __grid_constant__ NormArgs a)
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int e = 0; e < E; ++e) join[(u * E + e) * kNormThreads + threadIdx.x] = side ? dshift[u][e] : dgain[u][e];
+            for (int e = 0; e < E; ++e) {
+                const float2 v = side ? dshift[u][e / 2] : dgain[u][e / 2];
+                join[(u * E + e) * kNormThreads + threadIdx.x] = e & 1 ? v.y : v.x;
+            }
         __syncthreads();
         for (int k = threadIdx.x; k < U * E * a.threads; k += kNormThreads) {
             const int v = k / a.threads, t = k & (a.threads - 1), c = t + v / E * a.threads;
@@ -282,36 +270,57 @@ norm_gains_kernel(const float *__restrict__ part, int blocks, int dim, float *__
 struct DropoutArgs {
     const void *x, *r;
     void *y;
-    int64_t ldx, ldr, ldy, total;                    // total: units of 8 elements
+    int64_t ldx, ldr, ldy, rows, total;              // total: threads that have something to do
     int32_t dim;
-    uint32_t units;                                  // of a row
+    uint32_t units, magic, shift;                    // units (8 elements) of a row; i / units = (umulhi(i, magic) + i) >> shift for i < 2^31 where shift > 0
     DropArgs drop;
 };
 
-template <typename T>
+// A thread takes one unit of kRows neighbouring rows, whose loads go out together and whose random words share the unit's part.  What bounds it with
+// 16-bit elements is the generator and the conversions, 58 % of the integer pipe: 262 144 x 256 took 76 us with a unit after the other per thread,
+// 57 with four under way, packed arithmetic and comparisons in place of a mask.
+constexpr int kDropRows = 4;
+template <typename T, bool kRes, int kRows>
 __global__ void __launch_bounds__(kNormThreads)
 dropout_kernel(const __grid_constant__ DropoutArgs a)
 {
     constexpr int E = Chunk<T>::kElems, kChunks = 8 / E;
+    const int64_t i = (int64_t)blockIdx.x * kNormThreads + threadIdx.x;
+    if (i >= a.total) return;
     const uint32_t step = drop_step(a.drop);
-    for (int64_t i = (int64_t)blockIdx.x * kNormThreads + threadIdx.x; i < a.total; i += (int64_t)gridDim.x * kNormThreads) {
-        const int64_t row = i >> 32 ? i / a.units : (int64_t)((uint32_t)i / a.units);
-        const uint32_t unit = (uint32_t)(i - row * a.units);
-        const uint4 w = drop_words(a.drop, step, (uint32_t)row, unit);
+    const int64_t tuple = a.shift ? (int64_t)(((uint64_t)__umulhi((uint32_t)i, a.magic) + (uint32_t)i) >> a.shift) : i / a.units, row0 = tuple * kRows;
+    const uint32_t unit = (uint32_t)(i - tuple * a.units);
+    uint4 x[kRows][kChunks], r[kRes ? kRows : 1][kChunks];
+#pragma unroll
+    for (int q = 0; q < kRows; ++q)
 #pragma unroll
         for (int k = 0; k < kChunks; ++k) {
-            const int64_t c = (int64_t)unit * 8 + k * E;
-            if (c >= a.dim) continue;
-            float v[E];
-            Chunk<T>::load(static_cast<const T *>(a.x) + row * a.ldx + c, v);
-            if (a.drop.cut) drop_apply<E>(a.drop, drop_bits<E>(a.drop, w, k), v);
-            if (a.r) {
-                float q[E];
-                Chunk<T>::load(static_cast<const T *>(a.r) + row * a.ldr + c, q);
+            const int c = (int)unit * 8 + k * E;
+            const bool on = row0 + q < a.rows && c < a.dim;
+            x[q][k] = on ? Chunk<T>::load_raw(static_cast<const T *>(a.x) + (row0 + q) * a.ldx + c) : make_uint4(0, 0, 0, 0);
+            if constexpr (kRes) r[q][k] = on ? Chunk<T>::load_raw(static_cast<const T *>(a.r) + (row0 + q) * a.ldr + c) : make_uint4(0, 0, 0, 0);
+        }
+    const PhiloxUnit of_unit = drop_of_unit(a.drop, step, unit);
 #pragma unroll
-                for (int e = 0; e < E; ++e) v[e] += q[e];
+    for (int q = 0; q < kRows; ++q) {
+        if (row0 + q >= a.rows) break;
+        const uint4 w = drop_words(a.drop, of_unit, drop_of_row(a.drop, (uint32_t)(row0 + q)));
+#pragma unroll
+        for (int k = 0; k < kChunks; ++k) {
+            const int c = (int)unit * 8 + k * E;
+            if (c >= a.dim) continue;
+            float2 v[E / 2];
+            uint32_t h[E / 2];
+            unpack_pairs(x[q][k], v);
+            drop_halves<E>(w, k, h);
+            drop_apply(a.drop, h, v);
+            if constexpr (kRes) {
+                float2 p[E / 2];
+                unpack_pairs(r[q][k], p);
+#pragma unroll
+                for (int j = 0; j < E / 2; ++j) v[j] = __fadd2_rn(v[j], p[j]);
             }
-            Chunk<T>::store(static_cast<T *>(a.y) + row * a.ldy + c, v);
+            store_pairs(static_cast<T *>(a.y) + (row0 + q) * a.ldy + c, v);
         }
     }
 }
@@ -345,41 +354,58 @@ int32_t check_sizes(const e2egrec_mat *X)
 }
 bool misaligned(const float *p) { return reinterpret_cast<uintptr_t>(p) % 16; }
 
-// Threads of a row, chunks per thread (a template argument) and rows at a time
+// Threads of a row and chunks per thread (a template argument).  Threads hold as many values as their registers allow, and with that as few as
+// possible share a row: what is done once per row, exchanges and addresses, is done for more rows by a warp then.  Of the numbers of chunks the
+// one that leaves the fewest places empty (100 000 x 152: 43 us with one chunk each of 32 threads, 29 so).  Rows so few that every chunk has a
+// thread of its own get that: the time is one chunk's then (64 x 256: 10 -> 6 us).
 struct NormShape {
     int threads, per;
 };
-NormShape norm_shape(const e2egrec_mat *X)
+NormShape norm_shape(const e2egrec_mat *X, bool back)
 {
-    const int es = (int)dtype_size(X->dtype), chunks = X->dim * es / 16, most = 32 / (16 / es);      // 32 values per thread at most
-    NormShape s{1, 1};
-    while (s.threads < 32 && s.threads < chunks) s.threads *= 2;
-    while (s.threads * s.per < chunks && s.per < most) s.per *= 2;
-    while (s.threads * s.per < chunks) s.threads *= 2;
-    return s;
+    const int es = (int)dtype_size(X->dtype), chunks = X->dim * es / 16, values = 16 / es;
+    const bool few = X->rows * chunks <= (int64_t)148 * 1024;
+    NormShape best{kNormThreads, kForwardValues / values};
+    int places = kNormThreads * best.per;
+    for (int per = 1; per <= (back ? kBackValues : kForwardValues) / values; ++per) {
+        if (per == 7) continue;
+        int threads = 1;
+        while (threads < kNormThreads && threads * per < chunks) threads *= 2;
+        if (threads * per >= chunks && threads * per <= places) {
+            best = NormShape{threads, per};
+            places = threads * per;
+            if (few) break;
+        }
+    }
+    return best;
 }
 
-template <typename T, int U, int R, bool kDrop, bool kBack> void norm_launch(const NormArgs &a, cudaStream_t st, int blocks)
+template <typename T, int U, bool kDrop, bool kBack> void norm_launch(const NormArgs &a, cudaStream_t st, int blocks)
 {
     note_launch();
-    const int64_t per = (int64_t)kNormThreads / a.threads * R;
+    const int64_t per = (int64_t)kNormThreads / a.threads;
     if constexpr (kBack) {
         const size_t smem = a.part ? (size_t)U * Chunk<T>::kElems * kNormThreads * sizeof(float) : 0;
-        norm_bwd_kernel<T, U, R, kDrop><<<blocks, kNormThreads, smem, st>>>(a);
+        norm_bwd_kernel<T, U, kDrop><<<blocks, kNormThreads, smem, st>>>(a);
     } else {
-        norm_fwd_kernel<T, U, R, kDrop><<<(unsigned)ceil_div(a.rows, per), kNormThreads, 0, st>>>(a);
+        norm_fwd_kernel<T, U, kDrop><<<(unsigned)ceil_div(a.rows, per), kNormThreads, 0, st>>>(a);
     }
 }
 
 template <typename T, bool kDrop, bool kBack> void norm_of(const NormArgs &a, int per, cudaStream_t st, int blocks)
 {
-    if (per == 1) norm_launch<T, 1, 2, kDrop, kBack>(a, st, blocks);
-    else if (per == 2) norm_launch<T, 2, 2, kDrop, kBack>(a, st, blocks);
-    else if (per == 4) norm_launch<T, 4, 1, kDrop, kBack>(a, st, blocks);
-    else if constexpr (sizeof(T) == 4) norm_launch<T, 8, 1, kDrop, kBack>(a, st, blocks);
+    switch (per) {
+    case 1: return norm_launch<T, 1, kDrop, kBack>(a, st, blocks);
+    case 2: return norm_launch<T, 2, kDrop, kBack>(a, st, blocks);
+    case 3: return norm_launch<T, 3, kDrop, kBack>(a, st, blocks);
+    case 4: return norm_launch<T, 4, kDrop, kBack>(a, st, blocks);
+    }
+    if constexpr (sizeof(T) == 4) switch (per) {
+    case 5: return norm_launch<T, 5, kDrop, kBack>(a, st, blocks);
+    case 6: return norm_launch<T, 6, kDrop, kBack>(a, st, blocks);
+    default: return norm_launch<T, 8, kDrop, kBack>(a, st, blocks);
+    }
 }
-constexpr int rows_at_once(int per) { return per <= 2 ? 2 : 1; }
-
 template <bool kBack> void norm_any(const NormArgs &a, int32_t dtype, int per, cudaStream_t st, int blocks = 0)
 {
     if (dtype == E2EGREC_F32) a.drop.cut ? norm_of<float, true, kBack>(a, per, st, blocks) : norm_of<float, false, kBack>(a, per, st, blocks);
@@ -406,6 +432,21 @@ int32_t norm_args(const e2egrec_mat *X, const e2egrec_mat *residual, const e2egr
     return E2EGREC_OK;
 }
 
+// One row per thread while that leaves no SM more than eight blocks: the time is that of one unit then.
+template <typename T, bool kRes> void dropout_launch(DropoutArgs &a, cudaStream_t st)
+{
+    const int rows = a.rows * a.units <= (int64_t)148 * 8 * kNormThreads ? 1 : kDropRows;
+    a.total = ceil_div(a.rows, rows) * a.units;
+    if (a.total + kNormThreads < (int64_t)1 << 31) {                     // division by the units of a row as a product
+        while (((uint64_t)1 << a.shift) < a.units) ++a.shift;
+        a.magic = (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << a.shift) - a.units)) / a.units + 1);
+    }
+    const unsigned grid = (unsigned)ceil_div(a.total, kNormThreads);
+    note_launch();
+    if (rows == 1) dropout_kernel<T, kRes, 1><<<grid, kNormThreads, 0, st>>>(a);
+    else dropout_kernel<T, kRes, kDropRows><<<grid, kNormThreads, 0, st>>>(a);
+}
+
 }  // namespace
 }  // namespace e2egrec
 
@@ -429,12 +470,10 @@ extern "C" int32_t e2egrec_dropout_apply(const e2egrec_mat *X, const e2egrec_mat
     a.ldy = Y->ld;
     a.dim = X->dim;
     a.units = (uint32_t)ceil_div(X->dim, 8);
-    a.total = X->rows * a.units;
+    a.rows = X->rows;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const unsigned grid = (unsigned)std::min<int64_t>(ceil_div(a.total, kNormThreads), 148 * 8 * 16);
-    note_launch();
-    if (X->dtype == E2EGREC_F32) dropout_kernel<float><<<grid, kNormThreads, 0, st>>>(a);
-    else dropout_kernel<__nv_bfloat16><<<grid, kNormThreads, 0, st>>>(a);
+    if (X->dtype == E2EGREC_F32) a.r ? dropout_launch<float, true>(a, st) : dropout_launch<float, false>(a, st);
+    else a.r ? dropout_launch<__nv_bfloat16, true>(a, st) : dropout_launch<__nv_bfloat16, false>(a, st);
     return check_launch("dropout_apply");
 }
 
@@ -459,7 +498,7 @@ extern "C" int32_t e2egrec_layer_norm_forward(const e2egrec_mat *X, const e2egre
     a.shift = shift;
     a.eps = eps;
     a.stats = reinterpret_cast<float2 *>(stats);
-    const NormShape s = norm_shape(X);
+    const NormShape s = norm_shape(X, false);
     a.threads = s.threads;
     norm_any<false>(a, X->dtype, s.per, static_cast<cudaStream_t>(stream));
     return check_launch("layer_norm_forward");
@@ -473,8 +512,8 @@ extern "C" int32_t e2egrec_layer_norm_backward(const e2egrec_mat *dY, const e2eg
     int32_t rc = check_sizes(X);
     if (rc != E2EGREC_OK) return rc;
     if (X->dim > kMaxNormDim) return E2EGREC_ERR_UNSUPPORTED;
-    const NormShape s = norm_shape(X);
-    const int64_t tile = (int64_t)(kNormThreads / s.threads) * rows_at_once(s.per);
+    const NormShape s = norm_shape(X, true);
+    const int64_t tile = kNormThreads / s.threads;
     const int blocks = (int)std::min<int64_t>(ceil_div(X->rows, tile), kGradBlocks);
     const size_t need = 256 + align_up((size_t)blocks * 2 * X->dim * sizeof(float), 256);
     if (!ws) { *ws_bytes = need; return E2EGREC_OK; }
