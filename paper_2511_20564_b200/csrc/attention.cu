@@ -206,10 +206,11 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
         if (!backward) p.ml_bytes = align_up(p.splits * cells * sizeof(float2), 256);
     }
     if (backward && a.bias.buckets) {
-        p.table = few_table_plan(a, dtype);
-        p.table_fused = p.path == Path::tc ? a.bias.buckets * a.group <= kTcBins : p.path == Path::simt && simt_forms_table(a, p.simt);
-        p.table_rows = p.path == Path::few || !p.table_fused ? p.table.seq_slices * p.table.row_slices
-                                                              : a.n_seq * (p.path == Path::tc ? p.q_tiles : p.simt.q_tiles * p.simt.splits);
+        p.table = few_table_plan(a, k, dtype);
+        const int64_t slices = p.table.seq_slices * p.table.row_slices * p.table.key_slices;
+        p.table_fused = p.path == Path::tc ? a.bias.buckets * a.group <= kTcBins : p.path == Path::simt ? simt_forms_table(a, p.simt) : p.few.both;
+        p.table_rows = !p.table_fused ? slices
+                                      : p.path == Path::few ? p.few.blocks : a.n_seq * (p.path == Path::tc ? p.q_tiles : p.simt.q_tiles * p.simt.splits);
         p.table_bytes = align_up((size_t)p.table_rows * a.bias.buckets * a.kv_heads * a.group * sizeof(float), 256);
     }
     return p;
@@ -387,10 +388,10 @@ static int32_t attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q,
         ok = simt_attention_backward(a, plan.simt, part_dq, dots, plan.table_fused && dtable ? table_part : nullptr, st);
         if (ok && plan.splits > 1 && a.q_rows) join_dq(a, plan.splits, Q->dtype, false, part_dq, nullptr, st);
     } else {
-        ok = few_attention_backward(a, plan.few, Q->dtype, part_dq, dots, st);
+        ok = few_attention_backward(a, plan.few, Q->dtype, part_dq, dots, dtable ? table_part : nullptr, st);
     }
     if (ok && dtable) {
-        if (!plan.table_fused) ok = few_attention_table(a, plan.table, Q->dtype, table_part, st);
+        if (!plan.table_fused) ok = few_attention_table(a, plan.table, Q->dtype, dots, table_part, st);
         if (ok) launch_colsum<float>(table_part, table_size, nullptr, nullptr, plan.table_rows, table_size, 0, dtable, st);
     }
     if (!ok) return launch_refused("attention_backward");

@@ -141,18 +141,21 @@ struct FewPlan {
     int64_t batches;                      // units of rows per sequence and key head
     int warps, splits;                    // warps per unit, stretches of the keys
     int64_t key_batches;                  // units of keys of the dK, dV kernel
+    int64_t blocks;                       // of the kernel of all gradients, each of which leaves a row of the table's gradient
 };
 FewPlan few_plan(const AttnArgs &a, const Lengths &q, const Lengths &k, int es, bool backward);
 bool few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_o, float2 *part_ml, cudaStream_t st);
 // part_dq: [splits x q_rows x heads x head_dim] where splits > 1, twice that and [splits x q_rows x heads] with fit; dots: [q_rows x heads] where !both
-bool few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st);
+// table_part: with both and a bias [blocks, buckets x heads], or null where the table's gradient is not wanted
+bool few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, float *table_part, cudaStream_t st);
 
-// Gradient of the table of biases: part [slices x buckets x heads], one row per slice of the sequences' rows, which the caller adds up
+// Gradient of the table of biases where no other kernel forms it: part [slices x buckets x heads], a row per slice of the sequences, of their rows and
+// of their keys, which the caller adds up; dots: D of every row, made good for the rounding of the stored out
 struct TablePlan {
-    int64_t seq_slices, row_slices;       // slices of the sequences, and of each one's rows
+    int64_t seq_slices, row_slices, key_slices;
 };
-TablePlan few_table_plan(const AttnArgs &a, int32_t dtype);
-bool few_attention_table(const AttnArgs &a, const TablePlan &p, int32_t dtype, float *part, cudaStream_t st);
+TablePlan few_table_plan(const AttnArgs &a, const Lengths &k, int32_t dtype);
+bool few_attention_table(const AttnArgs &a, const TablePlan &p, int32_t dtype, const float *dots, float *part, cudaStream_t st);
 
 // dQ of stretches of the keys -> dQ, in order; with fit what D lacks is added to dots (where there are any)
 void join_dq(const AttnArgs &a, int splits, int32_t dtype, bool fit, const float *part_dq, float *dots, cudaStream_t st);

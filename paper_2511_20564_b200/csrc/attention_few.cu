@@ -10,6 +10,7 @@
 // at the end, in a fixed order.  A unit is up to R rows of one sequence and of each of its key heads.
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "attention.cuh"
 #include "ring_turns.h"
@@ -98,6 +99,7 @@ struct FewShape {
     int splits;                                      // stretches of the keys
     uint32_t units;
     int slice, packed;                               // bytes of a row's heads of a warp; whether those of consecutive rows are one stretch
+    int ring_bytes;                                  // of all rings; bins follow
 };
 
 // A warp's ring: turns of `keys` rows of K and of V (its heads' slice of them), visible rows as bits beside them.  Turn t of the warp is
@@ -289,11 +291,51 @@ template <int R> struct TurnBias {
 #pragma unroll
         for (int r = 0; r < R; ++r) buckets[r] = bucket_of(a.bias, a.bias.edges, apart(mine, pos[r]));
     }
-    __device__ inline float of(const AttnArgs &a, int r, int key) const
+    __device__ inline int bucket(int r, int key) const { return __shfl_sync(0xFFFFFFFFu, buckets[r], key); }
+    __device__ inline float value(const AttnArgs &a, int r, int bucket) const { return bias_at(a.bias, a.kv_heads * a.group, bucket, col[r]); }
+    __device__ inline float of(const AttnArgs &a, int r, int key) const { return value(a, r, bucket(r, key)); }
+};
+
+// Sums of dS by bucket that a warp keeps in shared memory.  Every key of a step and head has bins of its own, [rows x buckets x slots], so no two
+// lanes meet; the rows' bins go to the warp's sums, [buckets x heads of the warp], at the end of its rows.
+struct WarpBins {
+    float *bins, *sums;
+    int slots, nb, rows, columns;                        // slots: 32 / lanes; columns: heads of the warp
+    __device__ inline void clear(const AttnArgs &a, const FewShape &f, float *smem, int rows, int warp, int lane)
     {
-        return bias_at(a.bias, a.kv_heads * a.group, __shfl_sync(0xFFFFFFFFu, buckets[r], key), col[r]);
+        slots = 32 / f.lanes;
+        nb = a.bias.buckets;
+        this->rows = rows;
+        columns = f.heads * a.group;
+        bins = smem + (size_t)warp * nb * (rows * slots + columns);
+        sums = bins + nb * rows * slots;
+        for (int i = lane; i < nb * (rows * slots + columns); i += 32) bins[i] = 0.f;
+        __syncwarp();
+    }
+    __device__ inline void add(int r, int bucket, int slot, float v) { bins[(r * nb + bucket) * slots + slot] += v; }
+    // the bins of rows g, g + 1, ... of the group -> sums
+    __device__ inline void flush(const AttnArgs &a, const FewShape &f, int g, int lane)
+    {
+        __syncwarp();
+        for (int r = 0; r < rows; ++r) {
+            for (int i = lane; i < nb * f.heads; i += 32) {
+                float v = 0.f;
+                for (int k = i % f.heads; k < slots; k += f.heads) {
+                    float &bin = bins[(r * nb + i / f.heads) * slots + k];
+                    v += bin;
+                    bin = 0.f;
+                }
+                sums[i / f.heads * columns + i % f.heads * a.group + g] += v;
+            }
+            __syncwarp();
+            g = g + 1 == a.group ? 0 : g + 1;
+        }
     }
 };
+inline size_t bins_bytes(const AttnArgs &a, const FewShape &f, int rows)
+{
+    return (size_t)kFewWarps * a.bias.buckets * (rows * (32 / f.lanes) + f.heads * a.group) * sizeof(float);
+}
 
 // Rows of a unit one after the other: query row and head of (query, head of the group) pair r0, r0 + 1, ...
 struct RowWalk {
@@ -705,9 +747,11 @@ template <typename T, int U, int CPL> __device__ __noinline__ void clear_hidden(
 // (a turn holds all keys, the caller said) longer sequences go over their keys twice (lacking).
 template <typename T, int R, int U, int CPL, bool kBoth, bool kFit, bool kBias>
 __global__ void __launch_bounds__(kFewThreads, CPL == 2 || R > 2 ? 2 : (R == 1 ? 4 : 3))
-attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_dq, float *__restrict__ dots)
+attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_dq, float *__restrict__ dots,
+                    float *__restrict__ table_part)
 {
     constexpr int E = Piece<T, CPL>::E;
+    constexpr bool kTwice = kBias && kBoth && sizeof(T) == 2;
     extern __shared__ __align__(16) uint8_t ring_smem[];
     __shared__ uint64_t bars[kFewWarps * kStages];
     __shared__ uint32_t seen_words[kFewWarps * kStages];
@@ -726,6 +770,9 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     Ring ring = ring_of<U>(a, f, sizeof(T), ring_smem, bars, seen_words, warp, lane);
     ring_keys(ring, a, f, sizeof(T), x.kb, x.ke, x.hg, wu);
     const uint32_t mine = (uint32_t)(lane / f.lanes % f.heads * a.head_dim * (int)sizeof(T));       // the lane's head in a slice
+    const bool binned = kBias && kBoth && table_part != nullptr;
+    WarpBins bins;
+    if (binned) bins.clear(a, f, reinterpret_cast<float *>(ring_smem + f.ring_bytes), R, warp, lane);
     __syncthreads();
     for (int64_t n = 0;; ++n) {
         const int64_t r0 = (x.first + n * f.batches) * R;
@@ -740,7 +787,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         if constexpr (kBias)
             if (live) bias.fetch(a, x, ring, 0);
         RowSums<R> lack = {};
-        if constexpr (sizeof(T) == 2 && !kFit)
+        if constexpr (sizeof(T) == 2 && !kFit && !kTwice)
             if (live && !one_turn) lack = lacking<T, R, CPL, kBias>(a, f, unit, r0);       // one warp per unit and one stretch: few_plan
         RowWalk in(a, x, r0);
 #pragma unroll
@@ -760,7 +807,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     lse[r] = v * kLog2e;
                     p.load(static_cast<const T *>(a.q) + row * a.ldq + col, at, f.lanes, f.chunks);
                     t.load(static_cast<const T *>(a.dout) + row * a.ldg + col, at, f.lanes, f.chunks);
-                    if (!one_turn) {
+                    if (!one_turn && !kTwice) {
                         Piece<T, CPL> s;
                         s.load(static_cast<const T *>(a.o) + row * a.ldo + col, at, f.lanes, f.chunks);
                         float y[E];
@@ -780,9 +827,86 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 for (int e = 0; e < E; ++e) mean[r][e] = 0.f;
         }
         key_sums<R>(d, f.lanes);
-        if constexpr (sizeof(T) == 2 && !kFit)
+        if constexpr (sizeof(T) == 2 && !kFit && !kTwice)
 #pragma unroll
             for (int r = 0; r < R; ++r) d[r] += lack.of[r];
+        if constexpr (kTwice)
+            if (f.warps > 1 || !one_turn) {                  // (the unit's warps go this way together)
+                float total[R];
+#pragma unroll
+                for (int r = 0; r < R; ++r) total[r] = 0.f;
+                for (int t = 0; live && t < ring.turns && ring.ok; ++t) {
+                    uint32_t word;
+                    const uint32_t at_k = ring.wait(word, t, &abort_flag) + grp * f.slice + mine, at_v = at_k + ring.half;
+                    if (!ring.ok) {
+                        ring.land(t);
+                        break;
+                    }
+                    float s[2 * R * U];
+                    bool seen[U];
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        seen[u] = x.on && (word >> (u * kpw + grp) & 1u);
+                        Piece<T, CPL> k, v;
+                        float w[E], y[E];
+                        k.zero();
+                        v.zero();
+                        if (seen[u]) {
+                            k.load_shared(at_k + u * kpw * f.slice, at, f.lanes, f.chunks);
+                            v.load_shared(at_v + u * kpw * f.slice, at, f.lanes, f.chunks);
+                        }
+                        k.widen(w);
+                        v.widen(y);
+#pragma unroll
+                        for (int r = 0; r < R; ++r) {
+                            s[r * U + u] = dot<E>(q[r], w);
+                            s[(R + r) * U + u] = dot<E>(g[r], y);
+                        }
+                    }
+                    key_sums<2 * R * U>(s, f.lanes);
+                    bias.turn(a, x, ring, t);
+#pragma unroll
+                    for (int i = 0; i < R * U; ++i) {
+                        const float add = bias.of(a, i / U, i % U * kpw + grp) - lse[i / U];
+                        const float p = seen[i % U] ? exp2_fast(fmaf(s[i], c1, add)) : 0.f;
+                        total[i / U] += p;
+                        d[i / U] += p == 0.f ? 0.f : p * s[R * U + i];
+                    }
+                    ring.done(t);
+                }
+                if (live) ring.used += ring.turns;
+                for (int o = wide; o < 32; o <<= 1)
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        total[r] += __shfl_xor_sync(0xFFFFFFFFu, total[r], o);
+                        d[r] += __shfl_xor_sync(0xFFFFFFFFu, d[r], o);
+                    }
+                if (f.warps > 1) {
+                    __syncthreads();
+                    if (grp == 0)
+#pragma unroll
+                        for (int r = 0; r < R; ++r) {
+                            join[warp][2 * r * 32 + lane] = total[r];
+                            join[warp][(2 * r + 1) * 32 + lane] = d[r];
+                        }
+                    __syncthreads();
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        total[r] = d[r] = 0.f;
+                        for (int w = 0; w < f.warps; ++w) {
+                            total[r] += join[warp - wu + w][2 * r * 32 + lane % wide];
+                            d[r] += join[warp - wu + w][(2 * r + 1) * 32 + lane % wide];
+                        }
+                    }
+                    __syncthreads();
+                }
+#pragma unroll
+                for (int r = 0; r < R; ++r) d[r] = total[r] == 0.f ? 0.f : d[r] / total[r];
+                if (live) {
+                    bias.fetch(a, x, ring, 0);
+                    ring.start();
+                }
+            }
         for (int t = 0; live && t < ring.turns && ring.ok; ++t) {
             uint32_t word;
             const uint32_t at_k = ring.wait(word, t, &abort_flag) + grp * f.slice + mine, at_v = at_k + ring.half;
@@ -813,13 +937,18 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 }
             }
             key_sums<2 * R * U>(s, f.lanes);
-            if constexpr (kBias) bias.turn(a, x, ring, t);
+            int bucket[kBias ? R * U : 1];
+            if constexpr (kBias) {
+                bias.turn(a, x, ring, t);
+#pragma unroll
+                for (int i = 0; i < R * U; ++i) bucket[i] = bias.bucket(i / U, i % U * kpw + grp);
+            }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     float base = -lse[r];
-                    if constexpr (kBias) base += bias.of(a, r, u * kpw + grp);
+                    if constexpr (kBias) base += bias.value(a, r, bucket[r * U + u]);
                     s[r * U + u] = seen[u] ? exp2_fast(fmaf(s[r * U + u], c1, base)) : 0.f;
                 }
                 if (one_turn) {
@@ -840,6 +969,8 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 for (int u = 0; u < U; ++u) {
                     s[(R + r) * U + u] = seen[u] ? s[r * U + u] * (s[(R + r) * U + u] - d[r]) : 0.f;
                     rest[r] += s[(R + r) * U + u];
+                    if constexpr (kBias && kBoth)
+                        if (binned && at == 0 && seen[u]) bins.add(r, bucket[r * U + u], lane / f.lanes, s[(R + r) * U + u]);
                 }
             }
 #pragma unroll
@@ -872,6 +1003,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             ring.done(t);
         }
         if (live) ring.used += ring.turns;
+        if (binned && live) bins.flush(a, f, (int)(r0 % a.group), lane);
         for (int o = wide; o < 32; o <<= 1)
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -945,6 +1077,21 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
     if (kBoth && x.any && !whole)
         for (int64_t j0 = x.kb + (int64_t)wu * kKeys * kpw; j0 < x.ke; j0 += (int64_t)f.warps * kKeys * kpw)
             keys_gradients<T, CPL, kBias>(a, x.rg, x.h, x.on, j0, x.ke, grp, at, f, nullptr);
+    if (binned) {                                            // the block's warps, in order, each with its group of key heads
+        __syncthreads();
+        const int nb = a.bias.buckets, per = f.heads * a.group;
+        const float *sums = reinterpret_cast<float *>(ring_smem + f.ring_bytes) + nb * R * bins.slots;
+        for (int i = threadIdx.x; i < nb * heads; i += kFewThreads) {
+            const int b = i / heads, head = i % heads;
+            float v = 0.f;
+            for (int w = 0; w < kFewWarps; ++w) {
+                const uint32_t u = blockIdx.x * (uint32_t)(kFewWarps / f.warps) + w / f.warps;
+                const int hg = (int)(u / (uint32_t)(f.batches * f.splits) % (uint32_t)f.head_groups), at = head - hg * per;
+                if (u < f.units && at >= 0 && at < per) v += sums[w * nb * (R * bins.slots + per) + b * per + at];
+            }
+            table_part[(int64_t)blockIdx.x * nb * heads + i] = v;
+        }
+    }
 }
 
 // dK and dV where the rows of a sequence do not fit one unit
@@ -965,69 +1112,64 @@ attn_few_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         keys_gradients<T, CPL, kBias>(a, rg, h, h < a.kv_heads, j0, rg.k1, lane / wide, lane & (f.lanes - 1), f, dots);
 }
 
-// Gradient of the table of biases: dtable_bh = sum of dS over the pairs whose distance is in bucket b.  A warp takes every slices-th row of
-// a slice of the sequences, of its head group's key heads and one query head g of theirs.  Of a row it adds up, by bucket, a = sum p (dP - D)
-// with D from the stored out, and m = sum p; what D lacks, r = sum a / sum m over all buckets, is known at the row's end, and a - r m is the
-// row's part.  Lane groups (a key each) have bins of their own and keep the bucket that they are in in registers, so no two lanes meet.
+// Gradient of the table of biases: dtable_bh = sum of dS over the pairs whose distance is in bucket b.  A warp takes every row_slices-th row of
+// a slice of the sequences, a stretch of the keys, its head group's key heads and one query head g of theirs.  Lane groups (a key each) have bins
+// of their own and keep the bucket that they are in in registers, so no two lanes meet.
 template <typename T, int CPL>
 __global__ void __launch_bounds__(kFewThreads)
-attn_few_table_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, int64_t seq_slices, int64_t row_slices, float *__restrict__ part)
+attn_few_table_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, const __grid_constant__ TablePlan slices,
+                      const float *__restrict__ dots, float *__restrict__ part)
 {
     constexpr int E = Piece<T, CPL>::E, U = 4;
-    extern __shared__ float2 bins_smem[];
+    extern __shared__ float bins_smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wide = f.lanes * f.heads, grp = lane / wide, at = lane & (f.lanes - 1), kpw = 32 / wide;
-    const int heads = a.kv_heads * a.group, nb = a.bias.buckets, local = lane / f.lanes % f.heads;
+    const int heads = a.kv_heads * a.group, nb = a.bias.buckets, slots = 32 / f.lanes;
     uint32_t u = blockIdx.x * (uint32_t)kFewWarps + warp;
     if (u >= f.units) return;
     const int g = (int)(u % (uint32_t)a.group);
     u /= (uint32_t)a.group;
     const int hg = (int)(u % (uint32_t)f.head_groups);
     u /= (uint32_t)f.head_groups;
-    const int64_t slice = u, s0 = slice / row_slices, r0 = slice % row_slices;
-    const int h = hg * f.heads + local, head = h * a.group + g;
+    const int64_t slice = u, z = slice % slices.key_slices, r0 = slice / slices.key_slices % slices.row_slices, s0 = slice / slices.key_slices / slices.row_slices;
+    const int h = hg * f.heads + lane / f.lanes % f.heads, head = h * a.group + g;
     const bool on = h < a.kv_heads;
     const int64_t koff = h * (int64_t)a.head_dim, qoff = head * (int64_t)a.head_dim;
     const float c1 = a.scale * kLog2e;
-    // bins of (bucket, key of a step, head): float2 (a, m); behind them the warp's sums of the rows, (bucket, head)
-    float2 *bins = bins_smem + (size_t)warp * nb * (32 / f.lanes);
-    float *sums = reinterpret_cast<float *>(bins_smem + (size_t)kFewWarps * nb * (32 / f.lanes)) + (size_t)warp * nb * f.heads;
-    for (int i = lane; i < nb * (32 / f.lanes); i += 32) bins[i] = make_float2(0.f, 0.f);
-    for (int i = lane; i < nb * f.heads; i += 32) sums[i] = 0.f;
+    float *bins = bins_smem + (size_t)warp * nb * slots, *mine = bins + lane / f.lanes;      // [buckets x slots]
+    for (int i = lane; i < nb * slots; i += 32) bins[i] = 0.f;
     __syncwarp();
-    float2 *mine = bins + lane / f.lanes;                // stride 32 / lanes
-    for (int64_t s = s0; s < a.n_seq; s += seq_slices) {
+    float run = 0.f;
+    int cur = 0;
+    for (int64_t s = s0; s < a.n_seq; s += slices.seq_slices) {
         const SeqRange rg = seq_range(a, s, false);
-        for (int64_t row = rg.q0 + r0; row < rg.q1; row += row_slices) {
+        const int64_t per = ceil_div(rg.k1 - rg.k0, slices.key_slices), kb = min(rg.k0 + z * per, rg.k1), ke = min(kb + per, rg.k1);
+        if (kb >= ke) continue;
+        for (int64_t row = rg.q0 + r0; row < rg.q1; row += slices.row_slices) {
             const float l = on ? a.lse[row * heads + head] : -INFINITY;
             if (__all_sync(0xFFFFFFFFu, l == -INFINITY)) continue;
-            Piece<T, CPL> p, t, o;
+            Piece<T, CPL> p, t;
             p.zero();
             t.zero();
-            o.zero();
+            float d = 0.f;
             if (l != -INFINITY) {
                 p.load(static_cast<const T *>(a.q) + row * a.ldq + qoff, at, f.lanes, f.chunks);
                 t.load(static_cast<const T *>(a.dout) + row * a.ldg + qoff, at, f.lanes, f.chunks);
-                o.load(static_cast<const T *>(a.o) + row * a.ldo + qoff, at, f.lanes, f.chunks);
+                d = __ldg(dots + row * heads + head);
             }
-            float q[E], go[E], y[E], d[1];
+            float q[E], go[E];
             p.widen(q);
             t.widen(go);
-            o.widen(y);
-            d[0] = dot<E>(go, y);
-            key_sums<1>(d, f.lanes);
             const int pos_q = pos_of(a.bias.pos_q, row, rg.q0);
-            const float lse = l == -INFINITY ? INFINITY : l * kLog2e;
-            float run_a = 0.f, run_m = 0.f, all_a = 0.f, all_m = 0.f;
-            int cur = -1;
-            for (int64_t j0 = rg.k0; j0 < rg.k1; j0 += U * kpw) {
+            const float lse = l * kLog2e;
+            for (int64_t j0 = kb; j0 < ke; j0 += U * kpw) {
                 float sc[2 * U];
-                int pos[U];
+                int apart_by[U], bucket[U];
                 bool seen[U];
 #pragma unroll
                 for (int n = 0; n < U; ++n) {
                     const int64_t j = j0 + n * kpw + grp;
-                    seen[n] = on && j < rg.k1 && (!a.mask || a.mask[j]);
-                    pos[n] = seen[n] ? pos_of(a.bias.pos_k, j, rg.k0) : 0;
+                    seen[n] = l != -INFINITY && j < ke && (!a.mask || a.mask[j]);
+                    apart_by[n] = seen[n] ? apart(pos_of(a.bias.pos_k, j, rg.k0), pos_q) : 0;
                     Piece<T, CPL> k, v;
                     float w[E], x[E];
                     k.zero();
@@ -1043,58 +1185,28 @@ attn_few_table_kernel(const __grid_constant__ AttnArgs a, const __grid_constant_
                 }
                 key_sums<2 * U>(sc, f.lanes);
 #pragma unroll
+                for (int n = 0; n < U; ++n) bucket[n] = bucket_of(a.bias, a.bias.edges, apart_by[n]);
+#pragma unroll
                 for (int n = 0; n < U; ++n) {
                     if (!seen[n]) continue;
-                    const int b = bucket_of(a.bias, a.bias.edges, apart(pos[n], pos_q));
-                    const float pr = exp2_fast(fmaf(sc[n], c1, bias_at(a.bias, heads, b, head) - lse)), v = pr * (sc[U + n] - d[0]);
-                    if (b != cur) {
-                        if (at == 0 && cur >= 0) {
-                            float2 &bin = mine[cur * (32 / f.lanes)];
-                            bin = make_float2(bin.x + run_a, bin.y + run_m);
-                        }
-                        all_a += run_a;
-                        all_m += run_m;
-                        run_a = run_m = 0.f;
-                        cur = b;
+                    const float pr = exp2_fast(fmaf(sc[n], c1, bias_at(a.bias, heads, bucket[n], head) - lse));
+                    if (bucket[n] != cur) {
+                        if (at == 0) mine[cur * slots] += run;
+                        run = 0.f;
+                        cur = bucket[n];
                     }
-                    run_a += v;
-                    run_m += pr;
+                    run += pr * (sc[U + n] - d);
                 }
             }
-            if (at == 0 && cur >= 0) {
-                float2 &bin = mine[cur * (32 / f.lanes)];
-                bin = make_float2(bin.x + run_a, bin.y + run_m);
-            }
-            all_a += run_a;
-            all_m += run_m;
-            for (int i = wide; i < 32; i <<= 1) {
-                all_a += __shfl_xor_sync(0xFFFFFFFFu, all_a, i);
-                all_m += __shfl_xor_sync(0xFFFFFFFFu, all_m, i);
-            }
-            const float rest = all_m == 0.f ? 0.f : all_a / all_m;
-            __syncwarp();
-            // the row's bins -> the warp's sums: a lane per (bucket, head), whose rest the head's first lane has
-            for (int i0 = 0; i0 < nb * f.heads; i0 += 32) {
-                const int i = i0 + lane, hl = i & (f.heads - 1);
-                const float r = __shfl_sync(0xFFFFFFFFu, rest, hl * f.lanes);
-                if (i < nb * f.heads) {
-                    float v = 0.f, m = 0.f;
-                    for (int k = 0; k < kpw; ++k) {
-                        float2 &bin = bins[i / f.heads * (32 / f.lanes) + k * f.heads + hl];
-                        v += bin.x;
-                        m += bin.y;
-                        bin = make_float2(0.f, 0.f);
-                    }
-                    sums[i] += v - r * m;
-                }
-            }
-            __syncwarp();
         }
     }
+    if (at == 0) mine[cur * slots] += run;
     __syncwarp();
     for (int i = lane; i < nb * f.heads; i += 32) {
-        const int hl = i & (f.heads - 1), b = i / f.heads, to = hg * f.heads + hl;
-        if (to < a.kv_heads) part[(slice * nb + b) * heads + to * a.group + g] = sums[i];
+        const int b = i / f.heads, to = hg * f.heads + i % f.heads;
+        float v = 0.f;
+        for (int k = i % f.heads; k < slots; k += f.heads) v += bins[b * slots + k];
+        if (to < a.kv_heads) part[(slice * nb + b) * heads + to * a.group + g] = v;
     }
 }
 
@@ -1154,25 +1266,29 @@ bool launch_fwd(const AttnArgs &a, FewShape f, float *part_o, float2 *part_ml, c
 }
 
 template <typename T, int R, int U, int CPL, bool kBoth, bool kFit, bool kBias>
-bool launch_bwd_of(const AttnArgs &a, const FewShape &f, unsigned grid, float *part_dq, float *dots, cudaStream_t st)
+bool launch_bwd_of(const AttnArgs &a, FewShape f, unsigned grid, float *part_dq, float *dots, float *table_part, cudaStream_t st)
 {
     static std::atomic<bool> done[kMaxDevices] = {};
     if (!allow_smem(attn_few_bwd_kernel<T, R, U, CPL, kBoth, kFit, kBias>, done)) return false;
+    f.ring_bytes = (int)few_smem<U>(f);
     note_launch();
-    attn_few_bwd_kernel<T, R, U, CPL, kBoth, kFit, kBias><<<grid, kFewThreads, few_smem<U>(f), st>>>(a, f, part_dq, dots);
+    attn_few_bwd_kernel<T, R, U, CPL, kBoth, kFit, kBias>
+        <<<grid, kFewThreads, f.ring_bytes + (kBias && kBoth && table_part ? bins_bytes(a, f, R) : 0), st>>>(a, f, part_dq, dots, table_part);
     return true;
 }
 
 template <typename T, int R, int U, bool kBoth, bool kFit>
-bool launch_bwd(const AttnArgs &a, FewShape f, float *part_dq, float *dots, cudaStream_t st)
+bool launch_bwd(const AttnArgs &a, FewShape f, float *part_dq, float *dots, float *table_part, cudaStream_t st)
 {
     const unsigned grid = few_grid(a, f);
-    if (f.chunks <= 32)
-        return a.bias.table ? launch_bwd_of<T, R, U, 1, kBoth, kFit, true>(a, f, grid, part_dq, dots, st)
-                            : launch_bwd_of<T, R, U, 1, kBoth, kFit, false>(a, f, grid, part_dq, dots, st);
-    if constexpr (sizeof(T) == 4)
-        return a.bias.table ? launch_bwd_of<T, R, U, 2, kBoth, kFit, true>(a, f, grid, part_dq, dots, st)
-                            : launch_bwd_of<T, R, U, 2, kBoth, kFit, false>(a, f, grid, part_dq, dots, st);
+    auto launch = [&](auto wide) {
+        constexpr int CPL = decltype(wide)::value;
+        if constexpr (!(kBoth && kFit))                      // what all gradients in one kernel lack with a bias is found before, not fitted
+            if (a.bias.table) return launch_bwd_of<T, R, U, CPL, kBoth, kFit, true>(a, f, grid, part_dq, dots, table_part, st);
+        return launch_bwd_of<T, R, U, CPL, kBoth, kFit, false>(a, f, grid, part_dq, dots, nullptr, st);
+    };
+    if (f.chunks <= 32) return launch(std::integral_constant<int, 1>());
+    if constexpr (sizeof(T) == 4) return launch(std::integral_constant<int, 2>());
     return true;
 }
 
@@ -1191,27 +1307,27 @@ template <typename T> bool forward_of(const AttnArgs &a, const FewPlan &p, const
 }
 
 template <typename T, int R, bool kBoth, bool kFit>
-bool backward_steps(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_dq, float *dots, cudaStream_t st)
+bool backward_steps(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_dq, float *dots, float *table_part, cudaStream_t st)
 {
-    if (p.steps == 1) return launch_bwd<T, R, 1, kBoth, kFit>(a, f, part_dq, dots, st);
-    if (p.steps == 2) return launch_bwd<T, R, 2, kBoth, kFit>(a, f, part_dq, dots, st);
-    return launch_bwd<T, R, kUnroll, kBoth, kFit>(a, f, part_dq, dots, st);
+    if (p.steps == 1) return launch_bwd<T, R, 1, kBoth, kFit>(a, f, part_dq, dots, table_part, st);
+    if (p.steps == 2) return launch_bwd<T, R, 2, kBoth, kFit>(a, f, part_dq, dots, table_part, st);
+    return launch_bwd<T, R, kUnroll, kBoth, kFit>(a, f, part_dq, dots, table_part, st);
 }
 
-template <typename T, int R, bool kBoth> bool backward_rows(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_dq, float *dots, cudaStream_t st)
+template <typename T, int R, bool kBoth> bool backward_rows(const AttnArgs &a, const FewPlan &p, const FewShape &f, float *part_dq, float *dots, float *table_part, cudaStream_t st)
 {
     if constexpr (sizeof(T) == 2)
-        if (p.fit) return backward_steps<T, R, kBoth, true>(a, p, f, part_dq, dots, st);
-    return backward_steps<T, R, kBoth, false>(a, p, f, part_dq, dots, st);
+        if (p.fit) return backward_steps<T, R, kBoth, true>(a, p, f, part_dq, dots, table_part, st);
+    return backward_steps<T, R, kBoth, false>(a, p, f, part_dq, dots, table_part, st);
 }
 
-template <typename T> bool backward_of(const AttnArgs &a, const FewPlan &p, FewShape f, float *part_dq, float *dots, cudaStream_t st)
+template <typename T> bool backward_of(const AttnArgs &a, const FewPlan &p, FewShape f, float *part_dq, float *dots, float *table_part, cudaStream_t st)
 {
     bool ok;
-    if (!p.both) ok = backward_rows<T, 4, false>(a, p, f, part_dq, dots, st);
-    else if (p.rows == 1) ok = backward_rows<T, 1, true>(a, p, f, part_dq, dots, st);
-    else if (p.rows == 2) ok = backward_rows<T, 2, true>(a, p, f, part_dq, dots, st);
-    else ok = backward_rows<T, 4, true>(a, p, f, part_dq, dots, st);
+    if (!p.both) ok = backward_rows<T, 4, false>(a, p, f, part_dq, dots, table_part, st);
+    else if (p.rows == 1) ok = backward_rows<T, 1, true>(a, p, f, part_dq, dots, table_part, st);
+    else if (p.rows == 2) ok = backward_rows<T, 2, true>(a, p, f, part_dq, dots, table_part, st);
+    else ok = backward_rows<T, 4, true>(a, p, f, part_dq, dots, table_part, st);
     if (!ok) return false;
     if (f.splits > 1 && a.q_rows) join_dq(a, f.splits, sizeof(T) == 4 ? E2EGREC_F32 : E2EGREC_BF16, p.fit, part_dq, p.both ? nullptr : dots, st);
     if (!p.both && a.k_rows) {
@@ -1242,51 +1358,54 @@ FewPlan few_plan(const AttnArgs &a, const Lengths &q, const Lengths &k, int es, 
     p.both = backward && rows <= p.rows;
     p.steps = max_k <= step ? 1 : (max_k <= 2 * step || (p.rows > 2 && max_k > kUnroll * step) ? 2 : kUnroll);
     while (p.steps * step > 32) p.steps /= 2;        // a turn's rows are the bits of a word
+    // With a bias the kernel of all gradients goes over the keys twice, first for D, and keeps the table's bins: not where the keys go in stretches,
+    // nor where the bins of few buckets more than there are lanes leave less than two blocks per SM.
+    if (p.both && a.bias.buckets) {
+        const int64_t want = std::min(ceil_div(148 * 24, units0), ceil_div(max_k, step * p.steps));
+        if (std::min(want / kFewWarps, max_k / (step * p.steps * kFewWarps * 4)) > 1 || bins_bytes(a, f, p.rows) > 64 * 1024) {
+            p.both = false;
+            p.rows = 4;
+            p.steps = max_k <= step ? 1 : 2;
+            while (p.steps * step > 32) p.steps /= 2;
+        }
+    }
     const int64_t turn = step * p.steps;
-    p.fit = backward && es == 2 && max_k > turn;
+    p.fit = backward && es == 2 && max_k > turn && !(p.both && a.bias.buckets);
     p.batches = blocks_per_unit(q, a.group, p.rows, units0);
     const int64_t want = std::max<int64_t>(1, std::min(ceil_div(148 * 24, units0 * p.batches), ceil_div(max_k, turn)));
     p.warps = 1;
     while (p.warps < kFewWarps && p.warps < want) p.warps *= 2;
     // a stretch is worth its join where every warp has four turns of it
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want / p.warps, max_k / (turn * p.warps * 4), kMaxSplits, most / p.batches}));
+    if (p.both && a.bias.buckets) p.splits = 1;
+    p.blocks = ceil_div(units0 * p.batches, kFewWarps / p.warps);
     p.key_batches = blocks_per_unit(k, 1, step * kKeys, units0);
     return p;
 }
 
-// The table's kernel: its bins and sums fit shared memory with one key head side by side at least (32 keys of a step, 128 buckets: 130 KB)
-static size_t table_smem(const AttnArgs &a, const FewShape &f)
+// Warps enough for 16 per SM, each with a slice of the sequences; of their rows and their keys where there are fewer sequences than that.  (Its bins
+// fit: 32 slots of 128 buckets are 16 KB per warp.)
+TablePlan few_table_plan(const AttnArgs &a, const Lengths &k, int32_t dtype)
 {
-    return (size_t)kFewWarps * a.bias.buckets * (32 / f.lanes * sizeof(float2) + f.heads * sizeof(float));
-}
-static FewShape table_shape(const AttnArgs &a, int32_t dtype)
-{
-    FewShape f = few_shape(a, (int)dtype_size(dtype));
-    while (f.heads > 1 && table_smem(a, f) > (size_t)kMostSmem) f.heads /= 2;
-    f.head_groups = (a.kv_heads + f.heads - 1) / f.heads;
-    return f;
-}
-
-// Warps enough for 16 per SM, each with a slice of the sequences; of their rows where there are fewer sequences than that.
-TablePlan few_table_plan(const AttnArgs &a, int32_t dtype)
-{
-    const FewShape f = table_shape(a, dtype);
+    const FewShape f = few_shape(a, (int)dtype_size(dtype));
     const int64_t want = std::max<int64_t>(1, 148 * 16 / ((int64_t)f.head_groups * a.group)), n = std::max<int64_t>(a.n_seq, 1);
-    TablePlan p{std::min(n, want), 1};
+    TablePlan p{std::min(n, want), 1, 1};
     p.row_slices = std::max<int64_t>(1, std::min(want / p.seq_slices, ceil_div(a.q_rows, n)));
+    p.key_slices = std::max<int64_t>(1, std::min(want / (p.seq_slices * p.row_slices), k.typical / 64));
     return p;
 }
 
-bool few_attention_table(const AttnArgs &a, const TablePlan &p, int32_t dtype, float *part, cudaStream_t st)
+bool few_attention_table(const AttnArgs &a, const TablePlan &p, int32_t dtype, const float *dots, float *part, cudaStream_t st)
 {
     static std::atomic<bool> done[3][kMaxDevices] = {};
-    FewShape f = table_shape(a, dtype);
-    f.units = (uint32_t)(p.seq_slices * p.row_slices * f.head_groups * a.group);
+    FewShape f = few_shape(a, (int)dtype_size(dtype));
+    f.units = (uint32_t)(p.seq_slices * p.row_slices * p.key_slices * f.head_groups * a.group);
     const unsigned grid = (unsigned)ceil_div(f.units, kFewWarps);
+    const size_t smem = (size_t)kFewWarps * a.bias.buckets * (32 / f.lanes) * sizeof(float);
     auto launch = [&](auto *kernel, int i) {
         if (!allow_smem(kernel, done[i])) return false;
         note_launch();
-        kernel<<<grid, kFewThreads, table_smem(a, f), st>>>(a, f, p.seq_slices, p.row_slices, part);
+        kernel<<<grid, kFewThreads, smem, st>>>(a, f, p, dots, part);
         return true;
     };
     if (dtype == E2EGREC_BF16) return launch(attn_few_table_kernel<__nv_bfloat16, 1>, 0);
@@ -1308,10 +1427,10 @@ bool few_attention_forward(const AttnArgs &a, const FewPlan &p, int32_t dtype, f
                                 : forward_of<__nv_bfloat16>(a, p, planned(a, p, dtype), part_o, part_ml, st);
 }
 
-bool few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, cudaStream_t st)
+bool few_attention_backward(const AttnArgs &a, const FewPlan &p, int32_t dtype, float *part_dq, float *dots, float *table_part, cudaStream_t st)
 {
-    return dtype == E2EGREC_F32 ? backward_of<float>(a, p, planned(a, p, dtype), part_dq, dots, st)
-                                : backward_of<__nv_bfloat16>(a, p, planned(a, p, dtype), part_dq, dots, st);
+    return dtype == E2EGREC_F32 ? backward_of<float>(a, p, planned(a, p, dtype), part_dq, dots, table_part, st)
+                                : backward_of<__nv_bfloat16>(a, p, planned(a, p, dtype), part_dq, dots, table_part, st);
 }
 
 }  // namespace e2egrec
