@@ -101,6 +101,29 @@ template <int N> __device__ inline void look_up(const BiasArgs &b, const int32_t
     for (int i = 0; i < N; ++i) at[i] = min(at[i], b.buckets - 1);
 }
 
+// The bucket that a thread is in: its number and the distances low .. top that are in it
+struct Bucket {
+    int at, low, top;
+    __device__ inline void unknown() { at = 0, low = 1, top = 0; }
+    __device__ inline void up(const BiasArgs &b, const int32_t *edges)
+    {
+        ++at;
+        low = top + 1;
+        top = at < b.buckets - 1 ? edges[at] - 1 : INT32_MAX;
+    }
+    __device__ inline void seek(const BiasArgs &b, const int32_t *edges, int d)
+    {
+        at = bucket_of(b, edges, d);
+        low = at ? edges[at - 1] : INT32_MIN;
+        top = at < b.buckets - 1 ? edges[at] - 1 : INT32_MAX;
+    }
+    __device__ inline void to(const BiasArgs &b, const int32_t *edges, int d)
+    {
+        if (d > top && low <= top) up(b, edges);
+        if (d > top || d < low) seek(b, edges, d);
+    }
+};
+
 // A bias in powers of two, as the scores are
 __device__ __forceinline__ float bias_value(float b) { return b <= kHides ? -INFINITY : b * kLog2e; }
 __device__ __forceinline__ float bias_at(const BiasArgs &b, int heads, int bucket, int head) { return bias_value(__ldg(b.table + bucket * heads + head)); }

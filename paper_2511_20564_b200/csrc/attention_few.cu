@@ -269,31 +269,46 @@ __device__ inline Unit few_unit(const AttnArgs &a, const FewShape &f, uint32_t u
     return x;
 }
 
-// Biases of the scores of a turn: lane i finds the buckets of the turn's key i, which the lanes of that key then ask it for.  Positions of the
-// keys are fetched a turn ahead.
-template <int R> struct TurnBias {
-    int pos[R], col[R], buckets[R];                  // the rows' positions and heads
+// Biases of the scores of a turn: lane i finds the buckets of the turn's key i, which the lanes of that key then ask it for.  It is found from the
+// bucket of the turn before, mostly the same or the next one, and everything before the turn's keys are waited for; positions of the keys are
+// fetched a turn ahead.
+template <int R, int U> struct TurnBias {
+    int pos[R], col[R];                              // the rows' positions and heads
+    Bucket state[R];
     int next;
+    int bucket[R * U];                               // of the lane's scores
+    float value[R * U];
     __device__ inline void row(const AttnArgs &a, const Unit &x, bool on, int r, int64_t row, int head)
     {
         pos[r] = on ? pos_of(a.bias.pos_q, row, x.rg.q0) : 0;
         col[r] = on ? head : 0;
     }
+    // before the first turn of a walk
+    __device__ inline void begin(const AttnArgs &a, const Unit &x, const Ring &ring)
+    {
+#pragma unroll
+        for (int r = 0; r < R; ++r) state[r].unknown();
+        fetch(a, x, ring, 0);
+    }
     __device__ inline void fetch(const AttnArgs &a, const Unit &x, const Ring &ring, int t)
     {
-        const int j = ring.first + t * ring.stride + ring.lane;
-        next = ring.lane < ring.keys && j < ring.n ? pos_of(a.bias.pos_k, x.kb + j, x.rg.k0) : 0;
+        const int j = min(ring.first + t * ring.stride + ring.lane, ring.n - 1);      // (lanes without a key: near the others)
+        next = j >= 0 && ring.lane < ring.keys ? pos_of(a.bias.pos_k, x.kb + j, x.rg.k0) : 0;
     }
-    __device__ inline void turn(const AttnArgs &a, const Unit &x, const Ring &ring, int t)
+    __device__ inline void turn(const AttnArgs &a, const Unit &x, const Ring &ring, int t, int kpw, int grp)
     {
         const int mine = next;
         if (t + 1 < ring.turns) fetch(a, x, ring, t + 1);
+        if (ring.lane < ring.keys)
 #pragma unroll
-        for (int r = 0; r < R; ++r) buckets[r] = bucket_of(a.bias, a.bias.edges, apart(mine, pos[r]));
+            for (int r = 0; r < R; ++r) state[r].to(a.bias, a.bias.edges, apart(mine, pos[r]));
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < R * U; ++i) {
+            bucket[i] = __shfl_sync(0xFFFFFFFFu, state[i / U].at, i % U * kpw + grp);
+            value[i] = bias_at(a.bias, a.kv_heads * a.group, bucket[i], col[i / U]);
+        }
     }
-    __device__ inline int bucket(int r, int key) const { return __shfl_sync(0xFFFFFFFFu, buckets[r], key); }
-    __device__ inline float value(const AttnArgs &a, int r, int bucket) const { return bias_at(a.bias, a.kv_heads * a.group, bucket, col[r]); }
-    __device__ inline float of(const AttnArgs &a, int r, int key) const { return value(a, r, bucket(r, key)); }
 };
 
 // Sums of dS by bucket that a warp keeps in shared memory.  Every key of a step and head has bins of its own, [rows x buckets x slots], so no two
@@ -386,9 +401,9 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         if (f.warps == 1 ? !live : !__syncthreads_or((int)live)) break;      // barriers inside: all warps of the block go on, or none
         if (live) ring.start();
         float q[R][E], o[R][E], m[R], l[R];
-        TurnBias<R> bias;
+        TurnBias<R, U> bias;
         if constexpr (kBias)
-            if (live) bias.fetch(a, x, ring, 0);
+            if (live) bias.begin(a, x, ring);
         RowWalk in(a, x, r0);
 #pragma unroll
         for (int r = 0; r < R; ++r, in.next(a)) {
@@ -407,6 +422,7 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         }
         for (int t = 0; live && t < ring.turns && ring.ok; ++t) {
             uint32_t word;
+            if constexpr (kBias) bias.turn(a, x, ring, t, kpw, grp);
             const uint32_t at_k = ring.wait(word, t, &abort_flag) + grp * f.slice + mine, at_v = at_k + ring.half;
             if (!ring.ok) {
                 ring.land(t);
@@ -427,11 +443,9 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 for (int r = 0; r < R; ++r) s[r * U + u] = dot<E>(q[r], w);
             }
             key_sums<R * U>(s, f.lanes);
-            if constexpr (kBias) {
-                bias.turn(a, x, ring, t);
+            if constexpr (kBias)
 #pragma unroll
-                for (int i = 0; i < R * U; ++i) s[i] += bias.of(a, i / U, i % U * kpw + grp);
-            }
+                for (int i = 0; i < R * U; ++i) s[i] += bias.value[i];
 #pragma unroll
             for (int r = 0; r < R; ++r) {
                 float top = m[r];
@@ -783,9 +797,9 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         float q[R][E], g[R][E], dq[R][E], lse[R], d[R];
         float mean[kFit ? R : 1][E], rest[R];             // sum_j p_j k_j; what D lacked
         const bool one_turn = f.warps == 1 && f.splits == 1 && x.ke - x.kb <= U * kpw;
-        TurnBias<R> bias;
+        TurnBias<R, U> bias;
         if constexpr (kBias)
-            if (live) bias.fetch(a, x, ring, 0);
+            if (live) bias.begin(a, x, ring);
         RowSums<R> lack = {};
         if constexpr (sizeof(T) == 2 && !kFit && !kTwice)
             if (live && !one_turn) lack = lacking<T, R, CPL, kBias>(a, f, unit, r0);       // one warp per unit and one stretch: few_plan
@@ -837,6 +851,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 for (int r = 0; r < R; ++r) total[r] = 0.f;
                 for (int t = 0; live && t < ring.turns && ring.ok; ++t) {
                     uint32_t word;
+                    bias.turn(a, x, ring, t, kpw, grp);
                     const uint32_t at_k = ring.wait(word, t, &abort_flag) + grp * f.slice + mine, at_v = at_k + ring.half;
                     if (!ring.ok) {
                         ring.land(t);
@@ -864,10 +879,9 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                         }
                     }
                     key_sums<2 * R * U>(s, f.lanes);
-                    bias.turn(a, x, ring, t);
 #pragma unroll
                     for (int i = 0; i < R * U; ++i) {
-                        const float add = bias.of(a, i / U, i % U * kpw + grp) - lse[i / U];
+                        const float add = bias.value[i] - lse[i / U];
                         const float p = seen[i % U] ? exp2_fast(fmaf(s[i], c1, add)) : 0.f;
                         total[i / U] += p;
                         d[i / U] += p == 0.f ? 0.f : p * s[R * U + i];
@@ -903,12 +917,13 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
                 for (int r = 0; r < R; ++r) d[r] = total[r] == 0.f ? 0.f : d[r] / total[r];
                 if (live) {
-                    bias.fetch(a, x, ring, 0);
+                    bias.begin(a, x, ring);
                     ring.start();
                 }
             }
         for (int t = 0; live && t < ring.turns && ring.ok; ++t) {
             uint32_t word;
+            if constexpr (kBias) bias.turn(a, x, ring, t, kpw, grp);
             const uint32_t at_k = ring.wait(word, t, &abort_flag) + grp * f.slice + mine, at_v = at_k + ring.half;
             if (!ring.ok) {
                 ring.land(t);
@@ -937,18 +952,12 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 }
             }
             key_sums<2 * R * U>(s, f.lanes);
-            int bucket[kBias ? R * U : 1];
-            if constexpr (kBias) {
-                bias.turn(a, x, ring, t);
-#pragma unroll
-                for (int i = 0; i < R * U; ++i) bucket[i] = bias.bucket(i / U, i % U * kpw + grp);
-            }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     float base = -lse[r];
-                    if constexpr (kBias) base += bias.value(a, r, bucket[r * U + u]);
+                    if constexpr (kBias) base += bias.value[r * U + u];
                     s[r * U + u] = seen[u] ? exp2_fast(fmaf(s[r * U + u], c1, base)) : 0.f;
                 }
                 if (one_turn) {
@@ -970,7 +979,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     s[(R + r) * U + u] = seen[u] ? s[r * U + u] * (s[(R + r) * U + u] - d[r]) : 0.f;
                     rest[r] += s[(R + r) * U + u];
                     if constexpr (kBias && kBoth)
-                        if (binned && at == 0 && seen[u]) bins.add(r, bucket[r * U + u], lane / f.lanes, s[(R + r) * U + u]);
+                        if (binned && at == 0 && seen[u]) bins.add(r, bias.bucket[r * U + u], lane / f.lanes, s[(R + r) * U + u]);
                 }
             }
 #pragma unroll

@@ -315,32 +315,6 @@ struct Ahead {
 // kKey: the thread's own position is the key's, the columns' are the queries'
 template <bool kKey> __device__ inline int distance(int own, int column) { return kKey ? apart(own, column) : apart(column, own); }
 
-// The bucket that a thread is in: its number and the distances low .. top that are in it
-struct Bucket {
-    int at, low, top;
-    __device__ inline void unknown() { at = 0, low = 1, top = 0; }
-    __device__ inline void up(const BiasArgs &b, const int32_t *edges)
-    {
-        ++at;
-        low = top + 1;
-        top = at < b.buckets - 1 ? edges[at] - 1 : INT32_MAX;
-    }
-    __device__ inline void seek(const BiasArgs &b, const int32_t *edges, int d)
-    {
-        const int one[1] = {d};
-        int found[1];
-        look_up<1>(b, edges, one, found);
-        at = found[0];
-        low = at ? edges[at - 1] : INT32_MIN;
-        top = at < b.buckets - 1 ? edges[at] - 1 : INT32_MAX;
-    }
-    __device__ inline void to(const BiasArgs &b, const int32_t *edges, int d)
-    {
-        if (d > top && low <= top) up(b, edges);
-        if (d > top || d < low) seek(b, edges, d);
-    }
-};
-
 // The buckets of near distances, by the 32 W threads of W warps that have nothing else to do while the first tiles are on their way; the edges
 // are there.  A barrier of their own.
 template <int W> __device__ inline void stage_near(const BiasArgs &b, BiasShared &sh)
