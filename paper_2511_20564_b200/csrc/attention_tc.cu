@@ -329,181 +329,191 @@ template <int W> __device__ inline void stage_near(const BiasArgs &b, BiasShared
     asm volatile("bar.sync 1, %0;" ::"n"(W * 32) : "memory");
 }
 
-// The buckets that a thread meets in 32 columns: at .. at + n.  Up to three edges are thresholds: a column's position p is beyond edge k where
-// p > limit[k] (kKey: p < limit[k]); a limit of a bucket that is not met is never passed.
-constexpr int kMost = 3;
-template <bool kKey> struct Span {
-    int at, n, limit[kMost];
-    bool away;                                           // further than kNear from a column
-    __device__ inline void find(const BiasArgs &b, const int32_t *edges, const int2 &range, int own, Bucket &s)
+__device__ inline int add_sat(int x, int y)
+{
+    int s;
+    asm("add.sat.s32 %0, %1, %2;" : "=r"(s) : "r"(x), "r"(y));
+    return s;
+}
+// The bucket that a thread is in, by the columns' positions: from `in` to `out`, in the order of growing distances (kKey: of falling positions).
+// Comparisons of positions take no difference that could leave 32 bits.
+template <bool kKey> struct Place {
+    int at, in, out;
+    static constexpr int kFirst = kKey ? INT32_MAX : INT32_MIN, kLast = kKey ? INT32_MIN : INT32_MAX;
+    __device__ inline void unknown() { at = 0, in = kLast, out = kFirst; }
+    __device__ inline bool beyond(int p) const { return kKey ? p < out : p > out; }
+    __device__ inline bool before(int p) const { return kKey ? p > in : p < in; }
+    __device__ inline int end(const BiasArgs &b, const int32_t *edges, int own) const
     {
-        n = 0;
-#pragma unroll
-        for (int k = 0; k < kMost; ++k) limit[k] = kKey ? INT32_MIN : INT32_MAX;
-        at = s.at;
-        away = false;
-        if (range.x > range.y) return;                   // no column counts
-        const int near = distance<kKey>(own, kKey ? range.y : range.x), far = distance<kKey>(own, kKey ? range.x : range.y);
-        away = near < -kNear || far >= kNear;
-        s.to(b, edges, near);
-        at = s.at;
-#pragma unroll
-        for (int k = 0; k < kMost; ++k)
-            if (far > s.top) {
-                limit[k] = kKey ? own - s.top : own + s.top;      // a column lies on either side, so it is a position
-                s.up(b, edges);
-            }
-        if (far > s.top) s.seek(b, edges, far);
-        n = s.at - at;
+        return at < b.buckets - 1 ? (kKey ? apart(own, edges[at] - 1) : add_sat(own, edges[at] - 1)) : kLast;
     }
-    __device__ inline bool beyond(int k, int p) const { return kKey ? p < limit[k] : p > limit[k]; }
+    __device__ inline void up(const BiasArgs &b, const int32_t *edges, int own)
+    {
+        ++at;
+        in = kKey ? out - 1 : out + 1;
+        out = end(b, edges, own);
+    }
+    __device__ inline void seek(const BiasArgs &b, const int32_t *edges, int own, int p)
+    {
+        const int d[1] = {distance<kKey>(own, p)};
+        int found[1];
+        look_up<1>(b, edges, d, found);
+        at = found[0];
+        in = at ? (kKey ? apart(own, edges[at - 1]) : add_sat(own, edges[at - 1])) : kFirst;
+        out = end(b, edges, own);
+    }
+    __device__ inline void to(const BiasArgs &b, const int32_t *edges, int own, int p)
+    {
+        if (beyond(p) && (kKey ? in >= out : in <= out)) up(b, edges, own);
+        if (beyond(p) || before(p)) seek(b, edges, own, p);
+    }
 };
 
-// The buckets of 32 N columns of a thread's row (kKey: key), from column 32 c0 of a tile on.  Loops over the columns' 32s stay loops, their
-// results are put in place by selection.
+// The buckets of 32 N columns of a thread's row (kKey: key), from column 32 c0 of a tile on: in 32 columns at .. last.  Two of them: a column's
+// position p is in the second where it is beyond limit.
 template <bool kKey, int N> struct TileSpans {
-    Span<kKey> s[N];
-    int at;                                              // `one`: the bucket
-    uint32_t two, more, many, apart;                     // a bit per 32 columns: some lane meets two buckets and more in them, three, over four;
-                                                         // is further than kNear from one of them
+    int at[N], last[N], limit[N];                        // with `one` at[0] alone
+    uint32_t two, many, away;                            // a bit per 32 columns: some lane meets two buckets or more in them; more; is further than
+                                                         // kNear from a column of them
     bool one;                                            // every lane meets one bucket in the tile
+    __device__ static inline bool beyond(int limit, int p) { return kKey ? p < limit : p > limit; }
     // alive: the warp has a row (key) that counts
-    __device__ inline void find(const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c0, int own, bool alive, Bucket &bucket)
+    __device__ inline void find(const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c0, int own, bool alive, Place<kKey> &place)
     {
-        at = 0;
+        at[0] = 0;
         one = true;
         if (!alive) return;
         const int4 h = sh.halves[slot];
         const int2 r = N == 4 ? make_int2(min(h.x, h.z), max(h.y, h.w)) : (c0 ? make_int2(h.z, h.w) : make_int2(h.x, h.y));
-        Bucket next = bucket;
+        Place<kKey> next = place;
         bool mine = true;
-        two = more = many = apart = 0;
         if (r.x <= r.y) {
-            next.to(b, sh.edges, distance<kKey>(own, kKey ? r.y : r.x));
-            mine = distance<kKey>(own, kKey ? r.x : r.y) <= next.top;
+            next.to(b, sh.edges, own, kKey ? r.y : r.x);
+            mine = !next.beyond(kKey ? r.x : r.y);
         }
-        at = next.at;
+        at[0] = next.at;
         one = __all_sync(0xFFFFFFFFu, mine);
         if (one) {
-            bucket = next;
+            place = next;
             return;
         }
+        two = many = away = 0;
 #pragma unroll 1
         for (int c = 0; c < N; ++c) {
-            Span<kKey> x;
-            x.find(b, sh.edges, sh.range[slot][c0 + c], own, bucket);
+            const int2 range = sh.range[slot][c0 + c];
+            int stop = Place<kKey>::kLast;
+            bool more = false;
+            if (range.x <= range.y) place.to(b, sh.edges, own, kKey ? range.y : range.x);
+            const int from = place.at, far = kKey ? range.x : range.y;
+            if (range.x <= range.y && place.beyond(far)) {
+                stop = place.out;
+                place.up(b, sh.edges, own);
+                if (place.beyond(far)) {
+                    more = true;
+                    place.seek(b, sh.edges, own, far);
+                }
+            }
 #pragma unroll
             for (int k = 0; k < N; ++k)
-                if (c == k) s[k] = x;
-            two |= __any_sync(0xFFFFFFFFu, x.n > 0) ? 1u << c : 0u;
-            more |= __any_sync(0xFFFFFFFFu, x.n > 1) ? 1u << c : 0u;
-            many |= __any_sync(0xFFFFFFFFu, x.n > kMost) ? 1u << c : 0u;
-            apart |= __any_sync(0xFFFFFFFFu, x.away) ? 1u << c : 0u;
+                if (c == k) {
+                    at[k] = from;
+                    last[k] = place.at;
+                    limit[k] = stop;
+                }
+            if (__any_sync(0xFFFFFFFFu, from != place.at)) {
+                two |= 1u << c;
+                if (__any_sync(0xFFFFFFFFu, more)) {
+                    many |= 1u << c;
+                    const int d0 = distance<kKey>(own, range.x), d1 = distance<kKey>(own, range.y);
+                    if (__any_sync(0xFFFFFFFFu, min(d0, d1) < -kNear || max(d0, d1) >= kNear)) away |= 1u << c;
+                }
+            }
         }
     }
-    __device__ inline Span<kKey> of(int c) const
+    __device__ inline void of(int c, int &from, int &to, int &stop) const
     {
-        Span<kKey> x = s[0];
+        from = at[0];
+        to = last[0];
+        stop = limit[0];
 #pragma unroll
         for (int k = 1; k < N; ++k)
-            if (c == k) x = s[k];
-        return x;
+            if (c == k) {
+                from = at[k];
+                to = last[k];
+                stop = limit[k];
+            }
     }
-    // 32 products, of column 32 c and on -> scores in powers of two with their biases; apart_at() is false.  table: of the row's head
-    __device__ inline void add_to(uint32_t (&v)[32], int c, float c1, const BiasShared &sh, uint32_t slot, int c0, int own, const float *table) const
+    // 32 products, of column 32 c and on -> scores in powers of two with their biases, where no lane meets more than two buckets.  table: of the
+    // row's head
+    __device__ inline void add_to(uint32_t (&v)[32], int c, float c1, const BiasShared &sh, uint32_t slot, int c0, const float *table) const
     {
-        const int4 *pos = reinterpret_cast<const int4 *>(sh.pos[slot] + (c0 + c) * 32);
         const float2 scale2 = make_float2(c1, c1);
-        auto put = [&](int i, float t0, float t1) {
-            const float2 x = __ffma2_rn(pair_of(v[i], v[i + 1]), scale2, make_float2(t0, t1));
+        int from, to, stop;
+        of(c, from, to, stop);
+        const float t0 = table[from];
+        auto put = [&](int i, float x0, float x1) {
+            const float2 x = __ffma2_rn(pair_of(v[i], v[i + 1]), scale2, make_float2(x0, x1));
             v[i] = __float_as_uint(x.x);
             v[i + 1] = __float_as_uint(x.y);
         };
-        if (!(many >> c & 1u)) {
-            const Span<kKey> x = of(c);
-            const float t0 = table[x.at], t1 = table[x.at + min(x.n, 1)];
-            if (!(more >> c & 1u)) {
+        if (!(two >> c & 1u)) {
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    const int4 p = pos[i / 4];
-                    put(i, x.beyond(0, p.x) ? t1 : t0, x.beyond(0, p.y) ? t1 : t0);
-                    put(i + 2, x.beyond(0, p.z) ? t1 : t0, x.beyond(0, p.w) ? t1 : t0);
-                }
-            } else {
-                const float t2 = table[x.at + min(x.n, 2)], t3 = table[x.at + min(x.n, 3)];
-                auto pick = [&](int p) {
-                    float w = x.beyond(0, p) ? t1 : t0;
-                    w = x.beyond(1, p) ? t2 : w;
-                    return x.beyond(2, p) ? t3 : w;
-                };
+            for (int i = 0; i < 32; i += 2) put(i, t0, t0);
+            return;
+        }
+        const float t1 = table[to];
+        const int4 *pos = reinterpret_cast<const int4 *>(sh.pos[slot] + (c0 + c) * 32);
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    const int4 p = pos[i / 4];
-                    put(i, pick(p.x), pick(p.y));
-                    put(i + 2, pick(p.z), pick(p.w));
-                }
-            }
-        } else {                                         // (columns that do not count may lie anywhere)
-            auto look = [&](int p) { return table[sh.near[min((uint32_t)((kKey ? own - p : p - own) + kNear), 2u * kNear - 1)]]; };
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                const int4 p = pos[i / 4];
-                put(i, look(p.x), look(p.y));
-                put(i + 2, look(p.z), look(p.w));
-            }
+        for (int i = 0; i < 32; i += 4) {
+            const int4 p = pos[i / 4];
+            put(i, beyond(stop, p.x) ? t1 : t0, beyond(stop, p.y) ? t1 : t0);
+            put(i + 2, beyond(stop, p.z) ? t1 : t0, beyond(stop, p.w) ? t1 : t0);
         }
     }
-    // The same in tensor memory, where buckets have to be found by bisection or every column has its own head: eight columns at a time
-    __device__ inline bool apart_at(int c, int group) const { return (kKey && group > 1) || (many & apart) >> c & 1u; }
-    __device__ inline void one_by_one(uint32_t taddr, int c, float c1, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c0, int own,
-                                      const float *table, int group, int g) const
+    // The same in tensor memory for columns where some lane meets more buckets, or every column has its own head (kKey; g: the first one's, table
+    // the key head's first): each column looks its bucket up, 16 at a time
+    __device__ inline bool one_by_one(int c, int group) const { return (kKey && group > 1) || (!one && many >> c & 1u); }
+    __device__ inline void look_columns(uint32_t taddr, int c, float c1, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c0, int own,
+                                        const float *table, int group, int g) const
     {
 #pragma unroll 1
-        for (int i = 0; i < 32; i += 8) {
+        for (int i = 0; i < 32; i += 16) {
             const int4 *pos = reinterpret_cast<const int4 *>(sh.pos[slot] + (c0 + c) * 32 + i);
-            const int4 p = pos[0], o = pos[1];
-            int at8[8], d[8] = {distance<kKey>(own, p.x), distance<kKey>(own, p.y), distance<kKey>(own, p.z), distance<kKey>(own, p.w),
-                                distance<kKey>(own, o.x), distance<kKey>(own, o.y), distance<kKey>(own, o.z), distance<kKey>(own, o.w)};
+            int at16[16];
             if (one) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) at8[k] = at;
-            } else if (!(apart >> c & 1u)) {
+                for (int k = 0; k < 16; ++k) at16[k] = at[0];
+            } else if ((many & ~away) >> c & 1u) {       // (columns that do not count may lie anywhere)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) at8[k] = sh.near[min((uint32_t)(d[k] + kNear), 2u * kNear - 1)];
+                for (int k = 0; k < 16; k += 4) {
+                    const int4 p4 = pos[k / 4];
+                    const int p[4] = {p4.x, p4.y, p4.z, p4.w};
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) at16[k + m] = sh.near[min((uint32_t)((kKey ? own - p[m] : p[m] - own) + kNear), 2u * kNear - 1)];
+                }
             } else {
-                look_up<8>(b, sh.edges, d, at8);
+#pragma unroll
+                for (int k = 0; k < 16; k += 8) {
+                    const int4 p = pos[k / 4], o = pos[k / 4 + 1];
+                    const int d[8] = {distance<kKey>(own, p.x), distance<kKey>(own, p.y), distance<kKey>(own, p.z), distance<kKey>(own, p.w),
+                                      distance<kKey>(own, o.x), distance<kKey>(own, o.y), distance<kKey>(own, o.z), distance<kKey>(own, o.w)};
+                    int at8[8];
+                    look_up<8>(b, sh.edges, d, at8);
+#pragma unroll
+                    for (int m = 0; m < 8; ++m) at16[k + m] = at8[m];
+                }
             }
-            uint32_t v[8];
+            uint32_t v[16];
             __syncwarp();                                // tensor memory is for a converged warp
-            tmem_load8_async(taddr + i, v);
+            tmem_load16_async(taddr + i, v);
             tmem_load_wait();
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                v[k] = __float_as_uint(fmaf(__uint_as_float(v[k]), c1, table[(kKey ? g * b.buckets : 0) + at8[k]]));
+            for (int k = 0; k < 16; ++k) {
+                v[k] = __float_as_uint(fmaf(__uint_as_float(v[k]), c1, table[(kKey ? g * b.buckets : 0) + at16[k]]));
                 if (kKey) g = g + 1 == group ? 0 : g + 1;
             }
             __syncwarp();
-            tmem_store8(taddr + i, v);
-        }
-        tmem_store_wait();
-    }
-    // The same for all products of the tile, in tensor memory
-    __device__ inline void in_place(uint32_t taddr, float c1, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c0, int own, const float *table,
-                                    int group, int g0) const
-    {
-#pragma unroll 1
-        for (int c = 0; c < N; ++c) {
-            if (apart_at(c, group)) {
-                one_by_one(taddr + c * 32, c, c1, b, sh, slot, c0, own, table, group, kKey && group > 1 ? (g0 + c * 32) % group : 0);
-                continue;
-            }
-            uint32_t v[32];
-            __syncwarp();                                // tensor memory is for a converged warp
-            tmem_load32_async(taddr + c * 32, v);
-            tmem_load_wait();
-            add_to(v, c, c1, sh, slot, c0, own, table);
-            __syncwarp();
-            tmem_store32(taddr + c * 32, v);
+            tmem_store16(taddr + i, v);
         }
         tmem_store_wait();
         __syncwarp();
@@ -562,47 +572,31 @@ __device__ inline void bin_columns(float *bins, const BiasArgs &b, const BiasSha
 #pragma unroll 1
     for (int c = 0; c < 2; ++c) {
         float x[32];
-        Span<false> s1{};
+        int from = spans.at[0], to = from, stop = INT32_MAX;
         if (spans.one) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) x[i] = ds[i] + ds[32 + i];
-            s1.at = spans.at;
-            s1.n = 0;
         } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i) x[i] = c ? ds[32 + i] : ds[i];
-            s1 = spans.of(c);
+            spans.of(c, from, to, stop);
         }
         const int32_t *pos = sh.pos[slot] + q * 64 + c * 32;
-        const bool many = !spans.one && (spans.many >> c & 1u), more = !spans.one && (spans.more >> c & 1u);
-        const int first = __reduce_min_sync(0xFFFFFFFFu, s1.at), last = __reduce_max_sync(0xFFFFFFFFu, s1.at + s1.n);
+        const bool many = !spans.one && (spans.many >> c & 1u);
+        const int first = __reduce_min_sync(0xFFFFFFFFu, from), last = __reduce_max_sync(0xFFFFFFFFu, to);
         if (first != cur || first != last) {
             if (cur >= 0) add_to_bin(bins, cur, group, g0, run, lane);
             run = 0.f;
             cur = first == last ? first : -1;
         }
-        float part[kMost + 1] = {};                      // by bucket from at on
-        if (more && !many) {
-#pragma unroll
-            for (int i = 0; i < 32; i += 4) {
-                const int4 p4 = *reinterpret_cast<const int4 *>(pos + i);
-                const int p[4] = {p4.x, p4.y, p4.z, p4.w};
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const bool b0 = s1.beyond(0, p[k]), b1 = s1.beyond(1, p[k]), b2 = s1.beyond(2, p[k]);
-                    if (!b0) part[0] += x[i + k];
-                    if (b0 && !b1) part[1] += x[i + k];
-                    if (b1 && !b2) part[2] += x[i + k];
-                    if (b2) part[3] += x[i + k];
-                }
-            }
-        } else if (!many) {
+        float below = 0.f, above = 0.f;
+        if (!many) {
             float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
             if (!spans.one && (spans.two >> c & 1u)) {
 #pragma unroll
                 for (int i = 0; i < 32; i += 4) {
                     const int4 p = *reinterpret_cast<const int4 *>(pos + i);
-                    const bool b0 = s1.beyond(0, p.x), b1 = s1.beyond(0, p.y), b2 = s1.beyond(0, p.z), b3 = s1.beyond(0, p.w);
+                    const bool b0 = p.x > stop, b1 = p.y > stop, b2 = p.z > stop, b3 = p.w > stop;
                     s2 = __fadd2_rn(s2, make_float2(b0 ? 0.f : x[i], b1 ? 0.f : x[i + 1]));
                     t2 = __fadd2_rn(t2, make_float2(b0 ? x[i] : 0.f, b1 ? x[i + 1] : 0.f));
                     s2 = __fadd2_rn(s2, make_float2(b2 ? 0.f : x[i + 2], b3 ? 0.f : x[i + 3]));
@@ -612,23 +606,18 @@ __device__ inline void bin_columns(float *bins, const BiasArgs &b, const BiasSha
 #pragma unroll
                 for (int i = 0; i < 32; i += 2) s2 = __fadd2_rn(s2, make_float2(x[i], x[i + 1]));
             }
-            part[0] = s2.x + s2.y;
-            part[1] = t2.x + t2.y;
+            below = live ? s2.x + s2.y : 0.f;
+            above = live ? t2.x + t2.y : 0.f;
         }
-#pragma unroll
-        for (int k = 0; k <= kMost; ++k) part[k] = live ? part[k] : 0.f;
         if (first == last) {
-            run += part[0];
+            run += below;
         } else {
 #pragma unroll 1
             for (int e = first; e <= last; e += 4) {
                 float s[4];
                 if (!many) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int m = e + k - s1.at;
-                        s[k] = m == 0 ? part[0] : m == 1 ? part[1] : m == 2 ? part[2] : m == 3 ? part[3] : 0.f;
-                    }
+                    for (int k = 0; k < 4; ++k) s[k] = (e + k == from ? below : 0.f) + (e + k == to && to != from ? above : 0.f);
                 } else {
                     int top[4];
 #pragma unroll
@@ -926,7 +915,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 float m = -INFINITY, l = 0.f;
                 int pos_q = 0;
                 const float *table = table_s;
-                Bucket bucket;
+                Place<false> bucket;
                 bucket.unknown();
                 if constexpr (kBias) {
                     int64_t row;
@@ -957,17 +946,17 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     uint32_t v[kBias ? 1 : 4][32];
                     float tops[4], factor = c1, add = 0.f;            // factor, add: of the scores in powers of two
                     if constexpr (kBias) {
-                        if (spans.one) add = table[spans.at];
+                        if (spans.one) add = table[spans.at[0]];
                         else factor = 1.f;
                         float highest = -INFINITY;
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
-                            const bool apart = !spans.one && spans.apart_at(c, 1);
-                            if (apart) spans.one_by_one(s_addr + c * 32, c, c1, a.bias, bias_s, jj % kWordRing, 0, pos_q, table, 1, 0);
+                            const bool looked = spans.one_by_one(c, 1);
+                            if (looked) spans.look_columns(s_addr + c * 32, c, c1, a.bias, bias_s, jj % kWordRing, 0, pos_q, table, 1, 0);
                             __syncwarp();                    // tensor memory is for a converged warp
                             tmem_load32_async(s_addr + c * 32, v[0]);
                             tmem_load_wait();
-                            if (!spans.one && !apart) spans.add_to(v[0], c, c1, bias_s, jj % kWordRing, 0, pos_q, table);
+                            if (!spans.one && !looked) spans.add_to(v[0], c, c1, bias_s, jj % kWordRing, 0, table);
                             const uint32_t seen = words[jj % kWordRing][c];
                             if (seen != 0xFFFFFFFFu) {
 #pragma unroll
@@ -1408,7 +1397,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 }
                 float rest = 0.f, run = 0.f;
                 int pos_q = 0, cur = -1;
-                Bucket bucket;
+                Place<false> bucket;
                 bucket.unknown();
                 const int g0 = kBias ? (int)((t * kTile + w * 32) % a.group) : 0;
                 const float *table = table_s;
@@ -1435,15 +1424,25 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     float p[64];
                     {
                         if constexpr (kBias)
-                            if (!spans.one) spans.in_place(tmem + lanes + (jj & 1u) * kTile + q * 64, c1, a.bias, bias_s, jj % kWordRing, q * 2, pos_q, table, 1, 0);
+#pragma unroll 1
+                            for (int c = 0; c < 2; ++c)
+                                if (spans.one_by_one(c, 1))
+                                    spans.look_columns(tmem + lanes + (jj & 1u) * kTile + q * 64 + c * 32, c, c1, a.bias, bias_s, jj % kWordRing, q * 2, pos_q,
+                                                       table, 1, 0);
                         uint32_t v[2][32];
                         tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64, v[0]);
                         tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64 + 32, v[1]);
                         tmem_load_wait();
                         float factor = c1, add = -base;
                         if constexpr (kBias) {
-                            if (spans.one) add += table[spans.at];
-                            else factor = 1.f;
+                            if (spans.one) {
+                                add += table[spans.at[0]];
+                            } else {
+                                factor = 1.f;
+#pragma unroll
+                                for (int c = 0; c < 2; ++c)
+                                    if (!(spans.many >> c & 1u)) spans.add_to(v[c], c, c1, bias_s, jj % kWordRing, q * 2, table);
+                            }
                         }
 #pragma unroll
                         for (int e = 0; e < 64; e += 2) {
@@ -1807,7 +1806,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const int64_t key = x.kb + t * kTile + w * 32 + lane;
                 const bool live = key < x.ke, seen = live && (!a.mask || a.mask[key]);
                 int pos_k = 0;
-                Bucket bucket;
+                Place<true> bucket;
                 bucket.unknown();
                 if constexpr (kBias) pos_k = pos_of(a.bias.pos_k, min(key, x.ke - 1), x.rg.k0);
                 const bool alive = key - lane < x.ke;
@@ -1826,18 +1825,25 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     {
                         const float *table = table_s + x.h * a.group * a.bias.buckets;
                         if constexpr (kBias)
-                            if (a.group > 1 || !spans.one) {
-                                const int g0 = a.group == 1 ? 0 : (int)(((int64_t)j * kTile + q * 64) % a.group);
-                                spans.in_place(tmem + lanes + q * 64, c1, a.bias, bias_s, jj % kWordRing, q * 2, pos_k, table, a.group, g0);
-                            }
+#pragma unroll 1
+                            for (int c = 0; c < 2; ++c)
+                                if (spans.one_by_one(c, a.group))
+                                    spans.look_columns(tmem + lanes + q * 64 + c * 32, c, c1, a.bias, bias_s, jj % kWordRing, q * 2, pos_k, table, a.group,
+                                                       a.group == 1 ? 0 : (int)(((int64_t)j * kTile + q * 64 + c * 32) % a.group));
                         uint32_t v[2][32];
                         tmem_load32_async(tmem + lanes + q * 64, v[0]);
                         tmem_load32_async(tmem + lanes + q * 64 + 32, v[1]);
                         tmem_load_wait();
                         float2 factor = make_float2(c1, c1), add = make_float2(0.f, 0.f);
                         if constexpr (kBias) {
-                            if (a.group > 1 || !spans.one) factor = make_float2(1.f, 1.f);
-                            else add = make_float2(table[spans.at], table[spans.at]);
+                            if (a.group == 1 && spans.one) {
+                                add = make_float2(table[spans.at[0]], table[spans.at[0]]);
+                            } else {
+                                factor = make_float2(1.f, 1.f);
+#pragma unroll
+                                for (int c = 0; c < 2; ++c)
+                                    if (!spans.one_by_one(c, a.group)) spans.add_to(v[c], c, c1, bias_s, jj % kWordRing, q * 2, table);
+                            }
                         }
 #pragma unroll
                         for (int e = 0; e < 64; e += 4) {
