@@ -151,8 +151,8 @@ inline int64_t blocks_per_unit(const Lengths &l, int64_t factor, int64_t per, in
 bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, bool one_tile, float *part_o, float2 *part_ml, cudaStream_t st);
 // q_tiles, k_tiles: tiles of 128 rows and of 128 keys per sequence and key head; dots: [q_rows x heads] scratch
 // table_part: with a bias [n_seq x q_tiles, buckets x heads], or null where the table's gradient is not wanted
-constexpr int kTcTable = 1536;               // entries of a table of biases, buckets x heads, that fit beside the tiles
-constexpr int kTcBins = 512;                 // bins of a warp, buckets x heads of a group
+constexpr int kTcTable = 1280;               // entries of a table of biases, buckets x heads, that fit beside the tiles
+constexpr int kTcBins = 440;                 // bins of a warp, buckets x heads of a group
 bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, float *table_part, cudaStream_t st);
 
 // attention_few.cu: streaming kernels, fp32 and bf16, head_dim <= 256

@@ -94,6 +94,7 @@ struct TcShape {
     uint32_t units;
     int tiles, splits;                               // blocks of rows (or keys) per sequence and key head; stretches of the keys
     int boxes;                                       // rows of the group's heads come as boxes (the group divides 128)
+    int window;                                      // with a bias: buckets of a warp's window (dQ)
 };
 struct Work {
     SeqRange rg;
@@ -562,11 +563,60 @@ __device__ inline void add_to_bins(float *bins, int first, int last, int group, 
     __syncwarp();
     if (lane < 4 && first + lane <= last) bins[first + lane] += c;
 }
+// The dS of a thread's row in 32 columns that lie in many buckets, first .. last among the warp's rows: lanes add up theirs in a window of shared
+// memory, `wide` buckets x 32 lanes (33 apart: no two lanes in a bank), then a lane per bucket those of all lanes, in order.  (Each bucket's
+// columns picked out anew, four buckets at a time, took 3200 instructions for 26 buckets, 450 so.)
+constexpr int kWindow = 32;                              // most buckets of a window; the shared memory that is left says how many there are
+__device__ inline void bin_many(float *bins, float *window, int wide, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c, const float (&x)[32], int own,
+                                bool away, int first, int last, bool live, int group, int g0, int lane)
+{
+    const int32_t *pos = sh.pos[slot] + c * 32;
+    for (int base = first; base <= last; base += wide) {
+        __syncwarp();
+        for (int i = lane; i < wide * 33; i += 32) window[i] = 0.f;
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 32; i += 4) {
+            const int4 p4 = *reinterpret_cast<const int4 *>(pos + i);
+            const int p[4] = {p4.x, p4.y, p4.z, p4.w};
+            int at[4];
+            if (!away) {                                 // (columns that do not count may lie anywhere; their dS is 0)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) at[k] = sh.near[min((uint32_t)(p[k] - own + kNear), 2u * kNear - 1)];
+            } else {
+                const int d[4] = {apart(p[0], own), apart(p[1], own), apart(p[2], own), apart(p[3], own)};
+                look_up<4>(b, sh.edges, d, at);
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (live && (uint32_t)(at[k] - base) < (uint32_t)wide) window[(at[k] - base) * 33 + lane] += x[i + k];
+        }
+        __syncwarp();
+        if (lane < wide && base + lane <= last) {
+            const float *mine = window + lane * 33;
+            float *bin = bins + (base + lane) * group;
+            if (group == 1) {
+                float s = 0.f;
+#pragma unroll 8
+                for (int k = 0; k < 32; ++k) s += mine[k];
+                bin[0] += s;
+            } else {
+                int g = g0;
+                for (int k = 0; k < 32; ++k) {
+                    bin[g] += mine[k];
+                    g = g + 1 == group ? 0 : g + 1;
+                }
+            }
+        }
+    }
+    __syncwarp();
+}
+
 // The dS of a thread's row in the 64 columns of half q of a tile.  run, cur: sum of the bucket that the warp is in, kept in registers until it
 // leaves it.  Every bucket is summed up by itself (as differences of sums of what lies beyond its edges, a bucket of few pairs had the
 // rounding of all).
-__device__ inline void bin_columns(float *bins, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int q, const float (&ds)[64], int own,
-                                   const TileSpans<false, 2> &spans, bool live, int group, int g0, float &run, int &cur, int lane)
+__device__ inline void bin_columns(float *bins, float *window, int wide, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int q, const float (&ds)[64],
+                                   int own, const TileSpans<false, 2> &spans, bool live, int group, int g0, float &run, int &cur, int lane)
 {
     if (!__any_sync(0xFFFFFFFFu, live)) return;
 #pragma unroll 1
@@ -589,8 +639,12 @@ __device__ inline void bin_columns(float *bins, const BiasArgs &b, const BiasSha
             run = 0.f;
             cur = first == last ? first : -1;
         }
+        if (many) {
+            bin_many(bins, window, wide, b, sh, slot, q * 2 + c, x, own, spans.away >> c & 1u, first, last, live, group, g0, lane);
+            continue;
+        }
         float below = 0.f, above = 0.f;
-        if (!many) {
+        {
             float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
             if (!spans.one && (spans.two >> c & 1u)) {
 #pragma unroll
@@ -615,34 +669,8 @@ __device__ inline void bin_columns(float *bins, const BiasArgs &b, const BiasSha
 #pragma unroll 1
             for (int e = first; e <= last; e += 4) {
                 float s[4];
-                if (!many) {
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) s[k] = (e + k == from ? below : 0.f) + (e + k == to && to != from ? above : 0.f);
-                } else {
-                    int top[4];
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        s[k] = 0.f;
-                        top[k] = e + k >= last ? INT32_MAX : sh.edges[e + k] - 1;
-                    }
-#pragma unroll
-                    for (int i = 0; i < 32; i += 4) {
-                        const int4 p4 = *reinterpret_cast<const int4 *>(pos + i);
-                        const int d[4] = {apart(p4.x, own), apart(p4.y, own), apart(p4.z, own), apart(p4.w, own)};
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {                       // what is in the buckets below is gone already
-                            const float v = x[i + k];
-                            const bool b0 = d[k] <= top[0], b1 = d[k] <= top[1], b2 = d[k] <= top[2], b3 = d[k] <= top[3];
-                            if (b0) s[0] += v;
-                            if (b1 && !b0) s[1] += v;
-                            if (b2 && !b1) s[2] += v;
-                            if (b3 && !b2) s[3] += v;
-                            if (b3) x[i + k] = 0.f;
-                        }
-                    }
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) s[k] = live ? s[k] : 0.f;
-                }
+                for (int k = 0; k < 4; ++k) s[k] = (e + k == from ? below : 0.f) + (e + k == to && to != from ? above : 0.f);
                 add_to_bins(bins, e, last, group, g0, s, lane);
             }
         }
@@ -1103,7 +1131,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 // tile of keys; the scores are formed in both.  Two warpgroups share a tile of 128 x 128: 64 columns each, one row per thread.
 template <int NB, bool kBias> struct Bwd {
     static constexpr int kThreads = 12 * 32, kTileBytes = NB * kBlockBytes;      // copies, zeros, products; one idle
-    using KvRing = TileRing<NB == 2 ? 5 - kBias : 8 - 2 * kBias>;
+    using KvRing = TileRing<NB == 2 ? 5 - kBias : 8 - 2 * kBias>;      // (four slots at least: the next tile's values are waited for before its keys go)
     static constexpr int kQgStages = NB == 2 ? 4 : 8;
     static constexpr size_t kDqSmem = 1024 + (size_t)(2 + KvRing::kSlots) * kTileBytes, kDkvSmem = 1024 + (size_t)(2 + kQgStages) * kTileBytes;
 };
@@ -1194,7 +1222,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     if constexpr (kBias) {
         stage_bias(a, bias_s, table_s);
         if (table_part)
-            for (int i = threadIdx.x; i < 8 * a.bias.buckets * a.group; i += blockDim.x) bins_s[i] = 0.f;
+            for (int i = threadIdx.x; i < 8 * a.bias.buckets * a.group; i += blockDim.x) bins_s[8 * f.window * 33 + i] = 0.f;
     }
     if (threadIdx.x == 0) {
         for (int s = 0; s < R::kBarriers; ++s) mbar_init(&kv_full[s], 1);
@@ -1369,7 +1397,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         const int heads = a.kv_heads * a.group;
         uint32_t jj = 0, item = 0, corrected = 0, binned = 0;
         bool ok = true;
-        float *bins = bins_s + warp * a.bias.buckets * a.group;
+        float *window = bins_s + warp * f.window * 33, *bins = bins_s + 8 * f.window * 33 + warp * a.bias.buckets * a.group;
         for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
             const Work x = work_of(a, f, u, false);
             const int steps = x.n * passes_of<kBias>(x, a.head_dim), first = steps - x.n;
@@ -1517,7 +1545,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     }
                     if constexpr (kBias)
                         if (table_part) {
-                            bin_columns(bins, a.bias, bias_s, jj % kWordRing, q, p, pos_q, spans, live && base != INFINITY, a.group, g0, run, cur, lane);
+                            bin_columns(bins, window, f.window, a.bias, bias_s, jj % kWordRing, q, p, pos_q, spans, live && base != INFINITY, a.group, g0, run, cur, lane);
                             __syncwarp();
                         }
                     store_operand_and_rest(tmem + lanes + 256 + q * 64, tmem + lanes + (jj & 1u) * kTile + q * 64, p);
@@ -1552,7 +1580,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     for (int i = threadIdx.x; i < size; i += 256) {
                         float s = 0.f;
 #pragma unroll
-                        for (int k = 0; k < 8; ++k) s += bins_s[k * size + i];
+                        for (int k = 0; k < 8; ++k) s += bins_s[8 * f.window * 33 + k * size + i];
                         part[i / a.group * heads + i % a.group] = s;
                     }
                     __syncwarp();
@@ -1915,6 +1943,7 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
 // ------------------------------------------------------------------------------------------------- host side
 constexpr int kMaxDevices = 64;
+constexpr size_t kMostSmem = 227 * 1024 - 11 * 1024;       // dynamic, beside the 10.6 KB of a kernel with a bias
 template <typename Kernel> bool allow_smem(Kernel kernel, size_t bytes, std::atomic<bool> (&done)[kMaxDevices])
 {
     int dev = 0;
@@ -1974,14 +2003,21 @@ bool launch_bwd(const AttnArgs &a, const Maps &m, int64_t q_tiles, int64_t k_til
 {
     static std::atomic<bool> done[2][kMaxDevices] = {};
     using B = Bwd<NB, kBias>;
-    const size_t table = (size_t)a.bias.buckets * a.kv_heads * a.group * sizeof(float), bins = table_part ? 8 * (size_t)a.bias.buckets * a.group * sizeof(float) : 0;
-    if (!allow_smem(attn_tc_dq_kernel<NB, kBias>, B::kDqSmem + (kBias ? (kTcTable + 8 * kTcBins) * sizeof(float) : 0), done[0]) ||
+    const size_t table = (size_t)a.bias.buckets * a.kv_heads * a.group * sizeof(float), row = 8 * 33 * sizeof(float);
+    size_t dq_smem = B::kDqSmem + table;
+    int window = 0;
+    if (table_part) {                                    // the rest is the windows': four buckets at least (kTcTable, kTcBins)
+        dq_smem += 8 * (size_t)a.bias.buckets * a.group * sizeof(float);
+        window = (int)std::min<size_t>(kWindow, (kMostSmem - dq_smem) / row);
+        dq_smem += window * row;
+    }
+    if (!allow_smem(attn_tc_dq_kernel<NB, kBias>, kBias ? kMostSmem : B::kDqSmem, done[0]) ||
         !allow_smem(attn_tc_dkv_kernel<NB, kBias>, B::kDkvSmem + (kBias ? kTcTable * sizeof(float) : 0), done[1]))
         return false;
     const int64_t units = a.n_seq * a.kv_heads;
-    const TcShape fq{(uint32_t)(units * q_tiles), (int)q_tiles, 1, m.boxes}, fk{(uint32_t)(units * k_tiles), (int)k_tiles, 1, m.boxes};
+    const TcShape fq{(uint32_t)(units * q_tiles), (int)q_tiles, 1, m.boxes, window}, fk{(uint32_t)(units * k_tiles), (int)k_tiles, 1, m.boxes};
     note_launch();
-    attn_tc_dq_kernel<NB, kBias><<<tc_grid(fq.units, 1), B::kThreads, B::kDqSmem + table + bins, st>>>(m.q, m.g, m.k, m.v, a, fq, dots, table_part);
+    attn_tc_dq_kernel<NB, kBias><<<tc_grid(fq.units, 1), B::kThreads, dq_smem, st>>>(m.q, m.g, m.k, m.v, a, fq, dots, table_part);
     note_launch();
     attn_tc_dkv_kernel<NB, kBias><<<tc_grid(fk.units, 1), B::kThreads, B::kDkvSmem + table, st>>>(m.q, m.g, m.k, m.v, a, fk, dots);
     return true;
