@@ -632,7 +632,8 @@ SimtShape shape_of(const AttnArgs &a, int64_t tiles, int splits, int kept_rows, 
     while (f.cols > 1 && f.cols * 2 >= a.head_dim) f.cols /= 2;
     const size_t fixed = ((size_t)kept_rows * f.ld + (size_t)p_rows * kLdP) * sizeof(float), pair = (size_t)pair_rows * f.ld * sizeof(float);
     const size_t beside = a.bias.buckets ? ((size_t)kMaxBuckets + (size_t)a.bias.buckets * (a.group + bins)) * sizeof(float) : 0;
-    f.stages = (fixed + 2 * pair + beside + 2048) * blocks <= (size_t)kSmSmem ? 2 : 1;
+    const size_t two = fixed + 2 * pair + beside;
+    f.stages = (two + 2048) * blocks <= (size_t)kSmSmem && two <= (size_t)kMostSmem ? 2 : 1;
     f.tile_floats = (int)((fixed + f.stages * pair) / sizeof(float));
     smem = fixed + f.stages * pair + beside;
     return f;

@@ -174,10 +174,29 @@ def test_calls_at_once_on_two_streams():
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("heads,kv_heads,buckets", [(128, 128, 64), (64, 4, 128), (32, 1, 100), (20, 4, 64), (24, 2, 128), (512, 512, 128), (1, 1, 1), (96, 96, 3)])
+@pytest.mark.parametrize("heads,kv_heads,buckets", [(128, 128, 64), (64, 4, 128), (32, 1, 100), (20, 4, 64), (24, 2, 128), (512, 512, 128), (1, 1, 1), (96, 96, 3), (10, 1, 128),
+                                                    (8, 1, 56), (4, 1, 110), (9, 1, 64), (8, 2, 128), (3, 1, 128)])
 def test_large_tables_and_odd_groups(dtype, heads, kv_heads, buckets):
     """Tables that no block's shared memory holds whole, bins that it does not hold, groups of heads that divide no tile."""
     hd = 8 if heads > 64 else 16
     edge = [4 * (i - buckets // 2) for i in range(buckets - 1)]
     for lens, pos in ((([1, 2, 1], [60, 7, 90]), "any"), (([40, 90], [150, 33]), "any"), (([2], [2500]), "times")):
         _go(*lens, heads, kv_heads, hd, dtype, edge, pos=pos)
+
+
+@pytest.mark.parametrize("heads,kv_heads,buckets", [(10, 1, 128), (8, 1, 56), (4, 4, 127), (4, 2, 128)])
+def test_large_tables_beside_wide_heads(heads, kv_heads, buckets):
+    """Values with much in common: what the stored out lacks must not show in the table's gradient, whichever kernel forms it."""
+    edge = [9 * (i - buckets // 2) for i in range(buckets - 1)]
+    for dtype in (BF16, F32):
+        _go([150, 0, 33], [333, 40, 128], heads, kv_heads, 128, dtype, edge, pos="times", mean=4.0, runs=(dict(), dict(hints=0)))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("hd", [128, 100, 72, 64, 32])
+@pytest.mark.parametrize("heads,kv_heads", [(1, 1), (2, 1), (3, 3)])
+def test_every_size_of_table_beside_the_tiles(dtype, hd, heads, kv_heads):
+    """What a bias takes beside the tiles grows by little steps: none of them may tip over what a block is given."""
+    hd = (hd + 7) // 8 * 8
+    for buckets in [1, 2, 4, 6, 7, 8, 9, 10, 11, 12, 14, 16, 20, 24, 32, 47, 63, 80, 101, 128]:
+        _go([70], [130], heads, kv_heads, hd, dtype, [3 * (i - buckets // 2) for i in range(buckets - 1)], pos="rows")
