@@ -587,7 +587,7 @@ int32_t e2egrec_biased_attention_backward(const e2egrec_mat *dOut, const e2egrec
  * e2egrec_layer_norm_forward: z = residual + dropout(X) (residual, drop: NULL for none), Y = gain (z - m) s + shift with m the mean of a row of z
  *   and s = 1 / sqrt(mean((z - m)^2) + eps).  gain, shift: device float[dim], 16-byte aligned, NULL for ones and zeros.  Z: NULL, or receives z (a
  *   layer that norms its input carries the sum on).  stats: NULL, or device float[2 rows], 8-byte aligned, receives (m, s) of every row, all
- *   that the backward call needs besides the inputs.  Y or Z may be X or the residual.  dim <= 8192, eps > 0.
+ *   that the backward call needs besides the inputs.  Y or Z may be X or the residual, Y and Z are apart.  dim <= 8192, eps > 0.
  * e2egrec_layer_norm_backward: with g = dY gain, n = (z - m) s:  dz = s (g - mean(g) - n mean(g n)) + dZ (the gradient that comes back along Z,
  *   NULL for none);  dR = dz, the gradient with respect to the residual (NULL to skip: without dropout it equals dX);  dX = dropout(dz);
  *   dgain = sum dY n, dshift = sum dY over the rows (device float[dim], overwritten; NULL to skip).  X, residual, drop, gain and stats as in the

@@ -1368,7 +1368,7 @@ FewPlan few_plan(const AttnArgs &a, const Lengths &q, const Lengths &k, int es, 
     p.steps = max_k <= step ? 1 : (max_k <= 2 * step || (p.rows > 2 && max_k > kUnroll * step) ? 2 : kUnroll);
     while (p.steps * step > 32) p.steps /= 2;        // a turn's rows are the bits of a word
     // With a bias the kernel of all gradients goes over the keys twice, first for D, and keeps the table's bins: not where the keys go in stretches,
-    // nor where the bins of few buckets more than there are lanes leave less than two blocks per SM.
+    // nor where the bins take more shared memory than the rings of 64 KB beside them.
     if (p.both && a.bias.buckets) {
         const int64_t want = std::min(ceil_div(148 * 24, units0), ceil_div(max_k, step * p.steps));
         if (std::min(want / kFewWarps, max_k / (step * p.steps * kFewWarps * 4)) > 1 || bins_bytes(a, f, p.rows) > 64 * 1024) {

@@ -68,20 +68,6 @@ __device__ inline void tmem_load16_async(uint32_t taddr, uint32_t (&r)[16])
         : "r"(taddr));
 }
 
-__device__ inline void tmem_load8_async(uint32_t taddr, uint32_t (&r)[8])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(taddr));
-}
-
-__device__ inline void tmem_store8(uint32_t taddr, const uint32_t (&r)[8])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
-                 "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-                 : "memory");
-}
-
 // Registers are dealt out anew once the block runs, kCopies to the threads of copies and products, kScores to those of the scores.  One
 // block per SM: 384 threads x 168 at launch = 128 x 72 + 256 x 216 (forward) = 128 x 104 + 256 x 200 (backward, whose copies hold statistics
 // of rows a tile ahead; spilled, they were waited for).  Two blocks per SM: 256 threads x 128 = 128 x 72 + 128 x 184.
@@ -330,6 +316,9 @@ template <int W> __device__ inline void stage_near(const BiasArgs &b, BiasShared
     asm volatile("bar.sync 1, %0;" ::"n"(W * 32) : "memory");
 }
 
+// Where the bucket of a distance lies in that table; farther ones (of columns that do not count) have its last place
+__device__ inline uint32_t near_of(int pos_q, int pos_k) { return min((uint32_t)pos_k - (uint32_t)pos_q + kNear, 2u * kNear - 1); }
+
 __device__ inline int add_sat(int x, int y)
 {
     int s;
@@ -490,7 +479,7 @@ template <bool kKey, int N> struct TileSpans {
                     const int4 p4 = pos[k / 4];
                     const int p[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) at16[k + m] = sh.near[min((uint32_t)((kKey ? own - p[m] : p[m] - own) + kNear), 2u * kNear - 1)];
+                    for (int m = 0; m < 4; ++m) at16[k + m] = sh.near[near_of(kKey ? p[m] : own, kKey ? own : p[m])];
                 }
             } else {
 #pragma unroll
@@ -582,7 +571,7 @@ __device__ inline void bin_many(float *bins, float *window, int wide, const Bias
             int at[4];
             if (!away) {                                 // (columns that do not count may lie anywhere; their dS is 0)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) at[k] = sh.near[min((uint32_t)(p[k] - own + kNear), 2u * kNear - 1)];
+                for (int k = 0; k < 4; ++k) at[k] = sh.near[near_of(own, p[k])];
             } else {
                 const int d[4] = {apart(p[0], own), apart(p[1], own), apart(p[2], own), apart(p[3], own)};
                 look_up<4>(b, sh.edges, d, at);

@@ -353,6 +353,8 @@ int32_t check_sizes(const e2egrec_mat *X)
     return E2EGREC_OK;
 }
 bool misaligned(const float *p) { return reinterpret_cast<uintptr_t>(p) % 16; }
+// Two results in one place
+bool same_place(const e2egrec_mat *a, const e2egrec_mat *b) { return a && b && a->rows > 0 && a->data == b->data; }
 
 // Threads of a row and chunks per thread (a template argument).  Threads hold as many values as their registers allow, and with that as few as
 // possible share a row: what is done once per row, exchanges and addresses, is done for more rows by a warp then.  Of the numbers of chunks the
@@ -489,6 +491,7 @@ extern "C" int32_t e2egrec_layer_norm_forward(const e2egrec_mat *X, const e2egre
     rc = norm_args(X, residual, drop, gain, a);
     if (rc == E2EGREC_OK) rc = check_beside(Y, X);
     if (rc == E2EGREC_OK && Z) rc = check_beside(Z, X);
+    if (rc == E2EGREC_OK && same_place(Y, Z)) rc = E2EGREC_ERR_ARG;
     if (rc == E2EGREC_OK && (misaligned(shift) || reinterpret_cast<uintptr_t>(stats) % 8)) rc = E2EGREC_ERR_ALIGN;
     if (rc != E2EGREC_OK || X->rows == 0) return rc;
     a.y = Y->data;
@@ -526,7 +529,9 @@ extern "C" int32_t e2egrec_layer_norm_backward(const e2egrec_mat *dY, const e2eg
     if (rc == E2EGREC_OK) rc = check_beside(dX, X);
     if (rc == E2EGREC_OK && dR) rc = check_beside(dR, X);
     if (rc == E2EGREC_OK && X->rows && !stats) rc = E2EGREC_ERR_NULL;
-    if (rc == E2EGREC_OK && reinterpret_cast<uintptr_t>(stats) % 8) rc = E2EGREC_ERR_ALIGN;
+    if (rc == E2EGREC_OK && same_place(dX, dR)) rc = E2EGREC_ERR_ARG;
+    if (rc == E2EGREC_OK && (reinterpret_cast<uintptr_t>(stats) % 8 || reinterpret_cast<uintptr_t>(dgain) % 4 || reinterpret_cast<uintptr_t>(dshift) % 4))
+        rc = E2EGREC_ERR_ALIGN;
     if (rc != E2EGREC_OK) return rc;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (X->rows == 0) {

@@ -200,3 +200,32 @@ def test_every_size_of_table_beside_the_tiles(dtype, hd, heads, kv_heads):
     hd = (hd + 7) // 8 * 8
     for buckets in [1, 2, 4, 6, 7, 8, 9, 10, 11, 12, 14, 16, 20, 24, 32, 47, 63, 80, 101, 128]:
         _go([70], [130], heads, kv_heads, hd, dtype, [3 * (i - buckets // 2) for i in range(buckets - 1)], pos="rows")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("heads,kv_heads,hd", [(4, 4, 32), (6, 2, 72), (2, 1, 256), (3, 3, 128)])
+def test_sequences_longer_than_their_hints(dtype, heads, kv_heads, hd):
+    """Hints choose kernels, longer sequences are still right."""
+    for lens in (([1, 5, 0, 2], [40, 300, 7, 90]), ([70, 3, 130], [300, 1000, 150]), ([1, 1], [3000, 10])):
+        _go(*lens, heads, kv_heads, hd, dtype, BOTH, masked=True, mean=1.0, runs=(dict(hints=1), dict(hints=3), dict(hints=33), dict(hints=5000)))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("q_len", [1, 40, 200])
+def test_offsets_out_of_order_are_reported_and_stay_in_bounds(q_len, dtype):
+    import paper_2511_20564_b200 as E
+    x = torch.randn(3 * q_len, 64, generator=torch.Generator().manual_seed(1)).to(dtype).cuda()
+    pos = torch.arange(3 * q_len, dtype=torch.int32, device="cuda")
+    bias = E.RelativeBias(torch.ones(32, 2, device="cuda"), E.relative_edges(32, 1000), pos, pos)
+    good = torch.tensor([0, q_len, 2 * q_len, 3 * q_len], device="cuda")
+    for bad in ([0, 10 ** 12, 2 * q_len, 3 * q_len], [-5, q_len, 2 * q_len, 3 * q_len], [0, 2 * q_len, q_len, 3 * q_len]):
+        bad = torch.tensor(bad, device="cuda")
+        for hint in (q_len, 0):
+            for seqs in (E.Sequences(bad, good, hint, hint), E.Sequences(good, bad, hint, hint)):
+                status = torch.zeros(1, dtype=torch.int32, device="cuda")
+                out, lse, _ = E.biased_attention_forward(x, x, x, seqs, bias, 2, 2, 0.125, status=status)
+                assert status.item() == 1
+                status.zero_()
+                E.biased_attention_backward(x, x, x, x, torch.zeros_like(x), torch.zeros_like(lse), seqs, bias, 2, 2, 0.125, status=status)
+                assert status.item() == 1
+    torch.cuda.synchronize()

@@ -78,3 +78,14 @@ def test_the_binding_refuses_what_the_library_cannot_see():
                 lambda: E.dropout(x, None), lambda: E.layer_norm_forward(x), lambda: E.layer_norm_backward(x, x, None)):
         with pytest.raises(E.E2EGrecError):
             bad()
+
+
+def test_two_results_in_one_place_are_refused():
+    other = mat(data=8192)
+    assert forward(y=mat(), z=mat()) == ARG and backward(dx=mat(), dr=mat()) == ARG
+    assert forward(x=mat(rows=0), y=mat(rows=0), z=mat(rows=0)) == 0
+    n = C.c_size_t(1 << 40)
+    for k in (0, 1):
+        gains = [P, P]
+        gains[k] = C.c_void_p(4097)
+        assert B.lib().e2egrec_layer_norm_backward(mat(), None, mat(), None, None, P, P, mat(), other, *gains, P, C.byref(n), None) == ALIGN
