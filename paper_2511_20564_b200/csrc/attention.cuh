@@ -163,6 +163,7 @@ struct FewPlan {
     bool fit;                             // backward, bf16, more keys than one turn: dQ without what D of the stored outputs lacks
     int64_t batches;                      // units of rows per sequence and key head
     int warps, splits;                    // warps per unit, stretches of the keys
+    int kept;                             // backward with a bias, both: most keys of a warp whose p and dS are kept
     int64_t key_batches;                  // units of keys of the dK, dV kernel
     int64_t blocks;                       // of the kernel of all gradients, each of which leaves a row of the table's gradient
 };

@@ -99,7 +99,8 @@ struct FewShape {
     int splits;                                      // stretches of the keys
     uint32_t units;
     int slice, packed;                               // bytes of a row's heads of a warp; whether those of consecutive rows are one stretch
-    int ring_bytes;                                  // of all rings; bins follow
+    int ring_bytes;                                  // of all rings; bins follow, and what is kept of a warp's keys
+    int kept, kept_at;                               // most keys that a warp keeps p and dS of; where they lie
 };
 
 // A warp's ring: turns of `keys` rows of K and of V (its heads' slice of them), visible rows as bits beside them.  Turn t of the warp is
@@ -351,6 +352,10 @@ inline size_t bins_bytes(const AttnArgs &a, const FewShape &f, int rows)
 {
     return (size_t)kFewWarps * a.bias.buckets * (rows * (32 / f.lanes) + f.heads * a.group) * sizeof(float);
 }
+
+// p and dS of a warp's keys, with a key's buckets behind them
+__host__ __device__ inline int kept_bytes_of_warp(const FewShape &f, int rows, int keys) { return keys * rows * (f.heads * 8 + 1); }
+inline int kept_bytes(const FewShape &f, int rows, int keys) { return kFewWarps * kept_bytes_of_warp(f, rows, keys); }
 
 // Rows of a unit one after the other: query row and head of (query, head of the group) pair r0, r0 + 1, ...
 struct RowWalk {
@@ -821,7 +826,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     lse[r] = v * kLog2e;
                     p.load(static_cast<const T *>(a.q) + row * a.ldq + col, at, f.lanes, f.chunks);
                     t.load(static_cast<const T *>(a.dout) + row * a.ldg + col, at, f.lanes, f.chunks);
-                    if (!one_turn && !kTwice) {
+                    if (!one_turn) {
                         Piece<T, CPL> s;
                         s.load(static_cast<const T *>(a.o) + row * a.ldo + col, at, f.lanes, f.chunks);
                         float y[E];
@@ -844,11 +849,19 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         if constexpr (sizeof(T) == 2 && !kFit && !kTwice)
 #pragma unroll
             for (int r = 0; r < R; ++r) d[r] += lack.of[r];
+        bool again = true;                                   // over the keys
         if constexpr (kTwice)
-            if (f.warps > 1 || !one_turn) {                  // (the unit's warps go this way together)
-                float total[R];
+            if (!one_turn) {                                 // (the unit's warps go this way together)
+                const bool keeps = (x.ke - x.kb + ring.stride - 1) / ring.stride * ring.keys <= f.kept;
+                uint8_t *mine_kept = ring_smem + f.kept_at + warp * kept_bytes_of_warp(f, R, f.kept), *kept_bucket = mine_kept + f.kept * f.heads * 8 * R;
+                float2 *kept = reinterpret_cast<float2 *>(mine_kept) + lane / f.lanes % f.heads * R;
+                float total[R], lacks[R], mean[R][E];        // sums of p, of dS with D of the stored out, of p k
 #pragma unroll
-                for (int r = 0; r < R; ++r) total[r] = 0.f;
+                for (int r = 0; r < R; ++r) {
+                    total[r] = lacks[r] = 0.f;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) mean[r][e] = 0.f;
+                }
                 for (int t = 0; live && t < ring.turns && ring.ok; ++t) {
                     uint32_t word;
                     bias.turn(a, x, ring, t, kpw, grp);
@@ -883,8 +896,28 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     for (int i = 0; i < R * U; ++i) {
                         const float add = bias.value[i] - lse[i / U];
                         const float p = seen[i % U] ? exp2_fast(fmaf(s[i], c1, add)) : 0.f;
+                        s[i] = p;
+                        s[R * U + i] = p == 0.f ? 0.f : p * (s[R * U + i] - d[i / U]);
                         total[i / U] += p;
-                        d[i / U] += p == 0.f ? 0.f : p * s[R * U + i];
+                        lacks[i / U] += s[R * U + i];
+                    }
+                    if (keeps) {
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            Piece<T, CPL> k;
+                            float w[E];
+                            k.zero();
+                            if (seen[u]) k.load_shared(at_k + u * kpw * f.slice, at, f.lanes, f.chunks);
+                            k.widen(w);
+                            const int i = t * ring.keys + u * kpw + grp;
+#pragma unroll
+                            for (int r = 0; r < R; ++r) {
+                                axpy<E>(dq[r], s[(R + r) * U + u], w);
+                                axpy<E>(mean[r], s[r * U + u], w);
+                                if (at == 0) kept[i * f.heads * R + r] = make_float2(s[r * U + u], s[(R + r) * U + u]);
+                                if (lane % wide == 0) kept_bucket[i * R + r] = (uint8_t)bias.bucket[r * U + u];
+                            }
+                        }
                     }
                     ring.done(t);
                 }
@@ -893,7 +926,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
                         total[r] += __shfl_xor_sync(0xFFFFFFFFu, total[r], o);
-                        d[r] += __shfl_xor_sync(0xFFFFFFFFu, d[r], o);
+                        lacks[r] += __shfl_xor_sync(0xFFFFFFFFu, lacks[r], o);
                     }
                 if (f.warps > 1) {
                     __syncthreads();
@@ -901,27 +934,56 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
                         for (int r = 0; r < R; ++r) {
                             join[warp][2 * r * 32 + lane] = total[r];
-                            join[warp][(2 * r + 1) * 32 + lane] = d[r];
+                            join[warp][(2 * r + 1) * 32 + lane] = lacks[r];
                         }
                     __syncthreads();
 #pragma unroll
                     for (int r = 0; r < R; ++r) {
-                        total[r] = d[r] = 0.f;
+                        total[r] = lacks[r] = 0.f;
                         for (int w = 0; w < f.warps; ++w) {
                             total[r] += join[warp - wu + w][2 * r * 32 + lane % wide];
-                            d[r] += join[warp - wu + w][(2 * r + 1) * 32 + lane % wide];
+                            lacks[r] += join[warp - wu + w][(2 * r + 1) * 32 + lane % wide];
                         }
                     }
                     __syncthreads();
                 }
 #pragma unroll
-                for (int r = 0; r < R; ++r) d[r] = total[r] == 0.f ? 0.f : d[r] / total[r];
-                if (live) {
+                for (int r = 0; r < R; ++r) {
+                    lacks[r] = total[r] == 0.f ? 0.f : lacks[r] / total[r];
+                    d[r] += lacks[r];
+                }
+                again = !keeps;
+                if (again && live) {
                     bias.begin(a, x, ring);
                     ring.start();
+                } else if (live && ring.ok) {
+                    __syncwarp();
+#pragma unroll
+                    for (int r = 0; r < R; ++r) axpy<E>(dq[r], -lacks[r], mean[r]);
+                    for (int t = 0; t < ring.turns; ++t)
+#pragma unroll
+                        for (int u = 0; u < U; ++u) {
+                            const int i = t * ring.keys + u * kpw + grp;
+                            const int64_t j = x.kb + ring.first + t * ring.stride + u * kpw + grp;
+                            float dk[E], dv[E];
+#pragma unroll
+                            for (int e = 0; e < E; ++e) dk[e] = dv[e] = 0.f;
+#pragma unroll
+                            for (int r = 0; r < R; ++r) {
+                                const float2 w = kept[i * f.heads * R + r];
+                                const float ds = fmaf(-lacks[r], w.x, w.y);
+                                axpy<E>(dk, ds, q[r]);
+                                axpy<E>(dv, w.x, g[r]);
+                                if (binned && at == 0) bins.add(r, kept_bucket[i * R + r], lane / f.lanes, ds);
+                            }
+                            if (whole && x.on && j < x.ke) {
+                                store_piece<T, CPL>(static_cast<T *>(a.dk) + j * a.ldk2 + koff, at, f.lanes, f.chunks, dk, a.scale);
+                                store_piece<T, CPL>(static_cast<T *>(a.dv) + j * a.ldv2 + koff, at, f.lanes, f.chunks, dv, 1.f);
+                            }
+                        }
                 }
             }
-        for (int t = 0; live && t < ring.turns && ring.ok; ++t) {
+        for (int t = 0; live && again && t < ring.turns && ring.ok; ++t) {
             uint32_t word;
             if constexpr (kBias) bias.turn(a, x, ring, t, kpw, grp);
             const uint32_t at_k = ring.wait(word, t, &abort_flag) + grp * f.slice + mine, at_v = at_k + ring.half;
@@ -1011,7 +1073,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             }
             ring.done(t);
         }
-        if (live) ring.used += ring.turns;
+        if (live && again) ring.used += ring.turns;
         if (binned && live) bins.flush(a, f, (int)(r0 % a.group), lane);
         for (int o = wide; o < 32; o <<= 1)
 #pragma unroll
@@ -1280,9 +1342,9 @@ bool launch_bwd_of(const AttnArgs &a, FewShape f, unsigned grid, float *part_dq,
     static std::atomic<bool> done[kMaxDevices] = {};
     if (!allow_smem(attn_few_bwd_kernel<T, R, U, CPL, kBoth, kFit, kBias>, done)) return false;
     f.ring_bytes = (int)few_smem<U>(f);
+    f.kept_at = f.ring_bytes + (int)(kBias && kBoth && table_part ? bins_bytes(a, f, R) : 0);
     note_launch();
-    attn_few_bwd_kernel<T, R, U, CPL, kBoth, kFit, kBias>
-        <<<grid, kFewThreads, f.ring_bytes + (kBias && kBoth && table_part ? bins_bytes(a, f, R) : 0), st>>>(a, f, part_dq, dots, table_part);
+    attn_few_bwd_kernel<T, R, U, CPL, kBoth, kFit, kBias><<<grid, kFewThreads, f.kept_at + kept_bytes(f, R, f.kept), st>>>(a, f, part_dq, dots, table_part);
     return true;
 }
 
@@ -1386,7 +1448,13 @@ FewPlan few_plan(const AttnArgs &a, const Lengths &q, const Lengths &k, int es, 
     while (p.warps < kFewWarps && p.warps < want) p.warps *= 2;
     // a stretch is worth its join where every warp has four turns of it
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>({want / p.warps, max_k / (turn * p.warps * 4), kMaxSplits, most / p.batches}));
-    if (p.both && a.bias.buckets) p.splits = 1;
+    if (p.both && a.bias.buckets) {
+        p.splits = 1;
+        // what is known of a key is kept where that leaves two blocks per SM
+        const int64_t keys = align_up((size_t)(ceil_div(max_k, turn * p.warps) * turn), 8);
+        const size_t ring = (size_t)kFewWarps * kStages * 2 * turn * f.slice;
+        if (es == 2 && keys <= 4096 && ring + bins_bytes(a, f, p.rows) + kept_bytes(f, p.rows, (int)keys) <= 110 * 1024) p.kept = (int)keys;
+    }
     p.blocks = ceil_div(units0 * p.batches, kFewWarps / p.warps);
     p.key_batches = blocks_per_unit(k, 1, step * kKeys, units0);
     return p;
@@ -1424,6 +1492,7 @@ bool few_attention_table(const AttnArgs &a, const TablePlan &p, int32_t dtype, c
 static FewShape planned(const AttnArgs &a, const FewPlan &p, int32_t dtype)
 {
     FewShape f = few_shape(a, (int)dtype_size(dtype));
+    f.kept = p.kept;
     f.warps = p.warps;
     f.batches = (int)p.batches;
     f.splits = p.splits;
