@@ -960,6 +960,13 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     __syncwarp();
 #pragma unroll
                     for (int r = 0; r < R; ++r) axpy<E>(dq[r], -lacks[r], mean[r]);
+                    float run[R];                            // dS of the bucket that the lane is in
+                    int cur[R];
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        run[r] = 0.f;
+                        cur[r] = 0;
+                    }
                     for (int t = 0; t < ring.turns; ++t)
 #pragma unroll
                         for (int u = 0; u < U; ++u) {
@@ -974,13 +981,24 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                                 const float ds = fmaf(-lacks[r], w.x, w.y);
                                 axpy<E>(dk, ds, q[r]);
                                 axpy<E>(dv, w.x, g[r]);
-                                if (binned && at == 0) bins.add(r, kept_bucket[i * R + r], lane / f.lanes, ds);
+                                if (binned) {
+                                    const int bucket = kept_bucket[i * R + r];
+                                    if (bucket != cur[r]) {
+                                        if (at == 0) bins.add(r, cur[r], lane / f.lanes, run[r]);
+                                        run[r] = 0.f;
+                                        cur[r] = bucket;
+                                    }
+                                    run[r] += ds;
+                                }
                             }
                             if (whole && x.on && j < x.ke) {
                                 store_piece<T, CPL>(static_cast<T *>(a.dk) + j * a.ldk2 + koff, at, f.lanes, f.chunks, dk, a.scale);
                                 store_piece<T, CPL>(static_cast<T *>(a.dv) + j * a.ldv2 + koff, at, f.lanes, f.chunks, dv, 1.f);
                             }
                         }
+                    if (binned && at == 0)
+#pragma unroll
+                        for (int r = 0; r < R; ++r) bins.add(r, cur[r], lane / f.lanes, run[r]);
                 }
             }
         for (int t = 0; live && again && t < ring.turns && ring.ok; ++t) {
