@@ -68,6 +68,13 @@ __device__ inline void tmem_load16_async(uint32_t taddr, uint32_t (&r)[16])
         : "r"(taddr));
 }
 
+__device__ inline void tmem_load8_async(uint32_t taddr, uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr));
+}
+
 // Registers are dealt out anew once the block runs, kCopies to the threads of copies and products, kScores to those of the scores.  One
 // block per SM: 384 threads x 168 at launch = 128 x 72 + 256 x 216 (forward) = 128 x 104 + 256 x 200 (backward, whose copies hold statistics
 // of rows a tile ahead; spilled, they were waited for).  Two blocks per SM: 256 threads x 128 = 128 x 72 + 128 x 184.
@@ -554,9 +561,10 @@ __device__ inline void add_to_bins(float *bins, int first, int last, int group, 
 }
 // The dS of a thread's row in 32 columns that lie in many buckets, first .. last among the warp's rows: lanes add up theirs in a window of shared
 // memory, `wide` buckets x 32 lanes (33 apart: no two lanes in a bank), then a lane per bucket those of all lanes, in order.  (Each bucket's
-// columns picked out anew, four buckets at a time, took 3200 instructions for 26 buckets, 450 so.)
+// columns picked out anew, four buckets at a time, took 3200 instructions for 26 buckets, 450 so.  dS comes from tensor memory, eight columns after eight:
+// unrolled over 32 in registers the kernel's code did not fit the instruction cache as well, 8 x 2048 x 2048 backward 1621 us, 1514 so.)
 constexpr int kWindow = 32;                              // most buckets of a window; the shared memory that is left says how many there are
-__device__ inline void bin_many(float *bins, float *window, int wide, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c, const float (&x)[32], int own,
+__device__ inline void bin_many(float *bins, float *window, int wide, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c, uint32_t taddr, int own,
                                 bool away, int first, int last, bool live, int group, int g0, int lane)
 {
     const int32_t *pos = sh.pos[slot] + c * 32;
@@ -564,21 +572,28 @@ __device__ inline void bin_many(float *bins, float *window, int wide, const Bias
         __syncwarp();
         for (int i = lane; i < wide * 33; i += 32) window[i] = 0.f;
         __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 32; i += 4) {
-            const int4 p4 = *reinterpret_cast<const int4 *>(pos + i);
-            const int p[4] = {p4.x, p4.y, p4.z, p4.w};
-            int at[4];
+#pragma unroll 1
+        for (int i = 0; i < 32; i += 8) {
+            const int4 p4 = *reinterpret_cast<const int4 *>(pos + i), o4 = *reinterpret_cast<const int4 *>(pos + i + 4);
+            const int p[8] = {p4.x, p4.y, p4.z, p4.w, o4.x, o4.y, o4.z, o4.w};
+            int at[8];
+            uint32_t x[8];
+            __syncwarp();                                // tensor memory is for a converged warp
+            tmem_load8_async(taddr + i, x);
             if (!away) {                                 // (columns that do not count may lie anywhere; their dS is 0)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) at[k] = sh.near[near_of(own, p[k])];
+                for (int k = 0; k < 8; ++k) at[k] = sh.near[near_of(own, p[k])];
             } else {
-                const int d[4] = {apart(p[0], own), apart(p[1], own), apart(p[2], own), apart(p[3], own)};
-                look_up<4>(b, sh.edges, d, at);
-            }
+                int d[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (live && (uint32_t)(at[k] - base) < (uint32_t)wide) window[(at[k] - base) * 33 + lane] += x[i + k];
+                for (int k = 0; k < 8; ++k) d[k] = apart(p[k], own);
+                look_up<8>(b, sh.edges, d, at);
+            }
+            __syncwarp();
+            tmem_load_wait();
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (live && (uint32_t)(at[k] - base) < (uint32_t)wide) window[(at[k] - base) * 33 + lane] += __uint_as_float(x[k]);
         }
         __syncwarp();
         if (lane < wide && base + lane <= last) {
@@ -604,7 +619,7 @@ __device__ inline void bin_many(float *bins, float *window, int wide, const Bias
 // The dS of a thread's row in the 64 columns of half q of a tile.  run, cur: sum of the bucket that the warp is in, kept in registers until it
 // leaves it.  Every bucket is summed up by itself (as differences of sums of what lies beyond its edges, a bucket of few pairs had the
 // rounding of all).
-__device__ inline void bin_columns(float *bins, float *window, int wide, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int q, const float (&ds)[64],
+__device__ inline void bin_columns(float *bins, float *window, int wide, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int q, uint32_t taddr, const float (&ds)[64],
                                    int own, const TileSpans<false, 2> &spans, bool live, int group, int g0, float &run, int &cur, int lane)
 {
     if (!__any_sync(0xFFFFFFFFu, live)) return;
@@ -628,8 +643,14 @@ __device__ inline void bin_columns(float *bins, float *window, int wide, const B
             run = 0.f;
             cur = first == last ? first : -1;
         }
-        if (many) {
-            bin_many(bins, window, wide, b, sh, slot, q * 2 + c, x, own, spans.away >> c & 1u, first, last, live, group, g0, lane);
+        if (many) {                                      // the columns' dS to where dP was, to be read again in a loop
+            uint32_t v[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(x[i]);
+            __syncwarp();
+            tmem_store32(taddr + c * 32, v);
+            tmem_store_wait();
+            bin_many(bins, window, wide, b, sh, slot, q * 2 + c, taddr + c * 32, own, spans.away >> c & 1u, first, last, live, group, g0, lane);
             continue;
         }
         float below = 0.f, above = 0.f;
@@ -1534,7 +1555,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     }
                     if constexpr (kBias)
                         if (table_part) {
-                            bin_columns(bins, window, f.window, a.bias, bias_s, jj % kWordRing, q, p, pos_q, spans, live && base != INFINITY, a.group, g0, run, cur, lane);
+                            bin_columns(bins, window, f.window, a.bias, bias_s, jj % kWordRing, q, tmem + lanes + 256 + q * 64, p, pos_q, spans, live && base != INFINITY, a.group, g0, run, cur, lane);
                             __syncwarp();
                         }
                     store_operand_and_rest(tmem + lanes + 256 + q * 64, tmem + lanes + (jj & 1u) * kTile + q * 64, p);
