@@ -618,61 +618,67 @@ __device__ inline void bin_many(float *bins, float *window, int wide, const Bias
 
 // The dS of a thread's row in the 64 columns of half q of a tile.  run, cur: sum of the bucket that the warp is in, kept in registers until it
 // leaves it.  Every bucket is summed up by itself (as differences of sums of what lies beyond its edges, a bucket of few pairs had the
-// rounding of all).
+// rounding of all).  taddr: where dP was; a tile in more than one bucket puts dS there, to be read again in loops.
 __device__ inline void bin_columns(float *bins, float *window, int wide, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int q, uint32_t taddr, const float (&ds)[64],
                                    int own, const TileSpans<false, 2> &spans, bool live, int group, int g0, float &run, int &cur, int lane)
 {
     if (!__any_sync(0xFFFFFFFFu, live)) return;
+    float all = 0.f;
+    if (spans.one) {
+        float2 s2[2] = {};
+#pragma unroll
+        for (int i = 0; i < 64; i += 2) s2[i / 2 & 1] = __fadd2_rn(s2[i / 2 & 1], make_float2(ds[i], ds[i + 1]));
+        all = (s2[0].x + s2[0].y) + (s2[1].x + s2[1].y);
+    } else {
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            uint32_t v[32];
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(ds[c * 32 + i]);
+            tmem_store32(taddr + c * 32, v);
+        }
+        tmem_store_wait();
+    }
 #pragma unroll 1
     for (int c = 0; c < 2; ++c) {
-        float x[32];
         int from = spans.at[0], to = from, stop = INT32_MAX;
-        if (spans.one) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = ds[i] + ds[32 + i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) x[i] = c ? ds[32 + i] : ds[i];
-            spans.of(c, from, to, stop);
-        }
-        const int32_t *pos = sh.pos[slot] + q * 64 + c * 32;
-        const bool many = !spans.one && (spans.many >> c & 1u);
+        if (!spans.one) spans.of(c, from, to, stop);
         const int first = __reduce_min_sync(0xFFFFFFFFu, from), last = __reduce_max_sync(0xFFFFFFFFu, to);
         if (first != cur || first != last) {
             if (cur >= 0) add_to_bin(bins, cur, group, g0, run, lane);
             run = 0.f;
             cur = first == last ? first : -1;
         }
-        if (many) {                                      // the columns' dS to where dP was, to be read again in a loop
-            uint32_t v[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(x[i]);
-            __syncwarp();
-            tmem_store32(taddr + c * 32, v);
-            tmem_store_wait();
+        if (!spans.one && (spans.many >> c & 1u)) {
             bin_many(bins, window, wide, b, sh, slot, q * 2 + c, taddr + c * 32, own, spans.away >> c & 1u, first, last, live, group, g0, lane);
             continue;
         }
-        float below = 0.f, above = 0.f;
-        {
+        float below = all, above = 0.f;
+        if (!spans.one) {
+            const int32_t *pos = sh.pos[slot] + q * 64 + c * 32;
             float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
-            if (!spans.one && (spans.two >> c & 1u)) {
+#pragma unroll 1
+            for (int i = 0; i < 32; i += 8) {
+                const int4 p = *reinterpret_cast<const int4 *>(pos + i), o = *reinterpret_cast<const int4 *>(pos + i + 4);
+                const int at[8] = {p.x, p.y, p.z, p.w, o.x, o.y, o.z, o.w};
+                uint32_t v[8];
+                __syncwarp();                                // tensor memory is for a converged warp
+                tmem_load8_async(taddr + c * 32 + i, v);
+                tmem_load_wait();
 #pragma unroll
-                for (int i = 0; i < 32; i += 4) {
-                    const int4 p = *reinterpret_cast<const int4 *>(pos + i);
-                    const bool b0 = p.x > stop, b1 = p.y > stop, b2 = p.z > stop, b3 = p.w > stop;
-                    s2 = __fadd2_rn(s2, make_float2(b0 ? 0.f : x[i], b1 ? 0.f : x[i + 1]));
-                    t2 = __fadd2_rn(t2, make_float2(b0 ? x[i] : 0.f, b1 ? x[i + 1] : 0.f));
-                    s2 = __fadd2_rn(s2, make_float2(b2 ? 0.f : x[i + 2], b3 ? 0.f : x[i + 3]));
-                    t2 = __fadd2_rn(t2, make_float2(b2 ? x[i + 2] : 0.f, b3 ? x[i + 3] : 0.f));
+                for (int k = 0; k < 8; k += 2) {
+                    const bool b0 = at[k] > stop, b1 = at[k + 1] > stop;
+                    const float2 x = pair_of(v[k], v[k + 1]);
+                    s2 = __fadd2_rn(s2, make_float2(b0 ? 0.f : x.x, b1 ? 0.f : x.y));
+                    t2 = __fadd2_rn(t2, make_float2(b0 ? x.x : 0.f, b1 ? x.y : 0.f));
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 32; i += 2) s2 = __fadd2_rn(s2, make_float2(x[i], x[i + 1]));
             }
-            below = live ? s2.x + s2.y : 0.f;
-            above = live ? t2.x + t2.y : 0.f;
+            below = s2.x + s2.y;
+            above = t2.x + t2.y;
         }
+        below = live ? below : 0.f;
+        above = live ? above : 0.f;
         if (first == last) {
             run += below;
         } else {
