@@ -383,7 +383,7 @@ static int32_t attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q,
     float *dots = static_cast<float *>(ws), *part_dq = reinterpret_cast<float *>(static_cast<char *>(ws) + plan.dot_bytes);
     bool ok = true;
     if (plan.path == Path::tc) {
-        ok = tc_attention_backward(a, plan.q_tiles, plan.k_tiles, dots, plan.table_fused && dtable ? table_part : nullptr, st);
+        ok = tc_attention_backward(a, plan.q_tiles, plan.k_tiles, dots, plan.table_fused && dtable ? table_part : nullptr, dtable != nullptr, st);
     } else if (plan.path == Path::simt) {
         ok = simt_attention_backward(a, plan.simt, part_dq, dots, plan.table_fused && dtable ? table_part : nullptr, st);
         if (ok && plan.splits > 1 && a.q_rows) join_dq(a, plan.splits, Q->dtype, false, part_dq, nullptr, st);

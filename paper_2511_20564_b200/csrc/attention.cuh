@@ -153,7 +153,8 @@ bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, bool one
 // table_part: with a bias [n_seq x q_tiles, buckets x heads], or null where the table's gradient is not wanted
 constexpr int kTcTable = 1280;               // entries of a table of biases, buckets x heads, that fit beside the tiles
 constexpr int kTcBins = 440;                 // bins of a warp, buckets x heads of a group
-bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, float *table_part, cudaStream_t st);
+// exact: the table's gradient is formed, here or from dots
+bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, float *table_part, bool exact, cudaStream_t st);
 
 // attention_few.cu: streaming kernels, fp32 and bf16, head_dim <= 256
 struct FewPlan {

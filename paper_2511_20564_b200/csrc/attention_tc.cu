@@ -88,6 +88,7 @@ struct TcShape {
     int tiles, splits;                               // blocks of rows (or keys) per sequence and key head; stretches of the keys
     int boxes;                                       // rows of the group's heads come as boxes (the group divides 128)
     int window;                                      // with a bias: buckets of a warp's window (dQ)
+    int exact;                                       // with a bias: D goes into the table's gradient
 };
 struct Work {
     SeqRange rg;
@@ -1201,7 +1202,10 @@ __device__ inline void store_row(uint32_t taddr, bf16 *out, int head_dim, float 
 }
 
 // Passes over the keys
-template <bool kBias> __device__ inline int passes_of(const Work &x, int head_dim) { return kBias ? min(x.n, 2) : ((int64_t)x.n * kTile > 32 * head_dim ? 2 : 1); }
+template <bool kBias> __device__ inline int passes_of(const Work &x, const TcShape &f, int head_dim)
+{
+    return kBias && f.exact ? min(x.n, 2) : ((int64_t)x.n * kTile > 32 * head_dim ? 2 : 1);
+}
 
 // dQ, and D = dO . out of every row for the other kernel.  What the stored out's D lacks is the sum of p (dP - D) over the keys; it meets
 // sum p k in dQ, which does not get smaller with the number of keys, as dQ does.  Where one tile holds all keys it is added to D before dS is
@@ -1211,8 +1215,8 @@ template <bool kBias> __device__ inline int passes_of(const Work &x, int head_di
 // for values whose mean is a quarter of their spread.
 // dS goes into its product as two bf16 operands, its rounding and the rest: with dS rounded once dQ was 2.5 to 2.7e-3 off in the mean (a
 // rounding of the result: 1.8e-3), at most 2.4e-3 so; the training case's backward pass takes 550 us with one operand, 585 us so.
-// With a bias all sequences of more than one tile take the second pass: the table's gradient, sums of dS that are left from what cancels, needs
-// D as it is.  Each warp adds up its rows' dS by bucket in bins of its own; a unit's bins, in the order of the warps, are a row of part
+// Where the gradient of a table of biases is wanted all sequences of more than one tile take the second pass: sums of dS that are left from what
+// cancels need D as it is.  Each warp adds up its rows' dS by bucket in bins of its own; a unit's bins, in the order of the warps, are a row of part
 // [sequences x tiles, buckets x heads], which the caller adds up.
 template <int NB, bool kBias>
 __global__ void __launch_bounds__(Bwd<NB, kBias>::kThreads, 1)
@@ -1275,7 +1279,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             bool ok = true;
             for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
                 const Work x = work_of(a, f, u, lane == 0);
-                const int steps = x.n * passes_of<kBias>(x, a.head_dim);
+                const int steps = x.n * passes_of<kBias>(x, f, a.head_dim);
                 for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                     Visible seen;
                     Ahead places;
@@ -1334,7 +1338,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             bool ok = true;
             for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
                 const Work x = work_of(a, f, u, false);
-                const int steps = x.n * passes_of<kBias>(x, a.head_dim);
+                const int steps = x.n * passes_of<kBias>(x, f, a.head_dim);
                 for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles)
                     for (int j = 0; j < steps && ok; ++j, ++jj, g += 2) {
                         ok = warp_wait(&kv_full[R::full(0, jj)], R::parity(jj), &abort_flag);
@@ -1363,7 +1367,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 };
                 for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
                     const Work x = work_of(a, f, u, false);
-                    const int steps = x.n * passes_of<kBias>(x, a.head_dim), first = steps - x.n;      // of the last pass
+                    const int steps = x.n * passes_of<kBias>(x, f, a.head_dim), first = steps - x.n;      // of the last pass
                     for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                         ok = tile_ready(&q_full, item & 1u, &abort_flag);
                         if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
@@ -1416,7 +1420,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         float *window = bins_s + warp * f.window * 33, *bins = bins_s + 8 * f.window * 33 + warp * a.bias.buckets * a.group;
         for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
             const Work x = work_of(a, f, u, false);
-            const int steps = x.n * passes_of<kBias>(x, a.head_dim), first = steps - x.n;
+            const int steps = x.n * passes_of<kBias>(x, f, a.head_dim), first = steps - x.n;
             for (int64_t t = x.t0; t * kTile < x.rows && ok; t += f.tiles) {
                 const int64_t r = t * kTile + w * 32 + lane;
                 int64_t row;
@@ -2015,7 +2019,7 @@ template <int NB, int NT, bool kBias> bool launch_fwd(const AttnArgs &a, const M
 }
 
 template <int NB, bool kBias>
-bool launch_bwd(const AttnArgs &a, const Maps &m, int64_t q_tiles, int64_t k_tiles, float *dots, float *table_part, cudaStream_t st)
+bool launch_bwd(const AttnArgs &a, const Maps &m, int64_t q_tiles, int64_t k_tiles, float *dots, float *table_part, bool exact, cudaStream_t st)
 {
     static std::atomic<bool> done[2][kMaxDevices] = {};
     using B = Bwd<NB, kBias>;
@@ -2031,7 +2035,7 @@ bool launch_bwd(const AttnArgs &a, const Maps &m, int64_t q_tiles, int64_t k_til
         !allow_smem(attn_tc_dkv_kernel<NB, kBias>, B::kDkvSmem + (kBias ? kTcTable * sizeof(float) : 0), done[1]))
         return false;
     const int64_t units = a.n_seq * a.kv_heads;
-    const TcShape fq{(uint32_t)(units * q_tiles), (int)q_tiles, 1, m.boxes, window}, fk{(uint32_t)(units * k_tiles), (int)k_tiles, 1, m.boxes};
+    const TcShape fq{(uint32_t)(units * q_tiles), (int)q_tiles, 1, m.boxes, window, exact}, fk{(uint32_t)(units * k_tiles), (int)k_tiles, 1, m.boxes};
     note_launch();
     attn_tc_dq_kernel<NB, kBias><<<tc_grid(fq.units, 1), B::kThreads, dq_smem, st>>>(m.q, m.g, m.k, m.v, a, fq, dots, table_part);
     note_launch();
@@ -2056,13 +2060,15 @@ bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, bool one
     return a.bias.table ? forward_of<true>(a, m, f, one_tile, part_o, part_ml, st) : forward_of<false>(a, m, f, one_tile, part_o, part_ml, st);
 }
 
-bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, float *table_part, cudaStream_t st)
+bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, float *table_part, bool exact, cudaStream_t st)
 {
     Maps m;
     if (!make_maps(a, m)) return false;
     if (a.bias.table)
-        return a.head_dim <= 64 ? launch_bwd<1, true>(a, m, q_tiles, k_tiles, dots, table_part, st) : launch_bwd<2, true>(a, m, q_tiles, k_tiles, dots, table_part, st);
-    return a.head_dim <= 64 ? launch_bwd<1, false>(a, m, q_tiles, k_tiles, dots, nullptr, st) : launch_bwd<2, false>(a, m, q_tiles, k_tiles, dots, nullptr, st);
+        return a.head_dim <= 64 ? launch_bwd<1, true>(a, m, q_tiles, k_tiles, dots, table_part, exact, st)
+                                : launch_bwd<2, true>(a, m, q_tiles, k_tiles, dots, table_part, exact, st);
+    return a.head_dim <= 64 ? launch_bwd<1, false>(a, m, q_tiles, k_tiles, dots, nullptr, false, st)
+                            : launch_bwd<2, false>(a, m, q_tiles, k_tiles, dots, nullptr, false, st);
 }
 
 }  // namespace e2egrec

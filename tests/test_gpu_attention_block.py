@@ -229,3 +229,17 @@ def test_offsets_out_of_order_are_reported_and_stay_in_bounds(q_len, dtype):
                 E.biased_attention_backward(x, x, x, x, torch.zeros_like(x), torch.zeros_like(lse), seqs, bias, 2, 2, 0.125, status=status)
                 assert status.item() == 1
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_a_table_without_a_gradient(dtype):
+    """table_grad=False: nothing of the table's gradient is formed, the others are within the same bounds."""
+    import paper_2511_20564_b200 as E
+    for lens in (([1] * 30, [100] * 30), ([70, 3, 200], [300, 40, 700]), ([2, 1], [4000, 100])):
+        p = Problem(*lens, 4, 2, 64, dtype, BOTH, masked=True)
+        res, want = p.run(E), p.want()
+        args = [t.cuda() for t in (p.g_in, p.q_in, p.k_in, p.v_in)]
+        dq, dk, dv, dtable, _ = E.biased_attention_backward(*args, res["out"], res["lse"], p.seqs(E), p.bias(E), 4, 2, p.scale, table_grad=False)
+        assert dtable is None
+        for got, name, live in ((dq, "dq", p.live_q), (dk, "dk", p.live_k), (dv, "dv", p.live_k)):
+            _held(got[live], want[name][0][live], want[name][1][live], name)
