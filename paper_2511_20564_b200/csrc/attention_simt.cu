@@ -225,7 +225,8 @@ __device__ inline void row_of(const AttnArgs &a, const SimtUnit &x, int64_t r, i
 
 // ---- Bias by distance: positions of a tile's keys (and rows) lie beside it, every score looks its bucket up by bisection, the J of a row side by
 // side.  The gradient of the table is formed beside dQ: every thread has bins of its own in shared memory, [buckets x threads], added up at
-// the unit's end in a fixed order.  That wants a thread's rows to be of one head: groups that divide 16.
+// the unit's end in a fixed order.  That wants a thread's rows to be of one head: groups that divide 16.  77 x 61 x 307, 4 on 2 heads of 36:
+// forward 57 us (47 without a bias), backward 176 (135; 164 without the table's gradient).
 struct SimtBias {
     int32_t *edges;                                      // kMaxBuckets, beyond the last the highest number
     float *table;                                        // [heads of the group x buckets], in powers of two

@@ -236,8 +236,9 @@ struct Visible {
 // columns: the edge between them is a threshold that the columns' positions are compared with.  More (close to the diagonal): every score looks
 // its bucket up, in a table of the distances up to kNear, or by bisection, and gets its bias in tensor memory beforehand.  The buckets are found while the
 // tile's products are on their way: positions are there a tile ahead.
-// What decides is latency and the code's size.  Forward pass of 8 x 2048 x 2048, heads of 128 (123 us without a bias): 690 us with all ways in the
-// registers that hold a row of 128 scores (stalls for instructions), 270 with biases in tensor memory, 32 columns after 32.
+// What decides is latency and the code's size.  Forward pass of 8 x 2048 x 2048, heads of 128 (125 us without a bias): 690 us with all ways in the
+// registers that hold a row of 128 scores (stalls for instructions), 270 with biases in tensor memory, 32 columns after 32, 243 with thresholds of
+// positions.  One bucket for all pairs: 168 us.  Backward pass 1467 us (420 without a bias; 812 with one bucket; 832 without the table's gradient).
 constexpr int kNear = 2048;
 struct BiasShared {
     int32_t pos[kWordRing][kTile];                   // of the tile's columns: keys (forward pass, dQ), rows of Q (dK, dV)
@@ -562,8 +563,8 @@ __device__ inline void add_to_bins(float *bins, int first, int last, int group, 
 }
 // The dS of a thread's row in 32 columns that lie in many buckets, first .. last among the warp's rows: lanes add up theirs in a window of shared
 // memory, `wide` buckets x 32 lanes (33 apart: no two lanes in a bank), then a lane per bucket those of all lanes, in order.  (Each bucket's
-// columns picked out anew, four buckets at a time, took 3200 instructions for 26 buckets, 450 so.  dS comes from tensor memory, eight columns after eight:
-// unrolled over 32 in registers the kernel's code did not fit the instruction cache as well, 8 x 2048 x 2048 backward 1621 us, 1514 so.)
+// columns picked out anew, four buckets at a time, took 3200 instructions for 26 buckets, 450 so.)  dS comes from tensor memory, eight columns
+// after eight: unrolled over 32 in registers, with more code for the warps to fetch, the backward pass of 8 x 2048 x 2048 took 1621 us, 1514 so.
 constexpr int kWindow = 32;                              // most buckets of a window; the shared memory that is left says how many there are
 __device__ inline void bin_many(float *bins, float *window, int wide, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c, uint32_t taddr, int own,
                                 bool away, int first, int last, bool live, int group, int g0, int lane)
