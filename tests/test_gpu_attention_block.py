@@ -11,6 +11,7 @@ from test_gpu_residual import _held
 pytestmark = pytest.mark.gpu
 
 BF16, F32 = torch.bfloat16, torch.float32
+LOG_NEAR = F.edges(16, 200, True)
 
 
 def _same(got, want, problem):
@@ -243,3 +244,34 @@ def test_a_table_without_a_gradient(dtype):
         assert dtable is None
         for got, name, live in ((dq, "dq", p.live_q), (dk, "dk", p.live_k), (dv, "dv", p.live_k)):
             _held(got[live], want[name][0][live], want[name][1][live], name)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_further_apart_than_32_bits(dtype):
+    """One matrix of rows 2^26 elements apart holds everything: its last rows lie beyond 2^31 elements."""
+    import paper_2511_20564_b200 as E
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    for lens in (([45], [45]), ([1] * 45, [1] * 45)):
+        p = Problem(*lens, 4, 2, 32, dtype, LOG_NEAR, gap=0, pos="any")
+        want, rows = p.want(), 45
+        big = torch.empty(rows, 1 << 26, dtype=dtype, device="cuda")
+        place = lambda i, t: big[:, i * 256: i * 256 + t.shape[1]].copy_(t)
+        q, k, v, g = (place(i, t) for i, t in enumerate((p.q, p.k, p.v, p.g)))
+        out, dq, dk, dv, y, dx = (big[:, (4 + i) * 256: (4 + i) * 256 + t.shape[1]] for i, t in enumerate((p.q, p.q, p.k, p.k, p.q, p.q)))
+        seqs, bias = p.seqs(E), p.bias(E)
+        _, lse, _ = E.biased_attention_forward(q, k, v, seqs, bias, 4, 2, p.scale, out=out)
+        dtable = E.biased_attention_backward(g, q, k, v, out, lse, seqs, bias, 4, 2, p.scale, dQ=dq, dK=dk, dV=dv)[3]
+        for name, t in (("out", out), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv), ("dtable", dtable)):
+            _held(t, *want[name], name)
+        plan = E.Dropout(0.3, 5)
+        f, d = R.factors(rows, 128, 0.3, 5), lambda t: t.double().cpu()
+        norm = R.norm(d(out), d(q), f, None, None, 1e-5, dtype, d(g))
+        _, _, stats = E.layer_norm_forward(out, residual=q, drop=plan, Y=y)
+        dgain = E.layer_norm_backward(g, out, stats, residual=q, drop=plan, dX=dx)[2]
+        for name, t in (("y", y), ("dx", dx), ("dgain", dgain)):
+            _held(t, *norm[name], name)
+        E.dropout(q, plan, residual=g, out=y)
+        z, bz = R.total(d(q), d(g), f)
+        _held(y, z, R.HALF[dtype] * z.abs() + (1 + R.HALF[dtype]) * bz, "dropout")
+        del big, q, k, v, g, out, dq, dk, dv, y, dx
