@@ -279,10 +279,11 @@ template <int R, int U> struct TurnBias {
     int next;
     int bucket[R * U];                               // of the lane's scores
     float value[R * U];
-    __device__ inline void row(const AttnArgs &a, const Unit &x, bool on, int r, int64_t row, int head)
+    // there: there is such a row.  Its position is every lane's, those of heads that are not there too: they find buckets for the others' keys.
+    __device__ inline void row(const AttnArgs &a, const Unit &x, bool there, int r, int64_t row, int head)
     {
-        pos[r] = on ? pos_of(a.bias.pos_q, row, x.rg.q0) : 0;
-        col[r] = on ? head : 0;
+        pos[r] = there ? pos_of(a.bias.pos_q, row, x.rg.q0) : 0;
+        col[r] = there && x.on ? head : 0;
     }
     // before the first turn of a walk
     __device__ inline void begin(const AttnArgs &a, const Unit &x, const Ring &ring)
@@ -414,7 +415,7 @@ attn_few_fwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
         for (int r = 0; r < R; ++r, in.next(a)) {
             Piece<T, CPL> p;
             p.zero();
-            if constexpr (kBias) bias.row(a, x, live && x.on && r0 + r < x.rows, r, in.row, in.head(a, x));
+            if constexpr (kBias) bias.row(a, x, live && r0 + r < x.rows, r, in.row, in.head(a, x));
             if (live && x.on && r0 + r < x.rows) p.load(static_cast<const T *>(a.q) + in.row * a.ldq + in.head(a, x) * (int64_t)a.head_dim, at, f.lanes, f.chunks);
             p.widen(q[r]);
 #pragma unroll
@@ -821,7 +822,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             t.zero();
             lse[r] = INFINITY;
             d[r] = 0.f;
-            if constexpr (kBias) bias.row(a, x, live && x.on && r0 + r < x.rows, r, in.row, in.head(a, x));
+            if constexpr (kBias) bias.row(a, x, live && r0 + r < x.rows, r, in.row, in.head(a, x));
             if (live && x.on && r0 + r < x.rows) {
                 const int64_t row = in.row;
                 const int head = in.head(a, x);
