@@ -984,7 +984,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
                             for (int r = 0; r < R; ++r) {
                                 const float2 w = kept[i * f.heads * R + r];
-                                const float ds = fmaf(-lacks[r], w.x, w.y);
+                                const float ds = w.x == 0.f ? 0.f : fmaf(-lacks[r], w.x, w.y);      // (hidden keys: what D lacked may be NaN)
                                 axpy<E>(dk, ds, q[r]);
                                 axpy<E>(dv, w.x, g[r]);
                                 if (binned) {
