@@ -1041,9 +1041,9 @@ def cross_attention_backward(dOut, Q, K, V, out, lse, seqs: Sequences, n_heads: 
 
 def relative_edges(buckets: int, far: int, both=False, device="cuda"):
     """Edges (int32, ascending) of the usual buckets of distances (see e2egrec_relative_edges); RelativeBias takes one bucket more."""
-    buckets = int(buckets)
-    edges = torch.zeros(max(2 * buckets - 2 if both else buckets - 1, 0), dtype=torch.int32)
-    _check(lib().e2egrec_relative_edges(buckets, int(far), int(bool(both)), edges.data_ptr()), "e2egrec_relative_edges")
+    buckets, far = (min(max(int(n), 0), (1 << 31) - 1) for n in (buckets, far))       # refused beyond that as well
+    edges = torch.zeros(min(max(2 * buckets - 2 if both else buckets - 1, 0), 127), dtype=torch.int32)      # (at most 128 buckets)
+    _check(lib().e2egrec_relative_edges(buckets, far, int(bool(both)), edges.data_ptr()), "e2egrec_relative_edges")
     return edges.to(device)
 
 

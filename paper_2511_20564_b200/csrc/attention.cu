@@ -441,7 +441,7 @@ extern "C" int32_t e2egrec_biased_attention_backward(const e2egrec_mat *dOut, co
 extern "C" int32_t e2egrec_relative_edges(int32_t buckets, int64_t far, int32_t both, int32_t *edges)
 {
     if (buckets < 1 || far < 1 || far > (1 << 30)) return E2EGREC_ERR_ARG;
-    if ((both ? 2 * buckets - 1 : buckets) > kMaxBuckets) return E2EGREC_ERR_UNSUPPORTED;
+    if (buckets > (both ? (kMaxBuckets + 1) / 2 : kMaxBuckets)) return E2EGREC_ERR_UNSUPPORTED;
     if (!edges) return buckets == 1 ? E2EGREC_OK : E2EGREC_ERR_NULL;
     const int half = std::max(buckets / 2, 1);
     int64_t last = 0;
