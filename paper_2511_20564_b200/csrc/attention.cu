@@ -294,6 +294,7 @@ static int32_t attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, con
                                  const e2egrec_relative_bias *bias, int32_t n_heads, int32_t n_kv_heads, float scale, const e2egrec_mat *out,
                                  float *lse, int32_t *status, void *ws, size_t *ws_bytes, void *stream)
 {
+    const char *what = bias ? "biased_attention_forward" : "cross_attention_forward";
     if (!ws_bytes) return E2EGREC_ERR_NULL;
     AttnArgs a{};
     int32_t rc = check_shape(Q, K, seqs, n_heads, n_kv_heads, scale, a);
@@ -324,7 +325,7 @@ static int32_t attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, con
     if (plan.path == Path::tc) ok = tc_attention_forward(a, plan.q_tiles, plan.splits, plan.one_tile, part_o, part_ml, st);
     else if (plan.path == Path::simt) ok = simt_attention_forward(a, plan.simt, part_o, part_ml, st);
     else ok = few_attention_forward(a, plan.few, Q->dtype, part_o, part_ml, st);
-    if (!ok) return launch_refused("attention_forward");
+    if (!ok) return launch_refused(what);
     if (plan.splits > 1) {
         note_launch();
         const int warps = plan.splits > 8 ? kRowThreads / 32 : 1;
@@ -332,7 +333,7 @@ static int32_t attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, con
         if (Q->dtype == E2EGREC_F32) attn_join_kernel<float><<<grid, kRowThreads, 0, st>>>(a, plan.splits, warps, part_o, part_ml);
         else attn_join_kernel<__nv_bfloat16><<<grid, kRowThreads, 0, st>>>(a, plan.splits, warps, part_o, part_ml);
     }
-    return check_launch("attention_forward");
+    return check_launch(what);
 }
 
 static int32_t attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V,
@@ -340,6 +341,7 @@ static int32_t attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q,
                                   int32_t n_heads, int32_t n_kv_heads, float scale, const e2egrec_mat *dQ, const e2egrec_mat *dK,
                                   const e2egrec_mat *dV, float *dtable, int32_t *status, void *ws, size_t *ws_bytes, void *stream)
 {
+    const char *what = bias ? "biased_attention_backward" : "cross_attention_backward";
     if (!ws_bytes) return E2EGREC_ERR_NULL;
     AttnArgs a{};
     int32_t rc = check_shape(Q, K, seqs, n_heads, n_kv_heads, scale, a);
@@ -366,9 +368,11 @@ static int32_t attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q,
     if (dtable && (a.n_seq == 0 || a.q_rows == 0)) {
         note_launch();
         zero_table_kernel<<<(unsigned)ceil_div(table_size, 256), 256, 0, st>>>(dtable, table_size);
+        rc = check_launch(what);
+        if (rc != E2EGREC_OK) return rc;
         dtable = nullptr;
     }
-    if (a.n_seq == 0 || (a.q_rows == 0 && a.k_rows == 0)) return check_launch("attention_backward");
+    if (a.n_seq == 0 || (a.q_rows == 0 && a.k_rows == 0)) return E2EGREC_OK;
     a.q = Q->data; a.ldq = Q->ld;
     a.k = K->data; a.ldk = K->ld;
     a.v = V->data; a.ldv = V->ld;
@@ -394,8 +398,8 @@ static int32_t attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q,
         if (!plan.table_fused) ok = few_attention_table(a, plan.table, Q->dtype, dots, table_part, st);
         if (ok) launch_colsum<float>(table_part, table_size, nullptr, nullptr, plan.table_rows, table_size, 0, dtable, st);
     }
-    if (!ok) return launch_refused("attention_backward");
-    return check_launch("attention_backward");
+    if (!ok) return launch_refused(what);
+    return check_launch(what);
 }
 
 extern "C" int32_t e2egrec_cross_attention_forward(const e2egrec_mat *Q, const e2egrec_mat *K, const e2egrec_mat *V,
