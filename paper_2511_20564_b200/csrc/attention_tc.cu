@@ -1964,7 +1964,10 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
 // ------------------------------------------------------------------------------------------------- host side
 constexpr int kMaxDevices = 64;
-constexpr size_t kMostSmem = 227 * 1024 - 11 * 1024;       // dynamic, beside the 10.6 KB of a kernel with a bias
+// A block's shared memory, and how much of it may be dynamic beside what the kernels of the gradients with a bias declare (dQ 10.6 KB; dK and dV,
+// with lse and D of eight tiles of rows, 17.7 KB)
+constexpr size_t kBlockSmem = 227 * 1024, kMostSmem = kBlockSmem - 11 * 1024, kMostDkvSmem = kBlockSmem - 18 * 1024;
+constexpr int kLeastWindow = 4;                            // buckets of a window: one at least, or bin_many takes no step
 template <typename Kernel> bool allow_smem(Kernel kernel, size_t bytes, std::atomic<bool> (&done)[kMaxDevices])
 {
     int dev = 0;
@@ -2024,16 +2027,20 @@ bool launch_bwd(const AttnArgs &a, const Maps &m, int64_t q_tiles, int64_t k_til
 {
     static std::atomic<bool> done[2][kMaxDevices] = {};
     using B = Bwd<NB, kBias>;
-    const size_t table = (size_t)a.bias.buckets * a.kv_heads * a.group * sizeof(float), row = 8 * 33 * sizeof(float);
+    constexpr size_t row = 8 * 33 * sizeof(float), most_table = kTcTable * sizeof(float), most_bins = 8 * kTcBins * sizeof(float);
+    static_assert(!kBias || B::kDqSmem + most_table + most_bins + kLeastWindow * row <= kMostSmem, "the largest table and bins leave no window");
+    static_assert(!kBias || B::kDkvSmem + most_table <= kMostDkvSmem, "the largest table does not fit beside the tiles");
+    const size_t table = (size_t)a.bias.buckets * a.kv_heads * a.group * sizeof(float);
     size_t dq_smem = B::kDqSmem + table;
     int window = 0;
-    if (table_part) {                                    // the rest is the windows': four buckets at least (kTcTable, kTcBins)
+    if (table_part) {                                    // the rest is the windows'
         dq_smem += 8 * (size_t)a.bias.buckets * a.group * sizeof(float);
+        if (dq_smem + kLeastWindow * row > kMostSmem) return false;
         window = (int)std::min<size_t>(kWindow, (kMostSmem - dq_smem) / row);
         dq_smem += window * row;
     }
     if (!allow_smem(attn_tc_dq_kernel<NB, kBias>, kBias ? kMostSmem : B::kDqSmem, done[0]) ||
-        !allow_smem(attn_tc_dkv_kernel<NB, kBias>, B::kDkvSmem + (kBias ? kTcTable * sizeof(float) : 0), done[1]))
+        !allow_smem(attn_tc_dkv_kernel<NB, kBias>, B::kDkvSmem + (kBias ? most_table : 0), done[1]))
         return false;
     const int64_t units = a.n_seq * a.kv_heads;
     const TcShape fq{(uint32_t)(units * q_tiles), (int)q_tiles, 1, m.boxes, window, exact}, fk{(uint32_t)(units * k_tiles), (int)k_tiles, 1, m.boxes};
