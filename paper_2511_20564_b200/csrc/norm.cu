@@ -394,19 +394,20 @@ template <typename T, int U, bool kDrop, bool kBack> void norm_launch(const Norm
     }
 }
 
+// (the numbers of chunks that norm_shape gives, of either direction)
 template <typename T, bool kDrop, bool kBack> void norm_of(const NormArgs &a, int per, cudaStream_t st, int blocks)
 {
-    switch (per) {
-    case 1: return norm_launch<T, 1, kDrop, kBack>(a, st, blocks);
-    case 2: return norm_launch<T, 2, kDrop, kBack>(a, st, blocks);
-    case 3: return norm_launch<T, 3, kDrop, kBack>(a, st, blocks);
-    case 4: return norm_launch<T, 4, kDrop, kBack>(a, st, blocks);
+    constexpr bool kWide = sizeof(T) == 4;
+    if (per == 1) return norm_launch<T, 1, kDrop, kBack>(a, st, blocks);
+    if (per == 2) return norm_launch<T, 2, kDrop, kBack>(a, st, blocks);
+    if constexpr (kWide || !kBack)
+        if (per == 3) return norm_launch<T, 3, kDrop, kBack>(a, st, blocks);
+    if (per == 4) return norm_launch<T, 4, kDrop, kBack>(a, st, blocks);
+    if constexpr (kWide && !kBack) {
+        if (per == 5) return norm_launch<T, 5, kDrop, kBack>(a, st, blocks);
+        if (per == 6) return norm_launch<T, 6, kDrop, kBack>(a, st, blocks);
     }
-    if constexpr (sizeof(T) == 4) switch (per) {
-    case 5: return norm_launch<T, 5, kDrop, kBack>(a, st, blocks);
-    case 6: return norm_launch<T, 6, kDrop, kBack>(a, st, blocks);
-    default: return norm_launch<T, 8, kDrop, kBack>(a, st, blocks);
-    }
+    if constexpr (kWide) norm_launch<T, 8, kDrop, kBack>(a, st, blocks);
 }
 template <bool kBack> void norm_any(const NormArgs &a, int32_t dtype, int per, cudaStream_t st, int blocks = 0)
 {
