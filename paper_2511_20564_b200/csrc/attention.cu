@@ -348,7 +348,8 @@ static int32_t attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q,
     if (rc == E2EGREC_OK) rc = check_bias(bias, a);
     if (rc != E2EGREC_OK) return rc;
     const Plan plan = make_plan(a, *seqs, Q->dtype, true);
-    const size_t need = 256 + plan.part_bytes + plan.dot_bytes + plan.table_bytes;
+    // (a size query does not say whether the table's gradient is wanted)
+    const size_t need = 256 + plan.part_bytes + plan.dot_bytes + (!ws || dtable ? plan.table_bytes : 0);
     if (!ws) { *ws_bytes = need; return E2EGREC_OK; }
     if (*ws_bytes < need) { *ws_bytes = need; return E2EGREC_ERR_WORKSPACE; }
     if (reinterpret_cast<uintptr_t>(ws) % 256) return E2EGREC_ERR_ALIGN;
