@@ -953,13 +953,21 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     }
                     __syncthreads();
                 }
+                bool finite = true;
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     lacks[r] = total[r] == 0.f ? 0.f : lacks[r] / total[r];
                     d[r] += lacks[r];
+                    finite = finite && fabsf(lacks[r]) < INFINITY;
                 }
-                again = !keeps;
+                // what is kept goes by p alone: beside keys or values that hold infinities or NaN the second walk leaves hidden keys out
+                again = !keeps || !__all_sync(0xFFFFFFFFu, finite);
                 if (again && live) {
+                    if (keeps)
+#pragma unroll
+                        for (int r = 0; r < R; ++r)
+#pragma unroll
+                            for (int e = 0; e < E; ++e) dq[r][e] = 0.f;
                     bias.begin(a, x, ring);
                     ring.start();
                 } else if (live && ring.ok) {
@@ -984,7 +992,7 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
                             for (int r = 0; r < R; ++r) {
                                 const float2 w = kept[i * f.heads * R + r];
-                                const float ds = w.x == 0.f ? 0.f : fmaf(-lacks[r], w.x, w.y);      // (hidden keys: what D lacked may be NaN)
+                                const float ds = fmaf(-lacks[r], w.x, w.y);
                                 axpy<E>(dk, ds, q[r]);
                                 axpy<E>(dv, w.x, g[r]);
                                 if (binned) {
