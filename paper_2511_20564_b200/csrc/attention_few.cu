@@ -1059,10 +1059,10 @@ attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
 #pragma unroll
                     for (int u = 0; u < U; ++u) sum += s[r * U + u];
                     for (int o = wide; o < 32; o <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
-                    const float lone = lse[r] == INFINITY ? 0.f : 1.f, inv = sum == 0.f ? 0.f : __fdividef(1.f, sum);
+                    const float lone = lse[r] == INFINITY ? 0.f : 1.f, inv = sum > 0.f ? __fdividef(1.f, sum) : 0.f;      // NaN: hidden keys stay at 0
 #pragma unroll
                     for (int u = 0; u < U; ++u) {
-                        s[r * U + u] = !seen[u] ? 0.f : (s[r * U + u] == sum ? lone : s[r * U + u] * inv);
+                        s[r * U + u] = s[r * U + u] == sum ? lone : s[r * U + u] * inv;
                         t += seen[u] ? s[r * U + u] * s[(R + r) * U + u] : 0.f;
                     }
                     for (int o = wide; o < 32; o <<= 1) t += __shfl_xor_sync(0xFFFFFFFFu, t, o);
