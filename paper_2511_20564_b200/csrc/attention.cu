@@ -184,7 +184,8 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     const int n_heads = a.kv_heads * a.group;
     const bool small = rows <= (backward ? 4 : dtype == E2EGREC_F32 ? 3 : 2) || rows * k.typical <= (dtype == E2EGREC_F32 ? 256 : backward ? 700 : 800);
     // (without rows on one side there is nothing to form a product of)
-    p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows || (dtype == E2EGREC_F32 ? a.bias.buckets * a.group > kSimtTable : a.bias.buckets * n_heads > kTcTable) ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
+    const bool beside = dtype == E2EGREC_F32 ? a.bias.buckets * a.group <= kSimtTable : !a.bias.buckets || (!backward && a.bias.buckets * n_heads <= kTcTable);
+    p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows || !beside ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
     if (p.path == Path::tc) {
         p.one_tile = rows <= 128;
         p.q_tiles = blocks_per_unit(q, a.group, backward || p.one_tile ? 128 : 256, units);
@@ -208,9 +209,9 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     if (backward && a.bias.buckets) {
         p.table = few_table_plan(a, k, dtype);
         const int64_t slices = p.table.seq_slices * p.table.row_slices * p.table.key_slices;
-        p.table_fused = p.path == Path::tc ? a.bias.buckets * a.group <= kTcBins : p.path == Path::simt ? simt_forms_table(a, p.simt) : p.few.both;
+        p.table_fused = p.path == Path::simt ? simt_forms_table(a, p.simt) : p.few.both;
         p.table_rows = !p.table_fused ? slices
-                                      : p.path == Path::few ? p.few.blocks : a.n_seq * (p.path == Path::tc ? p.q_tiles : p.simt.q_tiles * p.simt.splits);
+                                      : p.path == Path::few ? p.few.blocks : a.n_seq * p.simt.q_tiles * p.simt.splits;
         p.table_bytes = align_up((size_t)p.table_rows * a.bias.buckets * a.kv_heads * a.group * sizeof(float), 256);
     }
     return p;
@@ -388,7 +389,7 @@ static int32_t attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q,
     float *dots = static_cast<float *>(ws), *part_dq = reinterpret_cast<float *>(static_cast<char *>(ws) + plan.dot_bytes);
     bool ok = true;
     if (plan.path == Path::tc) {
-        ok = tc_attention_backward(a, plan.q_tiles, plan.k_tiles, dots, plan.table_fused && dtable ? table_part : nullptr, dtable != nullptr, st);
+        ok = tc_attention_backward(a, plan.q_tiles, plan.k_tiles, dots, st);
     } else if (plan.path == Path::simt) {
         ok = simt_attention_backward(a, plan.simt, part_dq, dots, plan.table_fused && dtable ? table_part : nullptr, st);
         if (ok && plan.splits > 1 && a.q_rows) join_dq(a, plan.splits, Q->dtype, false, part_dq, nullptr, st);

@@ -150,11 +150,9 @@ inline int64_t blocks_per_unit(const Lengths &l, int64_t factor, int64_t per, in
 // part_o [splits x q_rows x heads x head_dim] and part_ml [splits x q_rows x heads] where splits > 1.
 bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, bool one_tile, float *part_o, float2 *part_ml, cudaStream_t st);
 // q_tiles, k_tiles: tiles of 128 rows and of 128 keys per sequence and key head; dots: [q_rows x heads] scratch
-// table_part: with a bias [n_seq x q_tiles, buckets x heads], or null where the table's gradient is not wanted
+// (without a bias)
+bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st);
 constexpr int kTcTable = 1280;               // entries of a table of biases, buckets x heads, that fit beside the tiles
-constexpr int kTcBins = 440;                 // bins of a warp, buckets x heads of a group
-// exact: the table's gradient is formed, here or from dots
-bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, float *table_part, bool exact, cudaStream_t st);
 
 // attention_few.cu: streaming kernels, fp32 and bf16, head_dim <= 256
 struct FewPlan {

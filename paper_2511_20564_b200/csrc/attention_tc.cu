@@ -68,13 +68,6 @@ __device__ inline void tmem_load16_async(uint32_t taddr, uint32_t (&r)[16])
         : "r"(taddr));
 }
 
-__device__ inline void tmem_load8_async(uint32_t taddr, uint32_t (&r)[8])
-{
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                 : "r"(taddr));
-}
-
 // Registers are dealt out anew once the block runs, kCopies to the threads of copies and products, kScores to those of the scores.  One
 // block per SM: 384 threads x 168 at launch = 128 x 72 + 256 x 216 (forward) = 128 x 104 + 256 x 200 (backward, whose copies hold statistics
 // of rows a tile ahead; spilled, they were waited for).  Two blocks per SM: 256 threads x 128 = 128 x 72 + 128 x 184.
@@ -87,8 +80,6 @@ struct TcShape {
     uint32_t units;
     int tiles, splits;                               // blocks of rows (or keys) per sequence and key head; stretches of the keys
     int boxes;                                       // rows of the group's heads come as boxes (the group divides 128)
-    int window;                                      // with a bias: buckets of a warp's window (dQ)
-    int exact;                                       // with a bias: D goes into the table's gradient
 };
 struct Work {
     SeqRange rg;
@@ -231,19 +222,19 @@ struct Visible {
 };
 
 // ---- Bias by distance.  Buckets are monotone in the distance, so the lowest and the highest position of neighbouring columns give the buckets
-// that a thread's row (or key) meets in them; positions need not be sorted for that, but where they are the next columns' bucket is the last
+// that a thread's row meets in them; positions need not be sorted for that, but where they are the next columns' bucket is the last
 // one's or its neighbour.  One bucket for a whole tile: its bias goes into the exponent's argument and costs nothing per score.  Two in 32
 // columns: the edge between them is a threshold that the columns' positions are compared with.  More (close to the diagonal): every score looks
 // its bucket up, in a table of the distances up to kNear, or by bisection, and gets its bias in tensor memory beforehand.  The buckets are found while the
 // tile's products are on their way: positions are there a tile ahead.
 // What decides is latency and the code's size.  Forward pass of 8 x 2048 x 2048, heads of 128 (125 us without a bias): 690 us with all ways in the
 // registers that hold a row of 128 scores (stalls for instructions), 270 with biases in tensor memory, 32 columns after 32, 243 with thresholds of
-// positions.  One bucket for all pairs: 168 us.  Backward pass 1467 us (420 without a bias; 812 with one bucket; 832 without the table's gradient).
+// positions.  One bucket for all pairs: 168 us.
 constexpr int kNear = 2048;
 struct BiasShared {
-    int32_t pos[kWordRing][kTile];                   // of the tile's columns: keys (forward pass, dQ), rows of Q (dK, dV)
+    int32_t pos[kWordRing][kTile];                   // of the tile's keys
     int2 range[kWordRing][4];                        // lowest and highest of each 32 columns that count; lowest > highest: none
-    int4 halves[kWordRing];                          // the same of each 64
+    int2 all[kWordRing];                             // the same of the tile
     int32_t edges[kMaxBuckets];                      // beyond the last: the highest number
     uint8_t near[2 * kNear];                         // buckets of the distances -kNear .. kNear - 1
 };
@@ -269,7 +260,7 @@ __device__ inline void place(BiasShared &s, uint32_t slot, const int (&pos)[4], 
         s.pos[slot][b * 32 + lane] = pos[b];
         if (lane == 0) s.range[slot][b] = r[b];
     }
-    if (lane == 0) s.halves[slot] = make_int4(min(r[0].x, r[1].x), max(r[0].y, r[1].y), min(r[2].x, r[3].x), max(r[2].y, r[3].y));
+    if (lane == 0) s.all[slot] = make_int2(min(min(r[0].x, r[1].x), min(r[2].x, r[3].x)), max(max(r[0].y, r[1].y), max(r[2].y, r[3].y)));
     __syncwarp();
 }
 // The positions of keys, by the copying warp: those of tile j + 1 are written before the copies of tile j are announced, so whoever has seen a tile's
@@ -308,9 +299,6 @@ struct Ahead {
     }
 };
 
-// kKey: the thread's own position is the key's, the columns' are the queries'
-template <bool kKey> __device__ inline int distance(int own, int column) { return kKey ? apart(own, column) : apart(column, own); }
-
 // The buckets of near distances, by the 32 W threads of W warps that have nothing else to do while the first tiles are on their way; the edges
 // are there.  A barrier of their own.
 template <int W> __device__ inline void stage_near(const BiasArgs &b, BiasShared &sh)
@@ -334,61 +322,54 @@ __device__ inline int add_sat(int x, int y)
     asm("add.sat.s32 %0, %1, %2;" : "=r"(s) : "r"(x), "r"(y));
     return s;
 }
-// The bucket that a thread is in, by the columns' positions: from `in` to `out`, in the order of growing distances (kKey: of falling positions).
-// Comparisons of positions take no difference that could leave 32 bits.
-template <bool kKey> struct Place {
+// The bucket that a thread's row is in, by the columns' positions: those from `in` to `out`.  Comparisons of positions take no difference that could
+// leave 32 bits.
+struct Place {
     int at, in, out;
-    static constexpr int kFirst = kKey ? INT32_MAX : INT32_MIN, kLast = kKey ? INT32_MIN : INT32_MAX;
-    __device__ inline void unknown() { at = 0, in = kLast, out = kFirst; }
-    __device__ inline bool beyond(int p) const { return kKey ? p < out : p > out; }
-    __device__ inline bool before(int p) const { return kKey ? p > in : p < in; }
-    __device__ inline int end(const BiasArgs &b, const int32_t *edges, int own) const
-    {
-        return at < b.buckets - 1 ? (kKey ? apart(own, edges[at] - 1) : add_sat(own, edges[at] - 1)) : kLast;
-    }
+    __device__ inline void unknown() { at = 0, in = INT32_MAX, out = INT32_MIN; }
+    __device__ inline bool beyond(int p) const { return p > out; }
+    __device__ inline int end(const BiasArgs &b, const int32_t *edges, int own) const { return at < b.buckets - 1 ? add_sat(own, edges[at] - 1) : INT32_MAX; }
     __device__ inline void up(const BiasArgs &b, const int32_t *edges, int own)
     {
         ++at;
-        in = kKey ? out - 1 : out + 1;
+        in = out + 1;
         out = end(b, edges, own);
     }
     __device__ inline void seek(const BiasArgs &b, const int32_t *edges, int own, int p)
     {
-        const int d[1] = {distance<kKey>(own, p)};
+        const int d[1] = {apart(p, own)};
         int found[1];
         look_up<1>(b, edges, d, found);
         at = found[0];
-        in = at ? (kKey ? apart(own, edges[at - 1]) : add_sat(own, edges[at - 1])) : kFirst;
+        in = at ? add_sat(own, edges[at - 1]) : INT32_MIN;
         out = end(b, edges, own);
     }
     __device__ inline void to(const BiasArgs &b, const int32_t *edges, int own, int p)
     {
-        if (beyond(p) && (kKey ? in >= out : in <= out)) up(b, edges, own);
-        if (beyond(p) || before(p)) seek(b, edges, own, p);
+        if (beyond(p) && in <= out) up(b, edges, own);
+        if (beyond(p) || p < in) seek(b, edges, own, p);
     }
 };
 
-// The buckets of 32 N columns of a thread's row (kKey: key), from column 32 c0 of a tile on: in 32 columns at .. last.  Two of them: a column's
-// position p is in the second where it is beyond limit.
-template <bool kKey, int N> struct TileSpans {
-    int at[N], last[N], limit[N];                        // with `one` at[0] alone
+// The buckets of a tile's columns of a thread's row: in 32 columns at .. last.  Two of them: a column's position p is in the second where it is
+// beyond limit.
+struct TileSpans {
+    int at[4], last[4], limit[4];                        // with `one` at[0] alone
     uint32_t two, many, away;                            // a bit per 32 columns: some lane meets two buckets or more in them; more; is further than
                                                          // kNear from a column of them
     bool one;                                            // every lane meets one bucket in the tile
-    __device__ static inline bool beyond(int limit, int p) { return kKey ? p < limit : p > limit; }
-    // alive: the warp has a row (key) that counts
-    __device__ inline void find(const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c0, int own, bool alive, Place<kKey> &place)
+    // alive: the warp has a row that counts
+    __device__ inline void find(const BiasArgs &b, const BiasShared &sh, uint32_t slot, int own, bool alive, Place &place)
     {
         at[0] = 0;
         one = true;
         if (!alive) return;
-        const int4 h = sh.halves[slot];
-        const int2 r = N == 4 ? make_int2(min(h.x, h.z), max(h.y, h.w)) : (c0 ? make_int2(h.z, h.w) : make_int2(h.x, h.y));
-        Place<kKey> next = place;
+        const int2 r = sh.all[slot];
+        Place next = place;
         bool mine = true;
         if (r.x <= r.y) {
-            next.to(b, sh.edges, own, kKey ? r.y : r.x);
-            mine = !next.beyond(kKey ? r.x : r.y);
+            next.to(b, sh.edges, own, r.x);
+            mine = !next.beyond(r.y);
         }
         at[0] = next.at;
         one = __all_sync(0xFFFFFFFFu, mine);
@@ -398,22 +379,22 @@ template <bool kKey, int N> struct TileSpans {
         }
         two = many = away = 0;
 #pragma unroll 1
-        for (int c = 0; c < N; ++c) {
-            const int2 range = sh.range[slot][c0 + c];
-            int stop = Place<kKey>::kLast;
+        for (int c = 0; c < 4; ++c) {
+            const int2 range = sh.range[slot][c];
+            int stop = INT32_MAX;
             bool more = false;
-            if (range.x <= range.y) place.to(b, sh.edges, own, kKey ? range.y : range.x);
-            const int from = place.at, far = kKey ? range.x : range.y;
-            if (range.x <= range.y && place.beyond(far)) {
+            if (range.x <= range.y) place.to(b, sh.edges, own, range.x);
+            const int from = place.at;
+            if (range.x <= range.y && place.beyond(range.y)) {
                 stop = place.out;
                 place.up(b, sh.edges, own);
-                if (place.beyond(far)) {
+                if (place.beyond(range.y)) {
                     more = true;
-                    place.seek(b, sh.edges, own, far);
+                    place.seek(b, sh.edges, own, range.y);
                 }
             }
 #pragma unroll
-            for (int k = 0; k < N; ++k)
+            for (int k = 0; k < 4; ++k)
                 if (c == k) {
                     at[k] = from;
                     last[k] = place.at;
@@ -423,32 +404,25 @@ template <bool kKey, int N> struct TileSpans {
                 two |= 1u << c;
                 if (__any_sync(0xFFFFFFFFu, more)) {
                     many |= 1u << c;
-                    const int d0 = distance<kKey>(own, range.x), d1 = distance<kKey>(own, range.y);
+                    const int d0 = apart(range.x, own), d1 = apart(range.y, own);
                     if (__any_sync(0xFFFFFFFFu, min(d0, d1) < -kNear || max(d0, d1) >= kNear)) away |= 1u << c;
                 }
             }
         }
     }
-    __device__ inline void of(int c, int &from, int &to, int &stop) const
+    // 32 products, of column 32 c and on -> scores in powers of two with their biases, where no lane meets more than two buckets.  table: of the
+    // row's head
+    __device__ inline void add_to(uint32_t (&v)[32], int c, float c1, const BiasShared &sh, uint32_t slot, const float *table) const
     {
-        from = at[0];
-        to = last[0];
-        stop = limit[0];
+        const float2 scale2 = make_float2(c1, c1);
+        int from = at[0], to = last[0], stop = limit[0];
 #pragma unroll
-        for (int k = 1; k < N; ++k)
+        for (int k = 1; k < 4; ++k)
             if (c == k) {
                 from = at[k];
                 to = last[k];
                 stop = limit[k];
             }
-    }
-    // 32 products, of column 32 c and on -> scores in powers of two with their biases, where no lane meets more than two buckets.  table: of the
-    // row's head
-    __device__ inline void add_to(uint32_t (&v)[32], int c, float c1, const BiasShared &sh, uint32_t slot, int c0, const float *table) const
-    {
-        const float2 scale2 = make_float2(c1, c1);
-        int from, to, stop;
-        of(c, from, to, stop);
         const float t0 = table[from];
         auto put = [&](int i, float x0, float x1) {
             const float2 x = __ffma2_rn(pair_of(v[i], v[i + 1]), scale2, make_float2(x0, x1));
@@ -461,41 +435,35 @@ template <bool kKey, int N> struct TileSpans {
             return;
         }
         const float t1 = table[to];
-        const int4 *pos = reinterpret_cast<const int4 *>(sh.pos[slot] + (c0 + c) * 32);
+        const int4 *pos = reinterpret_cast<const int4 *>(sh.pos[slot] + c * 32);
 #pragma unroll
         for (int i = 0; i < 32; i += 4) {
             const int4 p = pos[i / 4];
-            put(i, beyond(stop, p.x) ? t1 : t0, beyond(stop, p.y) ? t1 : t0);
-            put(i + 2, beyond(stop, p.z) ? t1 : t0, beyond(stop, p.w) ? t1 : t0);
+            put(i, p.x > stop ? t1 : t0, p.y > stop ? t1 : t0);
+            put(i + 2, p.z > stop ? t1 : t0, p.w > stop ? t1 : t0);
         }
     }
-    // The same in tensor memory for columns where some lane meets more buckets, or every column has its own head (kKey; g: the first one's, table
-    // the key head's first): each column looks its bucket up, 16 at a time
-    __device__ inline bool one_by_one(int c, int group) const { return (kKey && group > 1) || (!one && many >> c & 1u); }
-    __device__ inline void look_columns(uint32_t taddr, int c, float c1, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c0, int own,
-                                        const float *table, int group, int g) const
+    // The same in tensor memory for columns where some lane meets more buckets: each column looks its bucket up, 16 at a time
+    __device__ inline bool one_by_one(int c) const { return !one && many >> c & 1u; }
+    __device__ inline void look_columns(uint32_t taddr, int c, float c1, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int own, const float *table) const
     {
 #pragma unroll 1
         for (int i = 0; i < 32; i += 16) {
-            const int4 *pos = reinterpret_cast<const int4 *>(sh.pos[slot] + (c0 + c) * 32 + i);
+            const int4 *pos = reinterpret_cast<const int4 *>(sh.pos[slot] + c * 32 + i);
             int at16[16];
-            if (one) {
-#pragma unroll
-                for (int k = 0; k < 16; ++k) at16[k] = at[0];
-            } else if ((many & ~away) >> c & 1u) {       // (columns that do not count may lie anywhere)
+            if (!(away >> c & 1u)) {                     // (columns that do not count may lie anywhere)
 #pragma unroll
                 for (int k = 0; k < 16; k += 4) {
                     const int4 p4 = pos[k / 4];
                     const int p[4] = {p4.x, p4.y, p4.z, p4.w};
 #pragma unroll
-                    for (int m = 0; m < 4; ++m) at16[k + m] = sh.near[near_of(kKey ? p[m] : own, kKey ? own : p[m])];
+                    for (int m = 0; m < 4; ++m) at16[k + m] = sh.near[near_of(own, p[m])];
                 }
             } else {
 #pragma unroll
                 for (int k = 0; k < 16; k += 8) {
                     const int4 p = pos[k / 4], o = pos[k / 4 + 1];
-                    const int d[8] = {distance<kKey>(own, p.x), distance<kKey>(own, p.y), distance<kKey>(own, p.z), distance<kKey>(own, p.w),
-                                      distance<kKey>(own, o.x), distance<kKey>(own, o.y), distance<kKey>(own, o.z), distance<kKey>(own, o.w)};
+                    const int d[8] = {apart(p.x, own), apart(p.y, own), apart(p.z, own), apart(p.w, own), apart(o.x, own), apart(o.y, own), apart(o.z, own), apart(o.w, own)};
                     int at8[8];
                     look_up<8>(b, sh.edges, d, at8);
 #pragma unroll
@@ -507,194 +475,15 @@ template <bool kKey, int N> struct TileSpans {
             tmem_load16_async(taddr + i, v);
             tmem_load_wait();
 #pragma unroll
-            for (int k = 0; k < 16; ++k) {
-                v[k] = __float_as_uint(fmaf(__uint_as_float(v[k]), c1, table[(kKey ? g * b.buckets : 0) + at16[k]]));
-                if (kKey) g = g + 1 == group ? 0 : g + 1;
-            }
+            for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(fmaf(__uint_as_float(v[k]), c1, table[at16[k]]));
             __syncwarp();
             tmem_store16(taddr + i, v);
         }
+        __syncwarp();
         tmem_store_wait();
         __syncwarp();
     }
 };
-
-// Sums of dS by bucket and head of the group, of one warp: bins [buckets x group].  Rows of a warp follow one another, so lane i has head
-// (g0 + i) mod group; lanes of one head are added up in a fixed order.
-__device__ inline void add_to_bin(float *bins, int bucket, int group, int g0, float s, int lane)
-{
-    __syncwarp();
-    if (group >= 32) {                                   // no two lanes of one head
-        const int g = g0 + lane;
-        bins[bucket * group + (g >= group ? g - group : g)] += s;
-    } else if ((group & (group - 1)) == 0) {
-        for (int o = 16; o >= group; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
-        if (lane < group) bins[bucket * group + lane] += s;      // g0 = 0: rows of a warp begin at a multiple of 32
-    } else {
-        float sum = s;
-        for (int o = group; o < 32; o += group) {
-            const float other = __shfl_down_sync(0xFFFFFFFFu, s, o);
-            if (lane + o < 32) sum += other;
-        }
-        const int g = g0 + lane;
-        if (lane < group) bins[bucket * group + (g >= group ? g - group : g)] += sum;
-    }
-}
-// The same for the buckets first .. first + 3 at once, of those up to `last`.  One head: lanes give away half of what they hold at each of two
-// steps, so six exchanges do for four sums.
-__device__ inline void add_to_bins(float *bins, int first, int last, int group, int g0, const float (&s)[4], int lane)
-{
-    if (group != 1) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (first + k <= last) add_to_bin(bins, first + k, group, g0, s[k], lane);
-        return;
-    }
-    const bool high = lane & 2, odd = lane & 1;
-    float a = high ? s[2] : s[0], b = high ? s[3] : s[1];
-    a += __shfl_xor_sync(0xFFFFFFFFu, high ? s[0] : s[2], 2);
-    b += __shfl_xor_sync(0xFFFFFFFFu, high ? s[1] : s[3], 2);
-    float c = odd ? b : a;
-    c += __shfl_xor_sync(0xFFFFFFFFu, odd ? a : b, 1);
-#pragma unroll
-    for (int o = 16; o >= 4; o >>= 1) c += __shfl_xor_sync(0xFFFFFFFFu, c, o);
-    __syncwarp();
-    if (lane < 4 && first + lane <= last) bins[first + lane] += c;
-}
-// The dS of a thread's row in 32 columns that lie in many buckets, first .. last among the warp's rows: lanes add up theirs in a window of shared
-// memory, `wide` buckets x 32 lanes (33 apart: no two lanes in a bank), then a lane per bucket those of all lanes, in order.  (Each bucket's
-// columns picked out anew, four buckets at a time, took 3200 instructions for 26 buckets, 450 so.)  dS comes from tensor memory, eight columns
-// after eight: unrolled over 32 in registers, with more code for the warps to fetch, the backward pass of 8 x 2048 x 2048 took 1621 us, 1514 so.
-constexpr int kWindow = 32;                              // most buckets of a window; the shared memory that is left says how many there are
-__device__ inline void bin_many(float *bins, float *window, int wide, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int c, uint32_t taddr, int own,
-                                bool away, int first, int last, bool live, int group, int g0, int lane)
-{
-    const int32_t *pos = sh.pos[slot] + c * 32;
-    for (int base = first; base <= last; base += wide) {
-        __syncwarp();
-        for (int i = lane; i < wide * 33; i += 32) window[i] = 0.f;
-        __syncwarp();
-#pragma unroll 1
-        for (int i = 0; i < 32; i += 8) {
-            const int4 p4 = *reinterpret_cast<const int4 *>(pos + i), o4 = *reinterpret_cast<const int4 *>(pos + i + 4);
-            const int p[8] = {p4.x, p4.y, p4.z, p4.w, o4.x, o4.y, o4.z, o4.w};
-            int at[8];
-            uint32_t x[8];
-            __syncwarp();                                // tensor memory is for a converged warp
-            tmem_load8_async(taddr + i, x);
-            if (!away) {                                 // (columns that do not count may lie anywhere; their dS is 0)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) at[k] = sh.near[near_of(own, p[k])];
-            } else {
-                int d[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k) d[k] = apart(p[k], own);
-                look_up<8>(b, sh.edges, d, at);
-            }
-            __syncwarp();
-            tmem_load_wait();
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (live && (uint32_t)(at[k] - base) < (uint32_t)wide) window[(at[k] - base) * 33 + lane] += __uint_as_float(x[k]);
-        }
-        __syncwarp();
-        if (lane < wide && base + lane <= last) {
-            const float *mine = window + lane * 33;
-            float *bin = bins + (base + lane) * group;
-            if (group == 1) {
-                float s = 0.f;
-#pragma unroll 8
-                for (int k = 0; k < 32; ++k) s += mine[k];
-                bin[0] += s;
-            } else {
-                int g = g0;
-                for (int k = 0; k < 32; ++k) {
-                    bin[g] += mine[k];
-                    g = g + 1 == group ? 0 : g + 1;
-                }
-            }
-        }
-    }
-    __syncwarp();
-}
-
-// The dS of a thread's row in the 64 columns of half q of a tile.  run, cur: sum of the bucket that the warp is in, kept in registers until it
-// leaves it.  Every bucket is summed up by itself (as differences of sums of what lies beyond its edges, a bucket of few pairs had the
-// rounding of all).  taddr: where dP was; a tile in more than one bucket puts dS there, to be read again in loops.
-__device__ inline void bin_columns(float *bins, float *window, int wide, const BiasArgs &b, const BiasShared &sh, uint32_t slot, int q, uint32_t taddr, const float (&ds)[64],
-                                   int own, const TileSpans<false, 2> &spans, bool live, int group, int g0, float &run, int &cur, int lane)
-{
-    if (!__any_sync(0xFFFFFFFFu, live)) return;
-    float all = 0.f;
-    if (spans.one) {
-        float2 s2[2] = {};
-#pragma unroll
-        for (int i = 0; i < 64; i += 2) s2[i / 2 & 1] = __fadd2_rn(s2[i / 2 & 1], make_float2(ds[i], ds[i + 1]));
-        all = (s2[0].x + s2[0].y) + (s2[1].x + s2[1].y);
-    } else {
-        __syncwarp();
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-            uint32_t v[32];
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(ds[c * 32 + i]);
-            tmem_store32(taddr + c * 32, v);
-        }
-        tmem_store_wait();
-    }
-#pragma unroll 1
-    for (int c = 0; c < 2; ++c) {
-        int from = spans.at[0], to = from, stop = INT32_MAX;
-        if (!spans.one) spans.of(c, from, to, stop);
-        const int first = __reduce_min_sync(0xFFFFFFFFu, from), last = __reduce_max_sync(0xFFFFFFFFu, to);
-        if (first != cur || first != last) {
-            if (cur >= 0) add_to_bin(bins, cur, group, g0, run, lane);
-            run = 0.f;
-            cur = first == last ? first : -1;
-        }
-        if (!spans.one && (spans.many >> c & 1u)) {
-            bin_many(bins, window, wide, b, sh, slot, q * 2 + c, taddr + c * 32, own, spans.away >> c & 1u, first, last, live, group, g0, lane);
-            continue;
-        }
-        float below = all, above = 0.f;
-        if (!spans.one) {
-            const int32_t *pos = sh.pos[slot] + q * 64 + c * 32;
-            float2 s2 = make_float2(0.f, 0.f), t2 = make_float2(0.f, 0.f);
-#pragma unroll 1
-            for (int i = 0; i < 32; i += 8) {
-                const int4 p = *reinterpret_cast<const int4 *>(pos + i), o = *reinterpret_cast<const int4 *>(pos + i + 4);
-                const int at[8] = {p.x, p.y, p.z, p.w, o.x, o.y, o.z, o.w};
-                uint32_t v[8];
-                __syncwarp();                                // tensor memory is for a converged warp
-                tmem_load8_async(taddr + c * 32 + i, v);
-                tmem_load_wait();
-#pragma unroll
-                for (int k = 0; k < 8; k += 2) {
-                    const bool b0 = at[k] > stop, b1 = at[k + 1] > stop;
-                    const float2 x = pair_of(v[k], v[k + 1]);
-                    s2 = __fadd2_rn(s2, make_float2(b0 ? 0.f : x.x, b1 ? 0.f : x.y));
-                    t2 = __fadd2_rn(t2, make_float2(b0 ? x.x : 0.f, b1 ? x.y : 0.f));
-                }
-            }
-            below = s2.x + s2.y;
-            above = t2.x + t2.y;
-        }
-        below = live ? below : 0.f;
-        above = live ? above : 0.f;
-        if (first == last) {
-            run += below;
-        } else {
-#pragma unroll 1
-            for (int e = first; e <= last; e += 4) {
-                float s[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) s[k] = (e + k == from ? below : 0.f) + (e + k == to && to != from ? above : 0.f);
-                add_to_bins(bins, e, last, group, g0, s, lane);
-            }
-        }
-        if (spans.one) break;
-    }
-}
 
 // the lane that issues the products: a tile has landed, whoever wrote it
 __device__ inline bool tile_ready(uint64_t *bar, uint32_t parity, volatile int *abort_flag)
@@ -961,7 +750,7 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 float m = -INFINITY, l = 0.f;
                 int pos_q = 0;
                 const float *table = table_s;
-                Place<false> bucket;
+                Place bucket;
                 bucket.unknown();
                 if constexpr (kBias) {
                     int64_t row;
@@ -972,12 +761,12 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     pos_q = pos_of(a.bias.pos_q, row, x.rg.q0);
                 }
                 const bool alive = r - lane < x.rows;
-                TileSpans<false, 4> spans;
+                TileSpans spans;
                 for (int j = 0; j < x.n; ++j, ++jj) {
                     if constexpr (kBias) {                   // positions are a tile ahead of the products, the first tile's are not
                         if (j == 0) ok = warp_wait(&s_full[q], sc & 1u, &abort_flag);
                         if (!ok) break;
-                        spans.find(a.bias, bias_s, jj % kWordRing, 0, pos_q, alive, bucket);
+                        spans.find(a.bias, bias_s, jj % kWordRing, pos_q, alive, bucket);
                         __syncwarp();
                     }
                     if (!kBias || j > 0) ok = warp_wait(&s_full[q], sc & 1u, &abort_flag);
@@ -997,12 +786,12 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         float highest = -INFINITY;
 #pragma unroll 1
                         for (int c = 0; c < 4; ++c) {
-                            const bool looked = spans.one_by_one(c, 1);
-                            if (looked) spans.look_columns(s_addr + c * 32, c, c1, a.bias, bias_s, jj % kWordRing, 0, pos_q, table, 1, 0);
+                            const bool looked = spans.one_by_one(c);
+                            if (looked) spans.look_columns(s_addr + c * 32, c, c1, a.bias, bias_s, jj % kWordRing, pos_q, table);
                             __syncwarp();                    // tensor memory is for a converged warp
                             tmem_load32_async(s_addr + c * 32, v[0]);
                             tmem_load_wait();
-                            if (!spans.one && !looked) spans.add_to(v[0], c, c1, bias_s, jj % kWordRing, 0, table);
+                            if (!spans.one && !looked) spans.add_to(v[0], c, c1, bias_s, jj % kWordRing, table);
                             const uint32_t seen = words[jj % kWordRing][c];
                             if (seen != 0xFFFFFFFFu) {
 #pragma unroll
@@ -1147,9 +936,9 @@ attn_tc_fwd_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 // ------------------------------------------------------------------------------------------------- backward
 // Two kernels, so that no gradient is added up by atomics: dQ goes over the keys of a tile of rows, dK and dV over the rows of a
 // tile of keys; the scores are formed in both.  Two warpgroups share a tile of 128 x 128: 64 columns each, one row per thread.
-template <int NB, bool kBias> struct Bwd {
+template <int NB> struct Bwd {
     static constexpr int kThreads = 12 * 32, kTileBytes = NB * kBlockBytes;      // copies, zeros, products; one idle
-    using KvRing = TileRing<NB == 2 ? 5 - kBias : 8 - 2 * kBias>;      // (four slots at least: the next tile's values are waited for before its keys go)
+    using KvRing = TileRing<NB == 2 ? 5 : 8>;
     static constexpr int kQgStages = NB == 2 ? 4 : 8;
     static constexpr size_t kDqSmem = 1024 + (size_t)(2 + KvRing::kSlots) * kTileBytes, kDkvSmem = 1024 + (size_t)(2 + kQgStages) * kTileBytes;
 };
@@ -1203,10 +992,7 @@ __device__ inline void store_row(uint32_t taddr, bf16 *out, int head_dim, float 
 }
 
 // Passes over the keys
-template <bool kBias> __device__ inline int passes_of(const Work &x, const TcShape &f, int head_dim)
-{
-    return kBias && f.exact ? min(x.n, 2) : ((int64_t)x.n * kTile > 32 * head_dim ? 2 : 1);
-}
+__device__ inline int passes_of(const Work &x, int head_dim) { return (int64_t)x.n * kTile > 32 * head_dim ? 2 : 1; }
 
 // dQ, and D = dO . out of every row for the other kernel.  What the stored out's D lacks is the sum of p (dP - D) over the keys; it meets
 // sum p k in dQ, which does not get smaller with the number of keys, as dQ does.  Where one tile holds all keys it is added to D before dS is
@@ -1216,19 +1002,15 @@ template <bool kBias> __device__ inline int passes_of(const Work &x, const TcSha
 // for values whose mean is a quarter of their spread.
 // dS goes into its product as two bf16 operands, its rounding and the rest: with dS rounded once dQ was 2.5 to 2.7e-3 off in the mean (a
 // rounding of the result: 1.8e-3), at most 2.4e-3 so; the training case's backward pass takes 550 us with one operand, 585 us so.
-// Where the gradient of a table of biases is wanted all sequences of more than one tile take the second pass: sums of dS that are left from what
-// cancels need D as it is.  Each warp adds up its rows' dS by bucket in bins of its own; a unit's bins, in the order of the warps, are a row of part
-// [sequences x tiles, buckets x heads], which the caller adds up.
-template <int NB, bool kBias>
-__global__ void __launch_bounds__(Bwd<NB, kBias>::kThreads, 1)
+template <int NB>
+__global__ void __launch_bounds__(Bwd<NB>::kThreads, 1)
 attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_k,
-                  const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f, float *__restrict__ dots,
-                  float *__restrict__ table_part)
+                  const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f, float *__restrict__ dots)
 {
-    using R = typename Bwd<NB, kBias>::KvRing;
-    constexpr int kTileBytes = Bwd<NB, kBias>::kTileBytes;
+    using R = typename Bwd<NB>::KvRing;
+    constexpr int kTileBytes = Bwd<NB>::kTileBytes;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t kv_full[R::kBarriers], kv_empty[R::kSlots], k_clean[kWordRing], q_full, q_empty, s_full[2], dp_full, ds_full, o_full, o_empty, rest_full, bins_full;
+    __shared__ uint64_t kv_full[R::kBarriers], kv_empty[R::kSlots], k_clean[kWordRing], q_full, q_empty, s_full[2], dp_full, ds_full, o_full, o_empty, rest_full;
     __shared__ float rests[2][kTile];                 // sums of p (dP - D) over each warpgroup's columns
     __shared__ __align__(16) uint32_t words[kWordRing][4];
     __shared__ uint32_t tmem_slot;
@@ -1238,13 +1020,6 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
     uint8_t *tiles_smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t q_smem = smem_u32(tiles_smem), g_smem = q_smem + kTileBytes, kv_smem = q_smem + 2 * kTileBytes;
     const int ksteps = (a.head_dim + 15) / 16;
-    __shared__ __align__(16) BiasShared_<kBias> bias_s;
-    float *table_s = reinterpret_cast<float *>(tiles_smem + (2 + R::kSlots) * kTileBytes), *bins_s = table_s + a.bias.buckets * a.kv_heads * a.group;
-    if constexpr (kBias) {
-        stage_bias(a, bias_s, table_s);
-        if (table_part)
-            for (int i = threadIdx.x; i < 8 * a.bias.buckets * a.group; i += blockDim.x) bins_s[8 * f.window * 33 + i] = 0.f;
-    }
     if (threadIdx.x == 0) {
         for (int s = 0; s < R::kBarriers; ++s) mbar_init(&kv_full[s], 1);
         for (int s = 0; s < R::kSlots; ++s) mbar_init(&kv_empty[s], 1);
@@ -1258,7 +1033,6 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         mbar_init(&o_full, 1);
         mbar_init(&o_empty, 8);
         mbar_init(&rest_full, 8);
-        mbar_init(&bins_full, 8);
         abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -1280,12 +1054,10 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             bool ok = true;
             for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
                 const Work x = work_of(a, f, u, lane == 0);
-                const int steps = x.n * passes_of<kBias>(x, f, a.head_dim);
+                const int steps = x.n * passes_of(x, a.head_dim);
                 for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                     Visible seen;
-                    Ahead places;
                     seen.ahead(a, x, 0, lane);
-                    if constexpr (kBias) places.begin(a, x, bias_s, steps, jj, lane);
                     if (item > 0) ok = warp_wait(&q_empty, (item - 1) & 1u, &abort_flag);
                     if (!ok) break;
                     if (f.boxes) {
@@ -1316,8 +1088,6 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                             const uint32_t s = R::slot(g);
                             if (g >= R::kSlots) ok = warp_wait(&kv_empty[s], (R::use(g) - 1) & 1u, &abort_flag);
                             if (!ok) break;
-                            if constexpr (kBias)
-                                if (v == 0) places.step(a, x, bias_s, j, j + 2 < steps ? (next + 1 < x.n ? next + 1 : 0) : -1, steps, jj, lane);
                             if (lane == 0) {
                                 if (v == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
                                 mbar_expect_tx(&kv_full[R::full(v, jj)], kTileBytes);
@@ -1339,7 +1109,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
             bool ok = true;
             for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
                 const Work x = work_of(a, f, u, false);
-                const int steps = x.n * passes_of<kBias>(x, f, a.head_dim);
+                const int steps = x.n * passes_of(x, a.head_dim);
                 for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles)
                     for (int j = 0; j < steps && ok; ++j, ++jj, g += 2) {
                         ok = warp_wait(&kv_full[R::full(0, jj)], R::parity(jj), &abort_flag);
@@ -1368,7 +1138,7 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 };
                 for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
                     const Work x = work_of(a, f, u, false);
-                    const int steps = x.n * passes_of<kBias>(x, f, a.head_dim), first = steps - x.n;      // of the last pass
+                    const int steps = x.n * passes_of(x, a.head_dim), first = steps - x.n;      // of the last pass
                     for (int64_t t = x.t0; t * kTile < x.rows && x.n > 0 && ok; t += f.tiles, ++item) {
                         ok = tile_ready(&q_full, item & 1u, &abort_flag);
                         if (item > 0 && ok) ok = mbar_wait(&o_empty, (item - 1) & 1u, &abort_flag);
@@ -1410,18 +1180,16 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
         }
     } else {
         more_registers<200>();
-        if constexpr (kBias) stage_near<8>(a.bias, bias_s);
         // ---- p and dS: 64 columns of one row per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
         const float c1 = a.scale * kLog2e;
         const int heads = a.kv_heads * a.group;
-        uint32_t jj = 0, item = 0, corrected = 0, binned = 0;
+        uint32_t jj = 0, item = 0, corrected = 0;
         bool ok = true;
-        float *window = bins_s + warp * f.window * 33, *bins = bins_s + 8 * f.window * 33 + warp * a.bias.buckets * a.group;
         for (uint32_t u = blockIdx.x; u < f.units && ok; u += gridDim.x) {
             const Work x = work_of(a, f, u, false);
-            const int steps = x.n * passes_of<kBias>(x, f, a.head_dim), first = steps - x.n;
+            const int steps = x.n * passes_of(x, a.head_dim), first = steps - x.n;
             for (int64_t t = x.t0; t * kTile < x.rows && ok; t += f.tiles) {
                 const int64_t r = t * kTile + w * 32 + lane;
                 int64_t row;
@@ -1444,58 +1212,20 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     }
                     if (l == -INFINITY) dot = 0.f;
                 }
-                float rest = 0.f, run = 0.f;
-                int pos_q = 0, cur = -1;
-                Place<false> bucket;
-                bucket.unknown();
-                const int g0 = kBias ? (int)((t * kTile + w * 32) % a.group) : 0;
-                const float *table = table_s;
-                if constexpr (kBias) {
-                    int64_t near;
-                    int any;
-                    row_of(a, x, min(r, x.rows - 1), near, any);      // rows that there are not are where the last one is
-                    pos_q = pos_of(a.bias.pos_q, near, x.rg.q0);
-                    table += head * a.bias.buckets;
-                }
-                const bool alive = r - lane < x.rows;
-                TileSpans<false, 2> spans;
+                float rest = 0.f;
                 for (int j = 0; j < steps; ++j, ++jj) {
-                    if constexpr (kBias) {                   // positions are a tile ahead of the products, the first tile's are not
-                        if (j == 0) ok = warp_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
-                        if (!ok) break;
-                        if (j == first) bucket.unknown();
-                        spans.find(a.bias, bias_s, jj % kWordRing, q * 2, pos_q, alive, bucket);
-                        __syncwarp();
-                    }
-                    if (!kBias || j > 0) ok = warp_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
+                    ok = warp_wait(&s_full[jj & 1u], (jj >> 1) & 1u, &abort_flag);
                     if (!ok) break;
                     tc_fence_after();
                     float p[64];
                     {
-                        if constexpr (kBias)
-#pragma unroll 1
-                            for (int c = 0; c < 2; ++c)
-                                if (spans.one_by_one(c, 1))
-                                    spans.look_columns(tmem + lanes + (jj & 1u) * kTile + q * 64 + c * 32, c, c1, a.bias, bias_s, jj % kWordRing, q * 2, pos_q,
-                                                       table, 1, 0);
                         uint32_t v[2][32];
                         tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64, v[0]);
                         tmem_load32_async(tmem + lanes + (jj & 1u) * kTile + q * 64 + 32, v[1]);
                         tmem_load_wait();
-                        float factor = c1, add = -base;
-                        if constexpr (kBias) {
-                            if (spans.one) {
-                                add += table[spans.at[0]];
-                            } else {
-                                factor = 1.f;
-#pragma unroll
-                                for (int c = 0; c < 2; ++c)
-                                    if (!(spans.many >> c & 1u)) spans.add_to(v[c], c, c1, bias_s, jj % kWordRing, q * 2, table);
-                            }
-                        }
 #pragma unroll
                         for (int e = 0; e < 64; e += 2) {
-                            const float2 y = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(factor, factor), make_float2(add, add)));
+                            const float2 y = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(c1, c1), make_float2(-base, -base)));
                             p[e] = y.x;
                             p[e + 1] = y.y;
                         }
@@ -1564,11 +1294,6 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                                 if (!((word >> e) & 1u)) p[c * 32 + e] = 0.f;
                         }
                     }
-                    if constexpr (kBias)
-                        if (table_part) {
-                            bin_columns(bins, window, f.window, a.bias, bias_s, jj % kWordRing, q, tmem + lanes + 256 + q * 64, p, pos_q, spans, live && base != INFINITY, a.group, g0, run, cur, lane);
-                            __syncwarp();
-                        }
                     store_operand_and_rest(tmem + lanes + 256 + q * 64, tmem + lanes + (jj & 1u) * kTile + q * 64, p);
                     tmem_store_wait();
                     tc_fence_before();
@@ -1576,8 +1301,6 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                     if (lane == 0) mbar_arrive(&ds_full);
                 }
                 if (!ok) break;
-                if constexpr (kBias)
-                    if (table_part && cur >= 0) add_to_bin(bins, cur, a.group, g0, run, lane);
                 if (live && q == 0) dots[row * heads + head] = dot;
                 if (x.n > 0) {
                     ok = warp_wait(&o_full, item++ & 1u, &abort_flag);
@@ -1589,28 +1312,6 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
                 __syncwarp();
                 if (lane == 0 && x.n > 0) mbar_arrive(&o_empty);
             }
-            if constexpr (kBias)
-                if (table_part && ok) {                      // the unit's bins: all warps have added theirs, and then all have read them
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&bins_full);
-                    ok = warp_wait(&bins_full, binned++ & 1u, &abort_flag);
-                    if (!ok) break;
-                    const int size = a.bias.buckets * a.group;
-                    const uint32_t seq = u / (uint32_t)f.tiles / (uint32_t)a.kv_heads;
-                    float *part = table_part + ((int64_t)seq * f.tiles + x.t0) * a.bias.buckets * heads + x.h * a.group;
-                    for (int i = threadIdx.x; i < size; i += 256) {
-                        float s = 0.f;
-#pragma unroll
-                        for (int k = 0; k < 8; ++k) s += bins_s[8 * f.window * 33 + k * size + i];
-                        part[i / a.group * heads + i % a.group] = s;
-                    }
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(&bins_full);
-                    ok = warp_wait(&bins_full, binned++ & 1u, &abort_flag);
-                    if (!ok) break;
-                    for (int i = lane; i < size; i += 32) bins[i] = 0.f;
-                    __syncwarp();
-                }
         }
     }
     __syncwarp();
@@ -1621,13 +1322,13 @@ attn_tc_dq_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_consta
 }
 
 // dK and dV of a tile of keys: S^T = K Q^T and dP^T = V dO^T over the rows of the sequence
-template <int NB, bool kBias>
-__global__ void __launch_bounds__(Bwd<NB, kBias>::kThreads, 1)
+template <int NB>
+__global__ void __launch_bounds__(Bwd<NB>::kThreads, 1)
 attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v, const __grid_constant__ AttnArgs a, const __grid_constant__ TcShape f,
                    const float *__restrict__ dots)
 {
-    constexpr int kStages = Bwd<NB, kBias>::kQgStages, kTileBytes = Bwd<NB, kBias>::kTileBytes;
+    constexpr int kStages = Bwd<NB>::kQgStages, kTileBytes = Bwd<NB>::kTileBytes;
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint64_t qg_full[kStages], qg_clean[kStages], qg_empty[kStages], kv_full, kv_empty, s_full, p_full, dp_full, ds_full, o_full, o_empty;
     __shared__ __align__(16) float stat_lse[kWordRing][kTile], stat_dot[kWordRing][kTile];
@@ -1639,9 +1340,6 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
     uint8_t *tiles_smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     const uint32_t k_smem = smem_u32(tiles_smem), v_smem = k_smem + kTileBytes, qg_smem = k_smem + 2 * kTileBytes;
     const int ksteps = (a.head_dim + 15) / 16;
-    __shared__ __align__(16) BiasShared_<kBias> bias_s;
-    float *table_s = reinterpret_cast<float *>(tiles_smem + (2 + kStages) * kTileBytes);
-    if constexpr (kBias) stage_bias(a, bias_s, table_s);
     if (threadIdx.x == 0) {
         for (int s = 0; s < kStages; ++s) {
             mbar_init(&qg_full[s], f.boxes ? 1 : kCopyArrivals);
@@ -1681,7 +1379,6 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                 const int64_t keys = x.ke - x.kb;
                 const int n = (int)((x.rows + kTile - 1) / kTile);
                 float lse[4], dot[4];
-                int pos[4];
                 auto ahead = [&](int j) {
 #pragma unroll
                     for (int b = 0; b < 4; ++b) {
@@ -1691,7 +1388,6 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                         row_of(a, x, r, row, head);
                         lse[b] = r < x.rows ? load_now(a.lse + row * heads + head) : -INFINITY;
                         dot[b] = r < x.rows ? load_now(dots + row * heads + head) : 0.f;
-                        if constexpr (kBias) pos[b] = r < x.rows ? (a.bias.pos_q ? load_now(a.bias.pos_q + row) : (int)(row - x.rg.q0)) : 0;
                     }
                 };
                 for (int64_t t = x.t0; t * kTile < keys && n > 0 && ok; t += f.tiles, ++item) {
@@ -1706,11 +1402,9 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                     for (int j = 0; j < n && ok; ++j, ++jj) {
                         float l[4], d[4];
                         uint32_t word[4];
-                        int here[4];
 #pragma unroll
                         for (int b = 0; b < 4; ++b) {
                             const bool on = lse[b] != -INFINITY;
-                            if constexpr (kBias) here[b] = pos[b];
                             l[b] = on ? lse[b] * kLog2e : INFINITY;
                             d[b] = on ? dot[b] : 0.f;
                             word[b] = __ballot_sync(0xFFFFFFFFu, on);
@@ -1727,7 +1421,6 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
                                     stat_dot[jj % kWordRing][b * 32 + lane] = -d[b];
                                 }
                                 if (lane == 0) *reinterpret_cast<uint4 *>(words[jj % kWordRing]) = make_uint4(word[0], word[1], word[2], word[3]);
-                                if constexpr (kBias) place(bias_s, jj % kWordRing, here, word, lane);
                                 __syncwarp();
                             }
                             if (f.boxes) {
@@ -1840,7 +1533,6 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
         }
     } else {
         more_registers<200>();
-        if constexpr (kBias) stage_near<8>(a.bias, bias_s);
         // ---- p and dS: 64 columns (rows of Q) of one key per thread
         const int q = warp >> 2, w = warp & 3;
         const uint32_t lanes = (uint32_t)(w * 32) << 16;
@@ -1854,62 +1546,29 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
             for (int64_t t = x.t0; t * kTile < keys && ok; t += f.tiles) {
                 const int64_t key = x.kb + t * kTile + w * 32 + lane;
                 const bool live = key < x.ke, seen = live && (!a.mask || a.mask[key]);
-                int pos_k = 0;
-                Place<true> bucket;
-                bucket.unknown();
-                if constexpr (kBias) pos_k = pos_of(a.bias.pos_k, min(key, x.ke - 1), x.rg.k0);
-                const bool alive = key - lane < x.ke;
-                TileSpans<true, 2> spans;
                 for (int j = 0; j < n; ++j, ++jj) {
                     ok = warp_wait(&s_full, jj & 1u, &abort_flag);
                     if (!ok) break;
                     tc_fence_after();
-                    if constexpr (kBias) {
-                        spans.find(a.bias, bias_s, jj % kWordRing, q * 2, pos_k, alive, bucket);
-                        __syncwarp();
-                    }
                     const float4 *lse4 = reinterpret_cast<const float4 *>(stat_lse[jj % kWordRing] + q * 64);
                     const float4 *dot4 = reinterpret_cast<const float4 *>(stat_dot[jj % kWordRing] + q * 64);
                     float p[64];
                     {
-                        const float *table = table_s + x.h * a.group * a.bias.buckets;
-                        if constexpr (kBias)
-#pragma unroll 1
-                            for (int c = 0; c < 2; ++c)
-                                if (spans.one_by_one(c, a.group))
-                                    spans.look_columns(tmem + lanes + q * 64 + c * 32, c, c1, a.bias, bias_s, jj % kWordRing, q * 2, pos_k, table, a.group,
-                                                       a.group == 1 ? 0 : (int)(((int64_t)j * kTile + q * 64 + c * 32) % a.group));
                         uint32_t v[2][32];
                         tmem_load32_async(tmem + lanes + q * 64, v[0]);
                         tmem_load32_async(tmem + lanes + q * 64 + 32, v[1]);
                         tmem_load_wait();
-                        float2 factor = make_float2(c1, c1), add = make_float2(0.f, 0.f);
-                        if constexpr (kBias) {
-                            if (a.group == 1 && spans.one) {
-                                add = make_float2(table[spans.at[0]], table[spans.at[0]]);
-                            } else {
-                                factor = make_float2(1.f, 1.f);
-#pragma unroll
-                                for (int c = 0; c < 2; ++c)
-                                    if (!spans.one_by_one(c, a.group)) spans.add_to(v[c], c, c1, bias_s, jj % kWordRing, q * 2, table);
-                            }
-                        }
 #pragma unroll
                         for (int e = 0; e < 64; e += 4) {
-                            float4 l = lse4[e / 4];                  // negated, as the sums of products below
-                            if constexpr (kBias) {
-                                const float2 l0 = __fadd2_rn(make_float2(l.x, l.y), add), l1 = __fadd2_rn(make_float2(l.z, l.w), add);
-                                l = make_float4(l0.x, l0.y, l1.x, l1.y);
-                            }
-                            const float2 y0 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), factor, make_float2(l.x, l.y)));
-                            const float2 y1 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][(e & 31) + 2], v[e >> 5][(e & 31) + 3]), factor, make_float2(l.z, l.w)));
+                            const float4 l = lse4[e / 4];            // negated, as the sums of products below
+                            const float2 y0 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][e & 31], v[e >> 5][(e & 31) + 1]), make_float2(c1, c1), make_float2(l.x, l.y)));
+                            const float2 y1 = exp2_pair(__ffma2_rn(pair_of(v[e >> 5][(e & 31) + 2], v[e >> 5][(e & 31) + 3]), make_float2(c1, c1), make_float2(l.z, l.w)));
                             p[e] = y0.x;
                             p[e + 1] = y0.y;
                             p[e + 2] = y1.x;
                             p[e + 3] = y1.y;
                         }
                     }
-                    if constexpr (kBias) __syncwarp();       // the stores to tensor memory are for a converged warp
                     store_operand(tmem + lanes + q * 64, p);
                     tmem_store_wait();
                     tc_fence_before();
@@ -1964,10 +1623,6 @@ attn_tc_dkv_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_const
 
 // ------------------------------------------------------------------------------------------------- host side
 constexpr int kMaxDevices = 64;
-// A block's shared memory, and how much of it may be dynamic beside what the kernels of the gradients with a bias declare (dQ 10.6 KB; dK and dV,
-// with lse and D of eight tiles of rows, 17.7 KB)
-constexpr size_t kBlockSmem = 227 * 1024, kMostSmem = kBlockSmem - 11 * 1024, kMostDkvSmem = kBlockSmem - 18 * 1024;
-constexpr int kLeastWindow = 4;                            // buckets of a window: one at least, or bin_many takes no step
 template <typename Kernel> bool allow_smem(Kernel kernel, size_t bytes, std::atomic<bool> (&done)[kMaxDevices])
 {
     int dev = 0;
@@ -2022,32 +1677,17 @@ template <int NB, int NT, bool kBias> bool launch_fwd(const AttnArgs &a, const M
     return true;
 }
 
-template <int NB, bool kBias>
-bool launch_bwd(const AttnArgs &a, const Maps &m, int64_t q_tiles, int64_t k_tiles, float *dots, float *table_part, bool exact, cudaStream_t st)
+template <int NB> bool launch_bwd(const AttnArgs &a, const Maps &m, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st)
 {
     static std::atomic<bool> done[2][kMaxDevices] = {};
-    using B = Bwd<NB, kBias>;
-    constexpr size_t row = 8 * 33 * sizeof(float), most_table = kTcTable * sizeof(float), most_bins = 8 * kTcBins * sizeof(float);
-    static_assert(!kBias || B::kDqSmem + most_table + most_bins + kLeastWindow * row <= kMostSmem, "the largest table and bins leave no window");
-    static_assert(!kBias || B::kDkvSmem + most_table <= kMostDkvSmem, "the largest table does not fit beside the tiles");
-    const size_t table = (size_t)a.bias.buckets * a.kv_heads * a.group * sizeof(float);
-    size_t dq_smem = B::kDqSmem + table;
-    int window = 0;
-    if (table_part) {                                    // the rest is the windows'
-        dq_smem += 8 * (size_t)a.bias.buckets * a.group * sizeof(float);
-        if (dq_smem + kLeastWindow * row > kMostSmem) return false;
-        window = (int)std::min<size_t>(kWindow, (kMostSmem - dq_smem) / row);
-        dq_smem += window * row;
-    }
-    if (!allow_smem(attn_tc_dq_kernel<NB, kBias>, kBias ? kMostSmem : B::kDqSmem, done[0]) ||
-        !allow_smem(attn_tc_dkv_kernel<NB, kBias>, B::kDkvSmem + (kBias ? most_table : 0), done[1]))
-        return false;
+    using B = Bwd<NB>;
+    if (!allow_smem(attn_tc_dq_kernel<NB>, B::kDqSmem, done[0]) || !allow_smem(attn_tc_dkv_kernel<NB>, B::kDkvSmem, done[1])) return false;
     const int64_t units = a.n_seq * a.kv_heads;
-    const TcShape fq{(uint32_t)(units * q_tiles), (int)q_tiles, 1, m.boxes, window, exact}, fk{(uint32_t)(units * k_tiles), (int)k_tiles, 1, m.boxes};
+    const TcShape fq{(uint32_t)(units * q_tiles), (int)q_tiles, 1, m.boxes}, fk{(uint32_t)(units * k_tiles), (int)k_tiles, 1, m.boxes};
     note_launch();
-    attn_tc_dq_kernel<NB, kBias><<<tc_grid(fq.units, 1), B::kThreads, dq_smem, st>>>(m.q, m.g, m.k, m.v, a, fq, dots, table_part);
+    attn_tc_dq_kernel<NB><<<tc_grid(fq.units, 1), B::kThreads, B::kDqSmem, st>>>(m.q, m.g, m.k, m.v, a, fq, dots);
     note_launch();
-    attn_tc_dkv_kernel<NB, kBias><<<tc_grid(fk.units, 1), B::kThreads, B::kDkvSmem + table, st>>>(m.q, m.g, m.k, m.v, a, fk, dots);
+    attn_tc_dkv_kernel<NB><<<tc_grid(fk.units, 1), B::kThreads, B::kDkvSmem, st>>>(m.q, m.g, m.k, m.v, a, fk, dots);
     return true;
 }
 
@@ -2068,15 +1708,11 @@ bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, bool one
     return a.bias.table ? forward_of<true>(a, m, f, one_tile, part_o, part_ml, st) : forward_of<false>(a, m, f, one_tile, part_o, part_ml, st);
 }
 
-bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, float *table_part, bool exact, cudaStream_t st)
+bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st)
 {
     Maps m;
     if (!make_maps(a, m)) return false;
-    if (a.bias.table)
-        return a.head_dim <= 64 ? launch_bwd<1, true>(a, m, q_tiles, k_tiles, dots, table_part, exact, st)
-                                : launch_bwd<2, true>(a, m, q_tiles, k_tiles, dots, table_part, exact, st);
-    return a.head_dim <= 64 ? launch_bwd<1, false>(a, m, q_tiles, k_tiles, dots, nullptr, false, st)
-                            : launch_bwd<2, false>(a, m, q_tiles, k_tiles, dots, nullptr, false, st);
+    return a.head_dim <= 64 ? launch_bwd<1>(a, m, q_tiles, k_tiles, dots, st) : launch_bwd<2>(a, m, q_tiles, k_tiles, dots, st);
 }
 
 }  // namespace e2egrec
