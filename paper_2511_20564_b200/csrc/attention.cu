@@ -152,12 +152,13 @@ constexpr int64_t kMaxRows = ((int64_t)1 << 31) - (1 << 16);      // the kernels
 // The kernels of a call.  A sequence's keys and rows stream (attention_few.cu) where a key head has up to two rows (fp32 three: 300 of
 // 3 x 200, 88 us against 113; four in the backward pass), or where a sequence is so small that the set-up of a tile costs more than its
 // products; bf16 heads of up to 128 go to the tensor cores otherwise, fp32 ones to tiles of fp32 FMA, wider heads always stream.
-enum class Path { few, tc, simt };
+enum class Path { few, tc, simt, mma };
 
 struct Plan {
     Path path;
     FewPlan few;
     SimtPlan simt;
+    MmaPlan mma;
     TablePlan table;
     bool one_tile;                        // tensor cores: a key head's rows fit one tile
     int64_t q_tiles, k_tiles;             // blocks of rows / tiles of keys per sequence and key head
@@ -184,8 +185,12 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     const int n_heads = a.kv_heads * a.group;
     const bool small = rows <= (backward ? 4 : dtype == E2EGREC_F32 ? 3 : 2) || rows * k.typical <= (dtype == E2EGREC_F32 ? 256 : backward ? 700 : 800);
     // (without rows on one side there is nothing to form a product of)
-    const bool beside = dtype == E2EGREC_F32 ? a.bias.buckets * a.group <= kSimtTable : !a.bias.buckets || (!backward && a.bias.buckets * n_heads <= kTcTable);
-    p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows || !beside ? Path::few : (dtype == E2EGREC_F32 ? Path::simt : Path::tc);
+    p.path = small || a.head_dim > 128 || !a.q_rows || !a.k_rows ? Path::few : dtype == E2EGREC_F32 ? Path::simt : backward && a.bias.buckets ? Path::mma : Path::tc;
+    // a table of biases that does not fit beside the tiles
+    if (p.path == Path::mma) p.mma = mma_plan(a, q, k);
+    if ((p.path == Path::simt && a.bias.buckets * a.group > kSimtTable) || (p.path == Path::tc && a.bias.buckets * n_heads > kTcTable) ||
+        (p.path == Path::mma && !p.mma.fits))
+        p.path = Path::few;
     if (p.path == Path::tc) {
         p.one_tile = rows <= 128;
         p.q_tiles = blocks_per_unit(q, a.group, backward || p.one_tile ? 128 : 256, units);
@@ -196,11 +201,11 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     } else if (p.path == Path::simt) {
         p.simt = simt_plan(a, q, k);
         p.splits = p.simt.splits;
-    } else {
+    } else if (p.path == Path::few) {
         p.few = few_plan(a, q, k, (int)dtype_size(dtype), backward);
         p.splits = p.few.splits;
     }
-    if (backward && !(p.path == Path::few && p.few.both)) p.dot_bytes = align_up(cells * sizeof(float), 256);
+    if (backward && !(p.path == Path::few && p.few.both)) p.dot_bytes = align_up(cells * sizeof(float), 256) * (p.path == Path::mma ? 2 : 1);
     if (p.splits > 1) {
         const bool fit = backward && p.path == Path::few && p.few.fit;
         p.part_bytes = align_up(p.splits * cells * (fit ? 2 * a.head_dim + 1 : a.head_dim) * sizeof(float), 256);
@@ -209,9 +214,9 @@ Plan make_plan(const AttnArgs &a, const e2egrec_sequences &s, int32_t dtype, boo
     if (backward && a.bias.buckets) {
         p.table = few_table_plan(a, k, dtype);
         const int64_t slices = p.table.seq_slices * p.table.row_slices * p.table.key_slices;
-        p.table_fused = p.path == Path::simt ? simt_forms_table(a, p.simt) : p.few.both;
+        p.table_fused = p.path == Path::mma ? p.mma.table : p.path == Path::simt ? simt_forms_table(a, p.simt) : p.few.both;
         p.table_rows = !p.table_fused ? slices
-                                      : p.path == Path::few ? p.few.blocks : a.n_seq * p.simt.q_tiles * p.simt.splits;
+                                      : p.path == Path::few ? p.few.blocks : a.n_seq * (p.path == Path::mma ? p.mma.q_tiles : p.simt.q_tiles * p.simt.splits);
         p.table_bytes = align_up((size_t)p.table_rows * a.bias.buckets * a.kv_heads * a.group * sizeof(float), 256);
     }
     return p;
@@ -390,6 +395,8 @@ static int32_t attention_backward(const e2egrec_mat *dOut, const e2egrec_mat *Q,
     bool ok = true;
     if (plan.path == Path::tc) {
         ok = tc_attention_backward(a, plan.q_tiles, plan.k_tiles, dots, st);
+    } else if (plan.path == Path::mma) {
+        ok = mma_attention_backward(a, plan.mma, dots, dots + plan.dot_bytes / 2 / sizeof(float), plan.table_fused && dtable ? table_part : nullptr, st);
     } else if (plan.path == Path::simt) {
         ok = simt_attention_backward(a, plan.simt, part_dq, dots, plan.table_fused && dtable ? table_part : nullptr, st);
         if (ok && plan.splits > 1 && a.q_rows) join_dq(a, plan.splits, Q->dtype, false, part_dq, nullptr, st);

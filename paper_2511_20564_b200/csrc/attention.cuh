@@ -150,7 +150,6 @@ inline int64_t blocks_per_unit(const Lengths &l, int64_t factor, int64_t per, in
 // part_o [splits x q_rows x heads x head_dim] and part_ml [splits x q_rows x heads] where splits > 1.
 bool tc_attention_forward(const AttnArgs &a, int64_t tiles, int splits, bool one_tile, float *part_o, float2 *part_ml, cudaStream_t st);
 // q_tiles, k_tiles: tiles of 128 rows and of 128 keys per sequence and key head; dots: [q_rows x heads] scratch
-// (without a bias)
 bool tc_attention_backward(const AttnArgs &a, int64_t q_tiles, int64_t k_tiles, float *dots, cudaStream_t st);
 constexpr int kTcTable = 1280;               // entries of a table of biases, buckets x heads, that fit beside the tiles
 
@@ -195,5 +194,16 @@ bool simt_attention_forward(const AttnArgs &a, const SimtPlan &p, float *part_o,
 // table_part: with a bias [n_seq x q_tiles x splits, buckets x heads], or null where the kernel of dQ does not form the table's gradient
 bool simt_attention_backward(const AttnArgs &a, const SimtPlan &p, float *part_dq, float *dots, float *table_part, cudaStream_t st);
 bool simt_forms_table(const AttnArgs &a, const SimtPlan &p);      // groups that divide 16, bins that fit
+
+
+// attention_mma.cu: gradients with a bias, bf16, head_dim <= 128
+struct MmaPlan {
+    bool fits, table;                     // tiles and the table of biases of a key head fit; the table's gradient is formed beside dQ
+    int q_warps, k_warps;                 // 16 rows / 16 keys each, of a block
+    int64_t q_tiles, k_tiles;             // blocks of rows / of keys per sequence and key head
+};
+MmaPlan mma_plan(const AttnArgs &a, const Lengths &q, const Lengths &k);
+// dots, some: [q_rows x heads] scratch; table_part: [n_seq x q_tiles, buckets x heads], or null where the kernel of dQ does not form the table's gradient
+bool mma_attention_backward(const AttnArgs &a, const MmaPlan &p, float *dots, float *some, float *table_part, cudaStream_t st);
 
 }  // namespace e2egrec
