@@ -146,42 +146,66 @@ __device__ inline int bucket_fast(const BiasArgs &b, const MmaBias &s, int d)
 }
 
 // How a warp finds the buckets of a tile's scores: from the lowest and the highest distance that a thread's two rows (of the product: queries, or
-// keys) meet there.  One bucket for each; up to three edges, compared with; a table of near distances; bisection.
-enum : int { kOne, kFew, kTable, kAny };
-struct Ways {
-    int lo[2], hi[2], edge[2][3], way;
-    // first, last: distances of the columns that count; first > last: there are none
-    __device__ inline void find(const BiasArgs &b, const MmaBias &s, const int (&first)[2], const int (&last)[2])
+// keys) meet there.  One bucket for each; one edge, or up to three, as positions that the columns' are compared with; a table of near distances;
+// bisection.  kKey: the rows are keys, the columns' positions are the queries'.
+enum : int { kOne, kTwo, kFew, kTable, kAny };
+__device__ inline int add_sat(int x, int y)
+{
+    int s;
+    asm("add.sat.s32 %0, %1, %2;" : "=r"(s) : "r"(x), "r"(y));
+    return s;
+}
+template <bool kKey> struct Ways {
+    int lo[2], hi[2], limit[2][3], way;                  // limit: where a bucket begins (kKey: ends)
+    __device__ static inline int distance(int row, int column) { return kKey ? apart(row, column) : apart(column, row); }
+    // low, high: positions of the columns that count; low > high: there are none
+    __device__ inline void find(const BiasArgs &b, const MmaBias &s, int low, int high, const int (&pos)[2])
     {
         int span = 0;
         bool close = true;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             lo[r] = hi[r] = 0;
-            if (first[r] <= last[r]) {
-                lo[r] = bucket_fast(b, s, first[r]);
-                hi[r] = bucket_fast(b, s, last[r]);
-                close = close && first[r] >= -kNear && last[r] < kNear;
+            if (low <= high) {
+                const int first = distance(pos[r], kKey ? high : low), last = distance(pos[r], kKey ? low : high);
+                lo[r] = bucket_fast(b, s, first);
+                hi[r] = max(bucket_fast(b, s, last), lo[r]);           // (edges out of order)
+                close = close && first >= -kNear && last < kNear;
             }
-            hi[r] = max(hi[r], lo[r]);               // (edges out of order)
             span = max(span, hi[r] - lo[r]);
         }
         span = __reduce_max_sync(0xFFFFFFFFu, span);
-        way = span == 0 ? kOne : span <= 3 ? kFew : __all_sync(0xFFFFFFFFu, close) ? kTable : kAny;
-        if (way == kFew)
+        way = span == 0 ? kOne : span == 1 ? kTwo : span <= 3 ? kFew : __all_sync(0xFFFFFFFFu, close) ? kTable : kAny;
+        if (way == kTwo || way == kFew)
 #pragma unroll
             for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int k = 0; k < 3; ++k) edge[r][k] = lo[r] + k < hi[r] ? s.edges[lo[r] + k] : INT32_MAX;
+                for (int k = 0; k < 3; ++k) {            // (an edge that some column has reached lies where it can be compared with)
+                    const int e = s.edges[min(lo[r] + k, kMaxBuckets - 1)];
+                    limit[r][k] = lo[r] + k >= hi[r] ? (kKey ? INT32_MIN : INT32_MAX) : kKey ? apart(pos[r], e) : add_sat(pos[r], e);
+                }
     }
-    template <int WAY> __device__ inline int of(const BiasArgs &b, const MmaBias &s, int r, int d) const
+    __device__ static inline bool beyond(int limit, int p) { return kKey ? p <= limit : p >= limit; }
+    // bucket of a column at p of row r at pos
+    template <int WAY> __device__ inline int of(const BiasArgs &b, const MmaBias &s, int r, int pos, int p) const
     {
-        if constexpr (WAY == kFew) return min(lo[r] + (d >= edge[r][0]) + (d >= edge[r][1]) + (d >= edge[r][2]), hi[r]);
-        if constexpr (WAY == kTable) return s.near[min((uint32_t)d + kNear, 2u * kNear - 1)];      // (columns that do not count may be far)
-        if constexpr (WAY == kAny) return bucket_of(b, s.edges, d);
+        if constexpr (WAY == kTwo) return beyond(limit[r][0], p) ? hi[r] : lo[r];
+        if constexpr (WAY == kFew) return min(lo[r] + beyond(limit[r][0], p) + beyond(limit[r][1], p) + beyond(limit[r][2], p), hi[r]);
+        if constexpr (WAY == kTable) return s.near[min((kKey ? (uint32_t)pos - (uint32_t)p : (uint32_t)p - (uint32_t)pos) + kNear, 2u * kNear - 1)];
+        if constexpr (WAY == kAny) return bucket_of(b, s.edges, distance(pos, p));
         return lo[r];
     }
 };
+template <int W> using Way = std::integral_constant<int, W>;
+template <typename F> __device__ inline void by_way(int way, F f)
+{
+    if (way == kOne) f(Way<kOne>());
+    else if (way == kTwo) f(Way<kTwo>());
+    else if (way == kFew) f(Way<kFew>());
+    else if (way == kTable) f(Way<kTable>());
+    else f(Way<kAny>());
+}
+__device__ inline float2 pair(float x, float y) { return make_float2(x, y); }
 
 struct MmaUnit {
     SeqRange rg;
@@ -307,7 +331,7 @@ attn_mma_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ M
         // the thread's two rows
         float lse[2], ref[2], d[2], total[2], lack[2], run[2];
         int pos[2], own[2], cur[2], count[2];                // count: keys whose p is not 0
-        bool alone[2];
+        bool alone[2], special = true;
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             const int64_t rr = r0 + warp * 16 + quad + 8 * r;
@@ -358,69 +382,73 @@ attn_mma_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ M
             const uint32_t k_at = base + f.stages + (step & 1) * 2 * kTileBytes, v_at = k_at + kTileBytes;
             const uint64_t word = (uint64_t)seen_s[slot][1] << 32 | seen_s[slot][0];
             const bool last_pass = step + n >= steps;
-            Ways ways;
+            Ways<false> ways;
             {
                 const int2 p0 = range_s[slot][0], p1 = range_s[slot][1];
-                const int low = min(p0.x, p1.x), high = max(p0.y, p1.y);
-                int first[2], last[2];
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    first[r] = low <= high ? apart(low, pos[r]) : 0;
-                    last[r] = low <= high ? apart(high, pos[r]) : -1;
-                }
-                ways.find(a.bias, bias, first, last);
+                ways.find(a.bias, bias, min(p0.x, p1.x), max(p0.y, p1.y), pos);
             }
             float p[8][4], ds[8][4];
-            uint32_t bucket[8];                          // of a column pair's four scores, a byte each
+            const int *columns = &pos_s[slot][t4 * 2];
             products<KS, 8>(p, base + warp * 16 * kPitch + at.left, k_at + at.right);
-            auto weigh = [&](auto way) {
+            by_way(ways.way, [&](auto way) {
                 constexpr int WAY = decltype(way)::value;
-                float one[2] = {};
-                if constexpr (WAY == kOne)
+                // biases of the buckets lo .. lo + 3 (or hi), less lse
+                constexpr int kValues = WAY == kOne ? 1 : WAY == kTwo ? 2 : WAY == kFew ? 4 : 0;
+                float value[2][kValues + 1];
 #pragma unroll
-                    for (int r = 0; r < 2; ++r) one[r] = table[own[r] + ways.lo[r]] - lse[r];
+                for (int r = 0; r < 2; ++r)
+#pragma unroll
+                    for (int k = 0; k < kValues; ++k) value[r][k] = table[own[r] + min(ways.lo[r] + k, ways.hi[r])] - lse[r];
 #pragma unroll
                 for (int c = 0; c < 8; ++c) {
                     int2 at2 = make_int2(0, 0);
-                    if constexpr (WAY != kOne) at2 = *reinterpret_cast<const int2 *>(&pos_s[slot][c * 8 + t4 * 2]);
-                    bucket[c] = 0;
+                    if constexpr (WAY != kOne) at2 = *reinterpret_cast<const int2 *>(columns + c * 8);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = i >> 1;
-                        float add = one[r];
-                        if constexpr (WAY != kOne) {
-                            const int b = ways.of<WAY>(a.bias, bias, r, apart(i & 1 ? at2.y : at2.x, pos[r]));
-                            add = table[own[r] + b] - lse[r];
-                            bucket[c] |= (uint32_t)b << (8 * i);
+                    for (int r = 0; r < 2; ++r) {
+                        float add[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const int at1 = e ? at2.y : at2.x;
+                            if constexpr (WAY == kOne) add[e] = value[r][0];
+                            else if constexpr (WAY == kTwo) add[e] = at1 >= ways.limit[r][0] ? value[r][1] : value[r][0];
+                            else if constexpr (WAY == kFew)
+                                add[e] = at1 >= ways.limit[r][2] ? value[r][3] : at1 >= ways.limit[r][1] ? value[r][2] : at1 >= ways.limit[r][0] ? value[r][1] : value[r][0];
+                            else add[e] = table[own[r] + ways.template of<WAY>(a.bias, bias, r, pos[r], at1)] - lse[r];
                         }
-                        p[c][i] = exp2_fast(fmaf(p[c][i], c1, add));
+                        const float2 y = __ffma2_rn(pair(p[c][2 * r], p[c][2 * r + 1]), pair(c1, c1), pair(add[0], add[1]));
+                        p[c][2 * r] = exp2_fast(y.x);
+                        p[c][2 * r + 1] = exp2_fast(y.y);
                     }
                 }
-            };
-            if (ways.way == kOne) weigh(std::integral_constant<int, kOne>());
-            else if (ways.way == kFew) weigh(std::integral_constant<int, kFew>());
-            else if (ways.way == kTable) weigh(std::integral_constant<int, kTable>());
-            else weigh(std::integral_constant<int, kAny>());
+            });
+            const uint64_t mine = word >> (t4 * 2);      // the thread's columns: bits 8 c and 8 c + 1
             auto hide = [&](float (&v)[8][4]) {
-                if (word != ~0ull)
 #pragma unroll
-                    for (int c = 0; c < 8; ++c)
+                for (int c = 0; c < 8; ++c) {
+                    const uint32_t w = (uint32_t)(c < 4 ? mine : mine >> 32) >> (c % 4 * 8);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (!(word >> (c * 8 + t4 * 2 + (i & 1)) & 1u)) v[c][i] = 0.f;
+                    for (int i = 0; i < 4; ++i)
+                        if (!(w & (1u << (i & 1)))) v[c][i] = 0.f;
+                }
             };
-            hide(p);
+            if (word != ~0ull) hide(p);
             products<KS, 8>(ds, base + rows_bytes + warp * 16 * kPitch + at.left, v_at + at.right);
             if (!last_pass || n == 1) {                  // D
+                float2 sum[2] = {}, less2[2] = {};
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int r = i >> 1;
-                        total[r] += p[c][i];
-                        lack[r] = fmaf(p[c][i], ds[c][i] - ref[r], lack[r]);
-                        count[r] += p[c][i] != 0.f;
+                    for (int r = 0; r < 2; ++r) {
+                        const float2 w = pair(p[c][2 * r], p[c][2 * r + 1]);
+                        sum[r] = __fadd2_rn(sum[r], w);
+                        less2[r] = __ffma2_rn(w, __fadd2_rn(pair(ds[c][2 * r], ds[c][2 * r + 1]), pair(-ref[r], -ref[r])), less2[r]);
+                        count[r] += (w.x != 0.f) + (w.y != 0.f);
                     }
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    total[r] += sum[r].x + sum[r].y;
+                    lack[r] += less2[r].x + less2[r].y;
+                }
                 if (step + 1 == n) {
 #pragma unroll
                     for (int r = 0; r < 2; ++r) {
@@ -433,39 +461,74 @@ attn_mma_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ M
                         d[r] = total[r] == 0.f ? 0.f : ref[r] + lack[r] / total[r];
                         alone[r] = count[r] <= 1;
                     }
+                    // rows without dS, or with a D that is no number: looked at score by score
+                    special = __any_sync(0xFFFFFFFFu, alone[0] || alone[1] || !(fabsf(d[0]) < INFINITY) || !(fabsf(d[1]) < INFINITY));
                 }
             }
             if (last_pass) {
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) ds[c][i] = alone[i >> 1] ? 0.f : p[c][i] * (ds[c][i] - d[i >> 1]);
-                hide(ds);
+                    for (int r = 0; r < 2; ++r) {
+                        const float2 y = __fmul2_rn(pair(p[c][2 * r], p[c][2 * r + 1]), __fadd2_rn(pair(ds[c][2 * r], ds[c][2 * r + 1]), pair(-d[r], -d[r])));
+                        ds[c][2 * r] = y.x;
+                        ds[c][2 * r + 1] = y.y;
+                    }
+                if (special) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (alone[i >> 1]) ds[c][i] = 0.f;
+                    hide(ds);
+                }
                 if (table_part) {
                     auto flush = [&](int r, int b) {
                         bins[((f.slots == 2 ? r : 0) * nb + cur[r]) * 32] += run[r];
                         run[r] = 0.f;
                         cur[r] = b;
                     };
-                    if (ways.way == kOne) {
+                    auto add = [&](int r, int b, float v) {
+                        if (b != cur[r]) flush(r, b);
+                        run[r] += v;
+                    };
+                    by_way(ways.way, [&](auto way) {
+                        constexpr int WAY = decltype(way)::value;
+                        if constexpr (WAY == kOne) {
 #pragma unroll
-                        for (int r = 0; r < 2; ++r) {
-                            float s = 0.f;
+                            for (int r = 0; r < 2; ++r) {
+                                float2 v = make_float2(0.f, 0.f);
 #pragma unroll
-                            for (int c = 0; c < 8; ++c) s += ds[c][2 * r] + ds[c][2 * r + 1];
-                            if (ways.lo[r] != cur[r]) flush(r, ways.lo[r]);
-                            run[r] += s;
-                        }
-                    } else {
-#pragma unroll
-                        for (int c = 0; c < 8; ++c)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const int r = i >> 1, b = bucket[c] >> (8 * i) & 255;
-                                if (b != cur[r]) flush(r, b);
-                                run[r] += ds[c][i];
+                                for (int c = 0; c < 8; ++c) v = __fadd2_rn(v, pair(ds[c][2 * r], ds[c][2 * r + 1]));
+                                add(r, ways.lo[r], v.x + v.y);
                             }
-                    }
+                        } else if constexpr (WAY == kTwo) {
+                            float v[2][2] = {};
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) {
+                                const int2 at2 = *reinterpret_cast<const int2 *>(columns + c * 8);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) {
+                                    const bool second = (i & 1 ? at2.y : at2.x) >= ways.limit[i >> 1][0];
+                                    v[i >> 1][0] += second ? 0.f : ds[c][i];
+                                    v[i >> 1][1] += second ? ds[c][i] : 0.f;
+                                }
+                            }
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                add(r, ways.lo[r], v[r][0]);
+                                add(r, ways.hi[r], v[r][1]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int c = 0; c < 8; ++c) {
+                                const int2 at2 = *reinterpret_cast<const int2 *>(columns + c * 8);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i)
+                                    add(i >> 1, ways.template of<WAY>(a.bias, bias, i >> 1, pos[i >> 1], i & 1 ? at2.y : at2.x), ds[c][i]);
+                            }
+                        }
+                    });
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
@@ -659,21 +722,20 @@ attn_mma_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                 if (live_s[slot][half] == 0) continue;
                 const int c0 = half * 32 + t4 * 2;
                 const uint32_t off = half * 32 * kPitch;
-                Ways ways;
-                {
-                    const int2 p = range_s[slot][half];
-                    int first[2], last[2];
-#pragma unroll
-                    for (int r = 0; r < 2; ++r) {
-                        first[r] = apart(pos[r], p.y);
-                        last[r] = apart(pos[r], p.x);
-                    }
-                    ways.find(a.bias, bias, first, last);
-                }
+                Ways<true> ways;
+                ways.find(a.bias, bias, range_s[slot][half].x, range_s[slot][half].y, pos);
                 float p[4][4], ds[4][4];
                 products<KS, 4>(p, base + warp * 16 * kPitch + at.left, q_at + off + at.right);
-                auto weigh = [&](auto way) {
+                by_way(ways.way, [&](auto way) {
                     constexpr int WAY = decltype(way)::value;
+                    const bool one_head = a.group == 1 && WAY <= kTwo;
+                    float value[2][2];
+                    if (one_head)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            value[r][0] = table[ways.lo[r]];
+                            value[r][1] = table[ways.hi[r]];
+                        }
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
                         const float2 l = *reinterpret_cast<const float2 *>(&lse_s[slot][c0 + c * 8]);
@@ -681,16 +743,21 @@ attn_mma_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                         int2 at2 = make_int2(0, 0);
                         if constexpr (WAY != kOne) at2 = *reinterpret_cast<const int2 *>(&pos_s[slot][c0 + c * 8]);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int r = i >> 1, b = ways.of<WAY>(a.bias, bias, r, apart(pos[r], i & 1 ? at2.y : at2.x));
-                            p[c][i] = exp2_fast(fmaf(p[c][i], c1, table[(i & 1 ? own.y : own.x) + b] + (i & 1 ? l.y : l.x)));
+                        for (int r = 0; r < 2; ++r) {
+                            float2 add;
+                            if (one_head) {
+                                add = WAY == kOne ? pair(value[r][0], value[r][0])
+                                                  : pair(at2.x <= ways.limit[r][0] ? value[r][1] : value[r][0], at2.y <= ways.limit[r][0] ? value[r][1] : value[r][0]);
+                            } else {
+                                add = pair(table[own.x + ways.template of<WAY>(a.bias, bias, r, pos[r], at2.x)],
+                                           table[own.y + ways.template of<WAY>(a.bias, bias, r, pos[r], at2.y)]);
+                            }
+                            const float2 y = __ffma2_rn(pair(p[c][2 * r], p[c][2 * r + 1]), pair(c1, c1), __fadd2_rn(add, l));
+                            p[c][2 * r] = exp2_fast(y.x);
+                            p[c][2 * r + 1] = exp2_fast(y.y);
                         }
                     }
-                };
-                if (ways.way == kOne) weigh(std::integral_constant<int, kOne>());
-                else if (ways.way == kFew) weigh(std::integral_constant<int, kFew>());
-                else if (ways.way == kTable) weigh(std::integral_constant<int, kTable>());
-                else weigh(std::integral_constant<int, kAny>());
+                });
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     uint32_t u[4];
@@ -709,7 +776,12 @@ attn_mma_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
                     const float2 d = *reinterpret_cast<const float2 *>(&dot_s[slot][c0 + c * 8]);
                     const float2 m = *reinterpret_cast<const float2 *>(&some_s[slot][c0 + c * 8]);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) ds[c][i] = p[c][i] * (i & 1 ? m.y : m.x) * (ds[c][i] - (i & 1 ? d.y : d.x));
+                    for (int r = 0; r < 2; ++r) {
+                        const float2 y = __fmul2_rn(__fmul2_rn(pair(p[c][2 * r], p[c][2 * r + 1]), m),
+                                                    __fadd2_rn(pair(ds[c][2 * r], ds[c][2 * r + 1]), pair(-d.x, -d.y)));
+                        ds[c][2 * r] = y.x;
+                        ds[c][2 * r + 1] = y.y;
+                    }
                 }
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
