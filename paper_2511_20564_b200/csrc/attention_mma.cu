@@ -136,7 +136,18 @@ __device__ inline void stage_bias(const AttnArgs &a, MmaBias &s, float *table, i
     for (int i = threadIdx.x; i < kMaxBuckets; i += blockDim.x) s.edges[i] = i < nb - 1 ? __ldg(a.bias.edges + i) : INT32_MAX;
     for (int i = threadIdx.x; i < nb * a.group; i += blockDim.x) table[i] = bias_at(a.bias, heads, i % nb, h * a.group + i / nb);
     __syncthreads();
-    for (int i = threadIdx.x; i < 2 * kNear; i += blockDim.x) s.near[i] = (uint8_t)bucket_of(a.bias, s.edges, i - kNear);
+    // neighbouring distances by a thread: the bucket of the first, then the edges that follow (2000 x 32 x 100, a bisection each: 1833 us, 1625 so)
+    const int per = 2 * kNear / blockDim.x;
+    int d = (int)threadIdx.x * per - kNear, at = bucket_of(a.bias, s.edges, d);
+    for (int i = 0; i < per; i += 4) {
+        uint32_t four = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k, ++d) {
+            while (at < nb - 1 && s.edges[at] <= d) ++at;
+            four |= (uint32_t)at << (8 * k);
+        }
+        reinterpret_cast<uint32_t *>(s.near)[((int)threadIdx.x * per + i) / 4] = four;
+    }
     __syncthreads();
 }
 __device__ inline int bucket_fast(const BiasArgs &b, const MmaBias &s, int d)
@@ -240,9 +251,12 @@ __device__ inline void store_pair(bf16 *row, int col, int head_dim, float x, flo
 
 // ---- dQ, D (dots) and whether a row's p is not one key's alone (some), and the gradient of the table.  A thread has bins of its own in shared memory,
 // [slots x buckets x lanes] per warp; dS of a bucket that the thread stays in is added up in a register.  At the end of a block of rows lanes of one
-// row, then rows of one head are added up, in order.
+// row, then rows of one head are added up, in order.  The training case (8 x up to 2048 x 2048, 8 heads of 128): 1.6 ms, the kernel below 1.1 ms; what
+// bounds both is the latency of their instructions with two warps per scheduler (tensor pipe 20 and 29 %, reads of shared memory 33 and 56 %).
+// Two blocks of 8 warps per SM where heads take up to 64 columns: 1000 x 20 x 60, 8 heads of 32, backward 941 -> 670 us, of 64 2000 x 32 x 100
+// 1625 -> 1518.  Lanes of one head joined by exchange instead of row by row: 670 -> 433, 1518 -> 1129.
 template <int KS>
-__global__ void __launch_bounds__(32 * kMostWarps, 1)
+__global__ void __launch_bounds__(32 * kMostWarps, KS <= 4 ? 2 : 1)
 attn_mma_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ MmaShape f, float *__restrict__ dots, float *__restrict__ some,
                    float *__restrict__ table_part)
 {
@@ -575,6 +589,17 @@ attn_mma_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ M
             const int g0 = (int)(r0 % a.group), first = a.group;
             const float *all = reinterpret_cast<const float *>(smem + f.bins) + lane;
             for (int b = warp; b < nb; b += f.warps) {
+                if (16 % a.group == 0) {                 // rows of a lane have one head in every warp: heads of neighbouring rows by exchange
+                    for (int s = 0; s < f.slots; ++s) {
+                        float v = 0.f;
+                        for (int w = 0; w < f.warps; ++w) v += all[((w * f.slots + s) * nb + b) * 32];
+                        v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+                        v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+                        for (int o = 4 * a.group; o < 32; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+                        if (t4 == 0 && quad < a.group) sums[(s * 8 + quad) * nb + b] += v;
+                    }
+                    continue;
+                }
                 for (int w = 0; w < f.warps; ++w)
                     for (int s = 0; s < f.slots; ++s) {
                         float v = all[((w * f.slots + s) * nb + b) * 32];
@@ -592,7 +617,8 @@ attn_mma_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ M
                 __syncwarp();
             }
             __syncthreads();
-            for (int i = 0; i < f.slots * nb; ++i) bins[i * 32] = 0.f;
+            if ((t + f.tiles) * 16 * f.warps < x.rows)
+                for (int i = 0; i < f.slots * nb; ++i) bins[i * 32] = 0.f;
         }
     }
     if (table_part) {
@@ -604,7 +630,7 @@ attn_mma_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ M
 
 // ---- dK and dV of 16 keys per warp: S^T = K Q^T and dP^T = V dO^T over the rows of the sequence, 32 at a time
 template <int KS>
-__global__ void __launch_bounds__(32 * kMostWarps, 1)
+__global__ void __launch_bounds__(32 * kMostWarps, KS <= 4 ? 2 : 1)
 attn_mma_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ MmaShape f, const float *__restrict__ dots, const float *__restrict__ some)
 {
     constexpr uint32_t kPitch = Lane<KS>::kPitch, kTileBytes = kStep * kPitch;
