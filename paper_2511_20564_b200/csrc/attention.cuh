@@ -19,7 +19,6 @@ struct BiasArgs {
     const float *table;                   // [buckets x heads]
     const int32_t *edges;                 // [buckets - 1], ascending
     const int32_t *pos_q, *pos_k;         // null: a row's number in its sequence
-    float *dtable;                        // backward; may be null
     int32_t buckets, top;                 // top: the largest power of two that is not above buckets - 1 (0: one bucket)
 };
 
