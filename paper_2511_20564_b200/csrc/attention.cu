@@ -151,7 +151,8 @@ constexpr int64_t kMaxRows = ((int64_t)1 << 31) - (1 << 16);      // the kernels
 
 // The kernels of a call.  A sequence's keys and rows stream (attention_few.cu) where a key head has up to two rows (fp32 three: 300 of
 // 3 x 200, 88 us against 113; four in the backward pass), or where a sequence is so small that the set-up of a tile costs more than its
-// products; bf16 heads of up to 128 go to the tensor cores otherwise, fp32 ones to tiles of fp32 FMA, wider heads always stream.
+// products; bf16 heads of up to 128 go to the tensor cores otherwise (gradients with a bias to matrix products of a warp), fp32 ones to tiles of
+// fp32 FMA, wider heads always stream.
 enum class Path { few, tc, simt, mma };
 
 struct Plan {

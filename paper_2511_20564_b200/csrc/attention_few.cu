@@ -272,7 +272,7 @@ __device__ inline Unit few_unit(const AttnArgs &a, const FewShape &f, uint32_t u
 
 // Biases of the scores of a turn: lane i finds the buckets of the turn's key i, which the lanes of that key then ask it for.  It is found from the
 // bucket of the turn before, mostly the same or the next one, and everything before the turn's keys are waited for; positions of the keys are
-// fetched a turn ahead.  Forward pass of 4096 x 1 x 100 keys: 49 us, 39 without a bias.
+// fetched a turn ahead.  Forward pass of 4096 x 1 x 100 keys: 43 us, 39 without a bias.
 template <int R, int U> struct TurnBias {
     int pos[R], col[R];                              // the rows' positions and heads
     Bucket state[R];
@@ -768,8 +768,8 @@ template <typename T, int U, int CPL> __device__ __noinline__ void clear_hidden(
 // With a bias and 16-bit outputs (kTwice) D has to be exact before a dS is used: the table's gradient is what is left of dS that cancels, and D of the
 // stored out made dK visibly worse than its rounding.  p and dS with D of the stored out are kept for every key in shared memory (8 bytes
 // per key, head and row) where that leaves two blocks per SM; what D lacked is known behind the last key, and dK, dV and the table's sums are formed
-// from what was kept: keys and values are read once.  Others go over their keys twice.  4096 x 1 x 100, 4 heads of 32: 130 us (66 without a
-// bias, 106 without the table's gradient; 169 with two walks over the keys): the instructions and the latency of three blocks per SM, 3.2 TB/s.
+// from what was kept: keys and values are read once.  Others go over their keys twice.  4096 x 1 x 100, 4 heads of 32: 120 us (71 without a
+// bias; with two walks over the keys 169): the instructions and the latency of three blocks per SM, 3.5 TB/s.
 template <typename T, int R, int U, int CPL, bool kBoth, bool kFit, bool kBias>
 __global__ void __launch_bounds__(kFewThreads, CPL == 2 || R > 2 ? 2 : (R == 1 ? 4 : 3))
 attn_few_bwd_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ FewShape f, float *__restrict__ part_dq, float *__restrict__ dots,

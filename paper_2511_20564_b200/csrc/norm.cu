@@ -66,9 +66,9 @@ template <int N> __device__ inline void load_gains(const float *p, int chunk, fl
 }
 __device__ inline float2 both(float x) { return make_float2(x, x); }
 
-// U chunks of 16 bytes per thread; arithmetic on two elements at a time.  131 072 x 256 bf16 with residual and dropout: 50 us, 4.0 TB/s, 70 % of
-// the issue slots (half of them the generator's and the conversions'); without dropout 47 us; 32 768 x 1024, the sum stored as well: 55 us, 4.9 TB/s.
-// With a row per warp, an element at a time and the mask as bits the first took 55 us.
+// U chunks of 16 bytes per thread; arithmetic on two elements at a time.  The kernel's own time, 131 072 x 256 bf16 with residual and dropout: 46 us,
+// 4.4 TB/s; without dropout 39.5 us, 5.1 TB/s (the generator and the conversions are the difference); 32 768 x 1024, the sum stored as well: 50 us with
+// dropout, 46 without, 5.4 and 5.8 TB/s.
 template <typename T, int U, bool kDrop>
 __global__ void __launch_bounds__(kNormThreads, U * Chunk<T>::kElems > 24 ? 3 : 4)
 norm_fwd_kernel(const __grid_constant__ NormArgs a)
@@ -140,9 +140,10 @@ norm_fwd_kernel(const __grid_constant__ NormArgs a)
     if (a.stats && at == 0) a.stats[row] = make_float2(mean, rstd);
 }
 
-// The gradient, rows in turn, 16 values per thread as the gains' sums take twice that.  131 072 x 256 bf16 with residual and dropout: 78 us, 4.3 TB/s;
-// 32 768 x 1024 with the gradient of the sum 94 us, 4.3 TB/s (250 registers and a block per SM with 32 values per thread: 168 us).  Two blocks per SM
-// at most go over the rows: four and more have more partial sums to write than they hide latency (77 -> 79 us, 20 011 x 320 fp32 30 -> 34 us).
+// The gradient, rows in turn, 16 values per thread as the gains' sums take twice that.  The kernel's own time, 131 072 x 256 bf16 with residual and
+// dropout: 68 us, 4.9 TB/s (53 without dropout); 32 768 x 1024 with the gradient of the sum 84 us, 4.8 TB/s (twice that with 250 registers and a block
+// per SM, 32 values per thread).  Two blocks per SM at most go over the rows: four and more have more partial sums to write than they hide latency (call
+// by call 77 -> 79 us, 20 011 x 320 fp32 30 -> 34 us).
 constexpr int kBackValues = 16, kForwardValues = 32;
 template <typename T, int U, bool kDrop>
 __global__ void __launch_bounds__(kNormThreads, U * Chunk<T>::kElems > kBackValues ? 1 : 2)
@@ -277,8 +278,8 @@ struct DropoutArgs {
 };
 
 // A thread takes one unit of kRows neighbouring rows, whose loads go out together and whose random words share the unit's part.  What bounds it with
-// 16-bit elements is the generator and the conversions, 58 % of the integer pipe: 262 144 x 256 took 76 us with a unit after the other per thread,
-// 57 with four under way, packed arithmetic and comparisons in place of a mask.
+// 16-bit elements is the generator and the conversions, 58 % of the integer pipe: 262 144 x 256 takes 46 us, 5.8 TB/s (call by call
+// 76 us with a unit after the other per thread, 57 with four under way and comparisons in place of a mask).
 constexpr int kDropRows = 4;
 template <typename T, bool kRes, int kRows>
 __global__ void __launch_bounds__(kNormThreads)
@@ -358,8 +359,8 @@ bool same_place(const e2egrec_mat *a, const e2egrec_mat *b) { return a && b && a
 
 // Threads of a row and chunks per thread (a template argument).  Threads hold as many values as their registers allow, and with that as few as
 // possible share a row: what is done once per row, exchanges and addresses, is done for more rows by a warp then.  Of the numbers of chunks the
-// one that leaves the fewest places empty (100 000 x 152: 43 us with one chunk each of 32 threads, 29 so).  Rows so few that every chunk has a
-// thread of its own get that: the time is one chunk's then (64 x 256: 10 -> 6 us).
+// one that leaves the fewest places empty (100 000 x 152, call by call: 43 us with one chunk each of 32 threads, 29 so).  Rows so few that every chunk has a
+// thread of its own get that: the time is one chunk's then (64 x 256, call by call: 10 -> 6 us, of which the kernel is 4).
 struct NormShape {
     int threads, per;
 };
