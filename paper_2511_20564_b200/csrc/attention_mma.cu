@@ -121,6 +121,23 @@ template <int KS, typename Src> __device__ inline void load_tile(uint32_t dst, i
         cp_async16(dst + r * Lane<KS>::kPitch + u * 16, p ? static_cast<const void *>(p + u * 8) : any, p != nullptr);
     }
 }
+// The same of rows `ld` apart from `first` on; on(r): not zeros.  Where a block holds whole rows of units a thread keeps to one of them.
+template <int KS, typename On> __device__ inline void load_rows(uint32_t dst, int rows, int head_dim, const bf16 *first, int64_t ld, On on)
+{
+    constexpr int kUnits = 2 * KS;
+    if constexpr ((kUnits & (kUnits - 1)) == 0) {
+        const int u = threadIdx.x % kUnits, r0 = threadIdx.x / kUnits, per = blockDim.x / kUnits;
+        const bf16 *p = first + r0 * ld + u * 8;
+        const bool in = u * 8 < head_dim;
+        dst += r0 * Lane<KS>::kPitch + u * 16;
+        for (int r = r0; r < rows; r += per, p += per * ld, dst += per * Lane<KS>::kPitch) {
+            const bool take = in && on(r);
+            cp_async16(dst, take ? p : first, take);
+        }
+    } else {
+        load_tile<KS>(dst, rows, head_dim, first, [&](int r) { return on(r) ? first + r * ld : nullptr; });
+    }
+}
 __device__ inline void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ inline void landed() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
@@ -313,8 +330,8 @@ attn_mma_dq_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ M
         const uint32_t w0 = seen_s[step % kMeta][0], w1 = seen_s[step % kMeta][1];
         const int64_t key0 = x.rg.k0 + (int64_t)tile * kStep;
         auto on = [&](int r) { return (r < 32 ? w0 >> r : w1 >> (r - 32)) & 1u; };
-        load_tile<KS>(dst, kStep, a.head_dim, kp, [&](int r) { return on(r) ? kp + (key0 + r) * a.ldk : nullptr; });
-        load_tile<KS>(dst + kTileBytes, kStep, a.head_dim, kp, [&](int r) { return on(r) ? vp + (key0 + r) * a.ldv : nullptr; });
+        load_rows<KS>(dst, kStep, a.head_dim, kp + key0 * a.ldk, a.ldk, on);
+        load_rows<KS>(dst + kTileBytes, kStep, a.head_dim, vp + key0 * a.ldv, a.ldv, on);
         commit();
     };
     for (int64_t t = x.t0; t * 16 * f.warps < x.rows; t += f.tiles) {
@@ -699,8 +716,15 @@ attn_mma_dkv_kernel(const __grid_constant__ AttnArgs a, const __grid_constant__ 
             if (!((r < 32 ? w0 >> r : w1 >> (r - 32)) & 1u)) return nullptr;
             return static_cast<const bf16 *>(p) + (x.rg.q0 + query_s[slot][r]) * ld + (int64_t)head_s[slot][r] * a.head_dim;
         };
-        load_tile<KS>(dst, kStep, a.head_dim, a.q, [&](int r) { return from(a.q, a.ldq, r); });
-        load_tile<KS>(dst + kTileBytes, kStep, a.head_dim, a.q, [&](int r) { return from(a.dout, a.ldg, r); });
+        if (a.group == 1) {                              // rows follow one another
+            const int64_t row = x.rg.q0 + (int64_t)step * kStep, col = (int64_t)x.h * a.head_dim;
+            auto on = [&](int r) { return (r < 32 ? w0 >> r : w1 >> (r - 32)) & 1u; };
+            load_rows<KS>(dst, kStep, a.head_dim, static_cast<const bf16 *>(a.q) + row * a.ldq + col, a.ldq, on);
+            load_rows<KS>(dst + kTileBytes, kStep, a.head_dim, static_cast<const bf16 *>(a.dout) + row * a.ldg + col, a.ldg, on);
+        } else {
+            load_tile<KS>(dst, kStep, a.head_dim, a.q, [&](int r) { return from(a.q, a.ldq, r); });
+            load_tile<KS>(dst + kTileBytes, kStep, a.head_dim, a.q, [&](int r) { return from(a.dout, a.ldg, r); });
+        }
         commit();
     };
     for (int64_t t = x.t0; t * 16 * f.warps < keys; t += f.tiles) {
