@@ -268,7 +268,7 @@ __device__ inline void store_pair(bf16 *row, int col, int head_dim, float x, flo
 
 // ---- dQ, D (dots) and whether a row's p is not one key's alone (some), and the gradient of the table.  A thread has bins of its own in shared memory,
 // [slots x buckets x lanes] per warp; dS of a bucket that the thread stays in is added up in a register.  At the end of a block of rows lanes of one
-// row, then rows of one head are added up, in order.  The training case (8 x up to 2048 x 2048, 8 heads of 128): 1.61 ms, the kernel below 1.11 ms; what
+// row, then rows of one head are added up, in order.  The training case (8 x up to 2048 x 2048, 8 heads of 128): 1.52 ms, the kernel below 1.04 ms; what
 // bounds both is the latency of their instructions with two warps per scheduler (tensor pipe 20 and 29 %, reads of shared memory 33 and 56 %).
 // Two blocks of 8 warps per SM where heads take up to 64 columns: 1000 x 20 x 60, 8 heads of 32, backward 941 -> 670 us, of 64 2000 x 32 x 100
 // 1625 -> 1518.  Lanes of one head joined by exchange instead of row by row: 670 -> 433, 1518 -> 1129.
