@@ -1,4 +1,4 @@
-"""Attention with a bias on the tensor cores: tables and bins at the most that fit beside the tiles, where the windows of sums are smallest."""
+"""Attention with a bias of many rows: the largest tables that lie beside the tiles, and bins of blocks that become smaller for them."""
 import pytest
 import torch
 
